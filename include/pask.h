@@ -25,7 +25,8 @@
  *     calls that wait for the stream (pask_budget_state, pask_debug_*), the host-buffer steps, and the
  *     first pask_decode_attention_static call on a device.
  *   - Supported shapes: head_dim 128, 16-token pages, n_q_heads = 4 * n_kv_heads with
- *     n_kv_heads in {1, 2, 4, 8}.  Anything else: PASK_ERR_UNSUPPORTED_SHAPE.
+ *     n_kv_heads in {1, 2, 4, 8}.  Anything else: PASK_ERR_UNSUPPORTED_SHAPE -- but for latent caches
+ *     (head_dim PASK_LATENT_DIM), which have calls of their own, see pask_append_latent.
  *   - No function throws or aborts.
  *
  * Formats (the paper leaves them open; these are the library's documented readings)
@@ -84,6 +85,9 @@ typedef int32_t pask_status_t;
 #define PASK_MAX_GROUPS 8
 #define PASK_MAX_SEQS_PER_CALL 1024
 #define PASK_MAX_WINDOW 256
+#define PASK_LATENT_DIM 576       /* a latent cache's row: the shared latent vector, then the rotary key dims */
+#define PASK_LATENT_VALUE_DIM 512 /* the shared latent vector: the row's value for every head (absorbed form) */
+#define PASK_LATENT_MAX_HEADS 128
 
 typedef struct pask_policy pask_policy_t;
 typedef struct pask_cache pask_cache_t;
@@ -94,7 +98,7 @@ typedef struct {
     int32_t n_layers;
     int32_t n_q_heads;
     int32_t n_kv_heads;
-    int32_t head_dim;           /* 128 */
+    int32_t head_dim;           /* 128, or PASK_LATENT_DIM: a latent cache (n_kv_heads 1, no recent window) */
     int32_t page_tokens;        /* 16 */
     int32_t max_seqs;           /* sequence ids are 0 .. max_seqs-1 */
     int32_t max_tokens_per_seq; /* bound on each stream's length (sizes the page tables) */
@@ -410,6 +414,95 @@ pask_status_t pask_decode_step_pipelined_ahead(pask_cache_t *cache, int32_t laye
                                                size_t staging_bytes, void *workspace, size_t workspace_bytes,
                                                void *plan_area, size_t plan_area_bytes, pask_stream_t stream);
 pask_status_t pask_decode_step_drain(pask_cache_t *cache);
+
+/* ---------------------------------------------------------------------------------------------
+ * Latent caches: models whose attention shares one row a token among all heads (latent attention).
+ * (The paper's models keep K and V per head; the table, the streams and the budget are its own, the
+ * row is the library's reading.)
+ *
+ * A row is PASK_LATENT_DIM = 576 bf16 values: the 512-wide latent vector that each head's key and
+ * value are linear maps of, then the 64 rotary key dims that all heads share.  A cache is a latent
+ * one when its descriptor says head_dim = PASK_LATENT_DIM, n_kv_heads = 1, n_q_heads = 1 ..
+ * PASK_LATENT_MAX_HEADS, recent_window = 0.  Policies, pask_cache_*, pask_seq_reset, pask_decide,
+ * pask_budget_state, the timing hooks, pask_workspace_bytes, pask_debug_stream_len / _page_ids /
+ * _pool_state / _ctrl_words / _set_attention_ctas / _set_wait work on it as on any other; every other
+ * call on K and V refuses it with PASK_ERR_UNSUPPORTED_SHAPE, and these calls refuse the other caches.
+ * Costs: m(H) = 1152 bytes per token and layer, m(L) = 576 * low_bits / 8 + 36.
+ *   RETAIN-HIGH keeps the row's bits.  RETAIN-LOW stores, per group of 32 consecutive values, a bf16
+ *   scale s = bf16(amax / L) (L = 7, 127 or 1 for low_bits 4, 8 or 2; zero if below 2^-126) and codes
+ *   rint(x / s), ties to even (zero if s is); the value it stands for is bf16(code * s), which is what
+ *   attention computes with.  (bf16 scales, where the other caches have fp16 ones: the value is an
+ *   operand of a bf16 matrix product, and a bf16 product rounds it once, in any range.)
+ * The calls run on the device the cache was created on (PASK_ERR_INVALID_ARG if another is current).
+ */
+
+/* pask_append_latent -- pask_append_kv for a latent cache, or with `actions` != NULL
+ * pask_append_kv_decided: same table, streams, page numbering, refusals and accounting.
+ *   latent         dev bf16 [total_tokens][576]; values of retained tokens must be finite (rows of
+ *                  released tokens are not read); an infinity or a NaN makes what is stored of its
+ *                  32-value group undefined
+ *   actions        dev uint8 [total_tokens][n_groups] from pask_decide, or NULL: the table's actions
+ *   other arguments as for pask_append_kv (tags may be NULL only if total_tokens is 0). */
+pask_status_t pask_append_latent(pask_cache_t *cache, int32_t layer, int32_t n_seqs, int32_t total_tokens,
+                                 const int32_t *seq_ids, const int32_t *cu_tokens, const void *latent,
+                                 const uint8_t *tags, const uint8_t *actions, uint8_t *actions_out,
+                                 pask_stream_t stream);
+
+/* pask_read_latent -- the retained rows of sequences at `layer` as bf16, at stored precision: a
+ * sequence's HIGH stream in arrival order, then its LOW stream (order does not matter to attention:
+ * rotary dims are stored rotated).  For expanding a history to keys and values before a prompt chunk
+ * (pask_prompt_attention_latent), or for moving it elsewhere.
+ *   cu_rows    dev int32 [n_seqs+1], ascending, within 0 .. total_rows: where each sequence's rows go.
+ *              A range may be longer than its sequence's rows: the rest is left as it was.  A sequence
+ *              whose range is malformed or too short, or whose id is out of range, is not written at
+ *              all (sticky PASK_DEV_BAD_RAGGED / PASK_DEV_BAD_SEQ); the others are
+ *   rows_out   dev bf16 [total_rows][576]
+ *   lens_out   dev int32 [n_seqs][2] or NULL: rows in the HIGH and the LOW stream (0, 0 for a bad id)
+ * A sequence may be named more than once. */
+pask_status_t pask_read_latent(pask_cache_t *cache, int32_t layer, int32_t n_seqs, int32_t total_rows,
+                               const int32_t *seq_ids, const int32_t *cu_rows, void *rows_out,
+                               int32_t *lens_out, pask_stream_t stream);
+
+/* pask_decode_attention_latent -- pask_decode_attention for a latent cache: attention of one new query
+ * per sequence over its retained rows at stored precision, absorbed form (the key map is folded into
+ * the query, the value map is applied to the output by the caller): for head h
+ *   p_j = softmax_j(scale * q_h . row_j),   out_h = sum_j p_j row_j[0:512].
+ *   q         dev bf16 [n_seqs][n_q][576]
+ *   scale     positive and finite (1 / sqrt of the unabsorbed head dim, commonly)
+ *   out       dev bf16 [n_seqs][n_q][512]
+ *   lse       dev fp32 [n_seqs][n_q] or NULL: natural-log sum of exp of the scaled scores
+ *   workspace dev, at least pask_workspace_bytes(cache, n_seqs) bytes, 256-byte aligned; contents undefined
+ *             afterwards.  Calls that may overlap on the GPU (two streams, two captured graphs replayed
+ *             side by side) need one each.
+ * Softmax weights are rounded to bf16 for the product with the rows, sums are fp32.  A sequence with
+ * nothing retained, or an id out of range (sticky PASK_DEV_BAD_SEQ), gets out = 0 and lse = -inf.
+ * A sequence may be named more than once. */
+pask_status_t pask_decode_attention_latent(pask_cache_t *cache, int32_t layer, int32_t n_seqs,
+                                           const int32_t *seq_ids, const void *q, float scale, void *out,
+                                           float *lse, void *workspace, size_t workspace_bytes,
+                                           pask_stream_t stream);
+
+/* pask_prompt_attention_latent -- causal attention of a ragged batch of prompts, expanded form: each
+ * head has its own key (128 dims expanded from the latent, then the 64 shared rotary dims) and value
+ * (128 dims).  Query t of a sequence with nq queries and nk keys sees its keys 0 .. t + nk - nq: with
+ * nk = nq a prompt on its own, with nk > nq a chunk behind nk - nq keys of history that every query
+ * sees (rows from pask_read_latent, in any order).  nk < nq: the first nq - nk queries see nothing
+ * and get out = 0, lse = -inf.  Needs no cache: the prompt is attended as given, before the table
+ * decides what persists.
+ *   n_heads     1 .. PASK_LATENT_MAX_HEADS
+ *   cu_q, cu_k  dev int32 [n_seqs+1], ascending within 0 .. total_q (total_k).  A sequence whose ranges are
+ *               malformed is not written; so are rows of q outside every sequence
+ *   q           dev bf16 [total_q][n_heads][192]: 128 dims to meet the expanded key, 64 rotary dims
+ *   kv          dev bf16 [total_k][n_heads][256]: expanded key, value (the up-projection's output as it is)
+ *   k_rope      dev bf16, row j at k_rope + j * rope_stride elements, 64 values (rope_stride >= 64, a multiple of 8:
+ *               the last dims of latent rows can be used where they lie).  Must cover total_k rows
+ *   scale       positive and finite
+ *   out         dev bf16 [total_q][n_heads][128];  lse  dev fp32 [total_q][n_heads] or NULL
+ * Values of a sequence's rows must be finite; rows outside every sequence may hold anything. */
+pask_status_t pask_prompt_attention_latent(int32_t n_seqs, int32_t total_q, int32_t total_k, int32_t n_heads,
+                                           const int32_t *cu_q, const int32_t *cu_k, const void *q, const void *kv,
+                                           const void *k_rope, int32_t rope_stride, float scale, void *out,
+                                           float *lse, pask_stream_t stream);
 
 /* ---------------------------------------------------------------------------------------------
  * pask_distortion -- the inner term of the attention-output distortion (Eq. 4): for each row r

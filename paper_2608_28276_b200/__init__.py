@@ -24,12 +24,14 @@ ACTION_RELEASE, ACTION_RETAIN_LOW, ACTION_RETAIN_HIGH = 0, 1, 2
 TAG_PROTECTED = 0xFF
 MAX_GROUPS = 8
 MAX_WINDOW = 256
+LATENT_DIM, LATENT_VALUE_DIM, LATENT_MAX_HEADS = 576, 512, 128
 
 EXPORTS = [
     "pask_load_policy", "pask_free_policy", "pask_policy_action", "pask_cache_sizes", "pask_cache_create",
     "pask_cache_destroy", "pask_cache_reset", "pask_seq_reset", "pask_append_kv", "pask_decide",
     "pask_append_kv_decided", "pask_append_attend", "pask_plan_area_bytes", "pask_plan_ahead", "pask_decode_step_ahead", "pask_decode_attention",
     "pask_decode_attention_full", "pask_decode_attention_static", "pask_workspace_bytes", "pask_decode_step_host", "pask_step_staging_bytes", "pask_step_packed_layout", "pask_decode_step_packed", "pask_decode_step_pipelined", "pask_decode_step_pipelined_ahead", "pask_decode_step_drain",
+    "pask_append_latent", "pask_read_latent", "pask_decode_attention_latent", "pask_prompt_attention_latent",
     "pask_budget_state", "pask_distortion", "pask_cache_set_timing_events", "pask_cache_set_timing_span", "pask_debug_stream_len", "pask_debug_dump_high",
     "pask_debug_dump_low", "pask_debug_pool_state", "pask_debug_ctrl_words", "pask_debug_page_order", "pask_debug_page_ids", "pask_debug_partition", "pask_debug_set_attention_ctas", "pask_debug_set_wait", "pask_debug_plan_order_span", "pask_status_string",
 ]
@@ -96,6 +98,10 @@ _lib.pask_decode_step_drain.argtypes = [_vp]
 _lib.pask_step_staging_bytes.argtypes = [_vp, _i32]
 _lib.pask_step_staging_bytes.restype = _sz
 _lib.pask_distortion.argtypes = [_i32, _i32, _vp, _vp, _vp, _vp, _vp]
+_lib.pask_append_latent.argtypes = [_vp, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp]
+_lib.pask_read_latent.argtypes = [_vp, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp]
+_lib.pask_decode_attention_latent.argtypes = [_vp, _i32, _i32, _vp, _vp, C.c_float, _vp, _vp, _vp, _sz, _vp]
+_lib.pask_prompt_attention_latent.argtypes = [_i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _i32, C.c_float, _vp, _vp, _vp]
 _lib.pask_budget_state.argtypes = [_vp, _i32, C.POINTER(BudgetState), _vp]
 _lib.pask_cache_set_timing_events.argtypes = [_vp, _vp, _vp]
 _lib.pask_debug_stream_len.argtypes = [_vp, _i32, _i32, C.POINTER(C.c_uint32), C.POINTER(C.c_uint32), _vp]
@@ -158,6 +164,9 @@ def pask_policy_action(policy: int, tag: int, group: int) -> int:
     return int(_lib.pask_policy_action(policy, tag, group))
 
 
+_latent_shape = {}     # handle of a latent cache -> (query heads, layer groups): what shapes are checked against
+
+
 def pask_cache_sizes(desc: CacheDesc) -> CacheSizes:
     out = CacheSizes()
     _check(_lib.pask_cache_sizes(C.byref(desc), C.byref(out)), "pask_cache_sizes")
@@ -168,10 +177,14 @@ def pask_cache_create(desc: CacheDesc, policy: int, pool_high, pool_low, meta, s
     h = _vp()
     _check(_lib.pask_cache_create(C.byref(desc), policy, _dptr(pool_high), _dptr(pool_low), _dptr(meta),
                                   _stream(stream), C.byref(h)), "pask_cache_create")
+    if desc.head_dim == LATENT_DIM:
+        groups = next(g for g in range(MAX_GROUPS + 1) if pask_policy_action(policy, 0, g) < 0)
+        _latent_shape[h.value] = (desc.n_q_heads, groups)
     return h.value
 
 
 def pask_cache_destroy(cache: int):
+    _latent_shape.pop(cache, None)
     _lib.pask_cache_destroy(cache)
 
 
@@ -341,6 +354,75 @@ def pask_decode_step_drain(cache: int):
     _check(_lib.pask_decode_step_drain(cache), "pask_decode_step_drain")
 
 
+def _latent_args(where, device, *args):
+    """Checks of the latent calls: (name, tensor or None, dtype, shape with None for any size) each, all on one device."""
+    for name, t, dtype, shape in args:
+        if t is None:
+            continue
+        ok = (t.is_cuda and t.device == device and t.dtype == dtype and t.is_contiguous() and t.dim() == len(shape) and
+              all(want is None or want == have for want, have in zip(shape, t.shape)))
+        if not ok:
+            raise PaskError(ERR_INVALID_ARG, f"{where}: {name} must be a contiguous {dtype} tensor "
+                            f"[{', '.join('*' if n is None else str(n) for n in shape)}] on {device}, got {tuple(t.shape)} {t.dtype}")
+
+
+def _on(device, stream):
+    """The CUDA stream of a latent call: the given one, or the device's current one."""
+    return (torch.cuda.current_stream(device) if stream is None else stream).cuda_stream
+
+
+def pask_append_latent(cache: int, layer: int, seq_ids, cu_tokens, latent, tags, actions=None, actions_out=None, stream=None):
+    """pask_append_kv for a latent cache: latent bf16 [total][576]; `actions` u8 [total][n_groups] from pask_decide or None."""
+    n, total, dev = seq_ids.numel(), latent.shape[0], seq_ids.device
+    _latent_args("pask_append_latent", dev, ("seq_ids", seq_ids, torch.int32, (n,)), ("cu_tokens", cu_tokens, torch.int32, (n + 1,)),
+                 ("latent", latent, torch.bfloat16, (None, LATENT_DIM)), ("tags", tags, torch.uint8, (total,)),
+                 ("actions", actions, torch.uint8, (total, _latent_shape.get(cache, (None, None))[1])), ("actions_out", actions_out, torch.uint8, (total,)))
+    with torch.cuda.device(dev):
+        _check(_lib.pask_append_latent(cache, layer, n, total, _dptr(seq_ids), _dptr(cu_tokens), _dptr(latent), _dptr(tags),
+                                       _dptr(actions), _dptr(actions_out), _on(dev, stream)), "pask_append_latent")
+
+
+def pask_read_latent(cache: int, layer: int, seq_ids, cu_rows, rows_out, lens_out=None, stream=None):
+    """The retained rows of each sequence as bf16, HIGH stream then LOW stream, into rows_out[cu_rows[i]:]."""
+    n, dev = seq_ids.numel(), seq_ids.device
+    _latent_args("pask_read_latent", dev, ("seq_ids", seq_ids, torch.int32, (n,)), ("cu_rows", cu_rows, torch.int32, (n + 1,)),
+                 ("rows_out", rows_out, torch.bfloat16, (None, LATENT_DIM)), ("lens_out", lens_out, torch.int32, (n, 2)))
+    with torch.cuda.device(dev):
+        _check(_lib.pask_read_latent(cache, layer, n, rows_out.shape[0], _dptr(seq_ids), _dptr(cu_rows), _dptr(rows_out),
+                                     _dptr(lens_out), _on(dev, stream)), "pask_read_latent")
+
+
+def pask_decode_attention_latent(cache: int, layer: int, seq_ids, q, scale: float, out, lse, workspace, stream=None):
+    """One new query per sequence over a latent cache: q bf16 [n][n_q][576], out bf16 [n][n_q][512], lse fp32 [n][n_q] or None."""
+    n, dev = seq_ids.numel(), seq_ids.device
+    heads = _latent_shape.get(cache, (None, None))[0]
+    _latent_args("pask_decode_attention_latent", dev, ("seq_ids", seq_ids, torch.int32, (n,)),
+                 ("q", q, torch.bfloat16, (n, heads, LATENT_DIM)), ("out", out, torch.bfloat16, (n, heads, LATENT_VALUE_DIM)),
+                 ("lse", lse, torch.float32, (n, heads)))
+    with torch.cuda.device(dev):
+        _check(_lib.pask_decode_attention_latent(cache, layer, n, _dptr(seq_ids), _dptr(q), scale, _dptr(out), _dptr(lse),
+                                                 _dptr(workspace), workspace.numel() * workspace.element_size(), _on(dev, stream)),
+               "pask_decode_attention_latent")
+
+
+def pask_prompt_attention_latent(cu_q, cu_k, q, kv, k_rope, scale: float, out, lse=None, stream=None):
+    """Causal attention of a ragged batch of prompts (or chunks behind a history), keys and values expanded per head:
+    q bf16 [total_q][h][192], kv bf16 [total_k][h][256], k_rope bf16 [total_k][64] (rows may be strided, as in
+    latent[:, 512:]), out bf16 [total_q][h][128], lse fp32 [total_q][h] or None."""
+    n, dev = cu_q.numel() - 1, cu_q.device
+    tq, heads, tk = q.shape[0], q.shape[1] if q.dim() == 3 else 0, kv.shape[0]
+    where = "pask_prompt_attention_latent"
+    _latent_args(where, dev, ("cu_q", cu_q, torch.int32, (n + 1,)), ("cu_k", cu_k, torch.int32, (n + 1,)),
+                 ("q", q, torch.bfloat16, (None, heads, 192)), ("kv", kv, torch.bfloat16, (None, heads, 256)),
+                 ("out", out, torch.bfloat16, (tq, heads, 128)), ("lse", lse, torch.float32, (tq, heads)))
+    if not (k_rope.device == dev and k_rope.dtype == torch.bfloat16 and k_rope.shape == (tk, 64) and k_rope.stride(1) == 1):
+        raise PaskError(ERR_INVALID_ARG, f"{where}: k_rope must be a bfloat16 tensor [{tk}, 64] on {dev} with adjacent columns")
+    stride = k_rope.stride(0) if tk > 1 else 64
+    with torch.cuda.device(dev):
+        _check(_lib.pask_prompt_attention_latent(n, tq, tk, heads, _dptr(cu_q), _dptr(cu_k), _dptr(q), _dptr(kv), k_rope.data_ptr(),
+                                                 stride, scale, _dptr(out), _dptr(lse), _on(dev, stream)), where)
+
+
 def pask_budget_state(cache: int, seq: int, stream=None) -> BudgetState:
     out = BudgetState()
     _check(_lib.pask_budget_state(cache, seq, C.byref(out), _stream(stream)), "pask_budget_state")
@@ -453,9 +535,9 @@ class Cache:
     """Convenience owner of the device buffers a cache needs (torch allocations) plus its handle."""
 
     def __init__(self, blob: bytes, n_layers, n_q, n_kv, max_seqs, max_tokens_per_seq, max_append_tokens,
-                 pool_high_pages, pool_low_pages, device="cuda", recent_window=0, low_bits=4):
+                 pool_high_pages, pool_low_pages, device="cuda", recent_window=0, low_bits=4, head_dim=128):
         self.policy = pask_load_policy(blob)
-        self.desc = CacheDesc(n_layers, n_q, n_kv, 128, 16, max_seqs, max_tokens_per_seq, max_append_tokens,
+        self.desc = CacheDesc(n_layers, n_q, n_kv, head_dim, 16, max_seqs, max_tokens_per_seq, max_append_tokens,
                               pool_high_pages, pool_low_pages, recent_window, low_bits)
         self.sizes = pask_cache_sizes(self.desc)
         self.n_q, self.n_kv, self.n_layers = n_q, n_kv, n_layers
@@ -484,3 +566,13 @@ class Cache:
             self.close()
         except Exception:       # interpreter shutdown: the module's globals may already be gone
             pass
+
+
+class LatentCache(Cache):
+    """A Cache of latent rows (head_dim 576, one row a token; see pask_append_latent)."""
+
+    def __init__(self, blob: bytes, n_layers, n_q, max_seqs, max_tokens_per_seq, max_append_tokens, pool_high_pages, pool_low_pages,
+                 device="cuda", low_bits=4):
+        with torch.cuda.device(device):
+            super().__init__(blob, n_layers, n_q, 1, max_seqs, max_tokens_per_seq, max_append_tokens, pool_high_pages, pool_low_pages,
+                             device=device, low_bits=low_bits, head_dim=LATENT_DIM)

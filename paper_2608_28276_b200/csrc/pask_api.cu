@@ -24,8 +24,11 @@ uint32_t rd32(const uint8_t *p) {
 }
 
 bool shape_ok(const pask_cache_desc_t *d) {
-    if (d->head_dim != kHeadDim || d->page_tokens != kPageTokens) return false;
     const int kv = d->n_kv_heads;
+    if (d->page_tokens != kPageTokens) return false;
+    if (d->head_dim == kLatentDim)
+        return kv == 1 && d->n_q_heads >= 1 && d->n_q_heads <= kLatentMaxHeads && d->recent_window == 0;
+    if (d->head_dim != kHeadDim) return false;
     if (!(kv == 1 || kv == 2 || kv == 4 || kv == 8)) return false;
     return d->n_q_heads == 4 * kv;
 }
@@ -178,8 +181,9 @@ pask_status_t pask_cache_sizes(const pask_cache_desc_t *d, pask_cache_sizes_t *o
     if (!d || !out) return PASK_ERR_INVALID_ARG;
     if (!shape_ok(d)) return PASK_ERR_UNSUPPORTED_SHAPE;
     if (!desc_ok(d)) return PASK_ERR_INVALID_ARG;
-    out->high_page_bytes = (size_t)d->n_kv_heads * kHighHeadBytes;
-    out->low_page_bytes = (size_t)d->n_kv_heads * (d->low_bits == 8 ? kLow8HeadBytes : d->low_bits == 2 ? kLow2HeadBytes : kLowHeadBytes);
+    const bool latent = d->head_dim == kLatentDim;
+    out->high_page_bytes = latent ? (size_t)kLatentHighPageBytes : (size_t)d->n_kv_heads * kHighHeadBytes;
+    out->low_page_bytes = latent ? (size_t)latent_low_page_bytes(d->low_bits ? d->low_bits : 4) : (size_t)d->n_kv_heads * (d->low_bits == 8 ? kLow8HeadBytes : d->low_bits == 2 ? kLow2HeadBytes : kLowHeadBytes);
     out->pool_high_bytes = out->high_page_bytes * ((size_t)d->pool_high_pages + window_pages(d));
     out->pool_low_bytes = out->low_page_bytes * d->pool_low_pages;
     out->meta_bytes = meta_offsets(d, 255, PASK_MAX_GROUPS).total;  // independent of the policy loaded later
@@ -208,6 +212,8 @@ pask_status_t pask_cache_create(const pask_cache_desc_t *d, const pask_policy_t 
     c->desc = *d;
     c->meta = meta;
     c->sm_count = sms;
+    c->device = dev_id;
+    c->latent = d->head_dim == kLatentDim;
     c->ev_start = c->ev_stop = nullptr;
     c->span = nullptr;
     c->ahead.resize((size_t)d->n_layers);
@@ -263,6 +269,12 @@ pask_status_t pask_cache_create(const pask_cache_desc_t *d, const pask_policy_t 
     v.low_page_bytes = (uint32_t)d->n_kv_heads * v.low_head_bytes;
     v.bytes_h = 2u * d->n_kv_heads * kHeadDim * 2u;
     v.bytes_l = 2u * d->n_kv_heads * (kHeadDim * pol->low_bits / 8 + kGroupsPerHead * 2);
+    if (c->latent) {   // one row a token instead of n_kv K and V heads; the streams, pages and counters are the same
+        v.high_page_bytes = kLatentHighPageBytes;
+        v.low_page_bytes = v.low_head_bytes = (uint32_t)latent_low_page_bytes((int)pol->low_bits);
+        v.bytes_h = kLatentDim * 2u;
+        v.bytes_l = kLatentDim * pol->low_bits / 8u + kLatentGroups * 2u;
+    }
     c->attn_ctas = attention_grid(c);
     c->dev.attn_ctas = (uint32_t)c->attn_ctas;
     c->lut = pol->eff;
@@ -345,6 +357,7 @@ static pask_status_t append_common(pask_cache_t *c, int32_t layer, int32_t n_seq
                                    const uint8_t *tags, const uint8_t *decided, uint8_t *actions_out,
                                    pask_stream_t stream, const Workspace *fuse_ws = nullptr, bool *fused = nullptr) {
     if (!c || !seq_ids || !cu_tokens || !tags) return PASK_ERR_INVALID_ARG;
+    if (c->latent) return PASK_ERR_UNSUPPORTED_SHAPE;
     if (layer < 0 || layer >= c->desc.n_layers) return PASK_ERR_INVALID_ARG;
     if (n_seqs < 1 || n_seqs > PASK_MAX_SEQS_PER_CALL || n_seqs > c->desc.max_seqs) return PASK_ERR_INVALID_ARG;
     if (total_tokens < 0 || total_tokens > c->desc.max_append_tokens) return PASK_ERR_INVALID_ARG;
@@ -372,6 +385,70 @@ pask_status_t pask_append_kv_decided(pask_cache_t *c, int32_t layer, int32_t n_s
     return append_common(c, layer, n_seqs, total_tokens, seq_ids, cu_tokens, k, v, tags, actions, actions_out, stream);
 }
 
+// the calls on a latent cache run where the cache lives: a pointer of one device is no good on another
+static pask_status_t latent_cache_ok(const pask_cache_t *c, int32_t layer, int32_t n_seqs, const int32_t *seq_ids) {
+    if (!c || !seq_ids) return PASK_ERR_INVALID_ARG;
+    if (!c->latent) return PASK_ERR_UNSUPPORTED_SHAPE;
+    if (layer < 0 || layer >= c->desc.n_layers || n_seqs < 1 || n_seqs > PASK_MAX_SEQS_PER_CALL) return PASK_ERR_INVALID_ARG;
+    if ((uintptr_t)seq_ids & 3) return PASK_ERR_INVALID_ARG;
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess) return PASK_ERR_CUDA;
+    return dev == c->device ? PASK_OK : PASK_ERR_INVALID_ARG;
+}
+
+pask_status_t pask_append_latent(pask_cache_t *c, int32_t layer, int32_t n_seqs, int32_t total_tokens, const int32_t *seq_ids,
+                                 const int32_t *cu_tokens, const void *latent, const uint8_t *tags, const uint8_t *actions,
+                                 uint8_t *actions_out, pask_stream_t stream) {
+    const pask_status_t ok = latent_cache_ok(c, layer, n_seqs, seq_ids);
+    if (ok != PASK_OK) return ok;
+    if (!cu_tokens || ((uintptr_t)cu_tokens & 3) || n_seqs > c->desc.max_seqs) return PASK_ERR_INVALID_ARG;
+    if (total_tokens < 0 || total_tokens > c->desc.max_append_tokens) return PASK_ERR_INVALID_ARG;
+    if (total_tokens > 0 && (!latent || !tags)) return PASK_ERR_INVALID_ARG;
+    if ((uintptr_t)latent & 15) return PASK_ERR_INVALID_ARG;
+    NvtxRange range("pask_append_latent");
+    return launch_append_latent(c, layer, n_seqs, total_tokens, seq_ids, cu_tokens, latent, tags, actions, actions_out,
+                                static_cast<cudaStream_t>(stream));
+}
+
+pask_status_t pask_read_latent(pask_cache_t *c, int32_t layer, int32_t n_seqs, int32_t total_rows, const int32_t *seq_ids,
+                               const int32_t *cu_rows, void *rows_out, int32_t *lens_out, pask_stream_t stream) {
+    const pask_status_t ok = latent_cache_ok(c, layer, n_seqs, seq_ids);
+    if (ok != PASK_OK) return ok;
+    if (!cu_rows || total_rows < 0 || (total_rows > 0 && !rows_out)) return PASK_ERR_INVALID_ARG;
+    if (((uintptr_t)rows_out & 15) || (((uintptr_t)cu_rows | (uintptr_t)lens_out) & 3)) return PASK_ERR_INVALID_ARG;
+    NvtxRange range("pask_read_latent");
+    return launch_read_latent(c, layer, n_seqs, total_rows, seq_ids, cu_rows, rows_out, lens_out, static_cast<cudaStream_t>(stream));
+}
+
+pask_status_t pask_decode_attention_latent(pask_cache_t *c, int32_t layer, int32_t n_seqs, const int32_t *seq_ids, const void *q,
+                                           float scale, void *out, float *lse, void *ws, size_t ws_bytes, pask_stream_t stream) {
+    const pask_status_t ok = latent_cache_ok(c, layer, n_seqs, seq_ids);
+    if (ok != PASK_OK) return ok;
+    if (!q || !out || !ws) return PASK_ERR_INVALID_ARG;
+    if (!(scale > 0.0f) || !(scale < 1e30f)) return PASK_ERR_INVALID_ARG;
+    if (((uintptr_t)q | (uintptr_t)out) & 15 || ((uintptr_t)ws & 255) || ((uintptr_t)lse & 3)) return PASK_ERR_INVALID_ARG;
+    if (ws_bytes < latent_workspace_bytes(c, n_seqs)) return PASK_ERR_WORKSPACE;
+    NvtxRange range("pask_decode_attention_latent");
+    return launch_decode_latent(c, layer, n_seqs, seq_ids, q, scale, out, lse, ws, static_cast<cudaStream_t>(stream));
+}
+
+pask_status_t pask_prompt_attention_latent(int32_t n_seqs, int32_t total_q, int32_t total_k, int32_t n_heads, const int32_t *cu_q,
+                                           const int32_t *cu_k, const void *q, const void *kv, const void *k_rope,
+                                           int32_t rope_stride, float scale, void *out, float *lse, pask_stream_t stream) {
+    if (!cu_q || !cu_k || n_seqs < 1 || n_seqs > PASK_MAX_SEQS_PER_CALL) return PASK_ERR_INVALID_ARG;
+    if (n_heads < 1 || n_heads > kLatentMaxHeads) return PASK_ERR_UNSUPPORTED_SHAPE;
+    if (total_q < 0 || total_k < 0) return PASK_ERR_INVALID_ARG;
+    if (!(scale > 0.0f) || !(scale < 1e30f)) return PASK_ERR_INVALID_ARG;
+    if (total_q == 0) return PASK_OK;
+    if (!q || !out || (total_k > 0 && (!kv || !k_rope))) return PASK_ERR_INVALID_ARG;
+    if (rope_stride < 64 || rope_stride % 8) return PASK_ERR_INVALID_ARG;
+    if (((uintptr_t)q | (uintptr_t)out | (uintptr_t)kv | (uintptr_t)k_rope) & 15) return PASK_ERR_INVALID_ARG;
+    if (((uintptr_t)cu_q | (uintptr_t)cu_k | (uintptr_t)lse) & 3) return PASK_ERR_INVALID_ARG;
+    NvtxRange range("pask_prompt_attention_latent");
+    return launch_prompt_latent(n_seqs, total_q, total_k, n_heads, cu_q, cu_k, q, kv, k_rope, rope_stride, scale, out, lse,
+                                static_cast<cudaStream_t>(stream));
+}
+
 pask_status_t pask_decide(pask_cache_t *c, int32_t n_seqs, int32_t total_tokens, const int32_t *seq_ids,
                           const int32_t *cu_tokens, const uint8_t *tags, const uint16_t *states, uint8_t *actions_out,
                           pask_stream_t stream) {
@@ -388,6 +465,7 @@ static pask_status_t attention_common(pask_cache_t *c, bool has_low, int32_t lay
                                       const int32_t *seq_ids, const void *q, float *out, float *lse, void *ws,
                                       size_t ws_bytes, pask_stream_t stream, bool plan_done = false, bool check_only = false) {
     if (!c || !seq_ids || !q || !out || !ws) return PASK_ERR_INVALID_ARG;
+    if (c->latent) return PASK_ERR_UNSUPPORTED_SHAPE;
     if (layer < 0 || layer >= c->desc.n_layers) return PASK_ERR_INVALID_ARG;
     if (n_seqs < 1 || n_seqs > PASK_MAX_SEQS_PER_CALL) return PASK_ERR_INVALID_ARG;
     if (((uintptr_t)q | (uintptr_t)out) & 15 || ((uintptr_t)ws & 255) || ((uintptr_t)lse & 3)) return PASK_ERR_INVALID_ARG;
@@ -428,11 +506,11 @@ pask_status_t pask_decode_attention_full(pask_cache_t *c, int32_t layer, int32_t
 
 size_t pask_workspace_bytes(const pask_cache_t *c, int32_t n_seqs) {
     if (!c || n_seqs < 1) return 0;
-    return attention_workspace_bytes(c, n_seqs);
+    return c->latent ? latent_workspace_bytes(c, n_seqs) : attention_workspace_bytes(c, n_seqs);
 }
 
 size_t pask_plan_area_bytes(const pask_cache_t *c, int32_t n_seqs) {
-    if (!c || n_seqs < 1 || n_seqs > 255) return 0;
+    if (!c || c->latent || n_seqs < 1 || n_seqs > 255) return 0;
     return carve_plan_area(c, n_seqs, 0, 0, nullptr, nullptr);
 }
 
@@ -440,7 +518,7 @@ static pask_status_t ahead_args_ok(pask_cache_t *c, int32_t layer, int32_t n_seq
                                    size_t area_bytes) {
     if (!c || !seq_ids || !area) return PASK_ERR_INVALID_ARG;
     if (layer < 0 || layer >= c->desc.n_layers || n_seqs < 1 || n_seqs > c->desc.max_seqs) return PASK_ERR_INVALID_ARG;
-    if (n_seqs > 255 || c->dev.window) return PASK_ERR_UNSUPPORTED_SHAPE;
+    if (n_seqs > 255 || c->dev.window || c->latent) return PASK_ERR_UNSUPPORTED_SHAPE;
     if (((uintptr_t)seq_ids & 3) || ((uintptr_t)area & 255)) return PASK_ERR_INVALID_ARG;
     if (area_bytes < pask_plan_area_bytes(c, n_seqs)) return PASK_ERR_WORKSPACE;
     return PASK_OK;
@@ -489,7 +567,7 @@ pask_status_t pask_decode_step_ahead(pask_cache_t *c, int32_t layer, int32_t n_s
 }
 
 size_t pask_step_staging_bytes(const pask_cache_t *c, int32_t n_seqs) {
-    if (!c || n_seqs < 1) return 0;
+    if (!c || c->latent || n_seqs < 1) return 0;
     const size_t n = (size_t)n_seqs;
     size_t p = 0;
     p += align_up(n * 4, 256);                                    // seq_ids
@@ -513,6 +591,7 @@ pask_status_t pask_decode_step_host(pask_cache_t *c, int32_t layer, int32_t n_se
                                     void *ws, size_t ws_bytes, pask_stream_t stream_v) {
     if (!c || !seq_ids_host || !k_host || !v_host || !tags_host || !q_host || !out_host || !staging)
         return PASK_ERR_INVALID_ARG;
+    if (c->latent) return PASK_ERR_UNSUPPORTED_SHAPE;
     if (n_seqs < 1 || n_seqs > PASK_MAX_SEQS_PER_CALL) return PASK_ERR_INVALID_ARG;
     if (((uintptr_t)staging & 255) || staging_bytes < pask_step_staging_bytes(c, n_seqs)) return PASK_ERR_WORKSPACE;
     cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
@@ -543,6 +622,7 @@ pask_status_t pask_decode_step_host(pask_cache_t *c, int32_t layer, int32_t n_se
 
 pask_status_t pask_step_packed_layout(const pask_cache_t *c, int32_t n_seqs, size_t offsets[6], size_t *in_bytes) {
     if (!c || n_seqs < 1 || !offsets || !in_bytes) return PASK_ERR_INVALID_ARG;
+    if (c->latent) return PASK_ERR_UNSUPPORTED_SHAPE;
     const size_t n = (size_t)n_seqs;
     const size_t kv_bytes = n * c->desc.n_kv_heads * kHeadDim * 2, q_bytes = n * c->desc.n_q_heads * kHeadDim * 2;
     size_t p = 0;
@@ -560,6 +640,7 @@ pask_status_t pask_decode_step_packed(pask_cache_t *c, int32_t layer, int32_t n_
                                       float *out_host, void *staging, size_t staging_bytes, void *ws, size_t ws_bytes,
                                       pask_stream_t stream_v) {
     if (!c || !packed_host || !out_host || !staging) return PASK_ERR_INVALID_ARG;
+    if (c->latent) return PASK_ERR_UNSUPPORTED_SHAPE;
     if (n_seqs < 1 || n_seqs > PASK_MAX_SEQS_PER_CALL) return PASK_ERR_INVALID_ARG;
     if (((uintptr_t)staging & 255) || staging_bytes < pask_step_staging_bytes(c, n_seqs)) return PASK_ERR_WORKSPACE;
     size_t off[6], in_bytes = 0;
@@ -580,6 +661,7 @@ static pask_status_t step_pipelined(pask_cache_t *c, int32_t layer, int32_t n_se
                                     float *out_host, void *staging, size_t staging_bytes, void *ws, size_t ws_bytes,
                                     void *plan_area, size_t plan_area_bytes, pask_stream_t stream_v) {
     if (!c || !packed_host || !out_host || !staging) return PASK_ERR_INVALID_ARG;
+    if (c->latent) return PASK_ERR_UNSUPPORTED_SHAPE;
     if (n_seqs < 1 || n_seqs > PASK_MAX_SEQS_PER_CALL) return PASK_ERR_INVALID_ARG;
     const size_t slot_bytes = pask_step_staging_bytes(c, n_seqs);
     // The two slots are the two halves of the staging buffer, whatever the batch: a call's slot never overlaps the
@@ -733,6 +815,7 @@ pask_status_t pask_debug_page_ids(pask_cache_t *c, int32_t layer, int32_t seq, u
 pask_status_t pask_debug_dump_high(pask_cache_t *c, int32_t layer, int32_t seq, uint16_t *k_out, uint16_t *v_out,
                                    uint32_t *pages_out, pask_stream_t stream) try {
     if (!c || !seq_layer_ok(c, layer, seq)) return PASK_ERR_INVALID_ARG;
+    if (c->latent) return PASK_ERR_UNSUPPORTED_SHAPE;   // pask_read_latent
     uint32_t nh = 0, nl = 0;
     pask_status_t rc = read_lens(c, layer, seq, &nh, &nl, static_cast<cudaStream_t>(stream));
     if (rc != PASK_OK) return rc;
@@ -770,6 +853,7 @@ pask_status_t pask_debug_dump_high(pask_cache_t *c, int32_t layer, int32_t seq, 
 pask_status_t pask_debug_dump_low(pask_cache_t *c, int32_t layer, int32_t seq, uint8_t *k_codes, uint16_t *k_scales,
                                   uint8_t *v_codes, uint16_t *v_scales, uint32_t *pages_out, pask_stream_t stream) try {
     if (!c || !seq_layer_ok(c, layer, seq)) return PASK_ERR_INVALID_ARG;
+    if (c->latent) return PASK_ERR_UNSUPPORTED_SHAPE;   // pask_read_latent
     uint32_t nh = 0, nl = 0;
     pask_status_t rc = read_lens(c, layer, seq, &nh, &nl, static_cast<cudaStream_t>(stream));
     if (rc != PASK_OK) return rc;
@@ -851,6 +935,7 @@ pask_status_t pask_debug_plan_order_span(const pask_cache_t *c, int32_t n_seqs, 
                                          size_t *bytes) {
     if (!c || !offset || !bytes || n_seqs < 1 || n_seqs > 255 || layer < 0 || layer >= c->desc.n_layers || (parity & ~1))
         return PASK_ERR_INVALID_ARG;
+    if (c->latent) return PASK_ERR_UNSUPPORTED_SHAPE;
     PlanBlock pb;
     uint8_t origin = 0;                                             // any base will do: only the distance from it is used
     carve_plan_area(c, n_seqs, layer, parity, &origin, &pb);

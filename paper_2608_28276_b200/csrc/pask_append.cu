@@ -1226,6 +1226,14 @@ __global__ void __launch_bounds__(256) seq_reset_kernel(DevCache c, int seq) {
 
 }  // namespace
 
+pask_status_t launch_append_plan(pask_cache *c, int layer, int n_seqs, int total_tokens, const int32_t *seq_ids,
+                                 const int32_t *cu_tokens, const uint8_t *tags, const uint8_t *decided, uint8_t *actions_out,
+                                 cudaStream_t stream) {
+    append_plan_kernel<<<n_seqs, kBulkThreads, 0, stream>>>(c->dev, layer, n_seqs, total_tokens, seq_ids, cu_tokens, tags,
+                                                           decided, actions_out);
+    return cudaGetLastError() == cudaSuccess ? PASK_OK : PASK_ERR_CUDA;
+}
+
 pask_status_t launch_append(pask_cache *c, int layer, int n_seqs, int total_tokens, const int32_t *seq_ids,
                             const int32_t *cu_tokens, const void *k, const void *v, const uint8_t *tags,
                             const uint8_t *decided, uint8_t *actions_out, cudaStream_t stream, const Workspace *fuse_ws,

@@ -1078,7 +1078,7 @@ size_t carve_workspace(const pask_cache *c, int n_seqs, uint8_t *base, Workspace
 }
 
 
-int attention_grid(const pask_cache *c) { return 2 * c->sm_count; }
+int attention_grid(const pask_cache *c) { return c->latent ? c->sm_count : 2 * c->sm_count; }
 
 size_t attention_workspace_bytes(const pask_cache *c, int n_seqs) { return carve_workspace(c, n_seqs, nullptr, nullptr); }
 
@@ -1239,6 +1239,7 @@ extern "C" pask_status_t pask_decode_attention_static(pask_cache_t *c, int32_t l
                                                       const int32_t *seq_ids, const void *q, float *out, float *lse,
                                                       pask_stream_t stream) {
     if (!c || !seq_ids || !q || !out) return PASK_ERR_INVALID_ARG;
+    if (c->latent) return PASK_ERR_UNSUPPORTED_SHAPE;
     if (layer < 0 || layer >= c->desc.n_layers) return PASK_ERR_INVALID_ARG;
     if (n_seqs < 1 || n_seqs > PASK_MAX_SEQS_PER_CALL) return PASK_ERR_INVALID_ARG;
     if ((((uintptr_t)q | (uintptr_t)out) & 15) || ((uintptr_t)lse & 3)) return PASK_ERR_INVALID_ARG;

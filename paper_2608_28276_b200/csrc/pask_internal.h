@@ -133,6 +133,8 @@ struct pask_cache {
     void *meta;
     std::vector<uint8_t> lut, layer_group;   // host copies of the folded table [n_tags][n_groups] and the layer map
     int sm_count;
+    int device;                   // the device the cache was created on
+    bool latent;                  // head_dim 576: one latent row a token (pask_append_latent and its kind)
     int attn_ctas;                // grid of the decode-attention main kernel
     cudaEvent_t ev_start, ev_stop;
     unsigned long long *span;     // pask_cache_set_timing_span: where the next streaming kernel leaves its start and end
@@ -194,6 +196,23 @@ pask_status_t launch_append(pask_cache *c, int layer, int n_seqs, int total_toke
                             const int32_t *cu_tokens, const void *k, const void *v, const uint8_t *tags,
                             const uint8_t *decided, uint8_t *actions_out, cudaStream_t stream,
                             const Workspace *fuse_ws = nullptr, bool *fused = nullptr);
+// the first of a bulk append's two kernels: decides and ranks every token, allocates pages, commits -- or refuses the call
+// (kCtrlPlanOk); it knows nothing of what a token's payload is
+pask_status_t launch_append_plan(pask_cache *c, int layer, int n_seqs, int total_tokens, const int32_t *seq_ids,
+                                 const int32_t *cu_tokens, const uint8_t *tags, const uint8_t *decided, uint8_t *actions_out,
+                                 cudaStream_t stream);
+// latent caches
+pask_status_t launch_append_latent(pask_cache *c, int layer, int n_seqs, int total_tokens, const int32_t *seq_ids,
+                                   const int32_t *cu_tokens, const void *latent, const uint8_t *tags, const uint8_t *decided,
+                                   uint8_t *actions_out, cudaStream_t stream);
+pask_status_t launch_read_latent(pask_cache *c, int layer, int n_seqs, int total_rows, const int32_t *seq_ids,
+                                 const int32_t *cu_rows, void *rows_out, int32_t *lens_out, cudaStream_t stream);
+pask_status_t launch_decode_latent(pask_cache *c, int layer, int n_seqs, const int32_t *seq_ids, const void *q, float scale,
+                                   void *out, float *lse, void *workspace, cudaStream_t stream);
+size_t latent_workspace_bytes(const pask_cache *c, int n_seqs);
+pask_status_t launch_prompt_latent(int n_seqs, int total_q, int total_k, int n_heads, const int32_t *cu_q, const int32_t *cu_k,
+                                   const void *q, const void *kv, const void *k_rope, int rope_stride, float scale, void *out,
+                                   float *lse, cudaStream_t stream);
 pask_status_t launch_decide(pask_cache *c, int n_seqs, int total_tokens, const int32_t *seq_ids, const int32_t *cu_tokens,
                             const uint8_t *tags, const uint16_t *states, uint8_t *actions_out, cudaStream_t stream);
 pask_status_t launch_seq_reset(pask_cache *c, int seq, cudaStream_t stream);

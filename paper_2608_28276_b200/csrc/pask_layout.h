@@ -46,6 +46,18 @@
 //              high half-word token 2t+1 (+8 in byte 1); the field at bits 2i of a byte is dim
 //              32q + 4g + i: fields 0, 1 are rows g, g+8 of P.V tile 2q, fields 2, 3 of tile 2q+1
 //              (the row order of the other formats).
+//
+// Latent caches (head_dim 576: one row a token, a 512-wide latent and 64 rotary dims, no separate K and V)
+// HIGH page  : 2 half-pages of 8 tokens, each 9 blocks (64 dims) of 1024 B: token row r = 0..7 of 128 B, the 16-byte
+//              chunk k = 0..7 of a row at position k ^ r (the 128-byte swizzle of the tensor core's shared-memory
+//              operands).  A page brought in by one linear bulk copy is at once a K-major operand (tokens x dims, for
+//              q k^T) and an MN-major one (dims x tokens, for the values): 8-token groups lie 9216 B apart and 64-dim
+//              blocks 1024 B, in a page and from page to page.
+// LOW page   : codes [group 18][token 16], 4 * bits bytes each (eight-bit codes: two planes of 16 bytes, [group][half]
+//              [token]), then bf16 scales [group][token].  The 32 codes of a group in 32-bit words:
+//              4 bits: word j = dims 8j .. 8j+7, dim 8j + e at nibble (e >> 1) + 4 (e & 1); 2 bits: word j = dims 16j ..
+//              16j+15, dim 16j + e at bits (e & ~1) + 16 (e & 1): (word >> shift) & 0x000F000F (0x00030003) is a pair of
+//              consecutive dims; 8 bits: bytes in order.
 #pragma once
 #include <stdint.h>
 
@@ -78,6 +90,26 @@ constexpr uint32_t kCostHighPage = 32;
 constexpr uint32_t kCostLowPage = 9;
 constexpr uint32_t kCostLow8Page = 17;
 constexpr uint32_t kCostLow2Page = 5;
+
+// latent caches
+constexpr int kLatentDim = 576;                  // 512 latent + 64 rotary dims
+constexpr int kLatentValueDim = 512;             // the leading dims of a row, its value vector
+constexpr int kLatentChunks = kLatentDim / 8;    // 16-byte chunks of a bf16 row
+constexpr int kLatentGroups = kLatentDim / kQGroup;
+constexpr int kLatentHalfPage = 9 * 1024;        // 8 tokens
+constexpr int kLatentHighPageBytes = 2 * kLatentHalfPage;
+constexpr int kLatentMaxHeads = 128;
+PASK_HD int latent_code_bytes(int bits) { return kLatentGroups * kPageTokens * 4 * bits; }
+PASK_HD int latent_low_page_bytes(int bits) { return latent_code_bytes(bits) + kLatentGroups * kPageTokens * 2; }
+// HIGH page: offset of 16-byte chunk `chunk` (0..71) of token tau
+PASK_HD int latent_chunk_off(int tau, int chunk) {
+    return (tau >> 3) * kLatentHalfPage + (chunk >> 3) * 1024 + (tau & 7) * 128 + (((chunk ^ tau) & 7) << 4);
+}
+// LOW page: offset of the codes of (token, group); eight-bit codes: the first 16 of them, the others kPageTokens * 16 behind
+PASK_HD int latent_code_off(int tau, int group, int bits) {
+    return bits == 8 ? (2 * group * kPageTokens + tau) * 16 : (group * kPageTokens + tau) * 4 * bits;
+}
+PASK_HD int latent_scale_off(int tau, int group, int bits) { return latent_code_bytes(bits) + (group * kPageTokens + tau) * 2; }
 
 // HIGH K tile: offset of the 4-byte piece holding dims 2p, 2p+1 (p = 0..63) of token tau.
 PASK_HD int high_k_pair_off(int tau, int p) {
