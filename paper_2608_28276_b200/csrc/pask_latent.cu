@@ -8,6 +8,7 @@
 #include <cuda_bf16.h>
 
 #include "pask_internal.h"
+#include "pask_umma.h"
 
 namespace pask {
 
@@ -286,77 +287,658 @@ read_latent_kernel(DevCache c, int layer, int n_seqs, int total_rows, const int3
 }
 
 // ---------------------------------------------------------------- decode attention
+//
+// out_h = sum_j softmax_j(scale q_h . x_j) x_j[0:512] over a sequence's rows x_j (576 values): every head reads every row, so a
+// row is fetched once and used as key and value by all heads -- 2 n_q (576 + 512) operations for 1152 bytes, 121 (n_q = 64)
+// or 242 (n_q = 128) a byte, around the ratio of the tensor core's rate to the memory's.  Matrix products, then, on tcgen05:
+//
+//   S^T [64 tokens x heads] = X Q^T       X K-major from shared memory (M = 64), Q K-major (N = heads)
+//   O^T [512 dims x heads] += X^T P^T     X MN-major, the very same bytes (M = 128, four blocks), P [token][head] MN-major
+//
+// Rows on the M side and heads on the N side: a CTA takes up to 64 heads (kHeads = 16, 32 or 64, the next size up) and the
+// accumulators of all 512 value dims fit tensor memory (4 x 64 columns, beside two S tiles).  More than 64 heads are split
+// over that many CTAs that walk the same tiles side by side and find each other's rows in L2.
+//
+// A CTA is one of `slots` equal shares of the batch's rows (cost line over sequences, as the other decode kernel cuts it), in
+// tiles of 64 rows = four pages of one stream; a sequence's HIGH and LOW tiles are visited in turn, evenly mixed.  Roles:
+//   warp 8      HIGH tiles: one linear bulk copy a page (pages are stored in the operand layout) into one of two stages, and
+//               a prefetch into L2 some tiles ahead, which keeps memory busy while both stages are held by products
+//   warps 4-7   LOW tiles: codes to registers one tile ahead, values as bf16 into the stage; and the queries of a sequence
+//   warp 9      issues the products: S of tile i + 1, then O of tile i
+//   warps 0-3   softmax of a tile's S (warp w: page w of the tile), P to shared memory, and a sequence's end
+// The reference maximum of a head moves only when a score exceeds it by more than 2^8 (the sums have room for that), so that
+// the rescaling of O leaves the common path.  A share that covers a whole sequence writes its result; otherwise partial sums
+// go to the workspace and decode_latent_merge joins them in a fixed order: results do not depend on timing.
+constexpr int kTile = 64, kTilePages = 4;
+constexpr int kTileBytes = kTilePages * kLatentHighPageBytes;      // 73728
+constexpr int kDecThreads = 320;
+constexpr uint32_t kMaxSlots = 1024;
+constexpr int kPrefetch = 4;                       // tiles between a prefetch into L2 and the copy
+constexpr uint32_t kCostHighTile = 3, kCostLowTile = 2;
+constexpr float kLazy = 8.0f;                      // log2 of how far a score may exceed the reference maximum
 
-// One CTA per (query head, sequence); a warp takes every eighth row, lanes take the row's 18 groups' dims.
-template <int BITS>
-__global__ void __launch_bounds__(256)
-decode_latent_kernel(DevCache c, int layer, const int32_t *__restrict__ seq_ids, const __nv_bfloat16 *__restrict__ q, float scale,
-                     __nv_bfloat16 *__restrict__ out, float *__restrict__ lse) {
-    __shared__ float s_q[kLatentDim], s_m[8], s_l[8], s_o[8][kLatentValueDim];
-    const int head = blockIdx.x, i = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int seq = seq_ids[i];
-    const bool ok = seq >= 0 && seq < c.max_seqs;
-    if (!ok && tid == 0) atomicOr(&c.ctrl[kCtrlStatus], PASK_DEV_BAD_SEQ);
-    const size_t sl = (size_t)(ok ? seq : 0) * c.n_layers + layer;
-    const uint32_t nh = ok ? c.n_high[sl] : 0u, nl = ok ? c.n_low[sl] : 0u;
-    for (int d = tid; d < kLatentDim; d += 256) s_q[d] = __bfloat162float(q[((size_t)i * c.n_q + head) * kLatentDim + d]) * scale;
-    __syncthreads();
-    float m = -INFINITY, l = 0.0f, o[16];          // lane g < 18 holds group g: its 32 dims as two halves of 16 in turn
-    float o2[16];
-#pragma unroll
-    for (int e = 0; e < 16; e++) o[e] = o2[e] = 0.0f;
-    for (uint32_t r = warp; r < nh + nl; r += 8) {
-        const bool high = r < nh;
-        const uint32_t at = high ? r : r - nh;
-        const uint32_t page = (high ? c.tbl_high : c.tbl_low)[sl * c.max_pages + (at >> 4)];
-        if (page >= (high ? c.cap_high : c.cap_low)) {
-            if (lane == 0) atomicOr(&c.ctrl[kCtrlStatus], PASK_DEV_INTERNAL);
-            continue;
+struct DecParams {
+    DevCache c;
+    int layer, n_seqs, groups, heads;              // groups of `heads` heads each (the last one may have fewer)
+    uint32_t slots;
+    const int32_t *seq_ids;
+    const uint4 *q;
+    float scale_log2;
+    __nv_bfloat16 *out;
+    float *lse;
+    uint32_t *prefix;                              // [n_seqs + 1] cost of the sequences before s
+    float2 *part_ml;                               // [slots + n_seqs][n_q] (reference maximum in log2 units, sum)
+    float *part_o;                                 // [slots + n_seqs][n_q][512]
+    long long wait_cycles;
+    uint32_t surplus;
+    unsigned long long *span;
+};
+
+__device__ __forceinline__ uint32_t tiles_of(uint32_t tokens) { return (tokens + kTile - 1) / kTile; }
+__device__ __forceinline__ uint32_t cost_of(uint32_t nh, uint32_t nl) { return kCostHighTile * tiles_of(nh) + kCostLowTile * tiles_of(nl); }
+__device__ __forceinline__ uint32_t slot_start(uint32_t total, uint32_t slot, uint32_t slots) {
+    return (uint32_t)((uint64_t)total * slot / slots);
+}
+
+// The tiles of one share, in order; every role walks its own copy.
+struct TileWalk {
+    const DevCache *c;
+    const int32_t *seq_ids;
+    int layer, n_seqs, s;
+    uint32_t lo, hi, base, cost;
+    uint32_t nh, nl, th, tl, v, v0, v1;
+    size_t sl;
+    bool high;
+    uint32_t tile, valid, pages;                   // tile of the stream, its rows and pages
+
+    __device__ __forceinline__ void load() {
+        const int seq = seq_ids[s];
+        const bool ok = seq >= 0 && seq < c->max_seqs;
+        sl = (size_t)(ok ? seq : 0) * c->n_layers + layer;
+        nh = ok ? c->n_high[sl] : 0u;
+        nl = ok ? c->n_low[sl] : 0u;
+        th = tiles_of(nh);
+        tl = tiles_of(nl);
+        cost = kCostHighTile * th + kCostLowTile * tl;
+        v0 = v1 = 0;
+        if (cost) {
+            v0 = lo > base ? cut_positions(lo - base, cost, th + tl) : 0u;
+            v1 = cut_positions(hi - base, cost, th + tl);
         }
-        uint32_t xs[16];
+        v = v0;
+    }
+    __device__ __forceinline__ bool settle() {     // on to a sequence with tiles in the share
+        while (v >= v1) {
+            base += cost;
+            if (++s >= n_seqs || base >= hi) return false;
+            load();
+        }
+        high = page_at(v, th, tl, tile);
+        valid = min((uint32_t)kTile, (high ? nh : nl) - kTile * tile);
+        pages = (valid + kPageTokens - 1) / kPageTokens;
+        return true;
+    }
+    __device__ __forceinline__ bool begin(const DecParams &p, int first, uint32_t first_base, uint32_t lo_, uint32_t hi_) {
+        c = &p.c; seq_ids = p.seq_ids; layer = p.layer; n_seqs = p.n_seqs;
+        lo = lo_; hi = hi_; s = first; base = first_base;
+        if (s >= n_seqs) return false;
+        load();
+        return settle();
+    }
+    __device__ __forceinline__ bool next() { v++; return settle(); }
+    __device__ __forceinline__ bool first() const { return v == v0; }
+    __device__ __forceinline__ bool last() const { return v + 1 == v1; }
+    __device__ __forceinline__ bool whole() const { return v0 == 0 && v1 == th + tl; }
+    // id of the tile's page p; an id the pools cannot hold is never dereferenced
+    __device__ __forceinline__ uint32_t page(uint32_t p) const {
+        const uint32_t id = (high ? c->tbl_high : c->tbl_low)[sl * c->max_pages + kTilePages * tile + p];
+        if (id < (high ? c->cap_high : c->cap_low)) return id;
+        atomicOr(&c->ctrl[kCtrlStatus], PASK_DEV_INTERNAL);
+        return 0;
+    }
+};
+
+template <int kHeads>
+struct DecSmem {
+    static constexpr int kQ = 2 * kTileBytes, kP = kQ + kHeads * 1152, kMisc = kP + kTile * 128;
+    struct Misc {
+        uint64_t kv_full[2], kv_empty[2], s_full[2], s_empty[2], q_full, q_empty, p_full, p_empty, o_free, drain;
+        uint32_t tmem;
+        int first;
+        uint32_t first_base, total;
+        uint32_t warp_sum[kDecThreads / 32];
+        float red[4][kHeads], fac[kHeads], mref[kHeads];
+    };
+    static constexpr int kBytes = kMisc + (int)sizeof(Misc) + 1024;
+};
+
+template <int kHeads, int BITS>
+__global__ void __launch_bounds__(kDecThreads, 1)
+decode_latent_kernel(const __grid_constant__ DecParams p) {
+    using namespace umma;
+    using Sm = DecSmem<kHeads>;
+    extern __shared__ uint8_t s_raw[];
+    uint8_t *sm = reinterpret_cast<uint8_t *>(((uintptr_t)s_raw + 1023) & ~(uintptr_t)1023);
+    typename Sm::Misc &ms = *reinterpret_cast<typename Sm::Misc *>(sm + Sm::kMisc);
+    const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
+    const uint32_t slot = blockIdx.x / p.groups, group = blockIdx.x % p.groups;
+    const int h0 = (int)group * p.heads, nh_here = min(p.heads, p.c.n_q - h0);       // this CTA's query heads
+    pdl_launch_dependents();
+    pdl_wait();
+    unsigned long long t_start = 0;
+    if (p.span && tid == 0) asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t_start));
+
+    // ---- the share: cost prefix over the sequences (1024 at most, kPer a thread)
+    constexpr int kPer = (PASK_MAX_SEQS_PER_CALL + kDecThreads - 1) / kDecThreads;
+    uint32_t cost[kPer], sum = 0;
 #pragma unroll
-        for (int e = 0; e < 16; e++) xs[e] = 0;
-        if (lane < kLatentGroups) {
-            if (high) {
-                const uint8_t *src = c.pool_high + (size_t)page * kLatentHighPageBytes;
-#pragma unroll
-                for (int k = 0; k < 4; k++) {
-                    const uint4 x = *reinterpret_cast<const uint4 *>(src + latent_chunk_off((int)(at & 15), 4 * lane + k));
-                    xs[4 * k] = x.x; xs[4 * k + 1] = x.y; xs[4 * k + 2] = x.z; xs[4 * k + 3] = x.w;
-                }
-            } else {
-                const uint8_t *src = c.pool_low + (size_t)page * c.low_page_bytes;
-                uint32_t words[BITS];
-                load_codes<BITS>(src, (int)(at & 15), lane, words);
-                dequantise_group<BITS>(words, *reinterpret_cast<const uint16_t *>(src + latent_scale_off((int)(at & 15), lane, BITS)), xs);
+    for (int r = 0; r < kPer; r++) {
+        const int s = tid * kPer + r;
+        cost[r] = 0;
+        if (s < p.n_seqs) {
+            const int seq = p.seq_ids[s];
+            if (seq >= 0 && seq < p.c.max_seqs) {
+                const size_t sl = (size_t)seq * p.c.n_layers + p.layer;
+                cost[r] = cost_of(p.c.n_high[sl], p.c.n_low[sl]);
+            } else if (blockIdx.x == 0) {
+                atomicOr(&p.c.ctrl[kCtrlStatus], PASK_DEV_BAD_SEQ);
             }
         }
-        float s = 0.0f;
-        if (lane < kLatentGroups)
-#pragma unroll
-            for (int e = 0; e < 16; e++) s += bf16_lo(xs[e]) * s_q[32 * lane + 2 * e] + bf16_hi(xs[e]) * s_q[32 * lane + 2 * e + 1];
-#pragma unroll
-        for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
-        const float mn = fmaxf(m, s), a = expf(m - mn), p = expf(s - mn);
-        m = mn;
-        l = l * a + p;
-#pragma unroll
-        for (int e = 0; e < 16; e++) { o[e] = o[e] * a + p * bf16_lo(xs[e]); o2[e] = o2[e] * a + p * bf16_hi(xs[e]); }
+        sum += cost[r];
     }
-    if (lane == 0) { s_m[warp] = m; s_l[warp] = l; }
-    if (lane < 16)
+    uint32_t inc = sum;
 #pragma unroll
-        for (int e = 0; e < 16; e++) { s_o[warp][32 * lane + 2 * e] = o[e]; s_o[warp][32 * lane + 2 * e + 1] = o2[e]; }
+    for (int d = 1; d < 32; d <<= 1) {
+        const uint32_t o = __shfl_up_sync(0xffffffffu, inc, d);
+        if (lane >= d) inc += o;
+    }
+    if (lane == 31) ms.warp_sum[warp] = inc;
+    if (tid == 0) {
+        ms.first = p.n_seqs;
+        ms.first_base = 0;
+        for (int i = 0; i < 2; i++) {
+            bar_init(smem_u32(&ms.kv_full[i]), 1);
+            bar_init(smem_u32(&ms.kv_empty[i]), 1);
+            bar_init(smem_u32(&ms.s_full[i]), 1);
+            bar_init(smem_u32(&ms.s_empty[i]), 4);
+        }
+        bar_init(smem_u32(&ms.q_full), 1);
+        bar_init(smem_u32(&ms.q_empty), 1);
+        bar_init(smem_u32(&ms.p_full), 4);
+        bar_init(smem_u32(&ms.p_empty), 1);
+        bar_init(smem_u32(&ms.o_free), 4);
+        bar_init(smem_u32(&ms.drain), 1);
+        bar_init_fence();
+    }
     __syncthreads();
-    float mm = -INFINITY, ll = 0.0f;
-    for (int w = 0; w < 8; w++) mm = fmaxf(mm, s_m[w]);
-    for (int w = 0; w < 8; w++) ll += s_l[w] != 0.0f ? s_l[w] * expf(s_m[w] - mm) : 0.0f;
-    for (int d = tid; d < kLatentValueDim; d += 256) {
-        float acc = 0.0f;
-        for (int w = 0; w < 8; w++) if (s_l[w] != 0.0f) acc += s_o[w][d] * expf(s_m[w] - mm);
-        out[((size_t)i * c.n_q + head) * kLatentValueDim + d] = __float2bfloat16_rn(ll != 0.0f ? acc / ll : 0.0f);
+    uint32_t at = inc - sum, total = 0;
+#pragma unroll
+    for (int w = 0; w < kDecThreads / 32; w++) {
+        if (w < warp) at += ms.warp_sum[w];
+        total += ms.warp_sum[w];
     }
-    if (tid == 0 && lse) lse[(size_t)i * c.n_q + head] = ll != 0.0f ? mm + logf(ll) : -INFINITY;
+    const uint32_t lo = slot_start(total, slot, p.slots), hi = slot_start(total, slot + 1, p.slots);
+#pragma unroll
+    for (int r = 0; r < kPer; r++) {
+        const int s = tid * kPer + r;
+        if (s <= p.n_seqs && blockIdx.x == 0) p.prefix[s] = at;
+        if (s < p.n_seqs && at <= lo && lo < at + cost[r]) { ms.first = s; ms.first_base = at; }
+        at += cost[r];
+    }
+    if (lo >= hi) return;                          // nothing for this CTA
+    if (warp == 9) tmem_alloc(smem_u32(&ms.tmem), 512);
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = ms.tmem;
+    constexpr uint32_t kO = 128;                   // columns: S tiles at 0 and 64, O blocks from 128
+    const int first = ms.first;
+    const uint32_t first_base = ms.first_base;
+    const uint32_t kv0 = smem_u32(sm), qs = smem_u32(sm + Sm::kQ), ps = smem_u32(sm + Sm::kP);
+    const long long limit = p.wait_cycles;
+    TileWalk w;
+    bool more = w.begin(p, first, first_base, lo, hi), ok = true;
+
+    if (warp == 8) {
+        // ================================================= HIGH tiles
+        TileWalk ahead = w;
+        bool ahead_more = more;
+        uint32_t copied = 0, phase[2] = {0, 0};    // stages that were ever copied into, and the phase of the last copy
+        auto prefetch = [&]() {
+            if (!ahead_more) return;
+            if ((uint32_t)lane < ahead.pages) {
+                if (ahead.high) bulk_prefetch(p.c.pool_high + (size_t)ahead.page(lane) * kLatentHighPageBytes, kLatentHighPageBytes);
+                else bulk_prefetch(p.c.pool_low + (size_t)ahead.page(lane) * p.c.low_page_bytes, p.c.low_page_bytes);
+            }
+            ahead_more = ahead.next();
+        };
+        for (uint32_t i = 0; more; i++, more = w.next()) {
+            if (i == 0) for (int k = 0; k < kPrefetch; k++) prefetch();
+            const uint32_t st = i & 1, full = smem_u32(&ms.kv_full[st]);
+            const uint32_t id = w.high && (uint32_t)lane < w.pages ? w.page(lane) : 0u;
+            // (both producers wait for every tile's stage, their own or not: a phase's parity only tells it from its neighbours)
+            ok = __all_sync(0xffffffffu, i < 2 || bar_wait(smem_u32(&ms.kv_empty[st]), ((i >> 1) - 1) & 1, limit));
+            if (!ok) break;
+            if (w.high) {
+                copied |= 1u << st;
+                if (st) phase[1] = (i >> 1) & 1; else phase[0] = (i >> 1) & 1;
+                if (lane == 0) bar_expect(full, w.pages * kLatentHighPageBytes + (i == 0 ? p.surplus : 0u));
+                __syncwarp();
+                if ((uint32_t)lane < w.pages)
+                    bulk_load(kv0 + st * kTileBytes + lane * kLatentHighPageBytes, p.c.pool_high + (size_t)id * kLatentHighPageBytes,
+                              kLatentHighPageBytes, full);
+            }
+            prefetch();
+        }
+        if (!ok || p.surplus) {                    // gave up: let the copies in flight land (bounded) before the CTA ends
+            if (copied & 1u) bar_wait(smem_u32(&ms.kv_full[0]), phase[0], limit);
+            if (copied & 2u) bar_wait(smem_u32(&ms.kv_full[1]), phase[1], limit);
+        }
+    } else if (warp == 9) {
+        // ================================================= products
+        if (lane == 0) {
+            constexpr uint32_t kIdS = instr(kTile, kHeads, false, false), kIdO = instr(128, kHeads, true, true);
+            uint32_t n_seg = 0, prev_pages = 0;
+            bool prev_first = false, have_prev = false;
+            uint32_t i = 0;
+            for (; more || have_prev; i++) {
+                const uint32_t st = i & 1;
+                if (more) {
+                    if (w.first()) { n_seg++; ok = ok && bar_wait(smem_u32(&ms.q_full), (n_seg - 1) & 1, limit); }
+                    ok = ok && bar_wait(smem_u32(&ms.kv_full[st]), (i >> 1) & 1, limit);
+                    ok = ok && (i < 2 || bar_wait(smem_u32(&ms.s_empty[st]), ((i >> 1) - 1) & 1, limit));
+                    if (!ok) break;
+                    fence_after();
+                    const uint32_t kv = kv0 + st * kTileBytes;
+#pragma unroll
+                    for (int k = 0; k < kLatentDim / 16; k++) {
+                        const uint32_t off = (k >> 2) * 1024 + (k & 3) * 32;
+                        mma_ss(tmem + st * 64, desc(kv + off, 0, kLatentHalfPage), desc(qs + off, 0, kLatentHalfPage), kIdS, k > 0);
+                    }
+                    commit(smem_u32(&ms.s_full[st]));
+                    if (w.last()) commit(smem_u32(&ms.q_empty));
+                }
+                if (have_prev) {
+                    ok = ok && bar_wait(smem_u32(&ms.p_full), (i - 1) & 1, limit);
+                    // the segment before has been read out of O
+                    const uint32_t seg = n_seg - (more && w.first() ? 1u : 0u);          // segments up to the previous tile's
+                    ok = ok && (!prev_first || seg < 2 || bar_wait(smem_u32(&ms.o_free), (seg - 2) & 1, limit));
+                    if (!ok) break;
+                    fence_after();
+                    const uint32_t kv = kv0 + (st ^ 1) * kTileBytes;
+                    for (uint32_t k = 0; k < prev_pages; k++) {
+#pragma unroll
+                        for (int b = 0; b < 4; b++)
+                            mma_ss(tmem + kO + b * 64, desc(kv + k * kLatentHighPageBytes + b * 2048, 1024, kLatentHalfPage),
+                                   desc(ps + k * 2048, 0, 1024), kIdO, !(prev_first && k == 0));
+                    }
+                    commit(smem_u32(&ms.kv_empty[st ^ 1]));
+                    commit(smem_u32(&ms.p_empty));
+                }
+                have_prev = more;
+                if (more) {
+                    prev_pages = w.pages;
+                    prev_first = w.first();
+                    more = w.next();
+                }
+            }
+            if (!ok) {                             // gave up: the products in flight end before tensor memory is freed
+                commit(smem_u32(&ms.drain));
+                bar_wait(smem_u32(&ms.drain), 0, limit);
+            }
+        }
+        __syncwarp();
+    } else if (warp >= 4) {
+        // ================================================= queries and LOW tiles
+        const int t = tid - 128;                   // 0..127: token t & 15, (page, group) pairs t >> 4 + 8 k
+        constexpr int kItems = kTilePages * kLatentGroups / 8;
+        uint32_t codes[kItems][BITS], scales[kItems];
+        TileWalk ahead = w;                        // the next LOW tile, whose codes are in the registers
+        bool have = more;
+        auto fetch = [&]() {                       // codes of the tile `ahead` stands on
+            uint32_t ids[kTilePages];
+#pragma unroll
+            for (int pg = 0; pg < kTilePages; pg++) ids[pg] = (uint32_t)pg < ahead.pages ? ahead.page(pg) : 0u;
+#pragma unroll
+            for (int k = 0; k < kItems; k++) {
+                const int pair = 8 * k + (t >> 4), pg = pair / kLatentGroups, g = pair % kLatentGroups;
+                if ((uint32_t)pg < ahead.pages) {
+                    const uint32_t id = pg == 0 ? ids[0] : pg == 1 ? ids[1] : pg == 2 ? ids[2] : ids[3];
+                    const uint8_t *src = p.c.pool_low + (size_t)id * p.c.low_page_bytes;
+                    load_codes<BITS>(src, t & 15, g, codes[k]);
+                    scales[k] = *reinterpret_cast<const uint16_t *>(src + latent_scale_off(t & 15, g, BITS));
+                }
+            }
+        };
+        while (have && ahead.high) have = ahead.next();
+        if (have) fetch();
+        uint32_t n_seg = 0;
+        bool bad = false;
+        for (uint32_t i = 0; more; i++, more = w.next()) {
+            const uint32_t st = i & 1;
+            if (w.first()) {
+                if (n_seg > 0) ok = bar_wait(smem_u32(&ms.q_empty), (n_seg - 1) & 1, ok ? limit : 0) && ok;
+                n_seg++;
+                const uint4 *src = p.q + ((size_t)w.s * p.c.n_q + h0) * kLatentChunks;
+                constexpr int kIter = kHeads * kLatentChunks / 128;
+#pragma unroll 12
+                for (int k = 0; k < kIter; k++) {
+                    const int x = k * 128 + t, row = x / kLatentChunks, ch = x % kLatentChunks;
+                    const uint4 v = row < nh_here ? src[x] : make_uint4(0, 0, 0, 0);
+                    *reinterpret_cast<uint4 *>(sm + Sm::kQ + (row >> 4) * kLatentHighPageBytes + latent_chunk_off(row & 15, ch)) = v;
+                }
+                fence_async_shared();
+                bad = group_any(2, 128, !ok);
+                if (bad) break;
+                if (t == 0) bar_arrive(smem_u32(&ms.q_full));
+            }
+            if (i >= 2) ok = bar_wait(smem_u32(&ms.kv_empty[st]), ((i >> 1) - 1) & 1, ok ? limit : 0) && ok;
+            if (!w.high) {
+                uint8_t *dst = sm + st * kTileBytes;
+#pragma unroll
+                for (int k = 0; k < kItems; k++) {
+                    const int pair = 8 * k + (t >> 4), pg = pair / kLatentGroups, g = pair % kLatentGroups;
+                    if ((uint32_t)pg < w.pages) {
+                        uint32_t xs[16];
+                        dequantise_group<BITS>(codes[k], scales[k], xs);
+#pragma unroll
+                        for (int e = 0; e < 4; e++)
+                            *reinterpret_cast<uint4 *>(dst + pg * kLatentHighPageBytes + latent_chunk_off(t & 15, 4 * g + e)) =
+                                make_uint4(xs[4 * e], xs[4 * e + 1], xs[4 * e + 2], xs[4 * e + 3]);
+                    }
+                }
+                fence_async_shared();
+                bad = group_any(2, 128, !ok);
+                if (bad) break;
+                if (t == 0) bar_arrive(smem_u32(&ms.kv_full[st]));
+                do have = ahead.next(); while (have && ahead.high);
+                if (have) fetch();
+            }
+        }
+    } else {
+        // ================================================= softmax; warp = page of the tile, rows lane / 4 and lane / 4 + 8
+        constexpr int kJ = kHeads / 8;             // blocks of 8 heads; this lane's heads: 8 j + 2 (lane % 4) + {0, 1}
+        float m[2 * kJ], l[2 * kJ];
+        uint32_t n_seg = 0;
+        const int r0 = lane >> 2, hc = 2 * (lane & 3);
+        const uint32_t row16 = (uint32_t)(lane & 7), p_row = ps + (2 * warp + ((lane >> 3) & 1)) * 1024 + row16 * 128;
+        const uint32_t lanes = (uint32_t)(warp * 32) << 16;
+        bool bad = false;
+        for (uint32_t i = 0; more; i++) {
+            const uint32_t st = i & 1;
+            const bool is_first = w.first(), is_last = w.last();
+            ok = bar_wait(smem_u32(&ms.s_full[st]), (i >> 1) & 1, ok ? limit : 0) && ok;
+            __syncwarp();
+            fence_after();
+            uint32_t sr[4 * kJ];
+            tmem_ld_frag(tmem + lanes + st * 64, sr);
+            tmem_wait_ld();
+            fence_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive(smem_u32(&ms.s_empty[st]));
+            const int vp = (int)w.valid - 16 * warp;
+            const bool ok0 = r0 < vp, ok1 = r0 + 8 < vp;
+            float x[4 * kJ];
+#pragma unroll
+            for (int j = 0; j < kJ; j++)
+#pragma unroll
+                for (int e = 0; e < 4; e++)
+                    x[4 * j + e] = (e < 2 ? ok0 : ok1) ? __uint_as_float(sr[4 * j + e]) * p.scale_log2 : -INFINITY;
+            bool over = is_first;
+            if (!is_first) {
+                float top = -INFINITY;
+#pragma unroll
+                for (int j = 0; j < kJ; j++)
+#pragma unroll
+                    for (int e = 0; e < 2; e++) top = fmaxf(top, fmaxf(x[4 * j + e], x[4 * j + 2 + e]) - m[2 * j + e]);
+                over = top > kLazy;
+            }
+            if (group_any(1, 128, over || !ok)) {
+                bad = group_any(1, 128, !ok);
+                if (bad) break;
+                // a new reference maximum for the heads that need one
+                float top[2 * kJ];
+#pragma unroll
+                for (int j = 0; j < kJ; j++)
+#pragma unroll
+                    for (int e = 0; e < 2; e++) {
+                        float a = fmaxf(x[4 * j + e], x[4 * j + 2 + e]);
+                        a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 4));
+                        a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 8));
+                        top[2 * j + e] = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 16));
+                    }
+                if (lane < 4)
+#pragma unroll
+                    for (int j = 0; j < kJ; j++)
+#pragma unroll
+                        for (int e = 0; e < 2; e++) ms.red[warp][8 * j + hc + e] = top[2 * j + e];
+                group_sync(1, 128);
+#pragma unroll
+                for (int j = 0; j < kJ; j++)
+#pragma unroll
+                    for (int e = 0; e < 2; e++) {
+                        const int h = 8 * j + hc + e, k = 2 * j + e;
+                        const float a = fmaxf(fmaxf(ms.red[0][h], ms.red[1][h]), fmaxf(ms.red[2][h], ms.red[3][h]));
+                        float f = 1.0f;
+                        if (is_first) {
+                            m[k] = a;
+                            l[k] = 0.0f;
+                        } else if (a - m[k] > kLazy) {
+                            f = ex2(m[k] - a);
+                            l[k] *= f;
+                            m[k] = a;
+                        }
+                        if (warp == 0 && lane < 4) ms.fac[h] = f;
+                    }
+                group_sync(1, 128);
+                if (!is_first) {                   // O so far, in the new reference
+                    ok = bar_wait(smem_u32(&ms.p_empty), (i - 1) & 1, ok ? limit : 0) && ok;
+                    __syncwarp();
+                    fence_after();
+#pragma unroll 1
+                    for (int b = 0; b < 4; b++)
+#pragma unroll
+                        for (int cc = 0; cc < kHeads; cc += 16) {
+                            uint32_t o[16];
+                            tmem_ld16(tmem + lanes + kO + b * 64 + cc, o);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int e = 0; e < 16; e++) o[e] = __float_as_uint(__uint_as_float(o[e]) * ms.fac[cc + e]);
+                            tmem_st16(tmem + lanes + kO + b * 64 + cc, o);
+                        }
+                    tmem_wait_st();
+                    fence_before();
+                }
+            }
+            uint32_t pk[2 * kJ];                   // weights as pairs of heads: row 0 in [2j], row 1 in [2j + 1]
+#pragma unroll
+            for (int j = 0; j < kJ; j++) {
+                float e4[4];
+#pragma unroll
+                for (int e = 0; e < 4; e++) e4[e] = (e < 2 ? ok0 : ok1) ? ex2(x[4 * j + e] - m[2 * j + (e & 1)]) : 0.0f;
+                l[2 * j] += e4[0] + e4[2];
+                l[2 * j + 1] += e4[1] + e4[3];
+                pk[2 * j] = pack_bf16(e4[0], e4[1]);
+                pk[2 * j + 1] = pack_bf16(e4[2], e4[3]);
+            }
+            if (i > 0) ok = bar_wait(smem_u32(&ms.p_empty), (i - 1) & 1, ok ? limit : 0) && ok;     // P is free
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < kJ; j += 2)
+                stmatrix4(p_row + ((((uint32_t)j + (uint32_t)(lane >> 4)) ^ row16) << 4), pk[2 * j], pk[2 * j + 1], pk[2 * j + 2], pk[2 * j + 3]);
+            fence_async_shared();
+            fence_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive(smem_u32(&ms.p_full));
+            if (is_last) {
+                // ---- the sequence's share ends: sums over the rows, then O out of tensor memory
+#pragma unroll
+                for (int k = 0; k < 2 * kJ; k++) {
+                    l[k] += __shfl_xor_sync(0xffffffffu, l[k], 4);
+                    l[k] += __shfl_xor_sync(0xffffffffu, l[k], 8);
+                    l[k] += __shfl_xor_sync(0xffffffffu, l[k], 16);
+                }
+                group_sync(1, 128);                // everyone is done with red and fac
+                if (lane < 4)
+#pragma unroll
+                    for (int j = 0; j < kJ; j++)
+#pragma unroll
+                        for (int e = 0; e < 2; e++) {
+                            ms.red[warp][8 * j + hc + e] = l[2 * j + e];
+                            if (warp == 0) ms.mref[8 * j + hc + e] = m[2 * j + e];
+                        }
+                group_sync(1, 128);
+                const bool whole = w.whole();
+                const size_t row0 = (whole ? (size_t)w.s : (size_t)slot + w.s) * p.c.n_q + h0;
+                if (tid < kHeads) {
+                    const float ls = (ms.red[0][tid] + ms.red[1][tid]) + (ms.red[2][tid] + ms.red[3][tid]);
+                    ms.fac[tid] = whole ? 1.0f / ls : 1.0f;
+                    if (tid < nh_here) {
+                        if (!whole) p.part_ml[row0 + tid] = make_float2(ms.mref[tid], ls);
+                        else if (p.lse) p.lse[row0 + tid] = (ms.mref[tid] + log2f(ls)) * 0.69314718055994531f;
+                    }
+                }
+                group_sync(1, 128);
+                ok = bar_wait(smem_u32(&ms.p_empty), i & 1, ok ? limit : 0) && ok;
+                __syncwarp();
+                fence_after();
+#pragma unroll 1
+                for (int b = 0; b < 4; b++)
+#pragma unroll
+                    for (int cc = 0; cc < kHeads; cc += 16) {
+                        uint32_t o[16];
+                        tmem_ld16(tmem + lanes + kO + b * 64 + cc, o);
+                        tmem_wait_ld();
+                        const int dim = 128 * b + 32 * warp + lane;
+                        if (whole) {
+#pragma unroll
+                            for (int e = 0; e < 16; e++)
+                                if (cc + e < nh_here)
+                                    p.out[(row0 + cc + e) * kLatentValueDim + dim] = __float2bfloat16_rn(__uint_as_float(o[e]) * ms.fac[cc + e]);
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 16; e++)
+                                if (cc + e < nh_here) p.part_o[(row0 + cc + e) * kLatentValueDim + dim] = __uint_as_float(o[e]);
+                        }
+                    }
+                fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(smem_u32(&ms.o_free));
+            }
+            more = w.next();
+        }
+    }
+    if (!ok) atomicOr(&p.c.ctrl[kCtrlStatus], PASK_DEV_TIMEOUT);
+    fence_before();
+    __syncthreads();
+    fence_after();
+    if (warp == 9) tmem_free(tmem, 512);
+    if (p.span && tid == 0) {
+        unsigned long long t_end;
+        asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t_end));
+        atomicMin(p.span, t_start);
+        atomicMax(p.span + 1, t_end);
+    }
+}
+
+// Joins the partial sums of one (sequence, head): CTA = row, kSplit groups of 128 threads take every kSplit-th partial, a
+// thread has four of the 512 dims.  Sequences that one share covered are left alone; empty ones are written here.
+template <int kSplit>
+__global__ void __launch_bounds__(128 * kSplit)
+decode_latent_merge(int n_seqs, int n_q, uint32_t slots, const uint32_t *__restrict__ prefix, const int32_t *__restrict__ seq_ids,
+                    DevCache c, int layer, const float2 *__restrict__ part_ml, const float *__restrict__ part_o,
+                    __nv_bfloat16 *__restrict__ out, float *__restrict__ lse) {
+    __shared__ float s_w[kMaxSlots], s_red[4 * kSplit], s_l[4 * kSplit];
+    __shared__ float4 s_o[kSplit > 1 ? (kSplit - 1) * 128 : 1];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int s = blockIdx.x / n_q, h = blockIdx.x % n_q;
+    pdl_launch_dependents();
+    pdl_wait();
+    const uint32_t base = prefix[s], cost = prefix[s + 1] - base, total = prefix[n_seqs];
+    const size_t row = (size_t)s * n_q + h;
+    if (cost == 0) {
+        for (int d = tid; d < kLatentValueDim / 8; d += 128 * kSplit)
+            reinterpret_cast<uint4 *>(out)[row * (kLatentValueDim / 8) + d] = make_uint4(0, 0, 0, 0);
+        if (tid == 0 && lse) lse[row] = -INFINITY;
+        return;
+    }
+    const size_t sl = (size_t)seq_ids[s] * c.n_layers + layer;
+    const uint32_t n = tiles_of(c.n_high[sl]) + tiles_of(c.n_low[sl]);
+    uint32_t b0 = (uint32_t)((uint64_t)base * slots / total);
+    while (slot_start(total, b0 + 1, slots) <= base) b0++;
+    uint32_t b1 = b0 + 1;
+    {   // the first share that starts at or behind the sequence's end
+        const uint32_t end = base + cost;
+        b1 = (uint32_t)(((uint64_t)end * slots + total - 1) / total);
+        while (b1 > b0 + 1 && slot_start(total, b1 - 1, slots) >= end) b1--;
+        while (b1 < slots && slot_start(total, b1, slots) < end) b1++;
+    }
+    const uint32_t count = b1 - b0;
+    auto used = [&](uint32_t b) {
+        const uint32_t lo = slot_start(total, b, slots), hi = slot_start(total, b + 1, slots);
+        const uint32_t v0 = lo > base ? cut_positions(lo - base, cost, n) : 0u, v1 = cut_positions(hi - base, cost, n);
+        if (v1 <= v0) return 0;
+        return v0 == 0 && v1 == n ? 2 : 1;
+    };
+    float top = -INFINITY;
+    int whole = 0;
+    for (uint32_t k = tid; k < count; k += 128 * kSplit) {
+        const int u = used(b0 + k);
+        whole |= u == 2;
+        const float m = u ? part_ml[(size_t)(b0 + k + s) * n_q + h].x : -INFINITY;
+        if (u != 2) top = fmaxf(top, m);
+    }
+    if (__syncthreads_or(whole)) return;           // written by the share itself
+#pragma unroll
+    for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+    if (lane == 0) s_red[warp] = top;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 4 * kSplit; k++) top = fmaxf(top, s_red[k]);
+    float lsum = 0.0f;
+    for (uint32_t k = tid; k < count; k += 128 * kSplit) {
+        float wgt = 0.0f;
+        if (used(b0 + k)) {
+            const float2 ml = part_ml[(size_t)(b0 + k + s) * n_q + h];
+            wgt = umma::ex2(ml.x - top);
+            lsum += wgt * ml.y;
+            if (!(ml.y == ml.y)) wgt = ml.y;       // a NaN stays one
+        }
+        s_w[k] = wgt;
+    }
+#pragma unroll
+    for (int d = 16; d; d >>= 1) lsum += __shfl_xor_sync(0xffffffffu, lsum, d);
+    if (lane == 0) s_l[warp] = lsum;
+    __syncthreads();
+    lsum = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 4 * kSplit; k++) lsum += s_l[k];
+    float4 acc = make_float4(0, 0, 0, 0);
+    const int part = tid >> 7, d4 = tid & 127;
+    const float4 *src = reinterpret_cast<const float4 *>(part_o) + ((size_t)(b0 + s) * n_q + h) * (kLatentValueDim / 4) + d4;
+    const size_t step = (size_t)n_q * (kLatentValueDim / 4);
+#pragma unroll 8
+    for (uint32_t k = part; k < count; k += kSplit) {
+        const float wgt = s_w[k];
+        if (wgt != 0.0f) {
+            const float4 v = src[k * step];
+            acc.x += wgt * v.x; acc.y += wgt * v.y; acc.z += wgt * v.z; acc.w += wgt * v.w;
+        }
+    }
+    if (kSplit > 1) {
+        if (part > 0) s_o[(part - 1) * 128 + d4] = acc;
+        __syncthreads();
+        if (part > 0) return;
+#pragma unroll
+        for (int k = 0; k < kSplit - 1; k++) {
+            const float4 v = s_o[k * 128 + d4];
+            acc.x += v.x; acc.y += v.y; acc.z += v.z; acc.w += v.w;
+        }
+    }
+    const float inv = 1.0f / lsum;
+    reinterpret_cast<uint2 *>(out)[row * (kLatentValueDim / 4) + d4] =
+        make_uint2(umma::pack_bf16(acc.x * inv, acc.y * inv), umma::pack_bf16(acc.z * inv, acc.w * inv));
+    if (tid == 0 && lse) lse[row] = (top + log2f(lsum)) * 0.69314718055994531f;
 }
 
 }  // namespace
@@ -384,15 +966,86 @@ pask_status_t launch_read_latent(pask_cache *c, int layer, int n_seqs, int total
     return cudaGetLastError() == cudaSuccess ? PASK_OK : PASK_ERR_CUDA;
 }
 
-size_t latent_workspace_bytes(const pask_cache *c, int n_seqs) { (void)c; (void)n_seqs; return 256; }
+// heads are taken in groups of at most 64, evenly
+static void latent_shares(const pask_cache *c, int *groups, int *heads, uint32_t *slots) {
+    *groups = (c->desc.n_q_heads + 63) / 64;
+    *heads = (c->desc.n_q_heads + *groups - 1) / *groups;
+    const uint32_t n = (uint32_t)(c->attn_ctas / *groups);
+    *slots = n < 1 ? 1 : n > kMaxSlots ? kMaxSlots : n;
+}
+
+static size_t carve_latent(const pask_cache *c, int n_seqs, uint8_t *base, DecParams *p) {
+    int groups, heads;
+    uint32_t slots;
+    latent_shares(c, &groups, &heads, &slots);
+    size_t off = 0;
+    auto take = [&](size_t bytes) { const size_t at = off; off = (off + bytes + 255) / 256 * 256; return at; };
+    const size_t rows = ((size_t)slots + n_seqs) * c->desc.n_q_heads;
+    const size_t o_prefix = take((size_t)(n_seqs + 1) * 4), o_ml = take(rows * sizeof(float2)), o_o = take(rows * kLatentValueDim * sizeof(float));
+    if (p) {
+        p->groups = groups;
+        p->heads = heads;
+        p->slots = slots;
+        p->prefix = reinterpret_cast<uint32_t *>(base + o_prefix);
+        p->part_ml = reinterpret_cast<float2 *>(base + o_ml);
+        p->part_o = reinterpret_cast<float *>(base + o_o);
+    }
+    return off;
+}
+
+size_t latent_workspace_bytes(const pask_cache *c, int n_seqs) { return carve_latent(c, n_seqs, nullptr, nullptr); }
+
+template <int kHeads, int BITS>
+static cudaError_t launch_decode_kernel(const DecParams &p, cudaStream_t stream) {
+    static bool granted[64] = {};                  // the shared-memory opt-in, asked for once per device
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+    constexpr int kSmem = DecSmem<kHeads>::kBytes;
+    static_assert(kSmem <= 232448, "shared memory of a CTA");
+    if (!granted[dev]) {
+        const cudaError_t e = cudaFuncSetAttribute(decode_latent_kernel<kHeads, BITS>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+        if (e != cudaSuccess) return e;
+        granted[dev] = true;
+    }
+    return launch_pdl(decode_latent_kernel<kHeads, BITS>, dim3(p.slots * (uint32_t)p.groups), dim3(kDecThreads), kSmem, stream, p);
+}
+template <int BITS>
+static cudaError_t launch_decode_heads(const DecParams &p, cudaStream_t stream) {
+    return p.heads <= 16 ? launch_decode_kernel<16, BITS>(p, stream) : p.heads <= 32 ? launch_decode_kernel<32, BITS>(p, stream)
+                                                                     : launch_decode_kernel<64, BITS>(p, stream);
+}
 
 pask_status_t launch_decode_latent(pask_cache *c, int layer, int n_seqs, const int32_t *seq_ids, const void *q, float scale,
                                    void *out, float *lse, void *workspace, cudaStream_t stream) {
-    (void)workspace;
-    auto kern = c->dev.low_bits == 8 ? decode_latent_kernel<8> : c->dev.low_bits == 2 ? decode_latent_kernel<2> : decode_latent_kernel<4>;
-    kern<<<dim3(c->desc.n_q_heads, n_seqs), 256, 0, stream>>>(c->dev, layer, seq_ids, static_cast<const __nv_bfloat16 *>(q), scale,
-                                                              static_cast<__nv_bfloat16 *>(out), lse);
-    return cudaGetLastError() == cudaSuccess ? PASK_OK : PASK_ERR_CUDA;
+    DecParams p;
+    carve_latent(c, n_seqs, static_cast<uint8_t *>(workspace), &p);
+    p.c = c->dev;
+    p.layer = layer;
+    p.n_seqs = n_seqs;
+    p.seq_ids = seq_ids;
+    p.q = static_cast<const uint4 *>(q);
+    p.scale_log2 = scale * 1.4426950408889634f;
+    p.out = static_cast<__nv_bfloat16 *>(out);
+    p.lse = lse;
+    p.wait_cycles = c->wait_cycles;
+    p.surplus = c->wait_test_surplus;
+    p.span = c->span;
+    if (c->ev_start) cudaEventRecord(c->ev_start, stream);
+    cudaError_t e = c->dev.low_bits == 8 ? launch_decode_heads<8>(p, stream)
+                  : c->dev.low_bits == 2 ? launch_decode_heads<2>(p, stream) : launch_decode_heads<4>(p, stream);
+    if (c->ev_stop) cudaEventRecord(c->ev_stop, stream);
+    c->ev_start = c->ev_stop = nullptr;
+    c->span = nullptr;
+    if (e != cudaSuccess) return PASK_ERR_CUDA;
+    const int n_q = c->desc.n_q_heads;
+    // few sequences: many partials to a row, so four groups of threads share them (one round trip to L2 brings eight)
+    if (p.slots >= 16u * (uint32_t)n_seqs)
+        e = launch_pdl(decode_latent_merge<4>, dim3(n_seqs * n_q), dim3(512), 0, stream, n_seqs, n_q, p.slots, p.prefix, seq_ids, p.c, layer,
+                       p.part_ml, p.part_o, p.out, lse);
+    else
+        e = launch_pdl(decode_latent_merge<1>, dim3(n_seqs * n_q), dim3(128), 0, stream, n_seqs, n_q, p.slots, p.prefix, seq_ids, p.c, layer,
+                       p.part_ml, p.part_o, p.out, lse);
+    return e == cudaSuccess ? PASK_OK : PASK_ERR_CUDA;
 }
 
 }  // namespace pask
