@@ -315,6 +315,8 @@ constexpr int kDecThreads = 320;
 constexpr uint32_t kMaxSlots = 1024;
 constexpr int kPrefetch = 4;                       // tiles between a prefetch into L2 and the copy
 constexpr uint32_t kCostHighTile = 3, kCostLowTile = 2;
+enum : uint32_t { kInfoFirst = 1, kInfoLast = 2, kInfoWhole = 4, kInfoFinal = 8 };   // first, last tile of a sequence's part; the part
+                                                   // is the whole sequence; last tile of the share
 constexpr float kLazy = 8.0f;                      // log2 of how far a score may exceed the reference maximum
 
 struct DecParams {
@@ -403,6 +405,7 @@ struct DecSmem {
     static constexpr int kQ = 2 * kTileBytes, kP = kQ + kHeads * 1152, kMisc = kP + kTile * 128;
     struct Misc {
         uint64_t kv_full[2], kv_empty[2], s_full[2], s_empty[2], q_full, q_empty, p_full, p_empty, o_free, drain;
+        uint4 info[2];                             // of the tile whose S a stage holds: valid rows, flags, sequence
         uint32_t tmem;
         int first;
         uint32_t first_base, total;
@@ -459,7 +462,7 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
         for (int i = 0; i < 2; i++) {
             bar_init(smem_u32(&ms.kv_full[i]), 1);
             bar_init(smem_u32(&ms.kv_empty[i]), 1);
-            bar_init(smem_u32(&ms.s_full[i]), 1);
+            bar_init(smem_u32(&ms.s_full[i]), 2);
             bar_init(smem_u32(&ms.s_empty[i]), 4);
         }
         bar_init(smem_u32(&ms.q_full), 1);
@@ -536,56 +539,86 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
         }
     } else if (warp == 9) {
         // ================================================= products
-        if (lane == 0) {
-            constexpr uint32_t kIdS = instr(kTile, kHeads, false, false), kIdO = instr(128, kHeads, true, true);
-            uint32_t n_seg = 0, prev_pages = 0;
-            bool prev_first = false, have_prev = false;
-            uint32_t i = 0;
-            for (; more || have_prev; i++) {
-                const uint32_t st = i & 1;
-                if (more) {
-                    if (w.first()) { n_seg++; ok = ok && bar_wait(smem_u32(&ms.q_full), (n_seg - 1) & 1, limit); }
-                    ok = ok && bar_wait(smem_u32(&ms.kv_full[st]), (i >> 1) & 1, limit);
-                    ok = ok && (i < 2 || bar_wait(smem_u32(&ms.s_empty[st]), ((i >> 1) - 1) & 1, limit));
-                    if (!ok) break;
-                    fence_after();
-                    const uint32_t kv = kv0 + st * kTileBytes;
-#pragma unroll
-                    for (int k = 0; k < kLatentDim / 16; k++) {
-                        const uint32_t off = (k >> 2) * 1024 + (k & 3) * 32;
-                        mma_ss(tmem + st * 64, desc(kv + off, 0, kLatentHalfPage), desc(qs + off, 0, kLatentHalfPage), kIdS, k > 0);
-                    }
-                    commit(smem_u32(&ms.s_full[st]));
-                    if (w.last()) commit(smem_u32(&ms.q_empty));
+        constexpr uint32_t kIdS = instr(kTile, kHeads, false, false), kIdO = instr(128, kHeads, true, true);
+        const bool mine = elect_one();
+        uint32_t n_seg = 0, i = 0, j = 0;          // tiles whose S, whose O product has been issued (j <= i <= j + 1)
+        uint32_t pv_pages = 0, pv_seg = 0, next_pages = 0, next_seg = 0;
+        bool pv_first = false, next_first = false;
+        while (more || j < i) {
+            const uint32_t st = __shfl_sync(0xffffffffu, i & 1, 0);
+            bool qk = more;
+            if (more && j < i) {                   // whichever can go: the next tile's S, or O of the one before
+                const long long t0 = clock64();
+                int pick = 0;
+                while (!pick) {
+                    pick = bar_test(smem_u32(&ms.kv_full[st]), (i >> 1) & 1) ? 1 : bar_test(smem_u32(&ms.p_full), j & 1) ? 2 : 0;
+                    if (!pick && clock64() - t0 > limit) pick = 3;
+                    pick = __shfl_sync(0xffffffffu, pick, 0);
                 }
-                if (have_prev) {
-                    ok = ok && bar_wait(smem_u32(&ms.p_full), (i - 1) & 1, limit);
-                    // the segment before has been read out of O
-                    const uint32_t seg = n_seg - (more && w.first() ? 1u : 0u);          // segments up to the previous tile's
-                    ok = ok && (!prev_first || seg < 2 || bar_wait(smem_u32(&ms.o_free), (seg - 2) & 1, limit));
-                    if (!ok) break;
-                    fence_after();
-                    const uint32_t kv = kv0 + (st ^ 1) * kTileBytes;
-                    for (uint32_t k = 0; k < prev_pages; k++) {
+                if (pick == 3) { ok = false; break; }
+                qk = pick == 1;
+            }
+            if (qk) {
+                const bool is_first = w.first();
+                if (is_first) { n_seg++; ok = ok && bar_wait(smem_u32(&ms.q_full), (n_seg - 1) & 1, limit); }
+                ok = ok && bar_wait(smem_u32(&ms.kv_full[st]), (i >> 1) & 1, limit);
+                ok = ok && (i < 2 || bar_wait(smem_u32(&ms.s_empty[st]), ((i >> 1) - 1) & 1, limit));
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                fence_after();
+                const uint32_t kv = kv0 + st * kTileBytes;
+                const uint64_t dk = desc(kv, 0, kLatentHalfPage), dq = desc(qs, 0, kLatentHalfPage);
+#pragma unroll
+                for (int k = 0; k < kLatentDim / 16; k++) {
+                    const uint64_t off = (uint64_t)(((k >> 2) * 1024 + (k & 3) * 32) >> 4);
+                    mma_ss(tmem + st * 64, dk + off, dq + off, kIdS, k > 0, mine);
+                }
+                const bool is_last = w.last();
+                if (mine) {
+                    commit(smem_u32(&ms.s_full[st]));
+                    if (is_last) commit(smem_u32(&ms.q_empty));
+                }
+                const uint32_t valid = w.valid, flags = (is_first ? kInfoFirst : 0u) | (is_last ? kInfoLast : 0u) | (w.whole() ? kInfoWhole : 0u);
+                const uint32_t seq = (uint32_t)w.s;
+                const uint32_t now_pages = w.pages;
+                more = w.next();
+                if (mine) {
+                    ms.info[st] = make_uint4(valid, flags | (more ? 0u : kInfoFinal), seq, 0);
+                    bar_arrive(smem_u32(&ms.s_full[st]));
+                }
+                i++;
+                if (i == j + 1) { pv_pages = now_pages; pv_seg = n_seg; pv_first = is_first; }
+                else { next_pages = now_pages; next_seg = n_seg; next_first = is_first; }
+            }
+            if (j + 1 < i || !more || !qk) {
+                ok = ok && bar_wait(smem_u32(&ms.p_full), j & 1, limit);
+                // the segment before has been read out of O
+                ok = ok && (!pv_first || pv_seg < 2 || bar_wait(smem_u32(&ms.o_free), (pv_seg - 2) & 1, limit));
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                fence_after();
+                const uint32_t sv = __shfl_sync(0xffffffffu, j & 1, 0), np = __shfl_sync(0xffffffffu, pv_pages, 0);
+                const bool fresh = __shfl_sync(0xffffffffu, (int)pv_first, 0) != 0;
+                const uint64_t dv = desc(kv0 + sv * kTileBytes, 1024, kLatentHalfPage), dp = desc(ps, 0, 1024);
+#pragma unroll
+                for (int k = 0; k < kTilePages; k++)
+                    if ((uint32_t)k < np) {
 #pragma unroll
                         for (int b = 0; b < 4; b++)
-                            mma_ss(tmem + kO + b * 64, desc(kv + k * kLatentHighPageBytes + b * 2048, 1024, kLatentHalfPage),
-                                   desc(ps + k * 2048, 0, 1024), kIdO, !(prev_first && k == 0));
+                            mma_ss(tmem + kO + b * 64, dv + (uint64_t)((k * kLatentHighPageBytes + b * 2048) >> 4), dp + (uint64_t)(k * 2048 >> 4),
+                                   kIdO, k > 0 || !fresh, mine);
                     }
-                    commit(smem_u32(&ms.kv_empty[st ^ 1]));
+                if (mine) {
+                    commit(smem_u32(&ms.kv_empty[sv]));
                     commit(smem_u32(&ms.p_empty));
                 }
-                have_prev = more;
-                if (more) {
-                    prev_pages = w.pages;
-                    prev_first = w.first();
-                    more = w.next();
-                }
+                j++;
+                if (j < i) { pv_pages = next_pages; pv_seg = next_seg; pv_first = next_first; }
             }
-            if (!ok) {                             // gave up: the products in flight end before tensor memory is freed
-                commit(smem_u32(&ms.drain));
-                bar_wait(smem_u32(&ms.drain), 0, limit);
-            }
+        }
+        if (!ok) {                                 // gave up: the products in flight end before tensor memory is freed
+            if (mine) commit(smem_u32(&ms.drain));
+            bar_wait(smem_u32(&ms.drain), 0, limit);
         }
         __syncwarp();
     } else if (warp >= 4) {
@@ -658,46 +691,49 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
     } else {
         // ================================================= softmax; warp = page of the tile, rows lane / 4 and lane / 4 + 8
         constexpr int kJ = kHeads / 8;             // blocks of 8 heads; this lane's heads: 8 j + 2 (lane % 4) + {0, 1}
-        float m[2 * kJ], l[2 * kJ];
-        uint32_t n_seg = 0;
+        float l[2 * kJ];                           // sums of this lane's rows; the reference maxima are in ms.mref
         const int r0 = lane >> 2, hc = 2 * (lane & 3);
-        const uint32_t row16 = (uint32_t)(lane & 7), p_row = ps + (2 * warp + ((lane >> 3) & 1)) * 1024 + row16 * 128;
+        const uint32_t row8 = (uint32_t)(lane & 7), p_row = ps + (2 * warp + ((lane >> 3) & 1)) * 1024 + row8 * 128;
         const uint32_t lanes = (uint32_t)(warp * 32) << 16;
-        bool bad = false;
+#pragma unroll
+        for (int k = 0; k < 2 * kJ; k++) l[k] = 0.0f;
         for (uint32_t i = 0; more; i++) {
             const uint32_t st = i & 1;
-            const bool is_first = w.first(), is_last = w.last();
             ok = bar_wait(smem_u32(&ms.s_full[st]), (i >> 1) & 1, ok ? limit : 0) && ok;
             __syncwarp();
             fence_after();
-            uint32_t sr[4 * kJ];
-            tmem_ld_frag(tmem + lanes + st * 64, sr);
-            tmem_wait_ld();
+            const uint4 info = ms.info[st];
+            const bool is_first = info.y & kInfoFirst;
+            float x[4 * kJ];
+            {
+                uint32_t sr[4 * kJ];
+                tmem_ld_frag(tmem + lanes + st * 64, sr);
+                tmem_wait_ld();
+#pragma unroll
+                for (int k = 0; k < 4 * kJ; k++) x[k] = __uint_as_float(sr[k]) * p.scale_log2;
+            }
             fence_before();
             __syncwarp();
             if (lane == 0) bar_arrive(smem_u32(&ms.s_empty[st]));
-            const int vp = (int)w.valid - 16 * warp;
-            const bool ok0 = r0 < vp, ok1 = r0 + 8 < vp;
-            float x[4 * kJ];
+            const int vp = (int)info.x - 16 * warp;
+            if (vp < 16) {                         // rows behind the stream's end
 #pragma unroll
-            for (int j = 0; j < kJ; j++)
-#pragma unroll
-                for (int e = 0; e < 4; e++)
-                    x[4 * j + e] = (e < 2 ? ok0 : ok1) ? __uint_as_float(sr[4 * j + e]) * p.scale_log2 : -INFINITY;
+                for (int k = 0; k < 4 * kJ; k++)
+                    if (!((k & 2) ? r0 + 8 < vp : r0 < vp)) x[k] = -INFINITY;
+            }
             bool over = is_first;
             if (!is_first) {
                 float top = -INFINITY;
 #pragma unroll
-                for (int j = 0; j < kJ; j++)
-#pragma unroll
-                    for (int e = 0; e < 2; e++) top = fmaxf(top, fmaxf(x[4 * j + e], x[4 * j + 2 + e]) - m[2 * j + e]);
+                for (int j = 0; j < kJ; j++) {
+                    const float2 m = *reinterpret_cast<const float2 *>(&ms.mref[8 * j + hc]);
+                    top = fmaxf(top, fmaxf(fmaxf(x[4 * j], x[4 * j + 2]) - m.x, fmaxf(x[4 * j + 1], x[4 * j + 3]) - m.y));
+                }
                 over = top > kLazy;
             }
             if (group_any(1, 128, over || !ok)) {
-                bad = group_any(1, 128, !ok);
-                if (bad) break;
+                if (group_any(1, 128, !ok)) break;
                 // a new reference maximum for the heads that need one
-                float top[2 * kJ];
 #pragma unroll
                 for (int j = 0; j < kJ; j++)
 #pragma unroll
@@ -705,39 +741,31 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
                         float a = fmaxf(x[4 * j + e], x[4 * j + 2 + e]);
                         a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 4));
                         a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 8));
-                        top[2 * j + e] = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 16));
-                    }
-                if (lane < 4)
-#pragma unroll
-                    for (int j = 0; j < kJ; j++)
-#pragma unroll
-                        for (int e = 0; e < 2; e++) ms.red[warp][8 * j + hc + e] = top[2 * j + e];
-                group_sync(1, 128);
-#pragma unroll
-                for (int j = 0; j < kJ; j++)
-#pragma unroll
-                    for (int e = 0; e < 2; e++) {
-                        const int h = 8 * j + hc + e, k = 2 * j + e;
-                        const float a = fmaxf(fmaxf(ms.red[0][h], ms.red[1][h]), fmaxf(ms.red[2][h], ms.red[3][h]));
-                        float f = 1.0f;
-                        if (is_first) {
-                            m[k] = a;
-                            l[k] = 0.0f;
-                        } else if (a - m[k] > kLazy) {
-                            f = ex2(m[k] - a);
-                            l[k] *= f;
-                            m[k] = a;
-                        }
-                        if (warp == 0 && lane < 4) ms.fac[h] = f;
+                        a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 16));
+                        if (lane < 4) ms.red[warp][8 * j + hc + e] = a;
                     }
                 group_sync(1, 128);
+                if (tid < kHeads) {
+                    const float a = fmaxf(fmaxf(ms.red[0][tid], ms.red[1][tid]), fmaxf(ms.red[2][tid], ms.red[3][tid]));
+                    const float m = ms.mref[tid];
+                    const bool raise = is_first || a - m > kLazy;
+                    ms.fac[tid] = is_first ? 0.0f : raise ? ex2(m - a) : 1.0f;
+                    if (raise) ms.mref[tid] = a;
+                }
+                group_sync(1, 128);
+#pragma unroll
+                for (int j = 0; j < kJ; j++) {
+                    const float2 f = *reinterpret_cast<const float2 *>(&ms.fac[8 * j + hc]);
+                    l[2 * j] = is_first ? 0.0f : l[2 * j] * f.x;
+                    l[2 * j + 1] = is_first ? 0.0f : l[2 * j + 1] * f.y;
+                }
                 if (!is_first) {                   // O so far, in the new reference
                     ok = bar_wait(smem_u32(&ms.p_empty), (i - 1) & 1, ok ? limit : 0) && ok;
                     __syncwarp();
                     fence_after();
 #pragma unroll 1
                     for (int b = 0; b < 4; b++)
-#pragma unroll
+#pragma unroll 1
                         for (int cc = 0; cc < kHeads; cc += 16) {
                             uint32_t o[16];
                             tmem_ld16(tmem + lanes + kO + b * 64 + cc, o);
@@ -753,43 +781,37 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
             uint32_t pk[2 * kJ];                   // weights as pairs of heads: row 0 in [2j], row 1 in [2j + 1]
 #pragma unroll
             for (int j = 0; j < kJ; j++) {
-                float e4[4];
-#pragma unroll
-                for (int e = 0; e < 4; e++) e4[e] = (e < 2 ? ok0 : ok1) ? ex2(x[4 * j + e] - m[2 * j + (e & 1)]) : 0.0f;
-                l[2 * j] += e4[0] + e4[2];
-                l[2 * j + 1] += e4[1] + e4[3];
-                pk[2 * j] = pack_bf16(e4[0], e4[1]);
-                pk[2 * j + 1] = pack_bf16(e4[2], e4[3]);
+                const float2 m = *reinterpret_cast<const float2 *>(&ms.mref[8 * j + hc]);
+                const float a0 = ex2(x[4 * j] - m.x), a1 = ex2(x[4 * j + 1] - m.y), b0 = ex2(x[4 * j + 2] - m.x), b1 = ex2(x[4 * j + 3] - m.y);
+                l[2 * j] += a0 + b0;
+                l[2 * j + 1] += a1 + b1;
+                pk[2 * j] = pack_bf16(a0, a1);
+                pk[2 * j + 1] = pack_bf16(b0, b1);
             }
             if (i > 0) ok = bar_wait(smem_u32(&ms.p_empty), (i - 1) & 1, ok ? limit : 0) && ok;     // P is free
             __syncwarp();
 #pragma unroll
             for (int j = 0; j < kJ; j += 2)
-                stmatrix4(p_row + ((((uint32_t)j + (uint32_t)(lane >> 4)) ^ row16) << 4), pk[2 * j], pk[2 * j + 1], pk[2 * j + 2], pk[2 * j + 3]);
+                stmatrix4(p_row + ((((uint32_t)j + (uint32_t)(lane >> 4)) ^ row8) << 4), pk[2 * j], pk[2 * j + 1], pk[2 * j + 2], pk[2 * j + 3]);
             fence_async_shared();
             fence_before();
             __syncwarp();
             if (lane == 0) bar_arrive(smem_u32(&ms.p_full));
-            if (is_last) {
-                // ---- the sequence's share ends: sums over the rows, then O out of tensor memory
+            if (info.y & kInfoLast) {
+                // ---- the sequence's part ends: sums over the rows, then O out of tensor memory
 #pragma unroll
-                for (int k = 0; k < 2 * kJ; k++) {
-                    l[k] += __shfl_xor_sync(0xffffffffu, l[k], 4);
-                    l[k] += __shfl_xor_sync(0xffffffffu, l[k], 8);
-                    l[k] += __shfl_xor_sync(0xffffffffu, l[k], 16);
-                }
-                group_sync(1, 128);                // everyone is done with red and fac
-                if (lane < 4)
+                for (int j = 0; j < kJ; j++)
 #pragma unroll
-                    for (int j = 0; j < kJ; j++)
-#pragma unroll
-                        for (int e = 0; e < 2; e++) {
-                            ms.red[warp][8 * j + hc + e] = l[2 * j + e];
-                            if (warp == 0) ms.mref[8 * j + hc + e] = m[2 * j + e];
-                        }
+                    for (int e = 0; e < 2; e++) {
+                        float a = l[2 * j + e];
+                        a += __shfl_xor_sync(0xffffffffu, a, 4);
+                        a += __shfl_xor_sync(0xffffffffu, a, 8);
+                        a += __shfl_xor_sync(0xffffffffu, a, 16);
+                        if (lane < 4) ms.red[warp][8 * j + hc + e] = a;
+                    }
+                const bool whole = info.y & kInfoWhole;
+                const size_t row0 = (whole ? (size_t)info.z : (size_t)slot + info.z) * p.c.n_q + h0;
                 group_sync(1, 128);
-                const bool whole = w.whole();
-                const size_t row0 = (whole ? (size_t)w.s : (size_t)slot + w.s) * p.c.n_q + h0;
                 if (tid < kHeads) {
                     const float ls = (ms.red[0][tid] + ms.red[1][tid]) + (ms.red[2][tid] + ms.red[3][tid]);
                     ms.fac[tid] = whole ? 1.0f / ls : 1.0f;
@@ -804,28 +826,28 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
                 fence_after();
 #pragma unroll 1
                 for (int b = 0; b < 4; b++)
-#pragma unroll
+#pragma unroll 1
                     for (int cc = 0; cc < kHeads; cc += 16) {
                         uint32_t o[16];
                         tmem_ld16(tmem + lanes + kO + b * 64 + cc, o);
                         tmem_wait_ld();
-                        const int dim = 128 * b + 32 * warp + lane;
+                        const size_t at = (row0 + cc) * kLatentValueDim + 128 * b + 32 * warp + lane;
+                        const int left = nh_here - cc;
                         if (whole) {
 #pragma unroll
                             for (int e = 0; e < 16; e++)
-                                if (cc + e < nh_here)
-                                    p.out[(row0 + cc + e) * kLatentValueDim + dim] = __float2bfloat16_rn(__uint_as_float(o[e]) * ms.fac[cc + e]);
+                                if (e < left) p.out[at + e * kLatentValueDim] = __float2bfloat16_rn(__uint_as_float(o[e]) * ms.fac[cc + e]);
                         } else {
 #pragma unroll
                             for (int e = 0; e < 16; e++)
-                                if (cc + e < nh_here) p.part_o[(row0 + cc + e) * kLatentValueDim + dim] = __uint_as_float(o[e]);
+                                if (e < left) p.part_o[at + e * kLatentValueDim] = __uint_as_float(o[e]);
                         }
                     }
                 fence_before();
                 __syncwarp();
                 if (lane == 0) bar_arrive(smem_u32(&ms.o_free));
             }
-            more = w.next();
+            if (info.y & kInfoFinal) break;
         }
     }
     if (!ok) atomicOr(&p.c.ctrl[kCtrlStatus], PASK_DEV_TIMEOUT);
