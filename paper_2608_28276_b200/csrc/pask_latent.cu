@@ -301,9 +301,10 @@ read_latent_kernel(DevCache c, int layer, int n_seqs, int total_rows, const int3
 //
 // A CTA is one of `slots` equal shares of the batch's rows (cost line over sequences, as the other decode kernel cuts it), in
 // tiles of 64 rows = four pages of one stream; a sequence's HIGH and LOW tiles are visited in turn, evenly mixed.  Roles:
-//   warp 8      HIGH tiles: one linear bulk copy a page (pages are stored in the operand layout) into one of two stages, and
-//               a prefetch into L2 some tiles ahead, which keeps memory busy while both stages are held by products
-//   warps 4-7   LOW tiles: codes to registers one tile ahead, values as bf16 into the stage; and the queries of a sequence
+//   warp 8      one linear bulk copy a page (HIGH pages are stored in the operand layout) into its place in one of two stages,
+//               as soon as the product that last read the place is done, and a prefetch into L2 some tiles ahead, which
+//               keeps memory busy while both stages are held by products
+//   warps 4-7   LOW tiles: codes from the stage to registers, values as bf16 back over them; and the queries of a sequence
 //   warp 9      issues the products: S of tile i + 1, then O of tile i
 //   warps 0-3   softmax of a tile's S (warp w: page w of the tile), P to shared memory, and a sequence's end
 // The reference maximum of a head moves only when a score exceeds it by more than 2^8 (the sums have room for that), so that
@@ -328,7 +329,8 @@ struct DecParams {
     float scale_log2;
     __nv_bfloat16 *out;
     float *lse;
-    uint32_t *prefix;                              // [n_seqs + 1] cost of the sequences before s
+    uint4 *meta;                                   // [n_seqs + 1] per sequence {cost before it, its cost, its tiles, first share | shares
+                                                   // << 16}; behind them {cost of all, shares in use}
     float2 *part_ml;                               // [slots + n_seqs][n_q] (reference maximum in log2 units, sum)
     float *part_o;                                 // [slots + n_seqs][n_q][512]
     long long wait_cycles;
@@ -337,21 +339,19 @@ struct DecParams {
 };
 
 __device__ __forceinline__ uint32_t tiles_of(uint32_t tokens) { return (tokens + kTile - 1) / kTile; }
-__device__ __forceinline__ uint32_t cost_of(uint32_t nh, uint32_t nl) { return kCostHighTile * tiles_of(nh) + kCostLowTile * tiles_of(nl); }
 __device__ __forceinline__ uint32_t slot_start(uint32_t total, uint32_t slot, uint32_t slots) {
     return (uint32_t)((uint64_t)total * slot / slots);
 }
 
-// The tiles of one share, in order; every role walks its own copy.
+// The tiles of one share, in order; the roles walk their own copies.
 struct TileWalk {
     const DevCache *c;
     const int32_t *seq_ids;
     int layer, n_seqs, s;
     uint32_t lo, hi, base, cost;
-    uint32_t nh, nl, th, tl, v, v0, v1;
+    uint32_t nh, nl, th, n, v, v0, v1;             // rows of the streams; HIGH tiles, tiles, position and range of it
+    uint32_t h0, rem;                              // v * th = h0 * n + rem (page_at of pask_layout.h without its divisions)
     size_t sl;
-    bool high;
-    uint32_t tile, valid, pages;                   // tile of the stream, its rows and pages
 
     __device__ __forceinline__ void load() {
         const int seq = seq_ids[s];
@@ -360,12 +360,15 @@ struct TileWalk {
         nh = ok ? c->n_high[sl] : 0u;
         nl = ok ? c->n_low[sl] : 0u;
         th = tiles_of(nh);
-        tl = tiles_of(nl);
-        cost = kCostHighTile * th + kCostLowTile * tl;
-        v0 = v1 = 0;
+        n = th + tiles_of(nl);
+        cost = kCostHighTile * th + kCostLowTile * (n - th);
+        v0 = v1 = h0 = rem = 0;
         if (cost) {
-            v0 = lo > base ? cut_positions(lo - base, cost, th + tl) : 0u;
-            v1 = cut_positions(hi - base, cost, th + tl);
+            v0 = lo > base ? cut_positions(lo - base, cost, n) : 0u;
+            v1 = cut_positions(hi - base, cost, n);
+            const uint64_t x = (uint64_t)v0 * th;
+            h0 = (uint32_t)(x / n);
+            rem = (uint32_t)(x - (uint64_t)h0 * n);
         }
         v = v0;
     }
@@ -375,9 +378,6 @@ struct TileWalk {
             if (++s >= n_seqs || base >= hi) return false;
             load();
         }
-        high = page_at(v, th, tl, tile);
-        valid = min((uint32_t)kTile, (high ? nh : nl) - kTile * tile);
-        pages = (valid + kPageTokens - 1) / kPageTokens;
         return true;
     }
     __device__ __forceinline__ bool begin(const DecParams &p, int first, uint32_t first_base, uint32_t lo_, uint32_t hi_) {
@@ -387,16 +387,31 @@ struct TileWalk {
         load();
         return settle();
     }
-    __device__ __forceinline__ bool next() { v++; return settle(); }
+    __device__ __forceinline__ bool next() {
+        v++;
+        rem += th;
+        if (rem >= n) { rem -= n; h0++; }
+        return v < v1 || settle();
+    }
+    __device__ __forceinline__ bool high() const { return rem + th >= n; }
+    __device__ __forceinline__ uint32_t tile() const { return high() ? h0 : v - h0; }
+    __device__ __forceinline__ uint32_t valid() const { return min((uint32_t)kTile, (high() ? nh : nl) - kTile * tile()); }
+    __device__ __forceinline__ uint32_t pages() const { return (valid() + kPageTokens - 1) / kPageTokens; }
     __device__ __forceinline__ bool first() const { return v == v0; }
     __device__ __forceinline__ bool last() const { return v + 1 == v1; }
-    __device__ __forceinline__ bool whole() const { return v0 == 0 && v1 == th + tl; }
-    // id of the tile's page p; an id the pools cannot hold is never dereferenced
-    __device__ __forceinline__ uint32_t page(uint32_t p) const {
-        const uint32_t id = (high ? c->tbl_high : c->tbl_low)[sl * c->max_pages + kTilePages * tile + p];
-        if (id < (high ? c->cap_high : c->cap_low)) return id;
-        atomicOr(&c->ctrl[kCtrlStatus], PASK_DEV_INTERNAL);
-        return 0;
+    __device__ __forceinline__ bool whole() const { return v0 == 0 && v1 == n; }
+    // where the tile's page p lies, from its id (read a tile before it is looked at); an id the pools cannot hold is never
+    // dereferenced
+    __device__ __forceinline__ uint32_t page_id(uint32_t p) const {
+        return p < pages() ? (high() ? c->tbl_high : c->tbl_low)[sl * c->max_pages + kTilePages * tile() + p] : 0u;
+    }
+    __device__ __forceinline__ uint32_t page_bytes() const { return high() ? (uint32_t)kLatentHighPageBytes : c->low_page_bytes; }
+    __device__ __forceinline__ const uint8_t *page(uint32_t id) const {
+        if (id >= (high() ? c->cap_high : c->cap_low)) {
+            if (pages()) atomicOr(&c->ctrl[kCtrlStatus], PASK_DEV_INTERNAL);
+            id = 0;
+        }
+        return (high() ? c->pool_high : c->pool_low) + (size_t)id * page_bytes();
     }
 };
 
@@ -404,12 +419,12 @@ template <int kHeads>
 struct DecSmem {
     static constexpr int kQ = 2 * kTileBytes, kP = kQ + kHeads * 1152, kMisc = kP + kTile * 128;
     struct Misc {
-        uint64_t kv_full[2], kv_empty[2], s_full[2], s_empty[2], q_full, q_empty, p_full, p_empty, o_free, drain;
+        uint64_t full[2 * kTilePages], empty[2 * kTilePages], raw[2], s_full[2], s_empty[2], q_full, q_empty, q_first, p_full, p_empty, o_free, drain;
         uint4 info[2];                             // of the tile whose S a stage holds: valid rows, flags, sequence
         uint32_t tmem;
         int first;
         uint32_t first_base, total;
-        uint32_t warp_sum[kDecThreads / 32];
+        uint32_t warp_sum[kDecThreads / 32], warp_tiles[kDecThreads / 32];
         float red[4][kHeads], fac[kHeads], mref[kHeads];
     };
     static constexpr int kBytes = kMisc + (int)sizeof(Misc) + 1024;
@@ -433,40 +448,48 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
 
     // ---- the share: cost prefix over the sequences (1024 at most, kPer a thread)
     constexpr int kPer = (PASK_MAX_SEQS_PER_CALL + kDecThreads - 1) / kDecThreads;
-    uint32_t cost[kPer], sum = 0;
+    uint32_t cost[kPer], tiles[kPer], sum = 0, sum_tiles = 0;
 #pragma unroll
     for (int r = 0; r < kPer; r++) {
         const int s = tid * kPer + r;
-        cost[r] = 0;
+        cost[r] = tiles[r] = 0;
         if (s < p.n_seqs) {
             const int seq = p.seq_ids[s];
             if (seq >= 0 && seq < p.c.max_seqs) {
                 const size_t sl = (size_t)seq * p.c.n_layers + p.layer;
-                cost[r] = cost_of(p.c.n_high[sl], p.c.n_low[sl]);
+                const uint32_t th = tiles_of(p.c.n_high[sl]), tl = tiles_of(p.c.n_low[sl]);
+                cost[r] = kCostHighTile * th + kCostLowTile * tl;
+                tiles[r] = th + tl;
             } else if (blockIdx.x == 0) {
                 atomicOr(&p.c.ctrl[kCtrlStatus], PASK_DEV_BAD_SEQ);
             }
         }
         sum += cost[r];
+        sum_tiles += tiles[r];
     }
+    sum_tiles = __reduce_add_sync(0xffffffffu, sum_tiles);
     uint32_t inc = sum;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
         const uint32_t o = __shfl_up_sync(0xffffffffu, inc, d);
         if (lane >= d) inc += o;
     }
-    if (lane == 31) ms.warp_sum[warp] = inc;
+    if (lane == 31) { ms.warp_sum[warp] = inc; ms.warp_tiles[warp] = sum_tiles; }
     if (tid == 0) {
         ms.first = p.n_seqs;
         ms.first_base = 0;
         for (int i = 0; i < 2; i++) {
-            bar_init(smem_u32(&ms.kv_full[i]), 1);
-            bar_init(smem_u32(&ms.kv_empty[i]), 1);
+            bar_init(smem_u32(&ms.raw[i]), 1);
             bar_init(smem_u32(&ms.s_full[i]), 2);
             bar_init(smem_u32(&ms.s_empty[i]), 4);
         }
+        for (int i = 0; i < 2 * kTilePages; i++) {
+            bar_init(smem_u32(&ms.full[i]), 1);
+            bar_init(smem_u32(&ms.empty[i]), 1);
+        }
         bar_init(smem_u32(&ms.q_full), 1);
         bar_init(smem_u32(&ms.q_empty), 1);
+        bar_init(smem_u32(&ms.q_first), 1);          // completes once, with the first queries
         bar_init(smem_u32(&ms.p_full), 4);
         bar_init(smem_u32(&ms.p_empty), 1);
         bar_init(smem_u32(&ms.o_free), 4);
@@ -474,17 +497,40 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
         bar_init_fence();
     }
     __syncthreads();
-    uint32_t at = inc - sum, total = 0;
+    uint32_t at = inc - sum, total = 0, slots = 0;
 #pragma unroll
     for (int w = 0; w < kDecThreads / 32; w++) {
         if (w < warp) at += ms.warp_sum[w];
         total += ms.warp_sum[w];
+        slots += ms.warp_tiles[w];
     }
-    const uint32_t lo = slot_start(total, slot, p.slots), hi = slot_start(total, slot + 1, p.slots);
+    slots = min(slots, p.slots);                   // no more shares than tiles
+    if (blockIdx.x == 0) {                         // what the merge needs to know
+        if (tid == 0) p.meta[p.n_seqs] = make_uint4(total, slots, 0, 0);
+        uint32_t base = at;
+#pragma unroll 1
+        for (int r = 0; r < kPer; r++) {
+            const int s = tid * kPer + r;
+            if (s >= p.n_seqs) break;
+            const uint32_t cs = r == 0 ? cost[0] : r == 1 ? cost[1] : r == 2 ? cost[2] : cost[3];
+            const uint32_t ts = r == 0 ? tiles[0] : r == 1 ? tiles[1] : r == 2 ? tiles[2] : tiles[3];
+            uint32_t b0 = 0, b1 = 0;
+            if (cs) {                              // shares [b0, b1): the one the sequence starts in .. the last that starts before its end
+                b0 = (uint32_t)((uint64_t)base * slots / total);
+                while (slot_start(total, b0 + 1, slots) <= base) b0++;
+                b1 = (uint32_t)(((uint64_t)(base + cs) * slots + total - 1) / total);
+                while (b1 < slots && slot_start(total, b1, slots) < base + cs) b1++;
+                while (b1 > b0 + 1 && slot_start(total, b1 - 1, slots) >= base + cs) b1--;
+            }
+            p.meta[s] = make_uint4(base, cs, ts, b0 | (b1 - b0) << 16);
+            base += cs;
+        }
+    }
+    if (slot >= slots) return;
+    const uint32_t lo = slot_start(total, slot, slots), hi = slot_start(total, slot + 1, slots);
 #pragma unroll
     for (int r = 0; r < kPer; r++) {
         const int s = tid * kPer + r;
-        if (s <= p.n_seqs && blockIdx.x == 0) p.prefix[s] = at;
         if (s < p.n_seqs && at <= lo && lo < at + cost[r]) { ms.first = s; ms.first_base = at; }
         at += cost[r];
     }
@@ -503,69 +549,94 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
     bool more = w.begin(p, first, first_base, lo, hi), ok = true;
 
     if (warp == 8) {
-        // ================================================= HIGH tiles
+        // ================================================= copies
+        // (page ids are read an iteration before they are used: the read's way to L2 would otherwise sit between a freed
+        // place and the copy into it)
+        uint32_t lows[2] = {0, 0};                 // LOW tiles copied into each stage
+        uint32_t i = 0, id = more ? w.page_id(lane) : 0u, ahead_id = 0;
         TileWalk ahead = w;
         bool ahead_more = more;
-        uint32_t copied = 0, phase[2] = {0, 0};    // stages that were ever copied into, and the phase of the last copy
-        auto prefetch = [&]() {
-            if (!ahead_more) return;
-            if ((uint32_t)lane < ahead.pages) {
-                if (ahead.high) bulk_prefetch(p.c.pool_high + (size_t)ahead.page(lane) * kLatentHighPageBytes, kLatentHighPageBytes);
-                else bulk_prefetch(p.c.pool_low + (size_t)ahead.page(lane) * p.c.low_page_bytes, p.c.low_page_bytes);
-            }
-            ahead_more = ahead.next();
-        };
-        for (uint32_t i = 0; more; i++, more = w.next()) {
-            if (i == 0) for (int k = 0; k < kPrefetch; k++) prefetch();
-            const uint32_t st = i & 1, full = smem_u32(&ms.kv_full[st]);
-            const uint32_t id = w.high && (uint32_t)lane < w.pages ? w.page(lane) : 0u;
-            // (both producers wait for every tile's stage, their own or not: a phase's parity only tells it from its neighbours)
-            ok = __all_sync(0xffffffffu, i < 2 || bar_wait(smem_u32(&ms.kv_empty[st]), ((i >> 1) - 1) & 1, limit));
-            if (!ok) break;
-            if (w.high) {
-                copied |= 1u << st;
-                if (st) phase[1] = (i >> 1) & 1; else phase[0] = (i >> 1) & 1;
-                if (lane == 0) bar_expect(full, w.pages * kLatentHighPageBytes + (i == 0 ? p.surplus : 0u));
+        for (int k = 0; k < kPrefetch; k++) ahead_more = ahead_more && ahead.next();
+        if (ahead_more) ahead_id = ahead.page_id(lane);
+        for (; more; i++) {
+            const uint32_t st = i & 1, np = w.pages(), bytes = w.page_bytes();
+            const bool high = w.high();
+            const uint8_t *src = (uint32_t)lane < np ? w.page(id) : nullptr;
+            more = w.next();
+            if (more) id = w.page_id(lane);
+            const uint32_t raw = smem_u32(&ms.raw[st]), extra = i == 0 ? p.surplus : 0u;
+#pragma unroll 1
+            for (int pg = 0; pg < kTilePages; pg++) {
+                const uint32_t slot_of = 4 * st + pg, full = smem_u32(&ms.full[slot_of]);
+                ok = ok && (i < 2 || bar_wait(smem_u32(&ms.empty[slot_of]), ((i >> 1) - 1) & 1, limit));
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                if (lane == pg) {
+                    const uint32_t dst = kv0 + slot_of * kLatentHighPageBytes;
+                    if (high) {
+                        if ((uint32_t)pg < np) {
+                            bar_expect(full, bytes + (pg == 0 ? extra : 0u));
+                            bulk_load(dst, src, bytes, full);
+                        } else {
+                            bar_arrive(full);
+                        }
+                    } else if ((uint32_t)pg < np) {
+                        if (pg == 0) bar_expect(raw, np * bytes + extra);
+                        bulk_load(dst, src, bytes, raw);
+                    }
+                }
                 __syncwarp();
-                if ((uint32_t)lane < w.pages)
-                    bulk_load(kv0 + st * kTileBytes + lane * kLatentHighPageBytes, p.c.pool_high + (size_t)id * kLatentHighPageBytes,
-                              kLatentHighPageBytes, full);
             }
-            prefetch();
+            if (!ok) break;
+            if (!high) { if (st) lows[1]++; else lows[0]++; }
+            if (i == 1) {                          // the first queries go before rows that are not needed yet
+                ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&ms.q_first), 0, limit));
+                if (!ok) break;
+            }
+            if (ahead_more) {
+                if ((uint32_t)lane < ahead.pages()) bulk_prefetch(ahead.page(ahead_id), ahead.page_bytes());
+                ahead_more = ahead.next();
+                if (ahead_more) ahead_id = ahead.page_id(lane);
+            }
         }
         if (!ok || p.surplus) {                    // gave up: let the copies in flight land (bounded) before the CTA ends
-            if (copied & 1u) bar_wait(smem_u32(&ms.kv_full[0]), phase[0], limit);
-            if (copied & 2u) bar_wait(smem_u32(&ms.kv_full[1]), phase[1], limit);
+            for (int k = 0; k < 2; k++) {
+                if (lows[k]) bar_wait(smem_u32(&ms.raw[k]), (lows[k] - 1) & 1, limit);
+                if (i > (uint32_t)k)
+                    for (int pg = 0; pg < kTilePages; pg++) bar_wait(smem_u32(&ms.full[4 * k + pg]), ((i - 1 - k) >> 1) & 1, p.surplus ? 1000 : limit);
+            }
         }
     } else if (warp == 9) {
         // ================================================= products
         constexpr uint32_t kIdS = instr(kTile, kHeads, false, false), kIdO = instr(128, kHeads, true, true);
-        const bool mine = elect_one();
-        uint32_t n_seg = 0, i = 0, j = 0;          // tiles whose S, whose O product has been issued (j <= i <= j + 1)
+        const bool mine = elect_one();             // one lane looks at the barriers and issues; the warp follows it
+        uint32_t n_seg = 0, i = 0, j = 0;          // tiles whose S, whose O product has been issued (j <= i <= j + 2)
         uint32_t pv_pages = 0, pv_seg = 0, next_pages = 0, next_seg = 0;
         bool pv_first = false, next_first = false;
+        TileWalk wn = w;                           // one tile ahead of w, moved on behind the products: nothing waits for its loads
+        bool after = more && wn.next();
         while (more || j < i) {
-            const uint32_t st = __shfl_sync(0xffffffffu, i & 1, 0);
-            bool qk = more;
-            if (more && j < i) {                   // whichever can go: the next tile's S, or O of the one before
+            // O of the oldest tile if its weights are there (that frees its stage), else S of the next tile if it is
+            int pick = 0;
+            if (mine) {
                 const long long t0 = clock64();
-                int pick = 0;
-                while (!pick) {
-                    pick = bar_test(smem_u32(&ms.kv_full[st]), (i >> 1) & 1) ? 1 : bar_test(smem_u32(&ms.p_full), j & 1) ? 2 : 0;
-                    if (!pick && clock64() - t0 > limit) pick = 3;
-                    pick = __shfl_sync(0xffffffffu, pick, 0);
+                const uint32_t st = i & 1, ph = (i >> 1) & 1;
+                for (uint32_t spin = 0; !pick; spin++) {
+                    if (j < i && bar_test(smem_u32(&ms.p_full), j & 1) && (!pv_first || pv_seg < 2 || bar_test(smem_u32(&ms.o_free), (pv_seg - 2) & 1)))
+                        pick = 1;
+                    else if (more && i < j + 2 && bar_test(smem_u32(&ms.full[4 * st + 3]), ph) && bar_test(smem_u32(&ms.full[4 * st + 2]), ph) &&
+                             bar_test(smem_u32(&ms.full[4 * st + 1]), ph) && bar_test(smem_u32(&ms.full[4 * st]), ph) &&
+                             (i < 2 || bar_test(smem_u32(&ms.s_empty[st]), ph ^ 1)) && (!w.first() || bar_test(smem_u32(&ms.q_full), n_seg & 1)))
+                        pick = 2;
+                    else if ((spin & 255) == 255 && clock64() - t0 > limit)
+                        pick = 3;
                 }
-                if (pick == 3) { ok = false; break; }
-                qk = pick == 1;
             }
-            if (qk) {
-                const bool is_first = w.first();
-                if (is_first) { n_seg++; ok = ok && bar_wait(smem_u32(&ms.q_full), (n_seg - 1) & 1, limit); }
-                ok = ok && bar_wait(smem_u32(&ms.kv_full[st]), (i >> 1) & 1, limit);
-                ok = ok && (i < 2 || bar_wait(smem_u32(&ms.s_empty[st]), ((i >> 1) - 1) & 1, limit));
-                ok = __all_sync(0xffffffffu, ok);
-                if (!ok) break;
-                fence_after();
+            pick = __reduce_max_sync(0xffffffffu, pick);
+            if (pick == 3) { ok = false; break; }
+            fence_after();
+            if (pick == 2) {
+                const uint32_t st = __shfl_sync(0xffffffffu, i & 1, 0);
                 const uint32_t kv = kv0 + st * kTileBytes;
                 const uint64_t dk = desc(kv, 0, kLatentHalfPage), dq = desc(qs, 0, kLatentHalfPage);
 #pragma unroll
@@ -573,47 +644,40 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
                     const uint64_t off = (uint64_t)(((k >> 2) * 1024 + (k & 3) * 32) >> 4);
                     mma_ss(tmem + st * 64, dk + off, dq + off, kIdS, k > 0, mine);
                 }
-                const bool is_last = w.last();
+                const bool is_first = w.first(), is_last = w.last();
                 if (mine) {
                     commit(smem_u32(&ms.s_full[st]));
                     if (is_last) commit(smem_u32(&ms.q_empty));
-                }
-                const uint32_t valid = w.valid, flags = (is_first ? kInfoFirst : 0u) | (is_last ? kInfoLast : 0u) | (w.whole() ? kInfoWhole : 0u);
-                const uint32_t seq = (uint32_t)w.s;
-                const uint32_t now_pages = w.pages;
-                more = w.next();
-                if (mine) {
-                    ms.info[st] = make_uint4(valid, flags | (more ? 0u : kInfoFinal), seq, 0);
+                    const uint32_t flags = (is_first ? kInfoFirst : 0u) | (is_last ? kInfoLast : 0u) | (w.whole() ? kInfoWhole : 0u);
+                    ms.info[st] = make_uint4(w.valid(), flags | (after ? 0u : kInfoFinal), (uint32_t)w.s, 0);
                     bar_arrive(smem_u32(&ms.s_full[st]));
                 }
+                n_seg += is_first;
+                if (i == j) { pv_pages = w.pages(); pv_seg = n_seg; pv_first = is_first; }
+                else { next_pages = w.pages(); next_seg = n_seg; next_first = is_first; }
                 i++;
-                if (i == j + 1) { pv_pages = now_pages; pv_seg = n_seg; pv_first = is_first; }
-                else { next_pages = now_pages; next_seg = n_seg; next_first = is_first; }
-            }
-            if (j + 1 < i || !more || !qk) {
-                ok = ok && bar_wait(smem_u32(&ms.p_full), j & 1, limit);
-                // the segment before has been read out of O
-                ok = ok && (!pv_first || pv_seg < 2 || bar_wait(smem_u32(&ms.o_free), (pv_seg - 2) & 1, limit));
-                ok = __all_sync(0xffffffffu, ok);
-                if (!ok) break;
-                fence_after();
+                more = after;
+                if (more) {
+                    w = wn;
+                    after = wn.next();
+                }
+            } else {
                 const uint32_t sv = __shfl_sync(0xffffffffu, j & 1, 0), np = __shfl_sync(0xffffffffu, pv_pages, 0);
                 const bool fresh = __shfl_sync(0xffffffffu, (int)pv_first, 0) != 0;
                 const uint64_t dv = desc(kv0 + sv * kTileBytes, 1024, kLatentHalfPage), dp = desc(ps, 0, 1024);
 #pragma unroll
-                for (int k = 0; k < kTilePages; k++)
+                for (int k = 0; k < kTilePages; k++) {
                     if ((uint32_t)k < np) {
 #pragma unroll
                         for (int b = 0; b < 4; b++)
                             mma_ss(tmem + kO + b * 64, dv + (uint64_t)((k * kLatentHighPageBytes + b * 2048) >> 4), dp + (uint64_t)(k * 2048 >> 4),
                                    kIdO, k > 0 || !fresh, mine);
                     }
-                if (mine) {
-                    commit(smem_u32(&ms.kv_empty[sv]));
-                    commit(smem_u32(&ms.p_empty));
+                    if (mine) commit(smem_u32(&ms.empty[4 * sv + k]));
                 }
+                if (mine) commit(smem_u32(&ms.p_empty));
                 j++;
-                if (j < i) { pv_pages = next_pages; pv_seg = next_seg; pv_first = next_first; }
+                pv_pages = next_pages; pv_seg = next_seg; pv_first = next_first;
             }
         }
         if (!ok) {                                 // gave up: the products in flight end before tensor memory is freed
@@ -624,28 +688,9 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
     } else if (warp >= 4) {
         // ================================================= queries and LOW tiles
         const int t = tid - 128;                   // 0..127: token t & 15, (page, group) pairs t >> 4 + 8 k
-        constexpr int kItems = kTilePages * kLatentGroups / 8;
-        uint32_t codes[kItems][BITS], scales[kItems];
-        TileWalk ahead = w;                        // the next LOW tile, whose codes are in the registers
-        bool have = more;
-        auto fetch = [&]() {                       // codes of the tile `ahead` stands on
-            uint32_t ids[kTilePages];
-#pragma unroll
-            for (int pg = 0; pg < kTilePages; pg++) ids[pg] = (uint32_t)pg < ahead.pages ? ahead.page(pg) : 0u;
-#pragma unroll
-            for (int k = 0; k < kItems; k++) {
-                const int pair = 8 * k + (t >> 4), pg = pair / kLatentGroups, g = pair % kLatentGroups;
-                if ((uint32_t)pg < ahead.pages) {
-                    const uint32_t id = pg == 0 ? ids[0] : pg == 1 ? ids[1] : pg == 2 ? ids[2] : ids[3];
-                    const uint8_t *src = p.c.pool_low + (size_t)id * p.c.low_page_bytes;
-                    load_codes<BITS>(src, t & 15, g, codes[k]);
-                    scales[k] = *reinterpret_cast<const uint16_t *>(src + latent_scale_off(t & 15, g, BITS));
-                }
-            }
-        };
-        while (have && ahead.high) have = ahead.next();
-        if (have) fetch();
-        uint32_t n_seg = 0;
+        constexpr int kPasses = BITS == 8 ? 2 : 1, kPassPages = kTilePages / kPasses;        // what the registers hold at a time
+        constexpr int kItems = (kPassPages * kLatentGroups + 7) / 8;
+        uint32_t n_seg = 0, lows[2] = {0, 0};
         bool bad = false;
         for (uint32_t i = 0; more; i++, more = w.next()) {
             const uint32_t st = i & 1;
@@ -654,38 +699,53 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
                 n_seg++;
                 const uint4 *src = p.q + ((size_t)w.s * p.c.n_q + h0) * kLatentChunks;
                 constexpr int kIter = kHeads * kLatentChunks / 128;
-#pragma unroll 12
-                for (int k = 0; k < kIter; k++) {
+#pragma unroll 6
+                for (int k = 0; k < kIter; k++) {  // all in flight at once; heads this CTA does not have are zeros
                     const int x = k * 128 + t, row = x / kLatentChunks, ch = x % kLatentChunks;
-                    const uint4 v = row < nh_here ? src[x] : make_uint4(0, 0, 0, 0);
-                    *reinterpret_cast<uint4 *>(sm + Sm::kQ + (row >> 4) * kLatentHighPageBytes + latent_chunk_off(row & 15, ch)) = v;
+                    const bool there = row < nh_here;
+                    copy16(qs + (row >> 4) * kLatentHighPageBytes + latent_chunk_off(row & 15, ch), there ? src + x : src, there ? 16 : 0);
                 }
+                copy16_wait();
                 fence_async_shared();
-                bad = group_any(2, 128, !ok);
-                if (bad) break;
+                if (group_any(2, 128, !ok)) break;
                 if (t == 0) bar_arrive(smem_u32(&ms.q_full));
+                if (t == 0 && n_seg == 1) bar_arrive(smem_u32(&ms.q_first));
             }
-            if (i >= 2) ok = bar_wait(smem_u32(&ms.kv_empty[st]), ((i >> 1) - 1) & 1, ok ? limit : 0) && ok;
-            if (!w.high) {
+            if (!w.high()) {
+                // the codes of a page were copied to the start of its place in the stage: out to registers, then values over them
+                const uint32_t n = st ? lows[1]++ : lows[0]++, np = w.pages();
+                ok = bar_wait(smem_u32(&ms.raw[st]), n & 1, ok ? limit : 0) && ok;
                 uint8_t *dst = sm + st * kTileBytes;
+#pragma unroll 1
+                for (int pass = 0; pass < kPasses; pass++) {
+                    uint32_t codes[kItems][BITS], scales[kItems];
 #pragma unroll
-                for (int k = 0; k < kItems; k++) {
-                    const int pair = 8 * k + (t >> 4), pg = pair / kLatentGroups, g = pair % kLatentGroups;
-                    if ((uint32_t)pg < w.pages) {
-                        uint32_t xs[16];
-                        dequantise_group<BITS>(codes[k], scales[k], xs);
+                    for (int k = 0; k < kItems; k++) {
+                        const int pair = 8 * k + (t >> 4), pg = kPassPages * pass + pair / kLatentGroups, g = pair % kLatentGroups;
+                        if (pair < kPassPages * kLatentGroups && (uint32_t)pg < np) {
+                            load_codes<BITS>(dst + pg * kLatentHighPageBytes, t & 15, g, codes[k]);
+                            scales[k] = *reinterpret_cast<const uint16_t *>(dst + pg * kLatentHighPageBytes + latent_scale_off(t & 15, g, BITS));
+                        }
+                    }
+                    bad = group_any(2, 128, !ok);
+                    if (bad) break;
 #pragma unroll
-                        for (int e = 0; e < 4; e++)
-                            *reinterpret_cast<uint4 *>(dst + pg * kLatentHighPageBytes + latent_chunk_off(t & 15, 4 * g + e)) =
-                                make_uint4(xs[4 * e], xs[4 * e + 1], xs[4 * e + 2], xs[4 * e + 3]);
+                    for (int k = 0; k < kItems; k++) {
+                        const int pair = 8 * k + (t >> 4), pg = kPassPages * pass + pair / kLatentGroups, g = pair % kLatentGroups;
+                        if (pair < kPassPages * kLatentGroups && (uint32_t)pg < np) {
+                            uint32_t xs[16];
+                            dequantise_group<BITS>(codes[k], scales[k], xs);
+#pragma unroll
+                            for (int e = 0; e < 4; e++)
+                                *reinterpret_cast<uint4 *>(dst + pg * kLatentHighPageBytes + latent_chunk_off(t & 15, 4 * g + e)) =
+                                    make_uint4(xs[4 * e], xs[4 * e + 1], xs[4 * e + 2], xs[4 * e + 3]);
+                        }
                     }
                 }
-                fence_async_shared();
-                bad = group_any(2, 128, !ok);
                 if (bad) break;
-                if (t == 0) bar_arrive(smem_u32(&ms.kv_full[st]));
-                do have = ahead.next(); while (have && ahead.high);
-                if (have) fetch();
+                fence_async_shared();
+                group_sync(2, 128);
+                if (t < kTilePages) bar_arrive(smem_u32(&ms.full[4 * st + t]));
             }
         }
     } else {
@@ -704,13 +764,13 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
             fence_after();
             const uint4 info = ms.info[st];
             const bool is_first = info.y & kInfoFirst;
-            float x[4 * kJ];
+            float x[4 * kJ];                       // scores in log2 units, relative to the reference maximum
             {
                 uint32_t sr[4 * kJ];
                 tmem_ld_frag(tmem + lanes + st * 64, sr);
                 tmem_wait_ld();
 #pragma unroll
-                for (int k = 0; k < 4 * kJ; k++) x[k] = __uint_as_float(sr[k]) * p.scale_log2;
+                for (int k = 0; k < 4 * kJ; k++) x[k] = __uint_as_float(sr[k]);
             }
             fence_before();
             __syncwarp();
@@ -721,17 +781,16 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
                 for (int k = 0; k < 4 * kJ; k++)
                     if (!((k & 2) ? r0 + 8 < vp : r0 < vp)) x[k] = -INFINITY;
             }
-            bool over = is_first;
-            if (!is_first) {
-                float top = -INFINITY;
+            float most = -INFINITY;
 #pragma unroll
-                for (int j = 0; j < kJ; j++) {
-                    const float2 m = *reinterpret_cast<const float2 *>(&ms.mref[8 * j + hc]);
-                    top = fmaxf(top, fmaxf(fmaxf(x[4 * j], x[4 * j + 2]) - m.x, fmaxf(x[4 * j + 1], x[4 * j + 3]) - m.y));
-                }
-                over = top > kLazy;
+            for (int j = 0; j < kJ; j++) {
+                float2 m = *reinterpret_cast<const float2 *>(&ms.mref[8 * j + hc]);
+                if (is_first) m = make_float2(0.0f, 0.0f);
+#pragma unroll
+                for (int e = 0; e < 4; e++) x[4 * j + e] = __fmaf_rn(x[4 * j + e], p.scale_log2, -((e & 1) ? m.y : m.x));
+                most = fmaxf(most, fmaxf(fmaxf(x[4 * j], x[4 * j + 1]), fmaxf(x[4 * j + 2], x[4 * j + 3])));
             }
-            if (group_any(1, 128, over || !ok)) {
+            if (group_any(1, 128, is_first || most > kLazy || !ok)) {
                 if (group_any(1, 128, !ok)) break;
                 // a new reference maximum for the heads that need one
 #pragma unroll
@@ -745,19 +804,20 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
                         if (lane < 4) ms.red[warp][8 * j + hc + e] = a;
                     }
                 group_sync(1, 128);
-                if (tid < kHeads) {
+                if (tid < kHeads) {                // red: largest score above the reference
                     const float a = fmaxf(fmaxf(ms.red[0][tid], ms.red[1][tid]), fmaxf(ms.red[2][tid], ms.red[3][tid]));
-                    const float m = ms.mref[tid];
-                    const bool raise = is_first || a - m > kLazy;
-                    ms.fac[tid] = is_first ? 0.0f : raise ? ex2(m - a) : 1.0f;
-                    if (raise) ms.mref[tid] = a;
+                    const bool raise = is_first || a > kLazy;
+                    ms.fac[tid] = raise ? a : 0.0f;
+                    if (raise) ms.mref[tid] = is_first ? a : ms.mref[tid] + a;
                 }
                 group_sync(1, 128);
 #pragma unroll
                 for (int j = 0; j < kJ; j++) {
                     const float2 f = *reinterpret_cast<const float2 *>(&ms.fac[8 * j + hc]);
-                    l[2 * j] = is_first ? 0.0f : l[2 * j] * f.x;
-                    l[2 * j + 1] = is_first ? 0.0f : l[2 * j + 1] * f.y;
+#pragma unroll
+                    for (int e = 0; e < 4; e++) x[4 * j + e] -= (e & 1) ? f.y : f.x;
+                    l[2 * j] = is_first ? 0.0f : l[2 * j] * ex2(-f.x);
+                    l[2 * j + 1] = is_first ? 0.0f : l[2 * j + 1] * ex2(-f.y);
                 }
                 if (!is_first) {                   // O so far, in the new reference
                     ok = bar_wait(smem_u32(&ms.p_empty), (i - 1) & 1, ok ? limit : 0) && ok;
@@ -771,7 +831,7 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
                             tmem_ld16(tmem + lanes + kO + b * 64 + cc, o);
                             tmem_wait_ld();
 #pragma unroll
-                            for (int e = 0; e < 16; e++) o[e] = __float_as_uint(__uint_as_float(o[e]) * ms.fac[cc + e]);
+                            for (int e = 0; e < 16; e++) o[e] = __float_as_uint(__uint_as_float(o[e]) * ex2(-ms.fac[cc + e]));
                             tmem_st16(tmem + lanes + kO + b * 64 + cc, o);
                         }
                     tmem_wait_st();
@@ -781,8 +841,7 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
             uint32_t pk[2 * kJ];                   // weights as pairs of heads: row 0 in [2j], row 1 in [2j + 1]
 #pragma unroll
             for (int j = 0; j < kJ; j++) {
-                const float2 m = *reinterpret_cast<const float2 *>(&ms.mref[8 * j + hc]);
-                const float a0 = ex2(x[4 * j] - m.x), a1 = ex2(x[4 * j + 1] - m.y), b0 = ex2(x[4 * j + 2] - m.x), b1 = ex2(x[4 * j + 3] - m.y);
+                const float a0 = ex2(x[4 * j]), a1 = ex2(x[4 * j + 1]), b0 = ex2(x[4 * j + 2]), b1 = ex2(x[4 * j + 3]);
                 l[2 * j] += a0 + b0;
                 l[2 * j + 1] += a1 + b1;
                 pk[2 * j] = pack_bf16(a0, a1);
@@ -864,19 +923,21 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
 }
 
 // Joins the partial sums of one (sequence, head): CTA = row, kSplit groups of 128 threads take every kSplit-th partial, a
-// thread has four of the 512 dims.  Sequences that one share covered are left alone; empty ones are written here.
+// thread has four of the 512 dims.  A group's first eight partials are fetched before their weights are known: two trips to
+// L2 (what the sequence's shares are; their partials), not three.  Sequences that one share covered are left alone; empty
+// ones are written here.
 template <int kSplit>
 __global__ void __launch_bounds__(128 * kSplit)
-decode_latent_merge(int n_seqs, int n_q, uint32_t slots, const uint32_t *__restrict__ prefix, const int32_t *__restrict__ seq_ids,
-                    DevCache c, int layer, const float2 *__restrict__ part_ml, const float *__restrict__ part_o,
-                    __nv_bfloat16 *__restrict__ out, float *__restrict__ lse) {
+decode_latent_merge(int n_seqs, int n_q, const uint4 *__restrict__ meta, const float2 *__restrict__ part_ml,
+                    const float *__restrict__ part_o, __nv_bfloat16 *__restrict__ out, float *__restrict__ lse) {
     __shared__ float s_w[kMaxSlots], s_red[4 * kSplit], s_l[4 * kSplit];
     __shared__ float4 s_o[kSplit > 1 ? (kSplit - 1) * 128 : 1];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int s = blockIdx.x / n_q, h = blockIdx.x % n_q;
     pdl_launch_dependents();
     pdl_wait();
-    const uint32_t base = prefix[s], cost = prefix[s + 1] - base, total = prefix[n_seqs];
+    const uint4 ms = meta[s], all = meta[n_seqs];
+    const uint32_t base = ms.x, cost = ms.y, n = ms.z, b0 = ms.w & 0xffffu, count = ms.w >> 16, total = all.x, slots = all.y;
     const size_t row = (size_t)s * n_q + h;
     if (cost == 0) {
         for (int d = tid; d < kLatentValueDim / 8; d += 128 * kSplit)
@@ -884,33 +945,31 @@ decode_latent_merge(int n_seqs, int n_q, uint32_t slots, const uint32_t *__restr
         if (tid == 0 && lse) lse[row] = -INFINITY;
         return;
     }
-    const size_t sl = (size_t)seq_ids[s] * c.n_layers + layer;
-    const uint32_t n = tiles_of(c.n_high[sl]) + tiles_of(c.n_low[sl]);
-    uint32_t b0 = (uint32_t)((uint64_t)base * slots / total);
-    while (slot_start(total, b0 + 1, slots) <= base) b0++;
-    uint32_t b1 = b0 + 1;
-    {   // the first share that starts at or behind the sequence's end
-        const uint32_t end = base + cost;
-        b1 = (uint32_t)(((uint64_t)end * slots + total - 1) / total);
-        while (b1 > b0 + 1 && slot_start(total, b1 - 1, slots) >= end) b1--;
-        while (b1 < slots && slot_start(total, b1, slots) < end) b1++;
+    const int part = tid >> 7, d4 = tid & 127;
+    const float4 *src = reinterpret_cast<const float4 *>(part_o) + ((size_t)(b0 + s) * n_q + h) * (kLatentValueDim / 4) + d4;
+    const size_t step = (size_t)n_q * (kLatentValueDim / 4);
+    float4 v[8];
+#pragma unroll
+    for (int k = 0; k < 8; k++) {
+        v[k] = make_float4(0, 0, 0, 0);
+        if (count > 1 && part + (uint32_t)k * kSplit < count) v[k] = src[(part + k * kSplit) * step];
     }
-    const uint32_t count = b1 - b0;
+    // rows of the sequence in share b: 0 none, 1 some, 2 all (the share has written the result)
     auto used = [&](uint32_t b) {
         const uint32_t lo = slot_start(total, b, slots), hi = slot_start(total, b + 1, slots);
-        const uint32_t v0 = lo > base ? cut_positions(lo - base, cost, n) : 0u, v1 = cut_positions(hi - base, cost, n);
-        if (v1 <= v0) return 0;
-        return v0 == 0 && v1 == n ? 2 : 1;
+        const uint32_t v0 = lo > base ? cut_positions(lo - base, cost, n) : 0u, v1 = hi > base ? cut_positions(hi - base, cost, n) : 0u;
+        return v1 <= v0 ? 0 : v0 == 0 && v1 == n ? 2 : 1;
     };
     float top = -INFINITY;
     int whole = 0;
     for (uint32_t k = tid; k < count; k += 128 * kSplit) {
         const int u = used(b0 + k);
         whole |= u == 2;
-        const float m = u ? part_ml[(size_t)(b0 + k + s) * n_q + h].x : -INFINITY;
-        if (u != 2) top = fmaxf(top, m);
+        float2 ml = make_float2(-INFINITY, 0.0f);
+        if (u == 1) ml = part_ml[(size_t)(b0 + k + s) * n_q + h];
+        top = fmaxf(top, ml.x);
     }
-    if (__syncthreads_or(whole)) return;           // written by the share itself
+    if (__syncthreads_or(whole)) return;
 #pragma unroll
     for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
     if (lane == 0) s_red[warp] = top;
@@ -936,25 +995,23 @@ decode_latent_merge(int n_seqs, int n_q, uint32_t slots, const uint32_t *__restr
 #pragma unroll
     for (int k = 0; k < 4 * kSplit; k++) lsum += s_l[k];
     float4 acc = make_float4(0, 0, 0, 0);
-    const int part = tid >> 7, d4 = tid & 127;
-    const float4 *src = reinterpret_cast<const float4 *>(part_o) + ((size_t)(b0 + s) * n_q + h) * (kLatentValueDim / 4) + d4;
-    const size_t step = (size_t)n_q * (kLatentValueDim / 4);
+    auto add = [&](const float4 &x, float wgt) {
+        if (wgt != 0.0f) { acc.x += wgt * x.x; acc.y += wgt * x.y; acc.z += wgt * x.z; acc.w += wgt * x.w; }
+    };
+#pragma unroll
+    for (int k = 0; k < 8; k++)
+        if (part + (uint32_t)k * kSplit < count) add(v[k], s_w[part + k * kSplit]);
 #pragma unroll 8
-    for (uint32_t k = part; k < count; k += kSplit) {
-        const float wgt = s_w[k];
-        if (wgt != 0.0f) {
-            const float4 v = src[k * step];
-            acc.x += wgt * v.x; acc.y += wgt * v.y; acc.z += wgt * v.z; acc.w += wgt * v.w;
-        }
-    }
+    for (uint32_t k = part + 8 * kSplit; k < count; k += kSplit)
+        if (s_w[k] != 0.0f) add(src[k * step], s_w[k]);
     if (kSplit > 1) {
         if (part > 0) s_o[(part - 1) * 128 + d4] = acc;
         __syncthreads();
         if (part > 0) return;
 #pragma unroll
         for (int k = 0; k < kSplit - 1; k++) {
-            const float4 v = s_o[k * 128 + d4];
-            acc.x += v.x; acc.y += v.y; acc.z += v.z; acc.w += v.w;
+            const float4 x = s_o[k * 128 + d4];
+            acc.x += x.x; acc.y += x.y; acc.z += x.z; acc.w += x.w;
         }
     }
     const float inv = 1.0f / lsum;
@@ -1003,12 +1060,12 @@ static size_t carve_latent(const pask_cache *c, int n_seqs, uint8_t *base, DecPa
     size_t off = 0;
     auto take = [&](size_t bytes) { const size_t at = off; off = (off + bytes + 255) / 256 * 256; return at; };
     const size_t rows = ((size_t)slots + n_seqs) * c->desc.n_q_heads;
-    const size_t o_prefix = take((size_t)(n_seqs + 1) * 4), o_ml = take(rows * sizeof(float2)), o_o = take(rows * kLatentValueDim * sizeof(float));
+    const size_t o_meta = take((size_t)(n_seqs + 1) * sizeof(uint4)), o_ml = take(rows * sizeof(float2)), o_o = take(rows * kLatentValueDim * sizeof(float));
     if (p) {
         p->groups = groups;
         p->heads = heads;
         p->slots = slots;
-        p->prefix = reinterpret_cast<uint32_t *>(base + o_prefix);
+        p->meta = reinterpret_cast<uint4 *>(base + o_meta);
         p->part_ml = reinterpret_cast<float2 *>(base + o_ml);
         p->part_o = reinterpret_cast<float *>(base + o_o);
     }
@@ -1062,11 +1119,9 @@ pask_status_t launch_decode_latent(pask_cache *c, int layer, int n_seqs, const i
     const int n_q = c->desc.n_q_heads;
     // few sequences: many partials to a row, so four groups of threads share them (one round trip to L2 brings eight)
     if (p.slots >= 16u * (uint32_t)n_seqs)
-        e = launch_pdl(decode_latent_merge<4>, dim3(n_seqs * n_q), dim3(512), 0, stream, n_seqs, n_q, p.slots, p.prefix, seq_ids, p.c, layer,
-                       p.part_ml, p.part_o, p.out, lse);
+        e = launch_pdl(decode_latent_merge<4>, dim3(n_seqs * n_q), dim3(512), 0, stream, n_seqs, n_q, p.meta, p.part_ml, p.part_o, p.out, lse);
     else
-        e = launch_pdl(decode_latent_merge<1>, dim3(n_seqs * n_q), dim3(128), 0, stream, n_seqs, n_q, p.slots, p.prefix, seq_ids, p.c, layer,
-                       p.part_ml, p.part_o, p.out, lse);
+        e = launch_pdl(decode_latent_merge<1>, dim3(n_seqs * n_q), dim3(128), 0, stream, n_seqs, n_q, p.meta, p.part_ml, p.part_o, p.out, lse);
     return e == cudaSuccess ? PASK_OK : PASK_ERR_CUDA;
 }
 

@@ -33,17 +33,13 @@ __device__ __forceinline__ bool bar_test(uint32_t bar, uint32_t parity) {       
     return ok != 0;
 }
 // false if the phase did not complete within `limit` clock cycles
-static __device__ __noinline__ bool bar_wait_slow(uint32_t bar, uint32_t parity, long long limit) {
-    const long long t0 = clock64();
-    for (;;) {
-#pragma unroll 1
-        for (int i = 0; i < 64; i++)
-            if (bar_try(bar, parity)) return true;
-        if (clock64() - t0 > limit) return false;
-    }
-}
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, long long limit) {
-    return bar_try(bar, parity) || bar_wait_slow(bar, parity, limit);
+    if (bar_try(bar, parity)) return true;
+    const long long t0 = clock64();
+    for (uint32_t n = 1;; n++) {
+        if (bar_try(bar, parity)) return true;
+        if ((n & 63u) == 0 && clock64() - t0 > limit) return false;
+    }
 }
 
 // ---- ordering between plain accesses to shared memory and the asynchronous units, and between tcgen05 operations and barriers
@@ -174,6 +170,11 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_
                  ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 
+// 16 bytes by the calling thread, `bytes` (0 or 16) of them read and the rest zeros; done after copy16_wait()
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src, int bytes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy16_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 // brings a range into L2 ahead of its copy; the same alignment rules
 __device__ __forceinline__ void bulk_prefetch(const void *src, uint32_t bytes) {
     asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src), "r"(bytes) : "memory");

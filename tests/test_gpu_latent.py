@@ -340,6 +340,8 @@ def test_decode_splits(pask, ctas):
             b.append(0, [s], [normal(g, n, 576)], [tags_of(g, n)])
     pask.pask_debug_set_attention_ctas(b.h, ctas)
     b.check_decode(0, [0, 1, 2, 3, 4], normal(g, 5, 72, 576))
+    b.check_decode(0, [1, 4, 1, 2, 1, 0, 1, 1], normal(g, 8, 72, 576))       # many short parts in a share
+    assert b.status() == 0
 
 
 def test_decode_peaked_and_rising_scores(pask):
