@@ -419,7 +419,7 @@ template <int kHeads>
 struct DecSmem {
     static constexpr int kQ = 2 * kTileBytes, kP = kQ + kHeads * 1152, kMisc = kP + kTile * 128;
     struct Misc {
-        uint64_t full[2 * kTilePages], empty[2 * kTilePages], raw[2], s_full[2], s_empty[2], q_full, q_empty, q_first, p_full, p_empty, o_free, drain;
+        uint64_t full[2], empty[2][2], raw[2], s_full[2], s_empty[2], q_full, q_empty, q_first, p_full, p_empty, o_free, drain;
         uint4 info[2];                             // of the tile whose S a stage holds: valid rows, flags, sequence
         uint32_t tmem;
         int first;
@@ -479,13 +479,12 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
         ms.first = p.n_seqs;
         ms.first_base = 0;
         for (int i = 0; i < 2; i++) {
+            bar_init(smem_u32(&ms.full[i]), 2);
+            bar_init(smem_u32(&ms.empty[i][0]), 1);
+            bar_init(smem_u32(&ms.empty[i][1]), 1);
             bar_init(smem_u32(&ms.raw[i]), 1);
             bar_init(smem_u32(&ms.s_full[i]), 2);
             bar_init(smem_u32(&ms.s_empty[i]), 4);
-        }
-        for (int i = 0; i < 2 * kTilePages; i++) {
-            bar_init(smem_u32(&ms.full[i]), 1);
-            bar_init(smem_u32(&ms.empty[i]), 1);
         }
         bar_init(smem_u32(&ms.q_full), 1);
         bar_init(smem_u32(&ms.q_empty), 1);
@@ -564,28 +563,20 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
             const uint8_t *src = (uint32_t)lane < np ? w.page(id) : nullptr;
             more = w.next();
             if (more) id = w.page_id(lane);
-            const uint32_t raw = smem_u32(&ms.raw[st]), extra = i == 0 ? p.surplus : 0u;
-#pragma unroll 1
-            for (int pg = 0; pg < kTilePages; pg++) {
-                const uint32_t slot_of = 4 * st + pg, full = smem_u32(&ms.full[slot_of]);
-                ok = ok && (i < 2 || bar_wait(smem_u32(&ms.empty[slot_of]), ((i >> 1) - 1) & 1, limit));
+            const uint32_t raw = smem_u32(&ms.raw[st]), full = smem_u32(&ms.full[st]), extra = i == 0 ? p.surplus : 0u;
+            const uint32_t dst = kv0 + st * kTileBytes + lane * kLatentHighPageBytes;
+#pragma unroll
+            for (int half = 0; half < 2; half++) {            // two pages at a time: a copy's way through the issue is long
+                ok = ok && (i < 2 || bar_wait(smem_u32(&ms.empty[st][half]), ((i >> 1) - 1) & 1, limit));
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
-                if (lane == pg) {
-                    const uint32_t dst = kv0 + slot_of * kLatentHighPageBytes;
-                    if (high) {
-                        if ((uint32_t)pg < np) {
-                            bar_expect(full, bytes + (pg == 0 ? extra : 0u));
-                            bulk_load(dst, src, bytes, full);
-                        } else {
-                            bar_arrive(full);
-                        }
-                    } else if ((uint32_t)pg < np) {
-                        if (pg == 0) bar_expect(raw, np * bytes + extra);
-                        bulk_load(dst, src, bytes, raw);
-                    }
+                const uint32_t here = np > 2u * half ? min(2u, np - 2u * half) : 0u;      // pages of this half
+                if (lane == 0) {
+                    if (high) bar_expect(full, here * bytes + (half == 0 ? extra : 0u));
+                    else if (half == 0) bar_expect(raw, np * bytes + extra);
                 }
                 __syncwarp();
+                if ((lane >> 1) == half && (uint32_t)lane < np) bulk_load(dst, src, bytes, high ? full : raw);
             }
             if (!ok) break;
             if (!high) { if (st) lows[1]++; else lows[0]++; }
@@ -602,8 +593,7 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
         if (!ok || p.surplus) {                    // gave up: let the copies in flight land (bounded) before the CTA ends
             for (int k = 0; k < 2; k++) {
                 if (lows[k]) bar_wait(smem_u32(&ms.raw[k]), (lows[k] - 1) & 1, limit);
-                if (i > (uint32_t)k)
-                    for (int pg = 0; pg < kTilePages; pg++) bar_wait(smem_u32(&ms.full[4 * k + pg]), ((i - 1 - k) >> 1) & 1, p.surplus ? 1000 : limit);
+                if (i > (uint32_t)k) bar_wait(smem_u32(&ms.full[(i - 1 - k) & 1]), ((i - 1 - k) >> 1) & 1, limit);
             }
         }
     } else if (warp == 9) {
@@ -624,19 +614,19 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
                 for (uint32_t spin = 0; !pick; spin++) {
                     if (j < i && bar_test(smem_u32(&ms.p_full), j & 1) && (!pv_first || pv_seg < 2 || bar_test(smem_u32(&ms.o_free), (pv_seg - 2) & 1)))
                         pick = 1;
-                    else if (more && i < j + 2 && bar_test(smem_u32(&ms.full[4 * st + 3]), ph) && bar_test(smem_u32(&ms.full[4 * st + 2]), ph) &&
-                             bar_test(smem_u32(&ms.full[4 * st + 1]), ph) && bar_test(smem_u32(&ms.full[4 * st]), ph) &&
+                    else if (more && i < j + 2 && bar_test(smem_u32(&ms.full[st]), ph) &&
                              (i < 2 || bar_test(smem_u32(&ms.s_empty[st]), ph ^ 1)) && (!w.first() || bar_test(smem_u32(&ms.q_full), n_seg & 1)))
                         pick = 2;
                     else if ((spin & 255) == 255 && clock64() - t0 > limit)
                         pick = 3;
                 }
             }
-            pick = __reduce_max_sync(0xffffffffu, pick);
-            if (pick == 3) { ok = false; break; }
+            // (one word over the warp, so that what the products are made from is known to be the same in every lane)
+            const uint32_t word = __reduce_max_sync(0xffffffffu, (uint32_t)pick | (i & 1) << 2 | (j & 1) << 3 | pv_pages << 4 | (pv_first ? 128u : 0u));
+            if ((word & 3) == 3) { ok = false; break; }
             fence_after();
-            if (pick == 2) {
-                const uint32_t st = __shfl_sync(0xffffffffu, i & 1, 0);
+            if ((word & 3) == 2) {
+                const uint32_t st = (word >> 2) & 1;
                 const uint32_t kv = kv0 + st * kTileBytes;
                 const uint64_t dk = desc(kv, 0, kLatentHalfPage), dq = desc(qs, 0, kLatentHalfPage);
 #pragma unroll
@@ -662,8 +652,8 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
                     after = wn.next();
                 }
             } else {
-                const uint32_t sv = __shfl_sync(0xffffffffu, j & 1, 0), np = __shfl_sync(0xffffffffu, pv_pages, 0);
-                const bool fresh = __shfl_sync(0xffffffffu, (int)pv_first, 0) != 0;
+                const uint32_t sv = (word >> 3) & 1, np = (word >> 4) & 7;
+                const bool fresh = word & 128u;
                 const uint64_t dv = desc(kv0 + sv * kTileBytes, 1024, kLatentHalfPage), dp = desc(ps, 0, 1024);
 #pragma unroll
                 for (int k = 0; k < kTilePages; k++) {
@@ -673,7 +663,7 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
                             mma_ss(tmem + kO + b * 64, dv + (uint64_t)((k * kLatentHighPageBytes + b * 2048) >> 4), dp + (uint64_t)(k * 2048 >> 4),
                                    kIdO, k > 0 || !fresh, mine);
                     }
-                    if (mine) commit(smem_u32(&ms.empty[4 * sv + k]));
+                    if ((k & 1) && mine) commit(smem_u32(&ms.empty[sv][k >> 1]));
                 }
                 if (mine) commit(smem_u32(&ms.p_empty));
                 j++;
@@ -745,7 +735,7 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
                 if (bad) break;
                 fence_async_shared();
                 group_sync(2, 128);
-                if (t < kTilePages) bar_arrive(smem_u32(&ms.full[4 * st + t]));
+                if (t < 2) bar_arrive(smem_u32(&ms.full[st]));
             }
         }
     } else {
