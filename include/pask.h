@@ -498,7 +498,8 @@ pask_status_t pask_decode_attention_latent(pask_cache_t *cache, int32_t layer, i
  *               the last dims of latent rows can be used where they lie).  Must cover total_k rows
  *   scale       positive and finite
  *   out         dev bf16 [total_q][n_heads][128];  lse  dev fp32 [total_q][n_heads] or NULL
- * Values of a sequence's rows must be finite; rows outside every sequence may hold anything. */
+ * Values of a sequence's rows must be finite; rows outside every sequence may hold anything.  A bounded wait inside the
+ * kernel that runs out (never expected) leaves NaN in the rows it concerns: there is no cache whose status word could say so. */
 pask_status_t pask_prompt_attention_latent(int32_t n_seqs, int32_t total_q, int32_t total_k, int32_t n_heads,
                                            const int32_t *cu_q, const int32_t *cu_k, const void *q, const void *kv,
                                            const void *k_rope, int32_t rope_stride, float scale, void *out,

@@ -1,50 +1,518 @@
 // pask_prompt_attention_latent: causal attention of a ragged batch of prompts (or prompt chunks behind a history) with the
 // latent rows expanded to keys and values per head.
+//
+// Per head: S = Q K^T over 192 dims (128 expanded + 64 rotary that all heads share), P = softmax(scale S), O = P V over 128
+// dims: 640 operations per (query, visible key), and a key block of 128 keys (80 KB) serves 256 queries, so the tensor core
+// bounds it: per block 2 x 12 products of 128 x 128 x 16 for S and 2 x 8 for O, 40 x 64 = 2560 cycles (tcgen05, fp32 sums in
+// tensor memory; see pask_umma.h).  The 32768 exponentials of a block take the special-function units 2048 cycles.
+//
+// A CTA works on 256 queries of one head as two tiles of 128 rows, in turn: while the softmax warps of one tile turn its S into
+// P, the tensor core works for the other.
+//   warps 0-3, 4-7   softmax of tile 0, 1: a thread has a query (its row of S in registers, no exchange between lanes); P goes
+//                    back to tensor memory over S, in bf16, as the left operand of P V.  The reference maximum of a row moves
+//                    only when a score exceeds it by more than 2^8, so that O is rarely rescaled.  Then the row's result.
+//   warp 8           products, in the order  P V of tile t, block j;  Q K^T of tile t, block j + 1;  the other tile
+//   warp 9           copies: queries, key blocks (two stages: 128 expanded and 64 rotary dims side by side), value blocks (one)
+//   warp 10          the next item: blocks of 256 queries with the most visible keys first; a CTA that is done takes over one
+//                    that has not started (cluster launch control), so the tail evens out without a counter in memory
+// Shared memory: Q 96 KB + K 2 x 48 KB + V 32 KB.  Tensor memory: S 2 x 128 columns, O 2 x 128 columns: all of it.
+#include <cuda.h>
 #include <cuda_bf16.h>
 
 #include "pask_internal.h"
+#include "pask_umma.h"
 
 namespace pask {
 
 namespace {
 
 constexpr int kNope = 128, kRope = 64, kQk = kNope + kRope, kV = 128;
+constexpr int kTileQ = 128, kBlockQ = 2 * kTileQ, kBlockK = 128;
+constexpr int kSub = kBlockK * 128;                // 128 rows x 64 dims: 16 KB
+constexpr int kQBytes = 3 * kSub, kKBytes = 3 * kSub, kVBytes = 2 * kSub;
+constexpr int kThreads = 384;
+constexpr float kLazy = 8.0f;
+constexpr long long kWaitCycles = 4000000000LL;    // bound of a wait: about two seconds
 
-// One warp per (query, head): lanes hold 6 query dims and 4 output dims.
-__global__ void __launch_bounds__(256)
-prompt_latent_kernel(int n_seqs, int total_q, int total_k, int n_heads, const int32_t *__restrict__ cu_q, const int32_t *__restrict__ cu_k,
-                     const __nv_bfloat16 *__restrict__ q, const __nv_bfloat16 *__restrict__ kv, const __nv_bfloat16 *__restrict__ rope,
-                     int rope_stride, float scale, __nv_bfloat16 *__restrict__ out, float *__restrict__ lse) {
-    const int lane = threadIdx.x & 31;
-    const long long row = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
-    if (row >= (long long)total_q * n_heads) return;
-    const int t = (int)(row / n_heads), head = (int)(row % n_heads);
-    int i = -1;
-    for (int s = 0; s < n_seqs; s++) if (t >= cu_q[s] && t < cu_q[s + 1]) { i = s; break; }
-    if (i < 0 || cu_q[i] < 0 || cu_q[i + 1] > total_q || cu_k[i] < 0 || cu_k[i + 1] < cu_k[i] || cu_k[i + 1] > total_k) return;
-    const int nq = cu_q[i + 1] - cu_q[i], nk = cu_k[i + 1] - cu_k[i], k0 = cu_k[i];
-    const int visible = min(nk, t - cu_q[i] + nk - nq + 1);
-    float qv[6], m = -INFINITY, l = 0.0f, o[4] = {0, 0, 0, 0};
-#pragma unroll
-    for (int e = 0; e < 6; e++) qv[e] = __bfloat162float(q[row * kQk + 32 * e + lane]) * scale;
-    for (int j = 0; j < visible; j++) {
-        const __nv_bfloat16 *kr = kv + ((size_t)(k0 + j) * n_heads + head) * (kNope + kV), *rr = rope + (size_t)(k0 + j) * rope_stride;
-        float s = 0.0f;
-#pragma unroll
-        for (int e = 0; e < 4; e++) s += qv[e] * __bfloat162float(kr[32 * e + lane]);
-#pragma unroll
-        for (int e = 0; e < 2; e++) s += qv[4 + e] * __bfloat162float(rr[32 * e + lane]);
-#pragma unroll
-        for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
-        const float mn = fmaxf(m, s), a = expf(m - mn), p = expf(s - mn);
-        m = mn;
-        l = l * a + p;
-#pragma unroll
-        for (int e = 0; e < 4; e++) o[e] = o[e] * a + p * __bfloat162float(kr[kNope + 32 * e + lane]);
+struct PromptParams {
+    int n_seqs, total_q, total_k, n_heads;
+    const int32_t *cu_q, *cu_k;
+    float scale_log2;
+    __nv_bfloat16 *out;
+    float *lse;
+};
+
+struct Item {
+    int q0, nq, k0, nk, head;                      // first row of the sequence, rows; the same of its keys
+    int block;                                     // 256-query block of the sequence; -1: no further item
+};
+
+struct __align__(16) PromptSmem {
+    uint8_t q[2][kQBytes], k[2][kKBytes], v[kVBytes];
+    uint64_t q_full, q_empty, k_full[2], k_empty[2], v_full, v_empty, s_full[2], p_full[2], pv_done[2], o_free[2];
+    uint64_t item_full[2], item_empty[2], steal, drain;
+    uint4 answer;
+    Item item[2];
+    uint32_t tmem;
+};
+
+// visible keys of the query at position i of its sequence
+__device__ __forceinline__ int visible(const Item &it, int i) { return max(0, min(it.nk, i + 1 + it.nk - it.nq)); }
+// key blocks tile t of the item looks at
+__device__ __forceinline__ int key_blocks(const Item &it, int t) {
+    const int i0 = it.block * kBlockQ + t * kTileQ;
+    if (i0 >= it.nq) return 0;
+    return (visible(it, min(it.nq, i0 + kTileQ) - 1) + kBlockK - 1) / kBlockK;
+}
+
+// The item of grid position x, worked out by a warp: position r = x / heads among the blocks of 256 queries, head x % heads.
+// Up to 32 sequences (one a lane): blocks in the order of their visible keys, most first.  More: in the order of the batch.
+struct Ranker {
+    int nq = 0, nk = 0, q0 = 0, k0 = 0;            // of sequence `lane`
+    __device__ __forceinline__ static bool load(const PromptParams &p, int s, int &q0, int &nq, int &k0, int &nk) {
+        q0 = p.cu_q[s]; k0 = p.cu_k[s];
+        nq = p.cu_q[s + 1] - q0; nk = p.cu_k[s + 1] - k0;
+        if (q0 >= 0 && nq >= 0 && q0 + nq <= p.total_q && k0 >= 0 && nk >= 0 && k0 + nk <= p.total_k) return true;
+        nq = nk = 0;                               // malformed: not written
+        return false;
     }
+    __device__ __forceinline__ void init(const PromptParams &p, int lane) {
+        if (p.n_seqs <= 32 && lane < p.n_seqs) load(p, lane, q0, nq, k0, nk);
+    }
+    // blocks of this lane's sequence with at least t key blocks
+    __device__ __forceinline__ int at_least(int t) const {
+        const int nb = (nq + kBlockQ - 1) / kBlockQ;
+        if (t <= 0) return nb;
+        const long long y = 128LL * (t - 1) - (nk - nq);
+        if (y < 0) return nb;
+        return y >= nq ? 0 : nb - (int)(y / kBlockQ);
+    }
+    __device__ __forceinline__ bool find(const PromptParams &p, int x, int lane, Item &it) const {
+        const int r = x / p.n_heads;
+        it.head = x - r * p.n_heads;
+        if (p.n_seqs <= 32) {
+            if (r >= __reduce_add_sync(0xffffffffu, at_least(0))) return false;
+            int lo = 0, hi = (p.total_k + kBlockK - 1) / kBlockK;      // the largest t that more than r blocks reach
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if (__reduce_add_sync(0xffffffffu, at_least(mid)) > r) lo = mid; else hi = mid - 1;
+            }
+            const int above = at_least(lo + 1), here = at_least(lo) - above;
+            const int skip = r - __reduce_add_sync(0xffffffffu, above);
+            int inc = here;
 #pragma unroll
-    for (int e = 0; e < 4; e++) out[row * kV + 32 * e + lane] = __float2bfloat16_rn(visible > 0 ? o[e] / l : 0.0f);
-    if (lane == 0 && lse) lse[row] = visible > 0 ? m + logf(l) : -INFINITY;
+            for (int d = 1; d < 32; d <<= 1) {
+                const int o = __shfl_up_sync(0xffffffffu, inc, d);
+                if (lane >= d) inc += o;
+            }
+            const int owner = __ffs(__ballot_sync(0xffffffffu, inc > skip)) - 1;
+            // fewer keys come first in a sequence: its blocks with lo key blocks are the ones before those with more
+            const int block = (nq + kBlockQ - 1) / kBlockQ - above - 1 - (skip - (inc - here));
+            it.block = __shfl_sync(0xffffffffu, block, owner);
+            it.q0 = __shfl_sync(0xffffffffu, q0, owner);
+            it.nq = __shfl_sync(0xffffffffu, nq, owner);
+            it.k0 = __shfl_sync(0xffffffffu, k0, owner);
+            it.nk = __shfl_sync(0xffffffffu, nk, owner);
+            return true;
+        }
+        const int per = (p.n_seqs + 31) / 32, s0 = min(lane * per, p.n_seqs), s1 = min(s0 + per, p.n_seqs);
+        int a, b, c, d, sum = 0;
+        for (int s = s0; s < s1; s++) { load(p, s, a, b, c, d); sum += (b + kBlockQ - 1) / kBlockQ; }
+        int inc = sum;
+#pragma unroll
+        for (int e = 1; e < 32; e <<= 1) {
+            const int o = __shfl_up_sync(0xffffffffu, inc, e);
+            if (lane >= e) inc += o;
+        }
+        const uint32_t reach = __ballot_sync(0xffffffffu, inc > r);
+        if (!reach) return false;
+        const int owner = __ffs(reach) - 1;
+        Item mine = {};
+        if (lane == owner) {
+            int left = r - (inc - sum);
+            for (int s = s0; s < s1; s++) {
+                load(p, s, a, b, c, d);
+                const int nb = (b + kBlockQ - 1) / kBlockQ;
+                if (left < nb) { mine.q0 = a; mine.nq = b; mine.k0 = c; mine.nk = d; mine.block = left; break; }
+                left -= nb;
+            }
+        }
+        it.block = __shfl_sync(0xffffffffu, mine.block, owner);
+        it.q0 = __shfl_sync(0xffffffffu, mine.q0, owner);
+        it.nq = __shfl_sync(0xffffffffu, mine.nq, owner);
+        it.k0 = __shfl_sync(0xffffffffu, mine.k0, owner);
+        it.nk = __shfl_sync(0xffffffffu, mine.nk, owner);
+        return true;
+    }
+};
+
+__global__ void __launch_bounds__(kThreads, 1)
+prompt_latent_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CUtensorMap map_q,
+                     const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ CUtensorMap map_rope) {
+    using namespace umma;
+    extern __shared__ uint8_t s_raw[];
+    PromptSmem &sm = *reinterpret_cast<PromptSmem *>(((uintptr_t)s_raw + 1023) & ~(uintptr_t)1023);
+    const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
+    if (tid == 0) {
+        bar_init(smem_u32(&sm.q_full), 1);
+        bar_init(smem_u32(&sm.q_empty), 1);
+        bar_init(smem_u32(&sm.v_full), 1);
+        bar_init(smem_u32(&sm.v_empty), 1);
+        bar_init(smem_u32(&sm.steal), 1);
+        bar_init(smem_u32(&sm.drain), 1);
+        for (int i = 0; i < 2; i++) {
+            bar_init(smem_u32(&sm.k_full[i]), 1);
+            bar_init(smem_u32(&sm.k_empty[i]), 1);
+            bar_init(smem_u32(&sm.s_full[i]), 1);
+            bar_init(smem_u32(&sm.p_full[i]), 4);
+            bar_init(smem_u32(&sm.pv_done[i]), 1);
+            bar_init(smem_u32(&sm.o_free[i]), 4);
+            bar_init(smem_u32(&sm.item_full[i]), 1);
+            bar_init(smem_u32(&sm.item_empty[i]), 10);
+        }
+        bar_init_fence();
+    }
+    if (warp == 8) tmem_alloc(smem_u32(&sm.tmem), 512);
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = sm.tmem;
+    constexpr uint32_t kS = 0, kO = 256;           // columns of tile 0; tile 1 is 128 behind
+    bool ok = true;
+    // the CTA's n-th item; false behind the last one or after a wait ran out
+    auto next_item = [&](uint32_t n, Item &it) {
+        const uint32_t slot = n & 1;
+        ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.item_full[slot]), (n >> 1) & 1, kWaitCycles)) && ok;
+        if (!ok) return false;
+        it = sm.item[slot];
+        __syncwarp();
+        if (lane == 0) bar_arrive(smem_u32(&sm.item_empty[slot]));
+        return it.block >= 0;
+    };
+
+    if (warp == 10) {
+        // ================================================= items
+        Ranker rank;
+        rank.init(p, lane);
+        int x = (int)blockIdx.x;
+        uint32_t asked = 0;
+        bool live = true;
+        for (uint32_t n = 0; live; n++) {
+            const uint32_t slot = n & 1;
+            Item it;
+            live = x >= 0 && rank.find(p, x, lane, it);
+            if (!live) it.block = -1;
+            if (n >= 2) ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.item_empty[slot]), ((n >> 1) - 1) & 1, kWaitCycles));
+            if (!ok) break;
+            if (lane == 0) {
+                sm.item[slot] = it;
+                bar_arrive(smem_u32(&sm.item_full[slot]));
+            }
+            if (!live) break;
+            if (lane == 0) {
+                bar_expect(smem_u32(&sm.steal), 16);
+                steal_ask(smem_u32(&sm.answer), smem_u32(&sm.steal));
+            }
+            ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.steal), asked++ & 1, kWaitCycles));
+            if (!ok) break;
+            x = steal_answer(smem_u32(&sm.answer));
+            __syncwarp();
+            fence_async_shared();                  // the answer has been read before the next one is asked for
+        }
+    } else if (warp == 9) {
+        // ================================================= copies
+        Item it;
+        uint32_t kc = 0, vc = 0, qc = 0;           // key blocks, value blocks, items with queries copied so far
+        const uint32_t qf = smem_u32(&sm.q_full), vf = smem_u32(&sm.v_full);
+        for (uint32_t n = 0; next_item(n, it); n++) {
+            const int n0 = key_blocks(it, 0), n1 = key_blocks(it, 1), nb = max(n0, n1);
+            if (nb == 0) continue;
+            if (qc > 0) ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.q_empty), (qc - 1) & 1, kWaitCycles));
+            if (!ok) break;
+            qc++;
+            const bool mine = elect_one();
+            if (mine) {
+                bar_expect(qf, (n0 ? kQBytes : 0) + (n1 ? kQBytes : 0));
+                for (int t = 0; t < 2; t++)
+                    if (t ? n1 : n0)
+                        for (int c = 0; c < 3; c++)
+                            tile_load3(smem_u32(sm.q[t]) + c * kSub, &map_q, 64 * c, it.head, it.q0 + it.block * kBlockQ + t * kTileQ, qf);
+            }
+            for (int j = 0; j <= nb; j++) {        // keys of block j, then values of the block before
+                if (j < nb) {
+                    const uint32_t st = kc & 1, kf = smem_u32(&sm.k_full[st]);
+                    if (kc >= 2) ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.k_empty[st]), ((kc >> 1) - 1) & 1, kWaitCycles));
+                    if (!ok) break;
+                    if (mine) {
+                        bar_expect(kf, kKBytes);
+                        const int row = it.k0 + j * kBlockK;
+                        tile_load3(smem_u32(sm.k[st]), &map_kv, 0, it.head, row, kf);
+                        tile_load3(smem_u32(sm.k[st]) + kSub, &map_kv, 64, it.head, row, kf);
+                        tile_load2(smem_u32(sm.k[st]) + 2 * kSub, &map_rope, 0, row, kf);
+                    }
+                    kc++;
+                }
+                if (j > 0) {
+                    if (vc >= 1) ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.v_empty), (vc - 1) & 1, kWaitCycles));
+                    if (!ok) break;
+                    if (mine) {
+                        bar_expect(vf, kVBytes);
+                        tile_load3(smem_u32(sm.v), &map_kv, kNope, it.head, it.k0 + (j - 1) * kBlockK, vf);
+                        tile_load3(smem_u32(sm.v) + kSub, &map_kv, kNope + 64, it.head, it.k0 + (j - 1) * kBlockK, vf);
+                    }
+                    vc++;
+                }
+            }
+            if (!ok) break;
+        }
+        if (!ok) {                                 // gave up: let the copies in flight land (bounded) before the CTA ends
+            if (qc) bar_wait(qf, (qc - 1) & 1, kWaitCycles);
+            if (vc) bar_wait(vf, (vc - 1) & 1, kWaitCycles);
+            for (uint32_t b = kc > 2 ? kc - 2 : 0; b < kc; b++) bar_wait(smem_u32(&sm.k_full[b & 1]), (b >> 1) & 1, kWaitCycles);
+        }
+    } else if (warp == 8) {
+        // ================================================= products
+        constexpr uint32_t kIdS = instr(kTileQ, kBlockK, false, false), kIdO = instr(kTileQ, kV, false, true);
+        const bool mine = elect_one();
+        const uint64_t dq = desc(smem_u32(sm.q[0]), 0, 1024), dk = desc(smem_u32(sm.k[0]), 0, 1024), dv = desc(smem_u32(sm.v), kSub, 1024);
+        Item it;
+        uint32_t kc = 0, vc = 0, qc = 0, pc[2] = {0, 0}, oc[2] = {0, 0};   // ... weights and items of each tile so far
+        auto scores = [&](int t, uint32_t st) {
+            const uint64_t a = dq + (uint64_t)(t * kQBytes >> 4), b = dk + (uint64_t)(st * kKBytes >> 4);
+#pragma unroll
+            for (int k = 0; k < kQk / 16; k++) {
+                const uint64_t off = (uint64_t)(((k >> 2) * kSub + (k & 3) * 32) >> 4);
+                mma_ss(tmem + kS + t * 128, a + off, b + off, kIdS, k > 0, mine);
+            }
+            if (mine) commit(smem_u32(&sm.s_full[t]));
+        };
+        auto values = [&](int t, bool first, int steps) {
+#pragma unroll
+            for (int k = 0; k < kBlockK / 16; k++)
+                if (k < steps) mma_ts(tmem + kO + t * 128, tmem + kS + t * 128 + k * 8, dv + (uint64_t)(k * 2048 >> 4), kIdO, k > 0 || !first, mine);
+            if (mine) commit(smem_u32(&sm.pv_done[t]));
+        };
+        for (uint32_t n = 0; next_item(n, it); n++) {
+            const int nt[2] = {key_blocks(it, 0), key_blocks(it, 1)}, nb = max(nt[0], nt[1]);
+            if (nb == 0) continue;
+            ok = bar_wait(smem_u32(&sm.q_full), qc & 1, kWaitCycles);
+            qc++;
+            ok = bar_wait(smem_u32(&sm.k_full[kc & 1]), (kc >> 1) & 1, kWaitCycles) && ok;
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            fence_after();
+            {
+                const uint32_t st = __shfl_sync(0xffffffffu, kc & 1, 0);
+                if (nt[0]) scores(0, st);
+                if (nt[1]) scores(1, st);
+                if (mine) commit(smem_u32(&sm.k_empty[st]));
+                kc++;
+                if (nb == 1 && mine) commit(smem_u32(&sm.q_empty));
+            }
+            for (int j = 0; j < nb && ok; j++) {
+                const int valid = __shfl_sync(0xffffffffu, min(kBlockK, it.nk - j * kBlockK), 0), steps = (valid + 15) / 16;
+                const uint32_t st = __shfl_sync(0xffffffffu, kc & 1, 0);
+                bool have_v = false, have_k = false;
+#pragma unroll
+                for (int t = 0; t < 2; t++) {
+                    if (j < nt[t]) {
+                        if (!have_v) {
+                            ok = bar_wait(smem_u32(&sm.v_full), vc & 1, kWaitCycles) && ok;
+                            ok = __all_sync(0xffffffffu, ok);
+                            if (!ok) break;
+                            if (valid & 15) {      // rows behind the last key in its step of 16: whatever they hold counts as zero
+                                const int rows = 16 * steps - valid;
+                                for (int e = lane; e < rows * 16; e += 32) {
+                                    const int r = valid + (e >> 4), ch = e & 15;
+                                    *reinterpret_cast<uint4 *>(sm.v + (ch >> 3) * kSub + r * 128 + (ch & 7) * 16) = make_uint4(0, 0, 0, 0);
+                                }
+                                fence_async_shared();
+                                __syncwarp();
+                            }
+                            have_v = true;
+                        }
+                        ok = bar_wait(smem_u32(&sm.p_full[t]), pc[t] & 1, kWaitCycles) && ok;
+                        pc[t]++;
+                        if (j == 0) {              // the item before has been read out of O
+                            if (oc[t] > 0) ok = bar_wait(smem_u32(&sm.o_free[t]), (oc[t] - 1) & 1, kWaitCycles) && ok;
+                            oc[t]++;
+                        }
+                        ok = __all_sync(0xffffffffu, ok);
+                        if (!ok) break;
+                        fence_after();
+                        values(t, j == 0, steps);
+                    }
+                    if (j + 1 < nt[t]) {
+                        if (!have_k) {
+                            ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.k_full[st]), (kc >> 1) & 1, kWaitCycles) && ok);
+                            if (!ok) break;
+                            fence_after();
+                            have_k = true;
+                        }
+                        scores(t, st);
+                    }
+                }
+                if (!ok) break;
+                if (mine) commit(smem_u32(&sm.v_empty));
+                vc++;
+                if (j + 1 < nb) {
+                    if (mine) {
+                        commit(smem_u32(&sm.k_empty[st]));
+                        if (j + 2 == nb) commit(smem_u32(&sm.q_empty));
+                    }
+                    kc++;
+                }
+            }
+            if (!ok) break;
+        }
+        if (!ok) {                                 // gave up: the products in flight end before tensor memory is freed
+            if (mine) commit(smem_u32(&sm.drain));
+            bar_wait(smem_u32(&sm.drain), 0, kWaitCycles);
+        }
+        __syncwarp();
+    } else if (warp < 8) {
+        // ================================================= softmax: thread = query
+        const int t = warp >> 2;
+        const uint32_t base = tmem + ((uint32_t)((warp & 3) * 32) << 16) + t * 128;
+        const uint32_t s_full = smem_u32(&sm.s_full[t]), p_full = smem_u32(&sm.p_full[t]), pv_done = smem_u32(&sm.pv_done[t]);
+        Item it;
+        // a wait ran out (never expected): the row's result says so
+        auto spoil = [&](const Item &at, int i) {
+            if (i >= at.nq) return;
+            const size_t row = (size_t)(at.q0 + i) * p.n_heads + at.head;
+            for (int d = 0; d < kV; d++) p.out[row * kV + d] = __ushort_as_bfloat16((unsigned short)0x7FC0);
+            if (p.lse) p.lse[row] = __int_as_float(0x7FC00000);
+        };
+        uint32_t sc = 0;                           // blocks of this tile so far (S, P and P V alike)
+        for (uint32_t n = 0; next_item(n, it); n++) {
+            const int nb = key_blocks(it, t), i = it.block * kBlockQ + t * kTileQ + (warp & 3) * 32 + lane;
+            const int vis = i < it.nq ? visible(it, i) : 0;
+            float m = -INFINITY, l = 0.0f;
+            for (int j = 0; j < nb; j++, sc++) {
+                ok = bar_wait(s_full, sc & 1, ok ? kWaitCycles : 0) && ok;
+                if (!__all_sync(0xffffffffu, ok)) break;
+                fence_after();
+                float x[128];
+#pragma unroll
+                for (int c = 0; c < 4; c++) {
+                    uint32_t r[32];
+                    tmem_ld32(base + kS + 32 * c, r);
+#pragma unroll
+                    for (int e = 0; e < 32; e++) x[32 * c + e] = __uint_as_float(r[e]);
+                }
+                tmem_wait_ld();
+                const int left = vis - j * kBlockK;
+                if (__any_sync(0xffffffffu, left < kBlockK)) {
+#pragma unroll
+                    for (int e = 0; e < 128; e++) if (e >= left) x[e] = -INFINITY;
+                }
+                float top = -INFINITY;
+                {
+                    float a = x[0], b = x[1], c = x[2], d = x[3];
+#pragma unroll
+                    for (int e = 4; e < 128; e += 4) {
+                        a = fmaxf(a, x[e]); b = fmaxf(b, x[e + 1]); c = fmaxf(c, x[e + 2]); d = fmaxf(d, x[e + 3]);
+                    }
+                    top = fmaxf(fmaxf(a, b), fmaxf(c, d)) * p.scale_log2;
+                }
+                const bool raise = top > m + kLazy;
+                if (__any_sync(0xffffffffu, raise)) {
+                    const float f = raise ? ex2(m - top) : 1.0f;
+                    if (raise) { m = top; l *= f; }
+                    if (j > 0) {                   // O so far, in the new reference
+                        ok = bar_wait(pv_done, (sc - 1) & 1, ok ? kWaitCycles : 0) && ok;
+                        __syncwarp();
+                        fence_after();
+#pragma unroll 1
+                        for (int c = 0; c < 8; c++) {
+                            uint32_t r[16];
+                            tmem_ld16(base + kO + 16 * c, r);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int e = 0; e < 16; e++) r[e] = __float_as_uint(__uint_as_float(r[e]) * f);
+                            tmem_st16(base + kO + 16 * c, r);
+                        }
+                    }
+                }
+                const float ref = m == -INFINITY ? 0.0f : m;               // a row that has seen no key yet
+                float l0 = 0.0f, l1 = 0.0f;
+#pragma unroll
+                for (int c = 0; c < 4; c++) {
+                    uint32_t r[16];
+#pragma unroll
+                    for (int e = 0; e < 16; e++) {
+                        const float a = ex2(__fmaf_rn(x[32 * c + 2 * e], p.scale_log2, -ref)), b = ex2(__fmaf_rn(x[32 * c + 2 * e + 1], p.scale_log2, -ref));
+                        l0 += a;
+                        l1 += b;
+                        r[e] = pack_bf16(a, b);
+                    }
+                    tmem_st16(base + kS + 16 * c, r);
+                }
+                l += l0 + l1;
+                tmem_wait_st();
+                fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(p_full);
+            }
+            if (!__all_sync(0xffffffffu, ok)) { spoil(it, i); break; }
+            // ---- the row's result
+            if (nb > 0) {
+                ok = bar_wait(pv_done, (sc - 1) & 1, kWaitCycles);
+                if (!__all_sync(0xffffffffu, ok)) { spoil(it, i); break; }
+                fence_after();
+            }
+            const size_t row = (size_t)(it.q0 + i) * p.n_heads + it.head;
+            const float inv = vis > 0 ? 1.0f / l : 0.0f;
+#pragma unroll
+            for (int c = 0; c < 8; c++) {
+                uint32_t r[16];
+#pragma unroll
+                for (int e = 0; e < 16; e++) r[e] = 0;
+                if (nb > 0) {
+                    tmem_ld16(base + kO + 16 * c, r);
+                    tmem_wait_ld();
+                }
+                if (i < it.nq) {
+                    uint4 *dst = reinterpret_cast<uint4 *>(p.out + row * kV + 16 * c);
+#pragma unroll
+                    for (int h = 0; h < 2; h++) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int e = 0; e < 4; e++) {
+                            const float a = __uint_as_float(r[8 * h + 2 * e]) * inv, b = __uint_as_float(r[8 * h + 2 * e + 1]) * inv;
+                            w[e] = vis > 0 ? pack_bf16(a, b) : 0u;
+                        }
+                        dst[h] = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+                }
+            }
+            if (i < it.nq && p.lse) p.lse[row] = vis > 0 ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
+            if (nb > 0) {
+                fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(smem_u32(&sm.o_free[t]));
+            }
+        }
+    }
+    fence_before();
+    __syncthreads();
+    fence_after();
+    if (warp == 8) tmem_free(tmem, 512);
+}
+
+using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                 const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// rows of 64-dim pieces: dims {inner, heads, rows} (or {inner, rows}), a box of 64 x 1 x 128 with the 128-byte swizzle
+bool encode(EncodeTiled fn, CUtensorMap *map, const void *base, int inner, int heads, int rows, size_t head_stride, size_t row_stride) {
+    const int rank = heads ? 3 : 2;
+    const cuuint64_t dims3[3] = {(cuuint64_t)inner, (cuuint64_t)heads, (cuuint64_t)rows}, dims2[2] = {(cuuint64_t)inner, (cuuint64_t)rows};
+    const cuuint64_t str3[2] = {head_stride, row_stride}, str2[1] = {row_stride};
+    const cuuint32_t box3[3] = {64, 1, kBlockK}, box2[2] = {64, kBlockK}, one[3] = {1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void *>(base), rank == 3 ? dims3 : dims2,
+              rank == 3 ? str3 : str2, rank == 3 ? box3 : box2, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 }  // namespace
@@ -52,11 +520,34 @@ prompt_latent_kernel(int n_seqs, int total_q, int total_k, int n_heads, const in
 pask_status_t launch_prompt_latent(int n_seqs, int total_q, int total_k, int n_heads, const int32_t *cu_q, const int32_t *cu_k,
                                    const void *q, const void *kv, const void *k_rope, int rope_stride, float scale, void *out,
                                    float *lse, cudaStream_t stream) {
-    const long long ctas = ((long long)total_q * n_heads + 7) / 8;
-    if (ctas > 0x7fffffffLL) return PASK_ERR_INVALID_ARG;
-    prompt_latent_kernel<<<(int)ctas, 256, 0, stream>>>(n_seqs, total_q, total_k, n_heads, cu_q, cu_k, static_cast<const __nv_bfloat16 *>(q),
-                                                        static_cast<const __nv_bfloat16 *>(kv), static_cast<const __nv_bfloat16 *>(k_rope),
-                                                        rope_stride, scale, static_cast<__nv_bfloat16 *>(out), lse);
+    static EncodeTiled encode_fn = nullptr;
+    if (!encode_fn) {
+        void *fn = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found) != cudaSuccess || !fn ||
+            found != cudaDriverEntryPointSuccess)
+            return PASK_ERR_CUDA;
+        encode_fn = reinterpret_cast<EncodeTiled>(fn);
+    }
+    constexpr int kSmem = (int)sizeof(PromptSmem) + 1024;
+    static_assert(kSmem <= 232448, "shared memory of a CTA");
+    static bool granted[64] = {};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return PASK_ERR_CUDA;
+    if (!granted[dev]) {
+        if (cudaFuncSetAttribute(prompt_latent_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess) return PASK_ERR_CUDA;
+        granted[dev] = true;
+    }
+    CUtensorMap map_q{}, map_kv{}, map_rope{};
+    if (!encode(encode_fn, &map_q, q, kQk, n_heads, total_q, kQk * 2, (size_t)n_heads * kQk * 2)) return PASK_ERR_CUDA;
+    if (total_k > 0 &&
+        (!encode(encode_fn, &map_kv, kv, kNope + kV, n_heads, total_k, (kNope + kV) * 2, (size_t)n_heads * (kNope + kV) * 2) ||
+         !encode(encode_fn, &map_rope, k_rope, kRope, 0, total_k, 0, (size_t)rope_stride * 2)))
+        return PASK_ERR_CUDA;
+    const long long items = ((long long)total_q / kBlockQ + n_seqs) * n_heads;
+    if (items > 0x7fffffffLL) return PASK_ERR_INVALID_ARG;
+    const PromptParams p{n_seqs, total_q, total_k, n_heads, cu_q, cu_k, scale * 1.4426950408889634f, static_cast<__nv_bfloat16 *>(out), lse};
+    prompt_latent_kernel<<<(int)items, kThreads, kSmem, stream>>>(p, map_q, map_kv, map_rope);
     return cudaGetLastError() == cudaSuccess ? PASK_OK : PASK_ERR_CUDA;
 }
 
