@@ -12,10 +12,12 @@
 //                    back to tensor memory over S, in bf16, as the left operand of P V.  The reference maximum of a row moves
 //                    only when a score exceeds it by more than 2^8, so that O is rarely rescaled.  Then the row's result.
 //   warp 8           products, in the order  P V of tile t, block j;  Q K^T of tile t, block j + 1;  the other tile
-//   warp 9           copies: queries, key blocks (two stages: 128 expanded and 64 rotary dims side by side), value blocks (one)
+//   warp 9           copies: queries; key blocks (three pieces of 16 KB: 128 expanded and 64 rotary dims) and value blocks (two
+//                    pieces of 64 keys) in turn into a ring of eight pieces: a block's keys and values and the next one's keys
 //   warp 10          the next item: blocks of 256 queries with the most visible keys first; a CTA that is done takes over one
 //                    that has not started (cluster launch control), so the tail evens out without a counter in memory
-// Shared memory: Q 96 KB + K 2 x 48 KB + V 32 KB.  Tensor memory: S 2 x 128 columns, O 2 x 128 columns: all of it.
+// Shared memory: Q 96 KB + ring 128 KB.  (Two stages of keys and one of values in the same space let P V wait for the copy of
+// its values, which can only start when the product before it is done: 4516 cycles a block against 3500.)  Tensor memory: S 2 x 128 columns, O 2 x 128 columns: all of it.
 #include <cuda.h>
 #include <cuda_bf16.h>
 
@@ -29,7 +31,7 @@ namespace {
 constexpr int kNope = 128, kRope = 64, kQk = kNope + kRope, kV = 128;
 constexpr int kTileQ = 128, kBlockQ = 2 * kTileQ, kBlockK = 128;
 constexpr int kSub = kBlockK * 128;                // 128 rows x 64 dims: 16 KB
-constexpr int kQBytes = 3 * kSub, kKBytes = 3 * kSub, kVBytes = 2 * kSub;
+constexpr int kQBytes = 3 * kSub, kKBytes = 3 * kSub, kVBytes = 2 * kSub, kRing = 8;
 constexpr int kThreads = 384;
 constexpr float kLazy = 8.0f;
 constexpr long long kWaitCycles = 4000000000LL;    // bound of a wait: about two seconds
@@ -48,8 +50,8 @@ struct Item {
 };
 
 struct __align__(16) PromptSmem {
-    uint8_t q[2][kQBytes], k[2][kKBytes], v[kVBytes];
-    uint64_t q_full, q_empty, k_full[2], k_empty[2], v_full, v_empty, s_full[2], p_full[2], pv_done[2], o_free[2];
+    uint8_t q[2][kQBytes], ring[kRing * kSub];     // block g of the CTA: keys in pieces 5 g .. + 2, values in 5 g + 3, 5 g + 4 (mod 8)
+    uint64_t q_full, q_empty, k_full[2], k_empty[2], v_full[2], v_half[2], v_empty[2], s_full[2], p_half[2], p_full[2], pv_done[2], o_free[2];
     uint64_t item_full[2], item_empty[2], steal, drain;
     uint4 answer;
     Item item[2];
@@ -148,7 +150,8 @@ struct Ranker {
 
 __global__ void __launch_bounds__(kThreads, 1)
 prompt_latent_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CUtensorMap map_q,
-                     const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ CUtensorMap map_rope) {
+                     const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ CUtensorMap map_v,
+                     const __grid_constant__ CUtensorMap map_rope) {
     using namespace umma;
     extern __shared__ uint8_t s_raw[];
     PromptSmem &sm = *reinterpret_cast<PromptSmem *>(((uintptr_t)s_raw + 1023) & ~(uintptr_t)1023);
@@ -156,14 +159,16 @@ prompt_latent_kernel(const __grid_constant__ PromptParams p, const __grid_consta
     if (tid == 0) {
         bar_init(smem_u32(&sm.q_full), 1);
         bar_init(smem_u32(&sm.q_empty), 1);
-        bar_init(smem_u32(&sm.v_full), 1);
-        bar_init(smem_u32(&sm.v_empty), 1);
         bar_init(smem_u32(&sm.steal), 1);
         bar_init(smem_u32(&sm.drain), 1);
         for (int i = 0; i < 2; i++) {
             bar_init(smem_u32(&sm.k_full[i]), 1);
             bar_init(smem_u32(&sm.k_empty[i]), 1);
+            bar_init(smem_u32(&sm.v_full[i]), 1);
+            bar_init(smem_u32(&sm.v_half[i]), 1);
+            bar_init(smem_u32(&sm.v_empty[i]), 1);
             bar_init(smem_u32(&sm.s_full[i]), 1);
+            bar_init(smem_u32(&sm.p_half[i]), 4);
             bar_init(smem_u32(&sm.p_full[i]), 4);
             bar_init(smem_u32(&sm.pv_done[i]), 1);
             bar_init(smem_u32(&sm.o_free[i]), 4);
@@ -190,6 +195,9 @@ prompt_latent_kernel(const __grid_constant__ PromptParams p, const __grid_consta
         return it.block >= 0;
     };
 
+    // 384 threads x 168 registers at launch = 128 x (2 x 200 + 104): the rows of S in the softmax threads need the larger share
+    if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
     if (warp == 10) {
         // ================================================= items
         Ranker rank;
@@ -222,8 +230,8 @@ prompt_latent_kernel(const __grid_constant__ PromptParams p, const __grid_consta
     } else if (warp == 9) {
         // ================================================= copies
         Item it;
-        uint32_t kc = 0, vc = 0, qc = 0;           // key blocks, value blocks, items with queries copied so far
-        const uint32_t qf = smem_u32(&sm.q_full), vf = smem_u32(&sm.v_full);
+        uint32_t g = 0, qc = 0;                    // blocks, items with queries copied so far
+        const uint32_t qf = smem_u32(&sm.q_full), ring = smem_u32(sm.ring);
         for (uint32_t n = 0; next_item(n, it); n++) {
             const int n0 = key_blocks(it, 0), n1 = key_blocks(it, 1), nb = max(n0, n1);
             if (nb == 0) continue;
@@ -238,129 +246,138 @@ prompt_latent_kernel(const __grid_constant__ PromptParams p, const __grid_consta
                         for (int c = 0; c < 3; c++)
                             tile_load3(smem_u32(sm.q[t]) + c * kSub, &map_q, 64 * c, it.head, it.q0 + it.block * kBlockQ + t * kTileQ, qf);
             }
-            for (int j = 0; j <= nb; j++) {        // keys of block j, then values of the block before
-                if (j < nb) {
-                    const uint32_t st = kc & 1, kf = smem_u32(&sm.k_full[st]);
-                    if (kc >= 2) ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.k_empty[st]), ((kc >> 1) - 1) & 1, kWaitCycles));
-                    if (!ok) break;
-                    if (mine) {
-                        bar_expect(kf, kKBytes);
-                        const int row = it.k0 + j * kBlockK;
-                        tile_load3(smem_u32(sm.k[st]), &map_kv, 0, it.head, row, kf);
-                        tile_load3(smem_u32(sm.k[st]) + kSub, &map_kv, 64, it.head, row, kf);
-                        tile_load2(smem_u32(sm.k[st]) + 2 * kSub, &map_rope, 0, row, kf);
-                    }
-                    kc++;
+            for (int j = 0; j < nb; j++, g++) {
+                // keys, piece by piece: over the last piece of the keys two blocks before, over that block's values as their halves
+                // are done with (one piece takes 16 KB of copy time from a freed place to the product that waits for it, not 48)
+                const uint32_t st = g & 1, row = (uint32_t)(it.k0 + j * kBlockK), kf = smem_u32(&sm.k_full[st]), ph = ((g >> 1) - 1) & 1;
+                if (g >= 2) ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.k_empty[st]), ph, kWaitCycles));
+                if (!ok) break;
+                if (mine) {
+                    bar_expect(kf, kKBytes);
+                    tile_load3(ring + ((5 * g) & 7) * kSub, &map_kv, 0, it.head, row, kf);
                 }
-                if (j > 0) {
-                    if (vc >= 1) ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.v_empty), (vc - 1) & 1, kWaitCycles));
-                    if (!ok) break;
-                    if (mine) {
-                        bar_expect(vf, kVBytes);
-                        tile_load3(smem_u32(sm.v), &map_kv, kNope, it.head, it.k0 + (j - 1) * kBlockK, vf);
-                        tile_load3(smem_u32(sm.v) + kSub, &map_kv, kNope + 64, it.head, it.k0 + (j - 1) * kBlockK, vf);
-                    }
-                    vc++;
+                if (g >= 2) ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.v_half[st]), ph, kWaitCycles));
+                if (!ok) break;
+                if (mine) tile_load3(ring + ((5 * g + 1) & 7) * kSub, &map_kv, 64, it.head, row, kf);
+                if (g >= 2) ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.v_empty[st]), ph, kWaitCycles));
+                if (!ok) break;
+                if (mine) tile_load2(ring + ((5 * g + 2) & 7) * kSub, &map_rope, 0, row, kf);
+                // values: over the first two pieces of the keys one block before
+                if (g >= 1) ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.k_empty[st ^ 1]), ((g - 1) >> 1) & 1, kWaitCycles));
+                if (!ok) break;
+                if (mine) {
+                    const uint32_t vf = smem_u32(&sm.v_full[st]);
+                    bar_expect(vf, kVBytes);
+#pragma unroll
+                    for (int c = 0; c < 4; c++)
+                        tile_load3(ring + ((5 * g + 3 + (c >> 1)) & 7) * kSub + (c & 1) * (kSub / 2), &map_v, kNope + 64 * (c & 1), it.head,
+                                   row + 64 * (c >> 1), vf);
                 }
             }
             if (!ok) break;
         }
         if (!ok) {                                 // gave up: let the copies in flight land (bounded) before the CTA ends
             if (qc) bar_wait(qf, (qc - 1) & 1, kWaitCycles);
-            if (vc) bar_wait(vf, (vc - 1) & 1, kWaitCycles);
-            for (uint32_t b = kc > 2 ? kc - 2 : 0; b < kc; b++) bar_wait(smem_u32(&sm.k_full[b & 1]), (b >> 1) & 1, kWaitCycles);
+            for (uint32_t b = g > 1 ? g - 1 : 0; b <= g; b++) {
+                bar_wait(smem_u32(&sm.k_full[b & 1]), (b >> 1) & 1, b < g ? kWaitCycles : 1000000);
+                bar_wait(smem_u32(&sm.v_full[b & 1]), (b >> 1) & 1, b < g ? kWaitCycles : 1000000);
+            }
         }
     } else if (warp == 8) {
         // ================================================= products
         constexpr uint32_t kIdS = instr(kTileQ, kBlockK, false, false), kIdO = instr(kTileQ, kV, false, true);
         const bool mine = elect_one();
-        const uint64_t dq = desc(smem_u32(sm.q[0]), 0, 1024), dk = desc(smem_u32(sm.k[0]), 0, 1024), dv = desc(smem_u32(sm.v), kSub, 1024);
+        const uint64_t dq = desc(smem_u32(sm.q[0]), 0, 1024), dk = desc(smem_u32(sm.ring), 0, 1024), dv = desc(smem_u32(sm.ring), kSub / 2, 1024);
         Item it;
-        uint32_t kc = 0, vc = 0, qc = 0, pc[2] = {0, 0}, oc[2] = {0, 0};   // ... weights and items of each tile so far
-        auto scores = [&](int t, uint32_t st) {
-            const uint64_t a = dq + (uint64_t)(t * kQBytes >> 4), b = dk + (uint64_t)(st * kKBytes >> 4);
+        uint32_t g = 0, qc = 0, pc[2] = {0, 0}, oc[2] = {0, 0};            // blocks, items, weights and items of each tile so far
+        auto scores = [&](int t, uint32_t first) { // first: piece of the ring the keys start at
+            uint64_t a = dq + (uint64_t)(t * kQBytes >> 4);
+#pragma unroll 1
+            for (int c = 0; c < 3; c++, a += kSub >> 4) {      // (rolled: 24 descriptors kept apart would cost 100 registers)
+                const uint64_t b = dk + (uint64_t)(((first + c) & 7) * kSub >> 4);
 #pragma unroll
-            for (int k = 0; k < kQk / 16; k++) {
-                const uint64_t off = (uint64_t)(((k >> 2) * kSub + (k & 3) * 32) >> 4);
-                mma_ss(tmem + kS + t * 128, a + off, b + off, kIdS, k > 0, mine);
+                for (int k = 0; k < 4; k++) mma_ss(tmem + kS + t * 128, a + 2 * k, b + 2 * k, kIdS, c > 0 || k > 0, mine);
             }
             if (mine) commit(smem_u32(&sm.s_full[t]));
         };
-        auto values = [&](int t, bool first, int steps) {
+        auto values = [&](int t, uint32_t first, bool fresh, int from, int steps) {        // half of the keys
+            const uint64_t b = dv + (uint64_t)(((first + (from >> 2)) & 7) * kSub >> 4);
 #pragma unroll
-            for (int k = 0; k < kBlockK / 16; k++)
-                if (k < steps) mma_ts(tmem + kO + t * 128, tmem + kS + t * 128 + k * 8, dv + (uint64_t)(k * 2048 >> 4), kIdO, k > 0 || !first, mine);
-            if (mine) commit(smem_u32(&sm.pv_done[t]));
+            for (int k = 0; k < 4; k++)
+                if (from + k < steps)
+                    mma_ts(tmem + kO + t * 128, tmem + kS + t * 128 + (from + k) * 8, b + 128 * k, kIdO, from + k > 0 || !fresh, mine);
         };
         for (uint32_t n = 0; next_item(n, it); n++) {
             const int nt[2] = {key_blocks(it, 0), key_blocks(it, 1)}, nb = max(nt[0], nt[1]);
             if (nb == 0) continue;
             ok = bar_wait(smem_u32(&sm.q_full), qc & 1, kWaitCycles);
             qc++;
-            ok = bar_wait(smem_u32(&sm.k_full[kc & 1]), (kc >> 1) & 1, kWaitCycles) && ok;
+            ok = bar_wait(smem_u32(&sm.k_full[g & 1]), (g >> 1) & 1, kWaitCycles) && ok;
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             fence_after();
             {
-                const uint32_t st = __shfl_sync(0xffffffffu, kc & 1, 0);
-                if (nt[0]) scores(0, st);
-                if (nt[1]) scores(1, st);
-                if (mine) commit(smem_u32(&sm.k_empty[st]));
-                kc++;
-                if (nb == 1 && mine) commit(smem_u32(&sm.q_empty));
+                const uint32_t first = __shfl_sync(0xffffffffu, (5 * g) & 7, 0);
+                if (nt[0]) scores(0, first);
+                if (nt[1]) scores(1, first);
+                if (mine) {
+                    commit(smem_u32(&sm.k_empty[g & 1]));
+                    if (nb == 1) commit(smem_u32(&sm.q_empty));
+                }
             }
-            for (int j = 0; j < nb && ok; j++) {
+            for (int j = 0; j < nb; j++, g++) {
                 const int valid = __shfl_sync(0xffffffffu, min(kBlockK, it.nk - j * kBlockK), 0), steps = (valid + 15) / 16;
-                const uint32_t st = __shfl_sync(0xffffffffu, kc & 1, 0);
-                bool have_v = false, have_k = false;
+                const uint32_t at = __shfl_sync(0xffffffffu, (5 * g) & 7, 0), ph = (g >> 1) & 1;
+                const int last_t = j < nt[1] ? 1 : 0;       // the tile whose product is the last to use the block's values
+                bool have_k = false;
+                ok = bar_wait(smem_u32(&sm.v_full[g & 1]), ph, kWaitCycles) && ok;
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                if (valid & 15) {                  // rows behind the last key in its step of 16: whatever they hold counts as zero
+                    uint8_t *v = sm.ring + ((at + 3 + (valid >> 6)) & 7) * kSub;
+                    const int rows = 16 * steps - valid;
+                    for (int e = lane; e < rows * 16; e += 32)
+                        *reinterpret_cast<uint4 *>(v + ((e >> 3) & 1) * (kSub / 2) + ((valid & 63) + (e >> 4)) * 128 + (e & 7) * 16) =
+                            make_uint4(0, 0, 0, 0);
+                    fence_async_shared();
+                    __syncwarp();
+                }
 #pragma unroll
                 for (int t = 0; t < 2; t++) {
                     if (j < nt[t]) {
-                        if (!have_v) {
-                            ok = bar_wait(smem_u32(&sm.v_full), vc & 1, kWaitCycles) && ok;
-                            ok = __all_sync(0xffffffffu, ok);
-                            if (!ok) break;
-                            if (valid & 15) {      // rows behind the last key in its step of 16: whatever they hold counts as zero
-                                const int rows = 16 * steps - valid;
-                                for (int e = lane; e < rows * 16; e += 32) {
-                                    const int r = valid + (e >> 4), ch = e & 15;
-                                    *reinterpret_cast<uint4 *>(sm.v + (ch >> 3) * kSub + r * 128 + (ch & 7) * 16) = make_uint4(0, 0, 0, 0);
-                                }
-                                fence_async_shared();
-                                __syncwarp();
-                            }
-                            have_v = true;
-                        }
-                        ok = bar_wait(smem_u32(&sm.p_full[t]), pc[t] & 1, kWaitCycles) && ok;
-                        pc[t]++;
                         if (j == 0) {              // the item before has been read out of O
                             if (oc[t] > 0) ok = bar_wait(smem_u32(&sm.o_free[t]), (oc[t] - 1) & 1, kWaitCycles) && ok;
                             oc[t]++;
                         }
-                        ok = __all_sync(0xffffffffu, ok);
+                        ok = __all_sync(0xffffffffu, bar_spin(smem_u32(&sm.p_half[t]), pc[t] & 1, kWaitCycles) && ok);
                         if (!ok) break;
                         fence_after();
-                        values(t, j == 0, steps);
+                        values(t, at + 3, j == 0, 0, steps);
+                        if (t == last_t && mine) commit(smem_u32(&sm.v_half[g & 1]));
+                        ok = __all_sync(0xffffffffu, bar_spin(smem_u32(&sm.p_full[t]), pc[t] & 1, kWaitCycles));
+                        if (!ok) break;
+                        pc[t]++;
+                        fence_after();
+                        values(t, at + 3, false, 4, steps);
+                        if (mine) {
+                            if (t == last_t) commit(smem_u32(&sm.v_empty[g & 1]));
+                            if (j + 1 == nt[t]) commit(smem_u32(&sm.pv_done[t]));
+                        }
                     }
                     if (j + 1 < nt[t]) {
                         if (!have_k) {
-                            ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.k_full[st]), (kc >> 1) & 1, kWaitCycles) && ok);
+                            ok = __all_sync(0xffffffffu, bar_spin(smem_u32(&sm.k_full[(g + 1) & 1]), ((g + 1) >> 1) & 1, kWaitCycles));
                             if (!ok) break;
                             fence_after();
                             have_k = true;
                         }
-                        scores(t, st);
+                        scores(t, at + 5);
                     }
                 }
                 if (!ok) break;
-                if (mine) commit(smem_u32(&sm.v_empty));
-                vc++;
-                if (j + 1 < nb) {
-                    if (mine) {
-                        commit(smem_u32(&sm.k_empty[st]));
-                        if (j + 2 == nb) commit(smem_u32(&sm.q_empty));
-                    }
-                    kc++;
+                if (mine) {
+                    if (j + 1 < nb) commit(smem_u32(&sm.k_empty[(g + 1) & 1]));
+                    if (j + 2 == nb) commit(smem_u32(&sm.q_empty));
                 }
             }
             if (!ok) break;
@@ -370,11 +387,14 @@ prompt_latent_kernel(const __grid_constant__ PromptParams p, const __grid_consta
             bar_wait(smem_u32(&sm.drain), 0, kWaitCycles);
         }
         __syncwarp();
-    } else if (warp < 8) {
+    }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
         // ================================================= softmax: thread = query
         const int t = warp >> 2;
         const uint32_t base = tmem + ((uint32_t)((warp & 3) * 32) << 16) + t * 128;
-        const uint32_t s_full = smem_u32(&sm.s_full[t]), p_full = smem_u32(&sm.p_full[t]), pv_done = smem_u32(&sm.pv_done[t]);
+        const uint32_t s_full = smem_u32(&sm.s_full[t]), p_half = smem_u32(&sm.p_half[t]), p_full = smem_u32(&sm.p_full[t]),
+                       pv_done = smem_u32(&sm.pv_done[t]);
         Item it;
         // a wait ran out (never expected): the row's result says so
         auto spoil = [&](const Item &at, int i) {
@@ -383,13 +403,13 @@ prompt_latent_kernel(const __grid_constant__ PromptParams p, const __grid_consta
             for (int d = 0; d < kV; d++) p.out[row * kV + d] = __ushort_as_bfloat16((unsigned short)0x7FC0);
             if (p.lse) p.lse[row] = __int_as_float(0x7FC00000);
         };
-        uint32_t sc = 0;                           // blocks of this tile so far (S, P and P V alike)
+        uint32_t sc = 0, ic = 0;                   // blocks of this tile so far (S, P and P V alike), items with any
         for (uint32_t n = 0; next_item(n, it); n++) {
             const int nb = key_blocks(it, t), i = it.block * kBlockQ + t * kTileQ + (warp & 3) * 32 + lane;
             const int vis = i < it.nq ? visible(it, i) : 0;
             float m = -INFINITY, l = 0.0f;
             for (int j = 0; j < nb; j++, sc++) {
-                ok = bar_wait(s_full, sc & 1, ok ? kWaitCycles : 0) && ok;
+                ok = bar_spin(s_full, sc & 1, ok ? kWaitCycles : 0) && ok;
                 if (!__all_sync(0xffffffffu, ok)) break;
                 fence_after();
                 float x[128];
@@ -419,10 +439,7 @@ prompt_latent_kernel(const __grid_constant__ PromptParams p, const __grid_consta
                 if (__any_sync(0xffffffffu, raise)) {
                     const float f = raise ? ex2(m - top) : 1.0f;
                     if (raise) { m = top; l *= f; }
-                    if (j > 0) {                   // O so far, in the new reference
-                        ok = bar_wait(pv_done, (sc - 1) & 1, ok ? kWaitCycles : 0) && ok;
-                        __syncwarp();
-                        fence_after();
+                    if (j > 0) {                   // O so far, in the new reference (complete: this S was issued behind it)
 #pragma unroll 1
                         for (int c = 0; c < 8; c++) {
                             uint32_t r[16];
@@ -435,29 +452,37 @@ prompt_latent_kernel(const __grid_constant__ PromptParams p, const __grid_consta
                     }
                 }
                 const float ref = m == -INFINITY ? 0.0f : m;               // a row that has seen no key yet
-                float l0 = 0.0f, l1 = 0.0f;
+                const uint64_t scale2 = pair(p.scale_log2, p.scale_log2), ref2 = pair(-ref, -ref);
+                uint64_t l2 = pair(0.0f, 0.0f);
+                // Weights go out in two halves: the product over the first 64 keys runs beside the other exponentials.
 #pragma unroll
                 for (int c = 0; c < 4; c++) {
                     uint32_t r[16];
 #pragma unroll
                     for (int e = 0; e < 16; e++) {
-                        const float a = ex2(__fmaf_rn(x[32 * c + 2 * e], p.scale_log2, -ref)), b = ex2(__fmaf_rn(x[32 * c + 2 * e + 1], p.scale_log2, -ref));
-                        l0 += a;
-                        l1 += b;
+                        float a, b;
+                        unpair(fma2(pair(x[32 * c + 2 * e], x[32 * c + 2 * e + 1]), scale2, ref2), a, b);
+                        a = ex2(a);
+                        b = ex2(b);
+                        l2 = add2(l2, pair(a, b));
                         r[e] = pack_bf16(a, b);
                     }
                     tmem_st16(base + kS + 16 * c, r);
+                    if (c & 1) {
+                        tmem_wait_st();
+                        fence_before();
+                        __syncwarp();
+                        if (lane == 0) bar_arrive(c == 1 ? p_half : p_full);
+                    }
                 }
+                float l0, l1;
+                unpair(l2, l0, l1);
                 l += l0 + l1;
-                tmem_wait_st();
-                fence_before();
-                __syncwarp();
-                if (lane == 0) bar_arrive(p_full);
             }
             if (!__all_sync(0xffffffffu, ok)) { spoil(it, i); break; }
             // ---- the row's result
             if (nb > 0) {
-                ok = bar_wait(pv_done, (sc - 1) & 1, kWaitCycles);
+                ok = bar_wait(pv_done, ic++ & 1, kWaitCycles);
                 if (!__all_sync(0xffffffffu, ok)) { spoil(it, i); break; }
                 fence_after();
             }
@@ -504,12 +529,13 @@ using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t,
                                  const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-// rows of 64-dim pieces: dims {inner, heads, rows} (or {inner, rows}), a box of 64 x 1 x 128 with the 128-byte swizzle
-bool encode(EncodeTiled fn, CUtensorMap *map, const void *base, int inner, int heads, int rows, size_t head_stride, size_t row_stride) {
+// rows of 64-dim pieces: dims {inner, heads, rows} (or {inner, rows}), a box of 64 x 1 x box_rows with the 128-byte swizzle
+bool encode(EncodeTiled fn, CUtensorMap *map, const void *base, int inner, int heads, int rows, size_t head_stride, size_t row_stride,
+            int box_rows) {
     const int rank = heads ? 3 : 2;
     const cuuint64_t dims3[3] = {(cuuint64_t)inner, (cuuint64_t)heads, (cuuint64_t)rows}, dims2[2] = {(cuuint64_t)inner, (cuuint64_t)rows};
     const cuuint64_t str3[2] = {head_stride, row_stride}, str2[1] = {row_stride};
-    const cuuint32_t box3[3] = {64, 1, kBlockK}, box2[2] = {64, kBlockK}, one[3] = {1, 1, 1};
+    const cuuint32_t box3[3] = {64, 1, (cuuint32_t)box_rows}, box2[2] = {64, (cuuint32_t)box_rows}, one[3] = {1, 1, 1};
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void *>(base), rank == 3 ? dims3 : dims2,
               rank == 3 ? str3 : str2, rank == 3 ? box3 : box2, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
@@ -538,16 +564,17 @@ pask_status_t launch_prompt_latent(int n_seqs, int total_q, int total_k, int n_h
         if (cudaFuncSetAttribute(prompt_latent_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess) return PASK_ERR_CUDA;
         granted[dev] = true;
     }
-    CUtensorMap map_q{}, map_kv{}, map_rope{};
-    if (!encode(encode_fn, &map_q, q, kQk, n_heads, total_q, kQk * 2, (size_t)n_heads * kQk * 2)) return PASK_ERR_CUDA;
-    if (total_k > 0 &&
-        (!encode(encode_fn, &map_kv, kv, kNope + kV, n_heads, total_k, (kNope + kV) * 2, (size_t)n_heads * (kNope + kV) * 2) ||
-         !encode(encode_fn, &map_rope, k_rope, kRope, 0, total_k, 0, (size_t)rope_stride * 2)))
+    CUtensorMap map_q{}, map_kv{}, map_v{}, map_rope{};
+    const size_t q_row = (size_t)n_heads * kQk * 2, kv_head = (kNope + kV) * 2, kv_row = (size_t)n_heads * kv_head;
+    if (!encode(encode_fn, &map_q, q, kQk, n_heads, total_q, kQk * 2, q_row, kTileQ)) return PASK_ERR_CUDA;
+    if (total_k > 0 && (!encode(encode_fn, &map_kv, kv, kNope + kV, n_heads, total_k, kv_head, kv_row, kBlockK) ||
+                        !encode(encode_fn, &map_v, kv, kNope + kV, n_heads, total_k, kv_head, kv_row, kBlockK / 2) ||
+                        !encode(encode_fn, &map_rope, k_rope, kRope, 0, total_k, 0, (size_t)rope_stride * 2, kBlockK)))
         return PASK_ERR_CUDA;
     const long long items = ((long long)total_q / kBlockQ + n_seqs) * n_heads;
     if (items > 0x7fffffffLL) return PASK_ERR_INVALID_ARG;
     const PromptParams p{n_seqs, total_q, total_k, n_heads, cu_q, cu_k, scale * 1.4426950408889634f, static_cast<__nv_bfloat16 *>(out), lse};
-    prompt_latent_kernel<<<(int)items, kThreads, kSmem, stream>>>(p, map_q, map_kv, map_rope);
+    prompt_latent_kernel<<<(int)items, kThreads, kSmem, stream>>>(p, map_q, map_kv, map_v, map_rope);
     return cudaGetLastError() == cudaSuccess ? PASK_OK : PASK_ERR_CUDA;
 }
 

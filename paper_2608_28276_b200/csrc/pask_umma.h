@@ -41,6 +41,15 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, long lon
         if ((n & 63u) == 0 && clock64() - t0 > limit) return false;
     }
 }
+// the same without ever suspending the warp
+__device__ __forceinline__ bool bar_spin(uint32_t bar, uint32_t parity, long long limit) {
+    if (bar_test(bar, parity)) return true;
+    const long long t0 = clock64();
+    for (uint32_t n = 1;; n++) {
+        if (bar_test(bar, parity)) return true;
+        if ((n & 255u) == 0 && clock64() - t0 > limit) return false;
+    }
+}
 
 // ---- ordering between plain accesses to shared memory and the asynchronous units, and between tcgen05 operations and barriers
 __device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
@@ -87,16 +96,6 @@ __device__ __forceinline__ void tmem_ld32(uint32_t addr, uint32_t (&r)[32]) {
         : "r"(addr));
 }
 
-__device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t (&r)[32]) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {"
-                 "%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};"
-                 ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-                   "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
-                   "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
-                   "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]),
-                   "r"(addr)
-                 : "memory");
-}
 // 16 lanes x 8 / 16 / 32 / 64 columns as fragments: with t = lane of the warp, r[4j], r[4j+1] = row t / 4, columns 8j + 2 (t % 4)
 // and the next; r[4j+2], r[4j+3] = row t / 4 + 8, the same columns
 __device__ __forceinline__ void tmem_ld_frag(uint32_t addr, uint32_t (&r)[8]) {
@@ -217,6 +216,24 @@ __device__ __forceinline__ float ex2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+
+// ---- pairs of fp32 numbers, one instruction for both
+__device__ __forceinline__ uint64_t pair(float lo, float hi) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void unpair(uint64_t x, float &lo, float &hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(x)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
 }
 
 }  // namespace umma
