@@ -7,6 +7,7 @@ fails.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 
@@ -354,73 +355,66 @@ def pask_decode_step_drain(cache: int):
     _check(_lib.pask_decode_step_drain(cache), "pask_decode_step_drain")
 
 
-def _latent_args(where, device, *args):
-    """Checks of the latent calls: (name, tensor or None, dtype, shape with None for any size) each, all on one device."""
-    for name, t, dtype, shape in args:
-        if t is None:
-            continue
-        ok = (t.is_cuda and t.device == device and t.dtype == dtype and t.is_contiguous() and t.dim() == len(shape) and
-              all(want is None or want == have for want, have in zip(shape, t.shape)))
-        if not ok:
-            raise PaskError(ERR_INVALID_ARG, f"{where}: {name} must be a contiguous {dtype} tensor "
-                            f"[{', '.join('*' if n is None else str(n) for n in shape)}] on {device}, got {tuple(t.shape)} {t.dtype}")
+def _arg(where, name, t, dtype, dev, shape):
+    """Device pointer of a latent call's tensor: this type and shape, contiguous, on CUDA device `dev` (an index)."""
+    if t.dtype is not dtype or t.get_device() != dev or t.shape != shape or not t.is_contiguous():
+        raise PaskError(ERR_INVALID_ARG, f"{where}: {name} must be a contiguous {dtype} tensor {list(shape)} on cuda:{dev}, "
+                        f"got {t.dtype} {list(t.shape)} on {t.device}")
+    return t.data_ptr()
 
 
-def _on(device, stream):
-    """The CUDA stream of a latent call: the given one, or the device's current one."""
-    return (torch.cuda.current_stream(device) if stream is None else stream).cuda_stream
+def _call(where, fn, dev, stream, *args):
+    """Issue a latent call on the tensors' device: on the given stream or that device's current one."""
+    if dev < 0:
+        raise PaskError(ERR_INVALID_ARG, f"{where}: tensors must be on a CUDA device")
+    with contextlib.nullcontext() if dev == torch.cuda.current_device() else torch.cuda.device(dev):
+        _check(fn(*args, (torch.cuda.current_stream(dev) if stream is None else stream).cuda_stream), where)
 
 
 def pask_append_latent(cache: int, layer: int, seq_ids, cu_tokens, latent, tags, actions=None, actions_out=None, stream=None):
     """pask_append_kv for a latent cache: latent bf16 [total][576]; `actions` u8 [total][n_groups] from pask_decide or None."""
-    n, total, dev = seq_ids.numel(), latent.shape[0], seq_ids.device
-    _latent_args("pask_append_latent", dev, ("seq_ids", seq_ids, torch.int32, (n,)), ("cu_tokens", cu_tokens, torch.int32, (n + 1,)),
-                 ("latent", latent, torch.bfloat16, (None, LATENT_DIM)), ("tags", tags, torch.uint8, (total,)),
-                 ("actions", actions, torch.uint8, (total, _latent_shape.get(cache, (None, None))[1])), ("actions_out", actions_out, torch.uint8, (total,)))
-    with torch.cuda.device(dev):
-        _check(_lib.pask_append_latent(cache, layer, n, total, _dptr(seq_ids), _dptr(cu_tokens), _dptr(latent), _dptr(tags),
-                                       _dptr(actions), _dptr(actions_out), _on(dev, stream)), "pask_append_latent")
+    w, n, total, dev = "pask_append_latent", seq_ids.numel(), latent.shape[0], seq_ids.get_device()
+    groups = _latent_shape[cache][1] if cache in _latent_shape else 1
+    _call(w, _lib.pask_append_latent, dev, stream, cache, layer, n, total, _arg(w, "seq_ids", seq_ids, torch.int32, dev, (n,)),
+          _arg(w, "cu_tokens", cu_tokens, torch.int32, dev, (n + 1,)), _arg(w, "latent", latent, torch.bfloat16, dev, (total, LATENT_DIM)),
+          _arg(w, "tags", tags, torch.uint8, dev, (total,)),
+          None if actions is None else _arg(w, "actions", actions, torch.uint8, dev, (total, groups)),
+          None if actions_out is None else _arg(w, "actions_out", actions_out, torch.uint8, dev, (total,)))
 
 
 def pask_read_latent(cache: int, layer: int, seq_ids, cu_rows, rows_out, lens_out=None, stream=None):
     """The retained rows of each sequence as bf16, HIGH stream then LOW stream, into rows_out[cu_rows[i]:]."""
-    n, dev = seq_ids.numel(), seq_ids.device
-    _latent_args("pask_read_latent", dev, ("seq_ids", seq_ids, torch.int32, (n,)), ("cu_rows", cu_rows, torch.int32, (n + 1,)),
-                 ("rows_out", rows_out, torch.bfloat16, (None, LATENT_DIM)), ("lens_out", lens_out, torch.int32, (n, 2)))
-    with torch.cuda.device(dev):
-        _check(_lib.pask_read_latent(cache, layer, n, rows_out.shape[0], _dptr(seq_ids), _dptr(cu_rows), _dptr(rows_out),
-                                     _dptr(lens_out), _on(dev, stream)), "pask_read_latent")
+    w, n, total, dev = "pask_read_latent", seq_ids.numel(), rows_out.shape[0], seq_ids.get_device()
+    _call(w, _lib.pask_read_latent, dev, stream, cache, layer, n, total, _arg(w, "seq_ids", seq_ids, torch.int32, dev, (n,)),
+          _arg(w, "cu_rows", cu_rows, torch.int32, dev, (n + 1,)), _arg(w, "rows_out", rows_out, torch.bfloat16, dev, (total, LATENT_DIM)),
+          None if lens_out is None else _arg(w, "lens_out", lens_out, torch.int32, dev, (n, 2)))
 
 
 def pask_decode_attention_latent(cache: int, layer: int, seq_ids, q, scale: float, out, lse, workspace, stream=None):
     """One new query per sequence over a latent cache: q bf16 [n][n_q][576], out bf16 [n][n_q][512], lse fp32 [n][n_q] or None."""
-    n, dev = seq_ids.numel(), seq_ids.device
-    heads = _latent_shape.get(cache, (None, None))[0]
-    _latent_args("pask_decode_attention_latent", dev, ("seq_ids", seq_ids, torch.int32, (n,)),
-                 ("q", q, torch.bfloat16, (n, heads, LATENT_DIM)), ("out", out, torch.bfloat16, (n, heads, LATENT_VALUE_DIM)),
-                 ("lse", lse, torch.float32, (n, heads)))
-    with torch.cuda.device(dev):
-        _check(_lib.pask_decode_attention_latent(cache, layer, n, _dptr(seq_ids), _dptr(q), scale, _dptr(out), _dptr(lse),
-                                                 _dptr(workspace), workspace.numel() * workspace.element_size(), _on(dev, stream)),
-               "pask_decode_attention_latent")
+    w, n, dev = "pask_decode_attention_latent", seq_ids.numel(), seq_ids.get_device()
+    heads = _latent_shape[cache][0] if cache in _latent_shape else q.shape[1]
+    ws_bytes = workspace.numel() * workspace.element_size()
+    _call(w, _lib.pask_decode_attention_latent, dev, stream, cache, layer, n, _arg(w, "seq_ids", seq_ids, torch.int32, dev, (n,)),
+          _arg(w, "q", q, torch.bfloat16, dev, (n, heads, LATENT_DIM)), scale,
+          _arg(w, "out", out, torch.bfloat16, dev, (n, heads, LATENT_VALUE_DIM)),
+          None if lse is None else _arg(w, "lse", lse, torch.float32, dev, (n, heads)),
+          _arg(w, "workspace", workspace, workspace.dtype, dev, workspace.shape), ws_bytes)
 
 
 def pask_prompt_attention_latent(cu_q, cu_k, q, kv, k_rope, scale: float, out, lse=None, stream=None):
     """Causal attention of a ragged batch of prompts (or chunks behind a history), keys and values expanded per head:
     q bf16 [total_q][h][192], kv bf16 [total_k][h][256], k_rope bf16 [total_k][64] (rows may be strided, as in
     latent[:, 512:]), out bf16 [total_q][h][128], lse fp32 [total_q][h] or None."""
-    n, dev = cu_q.numel() - 1, cu_q.device
-    tq, heads, tk = q.shape[0], q.shape[1] if q.dim() == 3 else 0, kv.shape[0]
-    where = "pask_prompt_attention_latent"
-    _latent_args(where, dev, ("cu_q", cu_q, torch.int32, (n + 1,)), ("cu_k", cu_k, torch.int32, (n + 1,)),
-                 ("q", q, torch.bfloat16, (None, heads, 192)), ("kv", kv, torch.bfloat16, (None, heads, 256)),
-                 ("out", out, torch.bfloat16, (tq, heads, 128)), ("lse", lse, torch.float32, (tq, heads)))
-    if not (k_rope.device == dev and k_rope.dtype == torch.bfloat16 and k_rope.shape == (tk, 64) and k_rope.stride(1) == 1):
-        raise PaskError(ERR_INVALID_ARG, f"{where}: k_rope must be a bfloat16 tensor [{tk}, 64] on {dev} with adjacent columns")
-    stride = k_rope.stride(0) if tk > 1 else 64
-    with torch.cuda.device(dev):
-        _check(_lib.pask_prompt_attention_latent(n, tq, tk, heads, _dptr(cu_q), _dptr(cu_k), _dptr(q), _dptr(kv), k_rope.data_ptr(),
-                                                 stride, scale, _dptr(out), _dptr(lse), _on(dev, stream)), where)
+    w, n, dev = "pask_prompt_attention_latent", cu_q.numel() - 1, cu_q.get_device()
+    tq, heads, tk = q.shape[0], q.shape[1], kv.shape[0]
+    if k_rope.get_device() != dev or k_rope.dtype is not torch.bfloat16 or k_rope.shape != (tk, 64) or k_rope.stride(1) != 1:
+        raise PaskError(ERR_INVALID_ARG, f"{w}: k_rope must be a torch.bfloat16 tensor [{tk}, 64] on cuda:{dev} with adjacent columns")
+    _call(w, _lib.pask_prompt_attention_latent, dev, stream, n, tq, tk, heads, _arg(w, "cu_q", cu_q, torch.int32, dev, (n + 1,)),
+          _arg(w, "cu_k", cu_k, torch.int32, dev, (n + 1,)), _arg(w, "q", q, torch.bfloat16, dev, (tq, heads, 192)),
+          _arg(w, "kv", kv, torch.bfloat16, dev, (tk, heads, 256)), k_rope.data_ptr(), k_rope.stride(0) if tk > 1 else 64, scale,
+          _arg(w, "out", out, torch.bfloat16, dev, (tq, heads, 128)),
+          None if lse is None else _arg(w, "lse", lse, torch.float32, dev, (tq, heads)))
 
 
 def pask_budget_state(cache: int, seq: int, stream=None) -> BudgetState:

@@ -349,12 +349,12 @@ prompt_latent_kernel(const __grid_constant__ PromptParams p, const __grid_consta
                             if (oc[t] > 0) ok = bar_wait(smem_u32(&sm.o_free[t]), (oc[t] - 1) & 1, kWaitCycles) && ok;
                             oc[t]++;
                         }
-                        ok = __all_sync(0xffffffffu, bar_spin(smem_u32(&sm.p_half[t]), pc[t] & 1, kWaitCycles) && ok);
+                        ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.p_half[t]), pc[t] & 1, kWaitCycles) && ok);
                         if (!ok) break;
                         fence_after();
                         values(t, at + 3, j == 0, 0, steps);
                         if (t == last_t && mine) commit(smem_u32(&sm.v_half[g & 1]));
-                        ok = __all_sync(0xffffffffu, bar_spin(smem_u32(&sm.p_full[t]), pc[t] & 1, kWaitCycles));
+                        ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.p_full[t]), pc[t] & 1, kWaitCycles));
                         if (!ok) break;
                         pc[t]++;
                         fence_after();
@@ -366,7 +366,7 @@ prompt_latent_kernel(const __grid_constant__ PromptParams p, const __grid_consta
                     }
                     if (j + 1 < nt[t]) {
                         if (!have_k) {
-                            ok = __all_sync(0xffffffffu, bar_spin(smem_u32(&sm.k_full[(g + 1) & 1]), ((g + 1) >> 1) & 1, kWaitCycles));
+                            ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.k_full[(g + 1) & 1]), ((g + 1) >> 1) & 1, kWaitCycles));
                             if (!ok) break;
                             fence_after();
                             have_k = true;
@@ -409,7 +409,7 @@ prompt_latent_kernel(const __grid_constant__ PromptParams p, const __grid_consta
             const int vis = i < it.nq ? visible(it, i) : 0;
             float m = -INFINITY, l = 0.0f;
             for (int j = 0; j < nb; j++, sc++) {
-                ok = bar_spin(s_full, sc & 1, ok ? kWaitCycles : 0) && ok;
+                ok = bar_wait(s_full, sc & 1, ok ? kWaitCycles : 0) && ok;
                 if (!__all_sync(0xffffffffu, ok)) break;
                 fence_after();
                 float x[128];

@@ -41,16 +41,6 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, long lon
         if ((n & 63u) == 0 && clock64() - t0 > limit) return false;
     }
 }
-// the same without ever suspending the warp
-__device__ __forceinline__ bool bar_spin(uint32_t bar, uint32_t parity, long long limit) {
-    if (bar_test(bar, parity)) return true;
-    const long long t0 = clock64();
-    for (uint32_t n = 1;; n++) {
-        if (bar_test(bar, parity)) return true;
-        if ((n & 255u) == 0 && clock64() - t0 > limit) return false;
-    }
-}
-
 // ---- ordering between plain accesses to shared memory and the asynchronous units, and between tcgen05 operations and barriers
 __device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
