@@ -301,18 +301,18 @@ read_latent_kernel(DevCache c, int layer, int n_seqs, int total_rows, const int3
 //
 // A CTA is one of `slots` equal shares of the batch's rows (cost line over sequences, as the other decode kernel cuts it), in
 // tiles of 64 rows = four pages of one stream; a sequence's HIGH and LOW tiles are visited in turn, evenly mixed.  Roles:
-//   warp 8      one linear bulk copy a page (HIGH pages are stored in the operand layout) into its place in one of two stages,
-//               as soon as the product that last read the place is done, and a prefetch into L2 some tiles ahead, which
-//               keeps memory busy while both stages are held by products
-//   warps 4-7   LOW tiles: codes from the stage to registers, values as bf16 back over them; and the queries of a sequence
-//   warp 9      issues the products: S of tile i + 1, then O of tile i
+//   warp 12     HIGH tiles: one linear bulk copy a page (pages are stored in the operand layout) into its place in one of two
+//               stages, as soon as the product that last read the place is done, and a prefetch into L2 some tiles ahead
+//   warps 4-11  LOW tiles: codes in registers one tile ahead, values as bf16 into the stage; and the queries of a sequence
+//   warp 13     the products for S, two tiles ahead at most;  warp 14  those for O.  (One warp for both had to poll: waiting on a
+//               barrier wakes it 70 cycles after the arrival, polling two of them sees it after 150 to 350.)
 //   warps 0-3   softmax of a tile's S (warp w: page w of the tile), P to shared memory, and a sequence's end
 // The reference maximum of a head moves only when a score exceeds it by more than 2^8 (the sums have room for that), so that
 // the rescaling of O leaves the common path.  A share that covers a whole sequence writes its result; otherwise partial sums
 // go to the workspace and decode_latent_merge joins them in a fixed order: results do not depend on timing.
 constexpr int kTile = 64, kTilePages = 4;
 constexpr int kTileBytes = kTilePages * kLatentHighPageBytes;      // 73728
-constexpr int kDecThreads = 320;
+constexpr int kDecThreads = 480, kFillThreads = 256;
 constexpr uint32_t kMaxSlots = 1024;
 constexpr int kPrefetch = 4;                       // tiles between a prefetch into L2 and the copy
 constexpr uint32_t kCostHighTile = 3, kCostLowTile = 2;
@@ -339,9 +339,14 @@ struct DecParams {
 };
 
 __device__ __forceinline__ uint32_t tiles_of(uint32_t tokens) { return (tokens + kTile - 1) / kTile; }
-__device__ __forceinline__ uint32_t slot_start(uint32_t total, uint32_t slot, uint32_t slots) {
-    return (uint32_t)((uint64_t)total * slot / slots);
+// floor(a b / c), in 32 bits where the product fits (a 64-bit division is some 200 cycles of the set-up)
+__device__ __forceinline__ uint32_t mul_div(uint32_t a, uint32_t b, uint32_t c) {
+    const uint64_t x = (uint64_t)a * b;
+    return (x >> 32) == 0 ? (uint32_t)x / c : (uint32_t)(x / c);
 }
+__device__ __forceinline__ uint32_t slot_start(uint32_t total, uint32_t slot, uint32_t slots) { return mul_div(total, slot, slots); }
+// positions (of n) before offset x of a sequence of cost cs: cut_positions of pask_layout.h
+__device__ __forceinline__ uint32_t cut_at(uint32_t x, uint32_t cs, uint32_t n) { return x >= cs ? n : mul_div(x, n, cs); }
 
 // The tiles of one share, in order; the roles walk their own copies.
 struct TileWalk {
@@ -364,11 +369,10 @@ struct TileWalk {
         cost = kCostHighTile * th + kCostLowTile * (n - th);
         v0 = v1 = h0 = rem = 0;
         if (cost) {
-            v0 = lo > base ? cut_positions(lo - base, cost, n) : 0u;
-            v1 = cut_positions(hi - base, cost, n);
-            const uint64_t x = (uint64_t)v0 * th;
-            h0 = (uint32_t)(x / n);
-            rem = (uint32_t)(x - (uint64_t)h0 * n);
+            v0 = lo > base ? cut_at(lo - base, cost, n) : 0u;
+            v1 = cut_at(hi - base, cost, n);
+            h0 = mul_div(v0, th, n);
+            rem = (uint32_t)((uint64_t)v0 * th - (uint64_t)h0 * n);
         }
         v = v0;
     }
@@ -419,7 +423,7 @@ template <int kHeads>
 struct DecSmem {
     static constexpr int kQ = 2 * kTileBytes, kP = kQ + kHeads * 1152, kMisc = kP + kTile * 128;
     struct Misc {
-        uint64_t full[2], empty[2][2], raw[2], s_full[2], s_empty[2], q_full, q_empty, q_first, p_full, p_empty, o_free, drain;
+        uint64_t full[2], empty[2][2], s_full[2], s_empty[2], q_full, q_empty, q_first, p_full, p_empty, o_free, drain[2];
         uint4 info[2];                             // of the tile whose S a stage holds: valid rows, flags, sequence
         uint32_t tmem;
         int first;
@@ -479,20 +483,20 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
         ms.first = p.n_seqs;
         ms.first_base = 0;
         for (int i = 0; i < 2; i++) {
-            bar_init(smem_u32(&ms.full[i]), 2);
+            bar_init(smem_u32(&ms.full[i]), 2 + kFillThreads / 32);
             bar_init(smem_u32(&ms.empty[i][0]), 1);
             bar_init(smem_u32(&ms.empty[i][1]), 1);
-            bar_init(smem_u32(&ms.raw[i]), 1);
             bar_init(smem_u32(&ms.s_full[i]), 2);
             bar_init(smem_u32(&ms.s_empty[i]), 4);
         }
-        bar_init(smem_u32(&ms.q_full), 1);
+        bar_init(smem_u32(&ms.q_full), kFillThreads / 32);
         bar_init(smem_u32(&ms.q_empty), 1);
-        bar_init(smem_u32(&ms.q_first), 1);          // completes once, with the first queries
+        bar_init(smem_u32(&ms.q_first), kFillThreads / 32);          // completes once, with the first queries
         bar_init(smem_u32(&ms.p_full), 4);
         bar_init(smem_u32(&ms.p_empty), 1);
         bar_init(smem_u32(&ms.o_free), 4);
-        bar_init(smem_u32(&ms.drain), 1);
+        bar_init(smem_u32(&ms.drain[0]), 1);
+        bar_init(smem_u32(&ms.drain[1]), 1);
         bar_init_fence();
     }
     __syncthreads();
@@ -515,7 +519,7 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
             const uint32_t ts = r == 0 ? tiles[0] : r == 1 ? tiles[1] : r == 2 ? tiles[2] : tiles[3];
             uint32_t b0 = 0, b1 = 0;
             if (cs) {                              // shares [b0, b1): the one the sequence starts in .. the last that starts before its end
-                b0 = (uint32_t)((uint64_t)base * slots / total);
+                b0 = mul_div(base, slots, total);
                 while (slot_start(total, b0 + 1, slots) <= base) b0++;
                 b1 = (uint32_t)(((uint64_t)(base + cs) * slots + total - 1) / total);
                 while (b1 < slots && slot_start(total, b1, slots) < base + cs) b1++;
@@ -534,7 +538,7 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
         at += cost[r];
     }
     if (lo >= hi) return;                          // nothing for this CTA
-    if (warp == 9) tmem_alloc(smem_u32(&ms.tmem), 512);
+    if (warp == 13) tmem_alloc(smem_u32(&ms.tmem), 512);
     fence_before();
     __syncthreads();
     fence_after();
@@ -547,39 +551,42 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
     TileWalk w;
     bool more = w.begin(p, first, first_base, lo, hi), ok = true;
 
-    if (warp == 8) {
+    if (warp == 12) {
         // ================================================= copies
         // (page ids are read an iteration before they are used: the read's way to L2 would otherwise sit between a freed
         // place and the copy into it)
-        uint32_t lows[2] = {0, 0};                 // LOW tiles copied into each stage
-        uint32_t i = 0, id = more ? w.page_id(lane) : 0u, ahead_id = 0;
+        uint32_t i = 0, id = more ? w.page_id(lane) : 0u, ahead_id = 0, copied = 0, phase[2] = {0, 0};
         TileWalk ahead = w;
         bool ahead_more = more;
         for (int k = 0; k < kPrefetch; k++) ahead_more = ahead_more && ahead.next();
         if (ahead_more) ahead_id = ahead.page_id(lane);
         for (; more; i++) {
-            const uint32_t st = i & 1, np = w.pages(), bytes = w.page_bytes();
+            const uint32_t st = i & 1, np = w.pages();
             const bool high = w.high();
-            const uint8_t *src = (uint32_t)lane < np ? w.page(id) : nullptr;
+            const uint8_t *src = high && (uint32_t)lane < np ? w.page(id) : nullptr;
             more = w.next();
             if (more) id = w.page_id(lane);
-            const uint32_t raw = smem_u32(&ms.raw[st]), full = smem_u32(&ms.full[st]), extra = i == 0 ? p.surplus : 0u;
+            const uint32_t full = smem_u32(&ms.full[st]), extra = i == 0 ? p.surplus : 0u;
             const uint32_t dst = kv0 + st * kTileBytes + lane * kLatentHighPageBytes;
 #pragma unroll
             for (int half = 0; half < 2; half++) {            // two pages at a time: a copy's way through the issue is long
+                // (both producers wait for every tile's stage and report to its barrier, whoever fills it: a phase's parity only
+                // tells it from its neighbours, so nobody may fall two phases behind)
                 ok = ok && (i < 2 || bar_wait(smem_u32(&ms.empty[st][half]), ((i >> 1) - 1) & 1, limit));
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
-                const uint32_t here = np > 2u * half ? min(2u, np - 2u * half) : 0u;      // pages of this half
-                if (lane == 0) {
-                    if (high) bar_expect(full, here * bytes + (half == 0 ? extra : 0u));
-                    else if (half == 0) bar_expect(raw, np * bytes + extra);
+                if (!high) {
+                    if (lane == 0) bar_arrive(full);
+                    continue;
                 }
+                const uint32_t here = np > 2u * half ? min(2u, np - 2u * half) : 0u;      // pages of this half
+                if (lane == 0) bar_expect(full, here * kLatentHighPageBytes + (half == 0 ? extra : 0u));
                 __syncwarp();
-                if ((lane >> 1) == half && (uint32_t)lane < np) bulk_load(dst, src, bytes, high ? full : raw);
+                if ((lane >> 1) == half && (uint32_t)lane < np) bulk_load(dst, src, kLatentHighPageBytes, full);
+                copied |= 1u << st;
+                if (st) phase[1] = (i >> 1) & 1; else phase[0] = (i >> 1) & 1;
             }
             if (!ok) break;
-            if (!high) { if (st) lows[1]++; else lows[0]++; }
             if (i == 1) {                          // the first queries go before rows that are not needed yet
                 ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&ms.q_first), 0, limit));
                 if (!ok) break;
@@ -591,152 +598,164 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
             }
         }
         if (!ok || p.surplus) {                    // gave up: let the copies in flight land (bounded) before the CTA ends
-            for (int k = 0; k < 2; k++) {
-                if (lows[k]) bar_wait(smem_u32(&ms.raw[k]), (lows[k] - 1) & 1, limit);
-                if (i > (uint32_t)k) bar_wait(smem_u32(&ms.full[(i - 1 - k) & 1]), ((i - 1 - k) >> 1) & 1, limit);
-            }
+            if (copied & 1u) bar_wait(smem_u32(&ms.full[0]), phase[0], limit);
+            if (copied & 2u) bar_wait(smem_u32(&ms.full[1]), phase[1], limit);
         }
-    } else if (warp == 9) {
-        // ================================================= products
-        constexpr uint32_t kIdS = instr(kTile, kHeads, false, false), kIdO = instr(128, kHeads, true, true);
-        const bool mine = elect_one();             // one lane looks at the barriers and issues; the warp follows it
-        uint32_t n_seg = 0, i = 0, j = 0;          // tiles whose S, whose O product has been issued (j <= i <= j + 2)
-        uint32_t pv_pages = 0, pv_seg = 0, next_pages = 0, next_seg = 0;
-        bool pv_first = false, next_first = false;
+    } else if (warp == 13) {
+        // ================================================= products for S
+        constexpr uint32_t kIdS = instr(kTile, kHeads, false, false);
+        const bool mine = elect_one();
+        uint32_t n_seg = 0;
         TileWalk wn = w;                           // one tile ahead of w, moved on behind the products: nothing waits for its loads
         bool after = more && wn.next();
-        while (more || j < i) {
-            // O of the oldest tile if its weights are there (that frees its stage), else S of the next tile if it is
-            int pick = 0;
-            if (mine) {
-                const long long t0 = clock64();
-                const uint32_t st = i & 1, ph = (i >> 1) & 1;
-                for (uint32_t spin = 0; !pick; spin++) {
-                    if (j < i && bar_test(smem_u32(&ms.p_full), j & 1) && (!pv_first || pv_seg < 2 || bar_test(smem_u32(&ms.o_free), (pv_seg - 2) & 1)))
-                        pick = 1;
-                    else if (more && i < j + 2 && bar_test(smem_u32(&ms.full[st]), ph) &&
-                             (i < 2 || bar_test(smem_u32(&ms.s_empty[st]), ph ^ 1)) && (!w.first() || bar_test(smem_u32(&ms.q_full), n_seg & 1)))
-                        pick = 2;
-                    else if ((spin & 255) == 255 && clock64() - t0 > limit)
-                        pick = 3;
-                }
-            }
-            // (one word over the warp, so that what the products are made from is known to be the same in every lane)
-            const uint32_t word = __reduce_max_sync(0xffffffffu, (uint32_t)pick | (i & 1) << 2 | (j & 1) << 3 | pv_pages << 4 | (pv_first ? 128u : 0u));
-            if ((word & 3) == 3) { ok = false; break; }
+        for (uint32_t i = 0; more; i++) {
+            const uint32_t st = __shfl_sync(0xffffffffu, i & 1, 0), ph = (i >> 1) & 1;
+            const bool is_first = w.first(), is_last = w.last();
+            if (is_first) ok = bar_wait(smem_u32(&ms.q_full), n_seg++ & 1, limit);
+            if (i >= 2) ok = ok && bar_wait(smem_u32(&ms.s_empty[st]), ph ^ 1, limit);
+            ok = ok && bar_wait(smem_u32(&ms.full[st]), ph, limit);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
             fence_after();
-            if ((word & 3) == 2) {
-                const uint32_t st = (word >> 2) & 1;
-                const uint32_t kv = kv0 + st * kTileBytes;
-                const uint64_t dk = desc(kv, 0, kLatentHalfPage), dq = desc(qs, 0, kLatentHalfPage);
+            const uint64_t dk = desc(kv0 + st * kTileBytes, 0, kLatentHalfPage), dq = desc(qs, 0, kLatentHalfPage);
 #pragma unroll
-                for (int k = 0; k < kLatentDim / 16; k++) {
-                    const uint64_t off = (uint64_t)(((k >> 2) * 1024 + (k & 3) * 32) >> 4);
-                    mma_ss(tmem + st * 64, dk + off, dq + off, kIdS, k > 0, mine);
-                }
-                const bool is_first = w.first(), is_last = w.last();
-                if (mine) {
-                    commit(smem_u32(&ms.s_full[st]));
-                    if (is_last) commit(smem_u32(&ms.q_empty));
-                    const uint32_t flags = (is_first ? kInfoFirst : 0u) | (is_last ? kInfoLast : 0u) | (w.whole() ? kInfoWhole : 0u);
-                    ms.info[st] = make_uint4(w.valid(), flags | (after ? 0u : kInfoFinal), (uint32_t)w.s, 0);
-                    bar_arrive(smem_u32(&ms.s_full[st]));
-                }
-                n_seg += is_first;
-                if (i == j) { pv_pages = w.pages(); pv_seg = n_seg; pv_first = is_first; }
-                else { next_pages = w.pages(); next_seg = n_seg; next_first = is_first; }
-                i++;
-                more = after;
-                if (more) {
-                    w = wn;
-                    after = wn.next();
-                }
-            } else {
-                const uint32_t sv = (word >> 3) & 1, np = (word >> 4) & 7;
-                const bool fresh = word & 128u;
-                const uint64_t dv = desc(kv0 + sv * kTileBytes, 1024, kLatentHalfPage), dp = desc(ps, 0, 1024);
-#pragma unroll
-                for (int k = 0; k < kTilePages; k++) {
-                    if ((uint32_t)k < np) {
-#pragma unroll
-                        for (int b = 0; b < 4; b++)
-                            mma_ss(tmem + kO + b * 64, dv + (uint64_t)((k * kLatentHighPageBytes + b * 2048) >> 4), dp + (uint64_t)(k * 2048 >> 4),
-                                   kIdO, k > 0 || !fresh, mine);
-                    }
-                    if ((k & 1) && mine) commit(smem_u32(&ms.empty[sv][k >> 1]));
-                }
-                if (mine) commit(smem_u32(&ms.p_empty));
-                j++;
-                pv_pages = next_pages; pv_seg = next_seg; pv_first = next_first;
+            for (int k = 0; k < kLatentDim / 16; k++) {
+                const uint64_t off = (uint64_t)(((k >> 2) * 1024 + (k & 3) * 32) >> 4);
+                mma_ss(tmem + st * 64, dk + off, dq + off, kIdS, k > 0, mine);
+            }
+            if (mine) {
+                commit(smem_u32(&ms.s_full[st]));
+                if (is_last) commit(smem_u32(&ms.q_empty));
+                const uint32_t flags = (is_first ? kInfoFirst : 0u) | (is_last ? kInfoLast : 0u) | (w.whole() ? kInfoWhole : 0u);
+                ms.info[st] = make_uint4(w.valid(), flags | (after ? 0u : kInfoFinal), (uint32_t)w.s, 0);
+                bar_arrive(smem_u32(&ms.s_full[st]));
+            }
+            more = after;
+            if (more) {
+                w = wn;
+                after = wn.next();
             }
         }
         if (!ok) {                                 // gave up: the products in flight end before tensor memory is freed
-            if (mine) commit(smem_u32(&ms.drain));
-            bar_wait(smem_u32(&ms.drain), 0, limit);
+            if (mine) commit(smem_u32(&ms.drain[0]));
+            bar_wait(smem_u32(&ms.drain[0]), 0, limit);
+        }
+        __syncwarp();
+    } else if (warp == 14) {
+        // ================================================= products for O
+        constexpr uint32_t kIdO = instr(128, kHeads, true, true);
+        const bool mine = elect_one();
+        uint32_t n_seg = 0;
+        for (uint32_t i = 0; more; i++) {
+            const uint32_t st = __shfl_sync(0xffffffffu, i & 1, 0), np = __shfl_sync(0xffffffffu, w.pages(), 0);
+            const bool fresh = __shfl_sync(0xffffffffu, (int)w.first(), 0) != 0;
+            // (the segment before has been read out of O)
+            if (fresh && n_seg++ > 0) ok = bar_wait(smem_u32(&ms.o_free), (n_seg - 2) & 1, limit);
+            ok = ok && bar_wait(smem_u32(&ms.p_full), i & 1, limit);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            fence_after();
+            const uint64_t dv = desc(kv0 + st * kTileBytes, 1024, kLatentHalfPage), dp = desc(ps, 0, 1024);
+#pragma unroll
+            for (int k = 0; k < kTilePages; k++) {
+                if ((uint32_t)k < np) {
+#pragma unroll
+                    for (int b = 0; b < 4; b++)
+                        mma_ss(tmem + kO + b * 64, dv + (uint64_t)((k * kLatentHighPageBytes + b * 2048) >> 4), dp + (uint64_t)(k * 2048 >> 4),
+                               kIdO, k > 0 || !fresh, mine);
+                }
+                if ((k & 1) && mine) commit(smem_u32(&ms.empty[st][k >> 1]));
+            }
+            if (mine) commit(smem_u32(&ms.p_empty));
+            more = w.next();
+        }
+        if (!ok) {
+            if (mine) commit(smem_u32(&ms.drain[1]));
+            bar_wait(smem_u32(&ms.drain[1]), 0, limit);
         }
         __syncwarp();
     } else if (warp >= 4) {
         // ================================================= queries and LOW tiles
-        const int t = tid - 128;                   // 0..127: token t & 15, (page, group) pairs t >> 4 + 8 k
-        constexpr int kPasses = BITS == 8 ? 2 : 1, kPassPages = kTilePages / kPasses;        // what the registers hold at a time
-        constexpr int kItems = (kPassPages * kLatentGroups + 7) / 8;
-        uint32_t n_seg = 0, lows[2] = {0, 0};
-        bool bad = false;
+        const int t = tid - 128;                   // token t & 15 and (page, group) pairs t >> 4 + 16 k of a tile
+        constexpr int kPairs = kTilePages * kLatentGroups, kItems = (kPairs + kFillThreads / 16 - 1) / (kFillThreads / 16);
+        uint32_t codes[kItems][BITS], scales[kItems], ids[kItems];
+        TileWalk ahead = w;                        // codes: of the next LOW tile; ahead, ids: the one behind it
+        auto pair_of = [&](int k) { return (kFillThreads / 16) * k + (t >> 4); };
+        auto to_low = [&](bool here) { while (here && ahead.high()) here = ahead.next(); return here; };
+        auto fetch_ids = [&]() {
+#pragma unroll
+            for (int k = 0; k < kItems; k++) ids[k] = pair_of(k) < kPairs ? ahead.page_id((uint32_t)(pair_of(k) / kLatentGroups)) : 0u;
+        };
+        auto fetch_codes = [&]() {
+#pragma unroll
+            for (int k = 0; k < kItems; k++) {
+                const int pair = pair_of(k);
+                if (pair < kPairs && (uint32_t)(pair / kLatentGroups) < ahead.pages()) {
+                    const uint8_t *src = ahead.page(ids[k]);
+                    load_codes<BITS>(src, t & 15, pair % kLatentGroups, codes[k]);
+                    scales[k] = *reinterpret_cast<const uint16_t *>(src + latent_scale_off(t & 15, pair % kLatentGroups, BITS));
+                }
+            }
+        };
+        bool ahead_more = to_low(more);
+        if (ahead_more) fetch_ids();
+        bool primed = false;                       // the first codes are asked for behind the first queries
+        auto advance = [&]() {
+            if (ahead_more) {
+                fetch_codes();
+                ahead_more = to_low(ahead.next());
+                if (ahead_more) fetch_ids();
+            }
+        };
+        uint32_t n_seg = 0;
         for (uint32_t i = 0; more; i++, more = w.next()) {
             const uint32_t st = i & 1;
             if (w.first()) {
                 if (n_seg > 0) ok = bar_wait(smem_u32(&ms.q_empty), (n_seg - 1) & 1, ok ? limit : 0) && ok;
                 n_seg++;
                 const uint4 *src = p.q + ((size_t)w.s * p.c.n_q + h0) * kLatentChunks;
-                constexpr int kIter = kHeads * kLatentChunks / 128;
+                constexpr int kChunks = kHeads * kLatentChunks;
 #pragma unroll 6
-                for (int k = 0; k < kIter; k++) {  // all in flight at once; heads this CTA does not have are zeros
-                    const int x = k * 128 + t, row = x / kLatentChunks, ch = x % kLatentChunks;
+                for (int x = t; x < kChunks; x += kFillThreads) {      // all in flight at once; heads this CTA does not have are zeros
+                    const int row = x / kLatentChunks, ch = x % kLatentChunks;
                     const bool there = row < nh_here;
                     copy16(qs + (row >> 4) * kLatentHighPageBytes + latent_chunk_off(row & 15, ch), there ? src + x : src, there ? 16 : 0);
                 }
+                if (!primed) { advance(); primed = true; }
                 copy16_wait();
                 fence_async_shared();
-                if (group_any(2, 128, !ok)) break;
-                if (t == 0) bar_arrive(smem_u32(&ms.q_full));
-                if (t == 0 && n_seg == 1) bar_arrive(smem_u32(&ms.q_first));
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                if (lane == 0) bar_arrive(smem_u32(&ms.q_full));
+                if (lane == 0 && n_seg == 1) bar_arrive(smem_u32(&ms.q_first));
             }
-            if (!w.high()) {
-                // the codes of a page were copied to the start of its place in the stage: out to registers, then values over them
-                const uint32_t n = st ? lows[1]++ : lows[0]++, np = w.pages();
-                ok = bar_wait(smem_u32(&ms.raw[st]), n & 1, ok ? limit : 0) && ok;
+            if (i >= 2) {
+                ok = bar_wait(smem_u32(&ms.empty[st][0]), ((i >> 1) - 1) & 1, ok ? limit : 0) && ok;
+                ok = bar_wait(smem_u32(&ms.empty[st][1]), ((i >> 1) - 1) & 1, ok ? limit : 0) && ok;
+            }
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            const bool low = !w.high();
+            if (low) {
+                const uint32_t np = w.pages();
                 uint8_t *dst = sm + st * kTileBytes;
-#pragma unroll 1
-                for (int pass = 0; pass < kPasses; pass++) {
-                    uint32_t codes[kItems][BITS], scales[kItems];
 #pragma unroll
-                    for (int k = 0; k < kItems; k++) {
-                        const int pair = 8 * k + (t >> 4), pg = kPassPages * pass + pair / kLatentGroups, g = pair % kLatentGroups;
-                        if (pair < kPassPages * kLatentGroups && (uint32_t)pg < np) {
-                            load_codes<BITS>(dst + pg * kLatentHighPageBytes, t & 15, g, codes[k]);
-                            scales[k] = *reinterpret_cast<const uint16_t *>(dst + pg * kLatentHighPageBytes + latent_scale_off(t & 15, g, BITS));
-                        }
-                    }
-                    bad = group_any(2, 128, !ok);
-                    if (bad) break;
+                for (int k = 0; k < kItems; k++) {
+                    const int pair = pair_of(k), pg = pair / kLatentGroups, g = pair % kLatentGroups;
+                    if (pair < kPairs && (uint32_t)pg < np) {
+                        uint32_t xs[16];
+                        dequantise_group<BITS>(codes[k], scales[k], xs);
 #pragma unroll
-                    for (int k = 0; k < kItems; k++) {
-                        const int pair = 8 * k + (t >> 4), pg = kPassPages * pass + pair / kLatentGroups, g = pair % kLatentGroups;
-                        if (pair < kPassPages * kLatentGroups && (uint32_t)pg < np) {
-                            uint32_t xs[16];
-                            dequantise_group<BITS>(codes[k], scales[k], xs);
-#pragma unroll
-                            for (int e = 0; e < 4; e++)
-                                *reinterpret_cast<uint4 *>(dst + pg * kLatentHighPageBytes + latent_chunk_off(t & 15, 4 * g + e)) =
-                                    make_uint4(xs[4 * e], xs[4 * e + 1], xs[4 * e + 2], xs[4 * e + 3]);
-                        }
+                        for (int e = 0; e < 4; e++)
+                            *reinterpret_cast<uint4 *>(dst + pg * kLatentHighPageBytes + latent_chunk_off(t & 15, 4 * g + e)) =
+                                make_uint4(xs[4 * e], xs[4 * e + 1], xs[4 * e + 2], xs[4 * e + 3]);
                     }
                 }
-                if (bad) break;
                 fence_async_shared();
-                group_sync(2, 128);
-                if (t < 2) bar_arrive(smem_u32(&ms.full[st]));
+                __syncwarp();
             }
+            if (lane == 0) bar_arrive(smem_u32(&ms.full[st]));
+            if (low) advance();
         }
     } else {
         // ================================================= softmax; warp = page of the tile, rows lane / 4 and lane / 4 + 8
@@ -903,7 +922,7 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
     fence_before();
     __syncthreads();
     fence_after();
-    if (warp == 9) tmem_free(tmem, 512);
+    if (warp == 13) tmem_free(tmem, 512);
     if (p.span && tid == 0) {
         unsigned long long t_end;
         asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t_end));
@@ -947,7 +966,7 @@ decode_latent_merge(int n_seqs, int n_q, const uint4 *__restrict__ meta, const f
     // rows of the sequence in share b: 0 none, 1 some, 2 all (the share has written the result)
     auto used = [&](uint32_t b) {
         const uint32_t lo = slot_start(total, b, slots), hi = slot_start(total, b + 1, slots);
-        const uint32_t v0 = lo > base ? cut_positions(lo - base, cost, n) : 0u, v1 = hi > base ? cut_positions(hi - base, cost, n) : 0u;
+        const uint32_t v0 = lo > base ? cut_at(lo - base, cost, n) : 0u, v1 = hi > base ? cut_at(hi - base, cost, n) : 0u;
         return v1 <= v0 ? 0 : v0 == 0 && v1 == n ? 2 : 1;
     };
     float top = -INFINITY;

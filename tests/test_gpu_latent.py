@@ -370,6 +370,21 @@ def test_decode_after_growth_and_reuse(pask):
     assert b.status() == 0
 
 
+@pytest.mark.parametrize("mix", [(3, 0, 2), (1, 0, 9), (9, 0, 1), (1, 1, 1)])
+def test_decode_long_shares_of_both_formats(pask, mix):
+    # dozens of tiles in a share, formats alternating in every rhythm: neither producer may outrun the other's barriers
+    g = torch.Generator().manual_seed(14)
+    lut = [[2]] * mix[0] + [[0]] * mix[1] + [[1]] * mix[2]
+    b = Both(pask, heads=40, max_seqs=2, n_layers=1, lut=lut, max_tokens=6000, pages=800)
+    for s, n in enumerate([5200, 3100]):
+        b.append(0, [s], [normal(g, n, 576)], [tags_of(g, n, len(lut))])
+    for ctas in (2, 5):
+        pask.pask_debug_set_attention_ctas(b.h, ctas)
+        b.gpu._ws = None
+        b.check_decode(0, [0, 1], normal(g, 2, 40, 576))
+        assert b.status() == 0
+
+
 def test_decode_bad_ids_and_no_lse(pask):
     g = torch.Generator().manual_seed(6)
     b = Both(pask, heads=16, n_layers=1)
