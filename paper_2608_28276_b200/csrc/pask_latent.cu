@@ -682,19 +682,25 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
         TileWalk ahead = w;                        // codes: of the next LOW tile; ahead, ids: the one behind it
         auto pair_of = [&](int k) { return (kFillThreads / 16) * k + (t >> 4); };
         auto to_low = [&](bool here) { while (here && ahead.high()) here = ahead.next(); return here; };
+        // (no branch around the loads, items and pages that are not there read their last neighbour's: a load under a condition
+        // was waited for where the paths join, 2500 cycles a tile)
         auto fetch_ids = [&]() {
+            const uint32_t *tbl = p.c.tbl_low + ahead.sl * p.c.max_pages + kTilePages * ahead.tile();
+            const uint32_t last = ahead.pages() - 1;
 #pragma unroll
-            for (int k = 0; k < kItems; k++) ids[k] = pair_of(k) < kPairs ? ahead.page_id((uint32_t)(pair_of(k) / kLatentGroups)) : 0u;
+            for (int k = 0; k < kItems; k++) ids[k] = tbl[min((uint32_t)(min(pair_of(k), kPairs - 1) / kLatentGroups), last)];
         };
         auto fetch_codes = [&]() {
+            uint32_t most = 0;
+#pragma unroll
+            for (int k = 0; k < kItems; k++) most = max(most, ids[k]);
+            if (most >= p.c.cap_low) atomicOr(&p.c.ctrl[kCtrlStatus], PASK_DEV_INTERNAL);      // never expected, never dereferenced
 #pragma unroll
             for (int k = 0; k < kItems; k++) {
-                const int pair = pair_of(k);
-                if (pair < kPairs && (uint32_t)(pair / kLatentGroups) < ahead.pages()) {
-                    const uint8_t *src = ahead.page(ids[k]);
-                    load_codes<BITS>(src, t & 15, pair % kLatentGroups, codes[k]);
-                    scales[k] = *reinterpret_cast<const uint16_t *>(src + latent_scale_off(t & 15, pair % kLatentGroups, BITS));
-                }
+                const int pair = min(pair_of(k), kPairs - 1);
+                const uint8_t *src = p.c.pool_low + (size_t)(ids[k] < p.c.cap_low ? ids[k] : 0u) * p.c.low_page_bytes;
+                load_codes<BITS>(src, t & 15, pair % kLatentGroups, codes[k]);
+                scales[k] = *reinterpret_cast<const uint16_t *>(src + latent_scale_off(t & 15, pair % kLatentGroups, BITS));
             }
         };
         bool ahead_more = to_low(more);
