@@ -7,6 +7,8 @@
 //   decode_latent    attention of one new query per sequence, absorbed form
 #include <cuda_bf16.h>
 
+#include <cstddef>
+
 #include "pask_internal.h"
 #include "pask_umma.h"
 
@@ -299,8 +301,9 @@ read_latent_kernel(DevCache c, int layer, int n_seqs, int total_rows, const int3
 // accumulators of all 512 value dims fit tensor memory (4 x 64 columns, beside two S tiles).  More than 64 heads are split
 // over that many CTAs that walk the same tiles side by side and find each other's rows in L2.
 //
-// A CTA is one of `slots` equal shares of the batch's rows (cost line over sequences, as the other decode kernel cuts it), in
-// tiles of 64 rows = four pages of one stream; a sequence's HIGH and LOW tiles are visited in turn, evenly mixed.  Roles:
+// A CTA is one of `slots` equal shares of the batch's tiles: 64 rows = four pages of one stream, a sequence's HIGH and LOW tiles
+// visited in turn, evenly mixed.  (A LOW tile is a quarter of the bytes but as much work on chip: 4.2 and 4.5 thousand cycles
+// at 32 heads, so a tile counts as a tile.)  Roles:
 //   warp 12     HIGH tiles: one linear bulk copy a page (pages are stored in the operand layout) into its place in one of two
 //               stages, as soon as the product that last read the place is done, and a prefetch into L2 some tiles ahead
 //   warps 4-11  LOW tiles: codes in registers one tile ahead, values as bf16 into the stage; and the queries of a sequence
@@ -315,7 +318,6 @@ constexpr int kTileBytes = kTilePages * kLatentHighPageBytes;      // 73728
 constexpr int kDecThreads = 480, kFillThreads = 256;
 constexpr uint32_t kMaxSlots = 1024;
 constexpr int kPrefetch = 4;                       // tiles between a prefetch into L2 and the copy
-constexpr uint32_t kCostHighTile = 3, kCostLowTile = 2;
 enum : uint32_t { kInfoFirst = 1, kInfoLast = 2, kInfoWhole = 4, kInfoFinal = 8 };   // first, last tile of a sequence's part; the part
                                                    // is the whole sequence; last tile of the share
 constexpr float kLazy = 8.0f;                      // log2 of how far a score may exceed the reference maximum
@@ -329,8 +331,8 @@ struct DecParams {
     float scale_log2;
     __nv_bfloat16 *out;
     float *lse;
-    uint4 *meta;                                   // [n_seqs + 1] per sequence {cost before it, its cost, its tiles, first share | shares
-                                                   // << 16}; behind them {cost of all, shares in use}
+    uint4 *meta;                                   // [n_seqs + 1] per sequence {tiles before it, its tiles, first share, end of its
+                                                   // shares}; behind them {tiles of all, shares in use}
     float2 *part_ml;                               // [slots + n_seqs][n_q] (reference maximum in log2 units, sum)
     float *part_o;                                 // [slots + n_seqs][n_q][512]
     long long wait_cycles;
@@ -344,52 +346,42 @@ __device__ __forceinline__ uint32_t mul_div(uint32_t a, uint32_t b, uint32_t c) 
     const uint64_t x = (uint64_t)a * b;
     return (x >> 32) == 0 ? (uint32_t)x / c : (uint32_t)(x / c);
 }
+// share b of `slots` is tiles [start(b), start(b + 1)) of all
 __device__ __forceinline__ uint32_t slot_start(uint32_t total, uint32_t slot, uint32_t slots) { return mul_div(total, slot, slots); }
-// positions (of n) before offset x of a sequence of cost cs: cut_positions of pask_layout.h
-__device__ __forceinline__ uint32_t cut_at(uint32_t x, uint32_t cs, uint32_t n) { return x >= cs ? n : mul_div(x, n, cs); }
 
 // The tiles of one share, in order; the roles walk their own copies.
 struct TileWalk {
     const DevCache *c;
     const int32_t *seq_ids;
     int layer, n_seqs, s;
-    uint32_t lo, hi, base, cost;
+    uint32_t lo, hi, base;                         // the share; tiles of the sequences before s
     uint32_t nh, nl, th, n, v, v0, v1;             // rows of the streams; HIGH tiles, tiles, position and range of it
     uint32_t h0, rem;                              // v * th = h0 * n + rem (page_at of pask_layout.h without its divisions)
     size_t sl;
 
-    __device__ __forceinline__ void load() {
-        const int seq = seq_ids[s];
-        const bool ok = seq >= 0 && seq < c->max_seqs;
-        sl = (size_t)(ok ? seq : 0) * c->n_layers + layer;
-        nh = ok ? c->n_high[sl] : 0u;
-        nl = ok ? c->n_low[sl] : 0u;
+    __device__ __forceinline__ void enter(uint32_t high_rows, uint32_t low_rows) {
+        nh = high_rows;
+        nl = low_rows;
         th = tiles_of(nh);
         n = th + tiles_of(nl);
-        cost = kCostHighTile * th + kCostLowTile * (n - th);
-        v0 = v1 = h0 = rem = 0;
-        if (cost) {
-            v0 = lo > base ? cut_at(lo - base, cost, n) : 0u;
-            v1 = cut_at(hi - base, cost, n);
+        v = v0 = lo > base ? lo - base : 0u;
+        v1 = min(n, hi - base);
+        h0 = rem = 0;
+        if (v0) {
             h0 = mul_div(v0, th, n);
             rem = (uint32_t)((uint64_t)v0 * th - (uint64_t)h0 * n);
         }
-        v = v0;
     }
     __device__ __forceinline__ bool settle() {     // on to a sequence with tiles in the share
         while (v >= v1) {
-            base += cost;
+            base += n;
             if (++s >= n_seqs || base >= hi) return false;
-            load();
+            const int seq = seq_ids[s];
+            const bool ok = seq >= 0 && seq < c->max_seqs;
+            sl = (size_t)(ok ? seq : 0) * c->n_layers + layer;
+            enter(ok ? c->n_high[sl] : 0u, ok ? c->n_low[sl] : 0u);
         }
         return true;
-    }
-    __device__ __forceinline__ bool begin(const DecParams &p, int first, uint32_t first_base, uint32_t lo_, uint32_t hi_) {
-        c = &p.c; seq_ids = p.seq_ids; layer = p.layer; n_seqs = p.n_seqs;
-        lo = lo_; hi = hi_; s = first; base = first_base;
-        if (s >= n_seqs) return false;
-        load();
-        return settle();
     }
     __device__ __forceinline__ bool next() {
         v++;
@@ -426,11 +418,14 @@ struct DecSmem {
         uint64_t full[2], empty[2][2], s_full[2], s_empty[2], q_full, q_empty, q_first, p_full, p_empty, o_free, drain[2];
         uint4 info[2];                             // of the tile whose S a stage holds: valid rows, flags, sequence
         uint32_t tmem;
-        int first;
-        uint32_t first_base, total;
-        uint32_t warp_sum[kDecThreads / 32], warp_tiles[kDecThreads / 32];
-        float red[4][kHeads], fac[kHeads], mref[kHeads];
+        int first;                                 // the sequence of the share's first tile: index, tiles before it, rows, place
+        uint32_t first_base, first_high, first_low;
+        size_t first_sl;
+        uint32_t warp_sum[kDecThreads / 32];
+        alignas(16) float red[4][kHeads];
+        alignas(16) float fac[kHeads], mref[kHeads];           // read in pairs
     };
+    static_assert(offsetof(Misc, fac) % 8 == 0 && offsetof(Misc, mref) % 8 == 0 && offsetof(Misc, info) % 16 == 0 && kMisc % 16 == 0, "vector loads");
     static constexpr int kBytes = kMisc + (int)sizeof(Misc) + 1024;
 };
 
@@ -445,97 +440,96 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
     const uint32_t slot = blockIdx.x / p.groups, group = blockIdx.x % p.groups;
     const int h0 = (int)group * p.heads, nh_here = min(p.heads, p.c.n_q - h0);       // this CTA's query heads
-    pdl_launch_dependents();
-    pdl_wait();
-    unsigned long long t_start = 0;
-    if (p.span && tid == 0) asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t_start));
-
-    // ---- the share: cost prefix over the sequences (1024 at most, kPer a thread)
-    constexpr int kPer = (PASK_MAX_SEQS_PER_CALL + kDecThreads - 1) / kDecThreads;
-    uint32_t cost[kPer], tiles[kPer], sum = 0, sum_tiles = 0;
-#pragma unroll
-    for (int r = 0; r < kPer; r++) {
-        const int s = tid * kPer + r;
-        cost[r] = tiles[r] = 0;
-        if (s < p.n_seqs) {
-            const int seq = p.seq_ids[s];
-            if (seq >= 0 && seq < p.c.max_seqs) {
-                const size_t sl = (size_t)seq * p.c.n_layers + p.layer;
-                const uint32_t th = tiles_of(p.c.n_high[sl]), tl = tiles_of(p.c.n_low[sl]);
-                cost[r] = kCostHighTile * th + kCostLowTile * tl;
-                tiles[r] = th + tl;
-            } else if (blockIdx.x == 0) {
-                atomicOr(&p.c.ctrl[kCtrlStatus], PASK_DEV_BAD_SEQ);
-            }
-        }
-        sum += cost[r];
-        sum_tiles += tiles[r];
-    }
-    sum_tiles = __reduce_add_sync(0xffffffffu, sum_tiles);
-    uint32_t inc = sum;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-        const uint32_t o = __shfl_up_sync(0xffffffffu, inc, d);
-        if (lane >= d) inc += o;
-    }
-    if (lane == 31) { ms.warp_sum[warp] = inc; ms.warp_tiles[warp] = sum_tiles; }
     if (tid == 0) {
-        ms.first = p.n_seqs;
-        ms.first_base = 0;
         for (int i = 0; i < 2; i++) {
             bar_init(smem_u32(&ms.full[i]), 2 + kFillThreads / 32);
             bar_init(smem_u32(&ms.empty[i][0]), 1);
             bar_init(smem_u32(&ms.empty[i][1]), 1);
             bar_init(smem_u32(&ms.s_full[i]), 2);
             bar_init(smem_u32(&ms.s_empty[i]), 4);
+            bar_init(smem_u32(&ms.drain[i]), 1);
         }
         bar_init(smem_u32(&ms.q_full), kFillThreads / 32);
         bar_init(smem_u32(&ms.q_empty), 1);
-        bar_init(smem_u32(&ms.q_first), kFillThreads / 32);          // completes once, with the first queries
+        bar_init(smem_u32(&ms.q_first), kFillThreads / 32);    // completes once, with the first queries
         bar_init(smem_u32(&ms.p_full), 4);
         bar_init(smem_u32(&ms.p_empty), 1);
         bar_init(smem_u32(&ms.o_free), 4);
-        bar_init(smem_u32(&ms.drain[0]), 1);
-        bar_init(smem_u32(&ms.drain[1]), 1);
         bar_init_fence();
     }
+    pdl_launch_dependents();
+    pdl_wait();
+    unsigned long long t_start = 0;
+    if (p.span && tid == 0) asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t_start));
+
+    // ---- the share: prefix of tiles over the sequences (1024 at most, kPer a thread)
+    constexpr int kPer = (PASK_MAX_SEQS_PER_CALL + kDecThreads - 1) / kDecThreads;
+    uint32_t nh[kPer], nl[kPer], tiles[kPer], sum = 0;
+    size_t sl[kPer];
+#pragma unroll
+    for (int r = 0; r < kPer; r++) {
+        const int s = tid * kPer + r;
+        nh[r] = nl[r] = 0;
+        sl[r] = 0;
+        if (s < p.n_seqs) {
+            const int seq = p.seq_ids[s];
+            if (seq >= 0 && seq < p.c.max_seqs) {
+                sl[r] = (size_t)seq * p.c.n_layers + p.layer;
+                nh[r] = p.c.n_high[sl[r]];
+                nl[r] = p.c.n_low[sl[r]];
+            } else if (blockIdx.x == 0) {
+                atomicOr(&p.c.ctrl[kCtrlStatus], PASK_DEV_BAD_SEQ);
+            }
+        }
+        tiles[r] = tiles_of(nh[r]) + tiles_of(nl[r]);
+        sum += tiles[r];
+    }
+    uint32_t inc = sum;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const uint32_t o = __shfl_up_sync(0xffffffffu, inc, d);
+        if (lane >= d) inc += o;
+    }
+    if (lane == 31) ms.warp_sum[warp] = inc;
     __syncthreads();
-    uint32_t at = inc - sum, total = 0, slots = 0;
+    uint32_t at = inc - sum, total = 0;
 #pragma unroll
     for (int w = 0; w < kDecThreads / 32; w++) {
         if (w < warp) at += ms.warp_sum[w];
         total += ms.warp_sum[w];
-        slots += ms.warp_tiles[w];
     }
-    slots = min(slots, p.slots);                   // no more shares than tiles
-    if (blockIdx.x == 0) {                         // what the merge needs to know
-        if (tid == 0) p.meta[p.n_seqs] = make_uint4(total, slots, 0, 0);
-        uint32_t base = at;
-#pragma unroll 1
-        for (int r = 0; r < kPer; r++) {
-            const int s = tid * kPer + r;
-            if (s >= p.n_seqs) break;
-            const uint32_t cs = r == 0 ? cost[0] : r == 1 ? cost[1] : r == 2 ? cost[2] : cost[3];
-            const uint32_t ts = r == 0 ? tiles[0] : r == 1 ? tiles[1] : r == 2 ? tiles[2] : tiles[3];
-            uint32_t b0 = 0, b1 = 0;
-            if (cs) {                              // shares [b0, b1): the one the sequence starts in .. the last that starts before its end
-                b0 = mul_div(base, slots, total);
-                while (slot_start(total, b0 + 1, slots) <= base) b0++;
-                b1 = (uint32_t)(((uint64_t)(base + cs) * slots + total - 1) / total);
-                while (b1 < slots && slot_start(total, b1, slots) < base + cs) b1++;
-                while (b1 > b0 + 1 && slot_start(total, b1 - 1, slots) >= base + cs) b1--;
-            }
-            p.meta[s] = make_uint4(base, cs, ts, b0 | (b1 - b0) << 16);
-            base += cs;
-        }
-    }
-    if (slot >= slots) return;
-    const uint32_t lo = slot_start(total, slot, slots), hi = slot_start(total, slot + 1, slots);
+    const uint32_t slots = min(total, p.slots);    // no more shares than tiles
+    const uint32_t lo = slot < slots ? slot_start(total, slot, slots) : 0u, hi = slot < slots ? slot_start(total, slot + 1, slots) : 0u;
+    uint32_t base = at;
 #pragma unroll
     for (int r = 0; r < kPer; r++) {
-        const int s = tid * kPer + r;
-        if (s < p.n_seqs && at <= lo && lo < at + cost[r]) { ms.first = s; ms.first_base = at; }
-        at += cost[r];
+        if (base <= lo && lo < base + tiles[r] && lo < hi) {
+            ms.first = tid * kPer + r;
+            ms.first_base = base;
+            ms.first_high = nh[r];
+            ms.first_low = nl[r];
+            ms.first_sl = sl[r];
+        }
+        base += tiles[r];
+    }
+    if (blockIdx.x == 0) {                         // what the merge needs to know
+        if (tid == 0) p.meta[p.n_seqs] = make_uint4(total, slots, 0, 0);
+        base = at;
+#pragma unroll
+        for (int r = 0; r < kPer; r++) {
+            const int s = tid * kPer + r;
+            if (s < p.n_seqs) {
+                uint32_t b0 = 0, b1 = 0;
+                if (tiles[r]) {                    // shares [b0, b1): the one its first tile is in .. the one its last is in
+                    b0 = mul_div(base, slots, total);
+                    while (slot_start(total, b0 + 1, slots) <= base) b0++;
+                    b1 = mul_div(base + tiles[r] - 1, slots, total) + 1;
+                    while (slot_start(total, b1, slots) < base + tiles[r]) b1++;
+                }
+                p.meta[s] = make_uint4(base, tiles[r], b0, b1);
+            }
+            base += tiles[r];
+        }
     }
     if (lo >= hi) return;                          // nothing for this CTA
     if (warp == 13) tmem_alloc(smem_u32(&ms.tmem), 512);
@@ -544,12 +538,13 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
     fence_after();
     const uint32_t tmem = ms.tmem;
     constexpr uint32_t kO = 128;                   // columns: S tiles at 0 and 64, O blocks from 128
-    const int first = ms.first;
-    const uint32_t first_base = ms.first_base;
     const uint32_t kv0 = smem_u32(sm), qs = smem_u32(sm + Sm::kQ), ps = smem_u32(sm + Sm::kP);
     const long long limit = p.wait_cycles;
     TileWalk w;
-    bool more = w.begin(p, first, first_base, lo, hi), ok = true;
+    w.c = &p.c; w.seq_ids = p.seq_ids; w.layer = p.layer; w.n_seqs = p.n_seqs;
+    w.lo = lo; w.hi = hi; w.s = ms.first; w.base = ms.first_base; w.sl = ms.first_sl;
+    w.enter(ms.first_high, ms.first_low);
+    bool more = true, ok = true;
 
     if (warp == 12) {
         // ================================================= copies
@@ -558,8 +553,6 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
         uint32_t i = 0, id = more ? w.page_id(lane) : 0u, ahead_id = 0, copied = 0, phase[2] = {0, 0};
         TileWalk ahead = w;
         bool ahead_more = more;
-        for (int k = 0; k < kPrefetch; k++) ahead_more = ahead_more && ahead.next();
-        if (ahead_more) ahead_id = ahead.page_id(lane);
         for (; more; i++) {
             const uint32_t st = i & 1, np = w.pages();
             const bool high = w.high();
@@ -587,6 +580,11 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
                 if (st) phase[1] = (i >> 1) & 1; else phase[0] = (i >> 1) & 1;
             }
             if (!ok) break;
+            if (i == 0) {
+                for (int k = 0; k < kPrefetch; k++) ahead_more = ahead_more && ahead.next();
+                if (ahead_more) ahead_id = ahead.page_id(lane);
+                continue;
+            }
             if (i == 1) {                          // the first queries go before rows that are not needed yet
                 ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&ms.q_first), 0, limit));
                 if (!ok) break;
@@ -735,18 +733,13 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
                 if (lane == 0) bar_arrive(smem_u32(&ms.q_full));
                 if (lane == 0 && n_seg == 1) bar_arrive(smem_u32(&ms.q_first));
             }
-            if (i >= 2) {
-                ok = bar_wait(smem_u32(&ms.empty[st][0]), ((i >> 1) - 1) & 1, ok ? limit : 0) && ok;
-                ok = bar_wait(smem_u32(&ms.empty[st][1]), ((i >> 1) - 1) & 1, ok ? limit : 0) && ok;
-            }
-            ok = __all_sync(0xffffffffu, ok);
-            if (!ok) break;
             const bool low = !w.high();
-            if (low) {
-                const uint32_t np = w.pages();
-                uint8_t *dst = sm + st * kTileBytes;
+            const uint32_t np = w.pages();
+            uint8_t *dst = sm + st * kTileBytes;
+            // items [k0, k1), the first half of which lie in the stage's first two pages
+            auto fill = [&](int k0, int k1) {
 #pragma unroll
-                for (int k = 0; k < kItems; k++) {
+                for (int k = k0; k < k1; k++) {
                     const int pair = pair_of(k), pg = pair / kLatentGroups, g = pair % kLatentGroups;
                     if (pair < kPairs && (uint32_t)pg < np) {
                         uint32_t xs[16];
@@ -757,6 +750,15 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
                                 make_uint4(xs[4 * e], xs[4 * e + 1], xs[4 * e + 2], xs[4 * e + 3]);
                     }
                 }
+            };
+            static_assert(kItems == 5 && 2 * (kFillThreads / 16) <= 2 * kLatentGroups, "items 0 and 1 are pages 0 and 1");
+            if (i >= 2) ok = bar_wait(smem_u32(&ms.empty[st][0]), ((i >> 1) - 1) & 1, ok ? limit : 0) && ok;
+            if (low && ok) fill(0, 2);
+            if (i >= 2) ok = bar_wait(smem_u32(&ms.empty[st][1]), ((i >> 1) - 1) & 1, ok ? limit : 0) && ok;
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            if (low) {
+                fill(2, kItems);
                 fence_async_shared();
                 __syncwarp();
             }
@@ -937,102 +939,86 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
     }
 }
 
-// Joins the partial sums of one (sequence, head): CTA = row, kSplit groups of 128 threads take every kSplit-th partial, a
-// thread has four of the 512 dims.  A group's first eight partials are fetched before their weights are known: two trips to
-// L2 (what the sequence's shares are; their partials), not three.  Sequences that one share covered are left alone; empty
-// ones are written here.
-template <int kSplit>
+// Joins the partial sums of a sequence: a CTA takes kRows heads of it (few sequences: one, with the partials split over kSplit
+// groups of threads), a thread four of the 512 dims.  Two trips to L2: what the sequence's shares are, and their partials
+// (the first ones of every head fetched before their weights are known).  Sequences that one share covered are left alone;
+// empty ones are written here.
+template <int kSplit, int kRows>
 __global__ void __launch_bounds__(128 * kSplit)
 decode_latent_merge(int n_seqs, int n_q, const uint4 *__restrict__ meta, const float2 *__restrict__ part_ml,
                     const float *__restrict__ part_o, __nv_bfloat16 *__restrict__ out, float *__restrict__ lse) {
-    __shared__ float s_w[kMaxSlots], s_red[4 * kSplit], s_l[4 * kSplit];
+    constexpr int kAhead = kRows > 1 ? 3 : 8;      // partials of a head fetched at once
+    __shared__ float s_w[kRows][kMaxSlots], s_l[kRows], s_top[kRows];
     __shared__ float4 s_o[kSplit > 1 ? (kSplit - 1) * 128 : 1];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int s = blockIdx.x / n_q, h = blockIdx.x % n_q;
+    const int groups = (n_q + kRows - 1) / kRows, s = blockIdx.x / groups, h0 = (blockIdx.x % groups) * kRows;
+    const int rows = min(kRows, n_q - h0);
     pdl_launch_dependents();
     pdl_wait();
-    const uint4 ms = meta[s], all = meta[n_seqs];
-    const uint32_t base = ms.x, cost = ms.y, n = ms.z, b0 = ms.w & 0xffffu, count = ms.w >> 16, total = all.x, slots = all.y;
-    const size_t row = (size_t)s * n_q + h;
-    if (cost == 0) {
-        for (int d = tid; d < kLatentValueDim / 8; d += 128 * kSplit)
-            reinterpret_cast<uint4 *>(out)[row * (kLatentValueDim / 8) + d] = make_uint4(0, 0, 0, 0);
-        if (tid == 0 && lse) lse[row] = -INFINITY;
+    const uint4 ms = meta[s];
+    const uint32_t b0 = ms.z, count = ms.w - ms.z;
+    const size_t row0 = (size_t)s * n_q + h0;
+    if (ms.y == 0) {
+        for (int d = tid; d < rows * (kLatentValueDim / 8); d += 128 * kSplit)
+            reinterpret_cast<uint4 *>(out)[row0 * (kLatentValueDim / 8) + d] = make_uint4(0, 0, 0, 0);
+        if (tid < rows && lse) lse[row0 + tid] = -INFINITY;
         return;
     }
+    if (count == 1) return;                        // the share has written the result
     const int part = tid >> 7, d4 = tid & 127;
-    const float4 *src = reinterpret_cast<const float4 *>(part_o) + ((size_t)(b0 + s) * n_q + h) * (kLatentValueDim / 4) + d4;
+    const size_t first = (size_t)(b0 + s) * n_q + h0;          // row of the first partial; the next one's is n_q behind
+    const float4 *src = reinterpret_cast<const float4 *>(part_o) + first * (kLatentValueDim / 4) + d4;
     const size_t step = (size_t)n_q * (kLatentValueDim / 4);
-    float4 v[8];
+    float4 v[kRows][kAhead];
 #pragma unroll
-    for (int k = 0; k < 8; k++) {
-        v[k] = make_float4(0, 0, 0, 0);
-        if (count > 1 && part + (uint32_t)k * kSplit < count) v[k] = src[(part + k * kSplit) * step];
-    }
-    // rows of the sequence in share b: 0 none, 1 some, 2 all (the share has written the result)
-    auto used = [&](uint32_t b) {
-        const uint32_t lo = slot_start(total, b, slots), hi = slot_start(total, b + 1, slots);
-        const uint32_t v0 = lo > base ? cut_at(lo - base, cost, n) : 0u, v1 = hi > base ? cut_at(hi - base, cost, n) : 0u;
-        return v1 <= v0 ? 0 : v0 == 0 && v1 == n ? 2 : 1;
-    };
-    float top = -INFINITY;
-    int whole = 0;
-    for (uint32_t k = tid; k < count; k += 128 * kSplit) {
-        const int u = used(b0 + k);
-        whole |= u == 2;
-        float2 ml = make_float2(-INFINITY, 0.0f);
-        if (u == 1) ml = part_ml[(size_t)(b0 + k + s) * n_q + h];
-        top = fmaxf(top, ml.x);
-    }
-    if (__syncthreads_or(whole)) return;
+    for (int r = 0; r < kRows; r++)
 #pragma unroll
-    for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-    if (lane == 0) s_red[warp] = top;
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < 4 * kSplit; k++) top = fmaxf(top, s_red[k]);
-    float lsum = 0.0f;
-    for (uint32_t k = tid; k < count; k += 128 * kSplit) {
-        float wgt = 0.0f;
-        if (used(b0 + k)) {
-            const float2 ml = part_ml[(size_t)(b0 + k + s) * n_q + h];
-            wgt = umma::ex2(ml.x - top);
-            lsum += wgt * ml.y;
-            if (!(ml.y == ml.y)) wgt = ml.y;       // a NaN stays one
+        for (int k = 0; k < kAhead; k++) {
+            v[r][k] = make_float4(0, 0, 0, 0);
+            if (r < rows && part + (uint32_t)k * kSplit < count) v[r][k] = src[r * (kLatentValueDim / 4) + (part + k * kSplit) * step];
         }
-        s_w[k] = wgt;
+    // weights: a warp per head
+    for (int r = warp; r < rows; r += 4 * kSplit) {
+        float top = -INFINITY, sum = 0.0f;
+        for (uint32_t k = lane; k < count; k += 32) top = fmaxf(top, part_ml[first + r + (size_t)k * n_q].x);
+#pragma unroll
+        for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+        for (uint32_t k = lane; k < count; k += 32) {
+            const float2 ml = part_ml[first + r + (size_t)k * n_q];
+            const float wgt = umma::ex2(ml.x - top);
+            sum += wgt * ml.y;
+            s_w[r][k] = ml.y == ml.y ? wgt : ml.y; // a NaN stays one
+        }
+#pragma unroll
+        for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+        if (lane == 0) { s_l[r] = sum; s_top[r] = top; }
     }
-#pragma unroll
-    for (int d = 16; d; d >>= 1) lsum += __shfl_xor_sync(0xffffffffu, lsum, d);
-    if (lane == 0) s_l[warp] = lsum;
     __syncthreads();
-    lsum = 0.0f;
 #pragma unroll
-    for (int k = 0; k < 4 * kSplit; k++) lsum += s_l[k];
-    float4 acc = make_float4(0, 0, 0, 0);
-    auto add = [&](const float4 &x, float wgt) {
-        if (wgt != 0.0f) { acc.x += wgt * x.x; acc.y += wgt * x.y; acc.z += wgt * x.z; acc.w += wgt * x.w; }
-    };
+    for (int r = 0; r < kRows; r++) {
+        if (r >= rows) break;
+        float4 acc = make_float4(0, 0, 0, 0);
+        auto add = [&](const float4 &x, float wgt) { acc.x += wgt * x.x; acc.y += wgt * x.y; acc.z += wgt * x.z; acc.w += wgt * x.w; };
 #pragma unroll
-    for (int k = 0; k < 8; k++)
-        if (part + (uint32_t)k * kSplit < count) add(v[k], s_w[part + k * kSplit]);
+        for (int k = 0; k < kAhead; k++)
+            if (part + (uint32_t)k * kSplit < count) add(v[r][k], s_w[r][part + k * kSplit]);
 #pragma unroll 8
-    for (uint32_t k = part + 8 * kSplit; k < count; k += kSplit)
-        if (s_w[k] != 0.0f) add(src[k * step], s_w[k]);
-    if (kSplit > 1) {
-        if (part > 0) s_o[(part - 1) * 128 + d4] = acc;
-        __syncthreads();
-        if (part > 0) return;
+        for (uint32_t k = part + kAhead * kSplit; k < count; k += kSplit) add(src[r * (kLatentValueDim / 4) + k * step], s_w[r][k]);
+        if (kSplit > 1) {
+            if (part > 0) s_o[(part - 1) * 128 + d4] = acc;
+            __syncthreads();
+            if (part > 0) return;
 #pragma unroll
-        for (int k = 0; k < kSplit - 1; k++) {
-            const float4 x = s_o[k * 128 + d4];
-            acc.x += x.x; acc.y += x.y; acc.z += x.z; acc.w += x.w;
+            for (int k = 0; k < kSplit - 1; k++) {
+                const float4 x = s_o[k * 128 + d4];
+                acc.x += x.x; acc.y += x.y; acc.z += x.z; acc.w += x.w;
+            }
         }
+        const float inv = 1.0f / s_l[r];
+        reinterpret_cast<uint2 *>(out)[(row0 + r) * (kLatentValueDim / 4) + d4] =
+            make_uint2(umma::pack_bf16(acc.x * inv, acc.y * inv), umma::pack_bf16(acc.z * inv, acc.w * inv));
+        if (tid == 0 && lse) lse[row0 + r] = (s_top[r] + log2f(s_l[r])) * 0.69314718055994531f;
     }
-    const float inv = 1.0f / lsum;
-    reinterpret_cast<uint2 *>(out)[row * (kLatentValueDim / 4) + d4] =
-        make_uint2(umma::pack_bf16(acc.x * inv, acc.y * inv), umma::pack_bf16(acc.z * inv, acc.w * inv));
-    if (tid == 0 && lse) lse[row] = (top + log2f(lsum)) * 0.69314718055994531f;
 }
 
 }  // namespace
@@ -1132,11 +1118,13 @@ pask_status_t launch_decode_latent(pask_cache *c, int layer, int n_seqs, const i
     c->span = nullptr;
     if (e != cudaSuccess) return PASK_ERR_CUDA;
     const int n_q = c->desc.n_q_heads;
-    // few sequences: many partials to a row, so four groups of threads share them (one round trip to L2 brings eight)
+    // few sequences have many partials to a head, which four groups of threads share; many sequences have a few, and a CTA takes
+    // four heads so that all of them are resident at once
     if (p.slots >= 16u * (uint32_t)n_seqs)
-        e = launch_pdl(decode_latent_merge<4>, dim3(n_seqs * n_q), dim3(512), 0, stream, n_seqs, n_q, p.meta, p.part_ml, p.part_o, p.out, lse);
+        e = launch_pdl(decode_latent_merge<4, 1>, dim3(n_seqs * n_q), dim3(512), 0, stream, n_seqs, n_q, p.meta, p.part_ml, p.part_o, p.out, lse);
     else
-        e = launch_pdl(decode_latent_merge<1>, dim3(n_seqs * n_q), dim3(128), 0, stream, n_seqs, n_q, p.meta, p.part_ml, p.part_o, p.out, lse);
+        e = launch_pdl(decode_latent_merge<1, 4>, dim3(n_seqs * ((n_q + 3) / 4)), dim3(128), 0, stream, n_seqs, n_q, p.meta, p.part_ml, p.part_o,
+                       p.out, lse);
     return e == cudaSuccess ? PASK_OK : PASK_ERR_CUDA;
 }
 
