@@ -7,6 +7,7 @@
 #include <cuda_fp16.h>
 
 #include "pask_internal.h"
+#include "pask_latent.h"
 #include "pask_merge.h"
 
 namespace pask {
@@ -772,7 +773,24 @@ __device__ __forceinline__ bool page_at_rcp(uint32_t v, uint32_t nh, uint32_t n,
 constexpr int kSmallMax = 255;       // at most this many sequences and tokens (one thread each, index n_seqs included)
 constexpr int kSmallThreads = 256;
 
+// A latent cache's token: 16-byte chunk `chunk` (< 72 if `write`) of its row, all lanes of the warp together.
+__device__ __forceinline__ void persist_latent(const DevCache &c, uint32_t a, uint32_t at, uint32_t page, int chunk, const uint4 x, bool write) {
+    const int tau = (int)(at & 15u);
+    if (page >= (a == PASK_ACTION_RETAIN_HIGH ? c.cap_high : c.cap_low)) {   // never expected: refuse, do not write
+        atomicOr(&c.ctrl[kCtrlStatus], PASK_DEV_INTERNAL);
+    } else if (a == PASK_ACTION_RETAIN_HIGH) {
+        if (write) *reinterpret_cast<uint4 *>(c.pool_high + (size_t)page * kLatentHighPageBytes + latent_chunk_off(tau, chunk)) = x;
+    } else {
+        uint8_t *dst = c.pool_low + (size_t)page * c.low_page_bytes;
+        if (c.low_bits == 8) store_chunk<8>(dst, tau, chunk, x, write);
+        else if (c.low_bits == 2) store_chunk<2>(dst, tau, chunk, x, write);
+        else store_chunk<4>(dst, tau, chunk, x, write);
+    }
+}
+
 // (the kernel proper is the wrapper below: it places the dependency wait before or after this body)
+// kLatent: a token is one row of 72 chunks (`k`) instead of n_kv K and V heads.
+template <bool kLatent>
 __device__ __forceinline__ void
 append_small_body(const DevCache &c, int layer, int group, int n_seqs, int total, const int32_t *__restrict__ seq_ids,
                   const int32_t *__restrict__ cu_tokens, const uint4 *__restrict__ k, const uint4 *__restrict__ v,
@@ -790,8 +808,8 @@ append_small_body(const DevCache &c, int layer, int group, int n_seqs, int total
     const int tid = threadIdx.x;
     // this CTA's token and this thread's chunk of it: fetch the data first, it depends on nothing
     const int my_tok = blockIdx.x;
-    const int chunks = 16 * c.n_kv;
-    const bool writer = tid < 2 * chunks;
+    const int chunks = kLatent ? kLatentChunks : 16 * c.n_kv;
+    const bool writer = tid < (kLatent ? chunks : 2 * chunks);
     const int which = tid >= chunks, cg = which ? tid - chunks : tid;
     uint4 x = make_uint4(0, 0, 0, 0);
     if (writer) x = (which ? v : k)[(size_t)my_tok * chunks + cg];
@@ -1069,12 +1087,25 @@ append_small_body(const DevCache &c, int layer, int group, int n_seqs, int total
             if (s_new_l[tid]) { const uint32_t kk = s_base_l[tid]; pre_l = kk < s_ctrl[3] ? c.free_low[s_ctrl[3] - 1 - kk] : s_ctrl[2] + (kk - s_ctrl[3]); }
         }
         // ---- persist this CTA's token: one thread per 16-byte chunk of K and of V
-        if (writer && my_a != PASK_ACTION_RELEASE) persist_chunk(c, my_a, my_at, my_page, my_sl, cg >> 4, cg & 15, which, x);
+        if (kLatent) {
+            if (my_a != PASK_ACTION_RELEASE) {
+                persist_latent(c, my_a, my_at, my_page, tid, x, writer);
+                // a page this call is the first to touch: its rows behind the call's last token are zeros (see append_latent_kernel)
+                const bool high = my_a == PASK_ACTION_RETAIN_HIGH;
+                const uint32_t old = high ? s_old_h[my_i] : s_old_l[my_i], cnt = high ? s_cnt_h[my_i] : s_cnt_l[my_i];
+                if (s_pos[my_tok] + 1 == cnt && (my_at & ~15u) >= old && my_page < (high ? c.cap_high : c.cap_low)) {
+                    for (int tau = (int)(my_at & 15u) + 1; tau < kPageTokens; tau++) {
+                        if (high) clear_high_row(c.pool_high + (size_t)my_page * kLatentHighPageBytes, tau, tid, kSmallThreads);
+                        else clear_low_row(c.pool_low + (size_t)my_page * c.low_page_bytes, tau, (int)c.low_bits, tid, kSmallThreads);
+                    }
+                }
+            }
+        } else if (writer && my_a != PASK_ACTION_RELEASE) persist_chunk(c, my_a, my_at, my_page, my_sl, cg >> 4, cg & 15, which, x);
 
         // ---- protected recent window: every token, released ones too, also goes to slot (index mod W)
         // of its (sequence, layer) ring as bf16; of a sequence's tokens in this call only the last W can
         // still be in the window afterwards (and they have distinct slots)
-        if (c.window) {
+        if (!kLatent && c.window) {
             const int W = (int)c.window, r = my_tok - s_cu[my_i], n_i = s_cu[my_i + 1] - s_cu[my_i];
             if (r >= n_i - W) {
                 const uint32_t slot = (s_old_n[my_i] + (uint32_t)r) % (uint32_t)W;
@@ -1145,8 +1176,18 @@ append_small_kernel(DevCache c, int layer, int group, int n_seqs, int total, con
                     uint8_t *__restrict__ actions_out, const SmallLut lut, const int fuse_plan, const Workspace ws) {
     pdl_launch_dependents();
     pdl_wait();
-    append_small_body(c, layer, group, n_seqs, total, seq_ids, cu_tokens, k, v, tags, decided, actions_out, lut, fuse_plan, ws,
+    append_small_body<false>(c, layer, group, n_seqs, total, seq_ids, cu_tokens, k, v, tags, decided, actions_out, lut, fuse_plan, ws,
                       nullptr, gridDim.x);
+}
+
+__global__ void __launch_bounds__(kSmallThreads)
+append_small_latent_kernel(DevCache c, int layer, int group, int n_seqs, int total, const int32_t *__restrict__ seq_ids,
+                           const int32_t *__restrict__ cu_tokens, const uint4 *__restrict__ latent, const uint8_t *__restrict__ tags,
+                           const uint8_t *__restrict__ decided, uint8_t *__restrict__ actions_out, const SmallLut lut) {
+    pdl_launch_dependents();
+    pdl_wait();
+    append_small_body<true>(c, layer, group, n_seqs, total, seq_ids, cu_tokens, latent, latent, tags, decided, actions_out, lut, 0,
+                            Workspace{}, nullptr, gridDim.x);
 }
 
 // The kernel that ends a planned-ahead decode step.  Its first n_seqs CTAs run the one-launch append (one token per
@@ -1168,7 +1209,7 @@ step_tail_kernel(DevCache c, int layer, int group, int n_seqs, const int32_t *__
     pdl_launch_dependents();
     if ((int)blockIdx.x < n_seqs) {
         // (no wait of its own: the kernel is complete only when its merging CTAs are, and those have waited)
-        append_small_body(c, layer, group, n_seqs, n_seqs, seq_ids, cu_tokens, k, v, tags, decided, actions_out, lut, 1, plan_ws,
+        append_small_body<false>(c, layer, group, n_seqs, n_seqs, seq_ids, cu_tokens, k, v, tags, decided, actions_out, lut, 1, plan_ws,
                           ids_out, (uint32_t)n_seqs);
         return;
     }
@@ -1232,6 +1273,19 @@ pask_status_t launch_append_plan(pask_cache *c, int layer, int n_seqs, int total
     append_plan_kernel<<<n_seqs, kBulkThreads, 0, stream>>>(c->dev, layer, n_seqs, total_tokens, seq_ids, cu_tokens, tags,
                                                            decided, actions_out);
     return cudaGetLastError() == cudaSuccess ? PASK_OK : PASK_ERR_CUDA;
+}
+
+pask_status_t launch_append_small_latent(pask_cache *c, int layer, int n_seqs, int total_tokens, const int32_t *seq_ids,
+                                         const int32_t *cu_tokens, const void *latent, const uint8_t *tags, const uint8_t *decided,
+                                         uint8_t *actions_out, cudaStream_t stream, bool *done) {
+    *done = n_seqs <= kSmallMax && total_tokens <= kSmallMax;
+    if (!*done) return PASK_OK;
+    SmallLut lut;
+    fill_small_lut(c, layer, &lut);
+    const cudaError_t e = launch_pdl(append_small_latent_kernel, dim3(total_tokens), dim3(kSmallThreads), 0, stream, c->dev, layer,
+                                     (int)c->layer_group[layer], n_seqs, total_tokens, seq_ids, cu_tokens, static_cast<const uint4 *>(latent),
+                                     tags, decided, actions_out, lut);
+    return e == cudaSuccess ? PASK_OK : PASK_ERR_CUDA;
 }
 
 pask_status_t launch_append(pask_cache *c, int layer, int n_seqs, int total_tokens, const int32_t *seq_ids,

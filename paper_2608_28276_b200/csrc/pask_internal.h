@@ -202,6 +202,10 @@ pask_status_t launch_append_plan(pask_cache *c, int layer, int n_seqs, int total
                                  const int32_t *cu_tokens, const uint8_t *tags, const uint8_t *decided, uint8_t *actions_out,
                                  cudaStream_t stream);
 // latent caches
+// the one-launch append of small calls (as many as the other caches' take it); *done says whether it was one
+pask_status_t launch_append_small_latent(pask_cache *c, int layer, int n_seqs, int total_tokens, const int32_t *seq_ids,
+                                         const int32_t *cu_tokens, const void *latent, const uint8_t *tags, const uint8_t *decided,
+                                         uint8_t *actions_out, cudaStream_t stream, bool *done);
 pask_status_t launch_append_latent(pask_cache *c, int layer, int n_seqs, int total_tokens, const int32_t *seq_ids,
                                    const int32_t *cu_tokens, const void *latent, const uint8_t *tags, const uint8_t *decided,
                                    uint8_t *actions_out, cudaStream_t stream);

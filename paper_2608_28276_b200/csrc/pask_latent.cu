@@ -10,6 +10,7 @@
 #include <cstddef>
 
 #include "pask_internal.h"
+#include "pask_latent.h"
 #include "pask_umma.h"
 
 namespace pask {
@@ -17,191 +18,95 @@ namespace pask {
 namespace {
 
 constexpr int kRowThreads = 288;                  // 18 groups x 16 tokens of a page
-constexpr float kMinScale = 1.17549435e-38f;      // 2^-126: a smaller scale is stored as zero
-
-template <int BITS> struct Codes;                 // levels on each side of zero; the offset that makes codes unsigned
-template <> struct Codes<2> { static constexpr int kLevels = 1, kOffset = 2; };
-template <> struct Codes<4> { static constexpr int kLevels = 7, kOffset = 8; };
-template <> struct Codes<8> { static constexpr int kLevels = 127, kOffset = 128; };
-
-__device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
-
 __device__ __forceinline__ uint32_t pages_touched(uint32_t old, uint32_t cnt) {
     return cnt ? ((old + cnt - 1) >> 4) - (old >> 4) + 1 : 0u;
 }
 
-// The 32 values of one group (16 bf16 pairs) -> BITS packed words and the scale's bf16 bits.
-// scale = bf16(amax / levels) (zero unless a normal number), code = x / scale to the nearest integer, ties to even.
-// x and scale have 8 significant bits each, so a quotient that is no tie is at least 2^-9 away from one: rounding
-// x * (1 / scale) to a multiple of 2^-10 (the first addition, 1.5 * 2^13) removes the error of the reciprocal and leaves
-// exact ties exact; the second addition (up to 1.5 * 2^23 + offset) rounds to the integer, ties to even.  |x / scale| is
-// at most levels * (1 + 2^-8), which rounds to levels: no clamp.
-template <int BITS>
-__device__ __forceinline__ uint32_t quantise_group(const uint32_t (&xs)[16], uint32_t (&words)[BITS]) {
-    constexpr int kLevels = Codes<BITS>::kLevels, kOffset = Codes<BITS>::kOffset;
-    __nv_bfloat162 m2 = __habs2(*reinterpret_cast<const __nv_bfloat162 *>(&xs[0]));
-#pragma unroll
-    for (int e = 1; e < 16; e++) m2 = __hmax2(m2, __habs2(*reinterpret_cast<const __nv_bfloat162 *>(&xs[e])));
-    const uint32_t m = *reinterpret_cast<const uint32_t *>(&m2);
-    const float amax = fmaxf(bf16_lo(m), bf16_hi(m));
-    __nv_bfloat16 sh = __float2bfloat16_rn(__fdiv_rn(amax, (float)kLevels));
-    float s = __bfloat162float(sh);
-    if (!(s >= kMinScale)) { s = 0.0f; sh = __ushort_as_bfloat16(0); }
-    const float inv = s == 0.0f ? 0.0f : __fdiv_rn(1.0f, s);
-    uint32_t code[32];
-#pragma unroll
-    for (int e = 0; e < 32; e++) {
-        const float f = (e & 1) ? bf16_hi(xs[e >> 1]) : bf16_lo(xs[e >> 1]);
-        const float grid = __fmaf_rn(f, inv, 12288.0f);
-        code[e] = __float_as_uint(__fadd_rn(grid, 12582912.0f - 12288.0f + (float)kOffset)) & ((1u << BITS) - 1u);
-    }
-#pragma unroll
-    for (int j = 0; j < BITS; j++) words[j] = 0;
-#pragma unroll
-    for (int e = 0; e < 32; e++) {
-        if (BITS == 4) words[e >> 3] |= code[e] << (4 * ((e & 7) >> 1) + 16 * (e & 1));
-        else if (BITS == 2) words[e >> 4] |= code[e] << ((e & 14) + 16 * (e & 1));
-        else words[e >> 2] |= code[e] << (8 * (e & 3));
-    }
-    return (uint32_t)__bfloat16_as_ushort(sh);
-}
-
-// BITS packed words of a group and its scale -> 16 bf16 pairs: bf16((code - offset) * scale), one rounding each.
-// Two- and four-bit codes: 0x4300 | code is the bf16 number 128 + code, the difference is exact and the product rounded
-// once.  Eight-bit codes go through fp32 (0x4B000000 | code = 2^23 + code; the product of 7 and 8 bits is exact there).
-template <int BITS>
-__device__ __forceinline__ void dequantise_group(const uint32_t (&words)[BITS], uint32_t scale_bits, uint32_t (&xs)[16]) {
-    constexpr int kOffset = Codes<BITS>::kOffset;
-    if (BITS == 8) {
-        const float s = __uint_as_float(scale_bits << 16);
-#pragma unroll
-        for (int p = 0; p < 16; p++) {
-            const uint32_t w = words[(p >> 1) < BITS ? p >> 1 : 0];
-            const float a = (__uint_as_float(__byte_perm(w, 0x4B000000u, (p & 1) ? 0x7442 : 0x7440)) - (8388608.0f + kOffset)) * s;
-            const float b = (__uint_as_float(__byte_perm(w, 0x4B000000u, (p & 1) ? 0x7443 : 0x7441)) - (8388608.0f + kOffset)) * s;
-            const __nv_bfloat162 r = __floats2bfloat162_rn(a, b);
-            xs[p] = *reinterpret_cast<const uint32_t *>(&r);
-        }
-        return;
-    }
-    const __nv_bfloat162 s2 = __bfloat162bfloat162(__ushort_as_bfloat16((unsigned short)scale_bits));
-    const __nv_bfloat162 off = __float2bfloat162_rn(128.0f + kOffset);
-#pragma unroll
-    for (int p = 0; p < 16; p++) {
-        const uint32_t w = BITS == 4 ? words[(p >> 2) < BITS ? p >> 2 : 0] >> (4 * (p & 3)) : words[(p >> 3) < BITS ? p >> 3 : 0] >> (2 * (p & 7));
-        const uint32_t v = (w & (BITS == 4 ? 0x000F000Fu : 0x00030003u)) | 0x43004300u;
-        const __nv_bfloat162 r = __hmul2(__hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&v), off), s2);
-        xs[p] = *reinterpret_cast<const uint32_t *>(&r);
-    }
-}
-
-// the packed codes of (token, group) of a LOW page
-template <int BITS>
-__device__ __forceinline__ void load_codes(const uint8_t *page, int tau, int group, uint32_t (&words)[BITS]) {
-    const uint8_t *p = page + latent_code_off(tau, group, BITS);
-    if (BITS == 2) {
-        const uint2 a = *reinterpret_cast<const uint2 *>(p);
-        words[0] = a.x; words[1] = a.y;
-    } else {
-#pragma unroll
-        for (int h = 0; h < BITS / 4; h++) {
-            const uint4 a = *reinterpret_cast<const uint4 *>(p + h * kPageTokens * 16);
-            words[(4 * h) % BITS] = a.x; words[(4 * h + 1) % BITS] = a.y; words[(4 * h + 2) % BITS] = a.z; words[(4 * h + 3) % BITS] = a.w;
-        }
-    }
-}
-template <int BITS>
-__device__ __forceinline__ void store_codes(uint8_t *page, int tau, int group, const uint32_t (&words)[BITS], uint32_t scale_bits) {
-    uint8_t *p = page + latent_code_off(tau, group, BITS);
-    if (BITS == 2) {
-        *reinterpret_cast<uint2 *>(p) = make_uint2(words[0], words[1]);
-    } else {
-#pragma unroll
-        for (int h = 0; h < BITS / 4; h++)
-            *reinterpret_cast<uint4 *>(p + h * kPageTokens * 16) =
-                make_uint4(words[(4 * h) % BITS], words[(4 * h + 1) % BITS], words[(4 * h + 2) % BITS], words[(4 * h + 3) % BITS]);
-    }
-    *reinterpret_cast<uint16_t *>(page + latent_scale_off(tau, group, BITS)) = (uint16_t)scale_bits;
-}
-
-// Second kernel of an append: a work item is a stream page the call writes into (AppendPlan, tok_list and item_base of the
-// plan kernel); CTA b takes items b, b + grid, ...  A thread moves four 16-byte chunks of a HIGH page, or quantises one
-// (token, group) of a LOW page.  When the call is the first to touch a page, the rows behind its last token are written
-// as zeros: decode attention multiplies whole pages, and a row that has never been written could hold NaN patterns.
+// Second kernel of a bulk append: a work item is a stream page the call writes into (AppendPlan, tok_list and item_base of the
+// plan kernel); a CTA takes consecutive items, so that plan, table and token list are mostly at hand, and looks up the next
+// item's page and tokens while the rows of the current one are on their way.  A thread moves four 16-byte chunks of a HIGH
+// page, or quantises one (token, group) of a LOW page.  When the call is the first to touch a page, the rows behind its last
+// token are written as zeros: decode attention multiplies whole pages, and a row that has never been written could hold
+// NaN patterns.
 template <int BITS>
 __global__ void __launch_bounds__(kRowThreads)
 append_latent_kernel(DevCache c, int layer, int n_seqs, const uint4 *__restrict__ latent) {
-    __shared__ uint32_t s_tok[kPageTokens];
+    __shared__ uint32_t s_tok[2][kPageTokens];
     __shared__ uint32_t s_base[PASK_MAX_SEQS_PER_CALL + 1];
     if (c.ctrl[kCtrlPlanOk] == 0) return;
     const int tid = threadIdx.x;
     const uint32_t n_items = c.ctrl[kCtrlItems];
-    if (blockIdx.x >= n_items) return;
+    const uint32_t item0 = (uint32_t)((uint64_t)n_items * blockIdx.x / gridDim.x), item1 = (uint32_t)((uint64_t)n_items * (blockIdx.x + 1) / gridDim.x);
+    if (item0 >= item1) return;
     for (int x = tid; x <= n_seqs; x += kRowThreads) s_base[x] = c.item_base[x];
     __syncthreads();
-    for (uint32_t item = blockIdx.x; item < n_items; item += gridDim.x) {
-        int lo = 0, hi = n_seqs - 1;
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (s_base[mid] <= item) lo = mid; else hi = mid - 1;
-        }
-        const AppendPlan p = c.plan[lo];
-        const uint32_t in_seq = item - s_base[lo];
-        const uint32_t items_h = pages_touched(p.old_high, p.cnt_high);
-        const bool high = in_seq < items_h;
-        const uint32_t old = high ? p.old_high : p.old_low, cnt = high ? p.cnt_high : p.cnt_low;
-        const uint32_t pg = (old >> 4) + (high ? in_seq : in_seq - items_h);
-        const uint32_t first = 16u * pg, at0 = old > first ? old - first : 0u;                 // tokens of the page: [at0, at1) written,
-        const uint32_t at1 = old + cnt < first + 16u ? old + cnt - first : 16u;                 // the rest zeroed if the page is new
-        const uint32_t end = at0 == 0 ? 16u : at1;
-        const size_t sl = (size_t)p.seq * c.n_layers + layer;
-        const uint32_t page = (high ? c.tbl_high : c.tbl_low)[sl * c.max_pages + pg];
-        __syncthreads();                          // the previous item is done with s_tok
-        if ((uint32_t)tid >= at0 && (uint32_t)tid < at1) {
+    int j = 0;
+    for (int hi = n_seqs - 1; j < hi;) {
+        const int mid = (j + hi + 1) >> 1;
+        if (s_base[mid] <= item0) j = mid; else hi = mid - 1;
+    }
+    AppendPlan p = c.plan[j];
+    struct Page { bool high; uint32_t at0, at1, id; } now, then;
+    uint32_t tok = 0;
+    auto look_up = [&](uint32_t item, Page &g) {
+        bool moved = false;
+        while (item >= s_base[j + 1]) { j++; moved = true; }
+        if (moved) p = c.plan[j];
+        const uint32_t in_seq = item - s_base[j], items_h = pages_touched(p.old_high, p.cnt_high);
+        g.high = in_seq < items_h;
+        const uint32_t old = g.high ? p.old_high : p.old_low, cnt = g.high ? p.cnt_high : p.cnt_low;
+        const uint32_t pg = (old >> 4) + (g.high ? in_seq : in_seq - items_h), first = 16u * pg;
+        g.at0 = old > first ? old - first : 0u;                    // tokens [at0, at1) of the page are written, the rest zeroed if it is new
+        g.at1 = min(old + cnt - first, 16u);
+        g.id = (g.high ? c.tbl_high : c.tbl_low)[((size_t)p.seq * c.n_layers + layer) * c.max_pages + pg];
+        if ((uint32_t)tid >= g.at0 && (uint32_t)tid < g.at1) {
             const uint32_t r = first + tid - old;
-            s_tok[tid] = c.tok_list[high ? p.tok0 + r : p.tok1 - 1 - r];
+            tok = c.tok_list[g.high ? p.tok0 + r : p.tok1 - 1 - r];
         }
-        __syncthreads();
-        if (page >= (high ? c.cap_high : c.cap_low)) {   // never expected: refuse, do not write
-            if (tid == 0) atomicOr(&c.ctrl[kCtrlStatus], PASK_DEV_INTERNAL);
-            continue;
-        }
-        if (high) {
-            uint8_t *dst = c.pool_high + (size_t)page * kLatentHighPageBytes;
+    };
+    look_up(item0, now);
+    for (uint32_t item = item0; item < item1; item++) {
+        uint32_t *toks = s_tok[item & 1];
+        if (tid < kPageTokens) toks[tid] = tok;
+        __syncthreads();                           // (two buffers: nobody still reads the one before last)
+        const uint32_t at0 = now.at0, at1 = now.at1, end = at0 == 0 ? 16u : at1;
+        const bool fits = now.id < (now.high ? c.cap_high : c.cap_low);          // never expected not to: refuse, do not write
+        if (!fits && tid == 0) atomicOr(&c.ctrl[kCtrlStatus], PASK_DEV_INTERNAL);
+        if (now.high) {
+            uint8_t *dst = c.pool_high + (size_t)now.id * kLatentHighPageBytes;
             uint4 x[4];
 #pragma unroll
             for (int i = 0; i < 4; i++) {
                 const uint32_t at = (uint32_t)(tid / kLatentChunks + 4 * i), ch = tid % kLatentChunks;
                 x[i] = make_uint4(0, 0, 0, 0);
-                if (at >= at0 && at < at1) x[i] = __ldcs(&latent[(size_t)s_tok[at] * kLatentChunks + ch]);
+                if (at >= at0 && at < at1) x[i] = __ldcs(&latent[(size_t)toks[at] * kLatentChunks + ch]);
             }
+            if (item + 1 < item1) look_up(item + 1, then);
 #pragma unroll
             for (int i = 0; i < 4; i++) {
                 const uint32_t at = (uint32_t)(tid / kLatentChunks + 4 * i), ch = tid % kLatentChunks;
-                if (at >= at0 && at < end) *reinterpret_cast<uint4 *>(dst + latent_chunk_off((int)at, (int)ch)) = x[i];
+                if (fits && at >= at0 && at < end) *reinterpret_cast<uint4 *>(dst + latent_chunk_off((int)at, (int)ch)) = x[i];
             }
         } else {
-            uint8_t *dst = c.pool_low + (size_t)page * c.low_page_bytes;
+            uint8_t *dst = c.pool_low + (size_t)now.id * c.low_page_bytes;
             const uint32_t at = tid & 15, g = tid >> 4;
-            if (at >= at0 && at < end) {
-                uint32_t words[BITS];
-                uint32_t sb = 0;
-                if (at < at1) {
-                    uint32_t xs[16];
+            uint32_t xs[16], words[BITS], sb = 0;
 #pragma unroll
-                    for (int i = 0; i < 4; i++) {
-                        const uint4 x = latent[(size_t)s_tok[at] * kLatentChunks + 4 * g + i];
-                        xs[4 * i] = x.x; xs[4 * i + 1] = x.y; xs[4 * i + 2] = x.z; xs[4 * i + 3] = x.w;
-                    }
-                    sb = quantise_group<BITS>(xs, words);
-                } else {
-#pragma unroll
-                    for (int j = 0; j < BITS; j++) words[j] = 0;
-                }
-                store_codes<BITS>(dst, (int)at, (int)g, words, sb);
+            for (int i = 0; i < 4; i++) {
+                uint4 x = make_uint4(0, 0, 0, 0);
+                if (at >= at0 && at < at1) x = latent[(size_t)toks[at] * kLatentChunks + 4 * g + i];
+                xs[4 * i] = x.x; xs[4 * i + 1] = x.y; xs[4 * i + 2] = x.z; xs[4 * i + 3] = x.w;
             }
+            if (item + 1 < item1) look_up(item + 1, then);
+            if (at < at1) {
+                sb = quantise_group<BITS>(xs, words);
+            } else {
+#pragma unroll
+                for (int i = 0; i < BITS; i++) words[i] = 0;
+            }
+            if (fits && at >= at0 && at < end) store_codes<BITS>(dst, (int)at, (int)g, words, sb);
         }
+        now = then;
     }
 }
 
@@ -1027,11 +932,15 @@ pask_status_t launch_append_latent(pask_cache *c, int layer, int n_seqs, int tot
                                    const int32_t *cu_tokens, const void *latent, const uint8_t *tags, const uint8_t *decided,
                                    uint8_t *actions_out, cudaStream_t stream) {
     if (total_tokens == 0) return PASK_OK;
-    const pask_status_t rc = launch_append_plan(c, layer, n_seqs, total_tokens, seq_ids, cu_tokens, tags, decided, actions_out, stream);
+    bool done = false;
+    pask_status_t rc = launch_append_small_latent(c, layer, n_seqs, total_tokens, seq_ids, cu_tokens, latent, tags, decided, actions_out, stream, &done);
+    if (done || rc != PASK_OK) return rc;
+    rc = launch_append_plan(c, layer, n_seqs, total_tokens, seq_ids, cu_tokens, tags, decided, actions_out, stream);
     if (rc != PASK_OK) return rc;
-    // at most one item per 16 tokens plus two partly filled pages per stream
+    // at most one item per 16 tokens plus two partly filled pages per stream; twice the resident CTAs, since HIGH and LOW
+    // pages do not take the same time
     const long long bound = (long long)total_tokens / 16 + 4LL * n_seqs;
-    const int ctas = (int)(bound < (long long)c->sm_count * 6 ? bound : c->sm_count * 6);
+    const int ctas = (int)(bound < (long long)c->sm_count * 14 ? bound : c->sm_count * 14);
     auto kern = c->dev.low_bits == 8 ? append_latent_kernel<8> : c->dev.low_bits == 2 ? append_latent_kernel<2> : append_latent_kernel<4>;
     kern<<<ctas, kRowThreads, 0, stream>>>(c->dev, layer, n_seqs, static_cast<const uint4 *>(latent));
     return cudaGetLastError() == cudaSuccess ? PASK_OK : PASK_ERR_CUDA;
