@@ -29,13 +29,15 @@ __device__ __forceinline__ uint32_t pages_touched(uint32_t old, uint32_t cnt) {
 // token are written as zeros: decode attention multiplies whole pages, and a row that has never been written could hold
 // NaN patterns.
 template <int BITS>
-__global__ void __launch_bounds__(kRowThreads)
+__global__ void __launch_bounds__(kRowThreads, 5)
 append_latent_kernel(DevCache c, int layer, int n_seqs, const uint4 *__restrict__ latent) {
     __shared__ uint32_t s_tok[2][kPageTokens];
     __shared__ uint32_t s_base[PASK_MAX_SEQS_PER_CALL + 1];
-    if (c.ctrl[kCtrlPlanOk] == 0) return;
+    __shared__ uint32_t s_items;
     const int tid = threadIdx.x;
-    const uint32_t n_items = c.ctrl[kCtrlItems];
+    if (tid == 0) s_items = c.ctrl[kCtrlPlanOk] ? c.ctrl[kCtrlItems] : 0u;
+    __syncthreads();
+    const uint32_t n_items = s_items;
     const uint32_t item0 = (uint32_t)((uint64_t)n_items * blockIdx.x / gridDim.x), item1 = (uint32_t)((uint64_t)n_items * (blockIdx.x + 1) / gridDim.x);
     if (item0 >= item1) return;
     for (int x = tid; x <= n_seqs; x += kRowThreads) s_base[x] = c.item_base[x];
@@ -50,7 +52,7 @@ append_latent_kernel(DevCache c, int layer, int n_seqs, const uint4 *__restrict_
     uint32_t tok = 0;
     auto look_up = [&](uint32_t item, Page &g) {
         bool moved = false;
-        while (item >= s_base[j + 1]) { j++; moved = true; }
+        while (j + 1 < n_seqs && item >= s_base[j + 1]) { j++; moved = true; }
         if (moved) p = c.plan[j];
         const uint32_t in_seq = item - s_base[j], items_h = pages_touched(p.old_high, p.cnt_high);
         g.high = in_seq < items_h;
