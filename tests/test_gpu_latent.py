@@ -385,6 +385,66 @@ def test_decode_long_shares_of_both_formats(pask, mix):
         assert b.status() == 0
 
 
+def test_many_sequences(pask):
+    # more than a one-launch append takes, up to the largest call: single tokens, then a ragged second call
+    g = torch.Generator().manual_seed(15)
+    n = 1024
+    b = Both(pask, heads=3, max_seqs=n, max_tokens=64, max_append=40000, pages=3000, n_layers=1, lut=[[2], [1], [0]])
+    for lens in ([1] * n, [(7 * i) % 31 for i in range(n)]):
+        b.append(0, list(range(n)), [normal(g, k, 576) for k in lens], [tags_of(g, k, 3) for k in lens])
+    order = [(5 * i + 3) % n for i in range(n)]
+    b.check_rows(0, order[:400])
+    q = normal(g, n, 3, 576)
+    out, lse = b.decode(0, order, q)
+    for i in range(0, n, 7):
+        rows = b.ref.rows(0, order[i])
+        R.check(out[i], lse[i], R.attend(q[i], rows[None], rows[None, :, :512], SCALE), f"sequence {order[i]}")
+    assert b.status() == 0
+
+
+def test_decode_wait_that_runs_out_reports(pask):
+    # the first copy announces bytes it does not bring: the waits give up after the limit, nothing hangs, the cache stays usable
+    g = torch.Generator().manual_seed(16)
+    b = Both(pask, heads=70, max_seqs=3, n_layers=1, lut=[[2], [2], [1]])
+    x = [normal(g, n, 576) for n in (700, 90, 300)]
+    t = [tags_of(g, n, 3) for n in (700, 90, 300)]
+    b.append(0, [0, 1, 2], x, t)
+    q = normal(g, 3, 70, 576)
+    b.check_decode(0, [0, 1, 2], q)
+    pask.pask_debug_set_wait(b.h, 100_000, 16)
+    t0, t1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    b.decode(0, [0, 1, 2], q)
+    t0.record()
+    b.decode(0, [0, 1, 2], q)
+    t1.record()
+    torch.cuda.synchronize()
+    assert t0.elapsed_time(t1) < 1000.0
+    assert b.status() & pask.DEV_TIMEOUT
+    pask.pask_debug_set_wait(b.h)
+    pask.pask_cache_reset(b.h)
+    b.ref.__init__([[2], [2], [1]], [0], 4)
+    b.append(0, [0, 1, 2], x, t)
+    b.check_decode(0, [0, 1, 2], q)
+    assert b.status() == 0
+
+
+def test_decode_timing_hooks(pask):
+    g = torch.Generator().manual_seed(17)
+    b = Both(pask, heads=16, n_layers=1)
+    b.append(0, [0], [normal(g, 900, 576)], [tags_of(g, 900)])
+    q = normal(g, 1, 16, 576)
+    ev = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+    for e in ev:
+        e.record()
+    span = torch.tensor([-1, 0], dtype=torch.int64, device=D)
+    pask.pask_cache_set_timing_events(b.h, *ev)
+    pask.pask_cache_set_timing_span(b.h, span)
+    b.check_decode(0, [0], q)
+    torch.cuda.synchronize()
+    lo, hi = span.tolist()
+    assert 0 < hi - lo < 10_000_000 and 0.0 < ev[0].elapsed_time(ev[1]) < 1000.0
+
+
 def test_decode_bad_ids_and_no_lse(pask):
     g = torch.Generator().manual_seed(6)
     b = Both(pask, heads=16, n_layers=1)
@@ -504,6 +564,44 @@ def test_prompt_ragged_batch(pask, heads):
                                    ([1, 1, 1], [128, 129, 127]), ([256], [513]), ([128, 128], [128, 384]), ([0, 0, 2], [5, 0, 2])])
 def test_prompt_history_and_rows_that_see_nothing(pask, nq, nk):
     prompt(pask, nq, nk, 3, torch.Generator().manual_seed(sum(nq) + 7 * sum(nk)), junk=3)
+
+
+@pytest.mark.parametrize("n_seqs", [33, 70])
+def test_prompt_many_sequences(pask, n_seqs):
+    # beyond 32 sequences the blocks go in the order of the batch
+    g = torch.Generator().manual_seed(n_seqs)
+    nq = [(37 * i) % 301 for i in range(n_seqs)]
+    prompt(pask, nq, [n + (i % 3) * 40 for i, n in enumerate(nq)], 2, g, junk=2)
+
+
+def test_prompt_without_any_keys(pask):
+    prompt(pask, [5, 300], [0, 0], 2, torch.Generator().manual_seed(23))
+
+
+def test_prompt_in_a_graph_and_on_a_stream(pask):
+    g = torch.Generator().manual_seed(24)
+    n, h = 700, 24
+    q, kv, rope = normal(g, n, h, 192).to(D), normal(g, n, h, 256).to(D), normal(g, n, 64).to(D)
+    cu = torch.tensor([0, 650, n], dtype=torch.int32, device=D)
+    want, want_l = torch.empty((n, h, 128), dtype=torch.bfloat16, device=D), torch.empty((n, h), device=D)
+    pask.pask_prompt_attention_latent(cu, cu, q, kv, rope, SCALE, want, want_l)
+    torch.cuda.synchronize()
+    out, lse = torch.zeros_like(want), torch.zeros_like(want_l)
+    st = torch.cuda.Stream()
+    with torch.cuda.stream(st):
+        pask.pask_prompt_attention_latent(cu, cu, q, kv, rope, SCALE, out, lse)
+    st.synchronize()
+    assert torch.equal(out, want) and torch.equal(lse, want_l)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        pask.pask_prompt_attention_latent(cu, cu, q, kv, rope, SCALE, out, lse)
+    q.mul_(0.5)
+    pask.pask_prompt_attention_latent(cu, cu, q, kv, rope, SCALE, want, want_l)
+    for _ in range(2):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(lse, want_l)
 
 
 def test_prompt_scales_and_no_lse(pask):
