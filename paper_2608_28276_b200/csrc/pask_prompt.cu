@@ -17,9 +17,19 @@
 //   warp 10          the next item: blocks of 256 queries with the most visible keys first; a CTA that is done takes over one
 //                    that has not started (cluster launch control), so the tail evens out without a counter in memory
 // Shared memory: Q 96 KB + ring 128 KB.  (Two stages of keys and one of values in the same space let P V wait for the copy of
-// its values, which can only start when the product before it is done: 4516 cycles a block against 3500.)  Tensor memory: S 2 x 128 columns, O 2 x 128 columns: all of it.
+// its values, which can only start when the product before it is done.)  Tensor memory: S 2 x 128 columns, O 2 x 128 columns.
+//
+// Measured: 4123 cycles for a block of 128 keys, 1.6 of the bound; the chain S - exponentials - P - P V of a tile is longer than
+// the other tile's products.  Two threads a query (16 softmax warps) took as long: 155 us against 150 for 4 x 500 queries
+// behind 3333 keys, 32 heads.  4 prompts of 4 to 8 thousand, 16 heads: 681 us, 1.2 PFLOP/s at the 1.6 GHz that the power limit
+// leaves.
+//
+// kSplit > 1: a cluster of kSplit CTAs shares an item, each a range of its key blocks; the unscaled results meet in shared
+// memory, each CTA joining the rows of 256 / kSplit queries (no workspace, a fixed order).  No stealing there.
 #include <cuda.h>
 #include <cuda_bf16.h>
+
+#include <cmath>
 
 #include "pask_internal.h"
 #include "pask_umma.h"
@@ -56,6 +66,7 @@ struct __align__(16) PromptSmem {
     uint4 answer;
     Item item[2];
     uint32_t tmem;
+    float m[kBlockQ], l[kBlockQ];                  // kSplit > 1: reference maximum and sum of each query over this CTA's keys
 };
 
 // visible keys of the query at position i of its sequence
@@ -65,6 +76,18 @@ __device__ __forceinline__ int key_blocks(const Item &it, int t) {
     const int i0 = it.block * kBlockQ + t * kTileQ;
     if (i0 >= it.nq) return 0;
     return (visible(it, min(it.nq, i0 + kTileQ) - 1) + kBlockK - 1) / kBlockK;
+}
+
+// The blocks of keys CTA `part` of `split` looks at: [first, first + max(n[0], n[1])), tile t the first n[t] of them.
+struct Part { int first, n[2]; };
+__device__ __forceinline__ Part part_of(const Item &it, int part, int split) {
+    const int n0 = key_blocks(it, 0), n1 = key_blocks(it, 1), nb = max(n0, n1);
+    Part r;
+    r.first = split > 1 ? nb * part / split : 0;
+    const int mine = (split > 1 ? nb * (part + 1) / split : nb) - r.first;
+    r.n[0] = max(0, min(n0 - r.first, mine));
+    r.n[1] = max(0, min(n1 - r.first, mine));
+    return r;
 }
 
 // The item of grid position x, worked out by a warp: position r = x / heads among the blocks of 256 queries, head x % heads.
@@ -148,13 +171,14 @@ struct Ranker {
     }
 };
 
+template <int kSplit>
 __global__ void __launch_bounds__(kThreads, 1)
 prompt_latent_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CUtensorMap map_q,
                      const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ CUtensorMap map_v,
                      const __grid_constant__ CUtensorMap map_rope) {
     using namespace umma;
-    extern __shared__ uint8_t s_raw[];
-    PromptSmem &sm = *reinterpret_cast<PromptSmem *>(((uintptr_t)s_raw + 1023) & ~(uintptr_t)1023);
+    extern __shared__ __align__(1024) uint8_t s_raw[];
+    PromptSmem &sm = *reinterpret_cast<PromptSmem *>(s_raw);
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
     if (tid == 0) {
         bar_init(smem_u32(&sm.q_full), 1);
@@ -183,6 +207,9 @@ prompt_latent_kernel(const __grid_constant__ PromptParams p, const __grid_consta
     fence_after();
     const uint32_t tmem = sm.tmem;
     constexpr uint32_t kS = 0, kO = 256;           // columns of tile 0; tile 1 is 128 behind
+    const int part = kSplit > 1 ? (int)blockIdx.x % kSplit : 0;      // = rank in the cluster
+    Item item;                                     // kSplit > 1, softmax threads: the item of the cluster
+    item.block = -1;
     bool ok = true;
     // the CTA's n-th item; false behind the last one or after a wait ran out
     auto next_item = [&](uint32_t n, Item &it) {
@@ -202,7 +229,7 @@ prompt_latent_kernel(const __grid_constant__ PromptParams p, const __grid_consta
         // ================================================= items
         Ranker rank;
         rank.init(p, lane);
-        int x = (int)blockIdx.x;
+        int x = (int)blockIdx.x / kSplit;
         uint32_t asked = 0;
         bool live = true;
         for (uint32_t n = 0; live; n++) {
@@ -217,6 +244,7 @@ prompt_latent_kernel(const __grid_constant__ PromptParams p, const __grid_consta
                 bar_arrive(smem_u32(&sm.item_full[slot]));
             }
             if (!live) break;
+            if constexpr (kSplit > 1) { x = -1; continue; }
             if (lane == 0) {
                 bar_expect(smem_u32(&sm.steal), 16);
                 steal_ask(smem_u32(&sm.answer), smem_u32(&sm.steal));
@@ -233,7 +261,8 @@ prompt_latent_kernel(const __grid_constant__ PromptParams p, const __grid_consta
         uint32_t g = 0, qc = 0;                    // blocks, items with queries copied so far
         const uint32_t qf = smem_u32(&sm.q_full), ring = smem_u32(sm.ring);
         for (uint32_t n = 0; next_item(n, it); n++) {
-            const int n0 = key_blocks(it, 0), n1 = key_blocks(it, 1), nb = max(n0, n1);
+            const Part in = part_of(it, part, kSplit);
+            const int n0 = in.n[0], n1 = in.n[1], nb = max(n0, n1);
             if (nb == 0) continue;
             if (qc > 0) ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.q_empty), (qc - 1) & 1, kWaitCycles));
             if (!ok) break;
@@ -249,7 +278,7 @@ prompt_latent_kernel(const __grid_constant__ PromptParams p, const __grid_consta
             for (int j = 0; j < nb; j++, g++) {
                 // keys, piece by piece: over the last piece of the keys two blocks before, over that block's values as their halves
                 // are done with (one piece takes 16 KB of copy time from a freed place to the product that waits for it, not 48)
-                const uint32_t st = g & 1, row = (uint32_t)(it.k0 + j * kBlockK), kf = smem_u32(&sm.k_full[st]), ph = ((g >> 1) - 1) & 1;
+                const uint32_t st = g & 1, row = (uint32_t)(it.k0 + (in.first + j) * kBlockK), kf = smem_u32(&sm.k_full[st]), ph = ((g >> 1) - 1) & 1;
                 if (g >= 2) ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.k_empty[st]), ph, kWaitCycles));
                 if (!ok) break;
                 if (mine) {
@@ -308,7 +337,8 @@ prompt_latent_kernel(const __grid_constant__ PromptParams p, const __grid_consta
                     mma_ts(tmem + kO + t * 128, tmem + kS + t * 128 + (from + k) * 8, b + 128 * k, kIdO, from + k > 0 || !fresh, mine);
         };
         for (uint32_t n = 0; next_item(n, it); n++) {
-            const int nt[2] = {key_blocks(it, 0), key_blocks(it, 1)}, nb = max(nt[0], nt[1]);
+            const Part in = part_of(it, part, kSplit);
+            const int nt[2] = {in.n[0], in.n[1]}, nb = max(nt[0], nt[1]);
             if (nb == 0) continue;
             ok = bar_wait(smem_u32(&sm.q_full), qc & 1, kWaitCycles);
             qc++;
@@ -326,7 +356,7 @@ prompt_latent_kernel(const __grid_constant__ PromptParams p, const __grid_consta
                 }
             }
             for (int j = 0; j < nb; j++, g++) {
-                const int valid = __shfl_sync(0xffffffffu, min(kBlockK, it.nk - j * kBlockK), 0), steps = (valid + 15) / 16;
+                const int valid = __shfl_sync(0xffffffffu, min(kBlockK, it.nk - (in.first + j) * kBlockK), 0), steps = (valid + 15) / 16;
                 const uint32_t at = __shfl_sync(0xffffffffu, (5 * g) & 7, 0), ph = (g >> 1) & 1;
                 const int last_t = j < nt[1] ? 1 : 0;       // the tile whose product is the last to use the block's values
                 bool have_k = false;
@@ -395,7 +425,10 @@ prompt_latent_kernel(const __grid_constant__ PromptParams p, const __grid_consta
         const uint32_t base = tmem + ((uint32_t)((warp & 3) * 32) << 16) + t * 128;
         const uint32_t s_full = smem_u32(&sm.s_full[t]), p_half = smem_u32(&sm.p_half[t]), p_full = smem_u32(&sm.p_full[t]),
                        pv_done = smem_u32(&sm.pv_done[t]);
+        const int row_in = t * kTileQ + (warp & 3) * 32 + lane;
         Item it;
+        float m = -INFINITY, l = 0.0f;
+        bool none = true;                          // no keys here
         // a wait ran out (never expected): the row's result says so
         auto spoil = [&](const Item &at, int i) {
             if (i >= at.nq) return;
@@ -405,9 +438,11 @@ prompt_latent_kernel(const __grid_constant__ PromptParams p, const __grid_consta
         };
         uint32_t sc = 0, ic = 0;                   // blocks of this tile so far (S, P and P V alike), items with any
         for (uint32_t n = 0; next_item(n, it); n++) {
-            const int nb = key_blocks(it, t), i = it.block * kBlockQ + t * kTileQ + (warp & 3) * 32 + lane;
+            const Part in = part_of(it, part, kSplit);
+            const int nb = in.n[t], i = it.block * kBlockQ + row_in;
             const int vis = i < it.nq ? visible(it, i) : 0;
-            float m = -INFINITY, l = 0.0f;
+            m = -INFINITY;
+            l = 0.0f;
             for (int j = 0; j < nb; j++, sc++) {
                 ok = bar_wait(s_full, sc & 1, ok ? kWaitCycles : 0) && ok;
                 if (!__all_sync(0xffffffffu, ok)) break;
@@ -421,7 +456,7 @@ prompt_latent_kernel(const __grid_constant__ PromptParams p, const __grid_consta
                     for (int e = 0; e < 32; e++) x[32 * c + e] = __uint_as_float(r[e]);
                 }
                 tmem_wait_ld();
-                const int left = vis - j * kBlockK;
+                const int left = vis - (in.first + j) * kBlockK;
                 if (__any_sync(0xffffffffu, left < kBlockK)) {
 #pragma unroll
                     for (int e = 0; e < 128; e++) if (e >= left) x[e] = -INFINITY;
@@ -479,6 +514,12 @@ prompt_latent_kernel(const __grid_constant__ PromptParams p, const __grid_consta
                 unpair(l2, l0, l1);
                 l += l0 + l1;
             }
+            if constexpr (kSplit > 1) {            // one item: its parts are joined below
+                if (nb > 0 && ok) ok = bar_wait(pv_done, 0, kWaitCycles);
+                none = nb == 0;
+                item = it;
+                break;
+            }
             if (!__all_sync(0xffffffffu, ok)) { spoil(it, i); break; }
             // ---- the row's result
             if (nb > 0) {
@@ -518,11 +559,63 @@ prompt_latent_kernel(const __grid_constant__ PromptParams p, const __grid_consta
                 if (lane == 0) bar_arrive(smem_u32(&sm.o_free[t]));
             }
         }
+        if constexpr (kSplit > 1) {
+            // All products of this CTA are done, so that nothing reads or fills its tiles any more: [dim][query] over them.
+            const bool good = !group_any(1, 2 * kTileQ, !ok);
+            fence_after();
+            sm.m[row_in] = good ? m : __int_as_float(0x7FC00000);
+            sm.l[row_in] = l;
+            float *o = reinterpret_cast<float *>(sm.q);
+            if (good && item.block >= 0)
+#pragma unroll
+                for (int c = 0; c < 8; c++) {
+                    uint32_t r[16];
+#pragma unroll
+                    for (int e = 0; e < 16; e++) r[e] = 0;
+                    if (!none) {
+                        tmem_ld16(base + kO + 16 * c, r);
+                        tmem_wait_ld();
+                    }
+#pragma unroll
+                    for (int e = 0; e < 16; e++) o[(16 * c + e) * kBlockQ + row_in] = __uint_as_float(r[e]);
+                }
+        }
     }
     fence_before();
-    __syncthreads();
+    if constexpr (kSplit > 1) cluster_sync(); else __syncthreads();
     fence_after();
     if (warp == 8) tmem_free(tmem, 512);
+    if constexpr (kSplit > 1) {
+        // Each CTA joins the parts of 256 / kSplit queries, a thread 128 / kSplit dims of one, in the order of the parts.
+        constexpr int kRows = kBlockQ / kSplit, kDims = kV / kSplit;
+        const int r = part * kRows + tid % kRows, d0 = tid / kRows * kDims, i = item.block * kBlockQ + r;
+        if (warp < 8 && item.block >= 0 && i < item.nq) {
+            float w[kSplit], top = -INFINITY, l = 0.0f;
+#pragma unroll
+            for (int s = 0; s < kSplit; s++) { w[s] = peer_load(smem_u32(&sm.m[r]), s); top = fmaxf(top, w[s]); }
+            const float ref = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+            for (int s = 0; s < kSplit; s++) { w[s] = ex2(w[s] - ref); l += w[s] * peer_load(smem_u32(&sm.l[r]), s); }
+            const int vis = visible(item, i);
+            const float inv = vis > 0 ? 1.0f / l : 0.0f;
+            const size_t row = (size_t)(item.q0 + i) * p.n_heads + item.head;
+            const uint32_t o = smem_u32(sm.q) + (d0 * kBlockQ + r) * 4;
+#pragma unroll 2
+            for (int d = 0; d < kDims; d += 8) {
+                float x[8] = {};
+#pragma unroll
+                for (int s = 0; s < kSplit; s++)
+#pragma unroll
+                    for (int e = 0; e < 8; e++) x[e] += w[s] * peer_load(o + (d + e) * kBlockQ * 4, s);
+                uint32_t y[4];
+#pragma unroll
+                for (int e = 0; e < 4; e++) y[e] = vis > 0 ? pack_bf16(x[2 * e] * inv, x[2 * e + 1] * inv) : 0u;
+                *reinterpret_cast<uint4 *>(p.out + row * kV + d0 + d) = make_uint4(y[0], y[1], y[2], y[3]);
+            }
+            if (d0 == 0 && p.lse) p.lse[row] = vis > 0 ? (top + log2f(l)) * 0.69314718055994531f : -INFINITY;
+        }
+        cluster_sync();                            // the others may still be reading here
+    }
 }
 
 using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
@@ -541,6 +634,79 @@ bool encode(EncodeTiled fn, CUtensorMap *map, const void *base, int inner, int h
               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+template <int kSplit>
+void config(cudaLaunchConfig_t &cfg, cudaLaunchAttribute &attr, int items, cudaStream_t stream) {
+    constexpr int kSmem = (int)sizeof(PromptSmem);
+    static_assert(kSmem <= 232448, "shared memory of a CTA");
+    static_assert(kBlockQ * kV * 4 <= sizeof(PromptSmem::q) + sizeof(PromptSmem::ring), "partial results over the tiles");
+    attr = {};
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = kSplit;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg = {};
+    cfg.gridDim = dim3(items * kSplit);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = kSmem;
+    cfg.stream = stream;
+    cfg.attrs = &attr;
+    cfg.numAttrs = kSplit > 1 ? 1 : 0;
+}
+
+// Once per device: the right to the shared memory, and how many clusters of kSplit CTAs run at a time; 0 on an error.
+template <int kSplit>
+int places(int dev) {
+    static int n[64] = {};
+    if (n[dev]) return n[dev];
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute attr;
+    config<kSplit>(cfg, attr, 1, nullptr);
+    if (cudaFuncSetAttribute(prompt_latent_kernel<kSplit>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes) != cudaSuccess)
+        return 0;
+    int found = 0;
+    if (kSplit > 1 ? cudaOccupancyMaxActiveClusters(&found, prompt_latent_kernel<kSplit>, &cfg) != cudaSuccess
+                   : cudaDeviceGetAttribute(&found, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+        return 0;
+    return n[dev] = found;
+}
+
+template <int kSplit>
+pask_status_t launch(const PromptParams &p, const CUtensorMap &map_q, const CUtensorMap &map_kv, const CUtensorMap &map_v,
+                     const CUtensorMap &map_rope, int items, cudaStream_t stream) {
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute attr;
+    config<kSplit>(cfg, attr, items, stream);
+    return cudaLaunchKernelEx(&cfg, prompt_latent_kernel<kSplit>, p, map_q, map_kv, map_v, map_rope) == cudaSuccess ? PASK_OK : PASK_ERR_CUDA;
+}
+
+// Time of n items on p places in key blocks: the longest item has `longest`, the others go evenly down to longest - spread.
+double makespan(double n, double p, double longest, double spread) {
+    if (n <= p) return longest;
+    return fmax(longest, n <= 2 * p ? 2 * longest - 2 * spread * p / n : (longest - spread / 2) * n / p);
+}
+
+// CTAs an item's keys are split over.  Few blocks of queries would leave SMs idle while one walks all its keys (16 heads, 200
+// queries, 6000 keys: 101.7 us in 16 CTAs, 35.8 us in 64).  Each round of clusters costs some two key blocks more than the
+// unsplit kernel (queries read by every part, the joining, no overlap from item to item), so 128 keys stay whole: 10.4 against
+// 12.4 us.  Four and eight only while all items run at once (32 heads x 2 blocks, 3000 keys: 38.2 us by two, 51.5 by four).  Two
+// also where causal blocks of different lengths fill further rounds (5 heads, 8000 queries of 8000 keys: 136 -> 108 us) and the
+// estimate gains a tenth.  The host knows sums only: the rule takes a batch for one of equal sequences.
+int split_of(int n_seqs, int total_q, int total_k, int n_heads, int dev) {
+    const int nq = max(1, total_q / n_seqs), nk = total_k / n_seqs;
+    const double n = (double)n_seqs * ((nq + kBlockQ - 1) / kBlockQ) * n_heads, longest = (nk + kBlockK - 1) / kBlockK;
+    const double spread = fmin(longest, fmax(0.0, (double)(nq - kBlockQ) / kBlockK));
+    const double whole = makespan(n, places<1>(dev), longest, spread);
+    int split = 1;
+    double best = whole;
+    const int p2 = places<2>(dev), p4 = places<4>(dev), p8 = places<8>(dev);
+    if (p2 > 0) {
+        const double t = makespan(n, p2, longest / 2, spread / 2) + 2 * ceil(n / p2);
+        if (t < (n <= p2 ? best : 0.9 * best)) { best = t; split = 2; }
+    }
+    if (n <= p4 && longest / 4 + 2 < best) { best = longest / 4 + 2; split = 4; }
+    if (n <= p8 && longest / 8 + 2 < best) split = 8;
+    return split;
+}
+
 }  // namespace
 
 pask_status_t launch_prompt_latent(int n_seqs, int total_q, int total_k, int n_heads, const int32_t *cu_q, const int32_t *cu_k,
@@ -555,15 +721,9 @@ pask_status_t launch_prompt_latent(int n_seqs, int total_q, int total_k, int n_h
             return PASK_ERR_CUDA;
         encode_fn = reinterpret_cast<EncodeTiled>(fn);
     }
-    constexpr int kSmem = (int)sizeof(PromptSmem) + 1024;
-    static_assert(kSmem <= 232448, "shared memory of a CTA");
-    static bool granted[64] = {};
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return PASK_ERR_CUDA;
-    if (!granted[dev]) {
-        if (cudaFuncSetAttribute(prompt_latent_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess) return PASK_ERR_CUDA;
-        granted[dev] = true;
-    }
+    if (!places<1>(dev)) return PASK_ERR_CUDA;
     CUtensorMap map_q{}, map_kv{}, map_v{}, map_rope{};
     const size_t q_row = (size_t)n_heads * kQk * 2, kv_head = (kNope + kV) * 2, kv_row = (size_t)n_heads * kv_head;
     if (!encode(encode_fn, &map_q, q, kQk, n_heads, total_q, kQk * 2, q_row, kTileQ)) return PASK_ERR_CUDA;
@@ -574,8 +734,10 @@ pask_status_t launch_prompt_latent(int n_seqs, int total_q, int total_k, int n_h
     const long long items = ((long long)total_q / kBlockQ + n_seqs) * n_heads;
     if (items > 0x7fffffffLL) return PASK_ERR_INVALID_ARG;
     const PromptParams p{n_seqs, total_q, total_k, n_heads, cu_q, cu_k, scale * 1.4426950408889634f, static_cast<__nv_bfloat16 *>(out), lse};
-    prompt_latent_kernel<<<(int)items, kThreads, kSmem, stream>>>(p, map_q, map_kv, map_v, map_rope);
-    return cudaGetLastError() == cudaSuccess ? PASK_OK : PASK_ERR_CUDA;
+    const int split = split_of(n_seqs, total_q, total_k, n_heads, dev);
+    if (items * split > 0x7fffffffLL) return PASK_ERR_INVALID_ARG;
+    const auto fn = split == 8 ? launch<8> : split == 4 ? launch<4> : split == 2 ? launch<2> : launch<1>;
+    return fn(p, map_q, map_kv, map_v, map_rope, (int)items, stream);
 }
 
 }  // namespace pask

@@ -26,12 +26,6 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
                  : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
 }
-__device__ __forceinline__ bool bar_test(uint32_t bar, uint32_t parity) {       // without waiting
-    uint32_t ok;
-    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-    return ok != 0;
-}
 // false if the phase did not complete within `limit` clock cycles
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, long long limit) {
     if (bar_try(bar, parity)) return true;
@@ -160,6 +154,17 @@ __device__ __forceinline__ bool group_any(int id, int threads, bool flag) {
     asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %3, 0;\n\tbarrier.red.or.pred q, %1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
                  : "=r"(r) : "r"(id), "r"(threads), "r"((uint32_t)flag) : "memory");
     return r != 0;
+}
+
+// ---- clusters: all threads of all its CTAs; a word of another CTA's shared memory, by this CTA's address of the same
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+}
+__device__ __forceinline__ float peer_load(uint32_t addr, int rank) {
+    float x;
+    asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %1, %2;\n\tld.shared::cluster.f32 %0, [a];\n\t}"
+                 : "=f"(x) : "r"(addr), "r"(rank) : "memory");
+    return x;
 }
 
 // ---- copies

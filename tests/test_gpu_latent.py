@@ -604,6 +604,54 @@ def test_prompt_in_a_graph_and_on_a_stream(pask):
         assert torch.equal(out, want) and torch.equal(lse, want_l)
 
 
+# few blocks of queries: the keys of each are split over two, four or eight CTAs; parts without a key, queries without one,
+# more blocks than fit at a time
+@pytest.mark.parametrize("heads,nq,nk", [(5, [3], [6000]), (16, [200], [2000]), (24, [512], [2100]), (8, [2500], [2500]), (4, [900], [700]),
+                                         (3, [3, 1, 250, 2, 0], [4000, 1, 100, 0, 300]), (2, [1] * 40, [700 + 13 * i for i in range(40)]),
+                                         (1, [257, 255], [1025, 1023]), (20, [129], [1281])])
+def test_prompt_splits_long_keys(pask, heads, nq, nk):
+    prompt(pask, nq, nk, heads, torch.Generator().manual_seed(heads + sum(nk)), junk=2)
+
+
+def test_prompt_split_scores_that_rise_along_the_keys(pask):
+    # each part's reference maximum differs by far from the others'
+    g = torch.Generator().manual_seed(25)
+    prompt(pask, [60], [4000], 6, g, factor=20.0)
+    nq, nk, h = 60, 4000, 6
+    q, kv, rope = normal(g, nq, h, 192), normal(g, nk, h, 256), normal(g, nk, 64)
+    q[:, :, 128:] = 1.0
+    rope[:] = torch.linspace(-8, 8, nk)[:, None].to(torch.bfloat16)
+    out, lse = torch.empty((nq, h, 128), dtype=torch.bfloat16, device=D), torch.empty((nq, h), device=D)
+    pask.pask_prompt_attention_latent(torch.tensor([0, nq], dtype=torch.int32, device=D), torch.tensor([0, nk], dtype=torch.int32, device=D),
+                                      q.to(D), kv.to(D), rope.to(D), SCALE, out, lse)
+    kk = torch.cat([kv[:, :, :128], rope[:, None, :].expand(-1, h, -1)], -1).transpose(0, 1)
+    R.check(out, lse, R.attend(q, kk, kv[:, :, 128:].transpose(0, 1), SCALE, torch.arange(nq) + 1 + nk - nq), "rising")
+
+
+def test_prompt_split_repeats_bit_for_bit_in_a_graph_and_on_a_stream(pask):
+    g = torch.Generator().manual_seed(26)
+    nq, nk, h = 40, 3333, 8
+    q, kv, rope = normal(g, nq, h, 192).to(D), normal(g, nk, h, 256).to(D), normal(g, nk, 64).to(D)
+    cq, ck = (torch.tensor([0, n], dtype=torch.int32, device=D) for n in (nq, nk))
+    want, want_l = torch.empty((nq, h, 128), dtype=torch.bfloat16, device=D), torch.empty((nq, h), device=D)
+    pask.pask_prompt_attention_latent(cq, ck, q, kv, rope, SCALE, want, want_l)
+    torch.cuda.synchronize()
+    out, lse = torch.zeros_like(want), torch.zeros_like(want_l)
+    st = torch.cuda.Stream()
+    with torch.cuda.stream(st):
+        for _ in range(20):
+            pask.pask_prompt_attention_latent(cq, ck, q, kv, rope, SCALE, out, lse)
+    st.synchronize()
+    assert torch.equal(out, want) and torch.equal(lse, want_l)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        pask.pask_prompt_attention_latent(cq, ck, q, kv, rope, SCALE, out, lse)
+    out.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, want) and torch.equal(lse, want_l)
+
+
 def test_prompt_scales_and_no_lse(pask):
     g = torch.Generator().manual_seed(21)
     for scale, factor in ((1.0, 1.0), (1e-4, 1.0), (SCALE, 30.0)):
