@@ -27,7 +27,8 @@ __device__ __forceinline__ uint32_t pages_touched(uint32_t old, uint32_t cnt) {
 // item's page and tokens while the rows of the current one are on their way.  A thread moves four 16-byte chunks of a HIGH
 // page, or quantises one (token, group) of a LOW page.  When the call is the first to touch a page, the rows behind its last
 // token are written as zeros: decode attention multiplies whole pages, and a row that has never been written could hold
-// NaN patterns.
+// NaN patterns.  Bound by memory: 326 K tokens, a quarter HIGH, 0.4 LOW at 4 bits, 77 us behind the plan's 20 (383 MB: 5.0 TB/s;
+// five CTAs an SM and the look-ahead hide the table and list lookups: 85 us with three).
 template <int BITS>
 __global__ void __launch_bounds__(kRowThreads, 5)
 append_latent_kernel(DevCache c, int layer, int n_seqs, const uint4 *__restrict__ latent) {
@@ -113,7 +114,8 @@ append_latent_kernel(DevCache c, int layer, int n_seqs, const uint4 *__restrict_
 }
 
 // pask_read_latent: a work item is a page of a sequence; sequence i owns items cu_rows[i] / 16 + 2 i .. (at least as many as
-// it can have pages), so an item finds its sequence without a prefix over page counts.
+// it can have pages), so an item finds its sequence without a prefix over page counts.  Bound by memory: 213 K rows of the same
+// batch in 67 us (382 MB: 5.7 TB/s).
 template <int BITS>
 __global__ void __launch_bounds__(kRowThreads)
 read_latent_kernel(DevCache c, int layer, int n_seqs, int total_rows, const int32_t *__restrict__ seq_ids,
@@ -220,6 +222,11 @@ read_latent_kernel(DevCache c, int layer, int n_seqs, int total_rows, const int3
 // The reference maximum of a head moves only when a score exceeds it by more than 2^8 (the sums have room for that), so that
 // the rescaling of O leaves the common path.  A share that covers a whole sequence writes its result; otherwise partial sums
 // go to the workspace and decode_latent_merge joins them in a fixed order: results do not depend on timing.
+//
+// Bound by shared memory: a HIGH tile of 64 heads moves 327 KB through it (copy, X twice, Q, P), 2555 cycles at 128 B each; a
+// tile takes 3450, a LOW one about 6000 (4500 for 32 heads), its fill being as much traffic again.  Measured with the merge: 64
+// sequences of 2 to 8 thousand rows, 128 heads, all HIGH 163 us; 128 of 16 thousand tokens, 64 heads, a fifth HIGH and 0.3 LOW at
+// 4 bits 315 us; one of 1023 rows, 16 heads 12.5 us.
 constexpr int kTile = 64, kTilePages = 4;
 constexpr int kTileBytes = kTilePages * kLatentHighPageBytes;      // 73728
 constexpr int kDecThreads = 480, kFillThreads = 256;
