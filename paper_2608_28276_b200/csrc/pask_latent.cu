@@ -213,10 +213,12 @@ read_latent_kernel(DevCache c, int layer, int n_seqs, int total_rows, const int3
 // A CTA is one of `slots` equal shares of the batch's tiles: 64 rows = four pages of one stream, a sequence's HIGH and LOW tiles
 // visited in turn, evenly mixed.  (A LOW tile is a quarter of the bytes but as much work on chip: 4.2 and 4.5 thousand cycles
 // at 32 heads, so a tile counts as a tile.)  Roles:
-//   warp 12     HIGH tiles: one linear bulk copy a page (pages are stored in the operand layout) into its place in one of two
+//   warp 13     HIGH tiles: one linear bulk copy a page (pages are stored in the operand layout) into its place in one of two
 //               stages, as soon as the product that last read the place is done, and a prefetch into L2 some tiles ahead
-//   warps 4-11  LOW tiles: codes in registers one tile ahead, values as bf16 into the stage; and the queries of a sequence
-//   warp 13     the products for S, two tiles ahead at most;  warp 14  those for O.  (One warp for both had to poll: waiting on a
+//   warps 4-12  LOW tiles: a thread takes one (token, group) of each page, codes in registers one tile ahead, values as bf16 into
+//               the stage; and the queries of a sequence.  (The loop over pages is rolled, its codes move up a place instead:
+//               straight-line code for a whole tile waited for its instructions, 18 % a tile.)
+//   warp 14     the products for S, two tiles ahead at most;  warp 15  those for O.  (One warp for both had to poll: waiting on a
 //               barrier wakes it 70 cycles after the arrival, polling two of them sees it after 150 to 350.)
 //   warps 0-3   softmax of a tile's S (warp w: page w of the tile), P to shared memory, and a sequence's end
 // The reference maximum of a head moves only when a score exceeds it by more than 2^8 (the sums have room for that), so that
@@ -229,7 +231,7 @@ read_latent_kernel(DevCache c, int layer, int n_seqs, int total_rows, const int3
 // 4 bits 315 us; one of 1023 rows, 16 heads 12.5 us.
 constexpr int kTile = 64, kTilePages = 4;
 constexpr int kTileBytes = kTilePages * kLatentHighPageBytes;      // 73728
-constexpr int kDecThreads = 480, kFillThreads = 256;
+constexpr int kDecThreads = 512, kFillThreads = kPageTokens * kLatentGroups;      // 288: nine warps
 constexpr uint32_t kMaxSlots = 1024;
 constexpr int kPrefetch = 6;                       // tiles between a prefetch into L2 and the copy (2: 3 % slower; 4 to 8: within 1 %)
 enum : uint32_t { kInfoFirst = 1, kInfoLast = 2, kInfoWhole = 4, kInfoFinal = 8 };   // first, last tile of a sequence's part; the part
@@ -446,7 +448,7 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
         }
     }
     if (lo >= hi) return;                          // nothing for this CTA
-    if (warp == 13) tmem_alloc(smem_u32(&ms.tmem), 512);
+    if (warp == 14) tmem_alloc(smem_u32(&ms.tmem), 512);
     fence_before();
     __syncthreads();
     fence_after();
@@ -460,7 +462,7 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
     w.enter(ms.first_high, ms.first_low);
     bool more = true, ok = true;
 
-    if (warp == 12) {
+    if (warp == 13) {
         // ================================================= copies
         // (page ids are read an iteration before they are used: the read's way to L2 would otherwise sit between a freed
         // place and the copy into it)
@@ -513,7 +515,7 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
             if (copied & 1u) bar_wait(smem_u32(&ms.full[0]), phase[0], limit);
             if (copied & 2u) bar_wait(smem_u32(&ms.full[1]), phase[1], limit);
         }
-    } else if (warp == 13) {
+    } else if (warp == 14) {
         // ================================================= products for S
         constexpr uint32_t kIdS = instr(kTile, kHeads, false, false);
         const bool mine = elect_one();
@@ -553,7 +555,7 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
             bar_wait(smem_u32(&ms.drain[0]), 0, limit);
         }
         __syncwarp();
-    } else if (warp == 14) {
+    } else if (warp == 15) {
         // ================================================= products for O
         constexpr uint32_t kIdO = instr(128, kHeads, true, true);
         const bool mine = elect_one();
@@ -588,31 +590,28 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
         __syncwarp();
     } else if (warp >= 4) {
         // ================================================= queries and LOW tiles
-        const int t = tid - 128;                   // token t & 15 and (page, group) pairs t >> 4 + 16 k of a tile
-        constexpr int kPairs = kTilePages * kLatentGroups, kItems = (kPairs + kFillThreads / 16 - 1) / (kFillThreads / 16);
-        uint32_t codes[kItems][BITS], scales[kItems], ids[kItems];
+        const int t = tid - 128, tau = t & 15, g = t >> 4;     // token and group of every page
+        uint32_t codes[kTilePages][BITS], scales[kTilePages], ids[kTilePages];
         TileWalk ahead = w;                        // codes: of the next LOW tile; ahead, ids: the one behind it
-        auto pair_of = [&](int k) { return (kFillThreads / 16) * k + (t >> 4); };
         auto to_low = [&](bool here) { while (here && ahead.high()) here = ahead.next(); return here; };
-        // (no branch around the loads, items and pages that are not there read their last neighbour's: a load under a condition
-        // was waited for where the paths join, 2500 cycles a tile)
+        // (no branch around the loads, pages that are not there read their last neighbour's: a load under a condition was waited
+        // for where the paths join, 2500 cycles a tile)
         auto fetch_ids = [&]() {
             const uint32_t *tbl = p.c.tbl_low + ahead.sl * p.c.max_pages + kTilePages * ahead.tile();
             const uint32_t last = ahead.pages() - 1;
 #pragma unroll
-            for (int k = 0; k < kItems; k++) ids[k] = tbl[min((uint32_t)(min(pair_of(k), kPairs - 1) / kLatentGroups), last)];
+            for (int k = 0; k < kTilePages; k++) ids[k] = tbl[min((uint32_t)k, last)];
         };
         auto fetch_codes = [&]() {
             uint32_t most = 0;
 #pragma unroll
-            for (int k = 0; k < kItems; k++) most = max(most, ids[k]);
+            for (int k = 0; k < kTilePages; k++) most = max(most, ids[k]);
             if (most >= p.c.cap_low) atomicOr(&p.c.ctrl[kCtrlStatus], PASK_DEV_INTERNAL);      // never expected, never dereferenced
 #pragma unroll
-            for (int k = 0; k < kItems; k++) {
-                const int pair = min(pair_of(k), kPairs - 1);
+            for (int k = 0; k < kTilePages; k++) {
                 const uint8_t *src = p.c.pool_low + (size_t)(ids[k] < p.c.cap_low ? ids[k] : 0u) * p.c.low_page_bytes;
-                load_codes<BITS>(src, t & 15, pair % kLatentGroups, codes[k]);
-                scales[k] = *reinterpret_cast<const uint16_t *>(src + latent_scale_off(t & 15, pair % kLatentGroups, BITS));
+                load_codes<BITS>(src, tau, g, codes[k]);
+                scales[k] = *reinterpret_cast<const uint16_t *>(src + latent_scale_off(tau, g, BITS));
             }
         };
         bool ahead_more = to_low(more);
@@ -633,8 +632,9 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
                 n_seg++;
                 const uint4 *src = p.q + ((size_t)w.s * p.c.n_q + h0) * kLatentChunks;
 #pragma unroll
-                for (int k = 0; k < kHeads / 8; k++) {         // a warp takes every eighth head, all in flight at once; heads this
-                    const int row = 8 * k + warp - 4;          // CTA does not have are zeros
+                for (int k = 0; k < (kHeads + 8) / 9; k++) {   // a warp takes every ninth head, all in flight at once; heads this
+                    const int row = 9 * k + warp - 4;          // CTA does not have are zeros
+                    if (row >= kHeads) break;
                     const bool there = row < nh_here;
 #pragma unroll
                     for (int ch = lane; ch < kLatentChunks; ch += 32)
@@ -652,29 +652,32 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
             const bool low = !w.high();
             const uint32_t np = w.pages();
             uint8_t *dst = sm + st * kTileBytes;
-            // items [k0, k1), the first half of which lie in the stage's first two pages
-            auto fill = [&](int k0, int k1) {
-#pragma unroll
+            auto fill = [&](int k0, int k1) {      // pages [k0, k1) of the tile
+#pragma unroll 1
                 for (int k = k0; k < k1; k++) {
-                    const int pair = pair_of(k), pg = pair / kLatentGroups, g = pair % kLatentGroups;
-                    if (pair < kPairs && (uint32_t)pg < np) {
+                    if ((uint32_t)k < np) {
                         uint32_t xs[16];
-                        dequantise_group<BITS>(codes[k], scales[k], xs);
+                        dequantise_group<BITS>(codes[0], scales[0], xs);
 #pragma unroll
                         for (int e = 0; e < 4; e++)
-                            *reinterpret_cast<uint4 *>(dst + pg * kLatentHighPageBytes + latent_chunk_off(t & 15, 4 * g + e)) =
+                            *reinterpret_cast<uint4 *>(dst + k * kLatentHighPageBytes + latent_chunk_off(tau, 4 * g + e)) =
                                 make_uint4(xs[4 * e], xs[4 * e + 1], xs[4 * e + 2], xs[4 * e + 3]);
+                    }
+#pragma unroll
+                    for (int j = 0; j + 1 < kTilePages; j++) {
+                        scales[j] = scales[j + 1];
+#pragma unroll
+                        for (int e = 0; e < BITS; e++) codes[j][e] = codes[j + 1][e];
                     }
                 }
             };
-            static_assert(kItems == 5 && 2 * (kFillThreads / 16) <= 2 * kLatentGroups, "items 0 and 1 are pages 0 and 1");
             if (i >= 2) ok = bar_wait(smem_u32(&ms.empty[st][0]), ((i >> 1) - 1) & 1, ok ? limit : 0) && ok;
             if (low && ok) fill(0, 2);
             if (i >= 2) ok = bar_wait(smem_u32(&ms.empty[st][1]), ((i >> 1) - 1) & 1, ok ? limit : 0) && ok;
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             if (low) {
-                fill(2, kItems);
+                fill(2, kTilePages);
                 fence_async_shared();
                 __syncwarp();
             }
@@ -846,7 +849,7 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
     fence_before();
     __syncthreads();
     fence_after();
-    if (warp == 13) tmem_free(tmem, 512);
+    if (warp == 14) tmem_free(tmem, 512);
     if (p.span && tid == 0) {
         unsigned long long t_end;
         asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t_end));
