@@ -233,7 +233,6 @@ constexpr int kTile = 64, kTilePages = 4;
 constexpr int kTileBytes = kTilePages * kLatentHighPageBytes;      // 73728
 constexpr int kDecThreads = 512, kFillThreads = kPageTokens * kLatentGroups;      // 288: nine warps
 constexpr uint32_t kMaxSlots = 1024;
-constexpr int kPrefetch = 6;                       // tiles between a prefetch into L2 and the copy (2: 3 % slower; 4 to 8: within 1 %)
 enum : uint32_t { kInfoFirst = 1, kInfoLast = 2, kInfoWhole = 4, kInfoFinal = 8 };   // first, last tile of a sequence's part; the part
                                                    // is the whole sequence; last tile of the share
 constexpr float kLazy = 8.0f;                      // log2 of how far a score may exceed the reference maximum
@@ -469,6 +468,10 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
         uint32_t i = 0, id = more ? w.page_id(lane) : 0u, ahead_id = 0, copied = 0, phase[2] = {0, 0};
         TileWalk ahead = w;
         bool ahead_more = more;
+        // Tiles between a prefetch into L2 and the copy.  What is on its way may not crowd itself out: 4 x 148 tiles (43 MB) in all
+        // of the 126 MB, whose halves may both hold a line.  One group, all HIGH, 148 sequences of 2048 rows, 16 / 64 heads: 83 /
+        // 100 us with six tiles, 66 / 87 with two, 68 / 90 with one; two groups share their tiles: six 3 % before two.
+        const int look_ahead = 4 * p.groups - 2;
         for (; more; i++) {
             const uint32_t st = i & 1, np = w.pages();
             const bool high = w.high();
@@ -497,7 +500,7 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
             }
             if (!ok) break;
             if (i == 0) {
-                for (int k = 0; k < kPrefetch; k++) ahead_more = ahead_more && ahead.next();
+                for (int k = 0; k < look_ahead; k++) ahead_more = ahead_more && ahead.next();
                 if (ahead_more) ahead_id = ahead.page_id(lane);
                 continue;
             }
