@@ -1,6 +1,7 @@
 """Latent caches on the GPU against the plain 64-bit model (latent_ref): append, read-back, decode and prompt attention."""
 import math
 import os
+import subprocess
 import sys
 
 import numpy as np
@@ -722,3 +723,80 @@ def test_prompt_chunks_then_decode(pask):
         mag = float((q[0].double().abs() @ rows.double().abs().T).max() + (qe[:, :128].double().abs() @ kv.cpu().double()[:, :, :128].abs().amax(0).T).max()) * SCALE
         assert float((lse[0] - l[0]).abs().max()) <= 2 * R.BF16_HALF_STEP * mag
     assert b.status() == 0
+
+
+FIRST_CALLS = """
+import os, sys, torch
+sys.path[:0] = [ROOT, os.path.join(ROOT, "tests")]
+import paper_2608_28276_b200 as pask
+import latent_ref as R
+i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")
+c = pask.LatentCache(R.blob([[2], [1], [0]], 1, [0], 4), 1, 20, 4, 2048, 2048, 400, 400)
+x = torch.randn(1300, 576, device="cuda").bfloat16()
+tags = (torch.arange(1300, device="cuda") % 3).to(torch.uint8)
+ids, cu, ids1, cu1 = i32(0, 2), i32(0, 600, 1300), i32(1), i32(0, 40)
+rows, lens = torch.zeros(1300, 576, dtype=torch.bfloat16, device="cuda"), torch.zeros(2, 2, dtype=torch.int32, device="cuda")
+cu_rows = i32(0, 600, 1300)
+qd, od, ws = torch.randn(2, 20, 576, device="cuda").bfloat16(), torch.zeros(2, 20, 512, dtype=torch.bfloat16, device="cuda"), c.workspace(2)
+q, kv = torch.randn(300, 4, 192, device="cuda").bfloat16(), torch.randn(1300, 4, 256, device="cuda").bfloat16()
+outs = [torch.zeros(n, 4, 128, dtype=torch.bfloat16, device="cuda") for n in (300, 300)]
+one, cq, ck = i32(0, 100), i32(0, 300), i32(0, 1300)
+def step():
+    pask.pask_append_latent(c.handle, 0, ids, cu, x, tags)
+    pask.pask_append_latent(c.handle, 0, ids1, cu1, x[:40], tags[:40])
+    pask.pask_read_latent(c.handle, 0, ids, cu_rows, rows, lens)
+    pask.pask_decode_attention_latent(c.handle, 0, ids, qd, 0.07, od, None, ws)
+    pask.pask_prompt_attention_latent(cq, cq, q, kv[:300], x[:300, 512:], 0.07, outs[0])
+    pask.pask_prompt_attention_latent(cq, ck, q, kv, x[:, 512:], 0.07, outs[1])
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    step()
+g.replay()
+torch.cuda.synchronize()
+got = [t.clone() for t in (rows, lens, od, *outs)]
+assert all(bool(t.any()) for t in got)
+pask.pask_cache_reset(c.handle)
+for t in (rows, lens, od, *outs):
+    t.zero_()
+step()
+torch.cuda.synchronize()
+assert all(torch.equal(a, b) for a, b in zip(got, (rows, lens, od, *outs)))
+print("same")
+"""
+
+
+def test_first_calls_of_a_process_can_be_captured():
+    r = subprocess.run([sys.executable, "-c", f"ROOT = {ROOT!r}" + FIRST_CALLS], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "same" in r.stdout, r.stdout + r.stderr
+
+
+def test_calls_of_two_streams_side_by_side(pask):
+    # each with its own workspace; prompts have nothing to share
+    g = torch.Generator().manual_seed(33)
+    b = Both(pask, heads=40)
+    for s in (0, 1):
+        b.append(0, [s], [normal(g, 900, 576)], [tags_of(g, 900, 5)])
+    ids = [torch.tensor([s], dtype=torch.int32, device=D) for s in (0, 1)]
+    q = [normal(g, 1, 40, 576).to(D) for _ in ids]
+    ws = [b.gpu.workspace(1) for _ in ids]
+    pq, pkv, pr = normal(g, 50, 4, 192).to(D), normal(g, 3000, 4, 256).to(D), normal(g, 3000, 64).to(D)
+    cq, ck = (torch.tensor([0, n], dtype=torch.int32, device=D) for n in (50, 3000))
+    new = lambda: ([torch.zeros((1, 40, 512), dtype=torch.bfloat16, device=D) for _ in ids], [torch.zeros((50, 4, 128), dtype=torch.bfloat16, device=D) for _ in ids])
+
+    def go(i, out):
+        pask.pask_decode_attention_latent(b.h, 0, ids[i], q[i], 0.06, out[0][i], None, ws[i])
+        pask.pask_prompt_attention_latent(cq, ck, pq, pkv, pr, SCALE, out[1][i])
+
+    want, got = new(), new()
+    for i in (0, 1):
+        go(i, want)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in ids]
+    for _ in range(10):
+        for i, st in enumerate(streams):
+            with torch.cuda.stream(st):
+                go(i, got)
+    torch.cuda.synchronize()
+    for a, c in zip(want[0] + want[1], got[0] + got[1]):
+        assert torch.equal(a, c)
