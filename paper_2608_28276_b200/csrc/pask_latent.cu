@@ -211,7 +211,7 @@ read_latent_kernel(DevCache c, int layer, int n_seqs, int total_rows, const int3
 // over that many CTAs that walk the same tiles side by side and find each other's rows in L2.
 //
 // A CTA is one of `slots` equal shares of the batch's tiles: 64 rows = four pages of one stream, a sequence's HIGH and LOW tiles
-// visited in turn, evenly mixed.  (A LOW tile is a quarter of the bytes but as much work on chip: 4.2 and 4.5 thousand cycles
+// visited in turn, evenly mixed.  (A LOW tile is a quarter of the bytes but as much work on chip: 2.5 us against 2.0
 // at 32 heads, so a tile counts as a tile.)  Roles:
 //   warp 13     HIGH tiles: one linear bulk copy a page (pages are stored in the operand layout) into its place in one of two
 //               stages, as soon as the product that last read the place is done, and a prefetch into L2 some tiles ahead
@@ -225,10 +225,11 @@ read_latent_kernel(DevCache c, int layer, int n_seqs, int total_rows, const int3
 // the rescaling of O leaves the common path.  A share that covers a whole sequence writes its result; otherwise partial sums
 // go to the workspace and decode_latent_merge joins them in a fixed order: results do not depend on timing.
 //
-// Bound by shared memory: a HIGH tile of 64 heads moves 327 KB through it (copy, X twice, Q, P), 2555 cycles at 128 B each; a
-// tile takes 3450, a LOW one about 6000 (4500 for 32 heads), its fill being as much traffic again.  Measured with the merge: 64
-// sequences of 2 to 8 thousand rows, 128 heads, all HIGH 163 us; 128 of 16 thousand tokens, 64 heads, a fifth HIGH and 0.3 LOW at
-// 4 bits 315 us; one of 1023 rows, 16 heads 12.5 us.
+// HIGH tiles are bound by memory up to 32 heads (148 sequences of 2048 rows: 64 and 71 us, 5.4 and 4.9 TB/s) and by shared memory
+// at 64: 327 KB a tile (copy, X twice, Q, P), 2555 cycles at 128 B each of 4500.  LOW tiles are
+// bound by the fill, 2.2 us for 16 heads and 3.0 for 64: of 4070 cycles the codes' requests take 1250, four pages 2030.  With the
+// merge: 64 sequences of 2 to 8 thousand rows, 128 heads, all HIGH 161 us; 128 of 16 thousand tokens, 64 heads, a fifth HIGH and
+// 0.3 LOW at 4 bits 265 us; one of 1023 rows, 16 heads 11.2 us.
 constexpr int kTile = 64, kTilePages = 4;
 constexpr int kTileBytes = kTilePages * kLatentHighPageBytes;      // 73728
 constexpr int kDecThreads = 512, kFillThreads = kPageTokens * kLatentGroups;      // 288: nine warps
