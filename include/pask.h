@@ -454,8 +454,9 @@ pask_status_t pask_append_latent(pask_cache_t *cache, int32_t layer, int32_t n_s
  * (pask_prompt_attention_latent), or for moving it elsewhere.
  *   cu_rows    dev int32 [n_seqs+1], ascending, within 0 .. total_rows: where each sequence's rows go.
  *              A range may be longer than its sequence's rows: the rest is left as it was.  A sequence
- *              whose range is malformed or too short, or whose id is out of range, is not written at
- *              all (sticky PASK_DEV_BAD_RAGGED / PASK_DEV_BAD_SEQ); the others are
+ *              whose own range (cu_rows[i], cu_rows[i+1]) is malformed or too short, or whose id is out of
+ *              range, is not written at all (sticky PASK_DEV_BAD_RAGGED / PASK_DEV_BAD_SEQ); the others
+ *              are, wherever the malformed one stands (a row that two of them claim holds either's)
  *   rows_out   dev bf16 [total_rows][576]
  *   lens_out   dev int32 [n_seqs][2] or NULL: rows in the HIGH and the LOW stream (0, 0 for a bad id)
  * A sequence may be named more than once. */

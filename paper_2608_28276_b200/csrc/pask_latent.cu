@@ -18,6 +18,7 @@ namespace pask {
 namespace {
 
 constexpr int kRowThreads = 288;                  // 18 groups x 16 tokens of a page
+constexpr int kReadCtas = 6;                      // CTAs of the read-back an SM has at a time
 __device__ __forceinline__ uint32_t pages_touched(uint32_t old, uint32_t cnt) {
     return cnt ? ((old + cnt - 1) >> 4) - (old >> 4) + 1 : 0u;
 }
@@ -113,52 +114,69 @@ append_latent_kernel(DevCache c, int layer, int n_seqs, const uint4 *__restrict_
     }
 }
 
-// pask_read_latent: a work item is a page of a sequence; sequence i owns items cu_rows[i] / 16 + 2 i .. (at least as many as
-// it can have pages), so an item finds its sequence without a prefix over page counts.  Bound by memory: 213 K rows of the same
-// batch in 67 us (382 MB: 5.7 TB/s).
+// pask_read_latent: a work item is a page of a sequence.  Every CTA first counts the pages of the sequences that have a range to
+// go to (a prefix over the batch, a sequence a thread) and then finds an item's sequence in it: the order of the ranges, and
+// what a malformed one says, does not come into it.  Bound by memory: 213 K rows of the same batch in 67 us (382 MB: 5.7 TB/s).
 template <int BITS>
-__global__ void __launch_bounds__(kRowThreads)
+__global__ void __launch_bounds__(kRowThreads, kReadCtas)
 read_latent_kernel(DevCache c, int layer, int n_seqs, int total_rows, const int32_t *__restrict__ seq_ids,
                    const int32_t *__restrict__ cu_rows, uint4 *__restrict__ out, int32_t *__restrict__ lens_out) {
     __shared__ __align__(16) uint8_t s_rows[kPageTokens * (kLatentDim * 2 + 16)];
+    __shared__ uint32_t s_base[PASK_MAX_SEQS_PER_CALL], s_warp[kRowThreads / 32];
     constexpr int kStride = kLatentDim * 2 + 16;
-    const int tid = threadIdx.x;
-    if (lens_out)
-        for (int i = blockIdx.x * kRowThreads + tid; i < n_seqs; i += gridDim.x * kRowThreads) {
-            const int seq = seq_ids[i];
-            const bool ok = seq >= 0 && seq < c.max_seqs;
-            const size_t sl = (size_t)(ok ? seq : 0) * c.n_layers + layer;
-            lens_out[2 * i] = ok ? (int32_t)c.n_high[sl] : 0;
-            lens_out[2 * i + 1] = ok ? (int32_t)c.n_low[sl] : 0;
-        }
-    const uint32_t n_items = (uint32_t)(total_rows >> 4) + 2u * (uint32_t)n_seqs;
-    for (uint32_t item = blockIdx.x; item < n_items; item += gridDim.x) {
-        // the sequence: the last one whose first item is not behind this one
-        int cnt = 0;
-        for (int x = 0; x < n_seqs; x += kRowThreads) {
-            bool before = false;
-            if (x + tid < n_seqs) {
-                const int r = cu_rows[x + tid];
-                before = (uint32_t)(max(0, min(r, total_rows)) >> 4) + 2u * (uint32_t)(x + tid) <= item;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    uint32_t n_items = 0;
+    for (int x = 0; x < n_seqs; x += kRowThreads) {
+        const int i = x + tid;
+        uint32_t pages = 0;
+        if (i < n_seqs) {
+            const int seq = seq_ids[i], r0 = cu_rows[i], r1 = cu_rows[i + 1];
+            uint32_t err = 0, nh = 0, nl = 0;
+            if (seq < 0 || seq >= c.max_seqs) {
+                err = PASK_DEV_BAD_SEQ;
+            } else {
+                const size_t sl = (size_t)seq * c.n_layers + layer;
+                nh = c.n_high[sl];
+                nl = c.n_low[sl];
             }
-            cnt += __syncthreads_count(before);
+            if (r0 < 0 || r1 < r0 || r1 > total_rows || nh + nl > (uint32_t)(r1 - r0)) err |= PASK_DEV_BAD_RAGGED;
+            if (!err) pages = ((nh + 15) >> 4) + ((nl + 15) >> 4);
+            if (blockIdx.x == 0) {
+                if (err) atomicOr(&c.ctrl[kCtrlStatus], err);      // this sequence's rows are not written
+                if (lens_out) {
+                    lens_out[2 * i] = (int32_t)nh;
+                    lens_out[2 * i + 1] = (int32_t)nl;
+                }
+            }
         }
-        const int i = cnt - 1;
-        if (i < 0) continue;
-        const int seq = seq_ids[i], r0 = cu_rows[i], r1 = cu_rows[i + 1];
-        uint32_t err = 0;
-        if (seq < 0 || seq >= c.max_seqs) err |= PASK_DEV_BAD_SEQ;
-        if (r0 < 0 || r1 < r0 || r1 > total_rows) err |= PASK_DEV_BAD_RAGGED;
-        const size_t sl = (size_t)(err ? 0 : seq) * c.n_layers + layer;
-        const uint32_t nh = c.n_high[sl], nl = c.n_low[sl];
-        if (!err && nh + nl > (uint32_t)(r1 - r0)) err |= PASK_DEV_BAD_RAGGED;
-        if (err) {                                 // this sequence's rows are not written
-            if (tid == 0) atomicOr(&c.ctrl[kCtrlStatus], err);
-            continue;
+        uint32_t inc = pages;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const uint32_t o = __shfl_up_sync(0xffffffffu, inc, d);
+            if (lane >= d) inc += o;
         }
-        const uint32_t in_seq = item - ((uint32_t)(r0 >> 4) + 2u * (uint32_t)i);
-        const uint32_t ph = (nh + 15) >> 4, pl = (nl + 15) >> 4;
-        if (in_seq >= ph + pl) continue;
+        if (x > 0) __syncthreads();                // s_warp has been read
+        if (lane == 31) s_warp[warp] = inc;
+        __syncthreads();
+        uint32_t base = n_items + inc - pages;
+#pragma unroll
+        for (int w = 0; w < kRowThreads / 32; w++) {
+            if (w < warp) base += s_warp[w];
+            n_items += s_warp[w];
+        }
+        if (i < n_seqs) s_base[i] = base;
+    }
+    __syncthreads();
+    for (uint32_t item = blockIdx.x; item < n_items; item += gridDim.x) {
+        int i = 0;                                 // the last sequence that does not begin behind the item (its pages: the item's)
+        for (int hi = n_seqs - 1; i < hi;) {
+            const int mid = (i + hi + 1) >> 1;
+            if (s_base[mid] <= item) i = mid; else hi = mid - 1;
+        }
+        const uint32_t r0 = (uint32_t)cu_rows[i], in_seq = item - s_base[i];
+        const size_t sl = (size_t)seq_ids[i] * c.n_layers + layer;
+        const uint32_t nh = c.n_high[sl], nl = c.n_low[sl], ph = (nh + 15) >> 4, pl = (nl + 15) >> 4;
+        if (in_seq >= ph + pl) continue;           // (more than 2^32 pages: ranges that overlap many times over)
         const bool high = in_seq < ph;
         const uint32_t pg = high ? in_seq : in_seq - ph;
         const uint32_t valid = min(16u, (high ? nh : nl) - 16u * pg);
@@ -167,7 +185,7 @@ read_latent_kernel(DevCache c, int layer, int n_seqs, int total_rows, const int3
             if (tid == 0) atomicOr(&c.ctrl[kCtrlStatus], PASK_DEV_INTERNAL);
             continue;
         }
-        uint4 *dst = out + (size_t)((uint32_t)r0 + (high ? 0u : nh) + 16u * pg) * kLatentChunks;
+        uint4 *dst = out + (size_t)(r0 + (high ? 0u : nh) + 16u * pg) * kLatentChunks;
         if (high) {
             const uint8_t *src = c.pool_high + (size_t)page * kLatentHighPageBytes;
             uint4 x[4];
@@ -967,7 +985,7 @@ pask_status_t launch_append_latent(pask_cache *c, int layer, int n_seqs, int tot
 pask_status_t launch_read_latent(pask_cache *c, int layer, int n_seqs, int total_rows, const int32_t *seq_ids,
                                  const int32_t *cu_rows, void *rows_out, int32_t *lens_out, cudaStream_t stream) {
     const long long items = (long long)(total_rows >> 4) + 2LL * n_seqs;
-    const int ctas = (int)(items < (long long)c->sm_count * 6 ? items : c->sm_count * 6);
+    const int ctas = (int)(items < (long long)c->sm_count * kReadCtas ? items : c->sm_count * kReadCtas);
     auto kern = c->dev.low_bits == 8 ? read_latent_kernel<8> : c->dev.low_bits == 2 ? read_latent_kernel<2> : read_latent_kernel<4>;
     kern<<<ctas, kRowThreads, 0, stream>>>(c->dev, layer, n_seqs, total_rows, seq_ids, cu_rows, static_cast<uint4 *>(rows_out), lens_out);
     return cudaGetLastError() == cudaSuccess ? PASK_OK : PASK_ERR_CUDA;
