@@ -429,8 +429,10 @@ pask_status_t pask_decode_step_drain(pask_cache_t *cache);
  * call on K and V refuses it with PASK_ERR_UNSUPPORTED_SHAPE, and these calls refuse the other caches.
  * Costs: m(H) = 1152 bytes per token and layer, m(L) = 576 * low_bits / 8 + 36.
  *   RETAIN-HIGH keeps the row's bits.  RETAIN-LOW stores, per group of 32 consecutive values, a bf16
- *   scale s = bf16(amax / L) (L = 7, 127 or 1 for low_bits 4, 8 or 2; zero if below 2^-126) and codes
- *   rint(x / s), ties to even (zero if s is); the value it stands for is bf16(code * s), which is what
+ *   scale s = bf16(amax / L) (L = 7, 127 or 1 for low_bits 4, 8 or 2; zero if below 2^-126; at most the
+ *   largest for which bf16(L * s) is finite: 36.25 * 2^120 and 2 * 2^120 for L = 7 and 127, which only an
+ *   amax of the largest finite value exceeds) and codes rint(x / s), ties to even, at most L in magnitude
+ *   (zero if s is); the value it stands for is bf16(code * s), finite for finite x, and is what
  *   attention computes with.  (bf16 scales, where the other caches have fp16 ones: the value is an
  *   operand of a bf16 matrix product, and a bf16 product rounds it once, in any range.)
  * The calls run on the device the cache was created on (PASK_ERR_INVALID_ARG if another is current).
@@ -475,7 +477,9 @@ pask_status_t pask_read_latent(pask_cache_t *cache, int32_t layer, int32_t n_seq
  *   workspace dev, at least pask_workspace_bytes(cache, n_seqs) bytes, 256-byte aligned; contents undefined
  *             afterwards.  Calls that may overlap on the GPU (two streams, two captured graphs replayed
  *             side by side) need one each.
- * Softmax weights are rounded to bf16 for the product with the rows, sums are fp32.  A sequence with
+ * Softmax weights are rounded to bf16 for the product with the rows, sums are fp32.  The sums are taken
+ * before the division by the weights' total, each weight at most 2^8: rows so large that a score or such
+ * a sum leaves fp32's range give infinities or NaN.  A sequence with
  * nothing retained, or an id out of range (sticky PASK_DEV_BAD_SEQ), gets out = 0 and lse = -inf.
  * A sequence may be named more than once. */
 pask_status_t pask_decode_attention_latent(pask_cache_t *cache, int32_t layer, int32_t n_seqs,
@@ -499,7 +503,8 @@ pask_status_t pask_decode_attention_latent(pask_cache_t *cache, int32_t layer, i
  *               the last dims of latent rows can be used where they lie).  Must cover total_k rows
  *   scale       positive and finite
  *   out         dev bf16 [total_q][n_heads][128];  lse  dev fp32 [total_q][n_heads] or NULL
- * Values of a sequence's rows must be finite; rows outside every sequence may hold anything.  A bounded wait inside the
+ * Values of a sequence's rows must be finite (and within what fp32 sums can hold, as for pask_decode_attention_latent); rows
+ * outside every sequence may hold anything.  A bounded wait inside the
  * kernel that runs out (never expected) leaves NaN in the rows it concerns: there is no cache whose status word could say so. */
 pask_status_t pask_prompt_attention_latent(int32_t n_seqs, int32_t total_q, int32_t total_k, int32_t n_heads,
                                            const int32_t *cu_q, const int32_t *cu_k, const void *q, const void *kv,

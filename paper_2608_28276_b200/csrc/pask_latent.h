@@ -10,40 +10,58 @@ namespace {
 
 constexpr float kMinScale = 1.17549435e-38f;      // 2^-126: a smaller scale is stored as zero
 
-template <int BITS> struct Codes;                 // levels on each side of zero; the offset that makes codes unsigned
-template <> struct Codes<2> { static constexpr int kLevels = 1, kOffset = 2; };
-template <> struct Codes<4> { static constexpr int kLevels = 7, kOffset = 8; };
-template <> struct Codes<8> { static constexpr int kLevels = 127, kOffset = 128; };
+// levels on each side of zero; the offset that makes codes unsigned; the largest scale: bf16(levels * scale) has to be finite,
+// and the next bf16 number above 36.25 * 2^120 (2 * 2^120 for 127 levels) times the levels rounds to 2^128
+template <int BITS> struct Codes;
+template <> struct Codes<2> { static constexpr int kLevels = 1, kOffset = 2; static constexpr float kMaxScale = 3.3895314e38f; };
+template <> struct Codes<4> { static constexpr int kLevels = 7, kOffset = 8; static constexpr float kMaxScale = 36.25f * 0x1p120f; };
+template <> struct Codes<8> { static constexpr int kLevels = 127, kOffset = 128; static constexpr float kMaxScale = 2.0f * 0x1p120f; };
 
 __device__ __forceinline__ float latent_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float latent_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
 // The 32 values of one group (16 bf16 pairs) -> BITS packed words and the scale's bf16 bits.
-// scale = bf16(amax / levels) (zero unless a normal number), code = x / scale to the nearest integer, ties to even.
+// scale = bf16(amax / levels), at most kMaxScale (zero unless a normal number), code = x / scale to the nearest integer, ties to
+// even, at most `levels` in magnitude.
 // x and scale have 8 significant bits each, so a quotient that is no tie is at least 2^-9 away from one: rounding
 // x * (1 / scale) to a multiple of 2^-10 (the first addition, 1.5 * 2^13) removes the error of the reciprocal and leaves
 // exact ties exact; the second addition (up to 1.5 * 2^23 + offset) rounds to the integer, ties to even.  |x / scale| is
-// at most levels * (1 + 2^-8), which rounds to levels: no clamp.
+// at most levels * (1 + 2^-8), which rounds to levels; only under kMaxScale can it be more: 255 / 36.25 rounds to 7 all the same,
+// 255 / 2 to 128, so that with eight-bit codes limit_group moves those values to 254 first (rarely: a limit on every code
+// cost 2 us of a bulk append's 76).
 struct GroupScale { float inv; uint32_t bits; };
 template <int BITS>
 __device__ __forceinline__ GroupScale group_scale(float amax) {
-    __nv_bfloat16 sh = __float2bfloat16_rn(__fdiv_rn(amax, (float)Codes<BITS>::kLevels));
-    float s = __bfloat162float(sh);
-    if (!(s >= kMinScale)) { s = 0.0f; sh = __ushort_as_bfloat16(0); }
-    return {s == 0.0f ? 0.0f : __fdiv_rn(1.0f, s), (uint32_t)__bfloat16_as_ushort(sh)};
+    float s = __bfloat162float(__float2bfloat16_rn(__fdiv_rn(amax, (float)Codes<BITS>::kLevels)));
+    s = s >= kMinScale ? fminf(s, Codes<BITS>::kMaxScale) : 0.0f;
+    return {s == 0.0f ? 0.0f : __fdiv_rn(1.0f, s), __float_as_uint(s) >> 16};
 }
 template <int BITS>
 __device__ __forceinline__ uint32_t code_of(float x, float inv) {
     const float grid = __fmaf_rn(x, inv, 12288.0f);
     return __float_as_uint(__fadd_rn(grid, 12582912.0f - 12288.0f + (float)Codes<BITS>::kOffset)) & ((1u << BITS) - 1u);
 }
+template <int BITS, int N>
+__device__ __forceinline__ void limit_group(float amax, uint32_t (&xs)[N]) {
+    constexpr float kTop = Codes<8>::kLevels * Codes<8>::kMaxScale;
+    if (BITS == 8 && amax > kTop) {
+        const __nv_bfloat162 top = __float2bfloat162_rn(kTop), bottom = __float2bfloat162_rn(-kTop);
+#pragma unroll
+        for (int e = 0; e < N; e++) {
+            const __nv_bfloat162 x = __hmin2(__hmax2(*reinterpret_cast<const __nv_bfloat162 *>(&xs[e]), bottom), top);
+            xs[e] = *reinterpret_cast<const uint32_t *>(&x);
+        }
+    }
+}
 template <int BITS>
-__device__ __forceinline__ uint32_t quantise_group(const uint32_t (&xs)[16], uint32_t (&words)[BITS]) {
+__device__ __forceinline__ uint32_t quantise_group(uint32_t (&xs)[16], uint32_t (&words)[BITS]) {
     __nv_bfloat162 m2 = __habs2(*reinterpret_cast<const __nv_bfloat162 *>(&xs[0]));
 #pragma unroll
     for (int e = 1; e < 16; e++) m2 = __hmax2(m2, __habs2(*reinterpret_cast<const __nv_bfloat162 *>(&xs[e])));
     const uint32_t m = *reinterpret_cast<const uint32_t *>(&m2);
-    const GroupScale sc = group_scale<BITS>(fmaxf(latent_lo(m), latent_hi(m)));
+    const float amax = fmaxf(latent_lo(m), latent_hi(m));
+    const GroupScale sc = group_scale<BITS>(amax);
+    limit_group<BITS>(amax, xs);
     uint32_t code[32];
 #pragma unroll
     for (int e = 0; e < 32; e++) code[e] = code_of<BITS>((e & 1) ? latent_hi(xs[e >> 1]) : latent_lo(xs[e >> 1]), sc.inv);
@@ -120,13 +138,14 @@ __device__ __forceinline__ void store_codes(uint8_t *page, int tau, int group, c
 // warp.  Lanes without `write` only lend their chunk to the group's amax.
 template <int BITS>
 __device__ __forceinline__ void store_chunk(uint8_t *page, int tau, int chunk, const uint4 x, bool write) {
-    const uint32_t xs[4] = {x.x, x.y, x.z, x.w};
+    uint32_t xs[4] = {x.x, x.y, x.z, x.w};
     float amax = 0.0f;
 #pragma unroll
     for (int e = 0; e < 4; e++) amax = fmaxf(amax, fmaxf(fabsf(latent_lo(xs[e])), fabsf(latent_hi(xs[e]))));
     amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
     amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
     const GroupScale sc = group_scale<BITS>(amax);
+    limit_group<BITS>(amax, xs);
     uint32_t code[8];
 #pragma unroll
     for (int e = 0; e < 8; e++) code[e] = code_of<BITS>((e & 1) ? latent_hi(xs[e >> 1]) : latent_lo(xs[e >> 1]), sc.inv);

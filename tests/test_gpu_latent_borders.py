@@ -83,3 +83,46 @@ def test_read_of_a_thousand_ranges_in_descending_order(pask):
         ids += [k % 4, (k + 1) % 4]
         cu += places[k]
     read_and_check(pask, b, ids, cu + [0], at)
+
+
+# ------------------------------------------------------------------------------------------- the largest finite values
+
+TOP = 2.0 ** 120              # the last binade of bf16: 128 .. 255 times this
+
+
+def low_values(x, bits):
+    """What RETAIN-LOW stands for, in 64 bits: the largest scale is the one whose value of the last level is finite."""
+    levels = R.LEVELS[bits]
+    v = x.double().reshape(-1, 32)
+    s = (v.abs().amax(1, keepdim=True) / levels).to(torch.bfloat16).double()
+    s = s.clamp_max({1: 255 * TOP, 7: 36.25 * TOP, 127: 2 * TOP}[levels])
+    assert bool(torch.isfinite((s * levels).to(torch.bfloat16)).all())
+    code = torch.round(v / s).clamp(-levels, levels)
+    return (code * s).to(torch.bfloat16).reshape(-1, 576)
+
+
+@pytest.mark.parametrize("bits", [2, 4, 8])
+def test_finite_values_stay_finite(pask, bits):
+    # every mantissa of the last binade as a group's largest value, both signs, other values of the group anywhere below it
+    g = torch.Generator().manual_seed(60)
+    m = torch.arange(128, 256).repeat_interleave(4)
+    x = torch.randint(-255, 256, (512, 576), generator=g).double() * TOP * (torch.arange(512)[:, None] % 2 + 1) / 2
+    x = torch.minimum(torch.maximum(x, -m[:, None].double() * TOP), m[:, None].double() * TOP).to(torch.bfloat16)
+    x[:, ::32] = (m * torch.tensor([1, -1, 1, -1]).repeat(128)).double()[:, None].to(torch.bfloat16) * TOP
+    x[-1] = torch.finfo(torch.bfloat16).max
+    x[-2] = -x[-1]
+    want = low_values(x, bits)
+    assert bool(torch.isfinite(want).all())
+    b = Both(pask, bits, n_layers=1, lut=[[1]])
+    tags = torch.zeros(512, dtype=torch.uint8, device=D)
+    pask.pask_append_latent(b.h, 0, i32([0]), i32([0, 512]), x.to(D), tags)                   # two kernels
+    for at in range(0, 512, 128):                                                             # one launch
+        pask.pask_append_latent(b.h, 0, i32([1]), i32([0, 128]), x[at:at + 128].to(D), tags[:128])
+    rows = torch.zeros((1024, 576), dtype=torch.bfloat16, device=D)
+    pask.pask_read_latent(b.h, 0, i32([0, 1]), i32([0, 512, 1024]), rows)
+    assert torch.equal(rows[:512].cpu(), want) and torch.equal(rows[512:].cpu(), want)
+    # a row alone with a zero query: its values come out as they are stored
+    pask.pask_append_latent(b.h, 0, i32([2]), i32([0, 1]), x[-1:].to(D), tags[:1])
+    out, lse = b.decode(0, [2], torch.zeros((1, 16, 576), dtype=torch.bfloat16))
+    assert torch.equal(out[0].cpu(), want[-1, :512].expand(16, 512)) and bool((lse == 0).all())
+    assert b.status() == 0
