@@ -504,8 +504,9 @@ pask_status_t pask_decode_attention_latent(pask_cache_t *cache, int32_t layer, i
  *   scale       positive and finite
  *   out         dev bf16 [total_q][n_heads][128];  lse  dev fp32 [total_q][n_heads] or NULL
  * Values of a sequence's rows must be finite (and within what fp32 sums can hold, as for pask_decode_attention_latent); rows
- * outside every sequence may hold anything.  A bounded wait inside the
- * kernel that runs out (never expected) leaves NaN in the rows it concerns: there is no cache whose status word could say so. */
+ * outside every sequence may hold anything.  There is no cache whose status word could say that a bounded wait inside the
+ * kernel ran out (never expected): every row that the call does not finish for it gets NaN in out and lse, the others are
+ * as always; none is left as it was (see pask_debug_set_prompt_wait). */
 pask_status_t pask_prompt_attention_latent(int32_t n_seqs, int32_t total_q, int32_t total_k, int32_t n_heads,
                                            const int32_t *cu_q, const int32_t *cu_k, const void *q, const void *kv,
                                            const void *k_rope, int32_t rope_stride, float scale, void *out,
@@ -595,6 +596,13 @@ pask_status_t pask_debug_set_attention_ctas(pask_cache_t *cache, int32_t n_ctas)
  * barrier on top of what it brings: the copy completes as always, the barrier does not, the wait
  * runs out.  Host-side settings of the handle, used by the calls issued after it. */
 pask_status_t pask_debug_set_wait(pask_cache_t *cache, int64_t limit_cycles, uint32_t surplus_bytes);
+/* pask_debug_set_wait bounds the waits of pask_decode_attention_latent in the same way.  Those of
+ * pask_prompt_attention_latent, which has no cache, are bounded by this call's limit (100000 .. 1e12 cycles,
+ * default 4e9, about two seconds; the wait for a work item that was asked for: twice that); surplus_bytes as
+ * above, announced by the first copy of every second CTA (where CTAs share a block of queries, of every
+ * second cluster's first CTA), so that a test sees both kinds of rows.  Holds for the process, for the calls
+ * issued after it. */
+pask_status_t pask_debug_set_prompt_wait(int64_t limit_cycles, uint32_t surplus_bytes);
 /* Where, inside a plan area for n_seqs sequences, the page-order list of (layer, parity) lies: byte
  * offset and length.  For tests of the streaming kernel's own bounds check: a page id beyond what
  * the pools hold (a plan somebody overwrote) is never dereferenced -- the kernel reads page 0

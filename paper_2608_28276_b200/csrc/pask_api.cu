@@ -951,6 +951,12 @@ pask_status_t pask_debug_set_wait(pask_cache_t *c, int64_t limit_cycles, uint32_
     return PASK_OK;
 }
 
+pask_status_t pask_debug_set_prompt_wait(int64_t limit_cycles, uint32_t surplus_bytes) {
+    if (limit_cycles < 100000 || limit_cycles > 1000000000000LL || surplus_bytes > 65536u || (surplus_bytes & 15u)) return PASK_ERR_INVALID_ARG;
+    set_prompt_wait(limit_cycles, surplus_bytes);
+    return PASK_OK;
+}
+
 pask_status_t pask_debug_partition(int32_t n_seqs, const uint32_t *pages_high, const uint32_t *pages_low,
                                    int32_t n_ctas, uint32_t *ranges) try {
     if (n_seqs < 1 || n_ctas < 1 || !pages_high || !pages_low || !ranges) return PASK_ERR_INVALID_ARG;

@@ -214,6 +214,7 @@ pask_status_t launch_read_latent(pask_cache *c, int layer, int n_seqs, int total
 pask_status_t launch_decode_latent(pask_cache *c, int layer, int n_seqs, const int32_t *seq_ids, const void *q, float scale,
                                    void *out, float *lse, void *workspace, cudaStream_t stream);
 size_t latent_workspace_bytes(const pask_cache *c, int n_seqs);
+void set_prompt_wait(long long limit_cycles, uint32_t surplus_bytes);    // for the calls of the process from now on
 pask_status_t launch_prompt_latent(int n_seqs, int total_q, int total_k, int n_heads, const int32_t *cu_q, const int32_t *cu_k,
                                    const void *q, const void *kv, const void *k_rope, int rope_stride, float scale, void *out,
                                    float *lse, cudaStream_t stream);

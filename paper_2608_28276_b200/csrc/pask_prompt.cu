@@ -29,6 +29,7 @@
 #include <cuda.h>
 #include <cuda_bf16.h>
 
+#include <atomic>
 #include <cmath>
 
 #include "pask_internal.h"
@@ -44,15 +45,22 @@ constexpr int kSub = kBlockK * 128;                // 128 rows x 64 dims: 16 KB
 constexpr int kQBytes = 3 * kSub, kKBytes = 3 * kSub, kVBytes = 2 * kSub, kRing = 8;
 constexpr int kThreads = 384;
 constexpr float kLazy = 8.0f;
-constexpr long long kWaitCycles = 4000000000LL;    // bound of a wait: about two seconds
+// pask_debug_set_prompt_wait: bound of a wait in SM clock cycles (about two seconds), bytes a copy announces and does not bring
+std::atomic<long long> g_wait_cycles{4000000000LL};
+std::atomic<uint32_t> g_surplus{0};
 
 struct PromptParams {
     int n_seqs, total_q, total_k, n_heads;
     const int32_t *cu_q, *cu_k;
     float scale_log2;
+    uint32_t surplus;
     __nv_bfloat16 *out;
     float *lse;
+    uint32_t wait_kcycles;
+    __device__ __forceinline__ long long wait_cycles() const { return (long long)wait_kcycles << 10; }
 };
+// (another 64 bytes of parameters are another miss of the constant cache: 1 us a call)
+static_assert(sizeof(PromptParams) <= 64, "one line of the constant cache");
 
 struct Item {
     int q0, nq, k0, nk, head;                      // first row of the sequence, rows; the same of its keys
@@ -65,7 +73,7 @@ struct __align__(16) PromptSmem {
     uint64_t item_full[2], item_empty[2], steal, drain;
     uint4 answer;
     Item item[2];
-    uint32_t tmem;
+    uint32_t tmem, failed;                         // failed: a softmax warp's wait has run out
     float m[kBlockQ], l[kBlockQ];                  // kSplit > 1: reference maximum and sum of each query over this CTA's keys
 };
 
@@ -171,6 +179,28 @@ struct Ranker {
     }
 };
 
+// A softmax warp's wait ran out (never expected): its rows of item n and of those that the CTA has accepted behind it say so.  The
+// next one, or the -1 at their end, comes at most a wait for the other warps and one for an answer later, and an item's place is
+// not filled again before every softmax warp has read the next item.  begun: items this warp has read.  Out of line: inlined,
+// it cost 1 us of a call of 150.
+__device__ __noinline__ void give_up(const PromptParams &p, PromptSmem &sm, uint32_t n, uint32_t begun, int row_in, int lane) {
+    using namespace umma;
+    if (lane == 0) *(volatile uint32_t *)&sm.failed = 1;
+    for (; __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.item_full[n & 1]), (n >> 1) & 1, 4 * p.wait_cycles())); n++) {
+        const Item it = sm.item[n & 1];
+        __syncwarp();
+        if (lane == 0 && n >= begun) bar_arrive(smem_u32(&sm.item_empty[n & 1]));
+        if (it.block < 0) break;
+        const int i = it.block * kBlockQ + row_in;
+        if (i < it.nq) {
+            const size_t row = (size_t)(it.q0 + i) * p.n_heads + it.head;
+            for (int d = 0; d < kV; d++) p.out[row * kV + d] = __ushort_as_bfloat16((unsigned short)0x7FC0);
+            if (p.lse) p.lse[row] = __int_as_float(0x7FC00000);
+        }
+        __syncwarp();
+    }
+}
+
 template <int kSplit>
 __global__ void __launch_bounds__(kThreads, 1)
 prompt_latent_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CUtensorMap map_q,
@@ -181,6 +211,7 @@ prompt_latent_kernel(const __grid_constant__ PromptParams p, const __grid_consta
     PromptSmem &sm = *reinterpret_cast<PromptSmem *>(s_raw);
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
     if (tid == 0) {
+        sm.failed = 0;
         bar_init(smem_u32(&sm.q_full), 1);
         bar_init(smem_u32(&sm.q_empty), 1);
         bar_init(smem_u32(&sm.steal), 1);
@@ -208,13 +239,12 @@ prompt_latent_kernel(const __grid_constant__ PromptParams p, const __grid_consta
     const uint32_t tmem = sm.tmem;
     constexpr uint32_t kS = 0, kO = 256;           // columns of tile 0; tile 1 is 128 behind
     const int part = kSplit > 1 ? (int)blockIdx.x % kSplit : 0;      // = rank in the cluster
-    Item item;                                     // kSplit > 1, softmax threads: the item of the cluster
-    item.block = -1;
+    const long long limit = p.wait_cycles();
     bool ok = true;
     // the CTA's n-th item; false behind the last one or after a wait ran out
     auto next_item = [&](uint32_t n, Item &it) {
         const uint32_t slot = n & 1;
-        ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.item_full[slot]), (n >> 1) & 1, kWaitCycles)) && ok;
+        ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.item_full[slot]), (n >> 1) & 1, limit)) && ok;
         if (!ok) return false;
         it = sm.item[slot];
         __syncwarp();
@@ -245,13 +275,15 @@ prompt_latent_kernel(const __grid_constant__ PromptParams p, const __grid_consta
             if constexpr (kSplit > 1) { x = -1; continue; }
             // The next one only when the softmax has begun with this one: items held back behind others
             // make the tail longer (4 prompts of 4 to 8 thousand: 833 us with up to three ahead, 820 with one).
-            ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.item_empty[slot]), (n >> 1) & 1, kWaitCycles));
+            ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.item_empty[slot]), (n >> 1) & 1, limit));
             if (!ok) break;
+            if (*(volatile uint32_t *)&sm.failed) { x = -1; continue; }    // no further one
             if (lane == 0) {
                 bar_expect(smem_u32(&sm.steal), 16);
                 steal_ask(smem_u32(&sm.answer), smem_u32(&sm.steal));
             }
-            ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.steal), asked++ & 1, kWaitCycles));
+            // (longer than other waits: a CTA that has been taken over is nobody else's any more)
+            ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.steal), asked++ & 1, 2 * limit));
             if (!ok) break;
             x = steal_answer(smem_u32(&sm.answer));
             __syncwarp();
@@ -266,12 +298,13 @@ prompt_latent_kernel(const __grid_constant__ PromptParams p, const __grid_consta
             const Part in = part_of(it, part, kSplit);
             const int n0 = in.n[0], n1 = in.n[1], nb = max(n0, n1);
             if (nb == 0) continue;
-            if (qc > 0) ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.q_empty), (qc - 1) & 1, kWaitCycles));
+            if (qc > 0) ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.q_empty), (qc - 1) & 1, limit));
             if (!ok) break;
             qc++;
             const bool mine = elect_one();
             if (mine) {
-                bar_expect(qf, (n0 ? kQBytes : 0) + (n1 ? kQBytes : 0));
+                const uint32_t extra = qc == 1 && part == 0 && ((blockIdx.x / kSplit) & 1) ? p.surplus : 0u;
+                bar_expect(qf, (n0 ? kQBytes : 0) + (n1 ? kQBytes : 0) + extra);
                 for (int t = 0; t < 2; t++)
                     if (t ? n1 : n0)
                         for (int c = 0; c < 3; c++)
@@ -281,20 +314,20 @@ prompt_latent_kernel(const __grid_constant__ PromptParams p, const __grid_consta
                 // keys, piece by piece: over the last piece of the keys two blocks before, over that block's values as their halves
                 // are done with (one piece takes 16 KB of copy time from a freed place to the product that waits for it, not 48)
                 const uint32_t st = g & 1, row = (uint32_t)(it.k0 + (in.first + j) * kBlockK), kf = smem_u32(&sm.k_full[st]), ph = ((g >> 1) - 1) & 1;
-                if (g >= 2) ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.k_empty[st]), ph, kWaitCycles));
+                if (g >= 2) ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.k_empty[st]), ph, limit));
                 if (!ok) break;
                 if (mine) {
                     bar_expect(kf, kKBytes);
                     tile_load3(ring + ((5 * g) & 7) * kSub, &map_kv, 0, it.head, row, kf);
                 }
-                if (g >= 2) ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.v_half[st]), ph, kWaitCycles));
+                if (g >= 2) ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.v_half[st]), ph, limit));
                 if (!ok) break;
                 if (mine) tile_load3(ring + ((5 * g + 1) & 7) * kSub, &map_kv, 64, it.head, row, kf);
-                if (g >= 2) ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.v_empty[st]), ph, kWaitCycles));
+                if (g >= 2) ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.v_empty[st]), ph, limit));
                 if (!ok) break;
                 if (mine) tile_load2(ring + ((5 * g + 2) & 7) * kSub, &map_rope, 0, row, kf);
                 // values: over the first two pieces of the keys one block before
-                if (g >= 1) ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.k_empty[st ^ 1]), ((g - 1) >> 1) & 1, kWaitCycles));
+                if (g >= 1) ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.k_empty[st ^ 1]), ((g - 1) >> 1) & 1, limit));
                 if (!ok) break;
                 if (mine) {
                     const uint32_t vf = smem_u32(&sm.v_full[st]);
@@ -308,10 +341,10 @@ prompt_latent_kernel(const __grid_constant__ PromptParams p, const __grid_consta
             if (!ok) break;
         }
         if (!ok) {                                 // gave up: let the copies in flight land (bounded) before the CTA ends
-            if (qc) bar_wait(qf, (qc - 1) & 1, kWaitCycles);
+            if (qc) bar_wait(qf, (qc - 1) & 1, limit);
             for (uint32_t b = g > 1 ? g - 1 : 0; b <= g; b++) {
-                bar_wait(smem_u32(&sm.k_full[b & 1]), (b >> 1) & 1, b < g ? kWaitCycles : 1000000);
-                bar_wait(smem_u32(&sm.v_full[b & 1]), (b >> 1) & 1, b < g ? kWaitCycles : 1000000);
+                bar_wait(smem_u32(&sm.k_full[b & 1]), (b >> 1) & 1, b < g ? limit : 1000000);
+                bar_wait(smem_u32(&sm.v_full[b & 1]), (b >> 1) & 1, b < g ? limit : 1000000);
             }
         }
     } else if (warp == 8) {
@@ -342,9 +375,9 @@ prompt_latent_kernel(const __grid_constant__ PromptParams p, const __grid_consta
             const Part in = part_of(it, part, kSplit);
             const int nt[2] = {in.n[0], in.n[1]}, nb = max(nt[0], nt[1]);
             if (nb == 0) continue;
-            ok = bar_wait(smem_u32(&sm.q_full), qc & 1, kWaitCycles);
+            ok = bar_wait(smem_u32(&sm.q_full), qc & 1, limit);
             qc++;
-            ok = bar_wait(smem_u32(&sm.k_full[g & 1]), (g >> 1) & 1, kWaitCycles) && ok;
+            ok = bar_wait(smem_u32(&sm.k_full[g & 1]), (g >> 1) & 1, limit) && ok;
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             fence_after();
@@ -362,7 +395,7 @@ prompt_latent_kernel(const __grid_constant__ PromptParams p, const __grid_consta
                 const uint32_t at = __shfl_sync(0xffffffffu, (5 * g) & 7, 0), ph = (g >> 1) & 1;
                 const int last_t = j < nt[1] ? 1 : 0;       // the tile whose product is the last to use the block's values
                 bool have_k = false;
-                ok = bar_wait(smem_u32(&sm.v_full[g & 1]), ph, kWaitCycles) && ok;
+                ok = bar_wait(smem_u32(&sm.v_full[g & 1]), ph, limit) && ok;
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 if (valid & 15) {                  // rows behind the last key in its step of 16: whatever they hold counts as zero
@@ -378,15 +411,15 @@ prompt_latent_kernel(const __grid_constant__ PromptParams p, const __grid_consta
                 for (int t = 0; t < 2; t++) {
                     if (j < nt[t]) {
                         if (j == 0) {              // the item before has been read out of O
-                            if (oc[t] > 0) ok = bar_wait(smem_u32(&sm.o_free[t]), (oc[t] - 1) & 1, kWaitCycles) && ok;
+                            if (oc[t] > 0) ok = bar_wait(smem_u32(&sm.o_free[t]), (oc[t] - 1) & 1, limit) && ok;
                             oc[t]++;
                         }
-                        ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.p_half[t]), pc[t] & 1, kWaitCycles) && ok);
+                        ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.p_half[t]), pc[t] & 1, limit) && ok);
                         if (!ok) break;
                         fence_after();
                         values(t, at + 3, j == 0, 0, steps);
                         if (t == last_t && mine) commit(smem_u32(&sm.v_half[g & 1]));
-                        ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.p_full[t]), pc[t] & 1, kWaitCycles));
+                        ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.p_full[t]), pc[t] & 1, limit));
                         if (!ok) break;
                         pc[t]++;
                         fence_after();
@@ -398,7 +431,7 @@ prompt_latent_kernel(const __grid_constant__ PromptParams p, const __grid_consta
                     }
                     if (j + 1 < nt[t]) {
                         if (!have_k) {
-                            ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.k_full[(g + 1) & 1]), ((g + 1) >> 1) & 1, kWaitCycles));
+                            ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.k_full[(g + 1) & 1]), ((g + 1) >> 1) & 1, limit));
                             if (!ok) break;
                             fence_after();
                             have_k = true;
@@ -416,7 +449,7 @@ prompt_latent_kernel(const __grid_constant__ PromptParams p, const __grid_consta
         }
         if (!ok) {                                 // gave up: the products in flight end before tensor memory is freed
             if (mine) commit(smem_u32(&sm.drain));
-            bar_wait(smem_u32(&sm.drain), 0, kWaitCycles);
+            bar_wait(smem_u32(&sm.drain), 0, limit);
         }
         __syncwarp();
     }
@@ -429,24 +462,20 @@ prompt_latent_kernel(const __grid_constant__ PromptParams p, const __grid_consta
                        pv_done = smem_u32(&sm.pv_done[t]);
         const int row_in = t * kTileQ + (warp & 3) * 32 + lane;
         Item it;
+        it.block = -1;
         float m = -INFINITY, l = 0.0f;
         bool none = true;                          // no keys here
-        // a wait ran out (never expected): the row's result says so
-        auto spoil = [&](const Item &at, int i) {
-            if (i >= at.nq) return;
-            const size_t row = (size_t)(at.q0 + i) * p.n_heads + at.head;
-            for (int d = 0; d < kV; d++) p.out[row * kV + d] = __ushort_as_bfloat16((unsigned short)0x7FC0);
-            if (p.lse) p.lse[row] = __int_as_float(0x7FC00000);
-        };
         uint32_t sc = 0, ic = 0;                   // blocks of this tile so far (S, P and P V alike), items with any
-        for (uint32_t n = 0; next_item(n, it); n++) {
+        uint32_t n = 0, begun = 0;                 // the item at hand, items read so far
+        for (; next_item(n, it); n++) {
+            begun = n + 1;
             const Part in = part_of(it, part, kSplit);
             const int nb = in.n[t], i = it.block * kBlockQ + row_in;
             const int vis = i < it.nq ? visible(it, i) : 0;
             m = -INFINITY;
             l = 0.0f;
             for (int j = 0; j < nb; j++, sc++) {
-                ok = bar_wait(s_full, sc & 1, ok ? kWaitCycles : 0) && ok;
+                ok = bar_wait(s_full, sc & 1, limit);
                 if (!__all_sync(0xffffffffu, ok)) break;
                 fence_after();
                 float x[128];
@@ -517,18 +546,15 @@ prompt_latent_kernel(const __grid_constant__ PromptParams p, const __grid_consta
                 l += l0 + l1;
             }
             if constexpr (kSplit > 1) {            // one item: its parts are joined below
-                if (nb > 0 && ok) ok = bar_wait(pv_done, 0, kWaitCycles);
+                if (nb > 0 && ok) ok = bar_wait(pv_done, 0, limit);
                 none = nb == 0;
-                item = it;
                 break;
             }
-            if (!__all_sync(0xffffffffu, ok)) { spoil(it, i); break; }
             // ---- the row's result
-            if (nb > 0) {
-                ok = bar_wait(pv_done, ic++ & 1, kWaitCycles);
-                if (!__all_sync(0xffffffffu, ok)) { spoil(it, i); break; }
-                fence_after();
-            }
+            ok = __all_sync(0xffffffffu, ok);
+            if (ok && nb > 0) ok = __all_sync(0xffffffffu, bar_wait(pv_done, ic++ & 1, limit));
+            if (!ok) break;
+            fence_after();
             const size_t row = (size_t)(it.q0 + i) * p.n_heads + it.head;
             const float inv = vis > 0 ? 1.0f / l : 0.0f;
 #pragma unroll
@@ -561,14 +587,16 @@ prompt_latent_kernel(const __grid_constant__ PromptParams p, const __grid_consta
                 if (lane == 0) bar_arrive(smem_u32(&sm.o_free[t]));
             }
         }
-        if constexpr (kSplit > 1) {
+        if constexpr (kSplit == 1) {
+            if (!ok) give_up(p, sm, n, begun, row_in, lane);
+        } else {
             // All products of this CTA are done, so that nothing reads or fills its tiles any more: [dim][query] over them.
             const bool good = !group_any(1, 2 * kTileQ, !ok);
             fence_after();
             sm.m[row_in] = good ? m : __int_as_float(0x7FC00000);
             sm.l[row_in] = l;
             float *o = reinterpret_cast<float *>(sm.q);
-            if (good && item.block >= 0)
+            if (good && it.block >= 0)
 #pragma unroll
                 for (int c = 0; c < 8; c++) {
                     uint32_t r[16];
@@ -588,6 +616,7 @@ prompt_latent_kernel(const __grid_constant__ PromptParams p, const __grid_consta
     fence_after();
     if (warp == 8) tmem_free(tmem, 512);
     if constexpr (kSplit > 1) {
+        const Item item = sm.item[0];              // (from here and not from a wait that may have run out)
         // Each CTA joins the parts of 256 / kSplit queries, a thread 128 / kSplit dims of one, in the order of the parts.
         constexpr int kRows = kBlockQ / kSplit, kDims = kV / kSplit;
         const int r = part * kRows + tid % kRows, d0 = tid / kRows * kDims, i = item.block * kBlockQ + r;
@@ -711,6 +740,11 @@ int split_of(int n_seqs, int total_q, int total_k, int n_heads, int dev) {
 
 }  // namespace
 
+void set_prompt_wait(long long limit_cycles, uint32_t surplus_bytes) {
+    g_wait_cycles = limit_cycles;
+    g_surplus = surplus_bytes;
+}
+
 pask_status_t launch_prompt_latent(int n_seqs, int total_q, int total_k, int n_heads, const int32_t *cu_q, const int32_t *cu_k,
                                    const void *q, const void *kv, const void *k_rope, int rope_stride, float scale, void *out,
                                    float *lse, cudaStream_t stream) {
@@ -735,7 +769,8 @@ pask_status_t launch_prompt_latent(int n_seqs, int total_q, int total_k, int n_h
         return PASK_ERR_CUDA;
     const long long items = ((long long)total_q / kBlockQ + n_seqs) * n_heads;
     if (items > 0x7fffffffLL) return PASK_ERR_INVALID_ARG;
-    const PromptParams p{n_seqs, total_q, total_k, n_heads, cu_q, cu_k, scale * 1.4426950408889634f, static_cast<__nv_bfloat16 *>(out), lse};
+    const PromptParams p{n_seqs, total_q, total_k, n_heads, cu_q, cu_k, scale * 1.4426950408889634f, g_surplus.load(),
+                         static_cast<__nv_bfloat16 *>(out), lse, (uint32_t)(g_wait_cycles.load() >> 10)};
     const int split = split_of(n_seqs, total_q, total_k, n_heads, dev);
     if (items * split > 0x7fffffffLL) return PASK_ERR_INVALID_ARG;
     const auto fn = split == 8 ? launch<8> : split == 4 ? launch<4> : split == 2 ? launch<2> : launch<1>;

@@ -126,3 +126,41 @@ def test_finite_values_stay_finite(pask, bits):
     out, lse = b.decode(0, [2], torch.zeros((1, 16, 576), dtype=torch.bfloat16))
     assert torch.equal(out[0].cpu(), want[-1, :512].expand(16, 512)) and bool((lse == 0).all())
     assert b.status() == 0
+
+
+# ------------------------------------------------------------------------------------------- prompts: waits that run out
+
+# the first shape has more blocks of queries than SMs (a CTA that gives up has already accepted its next block); the others
+# split the keys of a block over a cluster, of two to eight CTAs, some parts without a key
+@pytest.mark.parametrize("heads,nq,nk", [(16, [256] * 40, [256 - 6 * i for i in range(40)]), (24, [512], [2100]), (30, [200], [2000]),
+                                         (16, [200], [2000]), (5, [3], [6000]), (6, [300, 40, 2], [280, 900, 1])])
+def test_prompt_wait_that_runs_out_leaves_nan(pask, heads, nq, nk):
+    g = torch.Generator().manual_seed(70)
+    tq, tk = sum(nq) + 2, sum(nk)
+    q, kv, rope = normal(g, tq, heads, 192).to(D), normal(g, tk, heads, 256).to(D), normal(g, tk, 64).to(D)
+    cq, ck = (i32([0] + torch.tensor(n).cumsum(0).tolist()) for n in (nq, nk))
+
+    def run():
+        out, lse = torch.full((tq, heads, 128), 7.0, dtype=torch.bfloat16, device=D), torch.full((tq, heads), 7.0, device=D)
+        t0, t1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        t0.record()
+        pask.pask_prompt_attention_latent(cq, ck, q, kv, rope, SCALE, out, lse)
+        t1.record()
+        torch.cuda.synchronize()
+        assert t0.elapsed_time(t1) < 1000.0
+        return out, lse
+
+    want, want_l = run()
+    assert not bool(torch.isnan(want).any())
+    pask.pask_debug_set_prompt_wait(1_000_000, 16)
+    try:
+        got, got_l = run()
+    finally:
+        pask.pask_debug_set_prompt_wait()
+    nan = torch.isnan(got).all(-1) & torch.isnan(got_l)
+    right = (got == want).all(-1) & (got_l == want_l)
+    assert bool((nan | right)[:-2].all()), "neither finished nor marked"
+    assert bool(nan.any()) and bool(right[:-2].any())
+    assert bool((got[-2:] == 7.0).all()) and bool((got_l[-2:] == 7.0).all())                 # rows of no sequence
+    again, again_l = run()
+    assert torch.equal(again, want) and torch.equal(again_l, want_l)
