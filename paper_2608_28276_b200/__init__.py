@@ -401,6 +401,8 @@ def pask_decode_attention_latent(cache: int, layer: int, seq_ids, q, scale: floa
           _arg(w, "out", out, torch.bfloat16, dev, (n, heads, LATENT_VALUE_DIM)),
           None if lse is None else _arg(w, "lse", lse, torch.float32, dev, (n, heads)),
           _arg(w, "workspace", workspace, workspace.dtype, dev, workspace.shape), ws_bytes)
+    if stream is not None:                         # a workspace the caller drops at once is not handed out again while the call runs
+        workspace.record_stream(stream)
 
 
 def pask_prompt_attention_latent(cu_q, cu_k, q, kv, k_rope, scale: float, out, lse=None, stream=None):
@@ -548,6 +550,7 @@ class Cache:
         self._ws = None
 
     def workspace(self, n_seqs: int):
+        """The cache's one workspace, for all its calls in turn; calls that may overlap on the GPU need buffers of their own."""
         need = pask_workspace_bytes(self.handle, n_seqs)
         if self._ws is None or self._ws.numel() < need:
             self._ws = torch.empty(need, dtype=torch.uint8, device=self.meta.device)
@@ -576,3 +579,7 @@ class LatentCache(Cache):
         with torch.cuda.device(device):
             super().__init__(blob, n_layers, n_q, 1, max_seqs, max_tokens_per_seq, max_append_tokens, pool_high_pages, pool_low_pages,
                              device=device, low_bits=low_bits, head_dim=LATENT_DIM)
+
+    def workspace(self, n_seqs: int):
+        """A workspace for pask_decode_attention_latent, another one for each who asks: calls that may overlap need one each."""
+        return torch.empty(pask_workspace_bytes(self.handle, n_seqs), dtype=torch.uint8, device=self.meta.device)

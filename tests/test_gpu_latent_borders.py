@@ -164,3 +164,61 @@ def test_prompt_wait_that_runs_out_leaves_nan(pask, heads, nq, nk):
     assert bool((got[-2:] == 7.0).all()) and bool((got_l[-2:] == 7.0).all())                 # rows of no sequence
     again, again_l = run()
     assert torch.equal(again, want) and torch.equal(again_l, want_l)
+
+
+# ------------------------------------------------------------------------------------------- workspaces and streams
+
+def test_workspaces_are_not_shared(pask):
+    b = Both(pask, heads=40)
+    ws = [b.gpu.workspace(1) for _ in range(3)]
+    assert len({w.data_ptr() for w in ws}) == 3 and all(w.numel() >= pask.pask_workspace_bytes(b.h, 1) for w in ws)
+
+
+def test_two_streams_with_a_workspace_each(pask):
+    g = torch.Generator().manual_seed(80)
+    b = Both(pask, heads=40)
+    for s, n in ((0, 1900), (1, 1700)):
+        b.append(0, [s], [normal(g, n, 576)], [tags_of(g, n)])
+    ids, q = [i32([0, 1]), i32([1])], [normal(g, 2, 40, 576).to(D), normal(g, 1, 40, 576).to(D)]
+    ws = [b.gpu.workspace(n.numel()) for n in ids]
+    assert ws[0].data_ptr() != ws[1].data_ptr()
+    rounds = 30
+    out = [[torch.zeros((n.numel(), 40, 512), dtype=torch.bfloat16, device=D) for _ in range(rounds + 1)] for n in ids]
+    lse = [[torch.zeros((n.numel(), 40), device=D) for _ in range(rounds + 1)] for n in ids]
+    for i in (0, 1):
+        pask.pask_decode_attention_latent(b.h, 0, ids[i], q[i], SCALE, out[i][rounds], lse[i][rounds], ws[i])
+        rows = b.ref.rows(0, 1)
+        R.check(out[i][rounds][-1], lse[i][rounds][-1], R.attend(q[i][-1].cpu(), rows[None], rows[None, :, :512], SCALE))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in ids]
+    for r in range(rounds):
+        for i, st in enumerate(streams):
+            with torch.cuda.stream(st):
+                pask.pask_decode_attention_latent(b.h, 0, ids[i], q[i], SCALE, out[i][r], lse[i][r], ws[i])
+    torch.cuda.synchronize()
+    for i in (0, 1):
+        for r in range(rounds):
+            assert torch.equal(out[i][r], out[i][rounds]) and torch.equal(lse[i][r], lse[i][rounds]), (i, r)
+
+
+def test_a_workspace_dropped_at_once_outlives_the_call(pask):
+    g = torch.Generator().manual_seed(81)
+    b = Both(pask, heads=16, n_layers=1)
+    b.append(0, [0], [normal(g, 1500, 576)], [tags_of(g, 1500)])
+    q = normal(g, 1, 16, 576).to(D)
+    want, want_l = b.decode(0, [0], q)
+    out, lse, st = torch.empty_like(want), torch.empty_like(want_l), torch.cuda.Stream()
+    n = pask.pask_workspace_bytes(b.h, 1)
+    st.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(st):
+        torch.cuda._sleep(20_000_000)                                                          # the call waits its turn there
+    ids = i32([0])
+    torch.cuda.current_stream().synchronize()
+    lent = b.gpu.workspace(1)
+    at = lent.data_ptr()
+    pask.pask_decode_attention_latent(b.h, 0, ids, q, SCALE, out, lse, lent, stream=st)
+    del lent
+    others = [torch.empty(n, dtype=torch.uint8, device=D) for _ in range(4)]
+    assert all(t.data_ptr() != at for t in others)
+    st.synchronize()
+    assert torch.equal(out, want) and torch.equal(lse, want_l)
