@@ -174,6 +174,18 @@ def test_workspaces_are_not_shared(pask):
     assert len({w.data_ptr() for w in ws}) == 3 and all(w.numel() >= pask.pask_workspace_bytes(b.h, 1) for w in ws)
 
 
+def test_decode_refuses_a_workspace_that_is_too_small(pask):
+    b = Both(pask, heads=16)
+    q, out = torch.zeros((2, 16, 576), dtype=torch.bfloat16, device=D), torch.full((2, 16, 512), 7.0, dtype=torch.bfloat16, device=D)
+    ws = b.gpu.workspace(2)
+    for n in (256, ws.numel() - 1):
+        with pytest.raises(pask.PaskError) as e:
+            pask.pask_decode_attention_latent(b.h, 0, i32([0, 1]), q, SCALE, out, None, ws[:n])
+        assert e.value.status == pask.ERR_WORKSPACE
+    torch.cuda.synchronize()
+    assert bool((out == 7.0).all())
+
+
 def test_two_streams_with_a_workspace_each(pask):
     g = torch.Generator().manual_seed(80)
     b = Both(pask, heads=40)
@@ -222,3 +234,47 @@ def test_a_workspace_dropped_at_once_outlives_the_call(pask):
     assert all(t.data_ptr() != at for t in others)
     st.synchronize()
     assert torch.equal(out, want) and torch.equal(lse, want_l)
+
+
+# ------------------------------------------------------------------------------------------- every row counts
+
+# Gaussian rows against a bound for the whole sum do not show a row that is left out among thousands: each row in turn gets a query
+# along itself, whose weight it then has nearly to itself.
+@pytest.mark.parametrize("mix", [(3, 0, 2), (9, 0, 1), (1, 1, 1), (1, 0, 0), (0, 0, 1)])
+@pytest.mark.parametrize("ctas", [148, 5])
+def test_decode_finds_every_row(pask, mix, ctas):
+    g = torch.Generator().manual_seed(90 + sum(mix))
+    lut = [[2]] * mix[0] + [[0]] * mix[1] + [[1]] * mix[2]
+    b = Both(pask, heads=40, max_seqs=2, n_layers=1, lut=lut, max_tokens=6000, pages=800)
+    for s, n in ((0, 5201), (1, 77)):
+        b.append(0, [s], [normal(g, n, 576)], [tags_of(g, n, len(lut))])
+    pask.pask_debug_set_attention_ctas(b.h, ctas)
+    for s in (0, 1):
+        rows = b.ref.rows(0, s)
+        m = rows.shape[0]
+        n = (m + 39) // 40
+        q = rows[torch.arange(40 * n).clamp_max(m - 1)].view(n, 40, 576)
+        dev = rows.to(D)
+        out, lse = b.decode(0, [s] * n, q)
+        for i in range(n):
+            ref = [t.cpu() for t in R.attend(q[i].to(D), dev[None], dev[None, :, :512], SCALE)]
+            R.check(out[i], lse[i], ref, f"rows from {40 * i}")
+            # the tolerance sees the row: its weight is more than nine tenths, and it is far longer than the bound
+            own = rows[40 * i:40 * i + 40].double()[:, :512]
+            assert bool((own.abs().amax(-1) > 4 * ref[2][:own.shape[0]].amax(-1)).all())
+    assert b.status() == 0
+
+
+@pytest.mark.parametrize("heads,nq,nk", [(2, 40, 3001), (40, 300, 1500), (3, 700, 700)])
+def test_prompt_finds_every_key(pask, heads, nq, nk):
+    # the same for prompts: query t of head h looks along key (t * heads + h) * step, whichever it can see
+    g = torch.Generator().manual_seed(95)
+    kv, rope = normal(g, nk, heads, 256), normal(g, nk, 64)
+    first = nk - nq
+    at = (torch.arange(nq)[:, None] * heads + torch.arange(heads)[None, :]) * 7 % nk
+    at = torch.minimum(at, first + torch.arange(nq)[:, None])
+    q = torch.cat([kv[at, torch.arange(heads)[None, :], :128], rope[at]], -1)
+    out, lse = torch.empty((nq, heads, 128), dtype=torch.bfloat16, device=D), torch.empty((nq, heads), device=D)
+    pask.pask_prompt_attention_latent(i32([0, nq]), i32([0, nk]), q.to(D), kv.to(D), rope.to(D), 2 * SCALE, out, lse)
+    k = torch.cat([kv[:, :, :128], rope[:, None].expand(-1, heads, -1)], -1).transpose(0, 1)
+    R.check(out, lse, R.attend(q, k, kv[:, :, 128:].transpose(0, 1), 2 * SCALE, torch.arange(nq) + 1 + first), "needles")
