@@ -252,8 +252,8 @@ constexpr int kTile = 64, kTilePages = 4;
 constexpr int kTileBytes = kTilePages * kLatentHighPageBytes;      // 73728
 constexpr int kDecThreads = 512, kFillThreads = kPageTokens * kLatentGroups;      // 288: nine warps
 constexpr uint32_t kMaxSlots = 1024;
-enum : uint32_t { kInfoFirst = 1, kInfoLast = 2, kInfoWhole = 4, kInfoFinal = 8 };   // first, last tile of a sequence's part; the part
-                                                   // is the whole sequence; last tile of the share
+// first, last tile of a sequence's part; the part is the whole sequence; last tile of the share; the sequence began in an earlier one
+enum : uint32_t { kInfoFirst = 1, kInfoLast = 2, kInfoWhole = 4, kInfoFinal = 8, kInfoGoesOn = 16 };
 constexpr float kLazy = 8.0f;                      // log2 of how far a score may exceed the reference maximum
 
 struct DecParams {
@@ -265,10 +265,11 @@ struct DecParams {
     float scale_log2;
     __nv_bfloat16 *out;
     float *lse;
-    uint4 *meta;                                   // [n_seqs + 1] per sequence {tiles before it, its tiles, first share, end of its
-                                                   // shares}; behind them {tiles of all, shares in use}
-    float2 *part_ml;                               // [slots + n_seqs][n_q] (reference maximum in log2 units, sum)
-    float *part_o;                                 // [slots + n_seqs][n_q][512]
+    uint4 *meta;                                   // [n_seqs] {tiles before it, its tiles, first share, end of its shares}
+    // A share leaves at most two partial results, those of its first sequence (if that began in an earlier share) and of its
+    // last: part 2 share, and 2 share + 1.
+    float2 *part_ml;                               // [2 slots][n_q] (reference maximum in log2 units, sum)
+    float *part_o;                                 // [2 slots][n_q][512]
     long long wait_cycles;
     uint32_t surplus;
     unsigned long long *span;
@@ -329,6 +330,7 @@ struct TileWalk {
     __device__ __forceinline__ uint32_t pages() const { return (valid() + kPageTokens - 1) / kPageTokens; }
     __device__ __forceinline__ bool first() const { return v == v0; }
     __device__ __forceinline__ bool last() const { return v + 1 == v1; }
+    __device__ __forceinline__ bool goes_on() const { return v0 > 0; }
     __device__ __forceinline__ bool whole() const { return v0 == 0 && v1 == n; }
     // where the tile's page p lies, from its id (read a tile before it is looked at); an id the pools cannot hold is never
     // dereferenced
@@ -447,7 +449,6 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
         base += tiles[r];
     }
     if (blockIdx.x == 0) {                         // what the merge needs to know
-        if (tid == 0) p.meta[p.n_seqs] = make_uint4(total, slots, 0, 0);
         base = at;
 #pragma unroll
         for (int r = 0; r < kPer; r++) {
@@ -562,7 +563,8 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
             if (mine) {
                 commit(smem_u32(&ms.s_full[st]));
                 if (is_last) commit(smem_u32(&ms.q_empty));
-                const uint32_t flags = (is_first ? kInfoFirst : 0u) | (is_last ? kInfoLast : 0u) | (w.whole() ? kInfoWhole : 0u);
+                const uint32_t flags = (is_first ? kInfoFirst : 0u) | (is_last ? kInfoLast : 0u) | (w.whole() ? kInfoWhole : 0u) |
+                                       (w.goes_on() ? kInfoGoesOn : 0u);
                 ms.info[st] = make_uint4(w.valid(), flags | (after ? 0u : kInfoFinal), (uint32_t)w.s, 0);
                 bar_arrive(smem_u32(&ms.s_full[st]));
             }
@@ -827,7 +829,7 @@ decode_latent_kernel(const __grid_constant__ DecParams p) {
                         if (lane < 4) ms.red[warp][8 * j + hc + e] = a;
                     }
                 const bool whole = info.y & kInfoWhole;
-                const size_t row0 = (whole ? (size_t)info.z : (size_t)slot + info.z) * p.c.n_q + h0;
+                const size_t row0 = (size_t)(whole ? info.z : 2 * slot + (info.y & kInfoGoesOn ? 0u : 1u)) * p.c.n_q + h0;
                 group_sync(1, 128);
                 if (tid < kHeads) {
                     const float ls = (ms.red[0][tid] + ms.red[1][tid]) + (ms.red[2][tid] + ms.red[3][tid]);
@@ -907,25 +909,24 @@ decode_latent_merge(int n_seqs, int n_q, const uint4 *__restrict__ meta, const f
     }
     if (count == 1) return;                        // the share has written the result
     const int part = tid >> 7, d4 = tid & 127;
-    const size_t first = (size_t)(b0 + s) * n_q + h0;          // row of the first partial; the next one's is n_q behind
-    const float4 *src = reinterpret_cast<const float4 *>(part_o) + first * (kLatentValueDim / 4) + d4;
-    const size_t step = (size_t)n_q * (kLatentValueDim / 4);
+    auto row_of = [&](uint32_t k) { return (size_t)(2 * (b0 + k) + (k == 0 ? 1u : 0u)) * n_q + h0; };   // of the k-th partial
+    const float4 *src = reinterpret_cast<const float4 *>(part_o) + d4;
     float4 v[kRows][kAhead];
 #pragma unroll
     for (int r = 0; r < kRows; r++)
 #pragma unroll
         for (int k = 0; k < kAhead; k++) {
             v[r][k] = make_float4(0, 0, 0, 0);
-            if (r < rows && part + (uint32_t)k * kSplit < count) v[r][k] = src[r * (kLatentValueDim / 4) + (part + k * kSplit) * step];
+            if (r < rows && part + (uint32_t)k * kSplit < count) v[r][k] = src[(row_of(part + k * kSplit) + r) * (kLatentValueDim / 4)];
         }
     // weights: a warp per head
     for (int r = warp; r < rows; r += 4 * kSplit) {
         float top = -INFINITY, sum = 0.0f;
-        for (uint32_t k = lane; k < count; k += 32) top = fmaxf(top, part_ml[first + r + (size_t)k * n_q].x);
+        for (uint32_t k = lane; k < count; k += 32) top = fmaxf(top, part_ml[row_of(k) + r].x);
 #pragma unroll
         for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
         for (uint32_t k = lane; k < count; k += 32) {
-            const float2 ml = part_ml[first + r + (size_t)k * n_q];
+            const float2 ml = part_ml[row_of(k) + r];
             const float wgt = umma::ex2(ml.x - top);
             sum += wgt * ml.y;
             s_w[r][k] = ml.y == ml.y ? wgt : ml.y; // a NaN stays one
@@ -944,7 +945,7 @@ decode_latent_merge(int n_seqs, int n_q, const uint4 *__restrict__ meta, const f
         for (int k = 0; k < kAhead; k++)
             if (part + (uint32_t)k * kSplit < count) add(v[r][k], s_w[r][part + k * kSplit]);
 #pragma unroll 8
-        for (uint32_t k = part + kAhead * kSplit; k < count; k += kSplit) add(src[r * (kLatentValueDim / 4) + k * step], s_w[r][k]);
+        for (uint32_t k = part + kAhead * kSplit; k < count; k += kSplit) add(src[(row_of(k) + r) * (kLatentValueDim / 4)], s_w[r][k]);
         if (kSplit > 1) {
             if (part > 0) s_o[(part - 1) * 128 + d4] = acc;
             __syncthreads();
@@ -1005,8 +1006,8 @@ static size_t carve_latent(const pask_cache *c, int n_seqs, uint8_t *base, DecPa
     latent_shares(c, &groups, &heads, &slots);
     size_t off = 0;
     auto take = [&](size_t bytes) { const size_t at = off; off = (off + bytes + 255) / 256 * 256; return at; };
-    const size_t rows = ((size_t)slots + n_seqs) * c->desc.n_q_heads;
-    const size_t o_meta = take((size_t)(n_seqs + 1) * sizeof(uint4)), o_ml = take(rows * sizeof(float2)), o_o = take(rows * kLatentValueDim * sizeof(float));
+    const size_t rows = (size_t)2 * slots * c->desc.n_q_heads;
+    const size_t o_meta = take((size_t)n_seqs * sizeof(uint4)), o_ml = take(rows * sizeof(float2)), o_o = take(rows * kLatentValueDim * sizeof(float));
     if (p) {
         p->groups = groups;
         p->heads = heads;

@@ -278,3 +278,25 @@ def test_prompt_finds_every_key(pask, heads, nq, nk):
     pask.pask_prompt_attention_latent(i32([0, nq]), i32([0, nk]), q.to(D), kv.to(D), rope.to(D), 2 * SCALE, out, lse)
     k = torch.cat([kv[:, :, :128], rope[:, None].expand(-1, heads, -1)], -1).transpose(0, 1)
     R.check(out, lse, R.attend(q, k, kv[:, :, 128:].transpose(0, 1), 2 * SCALE, torch.arange(nq) + 1 + first), "needles")
+
+
+def test_workspace_does_not_grow_with_the_batch_and_holds_what_is_written(pask):
+    # two partial results a share at most; the bytes behind the workspace stay as they were in batches of every shape
+    g = torch.Generator().manual_seed(82)
+    b = Both(pask, heads=72, max_seqs=5, n_layers=1, lut=LUT3, pages=800)
+    lens = [1000, 1, 333, 90]
+    b.append(0, [0, 1, 3, 4], [normal(g, n, 576) for n in lens], [tags_of(g, n, 3) for n in lens])
+    for ctas in (148, 2, 6, 40):
+        pask.pask_debug_set_attention_ctas(b.h, ctas)
+        assert pask.pask_workspace_bytes(b.h, 1024) - pask.pask_workspace_bytes(b.h, 1) <= 1024 * 16
+        for seqs in ([0], [0, 0], [1, 0, 2, 3, 4], [1, 1, 0, 1, 0, 3] * 8, [4] * 60):
+            n = pask.pask_workspace_bytes(b.h, len(seqs))
+            room = torch.full((n + 65536,), 0xA5, dtype=torch.uint8, device=D)
+            q = normal(g, len(seqs), 72, 576)
+            out, lse = torch.empty((len(seqs), 72, 512), dtype=torch.bfloat16, device=D), torch.empty((len(seqs), 72), device=D)
+            pask.pask_decode_attention_latent(b.h, 0, i32(seqs), q.to(D), SCALE, out, lse, room[:n])
+            for i, s in enumerate(seqs):
+                rows = b.ref.rows(0, s)
+                R.check(out[i], lse[i], R.attend(q[i], rows[None], rows[None, :, :512], SCALE), f"{ctas} CTAs, {seqs}")
+            assert bool((room[n:] == 0xA5).all())
+    assert b.status() == 0
