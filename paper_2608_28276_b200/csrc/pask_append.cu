@@ -1306,8 +1306,8 @@ pask_status_t launch_append(pask_cache *c, int layer, int n_seqs, int total_toke
                                          fuse ? *fuse_ws : Workspace{});
         return e == cudaSuccess ? PASK_OK : PASK_ERR_CUDA;
     }
-    append_plan_kernel<<<n_seqs, kBulkThreads, 0, stream>>>(c->dev, layer, n_seqs, total_tokens, seq_ids, cu_tokens, tags,
-                                                           decided, actions_out);
+    const pask_status_t rc = launch_append_plan(c, layer, n_seqs, total_tokens, seq_ids, cu_tokens, tags, decided, actions_out, stream);
+    if (rc != PASK_OK) return rc;
     if (total_tokens > 0) {
         // at most one item per 16 tokens plus two partly filled pages per stream
         const long long bound = (long long)total_tokens / 16 + 4LL * n_seqs;
