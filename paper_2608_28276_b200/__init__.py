@@ -364,6 +364,11 @@ def _arg(where, name, t, dtype, dev, shape):
     return t.data_ptr()
 
 
+def _dim(t, k):
+    """Size of dimension k, 0 if there is none: what `_arg` then refuses."""
+    return t.shape[k] if t.dim() > k else 0
+
+
 def _call(where, fn, dev, stream, *args):
     """Issue a latent call on the tensors' device: on the given stream or that device's current one."""
     if dev < 0:
@@ -374,7 +379,7 @@ def _call(where, fn, dev, stream, *args):
 
 def pask_append_latent(cache: int, layer: int, seq_ids, cu_tokens, latent, tags, actions=None, actions_out=None, stream=None):
     """pask_append_kv for a latent cache: latent bf16 [total][576]; `actions` u8 [total][n_groups] from pask_decide or None."""
-    w, n, total, dev = "pask_append_latent", seq_ids.numel(), latent.shape[0], seq_ids.get_device()
+    w, n, total, dev = "pask_append_latent", seq_ids.numel(), _dim(latent, 0), seq_ids.get_device()
     groups = _latent_shape[cache][1] if cache in _latent_shape else 1
     _call(w, _lib.pask_append_latent, dev, stream, cache, layer, n, total, _arg(w, "seq_ids", seq_ids, torch.int32, dev, (n,)),
           _arg(w, "cu_tokens", cu_tokens, torch.int32, dev, (n + 1,)), _arg(w, "latent", latent, torch.bfloat16, dev, (total, LATENT_DIM)),
@@ -385,7 +390,7 @@ def pask_append_latent(cache: int, layer: int, seq_ids, cu_tokens, latent, tags,
 
 def pask_read_latent(cache: int, layer: int, seq_ids, cu_rows, rows_out, lens_out=None, stream=None):
     """The retained rows of each sequence as bf16, HIGH stream then LOW stream, into rows_out[cu_rows[i]:]."""
-    w, n, total, dev = "pask_read_latent", seq_ids.numel(), rows_out.shape[0], seq_ids.get_device()
+    w, n, total, dev = "pask_read_latent", seq_ids.numel(), _dim(rows_out, 0), seq_ids.get_device()
     _call(w, _lib.pask_read_latent, dev, stream, cache, layer, n, total, _arg(w, "seq_ids", seq_ids, torch.int32, dev, (n,)),
           _arg(w, "cu_rows", cu_rows, torch.int32, dev, (n + 1,)), _arg(w, "rows_out", rows_out, torch.bfloat16, dev, (total, LATENT_DIM)),
           None if lens_out is None else _arg(w, "lens_out", lens_out, torch.int32, dev, (n, 2)))
@@ -394,7 +399,7 @@ def pask_read_latent(cache: int, layer: int, seq_ids, cu_rows, rows_out, lens_ou
 def pask_decode_attention_latent(cache: int, layer: int, seq_ids, q, scale: float, out, lse, workspace, stream=None):
     """One new query per sequence over a latent cache: q bf16 [n][n_q][576], out bf16 [n][n_q][512], lse fp32 [n][n_q] or None."""
     w, n, dev = "pask_decode_attention_latent", seq_ids.numel(), seq_ids.get_device()
-    heads = _latent_shape[cache][0] if cache in _latent_shape else q.shape[1]
+    heads = _latent_shape[cache][0] if cache in _latent_shape else _dim(q, 1)
     ws_bytes = workspace.numel() * workspace.element_size()
     _call(w, _lib.pask_decode_attention_latent, dev, stream, cache, layer, n, _arg(w, "seq_ids", seq_ids, torch.int32, dev, (n,)),
           _arg(w, "q", q, torch.bfloat16, dev, (n, heads, LATENT_DIM)), scale,
@@ -410,7 +415,7 @@ def pask_prompt_attention_latent(cu_q, cu_k, q, kv, k_rope, scale: float, out, l
     q bf16 [total_q][h][192], kv bf16 [total_k][h][256], k_rope bf16 [total_k][64] (rows may be strided, as in
     latent[:, 512:]), out bf16 [total_q][h][128], lse fp32 [total_q][h] or None."""
     w, n, dev = "pask_prompt_attention_latent", cu_q.numel() - 1, cu_q.get_device()
-    tq, heads, tk = q.shape[0], q.shape[1], kv.shape[0]
+    tq, heads, tk = _dim(q, 0), _dim(q, 1), _dim(kv, 0)
     if k_rope.get_device() != dev or k_rope.dtype is not torch.bfloat16 or k_rope.shape != (tk, 64) or k_rope.stride(1) != 1:
         raise PaskError(ERR_INVALID_ARG, f"{w}: k_rope must be a torch.bfloat16 tensor [{tk}, 64] on cuda:{dev} with adjacent columns")
     _call(w, _lib.pask_prompt_attention_latent, dev, stream, n, tq, tk, heads, _arg(w, "cu_q", cu_q, torch.int32, dev, (n + 1,)),

@@ -23,3 +23,20 @@ def test_prompt_wait_limits(pask):
         assert e.value.status == pask.ERR_INVALID_ARG
     pask.pask_debug_set_prompt_wait(100_000, 65536)
     pask.pask_debug_set_prompt_wait()
+
+
+def test_tensors_of_another_rank_are_refused(pask):
+    # one dimension too few in each tensor whose sizes a call goes by
+    ids, cu, bf = torch.zeros(1, dtype=torch.int32), torch.zeros(2, dtype=torch.int32), dict(dtype=torch.bfloat16)
+    u8, ws = torch.zeros(1, dtype=torch.uint8), torch.zeros(256, dtype=torch.uint8)
+    row, q, kv, rope = torch.zeros((1, 576), **bf), torch.zeros((1, 2, 192), **bf), torch.zeros((1, 2, 256), **bf), torch.zeros((1, 64), **bf)
+    out = torch.zeros((1, 2, 128), **bf)
+    for call in (lambda: pask.pask_append_latent(0, 0, ids, cu, row[0, 0], u8), lambda: pask.pask_append_latent(0, 0, ids, cu, row[0], u8),
+                 lambda: pask.pask_read_latent(0, 0, ids, cu, row[0, 0]), lambda: pask.pask_decode_attention_latent(0, 0, ids, row[0], 1.0, out, None, ws),
+                 lambda: pask.pask_prompt_attention_latent(cu, cu, q[0, 0], kv, rope, 1.0, out),
+                 lambda: pask.pask_prompt_attention_latent(cu, cu, q[0, 0, 0], kv, rope, 1.0, out),
+                 lambda: pask.pask_prompt_attention_latent(cu, cu, q, kv[0, 0, 0], rope, 1.0, out),
+                 lambda: pask.pask_prompt_attention_latent(cu, cu, q, kv, rope[0], 1.0, out)):
+        with pytest.raises(pask.PaskError) as e:
+            call()
+        assert e.value.status == pask.ERR_INVALID_ARG
