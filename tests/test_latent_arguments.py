@@ -40,3 +40,13 @@ def test_tensors_of_another_rank_are_refused(pask):
         with pytest.raises(pask.PaskError) as e:
             call()
         assert e.value.status == pask.ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("stride", [2 ** 31, 2 ** 31 + 64, 2 ** 32 + 64])
+def test_rope_rows_further_apart_than_the_call_can_say_are_refused(pask, stride):
+    # the C call's stride is an int32: the lower half of a larger one is another stride (2^32 + 64: adjacent rows)
+    cu, bf = torch.zeros(2, dtype=torch.int32), dict(dtype=torch.bfloat16)
+    rope = torch.empty_strided((2, 64), (stride, 1), dtype=torch.bfloat16, device="meta")
+    with pytest.raises(pask.PaskError, match="k_rope") as e:
+        pask.pask_prompt_attention_latent(cu, cu, torch.zeros((2, 2, 192), **bf), torch.zeros((2, 2, 256), **bf), rope, 1.0, torch.zeros((2, 2, 128), **bf))
+    assert e.value.status == pask.ERR_INVALID_ARG
