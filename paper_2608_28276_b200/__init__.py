@@ -417,7 +417,7 @@ def pask_prompt_attention_latent(cu_q, cu_k, q, kv, k_rope, scale: float, out, l
     w, n, dev = "pask_prompt_attention_latent", cu_q.numel() - 1, cu_q.get_device()
     tq, heads, tk = _dim(q, 0), _dim(q, 1), _dim(kv, 0)
     if k_rope.get_device() != dev or k_rope.dtype is not torch.bfloat16 or k_rope.shape != (tk, 64) or k_rope.stride(1) != 1 or \
-            k_rope.stride(0) > 0x7FFFFFFF:
+            tk > 1 and k_rope.stride(0) > 0x7FFFFFFF:
         raise PaskError(ERR_INVALID_ARG, f"{w}: k_rope must be a torch.bfloat16 tensor [{tk}, 64] on cuda:{dev} with adjacent columns and "
                         "rows less than 2^31 elements apart")
     _call(w, _lib.pask_prompt_attention_latent, dev, stream, n, tq, tk, heads, _arg(w, "cu_q", cu_q, torch.int32, dev, (n + 1,)),

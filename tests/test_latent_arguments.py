@@ -50,3 +50,10 @@ def test_rope_rows_further_apart_than_the_call_can_say_are_refused(pask, stride)
     with pytest.raises(pask.PaskError, match="k_rope") as e:
         pask.pask_prompt_attention_latent(cu, cu, torch.zeros((2, 2, 192), **bf), torch.zeros((2, 2, 256), **bf), rope, 1.0, torch.zeros((2, 2, 128), **bf))
     assert e.value.status == pask.ERR_INVALID_ARG
+
+
+def test_the_stride_of_a_single_rope_row_does_not_matter(pask):
+    cu, bf = torch.zeros(2, dtype=torch.int32), dict(dtype=torch.bfloat16)
+    rope = torch.empty_strided((1, 64), (2 ** 40, 1), dtype=torch.bfloat16, device="meta")
+    with pytest.raises(pask.PaskError, match="CUDA device"):                                  # as far as a call without a GPU gets
+        pask.pask_prompt_attention_latent(cu, cu, torch.zeros((1, 2, 192), **bf), torch.zeros((1, 2, 256), **bf), rope, 1.0, torch.zeros((1, 2, 128), **bf))
