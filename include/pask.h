@@ -435,7 +435,8 @@ pask_status_t pask_decode_step_drain(pask_cache_t *cache);
  *   (zero if s is); the value it stands for is bf16(code * s), finite for finite x, and is what
  *   attention computes with.  (bf16 scales, where the other caches have fp16 ones: the value is an
  *   operand of a bf16 matrix product, and a bf16 product rounds it once, in any range.)
- * The calls run on the device the cache was created on (PASK_ERR_INVALID_ARG if another is current).
+ * What is launched for a latent cache -- these calls, pask_cache_reset, pask_seq_reset, pask_decide -- runs on the
+ * device the cache was created on (PASK_ERR_INVALID_ARG if another is current).
  */
 
 /* pask_append_latent -- pask_append_kv for a latent cache, or with `actions` != NULL
@@ -471,7 +472,7 @@ pask_status_t pask_read_latent(pask_cache_t *cache, int32_t layer, int32_t n_seq
  * the query, the value map is applied to the output by the caller): for head h
  *   p_j = softmax_j(scale * q_h . row_j),   out_h = sum_j p_j row_j[0:512].
  *   q         dev bf16 [n_seqs][n_q][576]
- *   scale     positive and finite (1 / sqrt of the unabsorbed head dim, commonly)
+ *   scale     positive, below 1e30 (1 / sqrt of the unabsorbed head dim, commonly)
  *   out       dev bf16 [n_seqs][n_q][512]
  *   lse       dev fp32 [n_seqs][n_q] or NULL: natural-log sum of exp of the scaled scores
  *   workspace dev, at least pask_workspace_bytes(cache, n_seqs) bytes, 256-byte aligned; contents undefined
@@ -501,7 +502,7 @@ pask_status_t pask_decode_attention_latent(pask_cache_t *cache, int32_t layer, i
  *   kv          dev bf16 [total_k][n_heads][256]: expanded key, value (the up-projection's output as it is)
  *   k_rope      dev bf16, row j at k_rope + j * rope_stride elements, 64 values (rope_stride >= 64, a multiple of 8:
  *               the last dims of latent rows can be used where they lie).  Must cover total_k rows
- *   scale       positive and finite
+ *   scale       positive, below 1e30
  *   out         dev bf16 [total_q][n_heads][128];  lse  dev fp32 [total_q][n_heads] or NULL
  * Values of a sequence's rows must be finite (and within what fp32 sums can hold, as for pask_decode_attention_latent); rows
  * outside every sequence may hold anything.  There is no cache whose status word could say that a bounded wait inside the

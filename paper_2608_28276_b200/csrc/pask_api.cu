@@ -335,8 +335,18 @@ void pask_cache_destroy(pask_cache_t *c) {
     delete c;
 }
 
+// calls that launch work on a latent cache run where the cache lives: a pointer of one device is no good on another
+static pask_status_t latent_device_ok(const pask_cache_t *c) {
+    if (!c->latent) return PASK_OK;
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess) return PASK_ERR_CUDA;
+    return dev == c->device ? PASK_OK : PASK_ERR_INVALID_ARG;
+}
+
 pask_status_t pask_cache_reset(pask_cache_t *c, pask_stream_t stream_v) {
     if (!c) return PASK_ERR_INVALID_ARG;
+    const pask_status_t ok = latent_device_ok(c);
+    if (ok != PASK_OK) return ok;
     cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
     uint8_t *m = static_cast<uint8_t *>(c->meta);
     for (auto &a : c->ahead) a.valid = false;
@@ -348,6 +358,8 @@ pask_status_t pask_cache_reset(pask_cache_t *c, pask_stream_t stream_v) {
 pask_status_t pask_seq_reset(pask_cache_t *c, int32_t seq, pask_stream_t stream) {
     if (!c) return PASK_ERR_INVALID_ARG;
     if (seq < 0 || seq >= c->desc.max_seqs) return PASK_ERR_BAD_SEQ;
+    const pask_status_t ok = latent_device_ok(c);
+    if (ok != PASK_OK) return ok;
     for (auto &a : c->ahead) a.valid = false;
     return launch_seq_reset(c, seq, static_cast<cudaStream_t>(stream));
 }
@@ -385,15 +397,12 @@ pask_status_t pask_append_kv_decided(pask_cache_t *c, int32_t layer, int32_t n_s
     return append_common(c, layer, n_seqs, total_tokens, seq_ids, cu_tokens, k, v, tags, actions, actions_out, stream);
 }
 
-// the calls on a latent cache run where the cache lives: a pointer of one device is no good on another
 static pask_status_t latent_cache_ok(const pask_cache_t *c, int32_t layer, int32_t n_seqs, const int32_t *seq_ids) {
     if (!c || !seq_ids) return PASK_ERR_INVALID_ARG;
     if (!c->latent) return PASK_ERR_UNSUPPORTED_SHAPE;
     if (layer < 0 || layer >= c->desc.n_layers || n_seqs < 1 || n_seqs > PASK_MAX_SEQS_PER_CALL) return PASK_ERR_INVALID_ARG;
     if ((uintptr_t)seq_ids & 3) return PASK_ERR_INVALID_ARG;
-    int dev = -1;
-    if (cudaGetDevice(&dev) != cudaSuccess) return PASK_ERR_CUDA;
-    return dev == c->device ? PASK_OK : PASK_ERR_INVALID_ARG;
+    return latent_device_ok(c);
 }
 
 pask_status_t pask_append_latent(pask_cache_t *c, int32_t layer, int32_t n_seqs, int32_t total_tokens, const int32_t *seq_ids,
@@ -456,6 +465,8 @@ pask_status_t pask_decide(pask_cache_t *c, int32_t n_seqs, int32_t total_tokens,
     if (n_seqs < 1 || n_seqs > PASK_MAX_SEQS_PER_CALL || n_seqs > c->desc.max_seqs) return PASK_ERR_INVALID_ARG;
     if (total_tokens < 0) return PASK_ERR_INVALID_ARG;
     if (((uintptr_t)seq_ids | (uintptr_t)cu_tokens) & 3 || ((uintptr_t)states & 1)) return PASK_ERR_INVALID_ARG;
+    const pask_status_t ok = latent_device_ok(c);
+    if (ok != PASK_OK) return ok;
     NvtxRange range("pask_decide");
     return launch_decide(c, n_seqs, total_tokens, seq_ids, cu_tokens, tags, states, actions_out,
                          static_cast<cudaStream_t>(stream));
