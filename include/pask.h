@@ -497,7 +497,9 @@ pask_status_t pask_decode_attention_latent(pask_cache_t *cache, int32_t layer, i
  * decides what persists.
  *   n_heads     1 .. PASK_LATENT_MAX_HEADS
  *   cu_q, cu_k  dev int32 [n_seqs+1], ascending within 0 .. total_q (total_k).  A sequence whose ranges are
- *               malformed is not written; so are rows of q outside every sequence
+ *               malformed is not written, nor are rows of q outside every sequence; the others are.  (Ranges of q that
+ *               overlap, as behind a descending one, may be more rows than the call has work for: any of theirs may be
+ *               left as they were)
  *   q           dev bf16 [total_q][n_heads][192]: 128 dims to meet the expanded key, 64 rotary dims
  *   kv          dev bf16 [total_k][n_heads][256]: expanded key, value (the up-projection's output as it is)
  *   k_rope      dev bf16, row j at k_rope + j * rope_stride elements, 64 values (rope_stride >= 64, a multiple of 8:
@@ -583,7 +585,7 @@ pask_status_t pask_debug_page_order(uint32_t pages_high, uint32_t pages_low, uin
 pask_status_t pask_debug_partition(int32_t n_seqs, const uint32_t *pages_high, const uint32_t *pages_low,
                                    int32_t n_ctas, uint32_t *ranges);
 /* Override the number of CTAs the decode-attention main kernel is launched with (default: two per
- * SM).  Any value >= 1 gives the same result up to summation order; tests use it to check that.
+ * SM; latent caches: one).  Any value >= 1 gives the same result up to summation order; tests use it to check that.
  * Workspaces must be sized (pask_workspace_bytes) after the change. */
 pask_status_t pask_debug_set_attention_ctas(pask_cache_t *cache, int32_t n_ctas);
 /* The device-side waits of the library are those of the decode-attention kernel for its bulk copies

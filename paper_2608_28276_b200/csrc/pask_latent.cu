@@ -243,11 +243,17 @@ read_latent_kernel(DevCache c, int layer, int n_seqs, int total_rows, const int3
 // the rescaling of O leaves the common path.  A share that covers a whole sequence writes its result; otherwise partial sums
 // go to the workspace and decode_latent_merge joins them in a fixed order: results do not depend on timing.
 //
-// HIGH tiles are bound by memory up to 32 heads (148 sequences of 2048 rows: 64 and 71 us, 5.4 and 4.9 TB/s) and by shared memory
-// at 64: 327 KB a tile (copy, X twice, Q, P), 2555 cycles at 128 B each of 4500.  LOW tiles are
-// bound by the fill, 2.2 us for 16 heads and 3.0 for 64: of 4070 cycles the codes' requests take 1250, four pages 2030.  With the
-// merge: 64 sequences of 2 to 8 thousand rows, 128 heads, all HIGH 161 us; 128 of 16 thousand tokens, 64 heads, a fifth HIGH and
-// 0.3 LOW at 4 bits 265 us; one of 1023 rows, 16 heads 11.2 us.
+// Rounding: S is fp32; a weight is rounded to bf16 once, as an operand of the product with bf16 rows (its sum is taken before),
+// which is off by half a step at most, 2^-8 of each weight, as the rounding of the result is.  A second product with what the
+// rounding left would add 768 cycles to the 1920 of a tile's products.
+//
+// HIGH tiles are bound by memory up to 32 heads (148 sequences of 2048 rows, 16 / 32 heads, the captured call replayed back to back,
+// merge included: 64 / 69 us, 5.5 / 5.1 TB/s; the call alone, L2 flushed: 81 / 85).  At 64 heads (82 us replayed; 128 heads in two
+// groups 148) some 4500 cycles a tile are the chain copy - S - softmax - O over two stages of a whole tile and one place for P;
+// shared memory's own bandwidth accounts for 2555 of them (327 KB a tile: copy, X twice, Q, P; 128 B a cycle).  LOW tiles are
+// bound by the fill, 2.2 us for 16 heads and 3.0 for 64: of 4070 cycles the codes' requests take 1250, four pages 2030.  Replayed /
+// called: 64 sequences of 2 to 8 thousand rows, 128 heads, all HIGH 159 / 175 us; 128 of 16 thousand tokens, 64 heads, a fifth HIGH
+// and 0.3 LOW at 4 bits 260 / 281; one of 1023 rows, 16 heads 12.4 / 11.4.
 constexpr int kTile = 64, kTilePages = 4;
 constexpr int kTileBytes = kTilePages * kLatentHighPageBytes;      // 73728
 constexpr int kDecThreads = 512, kFillThreads = kPageTokens * kLatentGroups;      // 288: nine warps

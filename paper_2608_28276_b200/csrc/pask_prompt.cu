@@ -21,8 +21,12 @@
 //
 // Measured: 4123 cycles for a block of 128 keys, 1.6 of the bound; the chain S - exponentials - P - P V of a tile is longer than
 // the other tile's products.  Two threads a query (16 softmax warps) took as long: 155 us against 150 for 4 x 500 queries
-// behind 3333 keys, 32 heads.  4 prompts of 4 to 8 thousand, 16 heads: 681 us, 1.2 PFLOP/s at the 1.6 GHz that the power limit
-// leaves.
+// behind 3333 keys, 32 heads (the captured call replayed back to back; called on its own, L2 flushed, 180).  4 prompts of 4 to 8
+// thousand, 16 heads: 750 to 820 us, replayed or called, 1.0 to 1.1 PFLOP/s at the clock that the power limit leaves (681 at
+// 1.6 GHz, in a short burst).
+//
+// Rounding: S, O and the sums are fp32; a weight is rounded to bf16 once (half a step, 2^-8 of it), as an operand of a product with
+// bf16 values.  What the rounding left would take a second P V, 1024 cycles more a block of keys.
 //
 // kSplit > 1: a cluster of kSplit CTAs shares an item, each a range of its key blocks; the unscaled results meet in shared
 // memory, each CTA joining the rows of 256 / kSplit queries (no workspace, a fixed order).  No stealing there.

@@ -122,7 +122,7 @@ __host__ __device__ constexpr uint32_t instr(int m, int n, bool a_mn, bool b_mn)
 // 16 steps of K.  Called by a whole warp, issued by the lane whose `mine` is set (elect_one): code that is uniform over the warp
 // keeps the descriptors in uniform registers, and a product costs 32 cycles of issue less than from a one-thread branch.
 // Measured cycles of one product, both operands in shared memory: 32 (M 64, N 64), 48 (M 128, N 64), 64 (M 128, N 128), 128 (M
-// 128, N 256) -- the larger of M N / 256 x 2 cycles of arithmetic (M 64 counts as 128) and (M + N) 32 bytes at 128 a cycle.
+// 128, N 256) -- the larger of M N / 256 cycles of arithmetic (M 64 counts as 128) and (M + N) 32 bytes at 128 a cycle.
 __device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add, bool mine) {
     asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
                  "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
