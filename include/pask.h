@@ -516,6 +516,67 @@ pask_status_t pask_prompt_attention_latent(int32_t n_seqs, int32_t total_q, int3
                                            float *lse, pask_stream_t stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * Rotary positions.  The caches hold keys with their positions in them (K after its rotation; the last 64 dims of a
+ * latent row), so that the order of what is retained does not matter: this is the step between a layer's projections and
+ * pask_prompt_attention / pask_append_kv / pask_decode_attention and the latent calls.
+ *
+ * pask_rotary_table -- the frequencies of the rot_dim / 2 pairs, as fractions of a turn a position in units of 2^-64 (rounded to
+ * nearest).  Pair i turns by f_i = base^(-2 i / rot_dim) radians a position; for contexts longer than the trained one:
+ *   PASK_ROTARY_LINEAR     f_i / factor
+ *   PASK_ROTARY_ROTATIONS  pairs that turn often within the trained context keep f_i, the others are divided: with
+ *                          r = context f_i / (2 pi), w = clamp((r - few) / (many - few), 0, 1):  w f_i + (1 - w) f_i / factor
+ *                          (Peng et al. 2023, arXiv 2309.00071, section 3.2)
+ *   PASK_ROTARY_INDEX      the same mixture, linear in the pair's index: w = 1 - clamp((i - lo) / (hi - lo), 0, 1) with
+ *                          lo = max(0, floor(d(many))), hi = min(rot_dim - 1, ceil(d(few))) (hi - lo at least 0.001), where
+ *                          d(r) = rot_dim ln(context / (2 pi r)) / (2 ln base) is the index with r rotations
+ * Host only, needs no GPU; the caller copies the table to the device and keeps it.
+ * Errors: PASK_ERR_INVALID_ARG (null, unknown scaling, base not in (1, inf), factor not positive; for the last two scalings
+ * context not positive or few, many not 0 < few < many), PASK_ERR_UNSUPPORTED_SHAPE (rot_dim odd or not in 2 .. PASK_ROTARY_MAX_DIM). */
+#define PASK_ROTARY_PLAIN 0
+#define PASK_ROTARY_LINEAR 1
+#define PASK_ROTARY_ROTATIONS 2
+#define PASK_ROTARY_INDEX 3
+#define PASK_ROTARY_MAX_DIM 256
+#define PASK_ROTARY_MAX_TENSORS 4
+#define PASK_TYPE_BF16 0
+#define PASK_TYPE_FP16 1
+#define PASK_TYPE_FP32 2
+typedef struct {
+    int32_t rot_dim;
+    int32_t scaling;
+    double base;
+    double factor;    /* not read by PASK_ROTARY_PLAIN */
+    double context;   /* trained context, few, many: read by the last two scalings only */
+    double few, many;
+} pask_rotary_desc_t;
+typedef struct {
+    const void *in;
+    void *out;                                     /* in itself, with the same strides, or memory that shares nothing with any `in` */
+    int64_t in_token_stride, in_head_stride;       /* elements; the dims of a head are adjacent */
+    int64_t out_token_stride, out_head_stride;
+    int32_t n_heads, head_dim;
+} pask_rotary_tensor_t;
+pask_status_t pask_rotary_table(const pask_rotary_desc_t *desc, uint64_t *table_host);
+/* pask_rotary -- rotates the first rot_dim dims of every head of up to PASK_ROTARY_MAX_TENSORS tensors [n_tokens][n_heads][head_dim]
+ * (queries and keys, commonly) in one launch: pair (a, b) at the angle x = position * f_i becomes
+ *   magnitude * (a cos x - b sin x, b cos x + a sin x).
+ * The other dims are copied.  Angles are right for every 32-bit position, negative ones too; products are fp32 and each result is
+ * rounded once.
+ *   positions     dev int32 [n_tokens]
+ *   table         dev uint64 [rot_dim / 2], 8-byte aligned
+ *   interleaved   0: pair i is dims i and i + rot_dim / 2;  1: dims 2 i and 2 i + 1
+ *   transpose     1: the angle -x, i.e. the transposed map: takes the gradient of the output to that of the input, and (for
+ *                 magnitude 1) a rotation back
+ *   dtype         PASK_TYPE_*, of all tensors; pointers aligned to it (16-byte aligned pointers, with strides, head dims and rot_dim / 2
+ *                 that are multiples of 16 bytes, are moved 16 bytes at a time)
+ *   tensors       host, n_tensors of them; head_dim rot_dim .. PASK_ROTARY_MAX_DIM
+ * Errors: PASK_ERR_INVALID_ARG (null, counts, types, alignment, a negative or an overlapping output stride, out == in with other
+ * strides), PASK_ERR_UNSUPPORTED_SHAPE (rot_dim, head_dim). */
+pask_status_t pask_rotary(int32_t n_tokens, const int32_t *positions, const uint64_t *table, int32_t rot_dim, int32_t interleaved,
+                          int32_t transpose, float magnitude, int32_t dtype, int32_t n_tensors,
+                          const pask_rotary_tensor_t *tensors, pask_stream_t stream);
+
+/* ---------------------------------------------------------------------------------------------
  * pask_distortion -- the inner term of the attention-output distortion (Eq. 4): for each row r
  * (one decode position of one sequence at one layer) max over query heads h of
  * || o_ref[r][h][:] - o_test[r][h][:] ||_2^2, where o_ref is the output of pask_decode_attention_full

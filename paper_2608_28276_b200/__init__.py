@@ -26,6 +26,8 @@ TAG_PROTECTED = 0xFF
 MAX_GROUPS = 8
 MAX_WINDOW = 256
 LATENT_DIM, LATENT_VALUE_DIM, LATENT_MAX_HEADS = 576, 512, 128
+ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_ROTATIONS, ROTARY_INDEX = 0, 1, 2, 3
+ROTARY_MAX_DIM, ROTARY_MAX_TENSORS = 256, 4
 
 EXPORTS = [
     "pask_load_policy", "pask_free_policy", "pask_policy_action", "pask_cache_sizes", "pask_cache_create",
@@ -33,6 +35,7 @@ EXPORTS = [
     "pask_append_kv_decided", "pask_append_attend", "pask_plan_area_bytes", "pask_plan_ahead", "pask_decode_step_ahead", "pask_decode_attention",
     "pask_decode_attention_full", "pask_decode_attention_static", "pask_workspace_bytes", "pask_decode_step_host", "pask_step_staging_bytes", "pask_step_packed_layout", "pask_decode_step_packed", "pask_decode_step_pipelined", "pask_decode_step_pipelined_ahead", "pask_decode_step_drain",
     "pask_append_latent", "pask_read_latent", "pask_decode_attention_latent", "pask_prompt_attention_latent",
+    "pask_rotary_table", "pask_rotary",
     "pask_budget_state", "pask_distortion", "pask_cache_set_timing_events", "pask_cache_set_timing_span", "pask_debug_stream_len", "pask_debug_dump_high",
     "pask_debug_dump_low", "pask_debug_pool_state", "pask_debug_ctrl_words", "pask_debug_page_order", "pask_debug_page_ids", "pask_debug_partition", "pask_debug_set_attention_ctas", "pask_debug_set_wait", "pask_debug_set_prompt_wait", "pask_debug_plan_order_span", "pask_status_string",
 ]
@@ -59,6 +62,16 @@ class BudgetState(C.Structure):
                 ("device_status", C.c_uint32), ("reserved", C.c_uint32),
                 ("decided_full_bytes", C.c_uint64), ("decided_retained_bytes", C.c_uint64),
                 ("n_demoted", C.c_uint64), ("n_promoted", C.c_uint64), ("n_floor_conflicts", C.c_uint64)]
+
+
+class RotaryDesc(C.Structure):
+    _fields_ = [("rot_dim", C.c_int32), ("scaling", C.c_int32), ("base", C.c_double), ("factor", C.c_double), ("context", C.c_double),
+                ("few", C.c_double), ("many", C.c_double)]
+
+
+class RotaryTensor(C.Structure):
+    _fields_ = [("src", C.c_void_p), ("dst", C.c_void_p), ("in_token_stride", C.c_int64), ("in_head_stride", C.c_int64),
+                ("out_token_stride", C.c_int64), ("out_head_stride", C.c_int64), ("n_heads", C.c_int32), ("head_dim", C.c_int32)]
 
 
 if not os.path.exists(LIB_PATH):
@@ -103,6 +116,8 @@ _lib.pask_append_latent.argtypes = [_vp, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _
 _lib.pask_read_latent.argtypes = [_vp, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp]
 _lib.pask_decode_attention_latent.argtypes = [_vp, _i32, _i32, _vp, _vp, C.c_float, _vp, _vp, _vp, _sz, _vp]
 _lib.pask_prompt_attention_latent.argtypes = [_i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _i32, C.c_float, _vp, _vp, _vp]
+_lib.pask_rotary_table.argtypes = [C.POINTER(RotaryDesc), _vp]
+_lib.pask_rotary.argtypes = [_i32, _vp, _vp, _i32, _i32, _i32, C.c_float, _i32, _i32, C.POINTER(RotaryTensor), _vp]
 _lib.pask_budget_state.argtypes = [_vp, _i32, C.POINTER(BudgetState), _vp]
 _lib.pask_cache_set_timing_events.argtypes = [_vp, _vp, _vp]
 _lib.pask_debug_stream_len.argtypes = [_vp, _i32, _i32, C.POINTER(C.c_uint32), C.POINTER(C.c_uint32), _vp]
@@ -425,6 +440,40 @@ def pask_prompt_attention_latent(cu_q, cu_k, q, kv, k_rope, scale: float, out, l
           _arg(w, "kv", kv, torch.bfloat16, dev, (tk, heads, 256)), k_rope.data_ptr(), k_rope.stride(0) if tk > 1 else 64, scale,
           _arg(w, "out", out, torch.bfloat16, dev, (tq, heads, 128)),
           None if lse is None else _arg(w, "lse", lse, torch.float32, dev, (tq, heads)))
+
+
+def pask_rotary_table(rot_dim: int, base: float = 10000.0, scaling: int = ROTARY_PLAIN, factor: float = 1.0, context: float = 0.0,
+                      few: float = 1.0, many: float = 32.0, device="cuda"):
+    """Frequencies of rot_dim / 2 pairs for pask_rotary, int64 [rot_dim / 2] (the bits of the C call's uint64) on `device`."""
+    out = torch.zeros(max(1, min(rot_dim, ROTARY_MAX_DIM) // 2), dtype=torch.int64)
+    desc = RotaryDesc(rot_dim, scaling, base, factor, context, few, many)
+    _check(_lib.pask_rotary_table(C.byref(desc), out.data_ptr()), "pask_rotary_table")
+    return out.to(device)
+
+
+_ROTARY_TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+_ROTARY_ARRAYS = [RotaryTensor * i for i in range(ROTARY_MAX_TENSORS + 1)]
+
+
+def pask_rotary(positions, table, tensors, interleaved: bool = False, transpose: bool = False, magnitude: float = 1.0, stream=None):
+    """Rotates the first 2 * len(table) dims of every head by its token's position: positions int32 [tokens], table from pask_rotary_table,
+    tensors a list of (input, output) [tokens][heads][dims], both of one type (bf16, fp16 or fp32), dims adjacent, other strides free;
+    output may be input itself."""
+    w, dev, n, pairs, count = "pask_rotary", positions.get_device(), positions.numel(), table.numel(), len(tensors)
+    if not 1 <= count <= ROTARY_MAX_TENSORS:
+        raise PaskError(ERR_INVALID_ARG, f"{w}: 1 to {ROTARY_MAX_TENSORS} tensors, got {count}")
+    dtype, descs = tensors[0][0].dtype, _ROTARY_ARRAYS[count]()
+    code = _ROTARY_TYPES.get(dtype)
+    for i, (x, y) in enumerate(tensors):
+        sx = x.shape
+        if code is None or x.dtype is not dtype or y.dtype is not dtype or x.get_device() != dev or y.get_device() != dev or len(sx) != 3 or \
+                y.shape != sx or sx[0] != n or sx[2] > 1 and (x.stride(2) != 1 or y.stride(2) != 1):
+            raise PaskError(ERR_INVALID_ARG, f"{w}: input and output must be bfloat16, float16 or float32 tensors [{n}, heads, dims] of one type on "
+                            f"cuda:{dev} with adjacent dims, got {x.dtype} {list(sx)} on {x.device} and {y.dtype} {list(y.shape)} on {y.device}")
+        ix, iy = x.stride(), y.stride()
+        descs[i] = (x.data_ptr(), y.data_ptr(), ix[0], ix[1], iy[0], iy[1], sx[1], sx[2])
+    _call(w, _lib.pask_rotary, dev, stream, n, _arg(w, "positions", positions, torch.int32, dev, (n,)),
+          _arg(w, "table", table, torch.int64, dev, (pairs,)), 2 * pairs, int(interleaved), int(transpose), magnitude, code, count, descs)
 
 
 def pask_budget_state(cache: int, seq: int, stream=None) -> BudgetState:

@@ -1,4 +1,5 @@
 // Host side of libpask: policy blobs, cache set-up, budget state, canonical dumps.
+#include <cmath>
 #include <cstring>
 #include <memory>
 #include <new>
@@ -456,6 +457,72 @@ pask_status_t pask_prompt_attention_latent(int32_t n_seqs, int32_t total_q, int3
     NvtxRange range("pask_prompt_attention_latent");
     return launch_prompt_latent(n_seqs, total_q, total_k, n_heads, cu_q, cu_k, q, kv, k_rope, rope_stride, scale, out, lse,
                                 static_cast<cudaStream_t>(stream));
+}
+
+pask_status_t pask_rotary_table(const pask_rotary_desc_t *d, uint64_t *table) {
+    if (!d || !table) return PASK_ERR_INVALID_ARG;
+    if (d->rot_dim < 2 || d->rot_dim > PASK_ROTARY_MAX_DIM || d->rot_dim % 2) return PASK_ERR_UNSUPPORTED_SHAPE;
+    if (d->scaling < PASK_ROTARY_PLAIN || d->scaling > PASK_ROTARY_INDEX) return PASK_ERR_INVALID_ARG;
+    if (!(d->base > 1.0) || !std::isfinite(d->base)) return PASK_ERR_INVALID_ARG;
+    if (d->scaling != PASK_ROTARY_PLAIN && (!(d->factor > 0.0) || !std::isfinite(d->factor))) return PASK_ERR_INVALID_ARG;
+    if (d->scaling >= PASK_ROTARY_ROTATIONS && (!(d->context > 0.0) || !std::isfinite(d->context) || !(d->few > 0.0) || !(d->many > d->few) ||
+                                                !std::isfinite(d->many)))
+        return PASK_ERR_INVALID_ARG;
+    // (long double: the table has more places than double)
+    const long double two_pi = 6.283185307179586476925286766559L, base = d->base;
+    double lo = 0.0, hi = 0.0;
+    if (d->scaling == PASK_ROTARY_INDEX) {
+        auto index = [&](double r) { return d->rot_dim * std::log(d->context / (r * (double)two_pi)) / (2.0 * std::log(d->base)); };
+        lo = std::fmax(0.0, std::floor(index(d->many)));
+        hi = std::fmin(d->rot_dim - 1.0, std::ceil(index(d->few)));
+    }
+    for (int i = 0; i < d->rot_dim / 2; i++) {
+        long double f = std::pow(base, -2.0L * i / d->rot_dim), keep = 1.0L;
+        if (d->scaling == PASK_ROTARY_LINEAR) keep = 0.0L;
+        if (d->scaling == PASK_ROTARY_ROTATIONS) keep = ((long double)d->context * f / two_pi - d->few) / ((long double)d->many - d->few);
+        if (d->scaling == PASK_ROTARY_INDEX) keep = 1.0L - (i - (long double)lo) / std::fmax(hi - lo, 0.001);
+        keep = std::fmin(1.0L, std::fmax(0.0L, keep));
+        if (d->scaling != PASK_ROTARY_PLAIN) f = f * keep + f / d->factor * (1.0L - keep);
+        const long double turn = f / two_pi, part = std::rint(std::ldexp(turn - std::floor(turn), 64));
+        table[i] = part >= std::ldexp(1.0L, 64) ? 0 : (uint64_t)part;
+    }
+    return PASK_OK;
+}
+
+pask_status_t pask_rotary(int32_t n_tokens, const int32_t *positions, const uint64_t *table, int32_t rot_dim, int32_t interleaved,
+                          int32_t transpose, float magnitude, int32_t dtype, int32_t n_tensors, const pask_rotary_tensor_t *tensors,
+                          pask_stream_t stream) {
+    if ((!positions && n_tokens > 0) || !table || !tensors || n_tokens < 0) return PASK_ERR_INVALID_ARG;
+    if (((uintptr_t)positions & 3) || ((uintptr_t)table & 7)) return PASK_ERR_INVALID_ARG;
+    if ((interleaved | transpose) & ~1 || !std::isfinite(magnitude)) return PASK_ERR_INVALID_ARG;
+    if (dtype < PASK_TYPE_BF16 || dtype > PASK_TYPE_FP32 || n_tensors < 1 || n_tensors > PASK_ROTARY_MAX_TENSORS) return PASK_ERR_INVALID_ARG;
+    if (rot_dim < 2 || rot_dim > PASK_ROTARY_MAX_DIM || rot_dim % 2) return PASK_ERR_UNSUPPORTED_SHAPE;
+    const uintptr_t align = dtype == PASK_TYPE_FP32 ? 3 : 1;
+    constexpr int64_t kMaxStride = (int64_t)1 << 40;
+    pask_rotary_tensor_t t[PASK_ROTARY_MAX_TENSORS];
+    int64_t heads = 0;
+    for (int i = 0; i < n_tensors; i++) {
+        pask_rotary_tensor_t &x = t[i] = tensors[i];
+        if (x.head_dim < rot_dim || x.head_dim > PASK_ROTARY_MAX_DIM) return PASK_ERR_UNSUPPORTED_SHAPE;
+        if (x.n_heads < 1 || (n_tokens > 0 && (!x.in || !x.out)) || (((uintptr_t)x.in | (uintptr_t)x.out) & align)) return PASK_ERR_INVALID_ARG;
+        for (const int64_t s : {x.in_token_stride, x.in_head_stride, x.out_token_stride, x.out_head_stride})
+            if (s < 0 || s > kMaxStride) return PASK_ERR_INVALID_ARG;
+        if (n_tokens <= 1) x.in_token_stride = x.out_token_stride = 0;         // a single one: no step is taken
+        if (x.n_heads == 1) x.in_head_stride = x.out_head_stride = 0;
+        if (x.in == x.out && (x.in_token_stride != x.out_token_stride || x.in_head_stride != x.out_head_stride)) return PASK_ERR_INVALID_ARG;
+        // no two heads of the output may share an element: one of the two strides steps over all of the other dimension
+        const __int128 over_heads = (__int128)(x.n_heads - 1) * x.out_head_stride + x.head_dim;
+        const __int128 over_tokens = (__int128)(n_tokens - 1) * x.out_token_stride + x.head_dim;
+        const bool heads_apart = x.n_heads == 1 || x.out_head_stride >= x.head_dim, tokens_apart = n_tokens <= 1 || x.out_token_stride >= x.head_dim;
+        if (!heads_apart || !tokens_apart) return PASK_ERR_INVALID_ARG;
+        if (x.n_heads > 1 && n_tokens > 1 && x.out_token_stride < over_heads && x.out_head_stride < over_tokens) return PASK_ERR_INVALID_ARG;
+        heads += x.n_heads;
+    }
+    if (heads > (1 << 20)) return PASK_ERR_UNSUPPORTED_SHAPE;
+    if (n_tokens == 0) return PASK_OK;
+    NvtxRange range("pask_rotary");
+    return launch_rotary(n_tokens, positions, table, rot_dim, interleaved != 0, transpose != 0, magnitude, dtype, n_tensors, t,
+                         static_cast<cudaStream_t>(stream));
 }
 
 pask_status_t pask_decide(pask_cache_t *c, int32_t n_seqs, int32_t total_tokens, const int32_t *seq_ids,

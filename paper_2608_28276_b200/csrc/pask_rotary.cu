@@ -1,0 +1,161 @@
+// pask_rotary: rotary positions.  Pair i of a token's head, (a, b), becomes m (a cos x - b sin x, b cos x + a sin x) at the angle
+// x = position times frequency i (the transpose: -x).
+//
+// Angles.  A frequency is kept as the fraction of a turn that a position turns it by, in units of 2^-64, and its product with the
+// position is taken modulo 2^64: whole turns fall away by themselves, so that the angle of any 32-bit position is right to 2^-33
+// of a turn (a product in fp32 would be off by 0.03 rad at position 500 thousand).  Half turns go to sincospi in fp32.
+//
+// Bound: memory, each value read and written once (rot dims of 128 and 40 heads: 20 KB a token).  A CTA works out the sines and
+// cosines of its tokens once, in shared memory, for all their heads; then a thread has V pairs of a head (two 16-byte loads and
+// stores), the heads of all tensors of the call one behind the other.  16-byte accesses need everything aligned to them; otherwise
+// a thread has one pair.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "pask_internal.h"
+
+namespace pask {
+
+namespace {
+
+constexpr int kThreads = 256, kMaxPairs = kRotaryMaxDim / 2, kMaxTokens = 8;
+
+struct RotaryParams {
+    pask_rotary_tensor_t t[kRotaryMaxTensors];
+    int first[kRotaryMaxTensors + 1];              // heads of the tensors before
+    int n_tensors, n_tokens, tokens;               // tokens: of a CTA
+    int rot, tails;                                // tails: most pieces of a head behind its rotated dims
+    const int32_t *positions;
+    const uint64_t *table;
+    float magnitude;
+    int transpose;
+};
+
+__device__ __forceinline__ float to_f(float x) { return x; }
+__device__ __forceinline__ float to_f(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ float to_f(__half x) { return __half2float(x); }
+template <typename T> __device__ __forceinline__ T from_f(float x);
+template <> __device__ __forceinline__ float from_f<float>(float x) { return x; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+template <> __device__ __forceinline__ __half from_f<__half>(float x) { return __float2half_rn(x); }
+
+// V values, 16 bytes of them or one
+template <typename T, int V>
+struct Piece {
+    T x[V];
+    __device__ __forceinline__ void load(const T *p) {
+        if constexpr (V > 1) *reinterpret_cast<uint4 *>(x) = *reinterpret_cast<const uint4 *>(p);
+        else x[0] = *p;
+    }
+    __device__ __forceinline__ void store(T *p) const {
+        if constexpr (V > 1) *reinterpret_cast<uint4 *>(p) = *reinterpret_cast<const uint4 *>(x);
+        else *p = x[0];
+    }
+};
+
+template <typename T, int V, bool kNeighbours>
+__global__ void __launch_bounds__(kThreads)
+rotary_kernel(const __grid_constant__ RotaryParams p) {
+    __shared__ float s_cos[kMaxTokens * kMaxPairs], s_sin[kMaxTokens * kMaxPairs];
+    const int tid = threadIdx.x, pairs = p.rot / 2;
+    pdl_launch_dependents();
+    pdl_wait();
+    const int t0 = blockIdx.x * p.tokens, n = min(p.tokens, p.n_tokens - t0);
+    for (int e = tid; e < n * pairs; e += kThreads) {
+        const int t = e / pairs;
+        const uint64_t turn = (uint64_t)(int64_t)p.positions[t0 + t] * p.table[e - t * pairs];
+        float s, c;
+        sincospif((float)(int32_t)(uint32_t)((turn + 0x80000000u) >> 32) * 0x1p-31f, &s, &c);
+        s_cos[e] = c * p.magnitude;
+        s_sin[e] = (p.transpose ? -s : s) * p.magnitude;
+    }
+    __syncthreads();
+    // A row is a head of a token; a thread has piece u of the rows r, r + rows, ...: pairs V u .. V u + V - 1, then what is not rotated
+    const int units = pairs / V, per_row = units + p.tails, rows = kThreads / per_row, heads = p.first[p.n_tensors];
+    const int u = tid % per_row;
+    int t = 0, h = tid / per_row;
+    if (h >= rows) return;
+    for (;; h += rows) {
+        while (h >= heads) { h -= heads; t++; }
+        if (t >= n) return;
+        int i = 0;
+        while (h >= p.first[i + 1]) i++;
+        const pask_rotary_tensor_t &x = p.t[i];
+        const T *in = static_cast<const T *>(x.in) + (int64_t)(t0 + t) * x.in_token_stride + (int64_t)(h - p.first[i]) * x.in_head_stride;
+        T *out = static_cast<T *>(x.out) + (int64_t)(t0 + t) * x.out_token_stride + (int64_t)(h - p.first[i]) * x.out_head_stride;
+        if (u >= units) {                          // not rotated: copied, unless it is there already
+            const int d = p.rot + (u - units) * V;
+            if (d < x.head_dim && in != out) {
+                Piece<T, V> y;
+                y.load(in + d);
+                y.store(out + d);
+            }
+            continue;
+        }
+        const int lo = kNeighbours ? 2 * V * u : V * u, hi = kNeighbours ? lo + V : lo + pairs;
+        Piece<T, V> a, b;
+        a.load(in + lo);
+        b.load(in + hi);
+        const float *cs = s_cos + t * pairs + u * V, *sn = s_sin + t * pairs + u * V;
+#pragma unroll
+        for (int e = 0; e < V; e++) {
+            T &first = kNeighbours ? (2 * e < V ? a.x[2 * e % V] : b.x[2 * e % V]) : a.x[e];
+            T &second = kNeighbours ? (2 * e + 1 < V ? a.x[(2 * e + 1) % V] : b.x[(2 * e + 1) % V]) : b.x[e];
+            const float f = to_f(first), s = to_f(second), c = cs[e], z = sn[e];
+            first = from_f<T>(f * c - s * z);
+            second = from_f<T>(s * c + f * z);
+        }
+        a.store(out + lo);
+        b.store(out + hi);
+    }
+}
+
+template <typename T>
+cudaError_t launch(RotaryParams &p, bool neighbours, cudaStream_t stream) {
+    constexpr int V = 16 / sizeof(T);
+    int tail = 0;
+    bool wide = p.rot % (2 * V) == 0;
+    for (int i = 0; i < p.n_tensors; i++) {
+        const pask_rotary_tensor_t &x = p.t[i];
+        tail = x.head_dim - p.rot > tail ? x.head_dim - p.rot : tail;
+        wide = wide && x.head_dim % V == 0 && (((uintptr_t)x.in | (uintptr_t)x.out) & 15) == 0 &&
+               (x.in_token_stride | x.in_head_stride | x.out_token_stride | x.out_head_stride) % V == 0;
+    }
+    const int v = wide ? V : 1;
+    p.tails = (tail + v - 1) / v;
+    // Tokens a CTA: several where there are enough of them to fill the GPU all the same, so that a thread has some four rows and
+    // the sines are worked out beside other CTAs' copies; one in small calls.
+    const int rows = kThreads / (p.rot / 2 / v + p.tails), heads = p.first[p.n_tensors];
+    p.tokens = 1;
+    while (p.tokens < kMaxTokens && p.tokens * heads < 4 * rows && p.n_tokens >= p.tokens * 2 * 148 * 4) p.tokens *= 2;
+    const dim3 grid((p.n_tokens + p.tokens - 1) / p.tokens);
+    if (wide)
+        return neighbours ? launch_pdl(rotary_kernel<T, V, true>, grid, dim3(kThreads), 0, stream, p)
+                          : launch_pdl(rotary_kernel<T, V, false>, grid, dim3(kThreads), 0, stream, p);
+    return neighbours ? launch_pdl(rotary_kernel<T, 1, true>, grid, dim3(kThreads), 0, stream, p)
+                      : launch_pdl(rotary_kernel<T, 1, false>, grid, dim3(kThreads), 0, stream, p);
+}
+
+}  // namespace
+
+pask_status_t launch_rotary(int n_tokens, const int32_t *positions, const uint64_t *table, int rot_dim, bool neighbours, bool transpose,
+                            float magnitude, int dtype, int n_tensors, const pask_rotary_tensor_t *tensors, cudaStream_t stream) {
+    RotaryParams p{};
+    for (int i = 0; i < n_tensors; i++) {
+        p.t[i] = tensors[i];
+        p.first[i + 1] = p.first[i] + tensors[i].n_heads;
+    }
+    p.n_tensors = n_tensors;
+    p.n_tokens = n_tokens;
+    p.rot = rot_dim;
+    p.positions = positions;
+    p.table = table;
+    p.magnitude = magnitude;
+    p.transpose = transpose ? 1 : 0;
+    const cudaError_t e = dtype == PASK_TYPE_BF16   ? launch<__nv_bfloat16>(p, neighbours, stream)
+                          : dtype == PASK_TYPE_FP16 ? launch<__half>(p, neighbours, stream)
+                                                    : launch<float>(p, neighbours, stream);
+    return e == cudaSuccess ? PASK_OK : PASK_ERR_CUDA;
+}
+
+}  // namespace pask
