@@ -516,6 +516,31 @@ pask_status_t pask_prompt_attention_latent(int32_t n_seqs, int32_t total_q, int3
                                            float *lse, pask_stream_t stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * pask_prompt_attention -- causal attention of the tokens of a ragged batch behind what the cache retains of their sequences at
+ * `layer`: whole prompts (nothing retained yet), chunks of a prompt, tokens that the grammar forces or a draft proposes.  Token t of
+ * a sequence sees all of the retained history, as pask_decode_attention would attend it at this moment (the protected window's
+ * last tokens in bf16 whatever their action), and the call's own tokens 0 .. t of that sequence, as given: call it before
+ * the append that persists them.  out = softmax(q K^T / sqrt(128)) V; query head h reads key / value head h / 4.
+ *   n_seqs      1 .. PASK_MAX_SEQS_PER_CALL
+ *   seq_ids     dev int32 [n_seqs]; a sequence may be named more than once (drafts of one history: none sees another)
+ *   cu_tokens   dev int32 [n_seqs+1]: the rows of each sequence's tokens, ascending within 0 .. total_tokens
+ *   q           dev bf16 [total_tokens][n_q][128], post-RoPE;  k, v  dev bf16 [total_tokens][n_kv][128], post-RoPE
+ *   out         dev bf16 [total_tokens][n_q][128]
+ *   lse         dev fp32 [total_tokens][n_q] or NULL: natural-log sum of exp of the scaled scores
+ *   workspace   dev, at least pask_prompt_workspace_bytes(cache, n_seqs, total_tokens) bytes, 256-byte aligned; contents undefined
+ *               afterwards.  Calls that may overlap on the GPU (two streams, two captured graphs replayed side by side) need one each.
+ * RETAIN-LOW values enter as bf16(code * scale), the operands of a bf16 product (pask_decode_attention computes with the unrounded
+ * product); softmax weights are rounded to bf16, scores and sums are fp32, each output is rounded once.  Values must be finite, and
+ * scores and sums within what fp32 holds; rows outside every sequence may hold anything and are left as they were.
+ * A sequence whose range is malformed is not written (sticky PASK_DEV_BAD_RAGGED); one whose id is out of range gets out = 0 and
+ * lse = -inf (PASK_DEV_BAD_SEQ); the others are computed.  A bounded wait that runs out: PASK_DEV_TIMEOUT, out / lse void.
+ * Only reads the cache (but for the status word); runs on the device that the cache was created on. */
+size_t pask_prompt_workspace_bytes(const pask_cache_t *cache, int32_t n_seqs, int32_t total_tokens);
+pask_status_t pask_prompt_attention(pask_cache_t *cache, int32_t layer, int32_t n_seqs, int32_t total_tokens, const int32_t *seq_ids,
+                                    const int32_t *cu_tokens, const void *q, const void *k, const void *v, void *out, float *lse,
+                                    void *workspace, size_t workspace_bytes, pask_stream_t stream);
+
+/* ---------------------------------------------------------------------------------------------
  * Rotary positions.  The caches hold keys with their positions in them (K after its rotation; the last 64 dims of a
  * latent row), so that the order of what is retained does not matter: this is the step between a layer's projections and
  * pask_prompt_attention / pask_append_kv / pask_decode_attention and the latent calls.

@@ -35,7 +35,7 @@ EXPORTS = [
     "pask_append_kv_decided", "pask_append_attend", "pask_plan_area_bytes", "pask_plan_ahead", "pask_decode_step_ahead", "pask_decode_attention",
     "pask_decode_attention_full", "pask_decode_attention_static", "pask_workspace_bytes", "pask_decode_step_host", "pask_step_staging_bytes", "pask_step_packed_layout", "pask_decode_step_packed", "pask_decode_step_pipelined", "pask_decode_step_pipelined_ahead", "pask_decode_step_drain",
     "pask_append_latent", "pask_read_latent", "pask_decode_attention_latent", "pask_prompt_attention_latent",
-    "pask_rotary_table", "pask_rotary",
+    "pask_prompt_workspace_bytes", "pask_prompt_attention", "pask_rotary_table", "pask_rotary",
     "pask_budget_state", "pask_distortion", "pask_cache_set_timing_events", "pask_cache_set_timing_span", "pask_debug_stream_len", "pask_debug_dump_high",
     "pask_debug_dump_low", "pask_debug_pool_state", "pask_debug_ctrl_words", "pask_debug_page_order", "pask_debug_page_ids", "pask_debug_partition", "pask_debug_set_attention_ctas", "pask_debug_set_wait", "pask_debug_set_prompt_wait", "pask_debug_plan_order_span", "pask_status_string",
 ]
@@ -116,6 +116,9 @@ _lib.pask_append_latent.argtypes = [_vp, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _
 _lib.pask_read_latent.argtypes = [_vp, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp]
 _lib.pask_decode_attention_latent.argtypes = [_vp, _i32, _i32, _vp, _vp, C.c_float, _vp, _vp, _vp, _sz, _vp]
 _lib.pask_prompt_attention_latent.argtypes = [_i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _i32, C.c_float, _vp, _vp, _vp]
+_lib.pask_prompt_workspace_bytes.argtypes = [_vp, _i32, _i32]
+_lib.pask_prompt_workspace_bytes.restype = _sz
+_lib.pask_prompt_attention.argtypes = [_vp, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
 _lib.pask_rotary_table.argtypes = [C.POINTER(RotaryDesc), _vp]
 _lib.pask_rotary.argtypes = [_i32, _vp, _vp, _i32, _i32, _i32, C.c_float, _i32, _i32, C.POINTER(RotaryTensor), _vp]
 _lib.pask_budget_state.argtypes = [_vp, _i32, C.POINTER(BudgetState), _vp]
@@ -181,6 +184,7 @@ def pask_policy_action(policy: int, tag: int, group: int) -> int:
     return int(_lib.pask_policy_action(policy, tag, group))
 
 
+_heads = {}            # handle of a cache -> (query heads, key / value heads): what pask_prompt_attention checks shapes against
 _latent_shape = {}     # handle of a latent cache -> (query heads, layer groups): what shapes are checked against
 
 
@@ -194,6 +198,7 @@ def pask_cache_create(desc: CacheDesc, policy: int, pool_high, pool_low, meta, s
     h = _vp()
     _check(_lib.pask_cache_create(C.byref(desc), policy, _dptr(pool_high), _dptr(pool_low), _dptr(meta),
                                   _stream(stream), C.byref(h)), "pask_cache_create")
+    _heads[h.value] = (desc.n_q_heads, desc.n_kv_heads)
     if desc.head_dim == LATENT_DIM:
         groups = next(g for g in range(MAX_GROUPS + 1) if pask_policy_action(policy, 0, g) < 0)
         _latent_shape[h.value] = (desc.n_q_heads, groups)
@@ -201,6 +206,7 @@ def pask_cache_create(desc: CacheDesc, policy: int, pool_high, pool_low, meta, s
 
 
 def pask_cache_destroy(cache: int):
+    _heads.pop(cache, None)
     _latent_shape.pop(cache, None)
     _lib.pask_cache_destroy(cache)
 
@@ -442,6 +448,25 @@ def pask_prompt_attention_latent(cu_q, cu_k, q, kv, k_rope, scale: float, out, l
           None if lse is None else _arg(w, "lse", lse, torch.float32, dev, (tq, heads)))
 
 
+def pask_prompt_workspace_bytes(cache: int, n_seqs: int, total_tokens: int) -> int:
+    return int(_lib.pask_prompt_workspace_bytes(cache, n_seqs, total_tokens))
+
+
+def pask_prompt_attention(cache: int, layer: int, seq_ids, cu_tokens, q, k, v, out, lse, workspace, stream=None):
+    """Causal attention of a ragged batch of prompts, chunks or drafts behind the retained history of their sequences, before they are
+    appended: q bf16 [total][n_q][128], k, v bf16 [total][n_kv][128], out bf16 [total][n_q][128], lse fp32 [total][n_q] or None."""
+    w, n, total, dev = "pask_prompt_attention", seq_ids.numel(), _dim(q, 0), seq_ids.get_device()
+    heads, kv = _heads[cache] if cache in _heads else (_dim(q, 1), _dim(k, 1))
+    _call(w, _lib.pask_prompt_attention, dev, stream, cache, layer, n, total, _arg(w, "seq_ids", seq_ids, torch.int32, dev, (n,)),
+          _arg(w, "cu_tokens", cu_tokens, torch.int32, dev, (n + 1,)), _arg(w, "q", q, torch.bfloat16, dev, (total, heads, 128)),
+          _arg(w, "k", k, torch.bfloat16, dev, (total, kv, 128)), _arg(w, "v", v, torch.bfloat16, dev, (total, kv, 128)),
+          _arg(w, "out", out, torch.bfloat16, dev, (total, heads, 128)),
+          None if lse is None else _arg(w, "lse", lse, torch.float32, dev, (total, heads)),
+          _arg(w, "workspace", workspace, workspace.dtype, dev, workspace.shape), workspace.numel() * workspace.element_size())
+    if stream is not None:                         # a workspace the caller drops at once is not handed out again while the call runs
+        workspace.record_stream(stream)
+
+
 def pask_rotary_table(rot_dim: int, base: float = 10000.0, scaling: int = ROTARY_PLAIN, factor: float = 1.0, context: float = 0.0,
                       few: float = 1.0, many: float = 32.0, device="cuda"):
     """Frequencies of rot_dim / 2 pairs for pask_rotary, int64 [rot_dim / 2] (the bits of the C call's uint64) on `device`."""
@@ -611,6 +636,10 @@ class Cache:
         if self._ws is None or self._ws.numel() < need:
             self._ws = torch.empty(need, dtype=torch.uint8, device=self.meta.device)
         return self._ws
+
+    def prompt_workspace(self, n_seqs: int, total_tokens: int):
+        """A workspace for pask_prompt_attention, another one for each who asks: calls that may overlap need one each."""
+        return torch.empty(pask_prompt_workspace_bytes(self.handle, n_seqs, total_tokens), dtype=torch.uint8, device=self.meta.device)
 
     def close(self):
         if getattr(self, "handle", None):

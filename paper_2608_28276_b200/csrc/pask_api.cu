@@ -459,6 +459,29 @@ pask_status_t pask_prompt_attention_latent(int32_t n_seqs, int32_t total_q, int3
                                 static_cast<cudaStream_t>(stream));
 }
 
+size_t pask_prompt_workspace_bytes(const pask_cache_t *c, int32_t n_seqs, int32_t total_tokens) {
+    if (!c || c->latent || n_seqs < 1 || n_seqs > PASK_MAX_SEQS_PER_CALL || total_tokens < 0) return 0;
+    return prompt_workspace_bytes(c, n_seqs, total_tokens);
+}
+
+pask_status_t pask_prompt_attention(pask_cache_t *c, int32_t layer, int32_t n_seqs, int32_t total_tokens, const int32_t *seq_ids,
+                                    const int32_t *cu_tokens, const void *q, const void *k, const void *v, void *out, float *lse, void *ws,
+                                    size_t ws_bytes, pask_stream_t stream) {
+    if (!c || !seq_ids || !cu_tokens) return PASK_ERR_INVALID_ARG;
+    if (c->latent) return PASK_ERR_UNSUPPORTED_SHAPE;   // pask_prompt_attention_latent
+    if (layer < 0 || layer >= c->desc.n_layers || n_seqs < 1 || n_seqs > PASK_MAX_SEQS_PER_CALL || total_tokens < 0) return PASK_ERR_INVALID_ARG;
+    if (((uintptr_t)seq_ids | (uintptr_t)cu_tokens | (uintptr_t)lse) & 3) return PASK_ERR_INVALID_ARG;
+    if (total_tokens == 0) return PASK_OK;
+    if (!q || !k || !v || !out || !ws) return PASK_ERR_INVALID_ARG;
+    if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)out) & 15 || ((uintptr_t)ws & 255)) return PASK_ERR_INVALID_ARG;
+    if (ws_bytes < prompt_workspace_bytes(c, n_seqs, total_tokens)) return PASK_ERR_WORKSPACE;
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess) return PASK_ERR_CUDA;
+    if (dev != c->device) return PASK_ERR_INVALID_ARG;
+    NvtxRange range("pask_prompt_attention");
+    return launch_prompt(c, layer, n_seqs, total_tokens, seq_ids, cu_tokens, q, k, v, out, lse, ws, static_cast<cudaStream_t>(stream));
+}
+
 pask_status_t pask_rotary_table(const pask_rotary_desc_t *d, uint64_t *table) {
     if (!d || !table) return PASK_ERR_INVALID_ARG;
     if (d->rot_dim < 2 || d->rot_dim > PASK_ROTARY_MAX_DIM || d->rot_dim % 2) return PASK_ERR_UNSUPPORTED_SHAPE;

@@ -218,6 +218,9 @@ void set_prompt_wait(long long limit_cycles, uint32_t surplus_bytes);    // for 
 pask_status_t launch_prompt_latent(int n_seqs, int total_q, int total_k, int n_heads, const int32_t *cu_q, const int32_t *cu_k,
                                    const void *q, const void *kv, const void *k_rope, int rope_stride, float scale, void *out,
                                    float *lse, cudaStream_t stream);
+size_t prompt_workspace_bytes(const pask_cache *c, int n_seqs, int total_tokens);
+pask_status_t launch_prompt(pask_cache *c, int layer, int n_seqs, int total_tokens, const int32_t *seq_ids, const int32_t *cu_tokens, const void *q,
+                            const void *k, const void *v, void *out, float *lse, void *workspace, cudaStream_t stream);
 constexpr int kRotaryMaxDim = PASK_ROTARY_MAX_DIM, kRotaryMaxTensors = PASK_ROTARY_MAX_TENSORS;
 pask_status_t launch_rotary(int n_tokens, const int32_t *positions, const uint64_t *table, int rot_dim, bool neighbours, bool transpose,
                             float magnitude, int dtype, int n_tensors, const pask_rotary_tensor_t *tensors, cudaStream_t stream);

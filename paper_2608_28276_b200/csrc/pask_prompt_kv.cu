@@ -1,0 +1,1108 @@
+// pask_prompt_attention: causal attention of the tokens of a ragged batch behind what a cache retains of their sequences.
+//
+// Per query head: S = Q K^T over 128 dims, P = softmax(S / sqrt(128)), O = P V, where K and V are the history (pages of bf16 rows and of
+// 2, 4 or 8-bit rows, the protected window's ring) and the call's own tokens up to the query's.  The four query heads of a
+// key / value head are rows of one product: a tile is 32 tokens x 4 heads = 128 rows.
+//
+// Work.  An item is a block of tokens (one or two tiles) and a key / value head; its keys are blocks of 128: eight pages of the history,
+// or 128 tokens of the call.  plan_kernel lays all items end to end on a line of their costs (key blocks, and two more for the
+// beginning and the result) and every CTA of the grid, one an SM, takes an equal stretch: cuts fall inside items, at any key
+// block, and the parts of an item meet in the workspace, joined by the CTA that finishes last (in the order of the parts, so
+// that the result does not depend on who that is).  No more items than CTAs: each gets whole CTAs of its own instead.
+//
+// In a CTA
+//   softmax warps (four a tile)  a thread has a row: S in registers, P back to tensor memory over S in bf16, as the left operand of
+//                    P V.  The reference maximum moves only when a score exceeds it by more than 2^8, so that O is rarely rescaled
+//   products         P V of tile t, block j;  Q K^T of tile t, block j + 1;  the other tile
+//   copies           queries; the call's own keys and values (TMA)
+//   fill             history pages: read as they are stored, expanded to bf16 and laid out as the tensor core reads them
+//   items            which items, and which parts of them, are this CTA's
+// Shared memory: Q 32 KB a tile, stages of 64 KB (128 keys and values).  Tensor memory: S and O, 128 columns each a tile.
+//
+// Rounding: S, O and the sums are fp32; a weight is rounded to bf16 once, as an operand of a product with bf16 values; a low-precision
+// row enters as bf16(code * scale), rounded once from the exact product.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "pask_internal.h"
+#include "pask_tensormap.h"
+#include "pask_umma.h"
+
+namespace pask {
+
+namespace {
+
+constexpr int kDim = kHeadDim, kGqa = 4;
+constexpr int kTileRows = 128, kTileTokens = kTileRows / kGqa, kBlockK = 128, kBlockPages = kBlockK / kPageTokens;
+constexpr int kSub = kBlockK * 128;                // 128 rows x 64 dims: 16 KB
+constexpr int kTileBytes = 2 * kSub;               // 128 rows x 128 dims
+constexpr int kThreads = 512;
+constexpr int kItemCost = 2;                       // of an item's beginning and end, in key blocks
+constexpr int kMinPiece = 2;                       // no part of an item is shorter, in key blocks
+constexpr float kLazy = 8.0f;
+constexpr float kScaleLog2 = 0.08838834764831845f * 1.4426950408889634f;       // 1 / sqrt(128), log2 e
+
+// What the plan says of a sequence of the call.
+struct __align__(16) PromptSeq {
+    int q0, nq;                                    // its rows; none if its range is malformed or its id is out of range
+    uint32_t slot;                                 // sequence * layers + layer
+    uint32_t nh, nl, nw;                           // tokens attended from the two streams and from the window's ring
+    int blocks;                                    // key blocks of its history
+    int parts;                                     // CTAs an item of it has for itself (0: the line is cut evenly)
+};
+static_assert(sizeof(PromptSeq) == 32, "two 16-byte loads");
+
+struct PromptWorkspace {
+    uint64_t *prefix;                              // [n_seqs + 1] cost (or CTAs) of the sequences before
+    PromptSeq *seqs;                               // [n_seqs]
+    uint32_t *arrived;                             // [grid] parts of the item that begins with this CTA's part
+    float2 *ml;                                    // [2 grid][rows] reference maximum in log2 units, sum
+    float4 *o;                                     // [2 grid][32][rows] unscaled outputs, four dims a piece
+};
+
+size_t carve(int n_seqs, int grid, int rows, uint8_t *base, PromptWorkspace *ws) {
+    size_t off = 0;
+    auto take = [&](size_t bytes) { size_t at = off; off = (off + bytes + 255) / 256 * 256; return at; };
+    const size_t o_prefix = take((size_t)(n_seqs + 1) * 8), o_seqs = take((size_t)n_seqs * sizeof(PromptSeq)), o_arr = take((size_t)grid * 4);
+    const size_t o_ml = take((size_t)2 * grid * rows * sizeof(float2)), o_o = take((size_t)2 * grid * rows * kDim * 4);
+    if (ws) {
+        ws->prefix = reinterpret_cast<uint64_t *>(base + o_prefix);
+        ws->seqs = reinterpret_cast<PromptSeq *>(base + o_seqs);
+        ws->arrived = reinterpret_cast<uint32_t *>(base + o_arr);
+        ws->ml = reinterpret_cast<float2 *>(base + o_ml);
+        ws->o = reinterpret_cast<float4 *>(base + o_o);
+    }
+    return off;
+}
+
+struct PromptParams {
+    PromptWorkspace ws;
+    const uint8_t *pool_high, *pool_low;
+    const uint32_t *tbl_high, *tbl_low;
+    uint32_t *status;
+    uint32_t high_page_bytes, low_page_bytes, low_head_bytes, cap_low, high_limit, ring_first, ring_pages;
+    int max_pages, n_kv, n_seqs, grid;
+    __nv_bfloat16 *out;
+    float *lse;
+    long long wait_cycles;
+    uint32_t surplus;
+};
+
+PASK_HD int pages_of(uint32_t tokens) { return (int)((tokens + kPageTokens - 1) / kPageTokens); }
+// key blocks of the call's own tokens that token block j (of `tokens`) looks at, and the sum of that over blocks 0 .. j - 1
+__host__ __device__ __forceinline__ int own_blocks(int j, int tokens) { return j * tokens / kBlockK + 1; }
+__host__ __device__ __forceinline__ long long own_blocks_before(int j, int tokens) {
+    const long long r = kBlockK / tokens, m = j / r, k = j % r;
+    return r * m * (m + 1) / 2 + k * (m + 1);
+}
+
+// ------------------------------------------------------------------------------------------------ plan
+
+constexpr int kPlanThreads = 1024;
+
+// One CTA, a sequence a thread: what each has to attend, the line of costs, the parts' counters.
+__global__ void __launch_bounds__(kPlanThreads)
+prompt_plan_kernel(DevCache c, int layer, int n_seqs, int total, const int32_t *__restrict__ seq_ids, const int32_t *__restrict__ cu,
+                   PromptWorkspace ws, int grid, int block_tokens, uint4 *__restrict__ out, float *__restrict__ lse) {
+    __shared__ uint64_t s_sum[32];
+    __shared__ uint32_t s_parts, s_items, s_longest, s_bad;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    pdl_launch_dependents();
+    pdl_wait();
+    if (tid == 0) s_items = s_longest = s_bad = 0;
+    for (int i = tid; i < grid; i += kPlanThreads) ws.arrived[i] = 0;
+    __syncthreads();
+    PromptSeq s{};
+    uint32_t bad = 0;
+    bool unknown = false;
+    if (tid < n_seqs) {
+        const int id = seq_ids[tid], q0 = cu[tid], q1 = cu[tid + 1];
+        unknown = id < 0 || id >= c.max_seqs;
+        if (q0 < 0 || q1 < q0 || q1 > total) bad |= PASK_DEV_BAD_RAGGED;
+        else { s.q0 = q0; s.nq = q1 - q0; }
+        if (unknown) bad |= PASK_DEV_BAD_SEQ;
+        else {
+            s.slot = (uint32_t)id * (uint32_t)c.n_layers + (uint32_t)layer;
+            s.nh = c.n_high[s.slot];
+            s.nl = c.n_low[s.slot];
+            if (c.window) {
+                // The last min(W, tokens seen) tokens come from the ring, whatever their action; the streams are in arrival order, so
+                // that their members among those are the streams' last entries.
+                const uint32_t seen = c.n_tok[s.slot];
+                s.nw = min(seen, c.window);
+                const uint4 *act = reinterpret_cast<const uint4 *>(c.win_act + (size_t)s.slot * c.window);
+                for (uint32_t i = 0; 16 * i < s.nw; i++) {
+                    const uint4 a = act[i];
+                    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+                    for (uint32_t e = 0; e < 16 && 16 * i + e < s.nw; e++) {
+                        const uint32_t action = (w[e >> 2] >> (8 * (e & 3))) & 0xFF;
+                        if (action == PASK_ACTION_RETAIN_HIGH) s.nh--;
+                        if (action == PASK_ACTION_RETAIN_LOW) s.nl--;
+                    }
+                }
+            }
+        }
+        if (bad) { atomicOr(&s_bad, bad); }
+        s.blocks = (pages_of(s.nh) + pages_of(s.nl) + pages_of(s.nw) + kBlockPages - 1) / kBlockPages;
+    }
+    const int named = s.nq;                        // rows of an unknown sequence: cleared below, no item
+    if (unknown) s.nq = 0;
+    const int nqb = (s.nq + block_tokens - 1) / block_tokens, longest = nqb ? s.blocks + own_blocks(nqb - 1, block_tokens) : 0;
+    if (nqb && nqb <= grid) {                      // (more: no need to count)
+        atomicAdd(&s_items, (uint32_t)(nqb * c.n_kv));
+        atomicMax(&s_longest, (uint32_t)longest);
+    }
+    const bool many = __syncthreads_or(nqb > grid);
+    if (tid == 0 && s_bad) atomicOr(&c.ctrl[kCtrlStatus], s_bad);
+    uint64_t cost = (uint64_t)c.n_kv * ((uint64_t)nqb * (uint64_t)(s.blocks + kItemCost) + (uint64_t)own_blocks_before(nqb, block_tokens));
+    if (!many && s_items <= (uint32_t)grid) {
+        // Whole CTAs for each item: the shortest part length for which the grid has enough of them
+        uint32_t lo = kMinPiece, hi = max(s_longest, (uint32_t)kMinPiece);
+        while (lo < hi) {
+            const uint32_t mid = (lo + hi) / 2;
+            if (tid == 0) s_parts = 0;
+            __syncthreads();
+            if (nqb) atomicAdd(&s_parts, (uint32_t)(c.n_kv * nqb) * ((longest + mid - 1) / mid));
+            __syncthreads();
+            const bool fits = s_parts <= (uint32_t)grid;
+            __syncthreads();
+            if (fits) hi = mid; else lo = mid + 1;
+        }
+        if (nqb) s.parts = (int)((longest + lo - 1) / lo);
+        cost = (uint64_t)c.n_kv * nqb * s.parts;
+    }
+    // prefix over the sequences
+    uint64_t inc = cost;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const uint64_t o = __shfl_up_sync(0xffffffffu, inc, d);
+        if (lane >= d) inc += o;
+    }
+    if (lane == 31) s_sum[warp] = inc;
+    __syncthreads();
+    uint64_t before = 0;
+    for (int w = 0; w < warp; w++) before += s_sum[w];
+    if (tid < n_seqs) {
+        ws.prefix[tid + 1] = before + inc;
+        ws.seqs[tid] = s;
+    }
+    if (tid == 0) ws.prefix[0] = 0;
+    // rows of sequences that are none
+    if (s_bad & PASK_DEV_BAD_SEQ) {
+        __shared__ int s_q0, s_n;
+        for (int i = 0; i < n_seqs; i++) {
+            __syncthreads();
+            if (tid == i) { s_q0 = s.q0; s_n = unknown ? named : 0; }
+            __syncthreads();
+            const size_t heads = (size_t)kGqa * c.n_kv, from = (size_t)s_q0 * heads, count = (size_t)s_n * heads;
+            for (size_t e = tid; e < count * (kDim / 8); e += kPlanThreads) out[from * (kDim / 8) + e] = make_uint4(0, 0, 0, 0);
+            if (lse)
+                for (size_t e = tid; e < count; e += kPlanThreads) lse[from + e] = -INFINITY;
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ items
+
+struct Item {
+    int q0, nq, head, block;                       // rows of the sequence; key / value head; token block; block -1: no further item
+    uint32_t slot, nh, nl, nw;
+    int hist, blocks;                              // key blocks: of the history, in all
+    int b0, b1;                                    // this CTA's
+    int first, last;                               // the CTAs that have a part
+};
+
+// Walks over a CTA's items; all lanes of a warp hold the same.
+struct Walker {
+    uint64_t x0, x1, at;                           // the CTA's stretch of the line, beginning of the item to come
+    int cta, grid, n_seqs, tokens, n_kv, s, head, block;
+    PromptSeq q;
+    bool whole;                                    // whole CTAs for each item
+    const PromptWorkspace *ws;
+
+    __device__ __forceinline__ uint64_t edge(uint64_t total, int b) const { return total * (uint64_t)b / (uint64_t)grid; }
+    // sequences that end at or before x
+    __device__ __forceinline__ int seqs_before(uint64_t x, int lane) const {
+        const int step = (n_seqs + 31) / 32;
+        const int n = __popc(__ballot_sync(0xffffffffu, (lane + 1) * step <= n_seqs && ws->prefix[min((lane + 1) * step, n_seqs)] <= x)) * step;
+        const int k = n + lane + 1;
+        return n + __popc(__ballot_sync(0xffffffffu, lane < step && k <= n_seqs && ws->prefix[min(k, n_seqs)] <= x));
+    }
+    __device__ __forceinline__ int token_blocks() const { return (q.nq + tokens - 1) / tokens; }
+    __device__ __forceinline__ int key_blocks() const { return q.blocks + own_blocks(block, tokens); }
+
+    __device__ __forceinline__ void load_seq() { q = ws->seqs[s]; }
+
+    __device__ __forceinline__ void init(const PromptParams &p, int block_tokens, int lane) {
+        ws = &p.ws;
+        cta = blockIdx.x; grid = p.grid; n_seqs = p.n_seqs; tokens = block_tokens; n_kv = p.n_kv;
+        const uint64_t total = ws->prefix[n_seqs];
+        whole = ws->seqs[seqs_before(0, lane) < n_seqs ? seqs_before(0, lane) : 0].parts > 0;
+        if (whole) { x0 = cta; x1 = (uint64_t)cta + 1 <= total ? (uint64_t)cta + 1 : (uint64_t)cta; }
+        else { x0 = edge(total, cta); x1 = edge(total, cta + 1); }
+        if (x0 >= x1) { s = n_seqs; return; }
+        s = seqs_before(x0, lane);
+        if (s >= n_seqs) return;
+        load_seq();
+        uint64_t rest = x0 - ws->prefix[s];
+        if (whole) {
+            const int item = (int)(rest / q.parts), nb = token_blocks();
+            head = item / nb;
+            block = item % nb;
+            return;
+        }
+        const int nb = token_blocks();
+        const uint64_t per = (uint64_t)nb * (q.blocks + kItemCost) + own_blocks_before(nb, tokens);
+        head = (int)(rest / per);
+        rest -= per * head;
+        int lo = 0, hi = nb - 1;                   // the last block that begins at or before rest
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) / 2;
+            if ((uint64_t)mid * (q.blocks + kItemCost) + own_blocks_before(mid, tokens) <= rest) lo = mid; else hi = mid - 1;
+        }
+        block = lo;
+        at = x0 - rest + (uint64_t)block * (q.blocks + kItemCost) + own_blocks_before(block, tokens);
+    }
+    // key blocks of the item at `at` before point x of the line.  Both sides of a cut ask the same.
+    __device__ __forceinline__ int cut(uint64_t x, int nb) const {
+        if (x <= at + kItemCost) return 0;
+        if (x >= at + kItemCost + nb) return nb;
+        const int y = (int)(x - at - kItemCost);
+        return y < kMinPiece ? 0 : nb - y < kMinPiece ? nb : y;
+    }
+    __device__ __forceinline__ bool next(Item &it, int lane) {
+        while (s < n_seqs) {
+            const int nb = key_blocks();
+            it.q0 = q.q0; it.nq = q.nq; it.head = head; it.block = block;
+            it.slot = q.slot; it.nh = q.nh; it.nl = q.nl; it.nw = q.nw;
+            it.hist = q.blocks; it.blocks = nb;
+            if (whole) {
+                const int rest = (int)(x0 - ws->prefix[s]), part = rest % q.parts, parts = min(q.parts, nb);
+                s = n_seqs;
+                if (part >= parts) return false;
+                it.b0 = (int)((long long)nb * part / parts);
+                it.b1 = (int)((long long)nb * (part + 1) / parts);
+                it.first = cta - part;
+                it.last = it.first + parts - 1;
+                return true;
+            }
+            if (at >= x1) { s = n_seqs; return false; }
+            it.b0 = cut(x0, nb);
+            it.b1 = cut(x1, nb);
+            it.first = it.last = cta;
+            if (it.b0 < it.b1 && it.b1 - it.b0 < nb) {
+                // Who has the rest: the CTAs whose stretches meet the item's, a lane each
+                const uint64_t total = ws->prefix[n_seqs];
+                const double per = (double)grid / (double)total;
+                const int from = max(0, (int)((double)at * per) - 1), to = min(grid - 1, (int)((double)(at + kItemCost + nb) * per) + 1);
+                int lo = grid, hi = -1;
+                for (int b = from + lane; b <= to; b += 32)
+                    if (cut(edge(total, b), nb) < cut(edge(total, b + 1), nb)) { lo = min(lo, b); hi = max(hi, b); }
+                it.first = __reduce_min_sync(0xffffffffu, lo);
+                it.last = __reduce_max_sync(0xffffffffu, hi);
+            }
+            at += kItemCost + nb;
+            if (++block >= token_blocks()) {
+                block = 0;
+                if (++head >= n_kv) {
+                    head = 0;
+                    s = seqs_before(at, lane);
+                    if (s < n_seqs) load_seq();
+                }
+            }
+            if (it.b0 < it.b1) return true;
+        }
+        return false;
+    }
+};
+
+// ------------------------------------------------------------------------------------------------ pages to operands
+
+constexpr uint32_t kPageLow = 0, kPageBad = 1, kPageHigh = 2, kPageNone = 3;       // kinds of a page: bits 30, 31 of its entry
+
+// A page's key / value rows of one head as they are stored, a lane's share in registers.
+struct Raw { uint4 x[8]; uint4 s[2]; };
+
+// (code - kZero) * scale for two codes, as bf16, rounded once: the difference is exact, the scale is the sum of two bf16 numbers of which the
+// smaller has three bits, so that its product with a code is exact and one fma rounds the sum of both products.
+__device__ __forceinline__ uint32_t scaled_codes(uint32_t codes, uint32_t offset, uint32_t s_hi, uint32_t s_lo) {
+    uint32_t r;
+    asm("{\n\t.reg .b32 c, m;\n\tsub.rn.bf16x2 c, %1, %2;\n\tmul.rn.bf16x2 m, c, %4;\n\tfma.rn.bf16x2 %0, c, %3, m;\n\t}"
+        : "=r"(r) : "r"(codes | 0x43004300u), "r"(offset), "r"(s_hi), "r"(s_lo));
+    return r;
+}
+__device__ __forceinline__ float half_bits(uint32_t h) { return __half2float(__ushort_as_half((unsigned short)h)); }
+// fp16 bits of a scale as two bf16 numbers whose sum it is, each twice
+__device__ __forceinline__ void split_scale(uint32_t h, uint32_t &hi, uint32_t &lo) {
+    const float f = half_bits(h), a = __bfloat162float(__float2bfloat16_rn(f));
+    hi = umma::pack_bf16(f, f);
+    lo = umma::pack_bf16(f - a, f - a);
+}
+__device__ __forceinline__ float byte_value(uint32_t w, uint32_t k) {            // byte k of w, less 128
+    return __uint_as_float(__byte_perm(w, 0x4B000000u, 0x7440u | k)) - 8388736.0f;
+}
+__device__ __forceinline__ void store16(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+__device__ __forceinline__ void store8(uint32_t a, uint32_t x, uint32_t y) {
+    asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(a), "r"(x), "r"(y) : "memory");
+}
+__device__ __forceinline__ void store4(uint32_t a, uint32_t x) { asm volatile("st.shared.b32 [%0], %1;" ::"r"(a), "r"(x) : "memory"); }
+
+// Lanes of the fragment packing (g = token or dims, t): keys are stored 16 bytes a lane, eight lanes at a time, and rows g and g + 4 side by
+// side have their pieces in different banks; values 8 bytes, sixteen lanes at a time, in the packing's own order.
+struct Lanes {
+    int g, t;
+    bool keys;
+    __device__ __forceinline__ Lanes(bool k, int lane) : keys(k) {
+        g = k ? (lane >> 3) | (lane & 4) : lane >> 2;
+        t = lane & 3;
+    }
+    __device__ __forceinline__ int source() const { return 4 * g + t; }
+};
+
+template <int kBits, bool kKeys>
+struct Low {
+    static constexpr int kRounds = kBits / 2 < 1 ? 1 : kBits / 2;               // 512-byte rounds of codes: 1, 2, 4
+    static constexpr int kHalf = 512 * kRounds + kLowScalesBytes;
+};
+
+template <bool kKeys>
+__device__ __forceinline__ void load_high(Raw &r, const uint8_t *head, int lane) {
+    const uint4 *src = reinterpret_cast<const uint4 *>(head + (kKeys ? 0 : kHighTileBytes)) + Lanes(kKeys, lane).source();
+#pragma unroll
+    for (int i = 0; i < 8; i++) r.x[i] = __ldg(src + 32 * i);
+}
+// `row`: first row of the page in its block; the block is two pieces of 64 dims, 128 rows of 128 bytes with the 128-byte swizzle
+template <bool kKeys>
+__device__ __forceinline__ void store_high(const Raw &r, uint32_t block, int row, int lane) {
+    const Lanes l(kKeys, lane);
+    if (kKeys) {
+        const uint32_t base = block + (uint32_t)(row + l.g) * 128;
+#pragma unroll
+        for (int j = 0; j < 4; j++) {              // dims 8 (4 j + t) .. + 7 of tokens g and g + 8
+            const uint4 a = r.x[2 * j], b = r.x[2 * j + 1];
+            const uint32_t at = base + (j >> 1) * kSub + (((4 * (j & 1) + l.t) ^ l.g) << 4);
+            store16(at, a.x, a.z, b.x, b.z);
+            store16(at + 1024, a.y, a.w, b.y, b.w);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; i++) {              // token 2 t + (k & 1) + 8 (k >> 1), dims 64 e + 4 g .. and 32 on
+            const int e = i >> 2, k = i & 3, tok = 2 * l.t + (k & 1), sw = tok & 7;
+            const uint32_t base = block + e * kSub + (uint32_t)(row + tok + 8 * (k >> 1)) * 128 + 8 * (l.g & 1);
+            store8(base + (((l.g >> 1) ^ sw) << 4), r.x[i].x, r.x[i].y);
+            store8(base + (((4 + (l.g >> 1)) ^ sw) << 4), r.x[i].z, r.x[i].w);
+        }
+    }
+}
+
+template <int kBits, bool kKeys>
+__device__ __forceinline__ void load_low(Raw &r, const uint8_t *head, int lane) {
+    using L = Low<kBits, kKeys>;
+    const Lanes l(kKeys, lane);
+    const uint8_t *half = head + (kKeys ? 0 : L::kHalf);
+    const uint4 *src = reinterpret_cast<const uint4 *>(half) + l.source();
+#pragma unroll
+    for (int i = 0; i < L::kRounds; i++) r.x[i] = __ldg(src + 32 * i);
+    const uint8_t *scales = half + 512 * L::kRounds;
+    if (kKeys) {                                   // tokens g and g + 8
+        const uint2 a = __ldg(reinterpret_cast<const uint2 *>(scales) + l.g), b = __ldg(reinterpret_cast<const uint2 *>(scales) + l.g + 8);
+        r.s[0] = make_uint4(a.x, a.y, b.x, b.y);
+    } else {                                       // tokens 2 t, 2 t + 1 and 8 on
+        r.s[0] = __ldg(reinterpret_cast<const uint4 *>(scales) + l.t);
+        r.s[1] = __ldg(reinterpret_cast<const uint4 *>(scales) + l.t + 4);
+    }
+}
+
+__device__ __forceinline__ uint32_t word_of(const uint4 &v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+__device__ __forceinline__ uint32_t half_of(uint32_t w, int i) { return (w >> (16 * i)) & 0xFFFFu; }
+
+template <int kBits, bool kKeys>
+__device__ __forceinline__ void store_low(const Raw &r, uint32_t block, int row, int lane) {
+    const Lanes l(kKeys, lane);
+    constexpr uint32_t kOffset = kBits == 4 ? 0x43084308u : 0x43024302u;         // bf16 136 or 130, twice: 128 + the code of zero
+    constexpr uint32_t kMask = kBits == 4 ? 0x000F000Fu : 0x00030003u;
+    if constexpr (kBits == 8 && kKeys) {
+#pragma unroll
+        for (int rr = 0; rr < 4; rr++)             // group rr: k-chunks 2 rr, 2 rr + 1 of 16 dims
+#pragma unroll
+            for (int hi = 0; hi < 2; hi++) {       // tokens g, g + 8
+                const float s = half_bits(half_of(hi ? (rr < 2 ? r.s[0].z : r.s[0].w) : (rr < 2 ? r.s[0].x : r.s[0].y), rr & 1));
+                const uint32_t base = block + (rr >> 1) * kSub + (uint32_t)(row + l.g + 8 * hi) * 128 + 4 * l.t;
+#pragma unroll
+                for (int k = 0; k < 4; k++) {      // 8 dims each: dims 32 rr + 8 k + 2 t, + 1
+                    const uint32_t w = word_of(r.x[rr], k);
+                    store4(base + (((4 * (rr & 1) + k) ^ l.g) << 4), umma::pack_bf16(byte_value(w, 2 * hi) * s, byte_value(w, 2 * hi + 1) * s));
+                }
+            }
+    } else if constexpr (kBits == 8) {
+#pragma unroll
+        for (int q = 0; q < 4; q++)
+#pragma unroll
+            for (int ps = 0; ps < 2; ps++) {       // tokens 2 t + 8 ps and the next, dims 32 q + 4 g .. + 3
+                const uint32_t a = ps ? r.x[q].y : r.x[q].x, b = ps ? r.x[q].w : r.x[q].z;
+#pragma unroll
+                for (int odd = 0; odd < 2; odd++) {
+                    const uint32_t sw = odd ? (q < 2 ? r.s[ps].z : r.s[ps].w) : (q < 2 ? r.s[ps].x : r.s[ps].y);
+                    const float s = half_bits(half_of(sw, q & 1));
+                    const int tok = 2 * l.t + odd;
+                    store8(block + (q >> 1) * kSub + (uint32_t)(row + tok + 8 * ps) * 128 + (((4 * (q & 1) + (l.g >> 1)) ^ (tok & 7)) << 4) + 8 * (l.g & 1),
+                           umma::pack_bf16(byte_value(a, odd) * s, byte_value(a, 2 + odd) * s),
+                           umma::pack_bf16(byte_value(b, odd) * s, byte_value(b, 2 + odd) * s));
+                }
+            }
+    } else if constexpr (kKeys) {
+#pragma unroll
+        for (int hi = 0; hi < 2; hi++) {           // tokens g, g + 8
+            const uint32_t base = block + (uint32_t)(row + l.g + 8 * hi) * 128;
+#pragma unroll
+            for (int w = 0; w < 4; w++) {          // group w: dims 32 w + 8 t .. + 7
+                uint32_t s_hi, s_lo;
+                split_scale(half_of(hi ? (w < 2 ? r.s[0].z : r.s[0].w) : (w < 2 ? r.s[0].x : r.s[0].y), w & 1), s_hi, s_lo);
+                const uint32_t x = kBits == 4 ? word_of(r.x[hi], w) : word_of(r.x[0], w) >> (8 * hi);
+                constexpr int kStep = kBits;
+                store16(base + (w >> 1) * kSub + (((4 * (w & 1) + l.t) ^ l.g) << 4), scaled_codes(x & kMask, kOffset, s_hi, s_lo),
+                        scaled_codes((x >> kStep) & kMask, kOffset, s_hi, s_lo), scaled_codes((x >> 2 * kStep) & kMask, kOffset, s_hi, s_lo),
+                        scaled_codes((x >> 3 * kStep) & kMask, kOffset, s_hi, s_lo));
+            }
+        }
+    } else {
+#pragma unroll
+        for (int ps = 0; ps < 2; ps++)
+#pragma unroll
+            for (int q = 0; q < 4; q++)
+#pragma unroll
+                for (int odd = 0; odd < 2; odd++) {            // token 2 t + odd + 8 ps, dims 32 q + 4 g .. + 3
+                    const int tok = 2 * l.t + odd;
+                    const uint32_t sw = odd ? (q < 2 ? r.s[ps].z : r.s[ps].w) : (q < 2 ? r.s[ps].x : r.s[ps].y);
+                    uint32_t s_hi, s_lo;
+                    split_scale(half_of(sw, q & 1), s_hi, s_lo);
+                    uint32_t y;                    // dims i, i + 1 at bits kBits i and 16 + kBits i
+                    if constexpr (kBits == 4) {
+                        const uint32_t w = word_of(r.x[ps], q);
+                        y = odd ? (w >> 16) | ((w >> 4) & 0xFFFF0000u) : (w & 0xFFFFu) | (w << 12);
+                    } else {
+                        const uint32_t b = (word_of(r.x[0], q) >> (16 * odd + 8 * ps)) & 0xFFu;
+                        y = b | (b << 14);
+                    }
+                    store8(block + (q >> 1) * kSub + (uint32_t)(row + tok + 8 * ps) * 128 + (((4 * (q & 1) + (l.g >> 1)) ^ (tok & 7)) << 4) + 8 * (l.g & 1),
+                           scaled_codes(y & kMask, kOffset, s_hi, s_lo), scaled_codes((y >> 2 * kBits) & kMask, kOffset, s_hi, s_lo));
+                }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ attention
+
+// An item in parts that this CTA joins if rows > 0.
+struct Join { int row, rows, head, first, last; };
+
+template <int kTiles>
+struct __align__(16) PromptSmem {
+    static constexpr int kStages = kTiles == 2 ? 2 : 3;
+    uint8_t q[kTiles][kTileBytes], k[kStages][kTileBytes], v[kStages][kTileBytes];
+    uint64_t q_full, q_empty, k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages];
+    uint64_t s_full[kTiles], p_half[kTiles], p_full[kTiles], pv_done[kTiles], o_free[kTiles];
+    uint64_t item_full[2], item_empty[2], joined[2], drain;
+    Item item[2];
+    Join join[2];                                  // of the CTA's first and second item in parts
+    uint32_t tmem, arrived[2];                     // arrived: warps whose share of that part lies in the workspace
+};
+
+// Which of a block's key slots hold a token: pages 8 b .. of the history, of which the last of each kind may be partly filled.
+struct Filled {
+    int ph, pl, pages;
+    uint32_t nh, nl, nw;
+    __device__ __forceinline__ Filled(const volatile Item &it) : nh(it.nh), nl(it.nl), nw(it.nw) {
+        ph = pages_of(nh);
+        pl = pages_of(nl);
+        pages = ph + pl + pages_of(nw);
+    }
+    __device__ __forceinline__ int of_page(int page) const {
+        const int left = page < ph ? (int)nh - 16 * page : page < ph + pl ? (int)nl - 16 * (page - ph) : (int)nw - 16 * (page - ph - pl);
+        return min(16, max(0, left));
+    }
+    __device__ __forceinline__ bool whole_block(int b) const {
+        return 8 * b + 8 <= pages && !((nh & 15) && (ph - 1) >> 3 == b) && !((nl & 15) && (ph + pl - 1) >> 3 == b) &&
+               !((nw & 15) && (pages - 1) >> 3 == b);
+    }
+};
+
+// All parts of an item lie in the workspace: its rows, by the softmax warps, four dims of a row a thread.
+template <int kTiles>
+__device__ __forceinline__ void join_parts(const PromptParams &p, const Join &j, int tid) {
+    using namespace umma;
+    constexpr int kRows = kTiles * kTileRows;
+    const size_t heads = (size_t)kGqa * p.n_kv;
+    const int rows = j.rows;
+    for (int u = tid; u < rows * (kDim / 4); u += 128 * kTiles) {
+        const int d = u / rows, r = u - d * rows;
+        float top = -INFINITY, sum = 0.0f;
+        float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+        for (int c = j.first; c <= j.last; c++) {
+            const size_t at = 2 * (size_t)c + (c == j.first);
+            const float2 ml = __ldcg(p.ws.ml + at * kRows + r);
+            const float4 y = __ldcg(p.ws.o + (at * (kDim / 4) + d) * kRows + r);
+            const float next = fmaxf(top, ml.x), ref = next == -INFINITY ? 0.0f : next, a = ex2(top - ref), w = ex2(ml.x - ref);
+            top = next;
+            sum = sum * a + ml.y * w;
+            o.x = o.x * a + y.x * w; o.y = o.y * a + y.y * w; o.z = o.z * a + y.z * w; o.w = o.w * a + y.w * w;
+        }
+        const float inv = 1.0f / sum;
+        const size_t to = (size_t)(j.row + r / kGqa) * heads + kGqa * j.head + (r & 3);
+        *reinterpret_cast<uint2 *>(p.out + to * kDim + 4 * d) = make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+        if (d == 0 && p.lse) p.lse[to] = (top + log2f(sum)) * 0.69314718055994531f;
+    }
+}
+
+template <int kBits, int kTiles>
+__global__ void __launch_bounds__(kThreads, 1)
+prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+              const __grid_constant__ CUtensorMap map_v) {
+    using namespace umma;
+    using Smem = PromptSmem<kTiles>;
+    constexpr int kStages = Smem::kStages, kSoft = 4 * kTiles, kFill = 12 - kSoft;     // softmax and fill warps
+    constexpr int kTokens = kTiles * kTileTokens, kRows = kTiles * kTileRows;
+    extern __shared__ __align__(1024) uint8_t s_raw[];
+    Smem &sm = *reinterpret_cast<Smem *>(s_raw);
+    const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
+    if (tid == 0) {
+        sm.arrived[0] = sm.arrived[1] = 0;
+        bar_init(smem_u32(&sm.q_full), 1);
+        bar_init(smem_u32(&sm.q_empty), 1);
+        bar_init(smem_u32(&sm.drain), 1);
+        for (int i = 0; i < kStages; i++) {
+            bar_init(smem_u32(&sm.k_full[i]), 1 + kFill);
+            bar_init(smem_u32(&sm.k_empty[i]), 1);
+            bar_init(smem_u32(&sm.v_full[i]), 1 + kFill);
+            bar_init(smem_u32(&sm.v_empty[i]), 1);
+        }
+        for (int i = 0; i < kTiles; i++) {
+            bar_init(smem_u32(&sm.s_full[i]), 1);
+            bar_init(smem_u32(&sm.p_half[i]), 4);
+            bar_init(smem_u32(&sm.p_full[i]), 4);
+            bar_init(smem_u32(&sm.pv_done[i]), 1);
+            bar_init(smem_u32(&sm.o_free[i]), 4);
+        }
+        for (int i = 0; i < 2; i++) {
+            bar_init(smem_u32(&sm.joined[i]), 1);
+            bar_init(smem_u32(&sm.item_full[i]), 1);
+            bar_init(smem_u32(&sm.item_empty[i]), kSoft + 2 + kFill);
+        }
+        bar_init_fence();
+    }
+    constexpr uint32_t kColumns = kTiles * 256, kS = 0, kO = kTiles * 128;       // columns of tile 0; tile 1 is 128 behind
+    if (warp == kSoft) tmem_alloc(smem_u32(&sm.tmem), kColumns);
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = sm.tmem;
+    const long long limit = p.wait_cycles;
+    bool ok = true;
+    pdl_wait();                                    // the plan; and what came before it
+    pdl_launch_dependents();
+    // the CTA's n-th item; false behind the last one or after a wait ran out
+    auto next_item = [&](uint32_t n, Item &it) {
+        const uint32_t slot = n & 1;
+        ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.item_full[slot]), (n >> 1) & 1, limit)) && ok;
+        if (!ok) return false;
+        it = sm.item[slot];
+        __syncwarp();
+        if (lane == 0) bar_arrive(smem_u32(&sm.item_empty[slot]));
+        return it.block >= 0;
+    };
+    auto tiles_of = [&](const Item &it) { return kTiles == 2 && it.block * kTokens + kTileTokens < it.nq ? 2 : 1; };
+
+    // 512 threads x 128 registers at launch = 128 x (2 x 176 + 72 + 88) or 128 x (200 + 88 + 2 x 112)
+    if (warp >= kSoft + 4) {
+        if constexpr (kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+        else asm volatile("setmaxnreg.dec.sync.aligned.u32 112;");
+        // ================================================= fill
+        const int w = warp - kSoft - 4;
+        Item it;
+        uint32_t g = 0;                            // blocks so far
+        for (uint32_t n = 0; next_item(n, it); n++) {
+            const Filled f(it);
+            const uint32_t *tbl_high = p.tbl_high + (size_t)it.slot * p.max_pages, *tbl_low = p.tbl_low + (size_t)it.slot * p.max_pages;
+            const uint32_t ring = p.ring_first + it.slot * p.ring_pages;
+            const int b1 = min(it.b1, it.hist);
+            // the pages of four blocks at a time, a lane each: kind << 30 | id
+            auto entries = [&](int b) {
+                const int page = 8 * b + lane;
+                if (page >= f.pages || b >= b1) return kPageNone << 30;
+                const bool high = page < f.ph || page >= f.ph + f.pl;
+                const uint32_t id = page < f.ph ? __ldg(tbl_high + page) : high ? ring + (uint32_t)(page - f.ph - f.pl) : __ldg(tbl_low + page - f.ph);
+                if (id < (high ? p.high_limit : p.cap_low)) return (high ? kPageHigh << 30 : kPageLow << 30) | id;
+                atomicOr(p.status, PASK_DEV_INTERNAL);         // never expected
+                return kPageBad << 30;
+            };
+            uint32_t window = entries(it.b0);
+            // (The warps pass through every block, those that are copied too: a barrier's phase is only told from the next but one
+            // by who has to arrive on it.)
+            for (int b = it.b0; b < it.b1; b++, g++) {
+                const int in = (b - it.b0) & 3, pages = b < b1 ? kBlockPages : 0;
+                const uint32_t st = g % kStages, ph = (g / kStages - 1) & 1;
+#pragma unroll 1
+                for (int kv = 0; kv < 2; kv++) {
+                    const uint32_t block = smem_u32(kv ? sm.v[st] : sm.k[st]);
+                    bool waited = g < kStages;
+                    auto wait_free = [&] {
+                        if (!waited) ok = __all_sync(0xffffffffu, bar_wait(smem_u32(kv ? &sm.v_empty[st] : &sm.k_empty[st]), ph, limit));
+                        waited = true;
+                        return ok;
+                    };
+#pragma unroll 1
+                    for (int pg = w; pg < pages && ok; pg += kFill) {
+                        const uint32_t e = __shfl_sync(0xffffffffu, window, 8 * in + pg);
+                        const uint32_t kind = e >> 30, id = e & 0x3FFFFFFFu;
+                        // (what is read travels while the place is waited for)
+                        if (kind == kPageHigh) {
+                            const uint8_t *src = p.pool_high + (size_t)id * p.high_page_bytes + (size_t)it.head * kHighHeadBytes;
+                            Raw r;
+                            if (kv) load_high<false>(r, src, lane); else load_high<true>(r, src, lane);
+                            if (!wait_free()) break;
+                            if (kv) store_high<false>(r, block, 16 * pg, lane); else store_high<true>(r, block, 16 * pg, lane);
+                        } else if (kind == kPageLow) {
+                            const uint8_t *src = p.pool_low + (size_t)id * p.low_page_bytes + (size_t)it.head * p.low_head_bytes;
+                            Raw r;
+                            if (kv) load_low<kBits, false>(r, src, lane); else load_low<kBits, true>(r, src, lane);
+                            if (!wait_free()) break;
+                            if (kv) store_low<kBits, false>(r, block, 16 * pg, lane); else store_low<kBits, true>(r, block, 16 * pg, lane);
+                        } else if (!wait_free()) {
+                            break;
+                        }
+                        // slots without a token: whatever the page holds there counts as zero
+                        const int have = kind == kPageNone ? 16 : kind == kPageBad ? 0 : f.of_page(8 * b + pg);
+                        if (have < 16) {
+                            __syncwarp();
+                            for (int i = lane; i < (16 - have) * 16; i += 32)
+                                store16(block + ((i >> 3) & 1) * kSub + (uint32_t)(16 * pg + have + (i >> 4)) * 128 + (i & 7) * 16, 0, 0, 0, 0);
+                        }
+                    }
+                    if (ok) wait_free();
+                    if (!ok) break;
+                    fence_async_shared();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(smem_u32(kv ? &sm.v_full[st] : &sm.k_full[st]));
+                }
+                if (!ok) break;
+                if (in == 3) window = entries(b + 1);
+            }
+            if (!ok) break;
+        }
+    } else if (warp >= kSoft) {
+        if constexpr (kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        else asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+        if (warp == kSoft + 2) {
+            // ================================================= items
+            Walker walk;
+            walk.init(p, kTokens, lane);
+            bool live = true;
+            for (uint32_t n = 0; live; n++) {
+                const uint32_t slot = n & 1;
+                Item it;
+                live = walk.next(it, lane);
+                if (!live) it.block = -1;
+                if (n >= 2) ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.item_empty[slot]), ((n >> 1) - 1) & 1, limit));
+                if (!ok) break;
+                if (lane == 0) {
+                    sm.item[slot] = it;
+                    bar_arrive(smem_u32(&sm.item_full[slot]));
+                }
+                __syncwarp();
+            }
+        } else if (warp == kSoft + 1) {
+            // ================================================= copies
+            Item it;
+            uint32_t g = 0, qc = 0;                // blocks, items so far
+            const uint32_t qf = smem_u32(&sm.q_full);
+            for (uint32_t n = 0; next_item(n, it); n++) {
+                if (qc > 0) ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.q_empty), (qc - 1) & 1, limit));
+                if (!ok) break;
+                const bool mine = elect_one();
+                const int nt = tiles_of(it), first = it.q0 + it.block * kTokens;
+                if (mine) {
+                    bar_expect(qf, nt * kTileBytes + (qc == 0 ? p.surplus : 0u));
+                    for (int t = 0; t < nt; t++)
+                        for (int c = 0; c < 2; c++) tile_load3(smem_u32(sm.q[t]) + c * kSub, &map_q, 64 * c, kGqa * it.head, first + t * kTileTokens, qf);
+                }
+                qc++;
+                for (int b = it.b0; b < it.b1; b++, g++) {
+                    const uint32_t st = g % kStages, round = g / kStages;
+                    const int row = it.q0 + (b - it.hist) * kBlockK;
+#pragma unroll
+                    for (int kv = 0; kv < 2; kv++) {
+                        if (g >= kStages)
+                            ok = __all_sync(0xffffffffu, bar_wait(smem_u32(kv ? &sm.v_empty[st] : &sm.k_empty[st]), (round - 1) & 1, limit));
+                        if (!ok) break;
+                        const uint32_t full = smem_u32(kv ? &sm.v_full[st] : &sm.k_full[st]), dst = smem_u32(kv ? sm.v[st] : sm.k[st]);
+                        if (!mine) continue;
+                        if (b < it.hist) { bar_arrive(full); continue; }
+                        bar_expect(full, kTileBytes);
+                        for (int c = 0; c < 2; c++) tile_load3(dst + c * kSub, kv ? &map_v : &map_k, 64 * c, it.head, row, full);
+                    }
+                    if (!ok) break;
+                }
+                if (!ok) break;
+            }
+            if (!ok) {                             // gave up: let the copies in flight land (bounded) before the CTA ends
+                if (qc) bar_wait(qf, (qc - 1) & 1, limit);
+                for (uint32_t b = g >= kStages ? g - kStages + 1 : 0; b <= g; b++) {
+                    bar_wait(smem_u32(&sm.k_full[b % kStages]), (b / kStages) & 1, limit);
+                    bar_wait(smem_u32(&sm.v_full[b % kStages]), (b / kStages) & 1, limit);
+                }
+            }
+        } else if (warp == kSoft) {
+            // ================================================= products
+            constexpr uint32_t kIdS = instr(kTileRows, kBlockK, false, false), kIdO = instr(kTileRows, kDim, false, true);
+            const bool mine = elect_one();
+            const uint64_t dq = desc(smem_u32(sm.q[0]), 0, 1024), dk = desc(smem_u32(sm.k[0]), 0, 1024), dv = desc(smem_u32(sm.v[0]), kSub, 1024);
+            Item it;
+            uint32_t g = 0, qc = 0, pc[kTiles] = {}, oc[kTiles] = {};            // blocks, items, weights and items of each tile so far
+            auto scores = [&](int t, uint32_t st) {
+                const uint64_t a = dq + (uint64_t)(t * kTileBytes >> 4), b = dk + (uint64_t)(st * (kTileBytes >> 4));
+                __syncwarp();
+#pragma unroll 1
+                for (int c = 0; c < 2; c++)
+#pragma unroll
+                    for (int k = 0; k < 4; k++) mma_ss(tmem + kS + t * 128, a + c * (kSub >> 4) + 2 * k, b + c * (kSub >> 4) + 2 * k, kIdS, c > 0 || k > 0, mine);
+                if (mine) commit(smem_u32(&sm.s_full[t]));
+                __syncwarp();
+            };
+            auto values = [&](int t, uint32_t st, bool fresh, int from, int steps) {       // half of the keys
+                const uint64_t b = dv + (uint64_t)(st * (kTileBytes >> 4)) + 128 * from;
+                __syncwarp();
+#pragma unroll
+                for (int k = 0; k < 4; k++)
+                    if (from + k < steps)
+                        mma_ts(tmem + kO + t * 128, tmem + kS + t * 128 + (from + k) * 8, b + 128 * k, kIdO, from + k > 0 || !fresh, mine);
+            };
+            for (uint32_t n = 0; next_item(n, it); n++) {
+                // (what branches around products depend on has to be uniform for the compiler too: a warp that is not together issues
+                // a product once for each part of it)
+                const int nt = __shfl_sync(0xffffffffu, tiles_of(it), 0), nb = __shfl_sync(0xffffffffu, it.b1 - it.b0, 0);
+                ok = bar_wait(smem_u32(&sm.q_full), qc & 1, limit);
+                qc++;
+                ok = bar_wait(smem_u32(&sm.k_full[g % kStages]), (g / kStages) & 1, limit) && ok;
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                fence_after();
+                {
+                    const uint32_t st = __shfl_sync(0xffffffffu, g % kStages, 0);
+                    scores(0, st);
+                    if (kTiles == 2 && nt == 2) scores(kTiles - 1, st);
+                    if (mine) {
+                        commit(smem_u32(&sm.k_empty[st]));
+                        if (nb == 1) commit(smem_u32(&sm.q_empty));
+                    }
+                    __syncwarp();
+                }
+                const int pages = pages_of(it.nh) + pages_of(it.nl) + pages_of(it.nw);
+                for (int j = 0; j < nb; j++, g++) {
+                    const int b = it.b0 + j, left = b < it.hist ? (pages - kBlockPages * b) * kPageTokens : it.nq - (b - it.hist) * kBlockK;
+                    const int valid = __shfl_sync(0xffffffffu, min(kBlockK, left), 0), steps = (valid + 15) / 16;
+                    const uint32_t st = __shfl_sync(0xffffffffu, g % kStages, 0), ph = (g / kStages) & 1;
+                    const uint32_t st1 = __shfl_sync(0xffffffffu, (g + 1) % kStages, 0), ph1 = ((g + 1) / kStages) & 1;
+                    bool have_k = false;
+                    ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.v_full[st]), ph, limit));
+                    if (!ok) break;
+                    if (valid & 15) {              // the call's own rows behind the last token in its step of 16 count as zero
+                        const int rows = 16 * steps - valid;
+                        for (int e = lane; e < rows * 16; e += 32)
+                            *reinterpret_cast<uint4 *>(sm.v[st] + ((e >> 3) & 1) * kSub + (valid + (e >> 4)) * 128 + (e & 7) * 16) =
+                                make_uint4(0, 0, 0, 0);
+                        fence_async_shared();
+                        __syncwarp();
+                    }
+#pragma unroll
+                    for (int t = 0; t < kTiles; t++) {
+                        if (t >= nt) continue;
+                        if (j == 0) {              // the item before has been read out of O
+                            if (oc[t] > 0) ok = bar_wait(smem_u32(&sm.o_free[t]), (oc[t] - 1) & 1, limit) && ok;
+                            oc[t]++;
+                        }
+                        ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.p_half[t]), pc[t] & 1, limit) && ok);
+                        if (!ok) break;
+                        fence_after();
+                        values(t, st, j == 0, 0, steps);
+                        ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.p_full[t]), pc[t] & 1, limit));
+                        if (!ok) break;
+                        pc[t]++;
+                        fence_after();
+                        values(t, st, false, 4, steps);
+                        if (mine) {
+                            if (t + 1 == nt) commit(smem_u32(&sm.v_empty[st]));
+                            if (j + 1 == nb) commit(smem_u32(&sm.pv_done[t]));
+                        }
+                        __syncwarp();
+                        if (j + 1 < nb) {
+                            if (!have_k) {
+                                ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.k_full[st1]), ph1, limit));
+                                if (!ok) break;
+                                fence_after();
+                                have_k = true;
+                            }
+                            scores(t, st1);
+                        }
+                    }
+                    if (!ok) break;
+                    if (mine) {
+                        if (j + 1 < nb) commit(smem_u32(&sm.k_empty[st1]));
+                        if (j + 2 == nb) commit(smem_u32(&sm.q_empty));
+                    }
+                    __syncwarp();
+                }
+                if (!ok) break;
+            }
+            if (!ok) {                             // gave up: the products in flight end before tensor memory is freed
+                if (mine) commit(smem_u32(&sm.drain));
+                bar_wait(smem_u32(&sm.drain), 0, limit);
+            }
+            __syncwarp();
+        }
+    } else {
+        if constexpr (kTiles == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
+        else asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
+        // ================================================= softmax: thread = row
+        const int t = warp >> 2;
+        const uint32_t base = tmem + ((uint32_t)((warp & 3) * 32) << 16) + t * 128;
+        const uint32_t s_full = smem_u32(&sm.s_full[t]), p_half = smem_u32(&sm.p_half[t]), p_full = smem_u32(&sm.p_full[t]),
+                       pv_done = smem_u32(&sm.pv_done[t]);
+        const int row_in = t * kTileRows + (warp & 3) * 32 + lane;
+        uint32_t sc = 0, ic = 0, jc = 0;           // blocks of this tile (S, P and P V alike), items, items in parts so far
+        // (the item stays in shared memory until its end: a copy of it and the row of S do not fit the registers)
+        for (uint32_t n = 0;; n++) {
+            if (n > 0) {
+                __syncwarp();
+                if (lane == 0) bar_arrive(smem_u32(&sm.item_empty[(n - 1) & 1]));
+            }
+            ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.item_full[n & 1]), (n >> 1) & 1, limit)) && ok;
+            const volatile Item &it = sm.item[n & 1];
+            if (!ok || it.block < 0) break;
+            const int i = it.block * kTokens + row_in / kGqa, hist = it.hist, b0 = it.b0;
+            const bool here = t == 0 || it.block * kTokens + kTileTokens < it.nq, live = i < it.nq;
+            const int nb = here ? it.b1 - b0 : 0;
+            const bool idle = !__any_sync(0xffffffffu, live);          // no row of this warp is one
+            float m = -INFINITY, l = 0.0f;
+            for (int j = 0; j < nb; j++, sc++) {
+                const int b = b0 + j;
+                ok = bar_wait(s_full, sc & 1, limit);
+                if (!__all_sync(0xffffffffu, ok)) break;
+                if (idle) {
+                    if (lane == 0) { bar_arrive(p_half); bar_arrive(p_full); }
+                    continue;
+                }
+                fence_after();
+                float x[128];
+#pragma unroll
+                for (int c = 0; c < 4; c++) {
+                    uint32_t r[32];
+                    tmem_ld32(base + kS + 32 * c, r);
+#pragma unroll
+                    for (int e = 0; e < 32; e++) x[32 * c + e] = __uint_as_float(r[e]);
+                }
+                tmem_wait_ld();
+                if (b >= hist) {                   // the call's own tokens: those up to the row's
+                    const int left = live ? i + 1 - (b - hist) * kBlockK : 0;
+                    if (__any_sync(0xffffffffu, left < kBlockK)) {
+#pragma unroll
+                        for (int e = 0; e < 128; e++) if (e >= left) x[e] = -INFINITY;
+                    }
+                } else if (const Filled f(it); !f.whole_block(b)) {
+                    const uint32_t mine = (1u << f.of_page(8 * b + (lane & 7))) - 1u;
+#pragma unroll
+                    for (int pg = 0; pg < 8; pg++) {
+                        const uint32_t bits = __shfl_sync(0xffffffffu, mine, pg);
+#pragma unroll
+                        for (int e = 0; e < 16; e++) if (!((bits >> e) & 1)) x[16 * pg + e] = -INFINITY;
+                    }
+                }
+                float top = -INFINITY;
+                {
+                    float a0 = x[0], a1 = x[1], a2 = x[2], a3 = x[3];
+#pragma unroll
+                    for (int e = 4; e < 128; e += 4) {
+                        a0 = fmaxf(a0, x[e]); a1 = fmaxf(a1, x[e + 1]); a2 = fmaxf(a2, x[e + 2]); a3 = fmaxf(a3, x[e + 3]);
+                    }
+                    top = fmaxf(fmaxf(a0, a1), fmaxf(a2, a3)) * kScaleLog2;
+                }
+                const bool raise = top > m + kLazy;
+                if (__any_sync(0xffffffffu, raise)) {
+                    const float d = raise ? ex2(m - top) : 1.0f;
+                    if (raise) { m = top; l *= d; }
+                    if (j > 0) {                   // O so far, in the new reference (complete: this S was issued behind it)
+#pragma unroll 1
+                        for (int c = 0; c < 8; c++) {
+                            uint32_t r[16];
+                            tmem_ld16(base + kO + 16 * c, r);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int e = 0; e < 16; e++) r[e] = __float_as_uint(__uint_as_float(r[e]) * d);
+                            tmem_st16(base + kO + 16 * c, r);
+                        }
+                    }
+                }
+                const float ref = m == -INFINITY ? 0.0f : m;               // a row that has seen no key yet
+                const uint64_t scale2 = pair(kScaleLog2, kScaleLog2), ref2 = pair(-ref, -ref);
+                uint64_t l2 = pair(0.0f, 0.0f);
+                // Weights go out in two halves: the product over the first 64 keys runs beside the other exponentials.
+#pragma unroll
+                for (int c = 0; c < 4; c++) {
+                    uint32_t r[16];
+#pragma unroll
+                    for (int e = 0; e < 16; e++) {
+                        float u, v;
+                        unpair(fma2(pair(x[32 * c + 2 * e], x[32 * c + 2 * e + 1]), scale2, ref2), u, v);
+                        u = ex2(u);
+                        v = ex2(v);
+                        l2 = add2(l2, pair(u, v));
+                        r[e] = pack_bf16(u, v);
+                    }
+                    tmem_st16(base + kS + 16 * c, r);
+                    if (c & 1) {
+                        tmem_wait_st();
+                        fence_before();
+                        __syncwarp();
+                        if (lane == 0) bar_arrive(c == 1 ? p_half : p_full);
+                    }
+                }
+                float l0, l1;
+                unpair(l2, l0, l1);
+                l += l0 + l1;
+            }
+            ok = __all_sync(0xffffffffu, ok);
+            if (ok && here) ok = __all_sync(0xffffffffu, bar_wait(pv_done, ic++ & 1, limit));
+            if (!ok) break;
+            fence_after();
+            const size_t heads = (size_t)kGqa * p.n_kv, row = (size_t)(it.q0 + i) * heads + kGqa * it.head + (row_in & 3);
+            const bool whole = it.first == it.last;
+            const size_t part = 2 * (size_t)blockIdx.x + (it.first == (int)blockIdx.x);      // the place of a CTA's part of an item
+            if (here && !idle) {
+                const float inv = live ? 1.0f / l : 0.0f;
+#pragma unroll
+                for (int c = 0; c < 8; c++) {
+                    uint32_t r[16];
+                    tmem_ld16(base + kO + 16 * c, r);
+                    tmem_wait_ld();
+                    if (whole && live) {
+                        uint4 *dst = reinterpret_cast<uint4 *>(p.out + row * kDim + 16 * c);
+#pragma unroll
+                        for (int h = 0; h < 2; h++) {
+                            uint32_t y[4];
+#pragma unroll
+                            for (int e = 0; e < 4; e++)
+                                y[e] = pack_bf16(__uint_as_float(r[8 * h + 2 * e]) * inv, __uint_as_float(r[8 * h + 2 * e + 1]) * inv);
+                            dst[h] = make_uint4(y[0], y[1], y[2], y[3]);
+                        }
+                    } else if (live) {
+#pragma unroll
+                        for (int h = 0; h < 4; h++)
+                            __stcg(p.ws.o + (part * (kDim / 4) + 4 * c + h) * kRows + row_in,
+                                   make_float4(__uint_as_float(r[4 * h]), __uint_as_float(r[4 * h + 1]), __uint_as_float(r[4 * h + 2]), __uint_as_float(r[4 * h + 3])));
+                    }
+                }
+                if (live) {
+                    if (!whole) __stcg(p.ws.ml + part * kRows + row_in, make_float2(m, l));
+                    else if (p.lse) p.lse[row] = (m + log2f(l)) * 0.69314718055994531f;
+                }
+            }
+            if (here) {
+                fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(smem_u32(&sm.o_free[t]));
+            }
+            if (whole) continue;
+            // ---- a part of an item (a CTA's first, its last or both): the last of its CTAs to come here joins them, below
+            __threadfence();
+            __syncwarp();
+            if (lane == 0 && atomicAdd(&sm.arrived[jc], 1) == kSoft - 1) {
+                __threadfence();
+                const bool last = atomicAdd(p.ws.arrived + it.first, 1) == (uint32_t)(it.last - it.first);
+                __threadfence();
+                Join &to = sm.join[jc];
+                to.row = it.q0 + it.block * kTokens;
+                to.rows = last ? min(kRows, (it.nq - it.block * kTokens) * kGqa) : 0;
+                to.head = it.head; to.first = it.first; to.last = it.last;
+                bar_arrive(smem_u32(&sm.joined[jc]));
+            }
+            jc++;
+        }
+        for (uint32_t k = 0; k < jc && ok; k++) {
+            ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.joined[k]), 0, limit));
+            if (ok && sm.join[k].rows) {
+                __threadfence();
+                join_parts<kTiles>(p, sm.join[k], tid);
+            }
+        }
+    }
+    if (!ok && lane == 0) atomicOr(p.status, PASK_DEV_TIMEOUT);
+    fence_before();
+    __syncthreads();
+    fence_after();
+    if (warp == kSoft) tmem_free(tmem, kColumns);
+}
+
+template <int kBits, int kTiles>
+pask_status_t launch(const PromptParams &p, const CUtensorMap &map_q, const CUtensorMap &map_k, const CUtensorMap &map_v, int dev, cudaStream_t stream) {
+    constexpr int kSmem = (int)sizeof(PromptSmem<kTiles>);
+    static_assert(kSmem <= 232448, "shared memory of a CTA");
+    static bool granted[64] = {};                  // a property of (device, kernel)
+    if (!granted[dev]) {
+        if (cudaFuncSetAttribute(prompt_kernel<kBits, kTiles>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess) return PASK_ERR_CUDA;
+        granted[dev] = true;
+    }
+    return launch_pdl(prompt_kernel<kBits, kTiles>, dim3(p.grid), dim3(kThreads), kSmem, stream, p, map_q, map_k, map_v) == cudaSuccess ? PASK_OK
+                                                                                                                                     : PASK_ERR_CUDA;
+}
+
+// One tile of 32 tokens or two of 64 in a CTA
+int tiles_for(int n_seqs, int total_tokens) { return 2; }
+
+}  // namespace
+
+size_t prompt_workspace_bytes(const pask_cache *c, int n_seqs, int total_tokens) {
+    return carve(n_seqs, c->sm_count, tiles_for(n_seqs, total_tokens) * kTileRows, nullptr, nullptr);
+}
+
+pask_status_t launch_prompt(pask_cache *c, int layer, int n_seqs, int total_tokens, const int32_t *seq_ids, const int32_t *cu_tokens, const void *q,
+                            const void *k, const void *v, void *out, float *lse, void *workspace, cudaStream_t stream) {
+    const int n_kv = c->desc.n_kv_heads, tiles = tiles_for(n_seqs, total_tokens);
+    CUtensorMap map_q{}, map_k{}, map_v{};
+    const size_t head = kDim * 2;
+    if (!encode_heads(&map_q, q, kDim, kGqa * n_kv, total_tokens, head, head * kGqa * n_kv, kGqa, kTileTokens) ||
+        !encode_heads(&map_k, k, kDim, n_kv, total_tokens, head, head * n_kv, 1, kBlockK) ||
+        !encode_heads(&map_v, v, kDim, n_kv, total_tokens, head, head * n_kv, 1, kBlockK))
+        return PASK_ERR_CUDA;
+    const DevCache &d = c->dev;
+    PromptParams p{};
+    carve(n_seqs, c->sm_count, tiles * kTileRows, static_cast<uint8_t *>(workspace), &p.ws);
+    p.pool_high = d.pool_high;
+    p.pool_low = d.pool_low;
+    p.tbl_high = d.tbl_high;
+    p.tbl_low = d.tbl_low;
+    p.status = d.ctrl + kCtrlStatus;
+    p.high_page_bytes = d.high_page_bytes;
+    p.low_page_bytes = d.low_page_bytes;
+    p.low_head_bytes = d.low_head_bytes;
+    p.cap_low = d.cap_low;
+    p.high_limit = d.high_limit;
+    p.ring_first = d.cap_high;
+    p.ring_pages = d.window / kPageTokens;
+    p.max_pages = d.max_pages;
+    p.n_kv = n_kv;
+    p.n_seqs = n_seqs;
+    p.grid = c->sm_count;
+    p.out = static_cast<__nv_bfloat16 *>(out);
+    p.lse = lse;
+    p.wait_cycles = c->wait_cycles;
+    p.surplus = c->wait_test_surplus;
+    if (launch_pdl(prompt_plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, d, layer, n_seqs, total_tokens, seq_ids, cu_tokens, p.ws, p.grid,
+                   tiles * kTileTokens, static_cast<uint4 *>(out), lse) != cudaSuccess)
+        return PASK_ERR_CUDA;
+    const auto fn = tiles == 2 ? (d.low_bits == 8 ? launch<8, 2> : d.low_bits == 2 ? launch<2, 2> : launch<4, 2>)
+                               : (d.low_bits == 8 ? launch<8, 1> : d.low_bits == 2 ? launch<2, 1> : launch<4, 1>);
+    return fn(p, map_q, map_k, map_v, c->device, stream);
+}
+
+}  // namespace pask
