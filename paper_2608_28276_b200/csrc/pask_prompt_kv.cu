@@ -52,10 +52,13 @@ struct __align__(16) PromptSeq {
 };
 static_assert(sizeof(PromptSeq) == 32, "two 16-byte loads");
 
+// An item in parts: its rows (none: there is no such item), the CTAs that have one.
+struct Join { int row, rows, head, first, last; };
+
 struct PromptWorkspace {
     uint64_t *prefix;                              // [n_seqs + 1] cost (or CTAs) of the sequences before
     PromptSeq *seqs;                               // [n_seqs]
-    uint32_t *arrived;                             // [grid] parts of the item that begins with this CTA's part
+    Join *joins;                                   // [grid] the item in parts that begins with this CTA's part
     float2 *ml;                                    // [2 grid][rows] reference maximum in log2 units, sum
     float4 *o;                                     // [2 grid][32][rows] unscaled outputs, four dims a piece
 };
@@ -63,12 +66,12 @@ struct PromptWorkspace {
 size_t carve(int n_seqs, int grid, int rows, uint8_t *base, PromptWorkspace *ws) {
     size_t off = 0;
     auto take = [&](size_t bytes) { size_t at = off; off = (off + bytes + 255) / 256 * 256; return at; };
-    const size_t o_prefix = take((size_t)(n_seqs + 1) * 8), o_seqs = take((size_t)n_seqs * sizeof(PromptSeq)), o_arr = take((size_t)grid * 4);
+    const size_t o_prefix = take((size_t)(n_seqs + 1) * 8), o_seqs = take((size_t)n_seqs * sizeof(PromptSeq)), o_join = take((size_t)grid * sizeof(Join));
     const size_t o_ml = take((size_t)2 * grid * rows * sizeof(float2)), o_o = take((size_t)2 * grid * rows * kDim * 4);
     if (ws) {
         ws->prefix = reinterpret_cast<uint64_t *>(base + o_prefix);
         ws->seqs = reinterpret_cast<PromptSeq *>(base + o_seqs);
-        ws->arrived = reinterpret_cast<uint32_t *>(base + o_arr);
+        ws->joins = reinterpret_cast<Join *>(base + o_join);
         ws->ml = reinterpret_cast<float2 *>(base + o_ml);
         ws->o = reinterpret_cast<float4 *>(base + o_o);
     }
@@ -100,7 +103,7 @@ __host__ __device__ __forceinline__ long long own_blocks_before(int j, int token
 
 constexpr int kPlanThreads = 1024;
 
-// One CTA, a sequence a thread: what each has to attend, the line of costs, the parts' counters.
+// One CTA, a sequence a thread: what each has to attend, the line of costs.
 __global__ void __launch_bounds__(kPlanThreads)
 prompt_plan_kernel(DevCache c, int layer, int n_seqs, int total, const int32_t *__restrict__ seq_ids, const int32_t *__restrict__ cu,
                    PromptWorkspace ws, int grid, int block_tokens, uint4 *__restrict__ out, float *__restrict__ lse) {
@@ -110,7 +113,6 @@ prompt_plan_kernel(DevCache c, int layer, int n_seqs, int total, const int32_t *
     pdl_launch_dependents();
     pdl_wait();
     if (tid == 0) s_items = s_longest = s_bad = 0;
-    for (int i = tid; i < grid; i += kPlanThreads) ws.arrived[i] = 0;
     __syncthreads();
     PromptSeq s{};
     uint32_t bad = 0;
@@ -133,11 +135,12 @@ prompt_plan_kernel(DevCache c, int layer, int n_seqs, int total, const int32_t *
                 const uint4 *act = reinterpret_cast<const uint4 *>(c.win_act + (size_t)s.slot * c.window);
                 for (uint32_t i = 0; 16 * i < s.nw; i++) {
                     const uint4 a = act[i];
-                    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-                    for (uint32_t e = 0; e < 16 && 16 * i + e < s.nw; e++) {
-                        const uint32_t action = (w[e >> 2] >> (8 * (e & 3))) & 0xFF;
-                        if (action == PASK_ACTION_RETAIN_HIGH) s.nh--;
-                        if (action == PASK_ACTION_RETAIN_LOW) s.nl--;
+                    const uint32_t w[4] = {a.x, a.y, a.z, a.w}, in = min(16u, s.nw - 16 * i);
+#pragma unroll
+                    for (uint32_t e = 0; e < 4; e++) {         // actions are 0, 1, 2: bit 0 of a byte says LOW, bit 1 HIGH
+                        const uint32_t have = in > 4 * e ? in - 4 * e : 0, member = have >= 4 ? 0xFFFFFFFFu : (1u << (8 * have)) - 1u;
+                        s.nl -= __popc(w[e] & member & 0x01010101u);
+                        s.nh -= __popc(w[e] & member & 0x02020202u);
                     }
                 }
             }
@@ -321,7 +324,7 @@ struct Walker {
 constexpr uint32_t kPageLow = 0, kPageBad = 1, kPageHigh = 2, kPageNone = 3;       // kinds of a page: bits 30, 31 of its entry
 
 // A page's key / value rows of one head as they are stored, a lane's share in registers.
-struct Raw { uint4 x[8]; uint4 s[2]; };
+struct Raw { uint4 x[8]; };                        // (low precision: codes, then scales in x[4], x[5])
 
 // (code - kZero) * scale for two codes, as bf16, rounded once: the difference is exact, the scale is the sum of two bf16 numbers of which the
 // smaller has three bits, so that its product with a code is exact and one fma rounds the sum of both products.
@@ -408,10 +411,10 @@ __device__ __forceinline__ void load_low(Raw &r, const uint8_t *head, int lane) 
     const uint8_t *scales = half + 512 * L::kRounds;
     if (kKeys) {                                   // tokens g and g + 8
         const uint2 a = __ldg(reinterpret_cast<const uint2 *>(scales) + l.g), b = __ldg(reinterpret_cast<const uint2 *>(scales) + l.g + 8);
-        r.s[0] = make_uint4(a.x, a.y, b.x, b.y);
+        r.x[4] = make_uint4(a.x, a.y, b.x, b.y);
     } else {                                       // tokens 2 t, 2 t + 1 and 8 on
-        r.s[0] = __ldg(reinterpret_cast<const uint4 *>(scales) + l.t);
-        r.s[1] = __ldg(reinterpret_cast<const uint4 *>(scales) + l.t + 4);
+        r.x[4] = __ldg(reinterpret_cast<const uint4 *>(scales) + l.t);
+        r.x[5] = __ldg(reinterpret_cast<const uint4 *>(scales) + l.t + 4);
     }
 }
 
@@ -428,7 +431,7 @@ __device__ __forceinline__ void store_low(const Raw &r, uint32_t block, int row,
         for (int rr = 0; rr < 4; rr++)             // group rr: k-chunks 2 rr, 2 rr + 1 of 16 dims
 #pragma unroll
             for (int hi = 0; hi < 2; hi++) {       // tokens g, g + 8
-                const float s = half_bits(half_of(hi ? (rr < 2 ? r.s[0].z : r.s[0].w) : (rr < 2 ? r.s[0].x : r.s[0].y), rr & 1));
+                const float s = half_bits(half_of(hi ? (rr < 2 ? r.x[4].z : r.x[4].w) : (rr < 2 ? r.x[4].x : r.x[4].y), rr & 1));
                 const uint32_t base = block + (rr >> 1) * kSub + (uint32_t)(row + l.g + 8 * hi) * 128 + 4 * l.t;
 #pragma unroll
                 for (int k = 0; k < 4; k++) {      // 8 dims each: dims 32 rr + 8 k + 2 t, + 1
@@ -444,7 +447,7 @@ __device__ __forceinline__ void store_low(const Raw &r, uint32_t block, int row,
                 const uint32_t a = ps ? r.x[q].y : r.x[q].x, b = ps ? r.x[q].w : r.x[q].z;
 #pragma unroll
                 for (int odd = 0; odd < 2; odd++) {
-                    const uint32_t sw = odd ? (q < 2 ? r.s[ps].z : r.s[ps].w) : (q < 2 ? r.s[ps].x : r.s[ps].y);
+                    const uint32_t sw = odd ? (q < 2 ? r.x[4 + ps].z : r.x[4 + ps].w) : (q < 2 ? r.x[4 + ps].x : r.x[4 + ps].y);
                     const float s = half_bits(half_of(sw, q & 1));
                     const int tok = 2 * l.t + odd;
                     store8(block + (q >> 1) * kSub + (uint32_t)(row + tok + 8 * ps) * 128 + (((4 * (q & 1) + (l.g >> 1)) ^ (tok & 7)) << 4) + 8 * (l.g & 1),
@@ -459,7 +462,7 @@ __device__ __forceinline__ void store_low(const Raw &r, uint32_t block, int row,
 #pragma unroll
             for (int w = 0; w < 4; w++) {          // group w: dims 32 w + 8 t .. + 7
                 uint32_t s_hi, s_lo;
-                split_scale(half_of(hi ? (w < 2 ? r.s[0].z : r.s[0].w) : (w < 2 ? r.s[0].x : r.s[0].y), w & 1), s_hi, s_lo);
+                split_scale(half_of(hi ? (w < 2 ? r.x[4].z : r.x[4].w) : (w < 2 ? r.x[4].x : r.x[4].y), w & 1), s_hi, s_lo);
                 const uint32_t x = kBits == 4 ? word_of(r.x[hi], w) : word_of(r.x[0], w) >> (8 * hi);
                 constexpr int kStep = kBits;
                 store16(base + (w >> 1) * kSub + (((4 * (w & 1) + l.t) ^ l.g) << 4), scaled_codes(x & kMask, kOffset, s_hi, s_lo),
@@ -475,7 +478,7 @@ __device__ __forceinline__ void store_low(const Raw &r, uint32_t block, int row,
 #pragma unroll
                 for (int odd = 0; odd < 2; odd++) {            // token 2 t + odd + 8 ps, dims 32 q + 4 g .. + 3
                     const int tok = 2 * l.t + odd;
-                    const uint32_t sw = odd ? (q < 2 ? r.s[ps].z : r.s[ps].w) : (q < 2 ? r.s[ps].x : r.s[ps].y);
+                    const uint32_t sw = odd ? (q < 2 ? r.x[4 + ps].z : r.x[4 + ps].w) : (q < 2 ? r.x[4 + ps].x : r.x[4 + ps].y);
                     uint32_t s_hi, s_lo;
                     split_scale(half_of(sw, q & 1), s_hi, s_lo);
                     uint32_t y;                    // dims i, i + 1 at bits kBits i and 16 + kBits i
@@ -494,19 +497,19 @@ __device__ __forceinline__ void store_low(const Raw &r, uint32_t block, int row,
 
 // ------------------------------------------------------------------------------------------------ attention
 
-// An item in parts that this CTA joins if rows > 0.
-struct Join { int row, rows, head, first, last; };
-
-template <int kTiles>
+// kTiles 2: 64 tokens an item.  1: 32 / kCopies tokens, each row of S kCopies times in the tile.
+template <int kTiles, int kCopies>
 struct __align__(16) PromptSmem {
-    static constexpr int kStages = kTiles == 2 ? 2 : 3;
+    static constexpr int kStages = 2;
     uint8_t q[kTiles][kTileBytes], k[kStages][kTileBytes], v[kStages][kTileBytes];
+    float share[kCopies > 1 ? 32 : 1][kTileRows];  // 32 dims of the copies' results on their way to one another
+    float2 ml[kTileRows];
     uint64_t q_full, q_empty, k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages];
-    uint64_t s_full[kTiles], p_half[kTiles], p_full[kTiles], pv_done[kTiles], o_free[kTiles];
-    uint64_t item_full[2], item_empty[2], joined[2], drain;
+    uint64_t s_full[2], p_half[2], p_full[2], pv_done[2], o_free[2];             // of a tile; one tile: the first three of a place of S,
+                                                   // pv_done of a block and of an item's last one
+    uint64_t item_full[2], item_empty[2], copies, drain;
     Item item[2];
-    Join join[2];                                  // of the CTA's first and second item in parts
-    uint32_t tmem, arrived[2];                     // arrived: warps whose share of that part lies in the workspace
+    uint32_t tmem;
 };
 
 // Which of a block's key slots hold a token: pages 8 b .. of the history, of which the last of each kind may be partly filled.
@@ -528,49 +531,21 @@ struct Filled {
     }
 };
 
-// All parts of an item lie in the workspace: its rows, by the softmax warps, four dims of a row a thread.
-template <int kTiles>
-__device__ __forceinline__ void join_parts(const PromptParams &p, const Join &j, int tid) {
-    using namespace umma;
-    constexpr int kRows = kTiles * kTileRows;
-    const size_t heads = (size_t)kGqa * p.n_kv;
-    const int rows = j.rows;
-    for (int u = tid; u < rows * (kDim / 4); u += 128 * kTiles) {
-        const int d = u / rows, r = u - d * rows;
-        float top = -INFINITY, sum = 0.0f;
-        float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 4
-        for (int c = j.first; c <= j.last; c++) {
-            const size_t at = 2 * (size_t)c + (c == j.first);
-            const float2 ml = __ldcg(p.ws.ml + at * kRows + r);
-            const float4 y = __ldcg(p.ws.o + (at * (kDim / 4) + d) * kRows + r);
-            const float next = fmaxf(top, ml.x), ref = next == -INFINITY ? 0.0f : next, a = ex2(top - ref), w = ex2(ml.x - ref);
-            top = next;
-            sum = sum * a + ml.y * w;
-            o.x = o.x * a + y.x * w; o.y = o.y * a + y.y * w; o.z = o.z * a + y.z * w; o.w = o.w * a + y.w * w;
-        }
-        const float inv = 1.0f / sum;
-        const size_t to = (size_t)(j.row + r / kGqa) * heads + kGqa * j.head + (r & 3);
-        *reinterpret_cast<uint2 *>(p.out + to * kDim + 4 * d) = make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
-        if (d == 0 && p.lse) p.lse[to] = (top + log2f(sum)) * 0.69314718055994531f;
-    }
-}
-
-template <int kBits, int kTiles>
+template <int kBits, int kTiles, int kCopies>
 __global__ void __launch_bounds__(kThreads, 1)
 prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
               const __grid_constant__ CUtensorMap map_v) {
     using namespace umma;
-    using Smem = PromptSmem<kTiles>;
+    using Smem = PromptSmem<kTiles, kCopies>;
     constexpr int kStages = Smem::kStages, kSoft = 4 * kTiles, kFill = 12 - kSoft;     // softmax and fill warps
-    constexpr int kTokens = kTiles * kTileTokens, kRows = kTiles * kTileRows;
+    constexpr int kTokens = kTiles * kTileTokens / kCopies, kRows = kTokens * kGqa;
     extern __shared__ __align__(1024) uint8_t s_raw[];
     Smem &sm = *reinterpret_cast<Smem *>(s_raw);
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
     if (tid == 0) {
-        sm.arrived[0] = sm.arrived[1] = 0;
         bar_init(smem_u32(&sm.q_full), 1);
         bar_init(smem_u32(&sm.q_empty), 1);
+        bar_init(smem_u32(&sm.copies), kSoft);
         bar_init(smem_u32(&sm.drain), 1);
         for (int i = 0; i < kStages; i++) {
             bar_init(smem_u32(&sm.k_full[i]), 1 + kFill);
@@ -578,7 +553,7 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
             bar_init(smem_u32(&sm.v_full[i]), 1 + kFill);
             bar_init(smem_u32(&sm.v_empty[i]), 1);
         }
-        for (int i = 0; i < kTiles; i++) {
+        for (int i = 0; i < 2; i++) {
             bar_init(smem_u32(&sm.s_full[i]), 1);
             bar_init(smem_u32(&sm.p_half[i]), 4);
             bar_init(smem_u32(&sm.p_full[i]), 4);
@@ -586,14 +561,14 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
             bar_init(smem_u32(&sm.o_free[i]), 4);
         }
         for (int i = 0; i < 2; i++) {
-            bar_init(smem_u32(&sm.joined[i]), 1);
             bar_init(smem_u32(&sm.item_full[i]), 1);
             bar_init(smem_u32(&sm.item_empty[i]), kSoft + 2 + kFill);
         }
         bar_init_fence();
     }
-    constexpr uint32_t kColumns = kTiles * 256, kS = 0, kO = kTiles * 128;       // columns of tile 0; tile 1 is 128 behind
-    if (warp == kSoft) tmem_alloc(smem_u32(&sm.tmem), kColumns);
+    // Columns.  Two tiles: S (P over it) and O of tile 0, those of tile 1 128 behind.  One tile: two places of S, two of P, O
+    constexpr uint32_t kS = 0, kP = kTiles == 2 ? 0 : 256, kO = kTiles == 2 ? 256 : 384;
+    if (warp == kSoft) tmem_alloc(smem_u32(&sm.tmem), 512);
     fence_before();
     __syncthreads();
     fence_after();
@@ -602,6 +577,7 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
     bool ok = true;
     pdl_wait();                                    // the plan; and what came before it
     pdl_launch_dependents();
+    if (tid == 0) p.ws.joins[blockIdx.x].rows = 0;
     // the CTA's n-th item; false behind the last one or after a wait ran out
     auto next_item = [&](uint32_t n, Item &it) {
         const uint32_t slot = n & 1;
@@ -614,9 +590,9 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
     };
     auto tiles_of = [&](const Item &it) { return kTiles == 2 && it.block * kTokens + kTileTokens < it.nq ? 2 : 1; };
 
-    // 512 threads x 128 registers at launch = 128 x (2 x 176 + 72 + 88) or 128 x (200 + 88 + 2 x 112)
+    // 512 threads x 128 registers at launch = 128 x (2 x 168 + 72 + 104) or 128 x (200 + 88 + 2 x 112)
     if (warp >= kSoft + 4) {
-        if constexpr (kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+        if constexpr (kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
         else asm volatile("setmaxnreg.dec.sync.aligned.u32 112;");
         // ================================================= fill
         const int w = warp - kSoft - 4;
@@ -637,57 +613,61 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
                 atomicOr(p.status, PASK_DEV_INTERNAL);         // never expected
                 return kPageBad << 30;
             };
-            uint32_t window = entries(it.b0);
+            uint32_t window = entries(it.b0), window_next = entries(it.b0 + 4);
+            // A unit is the keys or the values of one of this warp's pages.  The next one is read while the current one is expanded.
+            Raw next;
+            uint32_t next_kind = kPageNone;
+            auto load = [&](int b, int kv, int i) {
+                const int in = (b - it.b0) & 3;
+                if (in == 0 && kv == 0 && i == 0 && b != it.b0) { window = window_next; window_next = entries(b + 4); }
+                const uint32_t e = __shfl_sync(0xffffffffu, window, 8 * in + w + i * kFill), id = e & 0x3FFFFFFFu;
+                next_kind = e >> 30;
+                if (next_kind == kPageHigh) {
+                    const uint8_t *src = p.pool_high + (size_t)id * p.high_page_bytes + (size_t)it.head * kHighHeadBytes;
+                    if (kv) load_high<false>(next, src, lane); else load_high<true>(next, src, lane);
+                } else if (next_kind == kPageLow) {
+                    const uint8_t *src = p.pool_low + (size_t)id * p.low_page_bytes + (size_t)it.head * p.low_head_bytes;
+                    if (kv) load_low<kBits, false>(next, src, lane); else load_low<kBits, true>(next, src, lane);
+                }
+            };
+            if (it.b0 < b1) load(it.b0, 0, 0);
             // (The warps pass through every block, those that are copied too: a barrier's phase is only told from the next but one
             // by who has to arrive on it.)
             for (int b = it.b0; b < it.b1; b++, g++) {
-                const int in = (b - it.b0) & 3, pages = b < b1 ? kBlockPages : 0;
                 const uint32_t st = g % kStages, ph = (g / kStages - 1) & 1;
 #pragma unroll 1
                 for (int kv = 0; kv < 2; kv++) {
                     const uint32_t block = smem_u32(kv ? sm.v[st] : sm.k[st]);
-                    bool waited = g < kStages;
-                    auto wait_free = [&] {
-                        if (!waited) ok = __all_sync(0xffffffffu, bar_wait(smem_u32(kv ? &sm.v_empty[st] : &sm.k_empty[st]), ph, limit));
-                        waited = true;
-                        return ok;
-                    };
-#pragma unroll 1
-                    for (int pg = w; pg < pages && ok; pg += kFill) {
-                        const uint32_t e = __shfl_sync(0xffffffffu, window, 8 * in + pg);
-                        const uint32_t kind = e >> 30, id = e & 0x3FFFFFFFu;
-                        // (what is read travels while the place is waited for)
-                        if (kind == kPageHigh) {
-                            const uint8_t *src = p.pool_high + (size_t)id * p.high_page_bytes + (size_t)it.head * kHighHeadBytes;
-                            Raw r;
-                            if (kv) load_high<false>(r, src, lane); else load_high<true>(r, src, lane);
-                            if (!wait_free()) break;
-                            if (kv) store_high<false>(r, block, 16 * pg, lane); else store_high<true>(r, block, 16 * pg, lane);
-                        } else if (kind == kPageLow) {
-                            const uint8_t *src = p.pool_low + (size_t)id * p.low_page_bytes + (size_t)it.head * p.low_head_bytes;
-                            Raw r;
-                            if (kv) load_low<kBits, false>(r, src, lane); else load_low<kBits, true>(r, src, lane);
-                            if (!wait_free()) break;
-                            if (kv) store_low<kBits, false>(r, block, 16 * pg, lane); else store_low<kBits, true>(r, block, 16 * pg, lane);
-                        } else if (!wait_free()) {
-                            break;
-                        }
-                        // slots without a token: whatever the page holds there counts as zero
-                        const int have = kind == kPageNone ? 16 : kind == kPageBad ? 0 : f.of_page(8 * b + pg);
-                        if (have < 16) {
-                            __syncwarp();
-                            for (int i = lane; i < (16 - have) * 16; i += 32)
-                                store16(block + ((i >> 3) & 1) * kSub + (uint32_t)(16 * pg + have + (i >> 4)) * 128 + (i & 7) * 16, 0, 0, 0, 0);
-                        }
-                    }
-                    if (ok) wait_free();
+                    if (g >= kStages) ok = __all_sync(0xffffffffu, bar_wait(smem_u32(kv ? &sm.v_empty[st] : &sm.k_empty[st]), ph, limit));
                     if (!ok) break;
-                    fence_async_shared();
-                    __syncwarp();
+                    if (b < b1) {
+#pragma unroll 1
+                        for (int i = 0; i < kBlockPages / kFill; i++) {
+                            const Raw r = next;
+                            const uint32_t kind = next_kind;
+                            const int page = w + i * kFill;
+                            if (i + 1 < kBlockPages / kFill) load(b, kv, i + 1);
+                            else if (kv == 0) load(b, 1, 0);
+                            else if (b + 1 < b1) load(b + 1, 0, 0);
+                            if (kind == kPageHigh) {
+                                if (kv) store_high<false>(r, block, 16 * page, lane); else store_high<true>(r, block, 16 * page, lane);
+                            } else if (kind == kPageLow) {
+                                if (kv) store_low<kBits, false>(r, block, 16 * page, lane); else store_low<kBits, true>(r, block, 16 * page, lane);
+                            }
+                            // slots without a token: whatever the page holds there counts as zero
+                            const int have = kind == kPageNone ? 16 : kind == kPageBad ? 0 : f.of_page(8 * b + page);
+                            if (have < 16) {
+                                __syncwarp();
+                                for (int e = lane; e < (16 - have) * 16; e += 32)
+                                    store16(block + ((e >> 3) & 1) * kSub + (uint32_t)(16 * page + have + (e >> 4)) * 128 + (e & 7) * 16, 0, 0, 0, 0);
+                            }
+                        }
+                        fence_async_shared();
+                        __syncwarp();
+                    }
                     if (lane == 0) bar_arrive(smem_u32(kv ? &sm.v_full[st] : &sm.k_full[st]));
                 }
                 if (!ok) break;
-                if (in == 3) window = entries(b + 1);
             }
             if (!ok) break;
         }
@@ -725,7 +705,9 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
                 if (mine) {
                     bar_expect(qf, nt * kTileBytes + (qc == 0 ? p.surplus : 0u));
                     for (int t = 0; t < nt; t++)
-                        for (int c = 0; c < 2; c++) tile_load3(smem_u32(sm.q[t]) + c * kSub, &map_q, 64 * c, kGqa * it.head, first + t * kTileTokens, qf);
+                        for (int c = 0; c < 2 * kCopies; c++)
+                            tile_load3(smem_u32(sm.q[t]) + (c & 1) * kSub + (c >> 1) * (kSub / kCopies), &map_q, 64 * (c & 1), kGqa * it.head,
+                                       first + t * kTileTokens, qf);
                 }
                 qc++;
                 for (int b = it.b0; b < it.b1; b++, g++) {
@@ -759,28 +741,42 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
             const bool mine = elect_one();
             const uint64_t dq = desc(smem_u32(sm.q[0]), 0, 1024), dk = desc(smem_u32(sm.k[0]), 0, 1024), dv = desc(smem_u32(sm.v[0]), kSub, 1024);
             Item it;
-            uint32_t g = 0, qc = 0, pc[kTiles] = {}, oc[kTiles] = {};            // blocks, items, weights and items of each tile so far
-            auto scores = [&](int t, uint32_t st) {
-                const uint64_t a = dq + (uint64_t)(t * kTileBytes >> 4), b = dk + (uint64_t)(st * (kTileBytes >> 4));
+            uint32_t g = 0, qc = 0, pc[2] = {}, oc[2] = {};            // blocks, items, weights and items of each tile so far
+            // (One thread issues: a branch around it, not a predicate on each product.  The predicate is taken for uniform over the warp and
+            // looked at once; where the warp was not together, as behind a wait, products were issued once for each part of it.)
+            auto scores = [&](int t, uint32_t st) {            // one tile: t is the place of S
                 __syncwarp();
-#pragma unroll 1
-                for (int c = 0; c < 2; c++)
+                if (mine) {
+                    const uint64_t a = dq + (uint64_t)(kTiles == 2 ? t * kTileBytes >> 4 : 0), b = dk + (uint64_t)(st * (kTileBytes >> 4));
 #pragma unroll
-                    for (int k = 0; k < 4; k++) mma_ss(tmem + kS + t * 128, a + c * (kSub >> 4) + 2 * k, b + c * (kSub >> 4) + 2 * k, kIdS, c > 0 || k > 0, mine);
-                if (mine) commit(smem_u32(&sm.s_full[t]));
+                    for (int k = 0; k < 8; k++)
+                        mma_ss(tmem + kS + t * 128, a + (k >> 2) * (kSub >> 4) + 2 * (k & 3), b + (k >> 2) * (kSub >> 4) + 2 * (k & 3), kIdS, k > 0, true);
+                    commit(smem_u32(&sm.s_full[t]));
+                }
                 __syncwarp();
             };
-            auto values = [&](int t, uint32_t st, bool fresh, int from, int steps) {       // half of the keys
-                const uint64_t b = dv + (uint64_t)(st * (kTileBytes >> 4)) + 128 * from;
+            auto values = [&](int t, uint32_t st, bool fresh, int from, int to) {          // keys 16 from .. 16 to - 1
                 __syncwarp();
+                if (mine) {
+                    const uint64_t b = dv + (uint64_t)(st * (kTileBytes >> 4));
 #pragma unroll
-                for (int k = 0; k < 4; k++)
-                    if (from + k < steps)
-                        mma_ts(tmem + kO + t * 128, tmem + kS + t * 128 + (from + k) * 8, b + 128 * k, kIdO, from + k > 0 || !fresh, mine);
+                    for (int k = 0; k < 8; k++)
+                        if (k >= from && k < to)
+                            mma_ts(tmem + kO + (kTiles == 2 ? t * 128 : 0), tmem + kP + t * (kTiles == 2 ? 128 : 64) + k * 8, b + 128 * k, kIdO,
+                                   k > 0 || !fresh, true);
+                }
+                __syncwarp();
+            };
+            // the call's own rows behind the last token in its step of 16 count as zero
+            auto zero_rows = [&](uint32_t st, int valid, int steps) {
+                if (!(valid & 15)) return;
+                const int rows = 16 * steps - valid;
+                for (int e = lane; e < rows * 16; e += 32)
+                    *reinterpret_cast<uint4 *>(sm.v[st] + ((e >> 3) & 1) * kSub + (valid + (e >> 4)) * 128 + (e & 7) * 16) = make_uint4(0, 0, 0, 0);
+                fence_async_shared();
+                __syncwarp();
             };
             for (uint32_t n = 0; next_item(n, it); n++) {
-                // (what branches around products depend on has to be uniform for the compiler too: a warp that is not together issues
-                // a product once for each part of it)
                 const int nt = __shfl_sync(0xffffffffu, tiles_of(it), 0), nb = __shfl_sync(0xffffffffu, it.b1 - it.b0, 0);
                 ok = bar_wait(smem_u32(&sm.q_full), qc & 1, limit);
                 qc++;
@@ -790,8 +786,8 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
                 fence_after();
                 {
                     const uint32_t st = __shfl_sync(0xffffffffu, g % kStages, 0);
-                    scores(0, st);
-                    if (kTiles == 2 && nt == 2) scores(kTiles - 1, st);
+                    scores(kTiles == 2 ? 0 : __shfl_sync(0xffffffffu, g & 1, 0), st);
+                    if (kTiles == 2 && nt == 2) scores(1, st);
                     if (mine) {
                         commit(smem_u32(&sm.k_empty[st]));
                         if (nb == 1) commit(smem_u32(&sm.q_empty));
@@ -804,17 +800,42 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
                     const int valid = __shfl_sync(0xffffffffu, min(kBlockK, left), 0), steps = (valid + 15) / 16;
                     const uint32_t st = __shfl_sync(0xffffffffu, g % kStages, 0), ph = (g / kStages) & 1;
                     const uint32_t st1 = __shfl_sync(0xffffffffu, (g + 1) % kStages, 0), ph1 = ((g + 1) / kStages) & 1;
+                    if constexpr (kTiles == 1) {
+                        // S of the next block goes to the other place while the softmax has this one
+                        const int at = __shfl_sync(0xffffffffu, g & 1, 0);
+                        if (j + 1 < nb) {
+                            ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.k_full[st1]), ph1, limit));
+                            if (!ok) break;
+                            fence_after();
+                            scores(at ^ 1, st1);
+                            if (mine) {
+                                commit(smem_u32(&sm.k_empty[st1]));
+                                if (j + 2 == nb) commit(smem_u32(&sm.q_empty));
+                            }
+                            __syncwarp();
+                        }
+                        if (j == 0) {
+                            if (oc[0] > 0) ok = bar_wait(smem_u32(&sm.o_free[0]), (oc[0] - 1) & 1, limit);
+                            oc[0]++;
+                        }
+                        ok = bar_wait(smem_u32(&sm.p_full[at]), (g >> 1) & 1, limit) && ok;
+                        ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.v_full[st]), ph, limit) && ok);
+                        if (!ok) break;
+                        fence_after();
+                        zero_rows(st, valid, steps);
+                        values(at, st, j == 0, 0, steps);
+                        if (mine) {
+                            commit(smem_u32(&sm.v_empty[st]));
+                            commit(smem_u32(&sm.pv_done[0]));
+                            if (j + 1 == nb) commit(smem_u32(&sm.pv_done[1]));
+                        }
+                        __syncwarp();
+                        continue;
+                    }
                     bool have_k = false;
                     ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.v_full[st]), ph, limit));
                     if (!ok) break;
-                    if (valid & 15) {              // the call's own rows behind the last token in its step of 16 count as zero
-                        const int rows = 16 * steps - valid;
-                        for (int e = lane; e < rows * 16; e += 32)
-                            *reinterpret_cast<uint4 *>(sm.v[st] + ((e >> 3) & 1) * kSub + (valid + (e >> 4)) * 128 + (e & 7) * 16) =
-                                make_uint4(0, 0, 0, 0);
-                        fence_async_shared();
-                        __syncwarp();
-                    }
+                    zero_rows(st, valid, steps);
 #pragma unroll
                     for (int t = 0; t < kTiles; t++) {
                         if (t >= nt) continue;
@@ -825,7 +846,7 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
                         ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.p_half[t]), pc[t] & 1, limit) && ok);
                         if (!ok) break;
                         fence_after();
-                        values(t, st, j == 0, 0, steps);
+                        values(t, st, j == 0, 0, min(4, steps));
                         ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.p_full[t]), pc[t] & 1, limit));
                         if (!ok) break;
                         pc[t]++;
@@ -862,15 +883,30 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
             __syncwarp();
         }
     } else {
-        if constexpr (kTiles == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
+        if constexpr (kTiles == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
         else asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
-        // ================================================= softmax: thread = row
-        const int t = warp >> 2;
-        const uint32_t base = tmem + ((uint32_t)((warp & 3) * 32) << 16) + t * 128;
+        // ================================================= softmax: thread = row, or one of a row's copies with its share of the keys
+        constexpr int kCols = kBlockK / kCopies, kCopyRows = kTileRows / kCopies;
+        const int t = warp >> 2, copy = (tid & (kTileRows - 1)) / kCopyRows;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, base = tmem + lanes + (kTiles == 2 ? t * 128 : copy * kCols);
+        const uint32_t p_base = tmem + lanes + kP + (kTiles == 2 ? t * 128 : copy * (kCols / 2)), o_base = tmem + lanes + kO + t * 128;
         const uint32_t s_full = smem_u32(&sm.s_full[t]), p_half = smem_u32(&sm.p_half[t]), p_full = smem_u32(&sm.p_full[t]),
                        pv_done = smem_u32(&sm.pv_done[t]);
-        const int row_in = t * kTileRows + (warp & 3) * 32 + lane;
-        uint32_t sc = 0, ic = 0, jc = 0;           // blocks of this tile (S, P and P V alike), items, items in parts so far
+        const int row_in = t * kTileRows + (tid & (kCopyRows - 1));
+        uint32_t sc = 0, ic = 0, cc = 0;           // blocks of this tile (S, P and P V alike), items, exchanges between copies so far
+        // a row's copies among themselves (all softmax warps)
+        auto meet = [&] {
+            __syncwarp();
+            if (lane == 0) bar_arrive(smem_u32(&sm.copies));
+            ok = __all_sync(0xffffffffu, ok && bar_wait(smem_u32(&sm.copies), cc++ & 1, limit));
+            return ok;
+        };
+        if constexpr (kCopies > 1) {               // weights of the other copies' keys: zero for good
+            const uint32_t zero[16] = {};
+#pragma unroll
+            for (int c = 0; c < 8; c++) tmem_st16(tmem + lanes + kP + 16 * c, zero);
+            tmem_wait_st();
+        }
         // (the item stays in shared memory until its end: a copy of it and the row of S do not fit the registers)
         for (uint32_t n = 0;; n++) {
             if (n > 0) {
@@ -887,33 +923,35 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
             float m = -INFINITY, l = 0.0f;
             for (int j = 0; j < nb; j++, sc++) {
                 const int b = b0 + j;
-                ok = bar_wait(s_full, sc & 1, limit);
+                const uint32_t place = kTiles == 2 ? 0 : sc & 1;
+                ok = kTiles == 2 ? bar_wait(s_full, sc & 1, limit) : bar_wait(smem_u32(&sm.s_full[place]), (sc >> 1) & 1, limit);
                 if (!__all_sync(0xffffffffu, ok)) break;
                 if (idle) {
-                    if (lane == 0) { bar_arrive(p_half); bar_arrive(p_full); }
+                    if (lane == 0 && kTiles == 2) { bar_arrive(p_half); bar_arrive(p_full); }
+                    if (lane == 0 && kTiles == 1) bar_arrive(smem_u32(&sm.p_full[place]));
                     continue;
                 }
                 fence_after();
-                float x[128];
+                float x[kCols];
 #pragma unroll
-                for (int c = 0; c < 4; c++) {
+                for (int c = 0; c < kCols / 32; c++) {
                     uint32_t r[32];
-                    tmem_ld32(base + kS + 32 * c, r);
+                    tmem_ld32(base + kS + place * 128 + 32 * c, r);
 #pragma unroll
                     for (int e = 0; e < 32; e++) x[32 * c + e] = __uint_as_float(r[e]);
                 }
                 tmem_wait_ld();
                 if (b >= hist) {                   // the call's own tokens: those up to the row's
-                    const int left = live ? i + 1 - (b - hist) * kBlockK : 0;
-                    if (__any_sync(0xffffffffu, left < kBlockK)) {
+                    const int left = live ? i + 1 - (b - hist) * kBlockK - copy * kCols : 0;
+                    if (__any_sync(0xffffffffu, left < kCols)) {
 #pragma unroll
-                        for (int e = 0; e < 128; e++) if (e >= left) x[e] = -INFINITY;
+                        for (int e = 0; e < kCols; e++) if (e >= left) x[e] = -INFINITY;
                     }
                 } else if (const Filled f(it); !f.whole_block(b)) {
                     const uint32_t mine = (1u << f.of_page(8 * b + (lane & 7))) - 1u;
 #pragma unroll
-                    for (int pg = 0; pg < 8; pg++) {
-                        const uint32_t bits = __shfl_sync(0xffffffffu, mine, pg);
+                    for (int pg = 0; pg < kCols / 16; pg++) {
+                        const uint32_t bits = __shfl_sync(0xffffffffu, mine, pg + copy * (kCols / 16));
 #pragma unroll
                         for (int e = 0; e < 16; e++) if (!((bits >> e) & 1)) x[16 * pg + e] = -INFINITY;
                     }
@@ -922,7 +960,7 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
                 {
                     float a0 = x[0], a1 = x[1], a2 = x[2], a3 = x[3];
 #pragma unroll
-                    for (int e = 4; e < 128; e += 4) {
+                    for (int e = 4; e < kCols; e += 4) {
                         a0 = fmaxf(a0, x[e]); a1 = fmaxf(a1, x[e + 1]); a2 = fmaxf(a2, x[e + 2]); a3 = fmaxf(a3, x[e + 3]);
                     }
                     top = fmaxf(fmaxf(a0, a1), fmaxf(a2, a3)) * kScaleLog2;
@@ -931,24 +969,29 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
                 if (__any_sync(0xffffffffu, raise)) {
                     const float d = raise ? ex2(m - top) : 1.0f;
                     if (raise) { m = top; l *= d; }
-                    if (j > 0) {                   // O so far, in the new reference (complete: this S was issued behind it)
+                    if (j > 0) {                   // O so far, in the new reference (two tiles: complete, this S was issued behind it)
+                        if (kTiles == 1) {         // (the product before that one is: this S was issued behind it)
+                            ok = __all_sync(0xffffffffu, bar_wait(pv_done, (sc - 1) & 1, limit));
+                            if (!ok) break;
+                            fence_after();
+                        }
 #pragma unroll 1
                         for (int c = 0; c < 8; c++) {
                             uint32_t r[16];
-                            tmem_ld16(base + kO + 16 * c, r);
+                            tmem_ld16(o_base + 16 * c, r);
                             tmem_wait_ld();
 #pragma unroll
                             for (int e = 0; e < 16; e++) r[e] = __float_as_uint(__uint_as_float(r[e]) * d);
-                            tmem_st16(base + kO + 16 * c, r);
+                            tmem_st16(o_base + 16 * c, r);
                         }
                     }
                 }
                 const float ref = m == -INFINITY ? 0.0f : m;               // a row that has seen no key yet
                 const uint64_t scale2 = pair(kScaleLog2, kScaleLog2), ref2 = pair(-ref, -ref);
                 uint64_t l2 = pair(0.0f, 0.0f);
-                // Weights go out in two halves: the product over the first 64 keys runs beside the other exponentials.
+                // Two tiles: weights go out in two halves, the product over the first 64 keys runs beside the other exponentials.
 #pragma unroll
-                for (int c = 0; c < 4; c++) {
+                for (int c = 0; c < kCols / 32; c++) {
                     uint32_t r[16];
 #pragma unroll
                     for (int e = 0; e < 16; e++) {
@@ -959,12 +1002,12 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
                         l2 = add2(l2, pair(u, v));
                         r[e] = pack_bf16(u, v);
                     }
-                    tmem_st16(base + kS + 16 * c, r);
-                    if (c & 1) {
+                    tmem_st16(p_base + place * 64 + 16 * c, r);
+                    if (kTiles == 2 ? (c & 1) : c + 1 == kCols / 32) {
                         tmem_wait_st();
                         fence_before();
                         __syncwarp();
-                        if (lane == 0) bar_arrive(c == 1 ? p_half : p_full);
+                        if (lane == 0) bar_arrive(kTiles == 1 ? smem_u32(&sm.p_full[place]) : c == 1 ? p_half : p_full);
                     }
                 }
                 float l0, l1;
@@ -972,18 +1015,69 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
                 l += l0 + l1;
             }
             ok = __all_sync(0xffffffffu, ok);
-            if (ok && here) ok = __all_sync(0xffffffffu, bar_wait(pv_done, ic++ & 1, limit));
+            if (ok && here) ok = __all_sync(0xffffffffu, bar_wait(kTiles == 2 ? pv_done : smem_u32(&sm.pv_done[1]), ic++ & 1, limit));
             if (!ok) break;
             fence_after();
             const size_t heads = (size_t)kGqa * p.n_kv, row = (size_t)(it.q0 + i) * heads + kGqa * it.head + (row_in & 3);
             const bool whole = it.first == it.last;
             const size_t part = 2 * (size_t)blockIdx.x + (it.first == (int)blockIdx.x);      // the place of a CTA's part of an item
+            if constexpr (kCopies > 1) {
+                // Each copy brings its sums to the row's reference; 32 dims at a time they meet in shared memory.
+                sm.ml[tid] = make_float2(m, l);
+                if (!meet()) break;
+                float top = -INFINITY, sum = 0.0f;
+#pragma unroll
+                for (int c = 0; c < kCopies; c++) top = fmaxf(top, sm.ml[c * kCopyRows + row_in].x);
+                const float ref = top == -INFINITY ? 0.0f : top, mine = ex2(m - ref);
+#pragma unroll
+                for (int c = 0; c < kCopies; c++) {
+                    const float2 y = sm.ml[c * kCopyRows + row_in];
+                    sum += y.y * ex2(y.x - ref);
+                }
+                const float inv = live ? 1.0f / sum : 0.0f;
+#pragma unroll 1
+                for (int d0 = 0; d0 < kDim; d0 += 32) {
+                    __syncwarp();
+                    uint32_t r[32];
+                    tmem_ld32(o_base + d0, r);
+                    tmem_wait_ld();
+                    if (d0 > 0 && !meet()) break;
+#pragma unroll
+                    for (int e = 0; e < 32; e++) sm.share[e][tid] = __uint_as_float(r[e]) * mine;
+                    if (!meet()) break;
+                    constexpr int kOwn = 32 / kCopies;         // dims of the row that this copy writes
+                    float y[kOwn];
+#pragma unroll
+                    for (int e = 0; e < kOwn; e++) {
+                        y[e] = 0.0f;
+#pragma unroll
+                        for (int c = 0; c < kCopies; c++) y[e] += sm.share[copy * kOwn + e][c * kCopyRows + row_in];
+                    }
+                    const int d = d0 + copy * kOwn;
+                    if (whole && live) {
+#pragma unroll
+                        for (int e = 0; e < kOwn; e += 8)
+                            *reinterpret_cast<uint4 *>(p.out + row * kDim + d + e) =
+                                make_uint4(pack_bf16(y[e] * inv, y[e + 1] * inv), pack_bf16(y[e + 2] * inv, y[e + 3] * inv),
+                                           pack_bf16(y[e + 4] * inv, y[e + 5] * inv), pack_bf16(y[e + 6] * inv, y[e + 7] * inv));
+                    } else if (live) {
+#pragma unroll
+                        for (int e = 0; e < kOwn; e += 4)
+                            __stcg(p.ws.o + (part * (kDim / 4) + (d + e) / 4) * kRows + row_in, make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]));
+                    }
+                }
+                if (!ok) break;
+                if (live && copy == 0) {
+                    if (!whole) __stcg(p.ws.ml + part * kRows + row_in, make_float2(top, sum));
+                    else if (p.lse) p.lse[row] = (top + log2f(sum)) * 0.69314718055994531f;
+                }
+            } else
             if (here && !idle) {
                 const float inv = live ? 1.0f / l : 0.0f;
 #pragma unroll
                 for (int c = 0; c < 8; c++) {
                     uint32_t r[16];
-                    tmem_ld16(base + kO + 16 * c, r);
+                    tmem_ld16(o_base + 16 * c, r);
                     tmem_wait_ld();
                     if (whole && live) {
                         uint4 *dst = reinterpret_cast<uint4 *>(p.out + row * kDim + 16 * c);
@@ -1012,27 +1106,11 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
                 __syncwarp();
                 if (lane == 0) bar_arrive(smem_u32(&sm.o_free[t]));
             }
-            if (whole) continue;
-            // ---- a part of an item (a CTA's first, its last or both): the last of its CTAs to come here joins them, below
-            __threadfence();
-            __syncwarp();
-            if (lane == 0 && atomicAdd(&sm.arrived[jc], 1) == kSoft - 1) {
-                __threadfence();
-                const bool last = atomicAdd(p.ws.arrived + it.first, 1) == (uint32_t)(it.last - it.first);
-                __threadfence();
-                Join &to = sm.join[jc];
+            if (tid == 0 && !whole && it.first == (int)blockIdx.x) {
+                Join &to = p.ws.joins[blockIdx.x];
                 to.row = it.q0 + it.block * kTokens;
-                to.rows = last ? min(kRows, (it.nq - it.block * kTokens) * kGqa) : 0;
+                to.rows = min(kRows, (it.nq - it.block * kTokens) * kGqa);
                 to.head = it.head; to.first = it.first; to.last = it.last;
-                bar_arrive(smem_u32(&sm.joined[jc]));
-            }
-            jc++;
-        }
-        for (uint32_t k = 0; k < jc && ok; k++) {
-            ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.joined[k]), 0, limit));
-            if (ok && sm.join[k].rows) {
-                __threadfence();
-                join_parts<kTiles>(p, sm.join[k], tid);
             }
         }
     }
@@ -1040,43 +1118,84 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
     fence_before();
     __syncthreads();
     fence_after();
-    if (warp == kSoft) tmem_free(tmem, kColumns);
+    if (warp == kSoft) tmem_free(tmem, 512);
 }
 
-template <int kBits, int kTiles>
+// The items in parts: eight CTAs each, four dims of a row a thread; their parts in order.
+constexpr int kJoinThreads = 256, kJoinCtas = 8;
+__global__ void __launch_bounds__(kJoinThreads)
+prompt_join_kernel(PromptWorkspace ws, int rows_max, int n_kv, __nv_bfloat16 *__restrict__ out, float *__restrict__ lse) {
+    using namespace umma;
+    pdl_launch_dependents();
+    pdl_wait();
+    const Join j = ws.joins[blockIdx.x];
+    const size_t heads = (size_t)kGqa * n_kv;
+    for (int u = blockIdx.y * kJoinThreads + threadIdx.x; u < j.rows * (kDim / 4); u += kJoinCtas * kJoinThreads) {
+        const int d = u / j.rows, r = u - d * j.rows;
+        float top = -INFINITY, sum = 0.0f;
+        float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 6
+        for (int c = j.first; c <= j.last; c++) {
+            const size_t at = 2 * (size_t)c + (c == j.first);
+            const float2 ml = __ldcg(ws.ml + at * rows_max + r);
+            const float4 y = __ldcg(ws.o + (at * (kDim / 4) + d) * rows_max + r);
+            const float next = fmaxf(top, ml.x), ref = next == -INFINITY ? 0.0f : next, a = ex2(top - ref), w = ex2(ml.x - ref);
+            top = next;
+            sum = sum * a + ml.y * w;
+            o.x = o.x * a + y.x * w; o.y = o.y * a + y.y * w; o.z = o.z * a + y.z * w; o.w = o.w * a + y.w * w;
+        }
+        const float inv = 1.0f / sum;
+        const size_t to = (size_t)(j.row + r / kGqa) * heads + kGqa * j.head + (r & 3);
+        *reinterpret_cast<uint2 *>(out + to * kDim + 4 * d) = make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+        if (d == 0 && lse) lse[to] = (top + log2f(sum)) * 0.69314718055994531f;
+    }
+}
+
+template <int kBits, int kTiles, int kCopies>
 pask_status_t launch(const PromptParams &p, const CUtensorMap &map_q, const CUtensorMap &map_k, const CUtensorMap &map_v, int dev, cudaStream_t stream) {
-    constexpr int kSmem = (int)sizeof(PromptSmem<kTiles>);
+    constexpr int kSmem = (int)sizeof(PromptSmem<kTiles, kCopies>);
     static_assert(kSmem <= 232448, "shared memory of a CTA");
     static bool granted[64] = {};                  // a property of (device, kernel)
     if (!granted[dev]) {
-        if (cudaFuncSetAttribute(prompt_kernel<kBits, kTiles>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess) return PASK_ERR_CUDA;
+        if (cudaFuncSetAttribute(prompt_kernel<kBits, kTiles, kCopies>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess) return PASK_ERR_CUDA;
         granted[dev] = true;
     }
-    return launch_pdl(prompt_kernel<kBits, kTiles>, dim3(p.grid), dim3(kThreads), kSmem, stream, p, map_q, map_k, map_v) == cudaSuccess ? PASK_OK
+    return launch_pdl(prompt_kernel<kBits, kTiles, kCopies>, dim3(p.grid), dim3(kThreads), kSmem, stream, p, map_q, map_k, map_v) == cudaSuccess ? PASK_OK
                                                                                                                                      : PASK_ERR_CUDA;
 }
 
-// One tile of 32 tokens or two of 64 in a CTA
-int tiles_for(int n_seqs, int total_tokens) { return 2; }
+template <int kTiles, int kCopies>
+pask_status_t launch_bits(uint32_t bits, const PromptParams &p, const CUtensorMap &map_q, const CUtensorMap &map_k, const CUtensorMap &map_v, int dev,
+                          cudaStream_t stream) {
+    return bits == 8 ? launch<8, kTiles, kCopies>(p, map_q, map_k, map_v, dev, stream)
+           : bits == 2 ? launch<2, kTiles, kCopies>(p, map_q, map_k, map_v, dev, stream)
+                       : launch<4, kTiles, kCopies>(p, map_q, map_k, map_v, dev, stream);
+}
+
+// Tokens of an item: 64 (two tiles), or 32, 16, 8 (one tile)
+int tokens_for(int n_seqs, int total_tokens) {
+    const long long n = (total_tokens + n_seqs - 1) / n_seqs;
+    return n <= 8 ? 8 : n <= 16 ? 16 : n <= 32 ? 32 : 64;
+}
 
 }  // namespace
 
 size_t prompt_workspace_bytes(const pask_cache *c, int n_seqs, int total_tokens) {
-    return carve(n_seqs, c->sm_count, tiles_for(n_seqs, total_tokens) * kTileRows, nullptr, nullptr);
+    return carve(n_seqs, c->sm_count, tokens_for(n_seqs, total_tokens) * kGqa, nullptr, nullptr);
 }
 
 pask_status_t launch_prompt(pask_cache *c, int layer, int n_seqs, int total_tokens, const int32_t *seq_ids, const int32_t *cu_tokens, const void *q,
                             const void *k, const void *v, void *out, float *lse, void *workspace, cudaStream_t stream) {
-    const int n_kv = c->desc.n_kv_heads, tiles = tiles_for(n_seqs, total_tokens);
+    const int n_kv = c->desc.n_kv_heads, tokens = tokens_for(n_seqs, total_tokens);
     CUtensorMap map_q{}, map_k{}, map_v{};
     const size_t head = kDim * 2;
-    if (!encode_heads(&map_q, q, kDim, kGqa * n_kv, total_tokens, head, head * kGqa * n_kv, kGqa, kTileTokens) ||
+    if (!encode_heads(&map_q, q, kDim, kGqa * n_kv, total_tokens, head, head * kGqa * n_kv, kGqa, tokens < kTileTokens ? tokens : kTileTokens) ||
         !encode_heads(&map_k, k, kDim, n_kv, total_tokens, head, head * n_kv, 1, kBlockK) ||
         !encode_heads(&map_v, v, kDim, n_kv, total_tokens, head, head * n_kv, 1, kBlockK))
         return PASK_ERR_CUDA;
     const DevCache &d = c->dev;
     PromptParams p{};
-    carve(n_seqs, c->sm_count, tiles * kTileRows, static_cast<uint8_t *>(workspace), &p.ws);
+    carve(n_seqs, c->sm_count, tokens * kGqa, static_cast<uint8_t *>(workspace), &p.ws);
     p.pool_high = d.pool_high;
     p.pool_low = d.pool_low;
     p.tbl_high = d.tbl_high;
@@ -1098,11 +1217,14 @@ pask_status_t launch_prompt(pask_cache *c, int layer, int n_seqs, int total_toke
     p.wait_cycles = c->wait_cycles;
     p.surplus = c->wait_test_surplus;
     if (launch_pdl(prompt_plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, d, layer, n_seqs, total_tokens, seq_ids, cu_tokens, p.ws, p.grid,
-                   tiles * kTileTokens, static_cast<uint4 *>(out), lse) != cudaSuccess)
+                   tokens, static_cast<uint4 *>(out), lse) != cudaSuccess)
         return PASK_ERR_CUDA;
-    const auto fn = tiles == 2 ? (d.low_bits == 8 ? launch<8, 2> : d.low_bits == 2 ? launch<2, 2> : launch<4, 2>)
-                               : (d.low_bits == 8 ? launch<8, 1> : d.low_bits == 2 ? launch<2, 1> : launch<4, 1>);
-    return fn(p, map_q, map_k, map_v, c->device, stream);
+    const auto fn = tokens == 64 ? launch_bits<2, 1> : tokens == 32 ? launch_bits<1, 1> : tokens == 16 ? launch_bits<1, 2> : launch_bits<1, 4>;
+    const pask_status_t ok = fn(d.low_bits, p, map_q, map_k, map_v, c->device, stream);
+    if (ok != PASK_OK) return ok;
+    return launch_pdl(prompt_join_kernel, dim3(p.grid, kJoinCtas), dim3(kJoinThreads), 0, stream, p.ws, tokens * kGqa, n_kv, p.out, lse) == cudaSuccess
+               ? PASK_OK
+               : PASK_ERR_CUDA;
 }
 
 }  // namespace pask
