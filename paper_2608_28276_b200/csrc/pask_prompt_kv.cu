@@ -36,7 +36,6 @@ constexpr int kDim = kHeadDim, kGqa = 4;
 constexpr int kTileRows = 128, kTileTokens = kTileRows / kGqa, kBlockK = 128, kBlockPages = kBlockK / kPageTokens;
 constexpr int kSub = kBlockK * 128;                // 128 rows x 64 dims: 16 KB
 constexpr int kTileBytes = 2 * kSub;               // 128 rows x 128 dims
-constexpr int kThreads = 512;
 constexpr int kItemCost = 2;                       // of an item's beginning and end, in key blocks
 constexpr int kMinPiece = 2;                       // no part of an item is shorter, in key blocks
 constexpr float kLazy = 8.0f;
@@ -323,8 +322,9 @@ struct Walker {
 
 constexpr uint32_t kPageLow = 0, kPageBad = 1, kPageHigh = 2, kPageNone = 3;       // kinds of a page: bits 30, 31 of its entry
 
-// A page's key / value rows of one head as they are stored, a lane's share in registers.
-struct Raw { uint4 x[8]; };                        // (low precision: codes, then scales in x[4], x[5])
+// A lane's share of what is expanded at a time, in registers: half of a bf16 page's keys or values of one head, or the codes of a
+// low-precision page's and two of its scales.
+struct Raw { uint4 x[4]; uint32_t s0, s1; };
 
 // (code - kZero) * scale for two codes, as bf16, rounded once: the difference is exact, the scale is the sum of two bf16 numbers of which the
 // smaller has three bits, so that its product with a code is exact and one fma rounds the sum of both products.
@@ -335,11 +335,15 @@ __device__ __forceinline__ uint32_t scaled_codes(uint32_t codes, uint32_t offset
     return r;
 }
 __device__ __forceinline__ float half_bits(uint32_t h) { return __half2float(__ushort_as_half((unsigned short)h)); }
-// fp16 bits of a scale as two bf16 numbers whose sum it is, each twice
-__device__ __forceinline__ void split_scale(uint32_t h, uint32_t &hi, uint32_t &lo) {
-    const float f = half_bits(h), a = __bfloat162float(__float2bfloat16_rn(f));
-    hi = umma::pack_bf16(f, f);
-    lo = umma::pack_bf16(f - a, f - a);
+// two scales as pairs of two bf16 numbers whose sums they are
+__device__ __forceinline__ void split_scales(float a, float b, uint32_t &hi, uint32_t &lo) {
+    hi = umma::pack_bf16(a, b);
+    lo = umma::pack_bf16(a - __uint_as_float(hi << 16), b - __uint_as_float(hi & 0xFFFF0000u));
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float x;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(x) : "f"(a), "f"(b), "f"(c));
+    return x;
 }
 __device__ __forceinline__ float byte_value(uint32_t w, uint32_t k) {            // byte k of w, less 128
     return __uint_as_float(__byte_perm(w, 0x4B000000u, 0x7440u | k)) - 8388736.0f;
@@ -370,137 +374,126 @@ struct Low {
     static constexpr int kHalf = 512 * kRounds + kLowScalesBytes;
 };
 
+// half 0: dims 0 .. 63, 1: 64 .. 127 (keys: rounds 2 j + h of dims 32 j ..; values: rounds 4 e + k of dims 64 e ..)
 template <bool kKeys>
-__device__ __forceinline__ void load_high(Raw &r, const uint8_t *head, int lane) {
-    const uint4 *src = reinterpret_cast<const uint4 *>(head + (kKeys ? 0 : kHighTileBytes)) + Lanes(kKeys, lane).source();
+__device__ __forceinline__ void load_high(Raw &r, const uint8_t *tile, int half, int lane) {
+    const uint4 *src = reinterpret_cast<const uint4 *>(tile + half * (kHighTileBytes / 2)) + Lanes(kKeys, lane).source();
 #pragma unroll
-    for (int i = 0; i < 8; i++) r.x[i] = __ldg(src + 32 * i);
+    for (int i = 0; i < 4; i++) r.x[i] = __ldg(src + 32 * i);
 }
 // `row`: first row of the page in its block; the block is two pieces of 64 dims, 128 rows of 128 bytes with the 128-byte swizzle
 template <bool kKeys>
-__device__ __forceinline__ void store_high(const Raw &r, uint32_t block, int row, int lane) {
+__device__ __forceinline__ void store_high(const Raw &r, uint32_t block, int row, int half, int lane) {
     const Lanes l(kKeys, lane);
+    block += half * kSub;
     if (kKeys) {
         const uint32_t base = block + (uint32_t)(row + l.g) * 128;
 #pragma unroll
-        for (int j = 0; j < 4; j++) {              // dims 8 (4 j + t) .. + 7 of tokens g and g + 8
+        for (int j = 0; j < 2; j++) {              // dims 64 half + 32 j + 8 t .. + 7 of tokens g and g + 8
             const uint4 a = r.x[2 * j], b = r.x[2 * j + 1];
-            const uint32_t at = base + (j >> 1) * kSub + (((4 * (j & 1) + l.t) ^ l.g) << 4);
+            const uint32_t at = base + (((4 * j + l.t) ^ l.g) << 4);
             store16(at, a.x, a.z, b.x, b.z);
             store16(at + 1024, a.y, a.w, b.y, b.w);
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; i++) {              // token 2 t + (k & 1) + 8 (k >> 1), dims 64 e + 4 g .. and 32 on
-            const int e = i >> 2, k = i & 3, tok = 2 * l.t + (k & 1), sw = tok & 7;
-            const uint32_t base = block + e * kSub + (uint32_t)(row + tok + 8 * (k >> 1)) * 128 + 8 * (l.g & 1);
-            store8(base + (((l.g >> 1) ^ sw) << 4), r.x[i].x, r.x[i].y);
-            store8(base + (((4 + (l.g >> 1)) ^ sw) << 4), r.x[i].z, r.x[i].w);
+        for (int k = 0; k < 4; k++) {              // token 2 t + (k & 1) + 8 (k >> 1), dims 64 half + 4 g .. and 32 on
+            const int tok = 2 * l.t + (k & 1), sw = tok & 7;
+            const uint32_t base = block + (uint32_t)(row + tok + 8 * (k >> 1)) * 128 + 8 * (l.g & 1);
+            store8(base + (((l.g >> 1) ^ sw) << 4), r.x[k].x, r.x[k].y);
+            store8(base + (((4 + (l.g >> 1)) ^ sw) << 4), r.x[k].z, r.x[k].w);
         }
     }
 }
 
 template <int kBits, bool kKeys>
-__device__ __forceinline__ void load_low(Raw &r, const uint8_t *head, int lane) {
+__device__ __forceinline__ void load_low(Raw &r, const uint8_t *half, int lane) {
     using L = Low<kBits, kKeys>;
     const Lanes l(kKeys, lane);
-    const uint8_t *half = head + (kKeys ? 0 : L::kHalf);
     const uint4 *src = reinterpret_cast<const uint4 *>(half) + l.source();
 #pragma unroll
     for (int i = 0; i < L::kRounds; i++) r.x[i] = __ldg(src + 32 * i);
-    const uint8_t *scales = half + 512 * L::kRounds;
-    if (kKeys) {                                   // tokens g and g + 8
-        const uint2 a = __ldg(reinterpret_cast<const uint2 *>(scales) + l.g), b = __ldg(reinterpret_cast<const uint2 *>(scales) + l.g + 8);
-        r.x[4] = make_uint4(a.x, a.y, b.x, b.y);
-    } else {                                       // tokens 2 t, 2 t + 1 and 8 on
-        r.x[4] = __ldg(reinterpret_cast<const uint4 *>(scales) + l.t);
-        r.x[5] = __ldg(reinterpret_cast<const uint4 *>(scales) + l.t + 4);
-    }
+    // Of the 64 scales a lane fetches two, and they go around: keys those of tokens g and g + 8 in group t; values those of tokens 2 t
+    // and 2 t + 1, 8 on for g > 3, in group g & 3.
+    const unsigned short *scales = reinterpret_cast<const unsigned short *>(half + 512 * L::kRounds) + (kKeys ? 4 * l.g + l.t : 8 * l.t + 32 * (l.g >> 2) + (l.g & 3));
+    r.s0 = __ldg(scales);
+    r.s1 = __ldg(scales + (kKeys ? 32 : 4));
 }
 
 __device__ __forceinline__ uint32_t word_of(const uint4 &v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
-__device__ __forceinline__ uint32_t half_of(uint32_t w, int i) { return (w >> (16 * i)) & 0xFFFFu; }
 
 template <int kBits, bool kKeys>
 __device__ __forceinline__ void store_low(const Raw &r, uint32_t block, int row, int lane) {
     const Lanes l(kKeys, lane);
     constexpr uint32_t kOffset = kBits == 4 ? 0x43084308u : 0x43024302u;         // bf16 136 or 130, twice: 128 + the code of zero
     constexpr uint32_t kMask = kBits == 4 ? 0x000F000Fu : 0x00030003u;
-    if constexpr (kBits == 8 && kKeys) {
-#pragma unroll
-        for (int rr = 0; rr < 4; rr++)             // group rr: k-chunks 2 rr, 2 rr + 1 of 16 dims
-#pragma unroll
-            for (int hi = 0; hi < 2; hi++) {       // tokens g, g + 8
-                const float s = half_bits(half_of(hi ? (rr < 2 ? r.x[4].z : r.x[4].w) : (rr < 2 ? r.x[4].x : r.x[4].y), rr & 1));
-                const uint32_t base = block + (rr >> 1) * kSub + (uint32_t)(row + l.g + 8 * hi) * 128 + 4 * l.t;
-#pragma unroll
-                for (int k = 0; k < 4; k++) {      // 8 dims each: dims 32 rr + 8 k + 2 t, + 1
-                    const uint32_t w = word_of(r.x[rr], k);
-                    store4(base + (((4 * (rr & 1) + k) ^ l.g) << 4), umma::pack_bf16(byte_value(w, 2 * hi) * s, byte_value(w, 2 * hi + 1) * s));
-                }
-            }
-    } else if constexpr (kBits == 8) {
-#pragma unroll
-        for (int q = 0; q < 4; q++)
-#pragma unroll
-            for (int ps = 0; ps < 2; ps++) {       // tokens 2 t + 8 ps and the next, dims 32 q + 4 g .. + 3
-                const uint32_t a = ps ? r.x[q].y : r.x[q].x, b = ps ? r.x[q].w : r.x[q].z;
-#pragma unroll
-                for (int odd = 0; odd < 2; odd++) {
-                    const uint32_t sw = odd ? (q < 2 ? r.x[4 + ps].z : r.x[4 + ps].w) : (q < 2 ? r.x[4 + ps].x : r.x[4 + ps].y);
-                    const float s = half_bits(half_of(sw, q & 1));
-                    const int tok = 2 * l.t + odd;
-                    store8(block + (q >> 1) * kSub + (uint32_t)(row + tok + 8 * ps) * 128 + (((4 * (q & 1) + (l.g >> 1)) ^ (tok & 7)) << 4) + 8 * (l.g & 1),
-                           umma::pack_bf16(byte_value(a, odd) * s, byte_value(a, 2 + odd) * s),
-                           umma::pack_bf16(byte_value(b, odd) * s, byte_value(b, 2 + odd) * s));
-                }
-            }
-    } else if constexpr (kKeys) {
+    const float f0 = half_bits(r.s0), f1 = half_bits(r.s1);
+    if constexpr (kKeys) {
+        uint32_t s_hi[2], s_lo[2];
+        if constexpr (kBits < 8) {
+            split_scales(f0, f0, s_hi[0], s_lo[0]);
+            split_scales(f1, f1, s_hi[1], s_lo[1]);
+        }
 #pragma unroll
         for (int hi = 0; hi < 2; hi++) {           // tokens g, g + 8
             const uint32_t base = block + (uint32_t)(row + l.g + 8 * hi) * 128;
 #pragma unroll
-            for (int w = 0; w < 4; w++) {          // group w: dims 32 w + 8 t .. + 7
-                uint32_t s_hi, s_lo;
-                split_scale(half_of(hi ? (w < 2 ? r.x[4].z : r.x[4].w) : (w < 2 ? r.x[4].x : r.x[4].y), w & 1), s_hi, s_lo);
-                const uint32_t x = kBits == 4 ? word_of(r.x[hi], w) : word_of(r.x[0], w) >> (8 * hi);
-                constexpr int kStep = kBits;
-                store16(base + (w >> 1) * kSub + (((4 * (w & 1) + l.t) ^ l.g) << 4), scaled_codes(x & kMask, kOffset, s_hi, s_lo),
-                        scaled_codes((x >> kStep) & kMask, kOffset, s_hi, s_lo), scaled_codes((x >> 2 * kStep) & kMask, kOffset, s_hi, s_lo),
-                        scaled_codes((x >> 3 * kStep) & kMask, kOffset, s_hi, s_lo));
+            for (int w = 0; w < 4; w++) {          // group w
+                const int from = (lane & ~3) | w;
+                if constexpr (kBits == 8) {        // dims 32 w + 8 k + 2 t, + 1
+                    const float s = __shfl_sync(0xffffffffu, hi ? f1 : f0, from);
+#pragma unroll
+                    for (int k = 0; k < 4; k++) {
+                        const uint32_t c = word_of(r.x[w], k);
+                        store4(base + (w >> 1) * kSub + (((4 * (w & 1) + k) ^ l.g) << 4) + 4 * l.t,
+                               umma::pack_bf16(byte_value(c, 2 * hi) * s, byte_value(c, 2 * hi + 1) * s));
+                    }
+                } else {                           // dims 32 w + 8 t .. + 7
+                    const uint32_t h = __shfl_sync(0xffffffffu, s_hi[hi], from), o = __shfl_sync(0xffffffffu, s_lo[hi], from);
+                    const uint32_t c = kBits == 4 ? word_of(r.x[hi], w) : word_of(r.x[0], w) >> (8 * hi);
+                    store16(base + (w >> 1) * kSub + (((4 * (w & 1) + l.t) ^ l.g) << 4), scaled_codes(c & kMask, kOffset, h, o),
+                            scaled_codes((c >> kBits) & kMask, kOffset, h, o), scaled_codes((c >> 2 * kBits) & kMask, kOffset, h, o),
+                            scaled_codes((c >> 3 * kBits) & kMask, kOffset, h, o));
+                }
             }
         }
     } else {
+        uint32_t s_hi, s_lo;
+        if constexpr (kBits < 8) split_scales(f0, f1, s_hi, s_lo);
+        // tokens 2 t (`even`) and 2 t + 1, 8 on for ps, dims 32 q + 4 g .. + 3
+        const uint32_t even = block + (uint32_t)(row + 2 * l.t) * 128 + 8 * (l.g & 1);
 #pragma unroll
         for (int ps = 0; ps < 2; ps++)
 #pragma unroll
-            for (int q = 0; q < 4; q++)
+            for (int q = 0; q < 4; q++) {
+                const int from = 4 * (4 * ps + q) + l.t;
+                const uint32_t to = even + (q >> 1) * kSub + 1024 * ps, chunk = 4 * (q & 1) + (l.g >> 1);
+                const uint32_t at0 = to + ((chunk ^ (2 * l.t)) << 4), at1 = to + 128 + ((chunk ^ (2 * l.t + 1)) << 4);
+                if constexpr (kBits == 8) {
+                    const float s = __shfl_sync(0xffffffffu, f0, from), z = __shfl_sync(0xffffffffu, f1, from);
+                    const uint32_t c = ps ? r.x[q].y : r.x[q].x, d = ps ? r.x[q].w : r.x[q].z;
+                    store8(at0, umma::pack_bf16(byte_value(c, 0) * s, byte_value(c, 2) * s), umma::pack_bf16(byte_value(d, 0) * s, byte_value(d, 2) * s));
+                    store8(at1, umma::pack_bf16(byte_value(c, 1) * z, byte_value(c, 3) * z), umma::pack_bf16(byte_value(d, 1) * z, byte_value(d, 3) * z));
+                } else {                           // a dim of both tokens at a time, then sorted by token
+                    const uint32_t h = __shfl_sync(0xffffffffu, s_hi, from), o = __shfl_sync(0xffffffffu, s_lo, from);
+                    const uint32_t c = kBits == 4 ? word_of(r.x[ps], q) : word_of(r.x[0], q) >> (8 * ps);
+                    uint32_t v[4];
 #pragma unroll
-                for (int odd = 0; odd < 2; odd++) {            // token 2 t + odd + 8 ps, dims 32 q + 4 g .. + 3
-                    const int tok = 2 * l.t + odd;
-                    const uint32_t sw = odd ? (q < 2 ? r.x[4 + ps].z : r.x[4 + ps].w) : (q < 2 ? r.x[4 + ps].x : r.x[4 + ps].y);
-                    uint32_t s_hi, s_lo;
-                    split_scale(half_of(sw, q & 1), s_hi, s_lo);
-                    uint32_t y;                    // dims i, i + 1 at bits kBits i and 16 + kBits i
-                    if constexpr (kBits == 4) {
-                        const uint32_t w = word_of(r.x[ps], q);
-                        y = odd ? (w >> 16) | ((w >> 4) & 0xFFFF0000u) : (w & 0xFFFFu) | (w << 12);
-                    } else {
-                        const uint32_t b = (word_of(r.x[0], q) >> (16 * odd + 8 * ps)) & 0xFFu;
-                        y = b | (b << 14);
-                    }
-                    store8(block + (q >> 1) * kSub + (uint32_t)(row + tok + 8 * ps) * 128 + (((4 * (q & 1) + (l.g >> 1)) ^ (tok & 7)) << 4) + 8 * (l.g & 1),
-                           scaled_codes(y & kMask, kOffset, s_hi, s_lo), scaled_codes((y >> 2 * kBits) & kMask, kOffset, s_hi, s_lo));
+                    for (int i = 0; i < 4; i++) v[i] = scaled_codes((c >> kBits * i) & kMask, kOffset, h, o);
+                    store8(at0, __byte_perm(v[0], v[1], 0x5410), __byte_perm(v[2], v[3], 0x5410));
+                    store8(at1, __byte_perm(v[0], v[1], 0x7632), __byte_perm(v[2], v[3], 0x7632));
                 }
+            }
     }
 }
 
 // ------------------------------------------------------------------------------------------------ attention
 
 // kTiles 2: 64 tokens an item.  1: 32 / kCopies tokens, each row of S kCopies times in the tile.
-template <int kTiles, int kCopies>
+template <int kTiles, int kCopies, bool kWide>
 struct __align__(16) PromptSmem {
-    static constexpr int kStages = 2;
+    // Warps: softmax, four for control, fill (kWide: one for the keys and one for the values of each page of a block)
+    static constexpr int kStages = 2, kSoft = 4 * kTiles, kFill = kWide ? 16 : 4, kThreads = 32 * (kSoft + 4 + kFill);
     uint8_t q[kTiles][kTileBytes], k[kStages][kTileBytes], v[kStages][kTileBytes];
     float share[kCopies > 1 ? 32 : 1][kTileRows];  // 32 dims of the copies' results on their way to one another
     float2 ml[kTileRows];
@@ -525,19 +518,15 @@ struct Filled {
         const int left = page < ph ? (int)nh - 16 * page : page < ph + pl ? (int)nl - 16 * (page - ph) : (int)nw - 16 * (page - ph - pl);
         return min(16, max(0, left));
     }
-    __device__ __forceinline__ bool whole_block(int b) const {
-        return 8 * b + 8 <= pages && !((nh & 15) && (ph - 1) >> 3 == b) && !((nl & 15) && (ph + pl - 1) >> 3 == b) &&
-               !((nw & 15) && (pages - 1) >> 3 == b);
-    }
 };
 
-template <int kBits, int kTiles, int kCopies>
-__global__ void __launch_bounds__(kThreads, 1)
+template <int kBits, int kTiles, int kCopies, bool kWide>
+__global__ void __launch_bounds__(PromptSmem<kTiles, kCopies, kWide>::kThreads, 1)
 prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
               const __grid_constant__ CUtensorMap map_v) {
     using namespace umma;
-    using Smem = PromptSmem<kTiles, kCopies>;
-    constexpr int kStages = Smem::kStages, kSoft = 4 * kTiles, kFill = 12 - kSoft;     // softmax and fill warps
+    using Smem = PromptSmem<kTiles, kCopies, kWide>;
+    constexpr int kStages = Smem::kStages, kSoft = Smem::kSoft, kFill = Smem::kFill, kFillOf = kWide ? 8 : 4;     // kFillOf: of a block's keys
     constexpr int kTokens = kTiles * kTileTokens / kCopies, kRows = kTokens * kGqa;
     extern __shared__ __align__(1024) uint8_t s_raw[];
     Smem &sm = *reinterpret_cast<Smem *>(s_raw);
@@ -548,9 +537,9 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
         bar_init(smem_u32(&sm.copies), kSoft);
         bar_init(smem_u32(&sm.drain), 1);
         for (int i = 0; i < kStages; i++) {
-            bar_init(smem_u32(&sm.k_full[i]), 1 + kFill);
+            bar_init(smem_u32(&sm.k_full[i]), 1 + kFillOf);
             bar_init(smem_u32(&sm.k_empty[i]), 1);
-            bar_init(smem_u32(&sm.v_full[i]), 1 + kFill);
+            bar_init(smem_u32(&sm.v_full[i]), 1 + kFillOf);
             bar_init(smem_u32(&sm.v_empty[i]), 1);
         }
         for (int i = 0; i < 2; i++) {
@@ -590,12 +579,15 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
     };
     auto tiles_of = [&](const Item &it) { return kTiles == 2 && it.block * kTokens + kTileTokens < it.nq ? 2 : 1; };
 
-    // 512 threads x 128 registers at launch = 128 x (2 x 168 + 72 + 104) or 128 x (200 + 88 + 2 x 112)
+    // 512 threads x 128 registers at launch = 128 x (2 x 176 + 72 + 88); wide: 896 x 72 = 128 x (2 x 104 + 72 + 4 x 56), one tile: 768 x 80 =
+    // 128 x (120 + 72 + 4 x 72)
     if (warp >= kSoft + 4) {
-        if constexpr (kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
-        else asm volatile("setmaxnreg.dec.sync.aligned.u32 112;");
+        if constexpr (!kWide) asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+        else if constexpr (kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        else asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         // ================================================= fill
-        const int w = warp - kSoft - 4;
+        constexpr int kKv = kWide ? 1 : 2, kPages = kBlockPages / kFillOf;      // of a warp, a block
+        const int page0 = (warp - kSoft - 4) % kFillOf, kv0 = (warp - kSoft - 4) / kFillOf;
         Item it;
         uint32_t g = 0;                            // blocks so far
         for (uint32_t n = 0; next_item(n, it); n++) {
@@ -603,56 +595,65 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
             const uint32_t *tbl_high = p.tbl_high + (size_t)it.slot * p.max_pages, *tbl_low = p.tbl_low + (size_t)it.slot * p.max_pages;
             const uint32_t ring = p.ring_first + it.slot * p.ring_pages;
             const int b1 = min(it.b1, it.hist);
-            // the pages of four blocks at a time, a lane each: kind << 30 | id
-            auto entries = [&](int b) {
+            // the pages of four blocks at a time, a lane each: their ids, then where this head's keys (one tile: or values) lie, and the kind
+            auto ids = [&](int b) {
                 const int page = 8 * b + lane;
-                if (page >= f.pages || b >= b1) return kPageNone << 30;
-                const bool high = page < f.ph || page >= f.ph + f.pl;
-                const uint32_t id = page < f.ph ? __ldg(tbl_high + page) : high ? ring + (uint32_t)(page - f.ph - f.pl) : __ldg(tbl_low + page - f.ph);
-                if (id < (high ? p.high_limit : p.cap_low)) return (high ? kPageHigh << 30 : kPageLow << 30) | id;
-                atomicOr(p.status, PASK_DEV_INTERNAL);         // never expected
-                return kPageBad << 30;
+                if (page >= f.pages || b >= b1) return 0u;
+                return page < f.ph ? __ldg(tbl_high + page) : page < f.ph + f.pl ? __ldg(tbl_low + page - f.ph) : ring + (uint32_t)(page - f.ph - f.pl);
             };
-            uint32_t window = entries(it.b0), window_next = entries(it.b0 + 4);
-            // A unit is the keys or the values of one of this warp's pages.  The next one is read while the current one is expanded.
-            Raw next;
-            uint32_t next_kind = kPageNone;
-            auto load = [&](int b, int kv, int i) {
+            auto places = [&](int b, uint32_t id) {
+                const int page = 8 * b + lane;
+                if (page >= f.pages || b >= b1) return (uint64_t)kPageNone;
+                const bool low = page >= f.ph && page < f.ph + f.pl;
+                if (id >= (low ? p.cap_low : p.high_limit)) {  // never expected
+                    atomicOr(p.status, PASK_DEV_INTERNAL);
+                    return (uint64_t)kPageBad;
+                }
+                const uint8_t *at = low ? p.pool_low + (size_t)id * p.low_page_bytes + (size_t)it.head * p.low_head_bytes + kv0 * Low<kBits, true>::kHalf
+                                        : p.pool_high + (size_t)id * p.high_page_bytes + (size_t)it.head * kHighHeadBytes + kv0 * kHighTileBytes;
+                return reinterpret_cast<uint64_t>(at) | (low ? kPageLow : kPageHigh);          // (16-byte aligned: the kind fits)
+            };
+            uint64_t window = places(it.b0, ids(it.b0));
+            uint32_t ids_next = ids(it.b0 + 4);
+            // The warp's units in turn: pages (wide: one) of a block, keys and values (wide: either).  What was stored makes room for the next unit's
+            // pieces, which travel while its place in the block is waited for: two pieces of a bf16 page, one of a low-precision one.
+            Raw x, y;
+            uint32_t kind = kPageNone;
+            const uint8_t *at = nullptr;
+            auto find = [&](int b, int i) {        // page i of block b
                 const int in = (b - it.b0) & 3;
-                if (in == 0 && kv == 0 && i == 0 && b != it.b0) { window = window_next; window_next = entries(b + 4); }
-                const uint32_t e = __shfl_sync(0xffffffffu, window, 8 * in + w + i * kFill), id = e & 0x3FFFFFFFu;
-                next_kind = e >> 30;
-                if (next_kind == kPageHigh) {
-                    const uint8_t *src = p.pool_high + (size_t)id * p.high_page_bytes + (size_t)it.head * kHighHeadBytes;
-                    if (kv) load_high<false>(next, src, lane); else load_high<true>(next, src, lane);
-                } else if (next_kind == kPageLow) {
-                    const uint8_t *src = p.pool_low + (size_t)id * p.low_page_bytes + (size_t)it.head * p.low_head_bytes;
-                    if (kv) load_low<kBits, false>(next, src, lane); else load_low<kBits, true>(next, src, lane);
+                const uint64_t e = __shfl_sync(0xffffffffu, window, 8 * in + page0 + i * kFillOf);
+                at = reinterpret_cast<const uint8_t *>(e & ~(uint64_t)15);
+                kind = (uint32_t)e & 15u;
+            };
+            auto load = [&](int kv) {
+                if (kind == kPageHigh) {
+                    const uint8_t *tile = at + (kWide || !kv ? 0 : kHighTileBytes);
+                    if (kv) { load_high<false>(x, tile, 0, lane); load_high<false>(y, tile, 1, lane); }
+                    else { load_high<true>(x, tile, 0, lane); load_high<true>(y, tile, 1, lane); }
+                } else if (kind == kPageLow) {
+                    if (kv) load_low<kBits, false>(x, at + (kWide ? 0 : Low<kBits, true>::kHalf), lane); else load_low<kBits, true>(x, at, lane);
                 }
             };
-            if (it.b0 < b1) load(it.b0, 0, 0);
+            if (it.b0 < b1) { find(it.b0, 0); load(kv0); }
             // (The warps pass through every block, those that are copied too: a barrier's phase is only told from the next but one
             // by who has to arrive on it.)
             for (int b = it.b0; b < it.b1; b++, g++) {
                 const uint32_t st = g % kStages, ph = (g / kStages - 1) & 1;
 #pragma unroll 1
-                for (int kv = 0; kv < 2; kv++) {
+                for (int kv = kv0; kv < kv0 + kKv; kv++) {
                     const uint32_t block = smem_u32(kv ? sm.v[st] : sm.k[st]);
                     if (g >= kStages) ok = __all_sync(0xffffffffu, bar_wait(smem_u32(kv ? &sm.v_empty[st] : &sm.k_empty[st]), ph, limit));
                     if (!ok) break;
                     if (b < b1) {
 #pragma unroll 1
-                        for (int i = 0; i < kBlockPages / kFill; i++) {
-                            const Raw r = next;
-                            const uint32_t kind = next_kind;
-                            const int page = w + i * kFill;
-                            if (i + 1 < kBlockPages / kFill) load(b, kv, i + 1);
-                            else if (kv == 0) load(b, 1, 0);
-                            else if (b + 1 < b1) load(b + 1, 0, 0);
+                        for (int i = 0; i < kPages; i++) {
+                            const int page = page0 + i * kFillOf;
                             if (kind == kPageHigh) {
-                                if (kv) store_high<false>(r, block, 16 * page, lane); else store_high<true>(r, block, 16 * page, lane);
+                                if (kv) { store_high<false>(x, block, 16 * page, 0, lane); store_high<false>(y, block, 16 * page, 1, lane); }
+                                else { store_high<true>(x, block, 16 * page, 0, lane); store_high<true>(y, block, 16 * page, 1, lane); }
                             } else if (kind == kPageLow) {
-                                if (kv) store_low<kBits, false>(r, block, 16 * page, lane); else store_low<kBits, true>(r, block, 16 * page, lane);
+                                if (kv) store_low<kBits, false>(x, block, 16 * page, lane); else store_low<kBits, true>(x, block, 16 * page, lane);
                             }
                             // slots without a token: whatever the page holds there counts as zero
                             const int have = kind == kPageNone ? 16 : kind == kPageBad ? 0 : f.of_page(8 * b + page);
@@ -661,6 +662,18 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
                                 for (int e = lane; e < (16 - have) * 16; e += 32)
                                     store16(block + ((e >> 3) & 1) * kSub + (uint32_t)(16 * page + have + (e >> 4)) * 128 + (e & 7) * 16, 0, 0, 0, 0);
                             }
+                            int nb = b, nkv = kv, ni = i + 1;
+                            if (ni == kPages) {
+                                ni = 0;
+                                if (++nkv == kv0 + kKv) {
+                                    nkv = kv0;
+                                    if ((++nb - it.b0 & 3) == 0) {
+                                        window = places(nb, ids_next);
+                                        ids_next = ids(nb + 4);
+                                    }
+                                }
+                            }
+                            if (nb < b1) { find(nb, ni); load(nkv); }
                         }
                         fence_async_shared();
                         __syncwarp();
@@ -672,8 +685,7 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
             if (!ok) break;
         }
     } else if (warp >= kSoft) {
-        if constexpr (kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-        else asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         if (warp == kSoft + 2) {
             // ================================================= items
             Walker walk;
@@ -883,8 +895,9 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
             __syncwarp();
         }
     } else {
-        if constexpr (kTiles == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
-        else asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
+        if constexpr (!kWide) asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
+        else if constexpr (kTiles == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
+        else asm volatile("setmaxnreg.inc.sync.aligned.u32 120;");
         // ================================================= softmax: thread = row, or one of a row's copies with its share of the keys
         constexpr int kCols = kBlockK / kCopies, kCopyRows = kTileRows / kCopies;
         const int t = warp >> 2, copy = (tid & (kTileRows - 1)) / kCopyRows;
@@ -920,6 +933,13 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
             const bool here = t == 0 || it.block * kTokens + kTileTokens < it.nq, live = i < it.nq;
             const int nb = here ? it.b1 - b0 : 0;
             const bool idle = !__any_sync(0xffffffffu, live);          // no row of this warp is one
+            int part_h, part_l, part_w;            // the blocks with slots without a token (-1: none): ends of the streams and of the history
+            {
+                const Filled f(it);
+                part_h = f.nh & 15 ? (f.ph - 1) >> 3 : -1;
+                part_l = f.nl & 15 ? (f.ph + f.pl - 1) >> 3 : -1;
+                part_w = f.nw & 15 || f.pages & 7 ? (f.pages - 1) >> 3 : -1;
+            }
             float m = -INFINITY, l = 0.0f;
             for (int j = 0; j < nb; j++, sc++) {
                 const int b = b0 + j;
@@ -932,39 +952,49 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
                     continue;
                 }
                 fence_after();
-                float x[kCols];
-#pragma unroll
-                for (int c = 0; c < kCols / 32; c++) {
-                    uint32_t r[32];
-                    tmem_ld32(base + kS + place * 128 + 32 * c, r);
-#pragma unroll
-                    for (int e = 0; e < 32; e++) x[32 * c + e] = __uint_as_float(r[e]);
+                // Wide, 128 columns: two looks at S, 32 columns at a time (the registers of a whole row are the fill warps')
+                constexpr bool kTwice = kWide && kCols == 128;
+                constexpr int kPart = kTwice ? 32 : kCols;
+                const bool causal = b >= hist;     // the call's own tokens: those up to the row's
+                const int left = !causal ? kCols : live ? i + 1 - (b - hist) * kBlockK - copy * kCols : 0;
+                uint32_t filled = 0xFFFFu;         // of page lane & 7 of the block
+                bool masked = __any_sync(0xffffffffu, left < kCols);
+                if (b == part_h || b == part_l || b == part_w) {
+                    masked = true;
+                    filled = (1u << Filled(it).of_page(8 * b + (lane & 7))) - 1u;
                 }
-                tmem_wait_ld();
-                if (b >= hist) {                   // the call's own tokens: those up to the row's
-                    const int left = live ? i + 1 - (b - hist) * kBlockK - copy * kCols : 0;
-                    if (__any_sync(0xffffffffu, left < kCols)) {
+                float x[kPart];
+                auto look = [&](int from) {        // columns from .. of the row
 #pragma unroll
-                        for (int e = 0; e < kCols; e++) if (e >= left) x[e] = -INFINITY;
+                    for (int c = 0; c < kPart / 32; c++) {
+                        uint32_t r[32];
+                        tmem_ld32(base + kS + place * 128 + from + 32 * c, r);
+#pragma unroll
+                        for (int e = 0; e < 32; e++) x[32 * c + e] = __uint_as_float(r[e]);
                     }
-                } else if (const Filled f(it); !f.whole_block(b)) {
-                    const uint32_t mine = (1u << f.of_page(8 * b + (lane & 7))) - 1u;
+                    tmem_wait_ld();
+                    if (!masked) return;
 #pragma unroll
-                    for (int pg = 0; pg < kCols / 16; pg++) {
-                        const uint32_t bits = __shfl_sync(0xffffffffu, mine, pg + copy * (kCols / 16));
+                    for (int pg = 0; pg < kPart / 16; pg++) {
+                        const uint32_t bits = __shfl_sync(0xffffffffu, filled, pg + (copy * kCols + from) / 16);
 #pragma unroll
-                        for (int e = 0; e < 16; e++) if (!((bits >> e) & 1)) x[16 * pg + e] = -INFINITY;
+                        for (int e = 0; e < 16; e++) if (16 * pg + e >= left - from || !((bits >> e) & 1)) x[16 * pg + e] = -INFINITY;
                     }
-                }
+                };
                 float top = -INFINITY;
-                {
-                    float a0 = x[0], a1 = x[1], a2 = x[2], a3 = x[3];
+#pragma unroll 1
+                for (int from = 0; from < kCols; from += kPart) {
+                    look(from);
+                    float a0 = max3(top, x[0], x[1]), a1 = max3(x[2], x[3], x[4]), a2 = max3(x[5], x[6], x[7]);
 #pragma unroll
-                    for (int e = 4; e < kCols; e += 4) {
-                        a0 = fmaxf(a0, x[e]); a1 = fmaxf(a1, x[e + 1]); a2 = fmaxf(a2, x[e + 2]); a3 = fmaxf(a3, x[e + 3]);
+                    for (int e = 8; e < kPart; e += 6) {
+                        a0 = max3(a0, x[e], x[e + 1]);
+                        if (e + 2 < kPart) a1 = max3(a1, x[e + 2], x[e + 3]);
+                        if (e + 4 < kPart) a2 = max3(a2, x[e + 4], x[e + 5]);
                     }
-                    top = fmaxf(fmaxf(a0, a1), fmaxf(a2, a3)) * kScaleLog2;
+                    top = max3(a0, a1, a2);
                 }
+                top *= kScaleLog2;
                 const bool raise = top > m + kLazy;
                 if (__any_sync(0xffffffffu, raise)) {
                     const float d = raise ? ex2(m - top) : 1.0f;
@@ -990,13 +1020,15 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
                 const uint64_t scale2 = pair(kScaleLog2, kScaleLog2), ref2 = pair(-ref, -ref);
                 uint64_t l2 = pair(0.0f, 0.0f);
                 // Two tiles: weights go out in two halves, the product over the first 64 keys runs beside the other exponentials.
-#pragma unroll
+#pragma unroll(kTwice ? 1 : 4)
                 for (int c = 0; c < kCols / 32; c++) {
+                    if constexpr (kTwice) look(32 * c);
+                    const int c0 = kTwice ? 0 : 32 * c;
                     uint32_t r[16];
 #pragma unroll
                     for (int e = 0; e < 16; e++) {
                         float u, v;
-                        unpair(fma2(pair(x[32 * c + 2 * e], x[32 * c + 2 * e + 1]), scale2, ref2), u, v);
+                        unpair(fma2(pair(x[c0 + 2 * e], x[c0 + 2 * e + 1]), scale2, ref2), u, v);
                         u = ex2(u);
                         v = ex2(v);
                         l2 = add2(l2, pair(u, v));
@@ -1151,25 +1183,25 @@ prompt_join_kernel(PromptWorkspace ws, int rows_max, int n_kv, __nv_bfloat16 *__
     }
 }
 
-template <int kBits, int kTiles, int kCopies>
+template <int kBits, int kTiles, int kCopies, bool kWide>
 pask_status_t launch(const PromptParams &p, const CUtensorMap &map_q, const CUtensorMap &map_k, const CUtensorMap &map_v, int dev, cudaStream_t stream) {
-    constexpr int kSmem = (int)sizeof(PromptSmem<kTiles, kCopies>);
+    constexpr int kSmem = (int)sizeof(PromptSmem<kTiles, kCopies, kWide>);
     static_assert(kSmem <= 232448, "shared memory of a CTA");
     static bool granted[64] = {};                  // a property of (device, kernel)
     if (!granted[dev]) {
-        if (cudaFuncSetAttribute(prompt_kernel<kBits, kTiles, kCopies>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess) return PASK_ERR_CUDA;
+        if (cudaFuncSetAttribute(prompt_kernel<kBits, kTiles, kCopies, kWide>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess) return PASK_ERR_CUDA;
         granted[dev] = true;
     }
-    return launch_pdl(prompt_kernel<kBits, kTiles, kCopies>, dim3(p.grid), dim3(kThreads), kSmem, stream, p, map_q, map_k, map_v) == cudaSuccess ? PASK_OK
+    return launch_pdl(prompt_kernel<kBits, kTiles, kCopies, kWide>, dim3(p.grid), dim3(PromptSmem<kTiles, kCopies, kWide>::kThreads), kSmem, stream, p, map_q, map_k, map_v) == cudaSuccess ? PASK_OK
                                                                                                                                      : PASK_ERR_CUDA;
 }
 
-template <int kTiles, int kCopies>
+template <int kTiles, int kCopies, bool kWide>
 pask_status_t launch_bits(uint32_t bits, const PromptParams &p, const CUtensorMap &map_q, const CUtensorMap &map_k, const CUtensorMap &map_v, int dev,
                           cudaStream_t stream) {
-    return bits == 8 ? launch<8, kTiles, kCopies>(p, map_q, map_k, map_v, dev, stream)
-           : bits == 2 ? launch<2, kTiles, kCopies>(p, map_q, map_k, map_v, dev, stream)
-                       : launch<4, kTiles, kCopies>(p, map_q, map_k, map_v, dev, stream);
+    return bits == 8 ? launch<8, kTiles, kCopies, kWide>(p, map_q, map_k, map_v, dev, stream)
+           : bits == 2 ? launch<2, kTiles, kCopies, kWide>(p, map_q, map_k, map_v, dev, stream)
+                       : launch<4, kTiles, kCopies, kWide>(p, map_q, map_k, map_v, dev, stream);
 }
 
 // Tokens of an item: 64 (two tiles), or 32, 16, 8 (one tile)
@@ -1219,7 +1251,8 @@ pask_status_t launch_prompt(pask_cache *c, int layer, int n_seqs, int total_toke
     if (launch_pdl(prompt_plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, d, layer, n_seqs, total_tokens, seq_ids, cu_tokens, p.ws, p.grid,
                    tokens, static_cast<uint4 *>(out), lse) != cudaSuccess)
         return PASK_ERR_CUDA;
-    const auto fn = tokens == 64 ? launch_bits<2, 1> : tokens == 32 ? launch_bits<1, 1> : tokens == 16 ? launch_bits<1, 2> : launch_bits<1, 4>;
+    const auto fn = tokens == 64 ? (true ? launch_bits<2, 1, true> : launch_bits<2, 1, false>)
+                    : tokens == 32 ? launch_bits<1, 1, true> : tokens == 16 ? launch_bits<1, 2, true> : launch_bits<1, 4, true>;
     const pask_status_t ok = fn(d.low_bits, p, map_q, map_k, map_v, c->device, stream);
     if (ok != PASK_OK) return ok;
     return launch_pdl(prompt_join_kernel, dim3(p.grid, kJoinCtas), dim3(kJoinThreads), 0, stream, p.ws, tokens * kGqa, n_kv, p.out, lse) == cudaSuccess
