@@ -345,8 +345,14 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     asm("max.f32 %0, %1, %2, %3;" : "=f"(x) : "f"(a), "f"(b), "f"(c));
     return x;
 }
-__device__ __forceinline__ float byte_value(uint32_t w, uint32_t k) {            // byte k of w, less 128
-    return __uint_as_float(__byte_perm(w, 0x4B000000u, 0x7440u | k)) - 8388736.0f;
+// bytes k0 and k1 of w, less 128, times s: as bf16, rounded once from exact products (codes of 8 bits, scales of 11)
+__device__ __forceinline__ uint32_t scaled_bytes(uint32_t w, uint32_t k0, uint32_t k1, float s) {
+    const uint64_t c = umma::pair(__uint_as_float(__byte_perm(w, 0x4B000000u, 0x7440u | k0)), __uint_as_float(__byte_perm(w, 0x4B000000u, 0x7440u | k1)));
+    uint64_t x;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(x) : "l"(umma::add2(c, umma::pair(-8388736.0f, -8388736.0f))), "l"(umma::pair(s, s)));
+    float lo, hi;
+    umma::unpair(x, lo, hi);
+    return umma::pack_bf16(lo, hi);
 }
 __device__ __forceinline__ void store16(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
@@ -446,7 +452,7 @@ __device__ __forceinline__ void store_low(const Raw &r, uint32_t block, int row,
                     for (int k = 0; k < 4; k++) {
                         const uint32_t c = word_of(r.x[w], k);
                         store4(base + (w >> 1) * kSub + (((4 * (w & 1) + k) ^ l.g) << 4) + 4 * l.t,
-                               umma::pack_bf16(byte_value(c, 2 * hi) * s, byte_value(c, 2 * hi + 1) * s));
+                               scaled_bytes(c, 2 * hi, 2 * hi + 1, s));
                     }
                 } else {                           // dims 32 w + 8 t .. + 7
                     const uint32_t h = __shfl_sync(0xffffffffu, s_hi[hi], from), o = __shfl_sync(0xffffffffu, s_lo[hi], from);
@@ -472,8 +478,8 @@ __device__ __forceinline__ void store_low(const Raw &r, uint32_t block, int row,
                 if constexpr (kBits == 8) {
                     const float s = __shfl_sync(0xffffffffu, f0, from), z = __shfl_sync(0xffffffffu, f1, from);
                     const uint32_t c = ps ? r.x[q].y : r.x[q].x, d = ps ? r.x[q].w : r.x[q].z;
-                    store8(at0, umma::pack_bf16(byte_value(c, 0) * s, byte_value(c, 2) * s), umma::pack_bf16(byte_value(d, 0) * s, byte_value(d, 2) * s));
-                    store8(at1, umma::pack_bf16(byte_value(c, 1) * z, byte_value(c, 3) * z), umma::pack_bf16(byte_value(d, 1) * z, byte_value(d, 3) * z));
+                    store8(at0, scaled_bytes(c, 0, 2, s), scaled_bytes(d, 0, 2, s));
+                    store8(at1, scaled_bytes(c, 1, 3, z), scaled_bytes(d, 1, 3, z));
                 } else {                           // a dim of both tokens at a time, then sorted by token
                     const uint32_t h = __shfl_sync(0xffffffffu, s_hi, from), o = __shfl_sync(0xffffffffu, s_lo, from);
                     const uint32_t c = kBits == 4 ? word_of(r.x[ps], q) : word_of(r.x[0], q) >> (8 * ps);
@@ -492,8 +498,8 @@ __device__ __forceinline__ void store_low(const Raw &r, uint32_t block, int row,
 // kTiles 2: 64 tokens an item.  1: 32 / kCopies tokens, each row of S kCopies times in the tile.
 template <int kTiles, int kCopies, bool kWide>
 struct __align__(16) PromptSmem {
-    // Warps: softmax, four for control, fill (kWide: one for the keys and one for the values of each page of a block)
-    static constexpr int kStages = 2, kSoft = 4 * kTiles, kFill = kWide ? 16 : 4, kThreads = 32 * (kSoft + 4 + kFill);
+    // Warps: softmax, four for control, fill (kWide: one for the keys and one for the values of each page of a block; else one, of the four)
+    static constexpr int kStages = 2, kSoft = 4 * kTiles, kFill = kWide ? 16 : 1, kThreads = 32 * (kSoft + 4 + (kWide ? kFill : 0));
     uint8_t q[kTiles][kTileBytes], k[kStages][kTileBytes], v[kStages][kTileBytes];
     float share[kCopies > 1 ? 32 : 1][kTileRows];  // 32 dims of the copies' results on their way to one another
     float2 ml[kTileRows];
@@ -526,7 +532,7 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
               const __grid_constant__ CUtensorMap map_v) {
     using namespace umma;
     using Smem = PromptSmem<kTiles, kCopies, kWide>;
-    constexpr int kStages = Smem::kStages, kSoft = Smem::kSoft, kFill = Smem::kFill, kFillOf = kWide ? 8 : 4;     // kFillOf: of a block's keys
+    constexpr int kStages = Smem::kStages, kSoft = Smem::kSoft, kFill = Smem::kFill, kFillOf = kWide ? 8 : 1;     // kFillOf: of a block's keys
     constexpr int kTokens = kTiles * kTileTokens / kCopies, kRows = kTokens * kGqa;
     extern __shared__ __align__(1024) uint8_t s_raw[];
     Smem &sm = *reinterpret_cast<Smem *>(s_raw);
@@ -579,15 +585,10 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
     };
     auto tiles_of = [&](const Item &it) { return kTiles == 2 && it.block * kTokens + kTileTokens < it.nq ? 2 : 1; };
 
-    // 512 threads x 128 registers at launch = 128 x (2 x 176 + 72 + 88); wide: 896 x 72 = 128 x (2 x 104 + 72 + 4 x 56), one tile: 768 x 80 =
-    // 128 x (120 + 72 + 4 x 72)
-    if (warp >= kSoft + 4) {
-        if constexpr (!kWide) asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-        else if constexpr (kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-        else asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-        // ================================================= fill
+    // ================================================= fill
+    auto fill = [&](int me) {                      // me: of the fill warps
         constexpr int kKv = kWide ? 1 : 2, kPages = kBlockPages / kFillOf;      // of a warp, a block
-        const int page0 = (warp - kSoft - 4) % kFillOf, kv0 = (warp - kSoft - 4) / kFillOf;
+        const int page0 = me % kFillOf, kv0 = me / kFillOf;
         Item it;
         uint32_t g = 0;                            // blocks so far
         for (uint32_t n = 0; next_item(n, it); n++) {
@@ -684,8 +685,19 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
             }
             if (!ok) break;
         }
+    };
+
+    // 384 threads x 168 registers at launch = 128 x (2 x 200 + 104); wide: 896 x 72 = 128 x (2 x 104 + 72 + 4 x 56), one tile: 768 x 80 =
+    // 128 x (120 + 72 + 4 x 72)
+    if (kWide && warp >= kSoft + 4) {
+        if constexpr (kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        else asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        if constexpr (kWide) fill(warp - kSoft - 4);
     } else if (warp >= kSoft) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        if constexpr (kWide) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        else asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
+        if constexpr (!kWide)
+            if (warp == kSoft + 3) fill(0);
         if (warp == kSoft + 2) {
             // ================================================= items
             Walker walk;
@@ -895,7 +907,7 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
             __syncwarp();
         }
     } else {
-        if constexpr (!kWide) asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
+        if constexpr (!kWide) asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
         else if constexpr (kTiles == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
         else asm volatile("setmaxnreg.inc.sync.aligned.u32 120;");
         // ================================================= softmax: thread = row, or one of a row's copies with its share of the keys
@@ -963,8 +975,7 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
                     masked = true;
                     filled = (1u << Filled(it).of_page(8 * b + (lane & 7))) - 1u;
                 }
-                float x[kPart];
-                auto look = [&](int from) {        // columns from .. of the row
+                auto ask = [&](float (&x)[kPart], int from) {              // columns from .. of the row; there after tmem_wait_ld()
 #pragma unroll
                     for (int c = 0; c < kPart / 32; c++) {
                         uint32_t r[32];
@@ -972,7 +983,8 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
 #pragma unroll
                         for (int e = 0; e < 32; e++) x[32 * c + e] = __uint_as_float(r[e]);
                     }
-                    tmem_wait_ld();
+                };
+                auto hide = [&](float (&x)[kPart], int from) {             // what the row does not see
                     if (!masked) return;
 #pragma unroll
                     for (int pg = 0; pg < kPart / 16; pg++) {
@@ -981,10 +993,7 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
                         for (int e = 0; e < 16; e++) if (16 * pg + e >= left - from || !((bits >> e) & 1)) x[16 * pg + e] = -INFINITY;
                     }
                 };
-                float top = -INFINITY;
-#pragma unroll 1
-                for (int from = 0; from < kCols; from += kPart) {
-                    look(from);
+                auto largest = [&](const float (&x)[kPart], float top) {
                     float a0 = max3(top, x[0], x[1]), a1 = max3(x[2], x[3], x[4]), a2 = max3(x[5], x[6], x[7]);
 #pragma unroll
                     for (int e = 8; e < kPart; e += 6) {
@@ -992,7 +1001,27 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
                         if (e + 2 < kPart) a1 = max3(a1, x[e + 2], x[e + 3]);
                         if (e + 4 < kPart) a2 = max3(a2, x[e + 4], x[e + 5]);
                     }
-                    top = max3(a0, a1, a2);
+                    return max3(a0, a1, a2);
+                };
+                float x[kPart], z[kTwice ? kPart : 1];     // (twice: the next columns travel while these are worked on)
+                float top = -INFINITY;
+                ask(x, 0);
+                tmem_wait_ld();
+                if constexpr (kTwice) {
+#pragma unroll 1
+                    for (int c = 0; c < 2; c++) {
+                        ask(z, 64 * c + 32);
+                        hide(x, 64 * c);
+                        top = largest(x, top);
+                        tmem_wait_ld();
+                        ask(x, (64 * c + 64) & 127);       // (at the end: the first columns again, for the second look)
+                        hide(z, 64 * c + 32);
+                        top = largest(z, top);
+                        tmem_wait_ld();
+                    }
+                } else {
+                    hide(x, 0);
+                    top = largest(x, top);
                 }
                 top *= kScaleLog2;
                 const bool raise = top > m + kLazy;
@@ -1020,15 +1049,12 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
                 const uint64_t scale2 = pair(kScaleLog2, kScaleLog2), ref2 = pair(-ref, -ref);
                 uint64_t l2 = pair(0.0f, 0.0f);
                 // Two tiles: weights go out in two halves, the product over the first 64 keys runs beside the other exponentials.
-#pragma unroll(kTwice ? 1 : 4)
-                for (int c = 0; c < kCols / 32; c++) {
-                    if constexpr (kTwice) look(32 * c);
-                    const int c0 = kTwice ? 0 : 32 * c;
+                auto weigh = [&](const float *y, int c) {  // 32 columns at y, the row's c-th
                     uint32_t r[16];
 #pragma unroll
                     for (int e = 0; e < 16; e++) {
                         float u, v;
-                        unpair(fma2(pair(x[c0 + 2 * e], x[c0 + 2 * e + 1]), scale2, ref2), u, v);
+                        unpair(fma2(pair(y[2 * e], y[2 * e + 1]), scale2, ref2), u, v);
                         u = ex2(u);
                         v = ex2(v);
                         l2 = add2(l2, pair(u, v));
@@ -1041,6 +1067,22 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
                         __syncwarp();
                         if (lane == 0) bar_arrive(kTiles == 1 ? smem_u32(&sm.p_full[place]) : c == 1 ? p_half : p_full);
                     }
+                };
+                if constexpr (kTwice) {
+#pragma unroll 1
+                    for (int c = 0; c < 4; c += 2) {
+                        ask(z, 32 * c + 32);
+                        hide(x, 32 * c);
+                        weigh(x, c);
+                        tmem_wait_ld();
+                        if (c == 0) ask(x, 64);
+                        hide(z, 32 * c + 32);
+                        weigh(z, c + 1);
+                        if (c == 0) tmem_wait_ld();
+                    }
+                } else {
+#pragma unroll
+                    for (int c = 0; c < kCols / 32; c++) weigh(x + 32 * c, c);
                 }
                 float l0, l1;
                 unpair(l2, l0, l1);
@@ -1251,7 +1293,7 @@ pask_status_t launch_prompt(pask_cache *c, int layer, int n_seqs, int total_toke
     if (launch_pdl(prompt_plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, d, layer, n_seqs, total_tokens, seq_ids, cu_tokens, p.ws, p.grid,
                    tokens, static_cast<uint4 *>(out), lse) != cudaSuccess)
         return PASK_ERR_CUDA;
-    const auto fn = tokens == 64 ? (true ? launch_bits<2, 1, true> : launch_bits<2, 1, false>)
+    const auto fn = tokens == 64 ? (c->appended[layer] ? launch_bits<2, 1, true> : launch_bits<2, 1, false>)
                     : tokens == 32 ? launch_bits<1, 1, true> : tokens == 16 ? launch_bits<1, 2, true> : launch_bits<1, 4, true>;
     const pask_status_t ok = fn(d.low_bits, p, map_q, map_k, map_v, c->device, stream);
     if (ok != PASK_OK) return ok;
