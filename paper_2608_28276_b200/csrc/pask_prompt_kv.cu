@@ -59,7 +59,7 @@ struct PromptWorkspace {
     PromptSeq *seqs;                               // [n_seqs]
     Join *joins;                                   // [grid] the item in parts that begins with this CTA's part
     float2 *ml;                                    // [2 grid][rows] reference maximum in log2 units, sum
-    float4 *o;                                     // [2 grid][32][rows] unscaled outputs, four dims a piece
+    float4 *o;                                     // [2 grid][rows][32] unscaled outputs, four dims a piece
 };
 
 size_t carve(int n_seqs, int grid, int rows, uint8_t *base, PromptWorkspace *ws) {
@@ -102,13 +102,15 @@ __host__ __device__ __forceinline__ long long own_blocks_before(int j, int token
 
 constexpr int kPlanThreads = 1024;
 
-// One CTA, a sequence a thread: what each has to attend, the line of costs.
+// One CTA, a sequence a thread: what each has to attend, the line of costs.  (A CTA of as few warps as there are sequences for: its
+// barriers are most of its time.)
 __global__ void __launch_bounds__(kPlanThreads)
 prompt_plan_kernel(DevCache c, int layer, int n_seqs, int total, const int32_t *__restrict__ seq_ids, const int32_t *__restrict__ cu,
                    PromptWorkspace ws, int grid, int block_tokens, uint4 *__restrict__ out, float *__restrict__ lse) {
     __shared__ uint64_t s_sum[32];
-    __shared__ uint32_t s_parts, s_items, s_longest, s_bad;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    __shared__ uint32_t s_part, s_items, s_longest, s_bad;
+    __shared__ int2 s_seq[kPlanThreads];           // items and key blocks of the longest, of each sequence
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x;
     pdl_launch_dependents();
     pdl_wait();
     if (tid == 0) s_items = s_longest = s_bad = 0;
@@ -154,23 +156,24 @@ prompt_plan_kernel(DevCache c, int layer, int n_seqs, int total, const int32_t *
         atomicAdd(&s_items, (uint32_t)(nqb * c.n_kv));
         atomicMax(&s_longest, (uint32_t)longest);
     }
+    s_seq[tid] = make_int2(nqb ? min(nqb, grid + 1) * c.n_kv : 0, longest);
     const bool many = __syncthreads_or(nqb > grid);
     if (tid == 0 && s_bad) atomicOr(&c.ctrl[kCtrlStatus], s_bad);
     uint64_t cost = (uint64_t)c.n_kv * ((uint64_t)nqb * (uint64_t)(s.blocks + kItemCost) + (uint64_t)own_blocks_before(nqb, block_tokens));
     if (!many && s_items <= (uint32_t)grid) {
         // Whole CTAs for each item: the shortest part length for which the grid has enough of them
-        uint32_t lo = kMinPiece, hi = max(s_longest, (uint32_t)kMinPiece);
-        while (lo < hi) {
-            const uint32_t mid = (lo + hi) / 2;
-            if (tid == 0) s_parts = 0;
-            __syncthreads();
-            if (nqb) atomicAdd(&s_parts, (uint32_t)(c.n_kv * nqb) * ((longest + mid - 1) / mid));
-            __syncthreads();
-            const bool fits = s_parts <= (uint32_t)grid;
-            __syncthreads();
-            if (fits) hi = mid; else lo = mid + 1;
+        if (warp == 0) {
+            uint32_t lo = kMinPiece, hi = max(s_longest, (uint32_t)kMinPiece);
+            while (lo < hi) {
+                const uint32_t mid = (lo + hi) / 2;
+                uint32_t need = 0;
+                for (int i = lane; i < n_seqs; i += 32) need += s_seq[i].x * ((s_seq[i].y + mid - 1) / mid);
+                if (__reduce_add_sync(0xffffffffu, need) <= (uint32_t)grid) hi = mid; else lo = mid + 1;
+            }
+            if (lane == 0) s_part = lo;
         }
-        if (nqb) s.parts = (int)((longest + lo - 1) / lo);
+        __syncthreads();
+        s.parts = max(1, (int)((longest + s_part - 1) / s_part));          // (at least one: says that items have CTAs of their own)
         cost = (uint64_t)c.n_kv * nqb * s.parts;
     }
     // prefix over the sequences
@@ -197,9 +200,9 @@ prompt_plan_kernel(DevCache c, int layer, int n_seqs, int total, const int32_t *
             if (tid == i) { s_q0 = s.q0; s_n = unknown ? named : 0; }
             __syncthreads();
             const size_t heads = (size_t)kGqa * c.n_kv, from = (size_t)s_q0 * heads, count = (size_t)s_n * heads;
-            for (size_t e = tid; e < count * (kDim / 8); e += kPlanThreads) out[from * (kDim / 8) + e] = make_uint4(0, 0, 0, 0);
+            for (size_t e = tid; e < count * (kDim / 8); e += threads) out[from * (kDim / 8) + e] = make_uint4(0, 0, 0, 0);
             if (lse)
-                for (size_t e = tid; e < count; e += kPlanThreads) lse[from + e] = -INFINITY;
+                for (size_t e = tid; e < count; e += threads) lse[from + e] = -INFINITY;
         }
     }
 }
@@ -221,12 +224,14 @@ struct Walker {
     PromptSeq q;
     bool whole;                                    // whole CTAs for each item
     const PromptWorkspace *ws;
+    int step;                                      // sequences a lane stands for
+    uint64_t mine;                                 // where the last of them ends
 
     __device__ __forceinline__ uint64_t edge(uint64_t total, int b) const { return total * (uint64_t)b / (uint64_t)grid; }
     // sequences that end at or before x
     __device__ __forceinline__ int seqs_before(uint64_t x, int lane) const {
-        const int step = (n_seqs + 31) / 32;
-        const int n = __popc(__ballot_sync(0xffffffffu, (lane + 1) * step <= n_seqs && ws->prefix[min((lane + 1) * step, n_seqs)] <= x)) * step;
+        const int n = __popc(__ballot_sync(0xffffffffu, (lane + 1) * step <= n_seqs && mine <= x)) * step;
+        if (step == 1) return n;
         const int k = n + lane + 1;
         return n + __popc(__ballot_sync(0xffffffffu, lane < step && k <= n_seqs && ws->prefix[min(k, n_seqs)] <= x));
     }
@@ -238,8 +243,10 @@ struct Walker {
     __device__ __forceinline__ void init(const PromptParams &p, int block_tokens, int lane) {
         ws = &p.ws;
         cta = blockIdx.x; grid = p.grid; n_seqs = p.n_seqs; tokens = block_tokens; n_kv = p.n_kv;
+        step = (n_seqs + 31) / 32;
+        mine = ws->prefix[min((lane + 1) * step, n_seqs)];
         const uint64_t total = ws->prefix[n_seqs];
-        whole = ws->seqs[seqs_before(0, lane) < n_seqs ? seqs_before(0, lane) : 0].parts > 0;
+        whole = ws->seqs[0].parts > 0;
         if (whole) { x0 = cta; x1 = (uint64_t)cta + 1 <= total ? (uint64_t)cta + 1 : (uint64_t)cta; }
         else { x0 = edge(total, cta); x1 = edge(total, cta + 1); }
         if (x0 >= x1) { s = n_seqs; return; }
@@ -1137,7 +1144,7 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
                     } else if (live) {
 #pragma unroll
                         for (int e = 0; e < kOwn; e += 4)
-                            __stcg(p.ws.o + (part * (kDim / 4) + (d + e) / 4) * kRows + row_in, make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]));
+                            __stcg(p.ws.o + (part * kRows + row_in) * (kDim / 4) + (d + e) / 4, make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]));
                     }
                 }
                 if (!ok) break;
@@ -1166,7 +1173,7 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
                     } else if (live) {
 #pragma unroll
                         for (int h = 0; h < 4; h++)
-                            __stcg(p.ws.o + (part * (kDim / 4) + 4 * c + h) * kRows + row_in,
+                            __stcg(p.ws.o + (part * kRows + row_in) * (kDim / 4) + 4 * c + h,
                                    make_float4(__uint_as_float(r[4 * h]), __uint_as_float(r[4 * h + 1]), __uint_as_float(r[4 * h + 2]), __uint_as_float(r[4 * h + 3])));
                     }
                 }
@@ -1195,33 +1202,68 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
     if (warp == kSoft) tmem_free(tmem, 512);
 }
 
-// The items in parts: eight CTAs each, four dims of a row a thread; their parts in order.
-constexpr int kJoinThreads = 256, kJoinCtas = 8;
+// The rows of the items in parts, a warp each in turn: the parts' weights (a lane a part), then the sums, four dims a lane, over the parts
+// in order.
+constexpr int kJoinThreads = 512, kJoinCtas = 2, kMaxGrid = 256;
 __global__ void __launch_bounds__(kJoinThreads)
-prompt_join_kernel(PromptWorkspace ws, int rows_max, int n_kv, __nv_bfloat16 *__restrict__ out, float *__restrict__ lse) {
+prompt_join_kernel(PromptWorkspace ws, int grid, int rows_max, int n_kv, __nv_bfloat16 *__restrict__ out, float *__restrict__ lse) {
     using namespace umma;
+    __shared__ int s_end[kMaxGrid];                // rows of the items up to this one
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     pdl_launch_dependents();
     pdl_wait();
-    const Join j = ws.joins[blockIdx.x];
+    if (warp == 0) {
+        int carry = 0;
+        for (int b = 0; b < grid; b += 32) {
+            int inc = b + lane < grid ? ws.joins[b + lane].rows : 0;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int o = __shfl_up_sync(0xffffffffu, inc, d);
+                if (lane >= d) inc += o;
+            }
+            if (b + lane < grid) s_end[b + lane] = carry + inc;
+            carry += __shfl_sync(0xffffffffu, inc, 31);
+        }
+    }
+    __syncthreads();
     const size_t heads = (size_t)kGqa * n_kv;
-    for (int u = blockIdx.y * kJoinThreads + threadIdx.x; u < j.rows * (kDim / 4); u += kJoinCtas * kJoinThreads) {
-        const int d = u / j.rows, r = u - d * j.rows;
+    for (int at = blockIdx.x * (kJoinThreads / 32) + warp; at < s_end[grid - 1]; at += gridDim.x * (kJoinThreads / 32)) {
+        int lo = 0, hi = grid - 1;                 // the first item that ends behind row `at`
+        while (lo < hi) {
+            const int mid = (lo + hi) / 2;
+            if (s_end[mid] > at) hi = mid; else lo = mid + 1;
+        }
+        const Join j = ws.joins[lo];
+        const int r = at - (lo ? s_end[lo - 1] : 0), parts = j.last - j.first + 1;
+        // a CTA's part of the item: place 2 c, the first one's 2 c + 1
+        auto place = [&](int c) { return (2 * (size_t)(j.first + c) + (c == 0)) * rows_max + r; };
         float top = -INFINITY, sum = 0.0f;
-        float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 6
-        for (int c = j.first; c <= j.last; c++) {
-            const size_t at = 2 * (size_t)c + (c == j.first);
-            const float2 ml = __ldcg(ws.ml + at * rows_max + r);
-            const float4 y = __ldcg(ws.o + (at * (kDim / 4) + d) * rows_max + r);
-            const float next = fmaxf(top, ml.x), ref = next == -INFINITY ? 0.0f : next, a = ex2(top - ref), w = ex2(ml.x - ref);
+        float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int c0 = 0; c0 < parts; c0 += 32) {
+            const int n = min(32, parts - c0);
+            const float2 ml = lane < n ? __ldcg(ws.ml + place(c0 + lane)) : make_float2(-INFINITY, 0.0f);
+            float next = ml.x;
+#pragma unroll
+            for (int d = 16; d; d >>= 1) next = fmaxf(next, __shfl_xor_sync(0xffffffffu, next, d));
+            next = fmaxf(next, top);
+            const float ref = next == -INFINITY ? 0.0f : next, old = ex2(top - ref), w = ex2(ml.x - ref);
+            float share = ml.y * w;
+#pragma unroll
+            for (int d = 16; d; d >>= 1) share += __shfl_xor_sync(0xffffffffu, share, d);
             top = next;
-            sum = sum * a + ml.y * w;
-            o.x = o.x * a + y.x * w; o.y = o.y * a + y.y * w; o.z = o.z * a + y.z * w; o.w = o.w * a + y.w * w;
+            sum = sum * old + share;
+            x.x *= old; x.y *= old; x.z *= old; x.w *= old;
+#pragma unroll 8
+            for (int c = 0; c < n; c++) {
+                const float4 y = __ldcg(ws.o + place(c0 + c) * (kDim / 4) + lane);
+                const float v = __shfl_sync(0xffffffffu, w, c);
+                x.x += y.x * v; x.y += y.y * v; x.z += y.z * v; x.w += y.w * v;
+            }
         }
         const float inv = 1.0f / sum;
         const size_t to = (size_t)(j.row + r / kGqa) * heads + kGqa * j.head + (r & 3);
-        *reinterpret_cast<uint2 *>(out + to * kDim + 4 * d) = make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
-        if (d == 0 && lse) lse[to] = (top + log2f(sum)) * 0.69314718055994531f;
+        *reinterpret_cast<uint2 *>(out + to * kDim + 4 * lane) = make_uint2(pack_bf16(x.x * inv, x.y * inv), pack_bf16(x.z * inv, x.w * inv));
+        if (lane == 0 && lse) lse[to] = (top + log2f(sum)) * 0.69314718055994531f;
     }
 }
 
@@ -1254,8 +1296,10 @@ int tokens_for(int n_seqs, int total_tokens) {
 
 }  // namespace
 
+static int prompt_grid(const pask_cache *c) { return c->sm_count < kMaxGrid ? c->sm_count : kMaxGrid; }
+
 size_t prompt_workspace_bytes(const pask_cache *c, int n_seqs, int total_tokens) {
-    return carve(n_seqs, c->sm_count, tokens_for(n_seqs, total_tokens) * kGqa, nullptr, nullptr);
+    return carve(n_seqs, prompt_grid(c), tokens_for(n_seqs, total_tokens) * kGqa, nullptr, nullptr);
 }
 
 pask_status_t launch_prompt(pask_cache *c, int layer, int n_seqs, int total_tokens, const int32_t *seq_ids, const int32_t *cu_tokens, const void *q,
@@ -1269,7 +1313,7 @@ pask_status_t launch_prompt(pask_cache *c, int layer, int n_seqs, int total_toke
         return PASK_ERR_CUDA;
     const DevCache &d = c->dev;
     PromptParams p{};
-    carve(n_seqs, c->sm_count, tokens * kGqa, static_cast<uint8_t *>(workspace), &p.ws);
+    carve(n_seqs, prompt_grid(c), tokens * kGqa, static_cast<uint8_t *>(workspace), &p.ws);
     p.pool_high = d.pool_high;
     p.pool_low = d.pool_low;
     p.tbl_high = d.tbl_high;
@@ -1285,19 +1329,20 @@ pask_status_t launch_prompt(pask_cache *c, int layer, int n_seqs, int total_toke
     p.max_pages = d.max_pages;
     p.n_kv = n_kv;
     p.n_seqs = n_seqs;
-    p.grid = c->sm_count;
+    p.grid = prompt_grid(c);
     p.out = static_cast<__nv_bfloat16 *>(out);
     p.lse = lse;
     p.wait_cycles = c->wait_cycles;
     p.surplus = c->wait_test_surplus;
-    if (launch_pdl(prompt_plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, d, layer, n_seqs, total_tokens, seq_ids, cu_tokens, p.ws, p.grid,
+    if (launch_pdl(prompt_plan_kernel, dim3(1), dim3((n_seqs + 31) / 32 * 32), 0, stream, d, layer, n_seqs, total_tokens, seq_ids, cu_tokens, p.ws, p.grid,
                    tokens, static_cast<uint4 *>(out), lse) != cudaSuccess)
         return PASK_ERR_CUDA;
     const auto fn = tokens == 64 ? (c->appended[layer] ? launch_bits<2, 1, true> : launch_bits<2, 1, false>)
                     : tokens == 32 ? launch_bits<1, 1, true> : tokens == 16 ? launch_bits<1, 2, true> : launch_bits<1, 4, true>;
     const pask_status_t ok = fn(d.low_bits, p, map_q, map_k, map_v, c->device, stream);
     if (ok != PASK_OK) return ok;
-    return launch_pdl(prompt_join_kernel, dim3(p.grid, kJoinCtas), dim3(kJoinThreads), 0, stream, p.ws, tokens * kGqa, n_kv, p.out, lse) == cudaSuccess
+    return launch_pdl(prompt_join_kernel, dim3(kJoinCtas * c->sm_count), dim3(kJoinThreads), 0, stream, p.ws, p.grid, tokens * kGqa, n_kv, p.out, lse) ==
+                   cudaSuccess
                ? PASK_OK
                : PASK_ERR_CUDA;
 }
