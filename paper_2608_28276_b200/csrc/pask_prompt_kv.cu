@@ -511,7 +511,7 @@ struct __align__(16) PromptSmem {
     float share[kCopies > 1 ? 32 : 1][kTileRows];  // 32 dims of the copies' results on their way to one another
     float2 ml[kTileRows];
     uint64_t q_full, q_empty, k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages];
-    uint64_t s_full[2], p_half[2], p_full[2], pv_done[2], o_free[2];             // of a tile; one tile: the first three of a place of S,
+    uint64_t s_full[2], p_half[2], p_full[2], pv_half[2], pv_done[2], o_free[2];             // of a tile; one tile: the first three of a place of S,
                                                    // pv_done of a block and of an item's last one
     uint64_t item_full[2], item_empty[2], copies, drain;
     Item item[2];
@@ -559,6 +559,7 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
             bar_init(smem_u32(&sm.s_full[i]), 1);
             bar_init(smem_u32(&sm.p_half[i]), 4);
             bar_init(smem_u32(&sm.p_full[i]), 4);
+            bar_init(smem_u32(&sm.pv_half[i]), 1);
             bar_init(smem_u32(&sm.pv_done[i]), 1);
             bar_init(smem_u32(&sm.o_free[i]), 4);
         }
@@ -799,11 +800,10 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
                 __syncwarp();
             };
             // the call's own rows behind the last token in its step of 16 count as zero
-            auto zero_rows = [&](uint32_t st, int valid, int steps) {
-                if (!(valid & 15)) return;
-                const int rows = 16 * steps - valid;
-                for (int e = lane; e < rows * 16; e += 32)
-                    *reinterpret_cast<uint4 *>(sm.v[st] + ((e >> 3) & 1) * kSub + (valid + (e >> 4)) * 128 + (e & 7) * 16) = make_uint4(0, 0, 0, 0);
+            auto zero_rows = [&](uint32_t st, int left, int steps) {
+                if (16 * steps <= left) return;
+                for (int e = lane; e < (16 * steps - left) * 16; e += 32)
+                    *reinterpret_cast<uint4 *>(sm.v[st] + ((e >> 3) & 1) * kSub + (left + (e >> 4)) * 128 + (e & 7) * 16) = make_uint4(0, 0, 0, 0);
                 fence_async_shared();
                 __syncwarp();
             };
@@ -827,8 +827,10 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
                 }
                 const int pages = pages_of(it.nh) + pages_of(it.nl) + pages_of(it.nw);
                 for (int j = 0; j < nb; j++, g++) {
+                    // slots of the block with a token, and of those the ones that the item looks at
                     const int b = it.b0 + j, left = b < it.hist ? (pages - kBlockPages * b) * kPageTokens : it.nq - (b - it.hist) * kBlockK;
-                    const int valid = __shfl_sync(0xffffffffu, min(kBlockK, left), 0), steps = (valid + 15) / 16;
+                    const int seen = b < it.hist ? left : min(it.nq, (it.block + 1) * kTokens) - (b - it.hist) * kBlockK;
+                    const int steps = __shfl_sync(0xffffffffu, (min(kBlockK, seen) + 15) / 16, 0);
                     const uint32_t st = __shfl_sync(0xffffffffu, g % kStages, 0), ph = (g / kStages) & 1;
                     const uint32_t st1 = __shfl_sync(0xffffffffu, (g + 1) % kStages, 0), ph1 = ((g + 1) / kStages) & 1;
                     if constexpr (kTiles == 1) {
@@ -849,12 +851,20 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
                             if (oc[0] > 0) ok = bar_wait(smem_u32(&sm.o_free[0]), (oc[0] - 1) & 1, limit);
                             oc[0]++;
                         }
-                        ok = bar_wait(smem_u32(&sm.p_full[at]), (g >> 1) & 1, limit) && ok;
                         ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.v_full[st]), ph, limit) && ok);
                         if (!ok) break;
+                        zero_rows(st, left, steps);
+                        if constexpr (kCopies == 1) {
+                            ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.p_half[at]), (g >> 1) & 1, limit));
+                            if (!ok) break;
+                            fence_after();
+                            values(at, st, j == 0, 0, min(4, steps));
+                            if (mine) commit(smem_u32(&sm.pv_half[0]));
+                        }
+                        ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.p_full[at]), (g >> 1) & 1, limit));
+                        if (!ok) break;
                         fence_after();
-                        zero_rows(st, valid, steps);
-                        values(at, st, j == 0, 0, steps);
+                        values(at, st, j == 0, kCopies == 1 ? 4 : 0, steps);
                         if (mine) {
                             commit(smem_u32(&sm.v_empty[st]));
                             commit(smem_u32(&sm.pv_done[0]));
@@ -866,7 +876,7 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
                     bool have_k = false;
                     ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.v_full[st]), ph, limit));
                     if (!ok) break;
-                    zero_rows(st, valid, steps);
+                    zero_rows(st, left, steps);
 #pragma unroll
                     for (int t = 0; t < kTiles; t++) {
                         if (t >= nt) continue;
@@ -878,6 +888,7 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
                         if (!ok) break;
                         fence_after();
                         values(t, st, j == 0, 0, min(4, steps));
+                        if (mine) commit(smem_u32(&sm.pv_half[t]));
                         ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.p_full[t]), pc[t] & 1, limit));
                         if (!ok) break;
                         pc[t]++;
@@ -918,12 +929,11 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
         else if constexpr (kTiles == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
         else asm volatile("setmaxnreg.inc.sync.aligned.u32 120;");
         // ================================================= softmax: thread = row, or one of a row's copies with its share of the keys
-        constexpr int kCols = kBlockK / kCopies, kCopyRows = kTileRows / kCopies;
+        constexpr int kCols = kBlockK / kCopies, kCopyRows = kTileRows / kCopies, kPart = kCols < 64 ? kCols : 64, kParts = kCols / kPart;
         const int t = warp >> 2, copy = (tid & (kTileRows - 1)) / kCopyRows;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, base = tmem + lanes + (kTiles == 2 ? t * 128 : copy * kCols);
         const uint32_t p_base = tmem + lanes + kP + (kTiles == 2 ? t * 128 : copy * (kCols / 2)), o_base = tmem + lanes + kO + t * 128;
-        const uint32_t s_full = smem_u32(&sm.s_full[t]), p_half = smem_u32(&sm.p_half[t]), p_full = smem_u32(&sm.p_full[t]),
-                       pv_done = smem_u32(&sm.pv_done[t]);
+        const uint32_t s_full = smem_u32(&sm.s_full[t]), pv_done = smem_u32(&sm.pv_done[t]);
         const int row_in = t * kTileRows + (tid & (kCopyRows - 1));
         uint32_t sc = 0, ic = 0, cc = 0;           // blocks of this tile (S, P and P V alike), items, exchanges between copies so far
         // a row's copies among themselves (all softmax warps)
@@ -952,12 +962,14 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
             const bool here = t == 0 || it.block * kTokens + kTileTokens < it.nq, live = i < it.nq;
             const int nb = here ? it.b1 - b0 : 0;
             const bool idle = !__any_sync(0xffffffffu, live);          // no row of this warp is one
+            int pages, own = min((int)it.nq, (it.block + 1) * kTokens);            // pages of the history, own tokens that the item looks at
             int part_h, part_l, part_w;            // the blocks with slots without a token (-1: none): ends of the streams and of the history
             {
                 const Filled f(it);
                 part_h = f.nh & 15 ? (f.ph - 1) >> 3 : -1;
                 part_l = f.nl & 15 ? (f.ph + f.pl - 1) >> 3 : -1;
                 part_w = f.nw & 15 || f.pages & 7 ? (f.pages - 1) >> 3 : -1;
+                pages = f.pages;
             }
             float m = -INFINITY, l = 0.0f;
             for (int j = 0; j < nb; j++, sc++) {
@@ -965,15 +977,15 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
                 const uint32_t place = kTiles == 2 ? 0 : sc & 1;
                 ok = kTiles == 2 ? bar_wait(s_full, sc & 1, limit) : bar_wait(smem_u32(&sm.s_full[place]), (sc >> 1) & 1, limit);
                 if (!__all_sync(0xffffffffu, ok)) break;
+                const uint32_t at = kTiles == 2 ? t : place;               // of p_half, p_full
                 if (idle) {
-                    if (lane == 0 && kTiles == 2) { bar_arrive(p_half); bar_arrive(p_full); }
-                    if (lane == 0 && kTiles == 1) bar_arrive(smem_u32(&sm.p_full[place]));
+                    if (lane == 0) {
+                        if (kParts == 2) bar_arrive(smem_u32(&sm.p_half[at]));
+                        bar_arrive(smem_u32(&sm.p_full[at]));
+                    }
                     continue;
                 }
                 fence_after();
-                // Wide, 128 columns: two looks at S, 32 columns at a time (the registers of a whole row are the fill warps')
-                constexpr bool kTwice = kWide && kCols == 128;
-                constexpr int kPart = kTwice ? 32 : kCols;
                 const bool causal = b >= hist;     // the call's own tokens: those up to the row's
                 const int left = !causal ? kCols : live ? i + 1 - (b - hist) * kBlockK - copy * kCols : 0;
                 uint32_t filled = 0xFFFFu;         // of page lane & 7 of the block
@@ -982,7 +994,17 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
                     masked = true;
                     filled = (1u << Filled(it).of_page(8 * b + (lane & 7))) - 1u;
                 }
-                auto ask = [&](float (&x)[kPart], int from) {              // columns from .. of the row; there after tmem_wait_ld()
+                // 128 columns go in two halves: the product over the first 64 keys runs beside the exponentials of the others
+                const int seen = causal ? own - (b - hist) * kBlockK : (pages - kBlockPages * b) * kPageTokens;
+#pragma unroll 1
+                for (int part = 0; part < kParts; part++) {
+                    const int from = part * kPart;
+                    if (kParts == 2 && from >= seen) {         // no row looks at the second half: no product takes it
+                        __syncwarp();
+                        if (lane == 0) bar_arrive(smem_u32(&sm.p_full[at]));
+                        break;
+                    }
+                    float x[kPart];
 #pragma unroll
                     for (int c = 0; c < kPart / 32; c++) {
                         uint32_t r[32];
@@ -990,110 +1012,70 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
 #pragma unroll
                         for (int e = 0; e < 32; e++) x[32 * c + e] = __uint_as_float(r[e]);
                     }
-                };
-                auto hide = [&](float (&x)[kPart], int from) {             // what the row does not see
-                    if (!masked) return;
+                    tmem_wait_ld();
+                    if (masked) {
 #pragma unroll
-                    for (int pg = 0; pg < kPart / 16; pg++) {
-                        const uint32_t bits = __shfl_sync(0xffffffffu, filled, pg + (copy * kCols + from) / 16);
+                        for (int pg = 0; pg < kPart / 16; pg++) {
+                            const uint32_t bits = __shfl_sync(0xffffffffu, filled, pg + (copy * kCols + from) / 16);
 #pragma unroll
-                        for (int e = 0; e < 16; e++) if (16 * pg + e >= left - from || !((bits >> e) & 1)) x[16 * pg + e] = -INFINITY;
+                            for (int e = 0; e < 16; e++) if (16 * pg + e >= left - from || !((bits >> e) & 1)) x[16 * pg + e] = -INFINITY;
+                        }
                     }
-                };
-                auto largest = [&](const float (&x)[kPart], float top) {
-                    float a0 = max3(top, x[0], x[1]), a1 = max3(x[2], x[3], x[4]), a2 = max3(x[5], x[6], x[7]);
+                    float a0 = max3(x[0], x[1], x[2]), a1 = max3(x[3], x[4], x[5]), a2 = fmaxf(x[6], x[7]);
 #pragma unroll
                     for (int e = 8; e < kPart; e += 6) {
                         a0 = max3(a0, x[e], x[e + 1]);
                         if (e + 2 < kPart) a1 = max3(a1, x[e + 2], x[e + 3]);
                         if (e + 4 < kPart) a2 = max3(a2, x[e + 4], x[e + 5]);
                     }
-                    return max3(a0, a1, a2);
-                };
-                float x[kPart], z[kTwice ? kPart : 1];     // (twice: the next columns travel while these are worked on)
-                float top = -INFINITY;
-                ask(x, 0);
-                tmem_wait_ld();
-                if constexpr (kTwice) {
-#pragma unroll 1
-                    for (int c = 0; c < 2; c++) {
-                        ask(z, 64 * c + 32);
-                        hide(x, 64 * c);
-                        top = largest(x, top);
-                        tmem_wait_ld();
-                        ask(x, (64 * c + 64) & 127);       // (at the end: the first columns again, for the second look)
-                        hide(z, 64 * c + 32);
-                        top = largest(z, top);
-                        tmem_wait_ld();
-                    }
-                } else {
-                    hide(x, 0);
-                    top = largest(x, top);
-                }
-                top *= kScaleLog2;
-                const bool raise = top > m + kLazy;
-                if (__any_sync(0xffffffffu, raise)) {
-                    const float d = raise ? ex2(m - top) : 1.0f;
-                    if (raise) { m = top; l *= d; }
-                    if (j > 0) {                   // O so far, in the new reference (two tiles: complete, this S was issued behind it)
-                        if (kTiles == 1) {         // (the product before that one is: this S was issued behind it)
-                            ok = __all_sync(0xffffffffu, bar_wait(pv_done, (sc - 1) & 1, limit));
+                    const float top = max3(a0, a1, a2) * kScaleLog2;
+                    const bool raise = top > m + kLazy;
+                    if (__any_sync(0xffffffffu, raise)) {
+                        const float d = raise ? ex2(m - top) : 1.0f;
+                        if (raise) { m = top; l *= d; }
+                        if (j > 0 || part > 0) {   // O so far, in the new reference, when the last product into it is done
+                            if (part > 0) ok = bar_wait(smem_u32(&sm.pv_half[t]), sc & 1, limit);
+                            else if (kTiles == 1) ok = bar_wait(pv_done, (sc - 1) & 1, limit);         // (two tiles: this S was issued behind it)
+                            ok = __all_sync(0xffffffffu, ok);
                             if (!ok) break;
                             fence_after();
-                        }
 #pragma unroll 1
-                        for (int c = 0; c < 8; c++) {
-                            uint32_t r[16];
-                            tmem_ld16(o_base + 16 * c, r);
-                            tmem_wait_ld();
+                            for (int c = 0; c < 8; c++) {
+                                uint32_t r[16];
+                                tmem_ld16(o_base + 16 * c, r);
+                                tmem_wait_ld();
 #pragma unroll
-                            for (int e = 0; e < 16; e++) r[e] = __float_as_uint(__uint_as_float(r[e]) * d);
-                            tmem_st16(o_base + 16 * c, r);
+                                for (int e = 0; e < 16; e++) r[e] = __float_as_uint(__uint_as_float(r[e]) * d);
+                                tmem_st16(o_base + 16 * c, r);
+                            }
                         }
                     }
-                }
-                const float ref = m == -INFINITY ? 0.0f : m;               // a row that has seen no key yet
-                const uint64_t scale2 = pair(kScaleLog2, kScaleLog2), ref2 = pair(-ref, -ref);
-                uint64_t l2 = pair(0.0f, 0.0f);
-                // Two tiles: weights go out in two halves, the product over the first 64 keys runs beside the other exponentials.
-                auto weigh = [&](const float *y, int c) {  // 32 columns at y, the row's c-th
-                    uint32_t r[16];
+                    const float ref = m == -INFINITY ? 0.0f : m;           // a row that has seen no key yet
+                    const uint64_t scale2 = pair(kScaleLog2, kScaleLog2), ref2 = pair(-ref, -ref);
+                    uint64_t l2 = pair(0.0f, 0.0f);
 #pragma unroll
-                    for (int e = 0; e < 16; e++) {
-                        float u, v;
-                        unpair(fma2(pair(y[2 * e], y[2 * e + 1]), scale2, ref2), u, v);
-                        u = ex2(u);
-                        v = ex2(v);
-                        l2 = add2(l2, pair(u, v));
-                        r[e] = pack_bf16(u, v);
-                    }
-                    tmem_st16(p_base + place * 64 + 16 * c, r);
-                    if (kTiles == 2 ? (c & 1) : c + 1 == kCols / 32) {
-                        tmem_wait_st();
-                        fence_before();
-                        __syncwarp();
-                        if (lane == 0) bar_arrive(kTiles == 1 ? smem_u32(&sm.p_full[place]) : c == 1 ? p_half : p_full);
-                    }
-                };
-                if constexpr (kTwice) {
-#pragma unroll 1
-                    for (int c = 0; c < 4; c += 2) {
-                        ask(z, 32 * c + 32);
-                        hide(x, 32 * c);
-                        weigh(x, c);
-                        tmem_wait_ld();
-                        if (c == 0) ask(x, 64);
-                        hide(z, 32 * c + 32);
-                        weigh(z, c + 1);
-                        if (c == 0) tmem_wait_ld();
-                    }
-                } else {
+                    for (int c = 0; c < kPart / 32; c++) {
+                        uint32_t r[16];
 #pragma unroll
-                    for (int c = 0; c < kCols / 32; c++) weigh(x + 32 * c, c);
+                        for (int e = 0; e < 16; e++) {
+                            float u, v;
+                            unpair(fma2(pair(x[32 * c + 2 * e], x[32 * c + 2 * e + 1]), scale2, ref2), u, v);
+                            u = ex2(u);
+                            v = ex2(v);
+                            l2 = add2(l2, pair(u, v));
+                            r[e] = pack_bf16(u, v);
+                        }
+                        tmem_st16(p_base + place * 64 + from / 2 + 16 * c, r);
+                    }
+                    tmem_wait_st();
+                    fence_before();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(smem_u32(part + 1 < kParts ? &sm.p_half[at] : &sm.p_full[at]));
+                    float l0, l1;
+                    unpair(l2, l0, l1);
+                    l += l0 + l1;
                 }
-                float l0, l1;
-                unpair(l2, l0, l1);
-                l += l0 + l1;
+                if (!ok) break;
             }
             ok = __all_sync(0xffffffffu, ok);
             if (ok && here) ok = __all_sync(0xffffffffu, bar_wait(kTiles == 2 ? pv_done : smem_u32(&sm.pv_done[1]), ic++ & 1, limit));

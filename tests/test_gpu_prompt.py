@@ -187,6 +187,61 @@ def test_the_same_sequence_twice_and_any_order(P):
     c.run([9, 9, 40, 3], ids=[2, 0, 2, 1])
 
 
+@pytest.mark.parametrize("bits", [2, 4, 8])
+@pytest.mark.parametrize("tokens", [8, 9, 16, 17, 32, 33])
+def test_few_tokens_behind_long_histories(P, bits, tokens):
+    """On both sides of where another number of tokens shares a tile; histories that end inside blocks, halves of blocks and pages."""
+    c = Case(P, [1500, 64, 65, 2049, 1023, 130], n_kv=2, bits=bits, seed=tokens + bits)
+    c.run([tokens] * 6)
+    c.run([max(1, tokens - i) for i in range(6)])
+
+
+def test_a_graph_recorded_before_anything_was_appended(P):
+    """What was recorded is the variant for prompts without a history; replayed behind one it is as right as any."""
+    for bits in (2, 4, 8):
+        c = Case(P, [0, 0, 0], n_kv=2, bits=bits, window=16, seed=20 + bits, chunk=1000)
+        nq = [100, 40, 130]
+        q, k, v = c.inputs(nq)
+        out, lse, ws = torch.empty_like(q), torch.empty(q.shape[:2], dtype=torch.float32, device="cuda"), c.cache.prompt_workspace(3, sum(nq))
+        ids, cu = torch.arange(3, dtype=torch.int32, device="cuda"), cu_of(nq)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            P.pask_prompt_attention(c.cache.handle, 0, ids, cu, q, k, v, out, lse, ws)
+        graph.replay()
+        c.verify([0, 1, 2], nq, q, k, v, out, lse, "nothing there")
+        for s in range(3):
+            c.append(s, 1, (0.0, 0.0))
+        graph.replay()
+        c.verify([0, 1, 2], nq, q, k, v, out, lse, "a token each")
+    c = Case(P, [900, 0, 77], n_kv=2, seed=24)     # and a cache that is filled, reset, recorded on and filled again
+    P.pask_cache_reset(c.cache.handle)
+    c.ref = R.Ref(2, 4, 0)
+    q, k, v = c.inputs([100, 40, 130])
+    out, lse, ws = torch.empty_like(q), torch.empty(q.shape[:2], dtype=torch.float32, device="cuda"), c.cache.prompt_workspace(3, 270)
+    ids, cu = torch.arange(3, dtype=torch.int32, device="cuda"), cu_of([100, 40, 130])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        P.pask_prompt_attention(c.cache.handle, 0, ids, cu, q, k, v, out, lse, ws)
+    for s, n in enumerate((900, 300, 77)):
+        c.append(s, n, (0.3, 0.4))
+    graph.replay()
+    c.verify([0, 1, 2], [100, 40, 130], q, k, v, out, lse, "behind histories")
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_drawn_batches(P, seed):
+    import random
+    r = random.Random(seed)
+    n = r.choice([1, 1, 2, 3, 7, 20, 45])
+    window, bits, n_kv = r.choice([0, 0, 16, 64]), r.choice([2, 4, 8]), r.choice([1, 2, 4, 8])
+    most = r.choice([1, 40, 300, 2500])
+    hist = [r.choice([0, r.randint(0, most), r.randint(0, most)]) for _ in range(n)]
+    longest = r.choice([1, 6, 14, 30, 70, 400])
+    mix = r.choice([(1.0, 0.0), (0.0, 1.0), (0.2, 0.5), (0.05, 0.1)])
+    c = Case(P, hist, n_kv=n_kv, bits=bits, window=window, mix=mix, seed=100 + seed)
+    c.run([r.randint(0 if n > 1 and i else 1, longest) for i in range(n)], scale=r.choice([1.0, 4.0]), where=f"seed {seed}")
+
+
 def test_large_and_small_scores(P):
     for scale in (0.0, 1e-3, 8.0, 30.0):
         Case(P, [400], seed=9).run([70], scale=scale, where=f"scale {scale}")
