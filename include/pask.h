@@ -532,6 +532,7 @@ pask_status_t pask_prompt_attention_latent(int32_t n_seqs, int32_t total_q, int3
  * RETAIN-LOW values enter as bf16(code * scale), the operands of a bf16 product (pask_decode_attention computes with the unrounded
  * product); softmax weights are rounded to bf16, scores and sums are fp32, each output is rounded once.  Values must be finite, and
  * scores and sums within what fp32 holds; rows outside every sequence may hold anything and are left as they were.
+ * A row belongs to one sequence: rows that two ranges share hold either's result, or pieces of both.
  * A sequence whose range is malformed is not written (sticky PASK_DEV_BAD_RAGGED); one whose id is out of range gets out = 0 and
  * lse = -inf (PASK_DEV_BAD_SEQ); the others are computed.  A bounded wait that runs out: PASK_DEV_TIMEOUT, out / lse void.
  * Only reads the cache (but for the status word); runs on the device that the cache was created on. */
@@ -685,7 +686,9 @@ pask_status_t pask_debug_set_attention_ctas(pask_cache_t *cache, int32_t n_ctas)
  * barrier on top of what it brings: the copy completes as always, the barrier does not, the wait
  * runs out.  Host-side settings of the handle, used by the calls issued after it. */
 pask_status_t pask_debug_set_wait(pask_cache_t *cache, int64_t limit_cycles, uint32_t surplus_bytes);
-/* pask_debug_set_wait bounds the waits of pask_decode_attention_latent in the same way.  Those of
+/* pask_debug_set_wait bounds the waits of pask_decode_attention_latent and of pask_prompt_attention in the
+ * same way (out / lse of the call are void then, PASK_DEV_TIMEOUT; surplus_bytes is announced by the queries of
+ * every CTA's first item).  Those of
  * pask_prompt_attention_latent, which has no cache, are bounded by this call's limit (100000 .. 1e12 cycles,
  * default 4e9, about two seconds; the wait for a work item that was asked for: twice that); surplus_bytes as
  * above, announced by the first copy of every second CTA (where CTAs share a block of queries, of every

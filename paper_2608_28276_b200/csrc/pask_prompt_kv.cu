@@ -4,20 +4,35 @@
 // 2, 4 or 8-bit rows, the protected window's ring) and the call's own tokens up to the query's.  The four query heads of a
 // key / value head are rows of one product: a tile is 32 tokens x 4 heads = 128 rows.
 //
-// Work.  An item is a block of tokens (one or two tiles) and a key / value head; its keys are blocks of 128: eight pages of the history,
-// or 128 tokens of the call.  plan_kernel lays all items end to end on a line of their costs (key blocks, and two more for the
-// beginning and the result) and every CTA of the grid, one an SM, takes an equal stretch: cuts fall inside items, at any key
-// block, and the parts of an item meet in the workspace, joined by the CTA that finishes last (in the order of the parts, so
-// that the result does not depend on who that is).  No more items than CTAs: each gets whole CTAs of its own instead.
+// Work.  An item is a block of tokens and a key / value head; its keys are blocks of 128: eight pages of the history, or 128 tokens of
+// the call.  prompt_plan_kernel lays all items end to end on a line of their costs (key blocks, and two more for the beginning and the
+// result) and every CTA of the grid, one an SM, takes an equal stretch: cuts fall inside items, at any key block.  No more items than
+// CTAs: each gets whole CTAs of its own instead.  An item's parts leave unscaled outputs, maxima and sums in the workspace;
+// prompt_join_kernel adds them up in the order of the parts, so that the result does not depend on which CTA was done first.
 //
-// In a CTA
-//   softmax warps (four a tile)  a thread has a row: S in registers, P back to tensor memory over S in bf16, as the left operand of
-//                    P V.  The reference maximum moves only when a score exceeds it by more than 2^8, so that O is rarely rescaled
-//   products         P V of tile t, block j;  Q K^T of tile t, block j + 1;  the other tile
+// In a CTA (one tile of 128 rows of S, or two)
+//   softmax          four warps a tile, a thread a row; P back to tensor memory in bf16, as the left operand of P V.  128 scores go in two
+//                    halves, so that the product over the first 64 keys runs beside the exponentials of the others.  The reference maximum
+//                    moves only when a score exceeds it by more than 2^8: O is rarely rescaled
+//   products         one warp.  Two tiles: P V of tile t, block j;  Q K^T of tile t, block j + 1;  the other tile.  One: Q K^T of block j + 1 into
+//                    the other place of S while the softmax has block j, then P V of block j
 //   copies           queries; the call's own keys and values (TMA)
 //   fill             history pages: read as they are stored, expanded to bf16 and laid out as the tensor core reads them
 //   items            which items, and which parts of them, are this CTA's
-// Shared memory: Q 32 KB a tile, stages of 64 KB (128 keys and values).  Tensor memory: S and O, 128 columns each a tile.
+// Few tokens do not fill 128 rows with 4 heads each.  Then the rows of Q stand kCopies times in the tile, and copy c of a row takes the
+// softmax of keys 128 / kCopies c on, with zero weights for the others: the exponentials, the chain that bounds short items, are spread
+// over all threads; the copies' O are summed at the end.
+// Shared memory: Q 32 KB a tile, stages of 64 KB (128 keys and values).  Tensor memory: two tiles, S (P over it) and O, 128 columns
+// each; one tile, two places of S, two of P, O.
+//
+// What bounds it, at 6539 GB/s and 1643 TFLOP/s (1394 sustained) measured:
+//   prompts without history (4 of 4096 - 8192, 32 heads) 1415 us, 942 at the sustained rate: some 3400 cycles for two tiles and 128 keys, of
+//       which the products need 2048 and the exponentials as many, beside them; the rest is waits between the two, at 1.34 GHz under the
+//       power limit
+//   chunks of 512 behind 9K rows in 8 bits 724 us (377): the same chain, 580 with no page read or expanded; expansion in its issue slots
+//   5 drafted tokens of 64 sequences of 2K - 8K 180 us (75: the pages once): 104 with no page read or expanded, the chain wait - S - P - P V
+//       of items that are half a block high; 123 with reads alone, 110 with expansion alone
+//   one prompt of 131: 15 us, three launches in a row: plan 4, items 8, join 3
 //
 // Rounding: S, O and the sums are fp32; a weight is rounded to bf16 once, as an operand of a product with bf16 values; a low-precision
 // row enters as bf16(code * scale), rounded once from the exact product.
@@ -327,7 +342,7 @@ struct Walker {
 
 // ------------------------------------------------------------------------------------------------ pages to operands
 
-constexpr uint32_t kPageLow = 0, kPageBad = 1, kPageHigh = 2, kPageNone = 3;       // kinds of a page: bits 30, 31 of its entry
+constexpr uint32_t kPageLow = 0, kPageBad = 1, kPageHigh = 2, kPageNone = 3;       // kinds of a page: the low bits of its place
 
 // A lane's share of what is expanded at a time, in registers: half of a bf16 page's keys or values of one head, or the codes of a
 // low-precision page's and two of its scales.
@@ -381,11 +396,10 @@ struct Lanes {
     __device__ __forceinline__ int source() const { return 4 * g + t; }
 };
 
-template <int kBits, bool kKeys>
-struct Low {
-    static constexpr int kRounds = kBits / 2 < 1 ? 1 : kBits / 2;               // 512-byte rounds of codes: 1, 2, 4
-    static constexpr int kHalf = 512 * kRounds + kLowScalesBytes;
-};
+template <int kBits>
+constexpr int kLowRounds = kBits / 2 < 1 ? 1 : kBits / 2;                       // 512-byte rounds of codes of a page's keys or values: 1, 2, 4
+template <int kBits>
+constexpr int kLowHalf = 512 * kLowRounds<kBits> + kLowScalesBytes;
 
 // half 0: dims 0 .. 63, 1: 64 .. 127 (keys: rounds 2 j + h of dims 32 j ..; values: rounds 4 e + k of dims 64 e ..)
 template <bool kKeys>
@@ -421,14 +435,13 @@ __device__ __forceinline__ void store_high(const Raw &r, uint32_t block, int row
 
 template <int kBits, bool kKeys>
 __device__ __forceinline__ void load_low(Raw &r, const uint8_t *half, int lane) {
-    using L = Low<kBits, kKeys>;
     const Lanes l(kKeys, lane);
     const uint4 *src = reinterpret_cast<const uint4 *>(half) + l.source();
 #pragma unroll
-    for (int i = 0; i < L::kRounds; i++) r.x[i] = __ldg(src + 32 * i);
+    for (int i = 0; i < kLowRounds<kBits>; i++) r.x[i] = __ldg(src + 32 * i);
     // Of the 64 scales a lane fetches two, and they go around: keys those of tokens g and g + 8 in group t; values those of tokens 2 t
     // and 2 t + 1, 8 on for g > 3, in group g & 3.
-    const unsigned short *scales = reinterpret_cast<const unsigned short *>(half + 512 * L::kRounds) + (kKeys ? 4 * l.g + l.t : 8 * l.t + 32 * (l.g >> 2) + (l.g & 3));
+    const unsigned short *scales = reinterpret_cast<const unsigned short *>(half + 512 * kLowRounds<kBits>) + (kKeys ? 4 * l.g + l.t : 8 * l.t + 32 * (l.g >> 2) + (l.g & 3));
     r.s0 = __ldg(scales);
     r.s1 = __ldg(scales + (kKeys ? 32 : 4));
 }
@@ -618,7 +631,7 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
                     atomicOr(p.status, PASK_DEV_INTERNAL);
                     return (uint64_t)kPageBad;
                 }
-                const uint8_t *at = low ? p.pool_low + (size_t)id * p.low_page_bytes + (size_t)it.head * p.low_head_bytes + kv0 * Low<kBits, true>::kHalf
+                const uint8_t *at = low ? p.pool_low + (size_t)id * p.low_page_bytes + (size_t)it.head * p.low_head_bytes + kv0 * kLowHalf<kBits>
                                         : p.pool_high + (size_t)id * p.high_page_bytes + (size_t)it.head * kHighHeadBytes + kv0 * kHighTileBytes;
                 return reinterpret_cast<uint64_t>(at) | (low ? kPageLow : kPageHigh);          // (16-byte aligned: the kind fits)
             };
@@ -641,7 +654,7 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
                     if (kv) { load_high<false>(x, tile, 0, lane); load_high<false>(y, tile, 1, lane); }
                     else { load_high<true>(x, tile, 0, lane); load_high<true>(y, tile, 1, lane); }
                 } else if (kind == kPageLow) {
-                    if (kv) load_low<kBits, false>(x, at + (kWide ? 0 : Low<kBits, true>::kHalf), lane); else load_low<kBits, true>(x, at, lane);
+                    if (kv) load_low<kBits, false>(x, at + (kWide ? 0 : kLowHalf<kBits>), lane); else load_low<kBits, true>(x, at, lane);
                 }
             };
             if (it.b0 < b1) { find(it.b0, 0); load(kv0); }
@@ -1270,7 +1283,10 @@ pask_status_t launch_bits(uint32_t bits, const PromptParams &p, const CUtensorMa
                        : launch<4, kTiles, kCopies, kWide>(p, map_q, map_k, map_v, dev, stream);
 }
 
-// Tokens of an item: 64 (two tiles), or 32, 16, 8 (one tile)
+// Tokens of an item: 64 (two tiles), or 32, 16, 8 (one tile, its rows once, twice, four times), by the mean of a sequence: the pages are read
+// and expanded once an item, so that one item holds all of its tokens, and the fewer there are, the more threads share a row.  With 8, 16, 32, 64
+// tokens: 5 tokens of 64 sequences 182, 194, 209, 228 us; 17 tokens behind 32K rows 58, 48, 38, 41; chunks of 33 - 120 behind 3K 70, 56, 47,
+// 47; of 512 behind 9K 3022, 1606, 961, 733; prompts of 8K without history 5208, 2767, 1771, 1426.
 int tokens_for(int n_seqs, int total_tokens) {
     const long long n = (total_tokens + n_seqs - 1) / n_seqs;
     return n <= 8 ? 8 : n <= 16 ? 16 : n <= 32 ? 32 : 64;
@@ -1319,6 +1335,9 @@ pask_status_t launch_prompt(pask_cache *c, int layer, int n_seqs, int total_toke
     if (launch_pdl(prompt_plan_kernel, dim3(1), dim3((n_seqs + 31) / 32 * 32), 0, stream, d, layer, n_seqs, total_tokens, seq_ids, cu_tokens, p.ws, p.grid,
                    tokens, static_cast<uint4 *>(out), lse) != cudaSuccess)
         return PASK_ERR_CUDA;
+    // Two tiles: sixteen fill warps, and few registers a softmax thread; or, with no pages to expand, as many as a softmax thread can use, and
+    // one fill warp (which is right with a history too: a graph may be replayed behind one).  With, without: prompts of 8K without history 1495, 1423
+    // us; chunks of 512 behind 9K 733, 3894.
     const auto fn = tokens == 64 ? (c->appended[layer] ? launch_bits<2, 1, true> : launch_bits<2, 1, false>)
                     : tokens == 32 ? launch_bits<1, 1, true> : tokens == 16 ? launch_bits<1, 2, true> : launch_bits<1, 4, true>;
     const pask_status_t ok = fn(d.low_bits, p, map_q, map_k, map_v, c->device, stream);
