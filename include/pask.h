@@ -525,7 +525,7 @@ pask_status_t pask_prompt_attention_latent(int32_t n_seqs, int32_t total_q, int3
  *   seq_ids     dev int32 [n_seqs]; a sequence may be named more than once (drafts of one history: none sees another)
  *   cu_tokens   dev int32 [n_seqs+1]: the rows of each sequence's tokens, ascending within 0 .. total_tokens
  *   q           dev bf16 [total_tokens][n_q][128], post-RoPE;  k, v  dev bf16 [total_tokens][n_kv][128], post-RoPE
- *   out         dev bf16 [total_tokens][n_q][128]
+ *   out         dev bf16 [total_tokens][n_q][128], sharing no memory with q, k, v (PASK_ERR_INVALID_ARG)
  *   lse         dev fp32 [total_tokens][n_q] or NULL: natural-log sum of exp of the scaled scores
  *   workspace   dev, at least pask_prompt_workspace_bytes(cache, n_seqs, total_tokens) bytes, 256-byte aligned; contents undefined
  *               afterwards.  Calls that may overlap on the GPU (two streams, two captured graphs replayed side by side) need one each.

@@ -376,7 +376,8 @@ def test_refusals(P):
 
     bad = [dict(layer=-1), dict(layer=1), dict(n=0), dict(n=1025), dict(total=-1), dict(i=None), dict(u=None), dict(qq=None), dict(kk=None), dict(vv=None),
            dict(o=None), dict(w=None), dict(i=ids.data_ptr() + 2), dict(l=lse.data_ptr() + 2), dict(qq=q.data_ptr() + 8), dict(kk=k.data_ptr() + 2),
-           dict(o=out.data_ptr() + 8), dict(w=ws.data_ptr() + 16)]
+           dict(o=out.data_ptr() + 8), dict(w=ws.data_ptr() + 16), dict(o=q.data_ptr()), dict(o=k.data_ptr()), dict(o=v.data_ptr()),
+           dict(o=q.data_ptr() + q.numel() * 2 - 16), dict(o=k.data_ptr() - q.numel() * 2 + 16)]
     assert all(raw(**x) == P.ERR_INVALID_ARG for x in bad)
     assert raw(b=need - 1) == P.ERR_WORKSPACE and raw(total=0, qq=None, o=None, w=None) == P.OK
     latent = P.LatentCache(R.blob(), 1, 16, 1, 16, 16, 4, 4)
