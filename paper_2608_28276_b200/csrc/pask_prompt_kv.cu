@@ -30,8 +30,8 @@
 //       which the products need 2048 and the exponentials as many, beside them; the rest is waits between the two, at 1.34 GHz under the
 //       power limit
 //   chunks of 512 behind 9K rows in 8 bits 724 us (377): the same chain, 580 with no page read or expanded; expansion in its issue slots
-//   5 drafted tokens of 64 sequences of 2K - 8K 180 us (75: the pages once): 104 with no page read or expanded, the chain wait - S - P - P V
-//       of items that are half a block high; 123 with reads alone, 110 with expansion alone
+//   5 drafted tokens of 64 sequences of 2K - 8K 180 us (75: the pages once): 104 with no page read or expanded, 110 with expansion
+//       alone: a fill warp's chain for a page (its pieces from memory, expansion, the block's hand-over) does not overlap with itself
 //   one prompt of 131: 15 us, three launches in a row: plan 4, items 8, join 3
 //
 // Rounding: S, O and the sums are fp32; a weight is rounded to bf16 once, as an operand of a product with bf16 values; a low-precision
