@@ -7,9 +7,9 @@ fails.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes as C
 import os
+import struct
 
 import torch
 
@@ -120,7 +120,7 @@ _lib.pask_prompt_workspace_bytes.argtypes = [_vp, _i32, _i32]
 _lib.pask_prompt_workspace_bytes.restype = _sz
 _lib.pask_prompt_attention.argtypes = [_vp, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
 _lib.pask_rotary_table.argtypes = [C.POINTER(RotaryDesc), _vp]
-_lib.pask_rotary.argtypes = [_i32, _vp, _vp, _i32, _i32, _i32, C.c_float, _i32, _i32, C.POINTER(RotaryTensor), _vp]
+_lib.pask_rotary.argtypes = [_i32, _vp, _vp, _i32, _i32, _i32, C.c_float, _i32, _i32, _vp, _vp]
 _lib.pask_budget_state.argtypes = [_vp, _i32, C.POINTER(BudgetState), _vp]
 _lib.pask_cache_set_timing_events.argtypes = [_vp, _vp, _vp]
 _lib.pask_debug_stream_len.argtypes = [_vp, _i32, _i32, C.POINTER(C.c_uint32), C.POINTER(C.c_uint32), _vp]
@@ -390,12 +390,20 @@ def _dim(t, k):
     return t.shape[k] if t.dim() > k else 0
 
 
+_current_device, _current_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+
+
 def _call(where, fn, dev, stream, *args):
     """Issue a latent call on the tensors' device: on the given stream or that device's current one."""
     if dev < 0:
         raise PaskError(ERR_INVALID_ARG, f"{where}: tensors must be on a CUDA device")
-    with contextlib.nullcontext() if dev == torch.cuda.current_device() else torch.cuda.device(dev):
-        _check(fn(*args, (torch.cuda.current_stream(dev) if stream is None else stream).cuda_stream), where)
+    if dev != _current_device():
+        with torch.cuda.device(dev):
+            return _call(where, fn, dev, stream, *args)
+    # (the bare handle: a stream object made for each call costs 1.5 us, half as much as a launch)
+    status = fn(*args, _current_stream(dev) if stream is None else stream.cuda_stream)
+    if status:
+        _check(status, where)
 
 
 def pask_append_latent(cache: int, layer: int, seq_ids, cu_tokens, latent, tags, actions=None, actions_out=None, stream=None):
@@ -477,7 +485,7 @@ def pask_rotary_table(rot_dim: int, base: float = 10000.0, scaling: int = ROTARY
 
 
 _ROTARY_TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
-_ROTARY_ARRAYS = [RotaryTensor * i for i in range(ROTARY_MAX_TENSORS + 1)]
+_ROTARY_PACK = struct.Struct("QQqqqqii").pack           # a RotaryTensor: a third of the time that ctypes takes to fill one
 
 
 def pask_rotary(positions, table, tensors, interleaved: bool = False, transpose: bool = False, magnitude: float = 1.0, stream=None):
@@ -487,16 +495,18 @@ def pask_rotary(positions, table, tensors, interleaved: bool = False, transpose:
     w, dev, n, pairs, count = "pask_rotary", positions.get_device(), positions.numel(), table.numel(), len(tensors)
     if not 1 <= count <= ROTARY_MAX_TENSORS:
         raise PaskError(ERR_INVALID_ARG, f"{w}: 1 to {ROTARY_MAX_TENSORS} tensors, got {count}")
-    dtype, descs = tensors[0][0].dtype, _ROTARY_ARRAYS[count]()
+    dtype, descs = tensors[0][0].dtype, b""
     code = _ROTARY_TYPES.get(dtype)
-    for i, (x, y) in enumerate(tensors):
-        sx = x.shape
-        if code is None or x.dtype is not dtype or y.dtype is not dtype or x.get_device() != dev or y.get_device() != dev or len(sx) != 3 or \
-                y.shape != sx or sx[0] != n or sx[2] > 1 and (x.stride(2) != 1 or y.stride(2) != 1):
+    for x, y in tensors:
+        sx, ix = x.shape, x.stride()
+        same = y is x                              # in place: one tensor to look at
+        iy = ix if same else y.stride()
+        if code is None or x.dtype is not dtype or x.get_device() != dev or len(sx) != 3 or sx[0] != n or \
+                not same and (y.dtype is not dtype or y.get_device() != dev or y.shape != sx) or sx[2] > 1 and (ix[2] != 1 or iy[2] != 1):
             raise PaskError(ERR_INVALID_ARG, f"{w}: input and output must be bfloat16, float16 or float32 tensors [{n}, heads, dims] of one type on "
                             f"cuda:{dev} with adjacent dims, got {x.dtype} {list(sx)} on {x.device} and {y.dtype} {list(y.shape)} on {y.device}")
-        ix, iy = x.stride(), y.stride()
-        descs[i] = (x.data_ptr(), y.data_ptr(), ix[0], ix[1], iy[0], iy[1], sx[1], sx[2])
+        at = x.data_ptr()
+        descs += _ROTARY_PACK(at, at if same else y.data_ptr(), ix[0], ix[1], iy[0], iy[1], sx[1], sx[2])
     _call(w, _lib.pask_rotary, dev, stream, n, _arg(w, "positions", positions, torch.int32, dev, (n,)),
           _arg(w, "table", table, torch.int64, dev, (pairs,)), 2 * pairs, int(interleaved), int(transpose), magnitude, code, count, descs)
 
