@@ -32,7 +32,7 @@
 //   chunks of 512 behind 9K rows in 8 bits 724 us (377): the same chain, 580 with no page read or expanded; expansion in its issue slots
 //   5 drafted tokens of 64 sequences of 2K - 8K 180 us (75: the pages once): 104 with no page read or expanded, 110 with expansion
 //       alone: a fill warp's chain for a page (its pieces from memory, expansion, the block's hand-over) does not overlap with itself
-//   one prompt of 131: 15 us, three launches in a row: plan 4, items 8, join 3
+//   one prompt of 131: 13 us replayed in a graph, 14 called; three launches in a row: plan 4, items 8, join 3
 //
 // Rounding: S, O and the sums are fp32; a weight is rounded to bf16 once, as an operand of a product with bf16 values; a low-precision
 // row enters as bf16(code * scale), rounded once from the exact product.
