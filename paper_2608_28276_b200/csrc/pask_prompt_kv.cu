@@ -524,8 +524,9 @@ struct __align__(16) PromptSmem {
     float share[kCopies > 1 ? 32 : 1][kTileRows];  // 32 dims of the copies' results on their way to one another
     float2 ml[kTileRows];
     uint64_t q_full, q_empty, k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages];
-    uint64_t s_full[2], p_half[2], p_full[2], pv_half[2], pv_done[2], o_free[2];             // of a tile; one tile: the first three of a place of S,
-                                                   // pv_done of a block and of an item's last one
+    // Of a tile; one tile: the first five of a place of S (pv_done: one tile only), so that whoever holds S of a block knows the phase before
+    // to be over on the barriers of its place, and a wait by parity cannot take that phase, two blocks ago, for its own.
+    uint64_t s_full[2], p_half[2], p_full[2], pv_half[2], pv_done[2], o_full[2], o_free[2];
     uint64_t item_full[2], item_empty[2], copies, drain;
     Item item[2];
     uint32_t tmem;
@@ -574,6 +575,7 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
             bar_init(smem_u32(&sm.p_full[i]), 4);
             bar_init(smem_u32(&sm.pv_half[i]), 1);
             bar_init(smem_u32(&sm.pv_done[i]), 1);
+            bar_init(smem_u32(&sm.o_full[i]), 1);
             bar_init(smem_u32(&sm.o_free[i]), 4);
         }
         for (int i = 0; i < 2; i++) {
@@ -872,7 +874,7 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
                             if (!ok) break;
                             fence_after();
                             values(at, st, j == 0, 0, min(4, steps));
-                            if (mine) commit(smem_u32(&sm.pv_half[0]));
+                            if (mine) commit(smem_u32(&sm.pv_half[at]));
                         }
                         ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.p_full[at]), (g >> 1) & 1, limit));
                         if (!ok) break;
@@ -880,8 +882,8 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
                         values(at, st, j == 0, kCopies == 1 ? 4 : 0, steps);
                         if (mine) {
                             commit(smem_u32(&sm.v_empty[st]));
-                            commit(smem_u32(&sm.pv_done[0]));
-                            if (j + 1 == nb) commit(smem_u32(&sm.pv_done[1]));
+                            commit(smem_u32(&sm.pv_done[at]));
+                            if (j + 1 == nb) commit(smem_u32(&sm.o_full[0]));
                         }
                         __syncwarp();
                         continue;
@@ -909,7 +911,7 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
                         values(t, st, false, 4, steps);
                         if (mine) {
                             if (t + 1 == nt) commit(smem_u32(&sm.v_empty[st]));
-                            if (j + 1 == nb) commit(smem_u32(&sm.pv_done[t]));
+                            if (j + 1 == nb) commit(smem_u32(&sm.o_full[t]));
                         }
                         __syncwarp();
                         if (j + 1 < nb) {
@@ -946,7 +948,7 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
         const int t = warp >> 2, copy = (tid & (kTileRows - 1)) / kCopyRows;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, base = tmem + lanes + (kTiles == 2 ? t * 128 : copy * kCols);
         const uint32_t p_base = tmem + lanes + kP + (kTiles == 2 ? t * 128 : copy * (kCols / 2)), o_base = tmem + lanes + kO + t * 128;
-        const uint32_t s_full = smem_u32(&sm.s_full[t]), pv_done = smem_u32(&sm.pv_done[t]);
+        const uint32_t s_full = smem_u32(&sm.s_full[t]);
         const int row_in = t * kTileRows + (tid & (kCopyRows - 1));
         uint32_t sc = 0, ic = 0, cc = 0;           // blocks of this tile (S, P and P V alike), items, exchanges between copies so far
         // a row's copies among themselves (all softmax warps)
@@ -1047,8 +1049,9 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
                         const float d = raise ? ex2(m - top) : 1.0f;
                         if (raise) { m = top; l *= d; }
                         if (j > 0 || part > 0) {   // O so far, in the new reference, when the last product into it is done
-                            if (part > 0) ok = bar_wait(smem_u32(&sm.pv_half[t]), sc & 1, limit);
-                            else if (kTiles == 1) ok = bar_wait(pv_done, (sc - 1) & 1, limit);         // (two tiles: this S was issued behind it)
+                            // (two tiles: this S was issued behind P V of the block before.  One: behind that of two blocks ago)
+                            if (part > 0) ok = kTiles == 2 ? bar_wait(smem_u32(&sm.pv_half[t]), sc & 1, limit) : bar_wait(smem_u32(&sm.pv_half[place]), (sc >> 1) & 1, limit);
+                            else if (kTiles == 1) ok = bar_wait(smem_u32(&sm.pv_done[place ^ 1]), ((sc - 1) >> 1) & 1, limit);
                             ok = __all_sync(0xffffffffu, ok);
                             if (!ok) break;
                             fence_after();
@@ -1091,7 +1094,7 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
                 if (!ok) break;
             }
             ok = __all_sync(0xffffffffu, ok);
-            if (ok && here) ok = __all_sync(0xffffffffu, bar_wait(kTiles == 2 ? pv_done : smem_u32(&sm.pv_done[1]), ic++ & 1, limit));
+            if (ok && here) ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.o_full[t]), ic++ & 1, limit));
             if (!ok) break;
             fence_after();
             const size_t heads = (size_t)kGqa * p.n_kv, row = (size_t)(it.q0 + i) * heads + kGqa * it.head + (row_in & 3);
