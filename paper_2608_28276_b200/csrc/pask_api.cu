@@ -476,11 +476,18 @@ pask_status_t pask_prompt_attention(pask_cache_t *c, int32_t layer, int32_t n_se
     if (total_tokens == 0) return PASK_OK;
     if (!q || !k || !v || !out || !ws) return PASK_ERR_INVALID_ARG;
     if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)out) & 15 || ((uintptr_t)ws & 255)) return PASK_ERR_INVALID_ARG;
+    const size_t need = prompt_workspace_bytes(c, n_seqs, total_tokens);
+    if (ws_bytes < need) return PASK_ERR_WORKSPACE;
     // an item's queries, keys and values are read by several CTAs, some after others have written its outputs
     const size_t kv_bytes = (size_t)total_tokens * c->desc.n_kv_heads * kHeadDim * 2, q_bytes = kv_bytes * (c->desc.n_q_heads / c->desc.n_kv_heads);
-    auto shares = [&](const void *in, size_t bytes) { return (uintptr_t)out < (uintptr_t)in + bytes && (uintptr_t)in < (uintptr_t)out + q_bytes; };
-    if (shares(q, q_bytes) || shares(k, kv_bytes) || shares(v, kv_bytes)) return PASK_ERR_INVALID_ARG;
-    if (ws_bytes < prompt_workspace_bytes(c, n_seqs, total_tokens)) return PASK_ERR_WORKSPACE;
+    const struct { const void *at; size_t bytes; } use[] = {{out, q_bytes}, {lse, lse ? (size_t)total_tokens * c->desc.n_q_heads * 4 : 0}, {ws, need},
+                                                            {q, q_bytes}, {k, kv_bytes}, {v, kv_bytes},
+                                                            {seq_ids, (size_t)n_seqs * 4}, {cu_tokens, (size_t)(n_seqs + 1) * 4}};
+    for (int i = 0; i < 3; i++)                    // what is written shares nothing with anything behind it
+        for (int j = i + 1; j < (int)(sizeof(use) / sizeof(use[0])); j++)
+            if (use[i].bytes && use[j].bytes && (uintptr_t)use[i].at < (uintptr_t)use[j].at + use[j].bytes &&
+                (uintptr_t)use[j].at < (uintptr_t)use[i].at + use[i].bytes)
+                return PASK_ERR_INVALID_ARG;
     int dev = -1;
     if (cudaGetDevice(&dev) != cudaSuccess) return PASK_ERR_CUDA;
     if (dev != c->device) return PASK_ERR_INVALID_ARG;
