@@ -390,7 +390,8 @@ def _dim(t, k):
     return t.shape[k] if t.dim() > k else 0
 
 
-_current_device, _current_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+# (a torch without CUDA has neither, and no tensor that gets as far as them)
+_current_device, _current_stream = (getattr(torch._C, name, None) for name in ("_cuda_getDevice", "_cuda_getCurrentRawStream"))
 
 
 def _call(where, fn, dev, stream, *args):
