@@ -578,7 +578,7 @@ typedef struct {
 } pask_rotary_desc_t;
 typedef struct {
     const void *in;
-    void *out;                                     /* in itself, with the same strides, or memory that shares nothing with any `in` */
+    void *out;                                     /* in itself, with the same strides, or memory that nothing else of the call uses */
     int64_t in_token_stride, in_head_stride;       /* elements; the dims of a head are adjacent */
     int64_t out_token_stride, out_head_stride;
     int32_t n_heads, head_dim;
@@ -597,8 +597,10 @@ pask_status_t pask_rotary_table(const pask_rotary_desc_t *desc, uint64_t *table_
  *   dtype         PASK_TYPE_*, of all tensors; pointers aligned to it (16-byte aligned pointers, with strides, head dims and rot_dim / 2
  *                 that are multiples of 16 bytes, are moved 16 bytes at a time)
  *   tensors       host, n_tensors of them; head_dim rot_dim .. PASK_ROTARY_MAX_DIM
- * Errors: PASK_ERR_INVALID_ARG (null, counts, types, alignment, a negative or an overlapping output stride, out == in with other
- * strides), PASK_ERR_UNSUPPORTED_SHAPE (rot_dim, head_dim). */
+ * Errors: PASK_ERR_INVALID_ARG (null, counts, types, alignment; a stride that is negative or above 2^40 elements, a tensor that spans
+ * more than 2^58, an overlapping output stride; out == in with other strides; an output that shares memory with the positions, the table, another tensor
+ * or, shifted, its own input: told for ranges without gaps and for tensors at the same strides, the caller's to avoid
+ * otherwise), PASK_ERR_UNSUPPORTED_SHAPE (rot_dim, head_dim, more than 2^20 heads in all). */
 pask_status_t pask_rotary(int32_t n_tokens, const int32_t *positions, const uint64_t *table, int32_t rot_dim, int32_t interleaved,
                           int32_t transpose, float magnitude, int32_t dtype, int32_t n_tensors,
                           const pask_rotary_tensor_t *tensors, pask_stream_t stream);

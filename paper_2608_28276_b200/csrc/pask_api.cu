@@ -1,8 +1,10 @@
 // Host side of libpask: policy blobs, cache set-up, budget state, canonical dumps.
+#include <algorithm>
 #include <cmath>
 #include <cstring>
 #include <memory>
 #include <new>
+#include <utility>
 
 #include <nvtx3/nvToolsExt.h>
 
@@ -19,6 +21,53 @@ struct NvtxRange {
     explicit NvtxRange(const char *name) { nvtxRangePushA(name); }
     ~NvtxRange() { nvtxRangePop(); }
 };
+
+// Memory in equal runs of bytes at two strides, the wider one outside; a dimension of one, or without a stride, is one step of stride zero.
+struct Runs {
+    int64_t at, n0, s0, n1, s1, len;
+    Runs(const void *p, int64_t bytes) : at((int64_t)(uintptr_t)p), n0(1), s0(0), n1(1), s1(0), len(bytes) {}
+    Runs(const void *p, int64_t tokens, int64_t token_stride, int64_t heads, int64_t head_stride, int64_t bytes)
+        : at((int64_t)(uintptr_t)p), n0(token_stride ? tokens : 1), s0(tokens > 1 ? token_stride : 0), n1(head_stride ? heads : 1),
+          s1(heads > 1 ? head_stride : 0), len(bytes) {
+        if (s1 > s0) { std::swap(n0, n1); std::swap(s0, s1); }
+    }
+    int64_t row() const { return (n1 - 1) * s1 + len; }        // bytes from an outer step's first to its last
+    int64_t end() const { return at + (n0 - 1) * s0 + row(); }
+    bool solid() const { return (n1 == 1 || s1 <= len) && (n0 == 1 || s0 <= row()); }      // no byte in between is left out
+    bool apart() const { return n0 == 1 || s0 >= row(); }      // outer steps do not reach into one another
+};
+// of n steps, `stride` apart and `len` long, from `at` on: the first and the last with a byte in lo .. hi - 1
+struct Steps { int64_t first, last; };
+Steps steps_in(int64_t at, int64_t n, int64_t stride, int64_t len, int64_t lo, int64_t hi) {
+    auto floored = [](int64_t a, int64_t b) { return a / b - (a % b < 0); };
+    if (n == 1) return at < hi && at + len > lo ? Steps{0, 0} : Steps{0, -1};
+    return {std::max<int64_t>(0, floored(lo - len - at, stride) + 1), std::min(n - 1, floored(hi - 1 - at, stride))};
+}
+bool touches(const Runs &x, int64_t lo, int64_t hi) {
+    const Steps rows = steps_in(x.at, x.n0, x.s0, x.row(), lo, hi);
+    if (rows.last - rows.first > 1) return true;   // one of them lies between the two ends
+    for (int64_t i = rows.first; i <= rows.last; i++) {
+        const Steps in = steps_in(x.at + i * x.s0, x.n1, x.s1, x.len, lo, hi);
+        if (in.first <= in.last) return true;
+    }
+    return false;
+}
+// Whether x and y have a byte in common, where that is told in a few steps: one of them without gaps, or both at the same strides
+bool share_memory(const Runs &x, const Runs &y) {
+    if (x.end() <= y.at || y.end() <= x.at) return false;
+    if (x.solid() && y.apart()) return touches(y, x.at, x.end());
+    if (y.solid() && x.apart()) return touches(x, y.at, y.end());
+    const int64_t s0 = x.n0 > 1 ? x.s0 : y.s0, s1 = x.n1 > 1 ? x.s1 : y.s1;
+    if ((y.n0 > 1 && y.s0 != s0) || (y.n1 > 1 && y.s1 != s1) || s0 < x.row() || s0 < y.row()) return false;
+    // runs i outer and j inner steps apart: -y.len < d + i s0 + j s1 < x.len
+    const int64_t d = y.at - x.at;
+    for (int64_t i = -d / s0 - 1; i <= -d / s0 + 1; i++) {
+        const int64_t e = d + i * s0, near = s1 ? std::clamp(-e / s1, 1 - x.n1, y.n1 - 1) : 0;
+        for (int64_t j = near - 1; j <= near + 1; j++)
+            if (i > -x.n0 && i < y.n0 && j > -x.n1 && j < y.n1 && e + j * s1 < x.len && e + j * s1 > -y.len) return true;
+    }
+    return false;
+}
 
 uint32_t rd32(const uint8_t *p) {
     return (uint32_t)p[0] | ((uint32_t)p[1] << 8) | ((uint32_t)p[2] << 16) | ((uint32_t)p[3] << 24);
@@ -552,10 +601,26 @@ pask_status_t pask_rotary(int32_t n_tokens, const int32_t *positions, const uint
         const bool heads_apart = x.n_heads == 1 || x.out_head_stride >= x.head_dim, tokens_apart = n_tokens <= 1 || x.out_token_stride >= x.head_dim;
         if (!heads_apart || !tokens_apart) return PASK_ERR_INVALID_ARG;
         if (x.n_heads > 1 && n_tokens > 1 && x.out_token_stride < over_heads && x.out_head_stride < over_tokens) return PASK_ERR_INVALID_ARG;
+        for (const __int128 span : {(__int128)(n_tokens - 1) * x.in_token_stride + (__int128)(x.n_heads - 1) * x.in_head_stride, over_heads + over_tokens})
+            if (span > (__int128)1 << 58) return PASK_ERR_INVALID_ARG;         // no memory reaches that far
         heads += x.n_heads;
     }
     if (heads > (1 << 20)) return PASK_ERR_UNSUPPORTED_SHAPE;
     if (n_tokens == 0) return PASK_OK;
+    // A result in memory that another part of the call reads or writes: what is read there, and what stays, would be a matter of timing
+    const int64_t size = dtype == PASK_TYPE_FP32 ? 4 : 2;
+    auto runs = [&](const pask_rotary_tensor_t &x, bool in) {
+        return in ? Runs(x.in, n_tokens, x.in_token_stride * size, x.n_heads, x.in_head_stride * size, x.head_dim * size)
+                  : Runs(x.out, n_tokens, x.out_token_stride * size, x.n_heads, x.out_head_stride * size, x.head_dim * size);
+    };
+    const Runs pos(positions, (int64_t)n_tokens * 4), freq(table, (int64_t)rot_dim * 4);
+    for (int i = 0; i < n_tensors; i++) {
+        const Runs y = runs(t[i], false);
+        if (share_memory(y, pos) || share_memory(y, freq)) return PASK_ERR_INVALID_ARG;
+        for (int j = 0; j < n_tensors; j++)
+            if ((!(i == j && t[i].in == t[i].out) && share_memory(y, runs(t[j], true))) || (j > i && share_memory(y, runs(t[j], false))))
+                return PASK_ERR_INVALID_ARG;
+    }
     NvtxRange range("pask_rotary");
     return launch_rotary(n_tokens, positions, table, rot_dim, interleaved != 0, transpose != 0, magnitude, dtype, n_tensors, t,
                          static_cast<cudaStream_t>(stream));
