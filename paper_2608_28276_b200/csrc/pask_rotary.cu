@@ -140,7 +140,7 @@ cudaError_t launch(RotaryParams &p, bool neighbours, cudaStream_t stream) {
     const int rows = kThreads / (p.rot / 2 / v + p.tails), heads = p.first[p.n_tensors];
     p.tokens = 1;
     while (p.tokens < kMaxTokens && p.tokens * heads < 4 * rows && p.n_tokens >= p.tokens * 2 * 148 * 4) p.tokens *= 2;
-    const dim3 grid((p.n_tokens + p.tokens - 1) / p.tokens);
+    const dim3 grid((p.n_tokens - 1) / p.tokens + 1);                  // (n_tokens + tokens may not be an int)
     if (wide)
         return neighbours ? launch_pdl(rotary_kernel<T, V, true>, grid, dim3(kThreads), 0, stream, p)
                           : launch_pdl(rotary_kernel<T, V, false>, grid, dim3(kThreads), 0, stream, p);
