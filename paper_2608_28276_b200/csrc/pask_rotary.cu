@@ -122,6 +122,16 @@ rotary_kernel(const __grid_constant__ RotaryParams p) {
     }
 }
 
+// SMs of the current device (the tensors': the caller's to set), asked for once; 0 on an error
+int sm_count() {
+    static int n[64] = {};
+    int dev = -1, found = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
+    if (n[dev]) return n[dev];
+    if (cudaDeviceGetAttribute(&found, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+    return n[dev] = found;
+}
+
 template <typename T>
 cudaError_t launch(RotaryParams &p, bool neighbours, cudaStream_t stream) {
     constexpr int V = 16 / sizeof(T);
@@ -138,8 +148,10 @@ cudaError_t launch(RotaryParams &p, bool neighbours, cudaStream_t stream) {
     // Tokens a CTA: several where there are enough of them to fill the GPU all the same, so that a thread has some four rows and
     // the sines are worked out beside other CTAs' copies; one in small calls.
     const int rows = kThreads / (p.rot / 2 / v + p.tails), heads = p.first[p.n_tensors];
+    const int sms = sm_count();
+    if (!sms) return cudaErrorInvalidDevice;
     p.tokens = 1;
-    while (p.tokens < kMaxTokens && p.tokens * heads < 4 * rows && p.n_tokens >= p.tokens * 2 * 148 * 4) p.tokens *= 2;
+    while (p.tokens < kMaxTokens && p.tokens * heads < 4 * rows && p.n_tokens >= p.tokens * 2 * sms * 4) p.tokens *= 2;
     const dim3 grid((p.n_tokens - 1) / p.tokens + 1);                  // (n_tokens + tokens may not be an int)
     if (wide)
         return neighbours ? launch_pdl(rotary_kernel<T, V, true>, grid, dim3(kThreads), 0, stream, p)
