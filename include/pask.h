@@ -527,8 +527,9 @@ pask_status_t pask_prompt_attention_latent(int32_t n_seqs, int32_t total_q, int3
  *   q           dev bf16 [total_tokens][n_q][128], post-RoPE;  k, v  dev bf16 [total_tokens][n_kv][128], post-RoPE
  *   out         dev bf16 [total_tokens][n_q][128]
  *   lse         dev fp32 [total_tokens][n_q] or NULL: natural-log sum of exp of the scaled scores
- *   workspace   dev, at least pask_prompt_workspace_bytes(cache, n_seqs, total_tokens) bytes, 256-byte aligned; contents undefined
- *               afterwards.  Calls that may overlap on the GPU (two streams, two captured graphs replayed side by side) need one each.
+ *   workspace   dev, at least pask_prompt_workspace_bytes(cache, n_seqs, total_tokens) bytes (by the mean of a sequence: as many tokens of
+ *               fewer sequences can need more), 256-byte aligned; contents undefined afterwards.  Calls that may overlap on the
+ *               GPU (two streams, two captured graphs replayed side by side) need one each.
  * out, lse and workspace share no memory with one another or with what is read (PASK_ERR_INVALID_ARG).
  * RETAIN-LOW values enter as bf16(code * scale), the operands of a bf16 product (pask_decode_attention computes with the unrounded
  * product); softmax weights are rounded to bf16, scores and sums are fp32, each output is rounded once.  Values must be finite, and

@@ -1291,7 +1291,7 @@ pask_status_t launch_bits(uint32_t bits, const PromptParams &p, const CUtensorMa
 // tokens: 5 tokens of 64 sequences 182, 194, 209, 228 us; 17 tokens behind 32K rows 58, 48, 38, 41; chunks of 33 - 120 behind 3K 70, 56, 47,
 // 47; of 512 behind 9K 3022, 1606, 961, 733; prompts of 8K without history 5208, 2767, 1771, 1426.
 int tokens_for(int n_seqs, int total_tokens) {
-    const long long n = (total_tokens + n_seqs - 1) / n_seqs;
+    const long long n = ((long long)total_tokens + n_seqs - 1) / n_seqs;
     return n <= 8 ? 8 : n <= 16 ? 16 : n <= 32 ? 32 : 64;
 }
 

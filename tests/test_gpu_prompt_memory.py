@@ -58,3 +58,11 @@ def test_neighbours_in_one_buffer_are_not(P):
     bq.copy_(q), bk.copy_(k), bv.copy_(v), ids.copy_(torch.arange(2)), cu.copy_(cu_of([4, 1]))
     P.pask_prompt_attention(c.cache.handle, 0, ids, cu, bq, bk, bv, out, lse, ws)
     c.verify([0, 1], [4, 1], q, k, v, out, lse)
+
+
+def test_workspace_of_as_many_tokens_as_an_int_holds(P):
+    """It depends on the tokens only by their mean, and that is as large as it gets from 33 on."""
+    c = Case(P, [3], seed=33)
+    for n in (1, 7, 1024):
+        assert P.pask_prompt_workspace_bytes(c.cache.handle, n, 2 ** 31 - 1) == P.pask_prompt_workspace_bytes(c.cache.handle, n, 64 * n)
+        assert P.pask_prompt_workspace_bytes(c.cache.handle, n, 64 * n) > P.pask_prompt_workspace_bytes(c.cache.handle, n, 8 * n) > 0
