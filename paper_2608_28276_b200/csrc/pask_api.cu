@@ -267,7 +267,6 @@ pask_status_t pask_cache_create(const pask_cache_desc_t *d, const pask_policy_t 
     c->ev_start = c->ev_stop = nullptr;
     c->span = nullptr;
     c->ahead.resize((size_t)d->n_layers);
-    c->appended.assign((size_t)d->n_layers, 0);
     c->wait_cycles = 2000000000LL;   // about one second: give up instead of hanging
     c->wait_test_surplus = 0;
     c->off = meta_offsets(d, 255, PASK_MAX_GROUPS);
@@ -400,7 +399,6 @@ pask_status_t pask_cache_reset(pask_cache_t *c, pask_stream_t stream_v) {
     if (ok != PASK_OK) return ok;
     cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
     uint8_t *m = static_cast<uint8_t *>(c->meta);
-    c->appended.assign(c->appended.size(), 0);
     for (auto &a : c->ahead) a.valid = false;
     cudaError_t e = cudaMemsetAsync(m + c->off.ctrl, 0, kCtrlWords * 4, stream);
     if (e == cudaSuccess) e = cudaMemsetAsync(m + c->off.zero_begin, 0, c->off.zero_end - c->off.zero_begin, stream);

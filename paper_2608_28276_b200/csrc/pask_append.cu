@@ -1292,7 +1292,6 @@ pask_status_t launch_append(pask_cache *c, int layer, int n_seqs, int total_toke
                             const int32_t *cu_tokens, const void *k, const void *v, const uint8_t *tags,
                             const uint8_t *decided, uint8_t *actions_out, cudaStream_t stream, const Workspace *fuse_ws,
                             bool *fused) {
-    if (total_tokens > 0) c->appended[layer] = 1;
     if (fused) *fused = false;
     if (n_seqs <= kSmallMax && total_tokens <= kSmallMax) {
         SmallLut lut;
@@ -1335,7 +1334,6 @@ pask_status_t launch_step_tail(pask_cache *c, int layer, int n_seqs, const int32
                                const void *k, const void *v, const uint8_t *tags, const uint8_t *decided, uint8_t *actions_out,
                                const Workspace &plan_ws, int32_t *ids_out, const uint32_t *prefix, const float2 *part_ml,
                                const float *part_o, float *out, float *lse, const NewTokens &nt, cudaStream_t stream) {
-    c->appended[layer] = 1;
     if (n_seqs < 1 || n_seqs > kSmallMax) return PASK_ERR_UNSUPPORTED_SHAPE;
     SmallLut lut;
     fill_small_lut(c, layer, &lut);

@@ -148,8 +148,6 @@ struct pask_cache {
     };
     std::vector<Ahead> ahead;     // [n_layers]
     uint64_t ahead_calls = 0;     // planned-ahead step calls issued so far
-    std::vector<uint8_t> appended;   // [n_layers] a call has asked for tokens to be appended at the layer since the last reset (a hint: which
-                                     // variant of the prompt kernel is quicker; both are right whatever the cache holds)
     long long wait_cycles;        // bound of a device-side wait for a bulk copy, in SM clock cycles (about a second)
     uint32_t wait_test_surplus;   // pask_debug_set_wait: bytes a warp's first copy announces but does not bring
     // pask_decode_step_pipelined: two copy streams and the events that order them against the caller's stream

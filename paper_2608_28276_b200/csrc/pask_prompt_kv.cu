@@ -17,7 +17,8 @@
 //   products         one warp.  Two tiles: P V of tile t, block j;  Q K^T of tile t, block j + 1;  the other tile.  One: Q K^T of block j + 1 into
 //                    the other place of S while the softmax has block j, then P V of block j
 //   copies           queries; the call's own keys and values (TMA)
-//   fill             history pages: read as they are stored, expanded to bf16 and laid out as the tensor core reads them
+//   fill             history pages: read as they are stored, expanded to bf16 and laid out as the tensor core reads them.  Sixteen warps; they leave
+//                    where the plan finds no history in the whole call, and a variant without them is launched beside for long sequences
 //   items            which items, and which parts of them, are this CTA's
 // Few tokens do not fill 128 rows with 4 heads each.  Then the rows of Q stand kCopies times in the tile, and copy c of a row takes the
 // softmax of keys 128 / kCopies c on, with zero weights for the others: the exponentials, the chain that bounds short items, are spread
@@ -71,6 +72,7 @@ struct Join { int row, rows, head, first, last; };
 
 struct PromptWorkspace {
     uint64_t *prefix;                              // [n_seqs + 1] cost (or CTAs) of the sequences before
+    int *paged;                                    // whether any sequence with tokens has a history
     PromptSeq *seqs;                               // [n_seqs]
     Join *joins;                                   // [grid] the item in parts that begins with this CTA's part
     float2 *ml;                                    // [2 grid][rows] reference maximum in log2 units, sum
@@ -81,9 +83,11 @@ size_t carve(int n_seqs, int grid, int rows, uint8_t *base, PromptWorkspace *ws)
     size_t off = 0;
     auto take = [&](size_t bytes) { size_t at = off; off = (off + bytes + 255) / 256 * 256; return at; };
     const size_t o_prefix = take((size_t)(n_seqs + 1) * 8), o_seqs = take((size_t)n_seqs * sizeof(PromptSeq)), o_join = take((size_t)grid * sizeof(Join));
+    const size_t o_paged = take(sizeof(int));
     const size_t o_ml = take((size_t)2 * grid * rows * sizeof(float2)), o_o = take((size_t)2 * grid * rows * kDim * 4);
     if (ws) {
         ws->prefix = reinterpret_cast<uint64_t *>(base + o_prefix);
+        ws->paged = reinterpret_cast<int *>(base + o_paged);
         ws->seqs = reinterpret_cast<PromptSeq *>(base + o_seqs);
         ws->joins = reinterpret_cast<Join *>(base + o_join);
         ws->ml = reinterpret_cast<float2 *>(base + o_ml);
@@ -99,6 +103,7 @@ struct PromptParams {
     uint32_t *status;
     uint32_t high_page_bytes, low_page_bytes, low_head_bytes, cap_low, high_limit, ring_first, ring_pages;
     int max_pages, n_kv, n_seqs, grid;
+    int only;                                      // 0, 1: nothing to do where `paged` is something else;  -1: always
     __nv_bfloat16 *out;
     float *lse;
     long long wait_cycles;
@@ -123,12 +128,12 @@ __global__ void __launch_bounds__(kPlanThreads)
 prompt_plan_kernel(DevCache c, int layer, int n_seqs, int total, const int32_t *__restrict__ seq_ids, const int32_t *__restrict__ cu,
                    PromptWorkspace ws, int grid, int block_tokens, uint4 *__restrict__ out, float *__restrict__ lse) {
     __shared__ uint64_t s_sum[32];
-    __shared__ uint32_t s_part, s_items, s_longest, s_bad;
+    __shared__ uint32_t s_part, s_items, s_longest, s_bad, s_paged;
     __shared__ int2 s_seq[kPlanThreads];           // items and key blocks of the longest, of each sequence
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x;
     pdl_launch_dependents();
     pdl_wait();
-    if (tid == 0) s_items = s_longest = s_bad = 0;
+    if (tid == 0) s_items = s_longest = s_bad = s_paged = 0;
     __syncthreads();
     PromptSeq s{};
     uint32_t bad = 0;
@@ -167,6 +172,7 @@ prompt_plan_kernel(DevCache c, int layer, int n_seqs, int total, const int32_t *
     const int named = s.nq;                        // rows of an unknown sequence: cleared below, no item
     if (unknown) s.nq = 0;
     const int nqb = (s.nq + block_tokens - 1) / block_tokens, longest = nqb ? s.blocks + own_blocks(nqb - 1, block_tokens) : 0;
+    if (nqb && s.blocks) s_paged = 1;
     if (nqb && nqb <= grid) {                      // (more: no need to count)
         atomicAdd(&s_items, (uint32_t)(nqb * c.n_kv));
         atomicMax(&s_longest, (uint32_t)longest);
@@ -206,7 +212,10 @@ prompt_plan_kernel(DevCache c, int layer, int n_seqs, int total, const int32_t *
         ws.prefix[tid + 1] = before + inc;
         ws.seqs[tid] = s;
     }
-    if (tid == 0) ws.prefix[0] = 0;
+    if (tid == 0) {
+        ws.prefix[0] = 0;
+        *ws.paged = (int)s_paged;
+    }
     // rows of sequences that are none
     if (s_bad & PASK_DEV_BAD_SEQ) {
         __shared__ int s_q0, s_n;
@@ -516,10 +525,11 @@ __device__ __forceinline__ void store_low(const Raw &r, uint32_t block, int row,
 // ------------------------------------------------------------------------------------------------ attention
 
 // kTiles 2: 64 tokens an item.  1: 32 / kCopies tokens, each row of S kCopies times in the tile.
-template <int kTiles, int kCopies, bool kWide>
+// kPaged false: for calls in which no sequence has a history (kBits is not looked at).
+template <int kTiles, int kCopies, bool kPaged>
 struct __align__(16) PromptSmem {
-    // Warps: softmax, four for control, fill (kWide: one for the keys and one for the values of each page of a block; else one, of the four)
-    static constexpr int kStages = 2, kSoft = 4 * kTiles, kFill = kWide ? 16 : 1, kThreads = 32 * (kSoft + 4 + (kWide ? kFill : 0));
+    // Warps: softmax, four for control, fill (one for the keys and one for the values of each page of a block)
+    static constexpr int kStages = 2, kSoft = 4 * kTiles, kFill = kPaged ? 2 * kBlockPages : 0, kThreads = 32 * (kSoft + 4 + kFill);
     uint8_t q[kTiles][kTileBytes], k[kStages][kTileBytes], v[kStages][kTileBytes];
     float share[kCopies > 1 ? 32 : 1][kTileRows];  // 32 dims of the copies' results on their way to one another
     float2 ml[kTileRows];
@@ -547,26 +557,30 @@ struct Filled {
     }
 };
 
-template <int kBits, int kTiles, int kCopies, bool kWide>
-__global__ void __launch_bounds__(PromptSmem<kTiles, kCopies, kWide>::kThreads, 1)
+template <int kBits, int kTiles, int kCopies, bool kPaged>
+__global__ void __launch_bounds__(PromptSmem<kTiles, kCopies, kPaged>::kThreads, 1)
 prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
               const __grid_constant__ CUtensorMap map_v) {
     using namespace umma;
-    using Smem = PromptSmem<kTiles, kCopies, kWide>;
-    constexpr int kStages = Smem::kStages, kSoft = Smem::kSoft, kFill = Smem::kFill, kFillOf = kWide ? 8 : 1;     // kFillOf: of a block's keys
+    using Smem = PromptSmem<kTiles, kCopies, kPaged>;
+    constexpr int kStages = Smem::kStages, kSoft = Smem::kSoft, kFill = Smem::kFill;
     constexpr int kTokens = kTiles * kTileTokens / kCopies, kRows = kTokens * kGqa;
     extern __shared__ __align__(1024) uint8_t s_raw[];
     Smem &sm = *reinterpret_cast<Smem *>(s_raw);
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
+    if (p.only >= 0) {
+        pdl_wait();
+        if (*p.ws.paged != p.only) return;         // the other variant's call
+    }
     if (tid == 0) {
         bar_init(smem_u32(&sm.q_full), 1);
         bar_init(smem_u32(&sm.q_empty), 1);
         bar_init(smem_u32(&sm.copies), kSoft);
         bar_init(smem_u32(&sm.drain), 1);
         for (int i = 0; i < kStages; i++) {
-            bar_init(smem_u32(&sm.k_full[i]), 1 + kFillOf);
+            bar_init(smem_u32(&sm.k_full[i]), 1 + kFill / 2);
             bar_init(smem_u32(&sm.k_empty[i]), 1);
-            bar_init(smem_u32(&sm.v_full[i]), 1 + kFillOf);
+            bar_init(smem_u32(&sm.v_full[i]), 1 + kFill / 2);
             bar_init(smem_u32(&sm.v_empty[i]), 1);
         }
         for (int i = 0; i < 2; i++) {
@@ -596,6 +610,8 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
     pdl_wait();                                    // the plan; and what came before it
     pdl_launch_dependents();
     if (tid == 0) p.ws.joins[blockIdx.x].rows = 0;
+    // No history in the whole call: the fill warps leave, and the copies arrive in their place.
+    const bool fills = kPaged && *p.ws.paged != 0;
     // the CTA's n-th item; false behind the last one or after a wait ran out
     auto next_item = [&](uint32_t n, Item &it) {
         const uint32_t slot = n & 1;
@@ -609,9 +625,8 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
     auto tiles_of = [&](const Item &it) { return kTiles == 2 && it.block * kTokens + kTileTokens < it.nq ? 2 : 1; };
 
     // ================================================= fill
-    auto fill = [&](int me) {                      // me: of the fill warps
-        constexpr int kKv = kWide ? 1 : 2, kPages = kBlockPages / kFillOf;      // of a warp, a block
-        const int page0 = me % kFillOf, kv0 = me / kFillOf;
+    auto fill = [&](int me) {                      // me: of the fill warps: page `slot` of each block, its keys or its values
+        const int slot = me % kBlockPages, kv0 = me / kBlockPages;
         Item it;
         uint32_t g = 0;                            // blocks so far
         for (uint32_t n = 0; next_item(n, it); n++) {
@@ -619,7 +634,7 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
             const uint32_t *tbl_high = p.tbl_high + (size_t)it.slot * p.max_pages, *tbl_low = p.tbl_low + (size_t)it.slot * p.max_pages;
             const uint32_t ring = p.ring_first + it.slot * p.ring_pages;
             const int b1 = min(it.b1, it.hist);
-            // the pages of four blocks at a time, a lane each: their ids, then where this head's keys (one tile: or values) lie, and the kind
+            // the pages of four blocks at a time, a lane each: their ids, then where this head's keys or values lie, and the kind
             auto ids = [&](int b) {
                 const int page = 8 * b + lane;
                 if (page >= f.pages || b >= b1) return 0u;
@@ -639,66 +654,52 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
             };
             uint64_t window = places(it.b0, ids(it.b0));
             uint32_t ids_next = ids(it.b0 + 4);
-            // The warp's units in turn: pages (wide: one) of a block, keys and values (wide: either).  What was stored makes room for the next unit's
-            // pieces, which travel while its place in the block is waited for: two pieces of a bf16 page, one of a low-precision one.
+            // What was stored makes room for the next page's pieces, which travel while its place in the block is waited for: two pieces of a
+            // bf16 page, one of a low-precision one.
             Raw x, y;
             uint32_t kind = kPageNone;
-            const uint8_t *at = nullptr;
-            auto find = [&](int b, int i) {        // page i of block b
-                const int in = (b - it.b0) & 3;
-                const uint64_t e = __shfl_sync(0xffffffffu, window, 8 * in + page0 + i * kFillOf);
-                at = reinterpret_cast<const uint8_t *>(e & ~(uint64_t)15);
+            auto load = [&](int b, int kv) {       // the warp's page of block b
+                const uint64_t e = __shfl_sync(0xffffffffu, window, 8 * ((b - it.b0) & 3) + slot);
+                const uint8_t *at = reinterpret_cast<const uint8_t *>(e & ~(uint64_t)15);
                 kind = (uint32_t)e & 15u;
-            };
-            auto load = [&](int kv) {
                 if (kind == kPageHigh) {
-                    const uint8_t *tile = at + (kWide || !kv ? 0 : kHighTileBytes);
-                    if (kv) { load_high<false>(x, tile, 0, lane); load_high<false>(y, tile, 1, lane); }
-                    else { load_high<true>(x, tile, 0, lane); load_high<true>(y, tile, 1, lane); }
+                    if (kv) { load_high<false>(x, at, 0, lane); load_high<false>(y, at, 1, lane); }
+                    else { load_high<true>(x, at, 0, lane); load_high<true>(y, at, 1, lane); }
                 } else if (kind == kPageLow) {
-                    if (kv) load_low<kBits, false>(x, at + (kWide ? 0 : kLowHalf<kBits>), lane); else load_low<kBits, true>(x, at, lane);
+                    if (kv) load_low<kBits, false>(x, at, lane); else load_low<kBits, true>(x, at, lane);
                 }
             };
-            if (it.b0 < b1) { find(it.b0, 0); load(kv0); }
+            if (it.b0 < b1) load(it.b0, kv0);
             // (The warps pass through every block, those that are copied too: a barrier's phase is only told from the next but one
             // by who has to arrive on it.)
             for (int b = it.b0; b < it.b1; b++, g++) {
-                const uint32_t st = g % kStages, ph = (g / kStages - 1) & 1;
+                const uint32_t st = g % kStages;
+                // (A loop of one pass: with `kv` plainly the same throughout, keys and values get a loop each over all blocks, whose addresses do not
+                // fit the registers: 5 drafted tokens of 64 sequences in 8 bits 173 us, 183 so.)
 #pragma unroll 1
-                for (int kv = kv0; kv < kv0 + kKv; kv++) {
+                for (int kv = kv0; kv < kv0 + 1; kv++) {
                     const uint32_t block = smem_u32(kv ? sm.v[st] : sm.k[st]);
-                    if (g >= kStages) ok = __all_sync(0xffffffffu, bar_wait(smem_u32(kv ? &sm.v_empty[st] : &sm.k_empty[st]), ph, limit));
+                    if (g >= kStages) ok = __all_sync(0xffffffffu, bar_wait(smem_u32(kv ? &sm.v_empty[st] : &sm.k_empty[st]), (g / kStages - 1) & 1, limit));
                     if (!ok) break;
                     if (b < b1) {
-#pragma unroll 1
-                        for (int i = 0; i < kPages; i++) {
-                            const int page = page0 + i * kFillOf;
-                            if (kind == kPageHigh) {
-                                if (kv) { store_high<false>(x, block, 16 * page, 0, lane); store_high<false>(y, block, 16 * page, 1, lane); }
-                                else { store_high<true>(x, block, 16 * page, 0, lane); store_high<true>(y, block, 16 * page, 1, lane); }
-                            } else if (kind == kPageLow) {
-                                if (kv) store_low<kBits, false>(x, block, 16 * page, lane); else store_low<kBits, true>(x, block, 16 * page, lane);
-                            }
-                            // slots without a token: whatever the page holds there counts as zero
-                            const int have = kind == kPageNone ? 16 : kind == kPageBad ? 0 : f.of_page(8 * b + page);
-                            if (have < 16) {
-                                __syncwarp();
-                                for (int e = lane; e < (16 - have) * 16; e += 32)
-                                    store16(block + ((e >> 3) & 1) * kSub + (uint32_t)(16 * page + have + (e >> 4)) * 128 + (e & 7) * 16, 0, 0, 0, 0);
-                            }
-                            int nb = b, nkv = kv, ni = i + 1;
-                            if (ni == kPages) {
-                                ni = 0;
-                                if (++nkv == kv0 + kKv) {
-                                    nkv = kv0;
-                                    if ((++nb - it.b0 & 3) == 0) {
-                                        window = places(nb, ids_next);
-                                        ids_next = ids(nb + 4);
-                                    }
-                                }
-                            }
-                            if (nb < b1) { find(nb, ni); load(nkv); }
+                        if (kind == kPageHigh) {
+                            if (kv) { store_high<false>(x, block, 16 * slot, 0, lane); store_high<false>(y, block, 16 * slot, 1, lane); }
+                            else { store_high<true>(x, block, 16 * slot, 0, lane); store_high<true>(y, block, 16 * slot, 1, lane); }
+                        } else if (kind == kPageLow) {
+                            if (kv) store_low<kBits, false>(x, block, 16 * slot, lane); else store_low<kBits, true>(x, block, 16 * slot, lane);
                         }
+                        // slots without a token: whatever the page holds there counts as zero
+                        const int have = kind == kPageNone ? 16 : kind == kPageBad ? 0 : f.of_page(8 * b + slot);
+                        if (have < 16) {
+                            __syncwarp();
+                            for (int e = lane; e < (16 - have) * 16; e += 32)
+                                store16(block + ((e >> 3) & 1) * kSub + (uint32_t)(16 * slot + have + (e >> 4)) * 128 + (e & 7) * 16, 0, 0, 0, 0);
+                        }
+                        if (((b + 1 - it.b0) & 3) == 0) {
+                            window = places(b + 1, ids_next);
+                            ids_next = ids(b + 5);
+                        }
+                        if (b + 1 < b1) load(b + 1, kv);
                         fence_async_shared();
                         __syncwarp();
                     }
@@ -710,17 +711,15 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
         }
     };
 
-    // 384 threads x 168 registers at launch = 128 x (2 x 200 + 104); wide: 896 x 72 = 128 x (2 x 104 + 72 + 4 x 56), one tile: 768 x 80 =
+    // 384 threads x 168 registers at launch = 128 x (2 x 200 + 104); with fill warps 896 x 72 = 128 x (2 x 104 + 72 + 4 x 56), one tile: 768 x 80 =
     // 128 x (120 + 72 + 4 x 72)
-    if (kWide && warp >= kSoft + 4) {
+    if (kPaged && warp >= kSoft + 4) {
         if constexpr (kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         else asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-        if constexpr (kWide) fill(warp - kSoft - 4);
+        if constexpr (kPaged) if (fills) fill(warp - kSoft - 4);
     } else if (warp >= kSoft) {
-        if constexpr (kWide) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        if constexpr (kPaged) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         else asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
-        if constexpr (!kWide)
-            if (warp == kSoft + 3) fill(0);
         if (warp == kSoft + 2) {
             // ================================================= items
             Walker walk;
@@ -745,6 +744,7 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
             uint32_t g = 0, qc = 0;                // blocks, items so far
             const uint32_t qf = smem_u32(&sm.q_full);
             for (uint32_t n = 0; next_item(n, it); n++) {
+                if (kPaged && !fills && lane == 0) bar_arrive(smem_u32(&sm.item_empty[n & 1]), kFill);
                 if (qc > 0) ok = __all_sync(0xffffffffu, bar_wait(smem_u32(&sm.q_empty), (qc - 1) & 1, limit));
                 if (!ok) break;
                 const bool mine = elect_one();
@@ -769,6 +769,7 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
                         if (!mine) continue;
                         if (b < it.hist) { bar_arrive(full); continue; }
                         bar_expect(full, kTileBytes);
+                        if (kPaged && !fills) bar_arrive(full, kFill / 2);
                         for (int c = 0; c < 2; c++) tile_load3(dst + c * kSub, kv ? &map_v : &map_k, 64 * c, it.head, row, full);
                     }
                     if (!ok) break;
@@ -940,7 +941,7 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
             __syncwarp();
         }
     } else {
-        if constexpr (!kWide) asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
+        if constexpr (!kPaged) asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
         else if constexpr (kTiles == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
         else asm volatile("setmaxnreg.inc.sync.aligned.u32 120;");
         // ================================================= softmax: thread = row, or one of a row's copies with its share of the keys
@@ -1265,25 +1266,27 @@ prompt_join_kernel(PromptWorkspace ws, int grid, int rows_max, int n_kv, __nv_bf
     }
 }
 
-template <int kBits, int kTiles, int kCopies, bool kWide>
+template <int kBits, int kTiles, int kCopies, bool kPaged>
 pask_status_t launch(const PromptParams &p, const CUtensorMap &map_q, const CUtensorMap &map_k, const CUtensorMap &map_v, int dev, cudaStream_t stream) {
-    constexpr int kSmem = (int)sizeof(PromptSmem<kTiles, kCopies, kWide>);
+    constexpr int kSmem = (int)sizeof(PromptSmem<kTiles, kCopies, kPaged>);
     static_assert(kSmem <= 232448, "shared memory of a CTA");
     static bool granted[64] = {};                  // a property of (device, kernel)
     if (!granted[dev]) {
-        if (cudaFuncSetAttribute(prompt_kernel<kBits, kTiles, kCopies, kWide>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess) return PASK_ERR_CUDA;
+        if (cudaFuncSetAttribute(prompt_kernel<kBits, kTiles, kCopies, kPaged>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess) return PASK_ERR_CUDA;
         granted[dev] = true;
     }
-    return launch_pdl(prompt_kernel<kBits, kTiles, kCopies, kWide>, dim3(p.grid), dim3(PromptSmem<kTiles, kCopies, kWide>::kThreads), kSmem, stream, p, map_q, map_k, map_v) == cudaSuccess ? PASK_OK
-                                                                                                                                     : PASK_ERR_CUDA;
+    return launch_pdl(prompt_kernel<kBits, kTiles, kCopies, kPaged>, dim3(p.grid), dim3(PromptSmem<kTiles, kCopies, kPaged>::kThreads), kSmem, stream, p, map_q,
+                      map_k, map_v) == cudaSuccess
+               ? PASK_OK
+               : PASK_ERR_CUDA;
 }
 
-template <int kTiles, int kCopies, bool kWide>
+template <int kTiles, int kCopies>
 pask_status_t launch_bits(uint32_t bits, const PromptParams &p, const CUtensorMap &map_q, const CUtensorMap &map_k, const CUtensorMap &map_v, int dev,
                           cudaStream_t stream) {
-    return bits == 8 ? launch<8, kTiles, kCopies, kWide>(p, map_q, map_k, map_v, dev, stream)
-           : bits == 2 ? launch<2, kTiles, kCopies, kWide>(p, map_q, map_k, map_v, dev, stream)
-                       : launch<4, kTiles, kCopies, kWide>(p, map_q, map_k, map_v, dev, stream);
+    return bits == 8 ? launch<8, kTiles, kCopies, true>(p, map_q, map_k, map_v, dev, stream)
+           : bits == 2 ? launch<2, kTiles, kCopies, true>(p, map_q, map_k, map_v, dev, stream)
+                       : launch<4, kTiles, kCopies, true>(p, map_q, map_k, map_v, dev, stream);
 }
 
 // Tokens of an item: 64 (two tiles), or 32, 16, 8 (one tile, its rows once, twice, four times), by the mean of a sequence: the pages are read
@@ -1294,6 +1297,10 @@ int tokens_for(int n_seqs, int total_tokens) {
     const long long n = ((long long)total_tokens + n_seqs - 1) / n_seqs;
     return n <= 8 ? 8 : n <= 16 ? 16 : n <= 32 ? 32 : 64;
 }
+
+// Mean tokens of a sequence from which the variant without fill warps is launched beside the other.  Without history, the one with fill warps
+// alone and both: one prompt of 1024 tokens 36, 39 us; of 2048 79, 78; four of 1400 112, 112; of 2048 191, 187; of 4096 - 8192 1470, 1415.
+constexpr int kBothFrom = 2048;
 
 }  // namespace
 
@@ -1338,12 +1345,15 @@ pask_status_t launch_prompt(pask_cache *c, int layer, int n_seqs, int total_toke
     if (launch_pdl(prompt_plan_kernel, dim3(1), dim3((n_seqs + 31) / 32 * 32), 0, stream, d, layer, n_seqs, total_tokens, seq_ids, cu_tokens, p.ws, p.grid,
                    tokens, static_cast<uint4 *>(out), lse) != cudaSuccess)
         return PASK_ERR_CUDA;
-    // Two tiles: sixteen fill warps, and few registers a softmax thread; or, with no pages to expand, as many as a softmax thread can use, and
-    // one fill warp (which is right with a history too: a graph may be replayed behind one).  With, without: prompts of 8K without history 1495, 1423
-    // us; chunks of 512 behind 9K 733, 3894.
-    const auto fn = tokens == 64 ? (c->appended[layer] ? launch_bits<2, 1, true> : launch_bits<2, 1, false>)
-                    : tokens == 32 ? launch_bits<1, 1, true> : tokens == 16 ? launch_bits<1, 2, true> : launch_bits<1, 4, true>;
-    const pask_status_t ok = fn(d.low_bits, p, map_q, map_k, map_v, c->device, stream);
+    // Long sequences: with fill warps and without, and the one that the plan's finding is not for leaves at once (the host knows neither
+    // what the cache holds nor what it will hold when a graph is replayed).
+    const bool both = tokens == 64 && total_tokens / n_seqs >= kBothFrom;
+    p.only = both ? 0 : -1;
+    pask_status_t ok = both ? launch<4, 2, 1, false>(p, map_q, map_k, map_v, c->device, stream) : PASK_OK;
+    if (ok != PASK_OK) return ok;
+    p.only = both ? 1 : -1;
+    const auto fn = tokens == 64 ? launch_bits<2, 1> : tokens == 32 ? launch_bits<1, 1> : tokens == 16 ? launch_bits<1, 2> : launch_bits<1, 4>;
+    ok = fn(d.low_bits, p, map_q, map_k, map_v, c->device, stream);
     if (ok != PASK_OK) return ok;
     return launch_pdl(prompt_join_kernel, dim3(kJoinCtas * c->sm_count), dim3(kJoinThreads), 0, stream, p.ws, p.grid, tokens * kGqa, n_kv, p.out, lse) ==
                    cudaSuccess
