@@ -588,8 +588,8 @@ pask_status_t pask_rotary_table(const pask_rotary_desc_t *desc, uint64_t *table_
 /* pask_rotary -- rotates the first rot_dim dims of every head of up to PASK_ROTARY_MAX_TENSORS tensors [n_tokens][n_heads][head_dim]
  * (queries and keys, commonly) in one launch: pair (a, b) at the angle x = position * f_i becomes
  *   magnitude * (a cos x - b sin x, b cos x + a sin x).
- * The other dims are copied.  Angles are right for every 32-bit position, negative ones too; products are fp32 and each result is
- * rounded once.
+ * The other dims are copied.  Angles are right to 2^-27 of a turn for every 32-bit position, negative ones too; sines and products are
+ * fp32 and each result is rounded once.
  *   positions     dev int32 [n_tokens]
  *   table         dev uint64 [rot_dim / 2], 8-byte aligned
  *   interleaved   0: pair i is dims i and i + rot_dim / 2;  1: dims 2 i and 2 i + 1

@@ -2,8 +2,10 @@
 // x = position times frequency i (the transpose: -x).
 //
 // Angles.  A frequency is kept as the fraction of a turn that a position turns it by, in units of 2^-64, and its product with the
-// position is taken modulo 2^64: whole turns fall away by themselves, so that the angle of any 32-bit position is right to 2^-33
-// of a turn (a product in fp32 would be off by 0.03 rad at position 500 thousand).  Half turns go to sincospi in fp32.
+// position is taken modulo 2^64: whole turns fall away by themselves (a product in fp32 would be off by 0.03 rad at position 500
+// thousand).  For any 32-bit position the product is right to 2^-34 of a turn (the table's rounding, 2^-65, times 2^31); its upper 32 bits are
+// rounded by 2^-33; quarter turns are taken off in whole numbers; what is left, an eighth of a turn at most, goes to sincospi as an
+// fp32 number of half turns, off by another 2^-28 of a turn.
 //
 // Bound: memory, each value read and written once (rot dims of 128 and 40 heads: 20 KB a token).  A CTA works out the sines and
 // cosines of its tokens once, in shared memory, for all their heads; then a thread has V pairs of a head (two 16-byte loads and
@@ -72,10 +74,12 @@ rotary_kernel(const __grid_constant__ RotaryParams p) {
     for (int e = tid; e < n * pairs; e += kThreads) {
         const int t = e / pairs;
         const uint64_t turn = (uint64_t)(int64_t)p.positions[t0 + t] * p.table[e - t * pairs];
+        const uint32_t angle = (uint32_t)((turn + 0x80000000u) >> 32), quarters = (angle + 0x20000000u) >> 30;
         float s, c;
-        sincospif((float)(int32_t)(uint32_t)((turn + 0x80000000u) >> 32) * 0x1p-31f, &s, &c);
-        s_cos[e] = c * p.magnitude;
-        s_sin[e] = (p.transpose ? -s : s) * p.magnitude;
+        sincospif((float)(int32_t)(angle - (quarters << 30)) * 0x1p-31f, &s, &c);
+        const float cq = quarters & 1 ? -s : c, sq = quarters & 1 ? c : s;          // a quarter on: (c, s) to (-s, c); half a turn: both change sign
+        s_cos[e] = (quarters & 2 ? -cq : cq) * p.magnitude;
+        s_sin[e] = (((quarters & 2) != 0) != (p.transpose != 0) ? -sq : sq) * p.magnitude;
     }
     __syncthreads();
     // A row is a head of a token; a thread has unit u of the rows r, r + rows, ...: two pieces of V dims, one of either half of the rotated
