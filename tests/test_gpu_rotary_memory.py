@@ -34,6 +34,19 @@ def test_slices_between_one_another(P):
             check(y, x, p, freq)
 
 
+@pytest.mark.parametrize("n", [1, 2, 33])
+@pytest.mark.parametrize("heads_k", [1, 2, 8])
+def test_queries_and_keys_in_place_in_one_projection(P, n, heads_k):
+    """Two tensors of the same rows, each its own input, values behind them left alone."""
+    table, freq = P.pask_rotary_table(128), R.frequencies(128, 10000.0)
+    pos = torch.arange(n, dtype=torch.int32, device="cuda") * 301
+    rows = torch.randn(n, 8 + 2 * heads_k, 128, device="cuda").to(torch.bfloat16)
+    q, k, old = rows[:, :8], rows[:, 8:8 + heads_k], rows.clone()
+    P.pask_rotary(pos, table, [(q, q), (k, k)])
+    check(rows[:, :8 + heads_k], old[:, :8 + heads_k], pos, freq)
+    assert torch.equal(rows[:, 8 + heads_k:], old[:, 8 + heads_k:])
+
+
 @pytest.mark.parametrize("seed", range(8))
 def test_drawn_pieces_of_one_buffer(P, seed):
     r, table, freq = random.Random(seed), P.pask_rotary_table(16), R.frequencies(16, 10000.0)
