@@ -532,7 +532,8 @@ pask_status_t pask_prompt_attention_latent(int32_t n_seqs, int32_t total_q, int3
  *               GPU (two streams, two captured graphs replayed side by side) need one each.
  * out, lse and workspace share no memory with one another or with what is read (PASK_ERR_INVALID_ARG).
  * RETAIN-LOW values enter as bf16(code * scale), the operands of a bf16 product (pask_decode_attention computes with the unrounded
- * product); softmax weights are rounded to bf16, scores and sums are fp32, each output is rounded once.  Values must be finite, and
+ * product); softmax weights are rounded to bf16 (there they keep two bf16 parts), scores and sums are fp32, each output is rounded once: a
+ * token's result here and in a later decode step agree to the error of those roundings, not to the last bits.  Values must be finite, and
  * scores and sums within what fp32 holds; rows outside every sequence may hold anything and are left as they were.
  * A row belongs to one sequence: rows that two ranges share hold either's result, or pieces of both.
  * A sequence whose range is malformed is not written (sticky PASK_DEV_BAD_RAGGED); one whose id is out of range gets out = 0 and

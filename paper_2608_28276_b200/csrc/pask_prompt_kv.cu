@@ -27,13 +27,13 @@
 // each; one tile, two places of S, two of P, O.
 //
 // What bounds it, at 6539 GB/s and 1643 TFLOP/s (1394 sustained) measured:
-//   prompts without history (4 of 4096 - 8192, 32 heads) 1415 us, 942 at the sustained rate: some 3400 cycles for two tiles and 128 keys, of
-//       which the products need 2048 and the exponentials as many, beside them; the rest is waits between the two, at 1.34 GHz under the
-//       power limit
-//   chunks of 512 behind 9K rows in 8 bits 724 us (377): the same chain, 580 with no page read or expanded; expansion in its issue slots
-//   5 drafted tokens of 64 sequences of 2K - 8K 180 us (75: the pages once): 104 with no page read or expanded, 110 with expansion
+//   prompts without history (4 of 4096 - 8192, 32 heads) 1400 - 1435 us, 942 at the sustained rate: some 3500 cycles for two tiles and 128
+//       keys, of which the products need 2048 and the exponentials as many, beside them; the rest is waits between the two (a row's halves are
+//       loaded, waited for and worked on one after the other), at 1.34 GHz under the power limit
+//   chunks of 512 behind 9K rows in 8 bits 726 - 738 us (377): the same chain, 580 with no page read or expanded; expansion in its issue slots
+//   5 drafted tokens of 64 sequences of 2K - 8K 180 - 184 us (75: the pages once): 104 with no page read or expanded, 110 with expansion
 //       alone: a fill warp's chain for a page (its pieces from memory, expansion, the block's hand-over) does not overlap with itself
-//   one prompt of 131: 13 us replayed in a graph, 14 called; three launches in a row: plan 4, items 8, join 3
+//   one prompt of 131: 14.4 us; three launches in a row: plan 4, items 8, join 3
 //
 // Rounding: S, O and the sums are fp32; a weight is rounded to bf16 once, as an operand of a product with bf16 values; a low-precision
 // row enters as bf16(code * scale), rounded once from the exact product.
@@ -711,7 +711,7 @@ prompt_kernel(const __grid_constant__ PromptParams p, const __grid_constant__ CU
         }
     };
 
-    // 384 threads x 168 registers at launch = 128 x (2 x 200 + 104); with fill warps 896 x 72 = 128 x (2 x 104 + 72 + 4 x 56), one tile: 768 x 80 =
+    // 384 threads x 168 registers at launch = 128 x (2 x 200 + 104) (more than a softmax thread needs, since rows go in halves); with fill warps 896 x 72 = 128 x (2 x 104 + 72 + 4 x 56), one tile: 768 x 80 =
     // 128 x (120 + 72 + 4 x 72)
     if (kPaged && warp >= kSoft + 4) {
         if constexpr (kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
@@ -1299,7 +1299,8 @@ int tokens_for(int n_seqs, int total_tokens) {
 }
 
 // Mean tokens of a sequence from which the variant without fill warps is launched beside the other.  Without history, the one with fill warps
-// alone and both: one prompt of 1024 tokens 36, 39 us; of 2048 79, 78; four of 1400 112, 112; of 2048 191, 187; of 4096 - 8192 1470, 1415.
+// alone and both: one prompt of 1024 tokens 36, 39 us; of 2048 79, 78; four of 1400 112, 112; of 2048 191, 187; of 4096 - 8192 1470, 1415.  With a
+// history, with fill warps and with one of the control warps in their place: chunks of 512 behind 9K 733, 3894.
 constexpr int kBothFrom = 2048;
 
 }  // namespace

@@ -10,8 +10,8 @@
 // Bound: memory, each value read and written once (rot dims of 128 and 40 heads: 20 KB a token).  A CTA works out the sines and
 // cosines of its tokens once, in shared memory, for all their heads; then a thread has V pairs of a head (two 16-byte loads and
 // stores), the heads of all tensors of the call one behind the other.  16-byte accesses need everything aligned to them; otherwise
-// a thread has one pair.  17 thousand tokens x 40 heads of 128 in bf16: 57 us, 6.1 TB/s (93 % of a copy's); 16 thousand x 33 heads of 64
-// cut out of wider rows 29.5 us, 4.6 TB/s.  Two rows of a thread at a time took 66 and 33 us (more registers, fewer CTAs an SM).
+// a thread has one pair.  17 thousand tokens x 40 heads of 128 in bf16: 58 us, 6.0 TB/s (92 % of a copy's); 16 thousand x 33 heads of 64
+// cut out of wider rows 28 us, 4.8 TB/s.  Two rows of a thread at a time took 66 and 33 us (more registers, fewer CTAs an SM).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
