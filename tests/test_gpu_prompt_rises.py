@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import prompt_ref as R
-from test_gpu_prompt import Case, cu_of
+from test_gpu_prompt import Case
 
 pytestmark = pytest.mark.gpu
 
